@@ -351,6 +351,89 @@ int sgd_update_multi(void *const *w, const void *const *dw, void *const *vel, co
                      int ntensors, float lr, float momentum, float weight_decay, float grad_scale,
                      void *stream);
 
+/*
+ * Group normalisation with an activation, for use between a convolution and what
+ * follows it.  A sample's C channels fall into `groups` groups of C / groups
+ * neighbouring channels; with M = (C / groups) * S values x in a sample's group:
+ *   mean = sum x / M,   var = sum (x - mean)^2 / M,   rstd = 1 / sqrt(var + eps)
+ *   xh = (x - mean) * rstd,   z = gamma[c] * xh + beta[c],   y = act(z)
+ * The statistics are a sample's own: a data-parallel shard needs no exchange for
+ * them, whatever its size.  S is the number of positions (H*W).
+ *   layout: CONV_LAYOUT_PLANES = [N][C][S] (NCHW, as the convolutions have it),
+ *           CONV_LAYOUT_CHANNELS_LAST = [N][S][C]; dense.
+ *   act:    CONV_ACT_NONE, CONV_ACT_RELU (slope 0 at 0), CONV_ACT_SILU (z / (1 + exp(-z)))
+ *   gamma, beta: fp32 [C] on the device, or NULL for ones / zeros
+ *   mean, rstd:  fp32 [N][groups]; group_norm_act_fwd writes them where they are
+ *           not NULL, group_norm_act_bwd reads them
+ * group_norm_act_bwd, with dz = dy * act'(z) (z computed again from x):
+ *   dbeta[c] = sum_{n,s} dz,   dgamma[c] = sum_{n,s} dz * xh   (fp32; each may be NULL)
+ *   dx = rstd * (gamma[c] * dz - m1 - xh * m2), m1 and m2 the group's means of
+ *        gamma[c] * dz and gamma[c] * dz * xh
+ * `dtype` names the element type of x, y, dy and dx as for the glue layers (fp32
+ * 4-byte aligned, bfloat16 2-byte aligned): values are read exactly, all
+ * arithmetic is fp32, the squares are taken of distances from a mean, and a bfloat16 result is
+ * rounded once.  eps > 0.  N = 0 is allowed (tensors over it may be NULL; dgamma and
+ * dbeta become 0); C * S and N * C must stay below 2^31.  Outputs must not overlap
+ * inputs.  Scratch:
+ * group_norm_act_workspace_bytes(op, ...) bytes, 256-byte aligned (op = CONV_OP_FWD or
+ * CONV_OP_BWD_DATA; 0 bytes for invalid arguments and where none is needed).
+ */
+enum { CONV_ACT_NONE = 0, CONV_ACT_RELU = 1, CONV_ACT_SILU = 2 };
+enum { CONV_LAYOUT_PLANES = 0, CONV_LAYOUT_CHANNELS_LAST = 1 };
+int group_norm_act_fwd(const void *x, const void *gamma, const void *beta, void *y, void *mean, void *rstd,
+                       int N, int C, int S, int groups, float eps, int act, int layout, int dtype,
+                       void *ws, size_t ws_bytes, void *stream);
+int group_norm_act_bwd(const void *x, const void *dy, const void *gamma, const void *beta, const void *mean,
+                       const void *rstd, void *dx, void *dgamma, void *dbeta, int N, int C, int S, int groups,
+                       int act, int layout, int dtype, void *ws, size_t ws_bytes, void *stream);
+size_t group_norm_act_workspace_bytes(int op, int N, int C, int S, int groups, int layout, int dtype);
+
+/*
+ * The loss of a network that learns from labels, from a teacher's top logits, or
+ * from both.  z: logits [N][V], rows z_stride elements apart (>= V).  Row n has
+ *   - a label, labels[n] (labels may be NULL), and
+ *   - up to K entries of a teacher: class top_idx[n][k], the teacher's logit
+ *     top_val[n][k] (dense [N][K]; K = 0: no teacher).  Their softmax over the row's
+ *     entries is the target, p = softmax(top_val / temperature).
+ * An index outside 0 .. V-1 (-1, say) means none: no label, an unused entry (its
+ * top_val is not used).  Classes named twice count twice.  With
+ * q_T = softmax(z / temperature) and q_1 = softmax(z) over all V classes:
+ *   loss[n]  = kd_weight * temperature^2 * sum_k p_k * (log p_k - log q_T[i_k])
+ *            + label_weight * (-log q_1[label])                                      fp32
+ *   dz[n][v] = g_n * (kd_weight * temperature * (q_T[v] - sum_{k: i_k = v} p_k)
+ *            + label_weight * (q_1[v] - [v = label])),    g_n = grad_scale * grad[n]
+ * where a term without target is absent, and so is one of weight 0; a row without any target has loss 0
+ * and dz 0 whatever its logits are.  Entries with p_k = 0 add nothing.  A logit of
+ * -infinity is a class left out (q = 0); a row with targets and no other logits is NaN.
+ * grad (fp32 [N]) may be NULL for ones: a mean over the rows has grad_scale = 1/N.
+ *   distill_loss_fwd:     loss, and the row's statistics for a later distill_loss_bwd:
+ *                         stats[n] = {m = max z, sum exp((z - m) / temperature), sum exp(z - m)},
+ *                         fp32 [N][3] or NULL; without a teacher the second is the third; a row without target: 0
+ *   distill_loss_bwd:     dz from the same arguments and stats
+ *   distill_loss_fwd_bwd: loss and dz in one call, for a step that knows g beforehand
+ * dtype: element type of z and dz (CONV_DTYPE_F32, or bfloat16 for the other two: dz rounded
+ * once); top_dtype: the same of top_val; index_bytes: 4 or 8, size of the signed integers in
+ * labels and top_idx.  All arithmetic is fp32; results do not depend on the order of work.
+ * Pointers aligned to their elements; rows may start anywhere.  dz [N][V], rows dz_stride apart,
+ * may be z itself (same stride), and may not overlap it otherwise.  K <= CONV_DISTILL_MAX_TOP.
+ * N = 0 is a no-op (pointers may be NULL).  Scratch: distill_loss_workspace_bytes bytes (fwd and fwd_bwd), 256-byte aligned.
+ */
+#define CONV_DISTILL_MAX_TOP 1024
+int distill_loss_fwd(const void *z, int64_t z_stride, const void *labels, const void *top_idx, const void *top_val,
+                     void *loss, void *stats, int N, int V, int K, float temperature, float kd_weight,
+                     float label_weight, int index_bytes, int top_dtype, int dtype,
+                     void *ws, size_t ws_bytes, void *stream);
+int distill_loss_bwd(const void *z, int64_t z_stride, const void *labels, const void *top_idx, const void *top_val,
+                     const void *stats, const void *grad, float grad_scale, void *dz, int64_t dz_stride,
+                     int N, int V, int K, float temperature, float kd_weight, float label_weight,
+                     int index_bytes, int top_dtype, int dtype, void *stream);
+int distill_loss_fwd_bwd(const void *z, int64_t z_stride, const void *labels, const void *top_idx,
+                         const void *top_val, const void *grad, float grad_scale, void *loss, void *dz,
+                         int64_t dz_stride, int N, int V, int K, float temperature, float kd_weight,
+                         float label_weight, int index_bytes, int top_dtype, int dtype,
+                         void *ws, size_t ws_bytes, void *stream);
+size_t distill_loss_workspace_bytes(int N, int V, int K, int dtype);
+
 #ifdef __cplusplus
 }
 #endif

@@ -34,6 +34,10 @@ from .oracle import (  # noqa: F401
     fc_bwd_data,
     fc_bwd_filter,
     sgd_update,
+    group_norm_stats,
+    group_norm_act_fwd,
+    group_norm_act_bwd,
+    distill_loss,
     bf16_bits,
     bf16_round,
     num_threads,

@@ -319,3 +319,87 @@ def bf16_round(a):
     """The float32 array rounded onto the bfloat16 grid, returned as float32 (exactly representable)."""
     b = bf16_bits(a)
     return (b.astype(np.uint32) << 16).view(np.float32).reshape(b.shape)
+
+
+# ---------------------------------------------------------------------------
+# Group normalisation with an activation, x as [N, C, S].
+# ---------------------------------------------------------------------------
+def _sigmoid(z):
+    e = np.exp(-np.abs(z))
+    return np.where(z >= 0, 1.0, e) / (1.0 + e)
+
+
+def group_norm_stats(x, groups, eps):
+    """mean and 1 / sqrt(var + eps) of every sample's groups, each [N, groups]."""
+    x = _f64(x)
+    v = x.reshape(x.shape[0], groups, -1)
+    mean = v.mean(axis=2)
+    var = ((v - mean[:, :, None]) ** 2).mean(axis=2)
+    return mean, 1.0 / np.sqrt(var + eps)
+
+
+def _per_channel(v, C):
+    return np.repeat(v, C // v.shape[1], axis=1)[:, :, None]
+
+
+def group_norm_act_fwd(x, groups, gamma, beta, eps, act):
+    """(y, mean, rstd)"""
+    x = _f64(x)
+    C = x.shape[1]
+    mean, rstd = group_norm_stats(x, groups, eps)
+    z = (x - _per_channel(mean, C)) * _per_channel(rstd, C) * _f64(gamma)[None, :, None] + _f64(beta)[None, :, None]
+    y = {"none": lambda: z, "relu": lambda: np.where(z > 0, z, 0.0), "silu": lambda: z * _sigmoid(z)}[act]()
+    return y, mean, rstd
+
+
+def group_norm_act_bwd(x, dy, mean, rstd, gamma, beta, act):
+    """(dx, dgamma, dbeta) for the statistics given."""
+    x, dy, mean, rstd, gamma = _f64(x), _f64(dy), _f64(mean), _f64(rstd), _f64(gamma)
+    N, C, S = x.shape
+    G = mean.shape[1]
+    xh = (x - _per_channel(mean, C)) * _per_channel(rstd, C)
+    z = gamma[None, :, None] * xh + _f64(beta)[None, :, None]
+    sig = _sigmoid(z)
+    slope = {"none": lambda: 1.0, "relu": lambda: (z > 0) * 1.0, "silu": lambda: sig + z * sig * (1.0 - sig)}[act]()
+    dz = dy * slope
+    g = gamma[None, :, None] * dz
+    m1 = g.reshape(N, G, -1).mean(axis=2)
+    m2 = (g * xh).reshape(N, G, -1).mean(axis=2)
+    dx = _per_channel(rstd, C) * (g - _per_channel(m1, C) - xh * _per_channel(m2, C))
+    return dx, (dz * xh).sum(axis=(0, 2)), dz.sum(axis=(0, 2))
+
+
+# ---------------------------------------------------------------------------
+# Loss of logits z [N, V] against labels and a teacher's top logits, row by row
+# (an index outside 0 .. V-1 names no class).
+# ---------------------------------------------------------------------------
+def distill_loss(z, labels=None, top_idx=None, top_val=None, temperature=1.0, kd_weight=1.0, label_weight=1.0, grad=None):
+    """(loss [N], dz [N, V]); dz is the gradient of sum_n grad[n] * loss[n]."""
+    z = _f64(z)
+    N, V = z.shape
+    loss, dz = np.zeros(N), np.zeros((N, V))
+    grad = np.ones(N) if grad is None else _f64(grad)
+    T = float(temperature)
+
+    def log_softmax(v):
+        with np.errstate(invalid="ignore", over="ignore", under="ignore"):
+            d = v - v.max()
+            return d - np.log(np.exp(d).sum())
+
+    for n in range(N):
+        if top_idx is not None and kd_weight != 0:
+            held = (top_idx[n] >= 0) & (top_idx[n] < V)
+            if held.any():
+                i = top_idx[n][held]
+                with np.errstate(over="ignore"):
+                    p = np.exp(log_softmax(_f64(top_val[n][held]) / T))
+                lq = log_softmax(z[n] / T)
+                loss[n] += kd_weight * T * T * sum(a * (np.log(a) - lq[j]) for a, j in zip(p, i) if not a <= 0)
+                dz[n] += grad[n] * kd_weight * T * np.exp(lq)
+                np.subtract.at(dz[n], i, grad[n] * kd_weight * T * p)
+        if labels is not None and label_weight != 0 and 0 <= labels[n] < V:
+            lq = log_softmax(z[n])
+            loss[n] -= label_weight * lq[labels[n]]
+            dz[n] += grad[n] * label_weight * np.exp(lq)
+            dz[n, labels[n]] -= grad[n] * label_weight
+    return loss, dz

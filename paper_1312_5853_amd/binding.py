@@ -21,6 +21,9 @@ ERR_INVALID_ARG, ERR_TOO_LARGE, ERR_BAD_DTYPE, ERR_WORKSPACE, ERR_MISALIGNED, ER
 ERR_SCRATCH_LIMIT = -7
 NOALLOC_SCRATCH_BYTES = 48 << 20
 DTYPE_F32, DTYPE_BF16, DTYPE_BF16_OUT_BF16 = 0, 1, 2
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2}
+LAYOUT_PLANES, LAYOUT_CHANNELS_LAST = 0, 1
+DISTILL_MAX_TOP = 1024
 OP_FWD, OP_BWD_DATA, OP_BWD_FILTER = 0, 1, 2
 
 EXPORTS = (
@@ -32,6 +35,8 @@ EXPORTS = (
     "relu_maxpool3x3s2_fwd", "relu_maxpool3x3s2_bwd", "convert_f32_to_bf16",
     "bias_fwd", "bias_bwd", "bias_bwd_workspace_bytes",
     "fc_fwd", "fc_bwd_data", "fc_bwd_filter", "fc_workspace_bytes", "sgd_update", "sgd_update_multi",
+    "group_norm_act_fwd", "group_norm_act_bwd", "group_norm_act_workspace_bytes",
+    "distill_loss_fwd", "distill_loss_bwd", "distill_loss_fwd_bwd", "distill_loss_workspace_bytes",
 )
 
 _lib = None
@@ -111,6 +116,19 @@ def lib():
     for name in ("relu_fwd", "relu_bwd", "maxpool3x3s2_fwd", "maxpool3x3s2_bwd", "relu_maxpool3x3s2_fwd",
                  "relu_maxpool3x3s2_bwd"):
         getattr(L, name).restype = i
+    L.group_norm_act_fwd.argtypes = [vp] * 6 + [i, i, i, i, f32, i, i, i, vp, sz, vp]
+    L.group_norm_act_bwd.argtypes = [vp] * 9 + [i, i, i, i, i, i, i, vp, sz, vp]
+    L.group_norm_act_workspace_bytes.argtypes = [i] * 7
+    terms = [i, i, i, f32, f32, f32, i, i, i]
+    L.distill_loss_fwd.argtypes = [vp, i64, vp, vp, vp, vp, vp] + terms + [vp, sz, vp]
+    L.distill_loss_bwd.argtypes = [vp, i64, vp, vp, vp, vp, vp, f32, vp, i64] + terms + [vp]
+    L.distill_loss_fwd_bwd.argtypes = [vp, i64, vp, vp, vp, vp, f32, vp, vp, i64] + terms + [vp, sz, vp]
+    L.distill_loss_workspace_bytes.argtypes = [i] * 4
+    for name in ("group_norm_act_fwd", "group_norm_act_bwd", "distill_loss_fwd", "distill_loss_bwd",
+                 "distill_loss_fwd_bwd"):
+        getattr(L, name).restype = i
+    for name in ("group_norm_act_workspace_bytes", "distill_loss_workspace_bytes"):
+        getattr(L, name).restype = sz
     _lib = L
     return L
 
@@ -567,3 +585,197 @@ def sgd_update_multi(ws, dws, vels, lr, momentum=0.0, weight_decay=0.0, grad_sca
     _check(lib().sgd_update_multi(ptrs(ws), ptrs(dws), ptrs(vels), counts, n, lr, momentum, weight_decay, grad_scale,
                                   _stream_handle(stream)), "sgd_update_multi")
     return ws
+
+
+# Workspace sizes of the calls below: kept for the same reason as those of the convolutions.
+@functools.lru_cache(maxsize=1024, typed=True)
+def _norm_workspace_bytes(op, N, C, S, groups, layout, dtype):
+    return int(lib().group_norm_act_workspace_bytes(op, N, C, S, groups, layout, dtype))
+
+
+@functools.lru_cache(maxsize=1024, typed=True)
+def _loss_workspace_bytes(N, V, K, dtype):
+    return int(lib().distill_loss_workspace_bytes(N, V, K, dtype))
+
+
+def _norm_layout(x, *others):
+    """The memory order that all of a call's [N,C,H,W] tensors have: NCHW, or channels last."""
+    for layout, order in ((LAYOUT_PLANES, torch.contiguous_format), (LAYOUT_CHANNELS_LAST, torch.channels_last)):
+        if all(t.is_contiguous(memory_format=order) for t in (x,) + others):
+            return layout
+    raise ValueError("the tensors of a normalisation must be dense, all NCHW or all channels last")
+
+
+def _per_channel(C, **vectors):
+    for name, v in vectors.items():
+        if v is not None and (v.dtype != torch.float32 or v.numel() != C or not v.is_contiguous()):
+            raise ValueError("%s must hold one fp32 value per channel" % name)
+
+
+def _row_stats_of(N, groups, **tensors):
+    for name, v in tensors.items():
+        if v.dtype != torch.float32 or tuple(v.shape) != (N, groups) or not v.is_contiguous():
+            raise ValueError("%s must be a dense fp32 tensor [N, groups]" % name)
+
+
+def _opt(t):
+    return 0 if t is None else t.data_ptr()
+
+
+def _on_device(first, *others):
+    for t in (first,) + others:
+        if t is not None and (not t.is_cuda or t.device != first.device):
+            raise ValueError("the tensors of a call must be on one GPU")
+
+
+def group_norm_act_fwd(x, groups, gamma=None, beta=None, eps=1e-5, act="relu", y=None, mean=None, rstd=None, ws=None,
+                       stream=None):
+    """y = act(group norm of x) for x [N,C,H,W], NCHW or channels last in memory (y has x's order and element type), and
+    the statistics that the backward pass needs: (y, mean [N,groups], rstd [N,groups]).  act: "none", "relu" or "silu";
+    gamma and beta: fp32 [C], or None."""
+    if type(groups) is not int:
+        groups, = _whole(groups)
+    N, C, H, W = x.shape
+    if act not in ACTIVATIONS:
+        raise ValueError("unknown activation %r" % (act,))
+    _per_channel(C, gamma=gamma, beta=beta)
+    if y is None:
+        y = torch.empty_like(x)
+    if y.shape != x.shape:
+        raise ValueError("y must have the shape of x")
+    if groups > 0:
+        f = dict(dtype=torch.float32, device=x.device)
+        mean = torch.empty((N, groups), **f) if mean is None else mean
+        rstd = torch.empty((N, groups), **f) if rstd is None else rstd
+        _row_stats_of(N, groups, mean=mean, rstd=rstd)
+    dtype, layout = _glue_dtype(x, y), _norm_layout(x, y)
+    _on_device(x, y, gamma, beta, mean, rstd)
+    buf, nbytes = _ws(ws).get(_norm_workspace_bytes(OP_FWD, N, C, H * W, groups, layout, dtype))
+    rc = lib().group_norm_act_fwd(_ptr(x), _opt(gamma), _opt(beta), _ptr(y), _opt(mean), _opt(rstd), N, C, H * W, groups,
+                                  eps, ACTIVATIONS[act], layout, dtype, _opt(buf), nbytes, _stream_handle(stream))
+    if rc != OK:
+        raise ConvError(rc, "group_norm_act_fwd")
+    return y, mean, rstd
+
+
+def group_norm_act_bwd(x, dy, mean, rstd, gamma=None, beta=None, act="relu", dx=None, dgamma=None, dbeta=None, ws=None,
+                       stream=None):
+    """(dx, dgamma [C], dbeta [C]) from the forward call's x, mean and rstd and the gradient dy of its y."""
+    N, C, H, W = x.shape
+    if act not in ACTIVATIONS:
+        raise ValueError("unknown activation %r" % (act,))
+    groups = mean.shape[1]
+    _row_stats_of(N, groups, mean=mean, rstd=rstd)
+    if dx is None:
+        dx = torch.empty_like(x)
+    if dy.shape != x.shape or dx.shape != x.shape:
+        raise ValueError("dy and dx must have the shape of x")
+    f = dict(dtype=torch.float32, device=x.device)
+    dgamma = torch.empty((C,), **f) if dgamma is None else dgamma
+    dbeta = torch.empty((C,), **f) if dbeta is None else dbeta
+    _per_channel(C, gamma=gamma, beta=beta, dgamma=dgamma, dbeta=dbeta)
+    dtype, layout = _glue_dtype(x, dy, dx), _norm_layout(x, dy, dx)
+    _on_device(x, dy, dx, mean, rstd, gamma, beta, dgamma, dbeta)
+    buf, nbytes = _ws(ws).get(_norm_workspace_bytes(OP_BWD_DATA, N, C, H * W, groups, layout, dtype))
+    rc = lib().group_norm_act_bwd(_ptr(x), _ptr(dy), _opt(gamma), _opt(beta), _ptr(mean), _ptr(rstd), _ptr(dx),
+                                  _ptr(dgamma), _ptr(dbeta), N, C, H * W, groups, ACTIVATIONS[act], layout, dtype,
+                                  _opt(buf), nbytes, _stream_handle(stream))
+    if rc != OK:
+        raise ConvError(rc, "group_norm_act_bwd")
+    return dx, dgamma, dbeta
+
+
+def _rows_of(t, what):
+    """Row stride of a [N,V] tensor whose rows are dense."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError("%s must be [N, V] with dense rows" % what)
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _fp32_rows(N, width, **tensors):
+    for name, v in tensors.items():
+        if v is not None and (v.dtype != torch.float32 or v.numel() != N * width or v.shape[0] != N
+                              or not v.is_contiguous()):
+            raise ValueError("%s must be a dense fp32 tensor with %d value(s) per row" % (name, width))
+
+
+def _targets(z, labels, top_idx, top_val):
+    """(K, bytes of an index, dtype code of the teacher's logits) of a loss call, its target tensors checked."""
+    N = z.shape[0]
+    if (top_idx is None) != (top_val is None):
+        raise ValueError("top_idx and top_val come together")
+    index = {t.dtype for t in (labels, top_idx) if t is not None}
+    if len(index) > 1 or not index <= {torch.int32, torch.int64}:
+        raise TypeError("labels and top_idx must have one type, int32 or int64")
+    if labels is not None and (tuple(labels.shape) != (N,) or not labels.is_contiguous()):
+        raise ValueError("labels must be a dense tensor with one class per row")
+    K = 0
+    if top_idx is not None:
+        K = top_idx.shape[-1]
+        if tuple(top_idx.shape) != (N, K) or top_val.shape != top_idx.shape:
+            raise ValueError("top_idx and top_val must be [N, K]")
+        _dense(top_idx, top_val)
+    return K, 8 if torch.int64 in index else 4, DTYPE_F32 if K == 0 else _dtype_of(top_val)
+
+
+def distill_loss_fwd(z, labels=None, top_idx=None, top_val=None, temperature=1.0, kd_weight=1.0, label_weight=1.0,
+                     loss=None, stats=None, ws=None, stream=None):
+    """Losses of the logits z [N,V] (fp32 or bfloat16, rows may be apart) against labels [N] and / or a teacher's top
+    logits (classes top_idx [N,K], logits top_val [N,K]); indexes int32 or int64, one outside 0..V-1 for none.  Returns
+    (loss [N], stats [N,3]); stats is what distill_loss_bwd takes."""
+    zs = _rows_of(z, "z")
+    N, V = z.shape
+    K, ib, td = _targets(z, labels, top_idx, top_val)
+    f = dict(dtype=torch.float32, device=z.device)
+    loss = torch.empty((N,), **f) if loss is None else loss
+    stats = torch.empty((N, 3), **f) if stats is None else stats
+    _fp32_rows(N, 1, loss=loss)
+    _fp32_rows(N, 3, stats=stats)
+    dtype = _dtype_of(z)
+    _on_device(z, labels, top_idx, top_val, loss, stats)
+    buf, nbytes = _ws(ws).get(_loss_workspace_bytes(N, V, K, dtype))
+    _check(lib().distill_loss_fwd(_ptr(z), zs, _opt(labels), _opt(top_idx), _opt(top_val), _ptr(loss), _ptr(stats), N, V,
+                                  K, temperature, kd_weight, label_weight, ib, td, dtype, _opt(buf), nbytes,
+                                  _stream_handle(stream)), "distill_loss_fwd")
+    return loss, stats
+
+
+def distill_loss_bwd(z, stats, labels=None, top_idx=None, top_val=None, temperature=1.0, kd_weight=1.0, label_weight=1.0,
+                     grad=None, grad_scale=1.0, dz=None, stream=None):
+    """dz = grad_scale * grad[n] * d loss[n] / d z (grad [N] fp32, or None for ones) from the forward call's arguments and
+    statistics.  dz has z's element type and may be z itself."""
+    zs = _rows_of(z, "z")
+    N, V = z.shape
+    K, ib, td = _targets(z, labels, top_idx, top_val)
+    _fp32_rows(N, 1, grad=grad)
+    _fp32_rows(N, 3, stats=stats)
+    dz = torch.empty((N, V), dtype=z.dtype, device=z.device) if dz is None else dz
+    if dz.shape != z.shape:
+        raise ValueError("dz must have the shape of z")
+    dtype = _glue_dtype(z, dz)
+    _on_device(z, labels, top_idx, top_val, stats, grad, dz)
+    _check(lib().distill_loss_bwd(_ptr(z), zs, _opt(labels), _opt(top_idx), _opt(top_val), _ptr(stats), _opt(grad),
+                                  grad_scale, _ptr(dz), _rows_of(dz, "dz"), N, V, K, temperature, kd_weight,
+                                  label_weight, ib, td, dtype, _stream_handle(stream)), "distill_loss_bwd")
+    return dz
+
+
+def distill_loss_fwd_bwd(z, labels=None, top_idx=None, top_val=None, temperature=1.0, kd_weight=1.0, label_weight=1.0,
+                         grad=None, grad_scale=1.0, loss=None, dz=None, ws=None, stream=None):
+    """(loss [N], dz [N,V]) of distill_loss_fwd and distill_loss_bwd in one call."""
+    zs = _rows_of(z, "z")
+    N, V = z.shape
+    K, ib, td = _targets(z, labels, top_idx, top_val)
+    loss = torch.empty((N,), dtype=torch.float32, device=z.device) if loss is None else loss
+    _fp32_rows(N, 1, grad=grad, loss=loss)
+    dz = torch.empty((N, V), dtype=z.dtype, device=z.device) if dz is None else dz
+    if dz.shape != z.shape:
+        raise ValueError("dz must have the shape of z")
+    dtype = _glue_dtype(z, dz)
+    _on_device(z, labels, top_idx, top_val, grad, loss, dz)
+    buf, nbytes = _ws(ws).get(_loss_workspace_bytes(N, V, K, dtype))
+    _check(lib().distill_loss_fwd_bwd(_ptr(z), zs, _opt(labels), _opt(top_idx), _opt(top_val), _opt(grad), grad_scale,
+                                      _ptr(loss), _ptr(dz), _rows_of(dz, "dz"), N, V, K, temperature, kd_weight,
+                                      label_weight, ib, td, dtype, _opt(buf), nbytes, _stream_handle(stream)),
+           "distill_loss_fwd_bwd")
+    return loss, dz

@@ -6,20 +6,24 @@ file as ``libconvnet_hotpath.so`` (kept out of version control).
 import os
 import subprocess
 import sys
+import tempfile
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(_HERE, "csrc", "convnet_hotpath.hip")
+TRAIN_SRC = os.path.join(_HERE, "csrc", "train_ops.hip")
+SOURCES = (SRC, TRAIN_SRC)
 LIB = os.path.join(_HERE, "libconvnet_hotpath.so")
 CEILING_SRC = os.path.join(_HERE, "csrc", "mfma_ceiling.hip")
 CEILING_EXE = os.path.join(_HERE, "mfma_ceiling")
-DEPS = [SRC] + [os.path.join(_HERE, "csrc", h) for h in (
+DEPS = [SRC, TRAIN_SRC] + [os.path.join(_HERE, "csrc", h) for h in (
     "plan.h", "fastdiv.h", "device_common.h", "conv_colgemm_kernels.h", "conv_bf16_dma_kernels.h",
     "conv_bf16_window_kernels.h", "conv_split_kernels.h", "conv_wgrad_split_kernels.h", "conv_direct_kernels.h",
-    "conv_wgrad_rows_kernels.h", "conv_wgrad_kernels.h", "fc_kernels.h", "glue_kernels.h")] + [os.path.join(os.path.dirname(_HERE), "include", "convnet_hotpath.h")]
+    "conv_wgrad_rows_kernels.h", "conv_wgrad_kernels.h", "fc_kernels.h", "glue_kernels.h",
+    "host_status.h", "elements.h", "norm_kernels.h", "loss_kernels.h")] + [os.path.join(os.path.dirname(_HERE), "include", "convnet_hotpath.h")]
 
 # no packed-fp32 instruction selection
 DEVICE_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
-HIPCC_FLAGS = DEVICE_FLAGS + ["-shared", "-fPIC", "-Wall"]
+HIPCC_FLAGS = DEVICE_FLAGS + ["-fPIC", "-Wall"]
 
 
 def is_stale():
@@ -32,12 +36,21 @@ def is_stale():
 def build(verbose=False):
     """Compile unconditionally."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc] + HIPCC_FLAGS + ["-o", LIB, SRC]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    err = "\n".join(l for l in res.stderr.splitlines() if "packed-fp32-ops" not in l)
-    if verbose or res.returncode != 0:
+    with tempfile.TemporaryDirectory() as tmp:
+        # one translation unit per process, then the link
+        objs = [os.path.join(tmp, os.path.basename(src) + ".o") for src in SOURCES]
+        runs = [subprocess.Popen([hipcc] + HIPCC_FLAGS + ["-c", "-o", obj, src], stdout=subprocess.DEVNULL,
+                                 stderr=subprocess.PIPE, text=True) for src, obj in zip(SOURCES, objs)]
+        results = [(r.communicate()[1], r.returncode) for r in runs]
+        if all(rc == 0 for _, rc in results):
+            res = subprocess.run([hipcc, "--offload-arch=gfx950", "-shared", "-o", LIB] + objs, capture_output=True,
+                                 text=True)
+            results.append((res.stderr, res.returncode))
+    err = "\n".join(l for text, _ in results for l in text.splitlines() if "packed-fp32-ops" not in l)
+    failed = any(rc != 0 for _, rc in results)
+    if verbose or failed:
         sys.stderr.write(err + "\n")
-    if res.returncode != 0:
+    if failed:
         raise RuntimeError("hipcc failed:\n" + err)
     # the stand-alone MFMA ceiling probe (no inputs, prints TFLOP/s)
     res = subprocess.run([hipcc] + DEVICE_FLAGS + ["-o", CEILING_EXE, CEILING_SRC], capture_output=True, text=True)

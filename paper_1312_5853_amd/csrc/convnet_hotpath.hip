@@ -12,7 +12,6 @@
 // the 16-deep slice it needs straight from the NCHW tensor into LDS.
 #include <hip/hip_runtime.h>
 
-#include <stdio.h>
 #include <algorithm>
 #include <mutex>
 #include <type_traits>
@@ -20,6 +19,7 @@
 #include <string.h>
 
 #include "../../include/convnet_hotpath.h"
+#include "host_status.h"
 #include "plan.h"
 
 using namespace convnet;
@@ -54,23 +54,6 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-thread_local char g_hip_error[256] = "";
-
-int hip_fail(hipError_t e)
-{
-    snprintf(g_hip_error, sizeof(g_hip_error), "%s", hipGetErrorString(e));
-    return kErrHip;
-}
-
-int check_launch()
-{
-    hipError_t e = hipGetLastError();
-    return e == hipSuccess ? kStatusOk : hip_fail(e);
-}
-
-bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
-
-
 // Tiles are spread evenly over the 8 XCDs (32 CUs each).  When that gives at
 // most `cap` <= 3 work-groups per CU, extra dynamic LDS is requested so that no
 // CU can hold more than `cap`: the dispatcher is then forced to balance, and
@@ -1177,14 +1160,6 @@ int pool_checks(int64_t planes, int H, int W, int &PH, int &PW)
     PW = (W - 3) / 2 + 1;
     if ((double)planes * H * W * 4.0 >= (double)((int64_t)1 << 40) || (int64_t)H * W >= (1 << 30)) return kErrTooLarge;
     return kStatusOk;
-}
-
-// element type of the glue tensors: fp32 for kDtypeF32, bfloat16 for the two bf16 codes
-int glue_elem_bytes(int dtype)
-{
-    if (dtype == kDtypeF32) return 4;
-    if (dtype == kDtypeBf16 || dtype == kDtypeBf16OutBf16) return 2;
-    return 0;
 }
 
 // window rows of loads a lane of the walking pooling kernels keeps in flight (4: best of 3, 4 and 6 as measured)

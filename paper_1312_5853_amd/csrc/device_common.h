@@ -61,26 +61,10 @@ __global__ void relayout_filters(const float *__restrict__ w, float *__restrict_
     wt[i] = v;
 }
 
-// fp32 -> bf16, round to nearest even (NaN stays NaN)
-// fp32 -> bfloat16 bits, round to nearest even; NaN stays a (quiet) NaN
-__device__ __forceinline__ unsigned short bf16_round(float f)
-{
-    const unsigned u = __float_as_uint(f);
-    unsigned r = (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
-    if ((u & 0x7FFFFFFFu) > 0x7F800000u) r = (u >> 16) | 0x40u;
-    return (unsigned short)r;
-}
+#include "elements.h"
 
-// element access of the glue kernels: fp32 tensors, or bfloat16 tensors read exactly and written rounded
-__device__ __forceinline__ float ld_elem(const float *p, int64_t i) { return p[i]; }
-__device__ __forceinline__ float ld_elem(const unsigned short *p, int64_t i)
-{
-    return __uint_as_float((unsigned)p[i] << 16);
-}
 __device__ __forceinline__ float widen_elem(float v) { return v; }
 __device__ __forceinline__ float widen_elem(unsigned short v) { return __uint_as_float((unsigned)v << 16); }
-__device__ __forceinline__ void st_elem(float *p, int64_t i, float v) { p[i] = v; }
-__device__ __forceinline__ void st_elem(unsigned short *p, int64_t i, float v) { p[i] = bf16_round(v); }
 
 // What a forward / backward-data kernel may apply to each sum before it is stored (in this order):
 //   bias: v += bias[row]        (row = output channel)

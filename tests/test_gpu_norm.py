@@ -1,0 +1,298 @@
+"""Group normalisation with an activation on the GPU against the oracle in 64 bits, element by element.
+
+The bounds: u = 2^-24 is one fp32 rounding.  A sum of M fp32 values is taken in chains of at most a few hundred joined in
+trees, so its error is below 64 u of the sum of magnitudes; everything else is a handful of roundings.  A result stored as
+bfloat16 adds 2^-8 of itself."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_1312_5853_amd import binding as hp
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+SUM = 64 * U
+
+
+def _tensors(N, C, H, W, layout, dtype, seed, mean=0.0, std=1.0):
+    """x and dy as [N,C,S] float64 holding values of the type, and on the GPU as [N,C,H,W] in the layout."""
+    g = np.random.Generator(np.random.Philox(seed))
+    host, dev = [], []
+    for off, s in ((mean, std), (0.0, 1.0)):
+        a = (off + s * g.standard_normal((N, C, H * W)) * (0.5 + g.random((1, C, 1)))).astype(np.float32)
+        if dtype == "bf16":
+            a = oracle.bf16_round(a)
+        host.append(a.astype(np.float64))
+        dev.append(_dev(a.reshape(N, C, H, W), layout, dtype))
+    gamma, beta = (1.0 + 0.3 * g.standard_normal(C)).astype(np.float32), (0.3 * g.standard_normal(C)).astype(np.float32)
+    return host, dev, gamma, beta
+
+
+def _dev(a, layout, dtype):
+    t = torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).cuda()
+    if dtype == "bf16":
+        t = t.to(torch.bfloat16)
+    return t.contiguous(memory_format=torch.channels_last) if layout == "last" else t
+
+
+def _cuda(v):
+    return torch.from_numpy(np.ascontiguousarray(v, dtype=np.float32)).cuda()
+
+
+def _host(t, shape=None):
+    a = t.float().cpu().numpy().astype(np.float64)
+    return a.reshape(shape) if shape else a
+
+
+def _per_channel(v, C):
+    return np.repeat(v, C // v.shape[1], axis=1)[:, :, None]
+
+
+def _group_mean(v, G):
+    return v.reshape(v.shape[0], G, -1).mean(2)
+
+
+def _store(v, dtype):
+    return np.abs(v) * (2.0 ** -8 if dtype == "bf16" else 2 * U)
+
+
+def check_fwd(got, x, G, gamma, beta, eps, act, dtype):
+    y, mean, rstd = got
+    N, C, S = x.shape
+    want, wm, wr = oracle.group_norm_act_fwd(x, G, gamma, beta, eps, act)
+    big = _group_mean(np.abs(x), G)
+    e_mean = SUM * big + 2 * U * np.abs(wm)
+    # a mean off by e changes the variance by e^2 at most; its own sum and the deviations' rounding are relative errors
+    var = 1.0 / wr ** 2
+    e_var = (e_mean ** 2 + SUM * var + 4 * U * np.sqrt(var) * (big + np.abs(wm)))
+    e_rstd = wr * (e_var / var / 2 + 4 * U)
+    assert (np.abs(_host(mean) - wm) <= e_mean).all()
+    assert (np.abs(_host(rstd) - wr) <= e_rstd).all()
+    d = x - _per_channel(wm, C)
+    g = np.abs(gamma)[None, :, None]
+    e_z = g * (_per_channel(wr, C) * (_per_channel(e_mean, C) + 2 * U * np.abs(x)) + np.abs(d) * _per_channel(e_rstd, C))
+    z = np.abs(d) * _per_channel(wr, C) * g + np.abs(beta)[None, :, None]
+    e_y = 1.2 * e_z + 16 * U * z + _store(want, dtype)               # slopes of the activations are below 1.1
+    err = np.abs(_host(y, x.shape) - want)
+    assert (err <= e_y + 1e-37).all(), (err / (e_y + 1e-37)).max()
+
+
+def check_bwd(got, x, dy, mean, rstd, gamma, beta, act, dtype):
+    dx, dgamma, dbeta = got
+    N, C, S = x.shape
+    G = mean.shape[1]
+    wx, wg, wb = oracle.group_norm_act_bwd(x, dy, mean, rstd, gamma, beta, act)
+    r, m = _per_channel(rstd, C), _per_channel(mean, C)
+    xh = (x - m) * r
+    ga, be = gamma[None, :, None].astype(np.float64), beta[None, :, None].astype(np.float64)
+    z = ga * xh + be
+    e_xh = 2 * U * np.abs(xh)
+    e_z = np.abs(ga) * e_xh + 2 * U * (np.abs(ga * xh) + np.abs(be))
+    if act == "silu":
+        e_dz = np.abs(dy) * (0.5 * e_z + 24 * U * (1.0 + np.abs(z)))
+    else:
+        e_dz = np.abs(dy) * 2 * U
+    one = oracle.group_norm_act_bwd(x, dy, mean, rstd, np.ones(C), np.zeros(C), "none")      # (shapes only)
+    assert one[0].shape == wx.shape
+    slope = {"none": lambda: 1.0, "relu": lambda: (z > 0) * 1.0,
+             "silu": lambda: oracle.oracle._sigmoid(z) * (1 + z * (1 - oracle.oracle._sigmoid(z)))}[act]()
+    dz = dy * slope
+    e_dzxh = e_dz * np.abs(xh) + np.abs(dz) * e_xh
+    assert (np.abs(_host(dbeta) - wb) <= SUM * np.abs(dz).sum((0, 2)) + e_dz.sum((0, 2)) + 1e-37).all()
+    assert (np.abs(_host(dgamma) - wg) <= SUM * np.abs(dz * xh).sum((0, 2)) + e_dzxh.sum((0, 2)) + 1e-37).all()
+    a1, a2 = _group_mean(np.abs(ga * dz), G), _group_mean(np.abs(ga * dz * xh), G)
+    e1 = SUM * a1 + _group_mean(np.abs(ga) * e_dz, G)
+    e2 = SUM * a2 + _group_mean(np.abs(ga) * e_dzxh, G)
+    pc = lambda v: _per_channel(v, C)
+    e = r * (np.abs(ga) * e_dz + pc(e1) + np.abs(xh) * pc(e2) + e_xh * pc(a2)
+             + 8 * U * (np.abs(ga * dz) + pc(a1) + np.abs(xh) * pc(a2))) + _store(wx, dtype)
+    err = np.abs(_host(dx, x.shape) - wx)
+    assert (err <= e + 1e-37).all(), (err / (e + 1e-37)).max()
+
+
+def run_case(N, C, H, W, G, act, layout, dtype, seed=0, mean=0.0, std=1.0, eps=1e-5, affine=True):
+    (x, dy), (xd, dyd), gamma, beta = _tensors(N, C, H, W, layout, dtype, seed, mean, std)
+    if not affine:
+        gamma, beta = np.ones(C, np.float32), np.zeros(C, np.float32)
+    ga, be = (_cuda(gamma), _cuda(beta)) if affine else (None, None)
+    y = torch.full_like(xd, float("nan"))
+    got = hp.group_norm_act_fwd(xd, G, ga, be, eps=eps, act=act, y=y)
+    check_fwd(got, x, G, gamma, beta, eps, act, dtype)
+    m, r = (v.astype(np.float32).astype(np.float64) for v in oracle.group_norm_stats(x, G, eps))
+    if act == "relu":
+        # no gradient where rounding decides the sign of the activation's argument
+        z = (x - _per_channel(m, C)) * _per_channel(r, C) * gamma[None, :, None] + beta[None, :, None]
+        near = np.abs(z) < 1e-4 * (1 + np.abs(_per_channel(m, C)) * _per_channel(r, C))
+        dy[near] = 0.0
+        dyd = _dev(dy.reshape(N, C, H, W), layout, dtype)
+    dx = torch.full_like(xd, float("nan"))
+    got = hp.group_norm_act_bwd(xd, dyd, _cuda(m), _cuda(r), ga, be, act=act, dx=dx)
+    check_bwd(got, x, dy, m, r, gamma, beta, act, dtype)
+
+
+# N, C, H, W, groups: groups of one channel and of all, planes of one position and of a few, planes that fill no vector, a
+# wavefront's worth and one more, the network's layers, a group larger than a work-group keeps
+SHAPES = [
+    (1, 1, 1, 1, 1), (2, 4, 1, 1, 2), (3, 32, 1, 1, 32), (2, 1030, 1, 1, 2), (5, 6, 1, 2, 3), (2, 6, 1, 3, 1),
+    (2, 12, 2, 2, 4), (1, 7, 5, 1, 7), (2, 10, 1, 7, 5), (3, 24, 3, 3, 8), (2, 48, 4, 4, 3), (2, 40, 1, 17, 4), (1, 200, 6, 6, 2),
+    (2, 6, 15, 17, 2), (2, 6, 16, 16, 2), (2, 6, 1, 257, 2), (3, 384, 13, 13, 32), (2, 256, 27, 27, 32),
+    (2, 96, 55, 55, 32), (1, 33, 31, 45, 3), (2, 72, 31, 45, 8), (1, 62, 19, 23, 31), (1, 16, 64, 64, 1), (1, 5, 120, 130, 1),
+    (1, 64, 112, 113, 2), (2, 2, 224, 224, 1), (1, 1, 401, 399, 1),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_against_the_oracle(shape, layout, dtype):
+    N, C, H, W, G = shape
+    act = ("none", "relu", "silu")[(C + H) % 3]
+    run_case(N, C, H, W, G, act, layout, dtype, seed=C * H + W)
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "silu"])
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_activations(act, layout, dtype):
+    run_case(2, 24, 9, 11, 4, act, layout, dtype, seed=5)
+
+
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("mean,std", [(1e4, 1.0), (-300.0, 1e-2), (1e-20, 1e-20), (1e15, 1e13), (2.0, 0.0)])
+def test_means_far_from_zero_and_extreme_scales(mean, std, layout):
+    """The variance comes from distances to the mean: values of 10000 +- 1 keep it."""
+    run_case(2, 12, 10, 13, 3, "silu", layout, "f32", seed=6, mean=mean, std=std)
+
+
+@pytest.mark.parametrize("layout", ["planes", "last"])
+def test_without_scale_and_shift(layout):
+    run_case(2, 12, 7, 9, 3, "relu", layout, "f32", seed=7, affine=False)
+
+
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_value_that_is_no_number_stays_in_its_group(bad, layout, dtype):
+    (x, _), (xd, dyd), gamma, beta = _tensors(2, 12, 9, 9, layout, dtype, 8)
+    ga, be = _cuda(gamma), _cuda(beta)
+    want = hp.group_norm_act_fwd(xd, 4, ga, be, act="silu")
+    back = hp.group_norm_act_bwd(xd, dyd, want[1], want[2], ga, be, act="silu")
+    xb = xd.clone(memory_format=torch.preserve_format)
+    xb[1, 4, 3, 3] = bad                                             # sample 1, group 1
+    got = hp.group_norm_act_fwd(xb, 4, ga, be, act="silu")
+    here = torch.zeros(2, 12, 9, 9, dtype=torch.bool)
+    here[1, 3:6] = True
+    assert torch.isnan(got[0].float().cpu()[here]).all()
+    assert torch.equal(got[0].cpu()[~here], want[0].cpu()[~here])
+    gb = hp.group_norm_act_bwd(xb, dyd, got[1], got[2], ga, be, act="silu")
+    assert torch.isnan(gb[0].float().cpu()[here]).all()
+    assert torch.equal(gb[0].cpu()[~here], back[0].cpu()[~here])
+    assert torch.equal(gb[1].cpu()[:3], back[1].cpu()[:3]) and torch.equal(gb[1].cpu()[6:], back[1].cpu()[6:])
+
+
+@pytest.mark.parametrize("layout", ["planes", "last"])
+def test_empty_batch(layout):
+    x = _dev(np.zeros((0, 8, 3, 3)), layout, "f32")
+    y, mean, rstd = hp.group_norm_act_fwd(x, 4)
+    dg, db = torch.full((8,), 7.0, device="cuda"), torch.full((8,), 7.0, device="cuda")
+    hp.group_norm_act_bwd(x, x.clone(), mean, rstd, dgamma=dg, dbeta=db)
+    assert y.shape == x.shape and not dg.any() and not db.any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("shape", [(2, 12, 5, 7, 3), (1, 96, 55, 55, 32), (2, 6, 230, 231, 2), (3, 20, 1, 1, 4)])
+def test_nothing_outside_the_outputs_is_written_and_nothing_is_left(shape, layout, dtype):
+    """Outputs inside larger buffers, at addresses aligned to nothing but their elements; inputs too."""
+    N, C, H, W, G = shape
+    (x, dy), (xd, dyd), gamma, beta = _tensors(N, C, H, W, layout, dtype, 9)
+    td = xd.dtype
+
+    def placed(like, off, fill=None):
+        buf = torch.full((like.numel() + 128,), 7.0, dtype=td, device="cuda")
+        v = buf[off:off + like.numel()]
+        t = v.view(N, H, W, C).permute(0, 3, 1, 2) if layout == "last" else v.view(N, C, H, W)
+        t.copy_(like) if fill is None else t.fill_(fill)
+        return buf, t
+
+    nan = float("nan")
+    _, xo = placed(xd, 61)
+    _, dyo = placed(dyd, 63)
+    by, y = placed(xd, 65, nan)
+    bx, dx = placed(xd, 67, nan)
+    ga, be = _cuda(gamma), _cuda(beta)
+    want = hp.group_norm_act_fwd(xd, G, ga, be, act="silu")
+    got = hp.group_norm_act_fwd(xo, G, ga, be, act="silu", y=y)
+    back = hp.group_norm_act_bwd(xd, dyd, want[1], want[2], ga, be, act="silu")
+    gb = hp.group_norm_act_bwd(xo, dyo, want[1], want[2], ga, be, act="silu", dx=dx)
+    for a, b in zip(want + back, got + gb):
+        assert torch.equal(a, b)
+    for buf, off in ((by, 65), (bx, 67)):
+        assert bool((buf[:off] == 7.0).all()) and bool((buf[off + xd.numel():] == 7.0).all())
+        assert not torch.isnan(buf).any()
+
+
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("shape", [(3, 96, 55, 55, 32), (4, 16, 160, 160, 2), (40, 24, 3, 5, 8)])
+def test_same_bits_every_time(shape, layout):
+    N, C, H, W, G = shape
+    _, (xd, dyd), gamma, beta = _tensors(N, C, H, W, layout, "f32", 10)
+    ga, be = _cuda(gamma), _cuda(beta)
+    first = None
+    for _ in range(3):
+        f = hp.group_norm_act_fwd(xd, G, ga, be, act="relu")
+        b = hp.group_norm_act_bwd(xd, dyd, f[1], f[2], ga, be, act="relu")
+        now = [t.clone() for t in f + b]
+        assert first is None or all(torch.equal(p, q) for p, q in zip(first, now))
+        first = now
+
+
+def test_a_sample_is_normalised_alone():
+    """Results of a sample are the same bits in whatever batch it stands: a shard needs no exchange."""
+    _, (xd, _), gamma, beta = _tensors(9, 48, 13, 13, "planes", "f32", 11)
+    ga, be = _cuda(gamma), _cuda(beta)
+    whole = hp.group_norm_act_fwd(xd, 16, ga, be)[0]
+    part = hp.group_norm_act_fwd(xd[4:6], 16, ga, be)[0]
+    assert torch.allclose(whole[4:6], part, rtol=1e-5, atol=1e-6)
+
+
+def test_on_another_stream_and_in_a_graph():
+    _, (xd, dyd), gamma, beta = _tensors(4, 96, 27, 27, "planes", "f32", 12)
+    ga, be, ws = _cuda(gamma), _cuda(beta), hp.Workspace()
+    want = hp.group_norm_act_fwd(xd, 32, ga, be)
+    wb = hp.group_norm_act_bwd(xd, dyd, want[1], want[2], ga, be)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = hp.group_norm_act_fwd(xd, 32, ga, be, ws=ws)
+        gb = hp.group_norm_act_bwd(xd, dyd, got[1], got[2], ga, be, ws=ws)
+    side.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(want + wb, got + gb))
+    outs = [torch.empty_like(t) for t in want + wb]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        hp.group_norm_act_fwd(xd, 32, ga, be, y=outs[0], mean=outs[1], rstd=outs[2], ws=ws)
+        hp.group_norm_act_bwd(xd, dyd, outs[1], outs[2], ga, be, dx=outs[3], dgamma=outs[4], dbeta=outs[5], ws=ws)
+    for _ in range(3):
+        for o in outs:
+            o.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(want + wb, outs))
+
+
+def test_offsets_past_32_bits():
+    """More than 2^32 bytes to a tensor: the last samples are what they are alone."""
+    N, C, H, W = 150, 64, 336, 336                                  # 1.08e9 values, 4.3 GB
+    x = torch.zeros((N, C, H, W), device="cuda")
+    x[-2:].normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    ga, be = torch.ones(C, device="cuda"), torch.zeros(C, device="cuda")
+    y, mean, rstd = hp.group_norm_act_fwd(x, 32, ga, be)
+    y2, mean2, rstd2 = hp.group_norm_act_fwd(x[-2:].clone(), 32, ga, be)
+    assert torch.allclose(y[-2:], y2, rtol=1e-5, atol=1e-5) and torch.allclose(mean[-2:], mean2, atol=1e-6)
+    assert not y[:-2].any()
+    dy = x
+    dx = hp.group_norm_act_bwd(x, dy, mean, rstd, ga, be, dx=y)[0]
+    dx2 = hp.group_norm_act_bwd(x[-2:].clone(), dy[-2:].clone(), mean2, rstd2, ga, be)[0]
+    assert torch.allclose(dx[-2:], dx2, rtol=1e-4, atol=1e-4)

@@ -19,7 +19,7 @@ DEPS = [SRC, TRAIN_SRC] + [os.path.join(_HERE, "csrc", h) for h in (
     "plan.h", "fastdiv.h", "device_common.h", "conv_colgemm_kernels.h", "conv_bf16_dma_kernels.h",
     "conv_bf16_window_kernels.h", "conv_split_kernels.h", "conv_wgrad_split_kernels.h", "conv_direct_kernels.h",
     "conv_wgrad_rows_kernels.h", "conv_wgrad_kernels.h", "fc_kernels.h", "glue_kernels.h",
-    "host_status.h", "elements.h", "norm_kernels.h", "loss_kernels.h")] + [os.path.join(os.path.dirname(_HERE), "include", "convnet_hotpath.h")]
+    "host_status.h", "elements.h", "vectors.h", "norm_kernels.h", "loss_kernels.h")] + [os.path.join(os.path.dirname(_HERE), "include", "convnet_hotpath.h")]
 
 # no packed-fp32 instruction selection
 DEVICE_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

@@ -34,13 +34,10 @@ __device__ __forceinline__ float teacher_logit(const LossArgs &a, int64_t i)
 __device__ __forceinline__ float block_max(float v, float *red)
 {
     __syncthreads();
-    red[threadIdx.x] = v;
+    v = wave_max(v);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
-    for (int w = 128; w > 0; w >>= 1) {
-        if ((int)threadIdx.x < w) red[threadIdx.x] = fmaxf(red[threadIdx.x], red[threadIdx.x + w]);
-        __syncthreads();
-    }
-    return red[0];
+    return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
 }
 
 // One work-group per row.  GRAD: dz too; the row's statistics are taken from the row, or from row_stats where given.

@@ -1,152 +1,852 @@
 // Group normalisation with an activation, forward and backward.
-// Part of train_ops.hip: included there, inside its anonymous namespace.
+// Part of train_ops.hip: included there, inside its anonymous namespace, after vectors.h.
 //
 //   mean = sum x / M, var = sum (x - mean)^2 / M, xh = (x - mean) rstd, z = gamma xh + beta, y = act(z)
 //   dz = dy act'(z); per channel A = sum dz, B = sum dz xh; m1 = sum_c gamma A / M, m2 = sum_c gamma B / M
 //   dx = rstd (gamma dz - m1 - xh m2); dbeta = sum_n A, dgamma = sum_n B
+//
+// Bound by memory: forward has to read x and write y, backward to read x and dy and write dx; some 10 to 30 vector
+// operations to a value fit beside that.  So a value is read once and stays in registers until its result is written
+// (whole), wherever what belongs to a statistic fits the registers of one work-group: 16 waves of up to 8 vectors of 16
+// bytes a lane, of each tensor (16 channels last, forward).  What does not fit is read twice: a launch that leaves sums of tiles
+// (kSums), one that joins them, and one that applies them (kApply).
+//
+// Planes: a group's C / groups planes are one run of memory.  A wave's unit is 64 vectors of a plane, or, of planes
+// shorter than that, as many whole planes as fit 64 lanes with a power of two of lanes to a plane: so the channel is known
+// for each lane, and sums per channel are sums over lanes.
+// Channels last: a work-group takes `cw` neighbouring channels (whole groups) of a sample; a lane keeps its columns and
+// walks down the positions.
+// A plane's (row's) last vector is moved back so that it ends where the plane ends: it then holds values of the vector
+// before it too (the first k0 ones), which take no part in sums and are written twice, the same.
+
+constexpr int kWhole = 0, kSums = 1, kApply = 2;
 
 struct NormArgs {
     const void *x, *dy;
     void *out;                       // y or dx
     const float *gamma, *beta;       // nullptr: ones, zeros
-    float *mean, *rstd;              // written by the forward kernels (nullptr: not), read by the backward ones
-    float *part;                     // backward: [2][N][C], A and B of every sample and channel
+    float *mean, *rstd;              // forward: results (nullptr: not wanted); backward and kApply: read
+    float *part;                     // sums of tiles.  forward: {mean, sum of squares, count}; backward: A, then B, of a row of C
+    float *group_sums;               // backward kApply: {m1, m2} of every sample and group
     float *dgamma, *dbeta;
-    int N, C, S, groups, cpg;
-    float eps;
-    int act, last;                   // last: channels last
+    int N, C, S, groups, cpg, act;
+    float eps, inv_m;                // inv_m: 1 / M
+    FastDiv div_groups, div_cpg;
+    int part_rows, rows_per_sample;  // rows of C sums in `part`, and of those a sample's
+    // planes
+    int units, chunks, lane_bits, channels;   // of a group; chunks to a plane; lanes to a plane (log2); planes to a unit
+    int run;                                  // units to a wave
+    int tiles, parts, span;                   // of a group; of a plane (0: a tile is whole planes); units of a tile
+    FastDiv div_chunks, div_tiles;
+    // channels last
+    int cw, slab_groups, slabs, lanes, rows;  // channels, groups of a slab; slabs; lanes to a row; rows at a time
+    int tile_rows, pitch, group_lanes, channel_lanes, units_per_xcd, work;
+    FastDiv div_lanes, div_slabs;
 };
 
 __device__ __forceinline__ float act_fwd(float z, int act)
 {
-    if (act == kActRelu) return z > 0.f ? z : 0.f;
-    if (act == kActSilu) return z / (1.f + __expf(-z));
+    if (act == kActRelu) return z > 0.f ? z : z != z ? z : 0.f;
+    if (act == kActSilu) return z * __builtin_amdgcn_rcpf(1.f + __expf(-z));
     return z;
 }
 
 // dy * act'(z)
 __device__ __forceinline__ float act_bwd(float dy, float z, int act)
 {
-    if (act == kActRelu) return z > 0.f ? dy : 0.f;
+    if (act == kActRelu) return z > 0.f ? dy : z != z ? z : 0.f;
     if (act == kActSilu) {
-        const float s = 1.f / (1.f + __expf(-z));
+        const float s = __builtin_amdgcn_rcpf(1.f + __expf(-z));
         return dy * (s * (1.f + z * (1.f - s)));
     }
     return dy;
 }
 
-// sum over a work-group of 256, in a fixed order; every thread gets it
+// the waves' values joined in their order; `red` holds one per wave.  Every thread gets the sum.
+__device__ __forceinline__ float join_waves(float v, float *red, int nw)
+{
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float s = red[0];
+    for (int i = 1; i < nw; ++i) s += red[i];
+    return s;
+}
+
+// ---------------------------------------------------------------------------
+// Planes
+// ---------------------------------------------------------------------------
+struct PlaneLane { int c, off, k0, k1; };    // channel in the group, element in the group, valid values k0 <= k < k1
+
+template <int V>
+__device__ __forceinline__ PlaneLane plane_lane(const NormArgs &a, int u, int lane)
+{
+    PlaneLane p;
+    const int cg = fastdiv(u, a.div_chunks), chunk = u - cg * a.chunks;
+    p.c = cg * a.channels + (lane >> a.lane_bits);
+    const int pos = ((chunk << a.lane_bits) + (lane & ((1 << a.lane_bits) - 1))) * V;
+    const bool on = p.c < a.cpg && pos < a.S;
+    if (!on) p.c = 0;
+    if (a.S >= V) {
+        const int q = min(pos, a.S - V);
+        p.off = on ? p.c * a.S + q : 0;
+        p.k0 = on ? pos - q : V;
+        p.k1 = V;
+    } else {
+        p.off = p.c * a.S;
+        p.k0 = 0;
+        p.k1 = on ? a.S : 0;
+    }
+    return p;
+}
+
+template <typename T>
+__device__ __forceinline__ typename Vec<T>::Raw plane_load(const NormArgs &a, const T *p, const PlaneLane &l)
+{
+    return a.S >= Vec<T>::V ? Vec<T>::load(p + l.off) : Vec<T>::some(p + l.off, l.k1);
+}
+
+template <typename T>
+__device__ __forceinline__ void plane_store(const NormArgs &a, T *p, const PlaneLane &l, const float (&v)[Vec<T>::V])
+{
+    if (a.S >= Vec<T>::V) {
+        if (l.k0 < Vec<T>::V) Vec<T>::store(p + l.off, v);
+    } else {
+        for (int k = 0; k < Vec<T>::V; ++k)
+            if (k < l.k1) st_elem(p, l.off + k, v[k]);
+    }
+}
+
+// The group and the units of a work-group (SOLO: of a wave; four groups to a work-group, then).
+struct PlaneTile { int64_t group; int g, tile, u0, u1; bool live; };
+
+template <bool SOLO, int MODE>
+__device__ __forceinline__ PlaneTile plane_tile(const NormArgs &a)
+{
+    PlaneTile t;
+    t.tile = 0;
+    t.u0 = 0;
+    t.u1 = a.units;
+    t.live = true;
+    int group;
+    if (SOLO) {
+        const int total = a.N * a.groups;
+        group = uniform((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+        t.live = group < total;
+        group = min(group, total - 1);
+    } else if (MODE == kWhole) {
+        group = blockIdx.x;
+    } else {
+        group = fastdiv(blockIdx.x, a.div_tiles);
+        t.tile = blockIdx.x - group * a.tiles;
+        if (a.parts) {
+            const int plane = t.tile / a.parts;
+            t.u0 = plane * a.chunks + (t.tile - plane * a.parts) * a.span;
+            t.u1 = min(t.u0 + a.span, (plane + 1) * a.chunks);
+        } else {
+            t.u0 = t.tile * a.span;
+            t.u1 = min(t.u0 + a.span, a.units);
+        }
+    }
+    t.g = group - fastdiv(group, a.div_groups) * a.groups;
+    t.group = group;
+    return t;
+}
+
+template <typename T, int R, bool SOLO, int MODE>
+__global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_fwd(NormArgs a)
+{
+    constexpr int V = Vec<T>::V;
+    __shared__ float red[3][16];
+    const int lane = threadIdx.x & 63, wave = SOLO ? 0 : uniform((int)(threadIdx.x >> 6));
+    const int nw = SOLO ? 1 : (int)(blockDim.x >> 6);
+    const PlaneTile t = plane_tile<SOLO, MODE>(a);
+    const int64_t base = t.group * a.cpg * a.S;
+    const T *x = static_cast<const T *>(a.x) + base;
+    typename Vec<T>::Raw raw[R];
+    PlaneLane pl[R];
+    const int u0 = t.u0 + wave * a.run, n = min(a.run, t.u1 - u0);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (r < n) {
+            pl[r] = plane_lane<V>(a, u0 + r, lane);
+            raw[r] = plane_load(a, x, pl[r]);
+        }
+    float mean, rstd;
+    if (MODE == kApply) {
+        mean = a.mean[t.group];
+        rstd = a.rstd[t.group];
+    } else {
+        float s = 0.f, cnt = 0.f;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (r < n) {
+                float v[V];
+                Vec<T>::open(raw[r], v);
+                if (pl[r].k0 == 0 && pl[r].k1 == V) {
+#pragma unroll
+                    for (int k = 0; k < V; ++k) s += v[k];
+                } else {
+#pragma unroll
+                    for (int k = 0; k < V; ++k) s += k >= pl[r].k0 && k < pl[r].k1 ? v[k] : 0.f;
+                }
+                if (MODE == kSums) cnt += max(0, pl[r].k1 - pl[r].k0);
+            }
+        s = wave_sum(s);
+        if (!SOLO) s = join_waves(s, red[0], nw);
+        float inv = a.inv_m;
+        if (MODE == kSums) {
+            cnt = join_waves(wave_sum(cnt), red[2], nw);       // at most 2^16 values to a tile: exact
+            inv = 1.f / cnt;
+        }
+        mean = s * inv;
+        s = 0.f;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (r < n) {
+                float v[V];
+                Vec<T>::open(raw[r], v);
+                if (pl[r].k0 == 0 && pl[r].k1 == V) {
+#pragma unroll
+                    for (int k = 0; k < V; ++k) s += (v[k] - mean) * (v[k] - mean);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < V; ++k) s += k >= pl[r].k0 && k < pl[r].k1 ? (v[k] - mean) * (v[k] - mean) : 0.f;
+                }
+            }
+        s = wave_sum(s);
+        if (!SOLO) s = join_waves(s, red[1], nw);
+        if (MODE == kSums) {
+            if (threadIdx.x == 0) {
+                float *p = a.part + (t.group * a.tiles + t.tile) * 3;
+                p[0] = mean;
+                p[1] = s;
+                p[2] = cnt;
+            }
+            return;
+        }
+        rstd = 1.f / sqrtf(s * a.inv_m + a.eps);
+        if (t.live && lane == 0 && wave == 0) {
+            if (a.mean) a.mean[t.group] = mean;
+            if (a.rstd) a.rstd[t.group] = rstd;
+        }
+    }
+    T *y = static_cast<T *>(a.out) + base;
+    const int c0 = t.g * a.cpg;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (r < n && t.live) {
+            const float scale = rstd * (a.gamma ? a.gamma[c0 + pl[r].c] : 1.f), shift = a.beta ? a.beta[c0 + pl[r].c] : 0.f;
+            float v[V];
+            Vec<T>::open(raw[r], v);
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = act_fwd((v[k] - mean) * scale + shift, a.act);
+            plane_store(a, y, pl[r], v);
+        }
+}
+
+// With d = x - mean: z = gamma rstd d + beta, B = rstd sum dz d, dx = gamma rstd dz - rstd m1 - d rstd^2 m2.
+// Sums per channel: of a unit over its lanes.  Consecutive units of a wave that lie in one plane are added before that.
+template <typename T, int R, bool SOLO, int MODE>
+__global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_bwd(NormArgs a)
+{
+    constexpr int V = Vec<T>::V;
+    constexpr bool kKeep = sizeof(T) == 4;       // fp32: d and dz take the place of x and dy
+    extern __shared__ float slots[];             // A of every unit's planes, then B
+    const int lane = threadIdx.x & 63, wave = SOLO ? 0 : uniform((int)(threadIdx.x >> 6));
+    const PlaneTile t = plane_tile<SOLO, MODE>(a);
+    const int64_t base = t.group * a.cpg * a.S;
+    const T *x = static_cast<const T *>(a.x) + base, *dy = static_cast<const T *>(a.dy) + base;
+    typename Vec<T>::Raw rx[R], rd[R];
+    PlaneLane pl[R];
+    float scale[R], shift[R];                    // gamma rstd, beta
+    const int u0 = t.u0 + wave * a.run, n = min(a.run, t.u1 - u0);
+    const int c0 = t.g * a.cpg;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (r < n) {
+            pl[r] = plane_lane<V>(a, u0 + r, lane);
+            rx[r] = plane_load(a, x, pl[r]);
+            rd[r] = plane_load(a, dy, pl[r]);
+            scale[r] = a.gamma ? a.gamma[c0 + pl[r].c] : 1.f;
+            shift[r] = a.beta ? a.beta[c0 + pl[r].c] : 0.f;
+        }
+    const float mean = a.mean[t.group], rstd = a.rstd[t.group];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (r < n) scale[r] *= rstd;
+    float m1, m2;
+    if (MODE == kApply) {
+        m1 = a.group_sums[2 * t.group];
+        m2 = a.group_sums[2 * t.group + 1];
+    } else {
+        const int count = (t.u1 - t.u0) * a.channels;                          // slots of the tile
+        float *slot_a = slots + (SOLO ? (int)(threadIdx.x >> 6) * 2 * count : 0), *slot_b = slot_a + count;
+        float A = 0.f, B = 0.f;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (r < n) {
+                float xv[V], dv[V];
+                Vec<T>::open(rx[r], xv);
+                Vec<T>::open(rd[r], dv);
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    xv[k] -= mean;
+                    dv[k] = act_bwd(dv[k], scale[r] * xv[k] + shift[r], a.act);
+                }
+                if (pl[r].k0 == 0 && pl[r].k1 == V) {
+#pragma unroll
+                    for (int k = 0; k < V; ++k) {
+                        A += dv[k];
+                        B += dv[k] * xv[k];
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < V; ++k)
+                        if (k >= pl[r].k0 && k < pl[r].k1) {
+                            A += dv[k];
+                            B += dv[k] * xv[k];
+                        }
+                }
+                if constexpr (kKeep) {
+#pragma unroll
+                    for (int k = 0; k < V; ++k) {
+                        rx[r][k] = xv[k];
+                        rd[r][k] = dv[k];
+                    }
+                }
+                const int u = u0 + r, slot = (u - t.u0) * a.channels;
+                if (a.lane_bits == 6) {
+                    // a wave's last unit in a plane gets the sum of those before it there
+                    const bool flush = r + 1 == n || (int)fastdiv(u + 1, a.div_chunks) != (int)fastdiv(u, a.div_chunks);
+                    float ta = 0.f, tb = 0.f;
+                    if (flush) {
+                        ta = wave_sum(A);
+                        tb = wave_sum(B) * rstd;
+                        A = B = 0.f;
+                    }
+                    if (lane == 0) {
+                        slot_a[slot] = ta;
+                        slot_b[slot] = tb;
+                    }
+                } else {
+                    A = run_sum(A, 1 << a.lane_bits);
+                    B = run_sum(B, 1 << a.lane_bits) * rstd;
+                    if ((lane & ((1 << a.lane_bits) - 1)) == 0) {
+                        slot_a[slot + (lane >> a.lane_bits)] = A;
+                        slot_b[slot + (lane >> a.lane_bits)] = B;
+                    }
+                    A = B = 0.f;
+                }
+            }
+        __syncthreads();
+        // the tile's channels: from the first unit's (there is one chunk to a plane wherever a unit holds several)
+        const int first = fastdiv(t.u0, a.div_chunks) * a.channels;
+        if (MODE == kWhole) {
+            float p = 0.f, q = 0.f;
+            for (int i = lane; i < count; i += 64) {
+                const int c = fastdiv(i, a.div_chunks);
+                const float gamma = c < a.cpg && a.gamma ? a.gamma[c0 + c] : 1.f;
+                p += gamma * slot_a[i];
+                q += gamma * slot_b[i];
+            }
+            m1 = wave_sum(p) * a.inv_m;
+            m2 = wave_sum(q) * a.inv_m;
+        }
+        const int64_t n_group = fastdiv((uint32_t)t.group, a.div_groups);
+        const int64_t row = n_group * a.rows_per_sample + (a.parts ? t.tile - t.tile / a.parts * a.parts : 0);
+        const int planes = a.parts ? 1 : (count + a.chunks - 1) / a.chunks, per = a.parts ? count : a.chunks;
+        for (int j = SOLO ? lane : (int)threadIdx.x; j < planes; j += SOLO ? 64 : (int)blockDim.x)
+            if (first + j < a.cpg && t.live) {
+                float sa = 0.f, sb = 0.f;
+                for (int i = 0; i < per; ++i) {
+                    sa += slot_a[j * per + i];
+                    sb += slot_b[j * per + i];
+                }
+                a.part[row * a.C + c0 + first + j] = sa;
+                a.part[((int64_t)a.part_rows + row) * a.C + c0 + first + j] = sb;
+            }
+        if (MODE == kSums) return;
+    }
+    const float c1 = rstd * m1, c2 = rstd * rstd * m2;
+    T *dx = static_cast<T *>(a.out) + base;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (r < n && t.live) {
+            float xv[V], dv[V];
+            Vec<T>::open(rx[r], xv);
+            Vec<T>::open(rd[r], dv);
+            if (!kKeep || MODE == kApply) {
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    xv[k] -= mean;
+                    dv[k] = act_bwd(dv[k], scale[r] * xv[k] + shift[r], a.act);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < V; ++k) dv[k] = (scale[r] * dv[k] - c1) - xv[k] * c2;
+            plane_store(a, dx, pl[r], dv);
+        }
+}
+
+// ---------------------------------------------------------------------------
+// Channels last
+// ---------------------------------------------------------------------------
+struct SlabTile {
+    int n, slab, tile, s0, count;    // sample, slab, tile of positions [s0, s0 + count)
+    int j, p;                        // this thread's column vector and first row
+    int q, k0, k1;                   // its first channel in the slab, valid values k0 <= k < k1
+    bool on, live;
+};
+
+// Neighbouring slabs share lines of memory, so that a sample's slabs and tiles go to one XCD: work item = (work-groups of
+// an XCD) * XCD + its number there, as work-groups go to the eight XCDs in turn.
+template <int V>
+__device__ __forceinline__ SlabTile slab_tile(const NormArgs &a)
+{
+    SlabTile t;
+    const int item = (int)(blockIdx.x & 7) * a.units_per_xcd + (int)(blockIdx.x >> 3);
+    t.live = (int)(blockIdx.x >> 3) < a.units_per_xcd && item < a.work;
+    const int i = t.live ? item : 0;
+    const int nt = fastdiv(i, a.div_slabs);
+    t.slab = i - nt * a.slabs;
+    t.n = fastdiv(nt, a.div_tiles);
+    t.tile = nt - t.n * a.tiles;
+    t.s0 = t.tile * a.tile_rows;
+    t.count = min(a.tile_rows, a.S - t.s0);
+    t.p = fastdiv(threadIdx.x, a.div_lanes);
+    t.j = threadIdx.x - t.p * a.lanes;
+    t.on = t.p < a.rows;
+    const int c = t.j * V;
+    if (a.cw >= V) {
+        t.q = min(c, a.cw - V);
+        t.k0 = c - t.q;
+        t.k1 = V;
+    } else {
+        t.q = 0;
+        t.k0 = 0;
+        t.k1 = a.cw;
+    }
+    return t;
+}
+
+template <typename T>
+__device__ __forceinline__ typename Vec<T>::Raw slab_load(const NormArgs &a, const T *p, const SlabTile &t)
+{
+    return a.cw >= Vec<T>::V ? Vec<T>::load(p) : Vec<T>::some(p, t.k1);
+}
+
+template <typename T>
+__device__ __forceinline__ void slab_store(const NormArgs &a, T *p, const SlabTile &t, const float (&v)[Vec<T>::V])
+{
+    if (a.cw >= Vec<T>::V) {
+        Vec<T>::store(p, v);
+    } else {
+        for (int k = 0; k < Vec<T>::V; ++k)
+            if (k < t.k1) st_elem(p, k, v[k]);
+    }
+}
+
+// where the sums of channel c of the slab over the rows of thread row p lie: [value of the vector][thread], so that the
+// lanes of a wave write neighbouring words
+template <int V>
+__device__ __forceinline__ int slab_slot(const NormArgs &a, int p, int c)
+{
+    const int j = c / V, q = a.cw >= V ? min(j * V, a.cw - V) : 0;
+    return (c - q) * a.pitch + p * a.lanes + j;
+}
+
+template <typename T, int R, int MODE>
+__global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
+{
+    constexpr int V = Vec<T>::V;
+    extern __shared__ float lds[];
+    float *sum = lds, *dev = lds + V * a.pitch, *gmean = dev + V * a.pitch, *grstd = gmean + a.slab_groups;
+    const SlabTile t = slab_tile<V>(a);
+    if (!t.live) return;
+    const int64_t base = ((int64_t)t.n * a.S + t.s0) * a.C + t.slab * a.cw + t.q;
+    const T *x = static_cast<const T *>(a.x) + base;
+    typename Vec<T>::Raw raw[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int s = t.p + r * a.rows;
+        if (t.on && s < t.count) raw[r] = slab_load(a, x + s * a.C, t);
+    }
+    const int64_t group0 = (int64_t)t.n * a.groups + t.slab * a.slab_groups;
+    if (MODE != kApply) {
+        // every thread's sums and squared distances from its own mean, channel by channel
+        const int whole = t.count / a.rows, extra = t.count - whole * a.rows;       // rows of a thread: whole (+ 1)
+        if (t.on) {
+            const int cnt = whole + (t.p < extra);
+            const float inv = cnt ? 1.f / cnt : 0.f;
+            float s[V], d[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) s[k] = d[k] = 0.f;
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (t.p + r * a.rows < t.count) {
+                    float v[V];
+                    Vec<T>::open(raw[r], v);
+#pragma unroll
+                    for (int k = 0; k < V; ++k) s[k] += v[k];
+                }
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (t.p + r * a.rows < t.count) {
+                    float v[V];
+                    Vec<T>::open(raw[r], v);
+#pragma unroll
+                    for (int k = 0; k < V; ++k) {
+                        const float e = v[k] - s[k] * inv;
+                        d[k] += e * e;
+                    }
+                }
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                sum[k * a.pitch + threadIdx.x] = s[k];
+                dev[k * a.pitch + threadIdx.x] = d[k];
+            }
+        }
+        __syncthreads();
+        // a group's sum, then its squared distances: those of the parts, and the parts' means' own
+        const int lane = threadIdx.x & (a.group_lanes - 1), entries = a.rows * a.cpg;
+        const int at = threadIdx.x / a.group_lanes, step = blockDim.x / a.group_lanes;
+        const float total = (float)t.count * a.cpg, inv_total = 1.f / total;
+        const float inv_whole = whole ? 1.f / whole : 0.f, inv_more = 1.f / (whole + 1);
+        for (int g0 = 0; g0 < a.slab_groups; g0 += step) {
+            const int g = g0 + at;
+            const bool some = g < a.slab_groups;
+            float s = 0.f, d = 0.f;
+            if (some)
+                for (int e = lane; e < entries; e += a.group_lanes) {
+                    const int p = fastdiv(e, a.div_cpg);
+                    s += sum[slab_slot<V>(a, p, g * a.cpg + e - p * a.cpg)];
+                }
+            const float mean = run_sum(s, a.group_lanes) * inv_total;
+            if (some)
+                for (int e = lane; e < entries; e += a.group_lanes) {
+                    const int p = fastdiv(e, a.div_cpg), at2 = slab_slot<V>(a, p, g * a.cpg + e - p * a.cpg);
+                    const bool more = p < extra;
+                    const float diff = sum[at2] * (more ? inv_more : inv_whole) - mean;
+                    if (more || whole) d += dev[at2] + (float)(whole + more) * diff * diff;
+                }
+            d = run_sum(d, a.group_lanes);
+            if (some && lane == 0) {
+                if (MODE == kSums) {
+                    float *p = a.part + ((group0 + g) * a.tiles + t.tile) * 3;
+                    p[0] = mean;
+                    p[1] = d;
+                    p[2] = total;
+                } else {
+                    const float rstd = 1.f / sqrtf(d * a.inv_m + a.eps);
+                    gmean[g] = mean;
+                    grstd[g] = rstd;
+                    if (a.mean) a.mean[group0 + g] = mean;
+                    if (a.rstd) a.rstd[group0 + g] = rstd;
+                }
+            }
+        }
+        if (MODE == kSums) return;
+        __syncthreads();
+    }
+    if (!t.on) return;
+    float mean[V], scale[V], shift[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const int c = min(t.q + k, a.cw - 1), g = fastdiv(c, a.div_cpg), ch = t.slab * a.cw + c;
+        mean[k] = MODE == kApply ? a.mean[group0 + g] : gmean[g];
+        scale[k] = (MODE == kApply ? a.rstd[group0 + g] : grstd[g]) * (a.gamma ? a.gamma[ch] : 1.f);
+        shift[k] = a.beta ? a.beta[ch] : 0.f;
+    }
+    T *y = static_cast<T *>(a.out) + base;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int s = t.p + r * a.rows;
+        if (s < t.count) {
+            float v[V];
+            Vec<T>::open(raw[r], v);
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = act_fwd((v[k] - mean[k]) * scale[k] + shift[k], a.act);
+            slab_store(a, y + s * a.C, t, v);
+        }
+    }
+}
+
+template <typename T, int R, int MODE>
+__global__ __launch_bounds__(1024) void group_norm_last_bwd(NormArgs a)
+{
+    constexpr int V = Vec<T>::V;
+    constexpr bool kKeep = sizeof(T) == 4;
+    extern __shared__ float lds[];
+    float *sa = lds, *sb = lds + V * a.pitch, *ca = sb + V * a.pitch, *cb = ca + a.cw, *g1 = cb + a.cw, *g2 = g1 + a.slab_groups;
+    const SlabTile t = slab_tile<V>(a);
+    if (!t.live) return;
+    const int64_t base = ((int64_t)t.n * a.S + t.s0) * a.C + t.slab * a.cw + t.q;
+    const T *x = static_cast<const T *>(a.x) + base, *dy = static_cast<const T *>(a.dy) + base;
+    typename Vec<T>::Raw rx[R], rd[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int s = t.p + r * a.rows;
+        if (t.on && s < t.count) {
+            rx[r] = slab_load(a, x + s * a.C, t);
+            rd[r] = slab_load(a, dy + s * a.C, t);
+        }
+    }
+    const int64_t group0 = (int64_t)t.n * a.groups + t.slab * a.slab_groups;
+    float mean[V], scale[V], shift[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const int c = min(t.q + k, a.cw - 1), ch = t.slab * a.cw + c;
+        const int64_t g = group0 + fastdiv(c, a.div_cpg);
+        mean[k] = a.mean[g];
+        scale[k] = a.rstd[g] * (a.gamma ? a.gamma[ch] : 1.f);
+        shift[k] = a.beta ? a.beta[ch] : 0.f;
+    }
+    if (MODE != kApply) {
+        if (t.on) {
+            float A[V], B[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) A[k] = B[k] = 0.f;
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (t.p + r * a.rows < t.count) {
+                    float xv[V], dv[V];
+                    Vec<T>::open(rx[r], xv);
+                    Vec<T>::open(rd[r], dv);
+#pragma unroll
+                    for (int k = 0; k < V; ++k) {
+                        xv[k] -= mean[k];
+                        dv[k] = act_bwd(dv[k], scale[k] * xv[k] + shift[k], a.act);
+                        A[k] += dv[k];
+                        B[k] += dv[k] * xv[k];
+                        if constexpr (kKeep) {
+                            rx[r][k] = xv[k];
+                            rd[r][k] = dv[k];
+                        }
+                    }
+                }
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                sa[k * a.pitch + threadIdx.x] = A[k];
+                sb[k * a.pitch + threadIdx.x] = B[k];
+            }
+        }
+        __syncthreads();
+        // channels: the sums over the thread rows
+        const int64_t row = (int64_t)t.n * a.rows_per_sample + t.tile;
+        {
+            const int lane = threadIdx.x & (a.channel_lanes - 1);
+            const int at = threadIdx.x / a.channel_lanes, step = blockDim.x / a.channel_lanes;
+            for (int c0 = 0; c0 < a.cw; c0 += step) {
+                const int c = c0 + at;
+                float A = 0.f, B = 0.f;
+                if (c < a.cw)
+                    for (int p = lane; p < a.rows; p += a.channel_lanes) {
+                        const int s = slab_slot<V>(a, p, c);
+                        A += sa[s];
+                        B += sb[s];
+                    }
+                A = run_sum(A, a.channel_lanes);
+                B = run_sum(B, a.channel_lanes);
+                if (c < a.cw && lane == 0) {
+                    const int ch = t.slab * a.cw + c;
+                    const float gamma = a.gamma ? a.gamma[ch] : 1.f;
+                    B *= a.rstd[group0 + fastdiv(c, a.div_cpg)];
+                    ca[c] = gamma * A;
+                    cb[c] = gamma * B;
+                    a.part[row * a.C + ch] = A;
+                    a.part[((int64_t)a.part_rows + row) * a.C + ch] = B;
+                }
+            }
+        }
+        if (MODE == kSums) return;
+        __syncthreads();
+        const int lane = threadIdx.x & (a.group_lanes - 1);
+        const int at = threadIdx.x / a.group_lanes, step = blockDim.x / a.group_lanes;
+        for (int g0 = 0; g0 < a.slab_groups; g0 += step) {
+            const int g = g0 + at;
+            float p = 0.f, q = 0.f;
+            if (g < a.slab_groups)
+                for (int e = lane; e < a.cpg; e += a.group_lanes) {
+                    p += ca[g * a.cpg + e];
+                    q += cb[g * a.cpg + e];
+                }
+            p = run_sum(p, a.group_lanes);
+            q = run_sum(q, a.group_lanes);
+            if (g < a.slab_groups && lane == 0) {
+                g1[g] = p * a.inv_m;
+                g2[g] = q * a.inv_m;
+            }
+        }
+        __syncthreads();
+    }
+    if (!t.on) return;
+    float c1[V], c2[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const int g = fastdiv(min(t.q + k, a.cw - 1), a.div_cpg);
+        const float rstd = a.rstd[group0 + g];
+        c1[k] = rstd * (MODE == kApply ? a.group_sums[2 * (group0 + g)] : g1[g]);
+        c2[k] = rstd * rstd * (MODE == kApply ? a.group_sums[2 * (group0 + g) + 1] : g2[g]);
+    }
+    T *dx = static_cast<T *>(a.out) + base;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int s = t.p + r * a.rows;
+        if (s < t.count) {
+            float xv[V], dv[V];
+            Vec<T>::open(rx[r], xv);
+            Vec<T>::open(rd[r], dv);
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                if (!kKeep || MODE == kApply) {
+                    xv[k] -= mean[k];
+                    dv[k] = act_bwd(dv[k], scale[k] * xv[k] + shift[k], a.act);
+                }
+                dv[k] = (scale[k] * dv[k] - c1[k]) - xv[k] * c2[k];
+            }
+            slab_store(a, dx + s * a.C, t, dv);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Joining the tiles
+// ---------------------------------------------------------------------------
+// A wave per sample and group: the tiles' means and squared distances, joined to the group's.
+__global__ __launch_bounds__(256) void group_norm_join_stats(const float *part, int tiles, int total, float inv_m, float eps,
+                                                             float *mean, float *rstd, float *mean_out, float *rstd_out)
+{
+    const int lane = threadIdx.x & 63, i = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const float *p = part + (int64_t)min(i, total - 1) * tiles * 3;
+    float s = 0.f, d = 0.f;
+    for (int t = lane; t < tiles; t += 64) s += p[3 * t] * p[3 * t + 2];
+    const float m = wave_sum(s) * inv_m;
+    for (int t = lane; t < tiles; t += 64) d += p[3 * t + 1] + p[3 * t + 2] * (p[3 * t] - m) * (p[3 * t] - m);
+    const float r = 1.f / sqrtf(wave_sum(d) * inv_m + eps);
+    if (lane == 0 && i < total) {
+        mean[i] = m;
+        rstd[i] = r;
+        if (mean_out) mean_out[i] = m;
+        if (rstd_out) rstd_out[i] = r;
+    }
+}
+
+// A wave per sample and group: {m1, m2} from the rows of channel sums.
+__global__ __launch_bounds__(256) void group_norm_join_groups(NormArgs a)
+{
+    const int lane = threadIdx.x & 63, total = a.N * a.groups, i = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int grp = min(i, total - 1), n = fastdiv(grp, a.div_groups), c0 = (grp - n * a.groups) * a.cpg;
+    float p = 0.f, q = 0.f;
+    for (int e = lane; e < a.rows_per_sample * a.cpg; e += 64) {
+        const int t = fastdiv(e, a.div_cpg), c = c0 + e - t * a.cpg;
+        const int64_t row = (int64_t)n * a.rows_per_sample + t;
+        const float gamma = a.gamma ? a.gamma[c] : 1.f;
+        p += gamma * a.part[row * a.C + c];
+        q += gamma * a.part[((int64_t)a.part_rows + row) * a.C + c];
+    }
+    p = wave_sum(p) * a.inv_m;
+    q = wave_sum(q) * a.inv_m;
+    if (lane == 0 && i < total) {
+        a.group_sums[2 * i] = p;
+        a.group_sums[2 * i + 1] = q;
+    }
+}
+
+// Gradients of gamma and beta: a work-group adds the rows of 32 channels, 32 rows at a time, then in a tree.
+__global__ __launch_bounds__(1024) void group_norm_join_channels(NormArgs a)
+{
+    __shared__ float red[2][32][33];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
+    float A = 0.f, B = 0.f;
+    if (c < a.C)
+        for (int r = y; r < a.part_rows; r += 32) {
+            A += a.part[(int64_t)r * a.C + c];
+            B += a.part[((int64_t)a.part_rows + r) * a.C + c];
+        }
+    red[0][y][x] = A;
+    red[1][y][x] = B;
+    __syncthreads();
+    // half a wave per channel: lane x of row y holds row x of channel y
+    A = run_sum(red[0][x][y], 32);
+    B = run_sum(red[1][x][y], 32);
+    const int ch = blockIdx.x * 32 + y;
+    if (x == 0 && ch < a.C) {
+        if (a.dbeta) a.dbeta[ch] = A;
+        if (a.dgamma) a.dgamma[ch] = B;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Groups of very many channels, channels last (a row of a group is more than a work-group's vectors): one work-group per
+// sample and group, a pass over memory for every step, a thread to a channel
+// ---------------------------------------------------------------------------
 __device__ __forceinline__ float block_sum(float v, float *red)
 {
     __syncthreads();
-    red[threadIdx.x] = v;
-    __syncthreads();
-    for (int w = 128; w > 0; w >>= 1) {
-        if ((int)threadIdx.x < w) red[threadIdx.x] += red[threadIdx.x + w];
-        __syncthreads();
-    }
-    return red[0];
+    const float s = join_waves(wave_sum(v), red, (int)(blockDim.x >> 6));
+    return s;
 }
 
-// element i of (sample n, group g), and its channel
-__device__ __forceinline__ int64_t norm_elem(const NormArgs &a, int n, int g, int i, int &c)
-{
-    if (a.last) {
-        c = g * a.cpg + i % a.cpg;
-        return ((int64_t)n * a.S + i / a.cpg) * a.C + c;
-    }
-    c = g * a.cpg + i / a.S;
-    return ((int64_t)n * a.C + g * a.cpg) * a.S + i;
-}
-
-// one work-group per sample and group, three passes over its values
 template <typename T>
-__global__ __launch_bounds__(256) void group_norm_fwd_kernel(NormArgs a)
+__global__ __launch_bounds__(1024) void group_norm_wide_fwd(NormArgs a)
 {
-    __shared__ float red[256];
-    const int n = blockIdx.x / a.groups, g = blockIdx.x % a.groups, M = a.cpg * a.S;
-    const T *x = static_cast<const T *>(a.x);
-    T *y = static_cast<T *>(a.out);
-    int c;
+    __shared__ float red[16];
+    const int n = fastdiv(blockIdx.x, a.div_groups), c0 = (blockIdx.x - n * a.groups) * a.cpg;
+    const T *x = static_cast<const T *>(a.x) + (int64_t)n * a.S * a.C;
+    T *y = static_cast<T *>(a.out) + (int64_t)n * a.S * a.C;
     float s = 0.f;
-    for (int i = threadIdx.x; i < M; i += 256) s += ld_elem(x, norm_elem(a, n, g, i, c));
-    const float mean = block_sum(s, red) / M;
+    for (int r = 0; r < a.S; ++r)
+        for (int c = c0 + threadIdx.x; c < c0 + a.cpg; c += blockDim.x) s += ld_elem(x, r * a.C + c);
+    const float mean = block_sum(s, red) * a.inv_m;
     s = 0.f;
-    for (int i = threadIdx.x; i < M; i += 256) {
-        const float d = ld_elem(x, norm_elem(a, n, g, i, c)) - mean;
-        s += d * d;
-    }
-    const float rstd = 1.f / sqrtf(block_sum(s, red) / M + a.eps);
+    for (int r = 0; r < a.S; ++r)
+        for (int c = c0 + threadIdx.x; c < c0 + a.cpg; c += blockDim.x) {
+            const float d = ld_elem(x, r * a.C + c) - mean;
+            s += d * d;
+        }
+    const float rstd = 1.f / sqrtf(block_sum(s, red) * a.inv_m + a.eps);
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[blockIdx.x] = mean;
         if (a.rstd) a.rstd[blockIdx.x] = rstd;
     }
-    for (int i = threadIdx.x; i < M; i += 256) {
-        const int64_t e = norm_elem(a, n, g, i, c);
-        const float z = (ld_elem(x, e) - mean) * rstd * (a.gamma ? a.gamma[c] : 1.f) + (a.beta ? a.beta[c] : 0.f);
-        st_elem(y, e, act_fwd(z, a.act));
-    }
-}
-
-// A and B of a sample's channel, one work-group each
-template <typename T>
-__global__ __launch_bounds__(256) void group_norm_bwd_sums(NormArgs a)
-{
-    __shared__ float red[256];
-    const int n = blockIdx.x / a.C, c = blockIdx.x % a.C, g = c / a.cpg;
-    const float mean = a.mean[(int64_t)n * a.groups + g], rstd = a.rstd[(int64_t)n * a.groups + g];
-    const float gamma = a.gamma ? a.gamma[c] : 1.f, beta = a.beta ? a.beta[c] : 0.f;
-    const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
-    float A = 0.f, B = 0.f;
-    for (int s = threadIdx.x; s < a.S; s += 256) {
-        const int64_t e = a.last ? ((int64_t)n * a.S + s) * a.C + c : ((int64_t)n * a.C + c) * a.S + s;
-        const float xh = (ld_elem(x, e) - mean) * rstd, dz = act_bwd(ld_elem(dy, e), gamma * xh + beta, a.act);
-        A += dz;
-        B += dz * xh;
-    }
-    A = block_sum(A, red);
-    B = block_sum(B, red);
-    if (threadIdx.x == 0) {
-        a.part[blockIdx.x] = A;
-        a.part[(int64_t)a.N * a.C + blockIdx.x] = B;
+    for (int c = c0 + threadIdx.x; c < c0 + a.cpg; c += blockDim.x) {
+        const float scale = rstd * (a.gamma ? a.gamma[c] : 1.f), shift = a.beta ? a.beta[c] : 0.f;
+        for (int r = 0; r < a.S; ++r)
+            st_elem(y, r * a.C + c, act_fwd((ld_elem(x, r * a.C + c) - mean) * scale + shift, a.act));
     }
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void group_norm_bwd_kernel(NormArgs a)
+__global__ __launch_bounds__(1024) void group_norm_wide_bwd(NormArgs a)
 {
-    __shared__ float red[256];
-    const int n = blockIdx.x / a.groups, g = blockIdx.x % a.groups, M = a.cpg * a.S;
-    const T *x = static_cast<const T *>(a.x), *dy = static_cast<const T *>(a.dy);
-    T *dx = static_cast<T *>(a.out);
+    __shared__ float red[16];
+    const int n = fastdiv(blockIdx.x, a.div_groups), c0 = (blockIdx.x - n * a.groups) * a.cpg;
+    const T *x = static_cast<const T *>(a.x) + (int64_t)n * a.S * a.C, *dy = static_cast<const T *>(a.dy) + (int64_t)n * a.S * a.C;
+    T *dx = static_cast<T *>(a.out) + (int64_t)n * a.S * a.C;
     const float mean = a.mean[blockIdx.x], rstd = a.rstd[blockIdx.x];
-    float p = 0.f, q = 0.f;
-    for (int j = threadIdx.x; j < a.cpg; j += 256) {
-        const int c = g * a.cpg + j;
-        const float gamma = a.gamma ? a.gamma[c] : 1.f;
-        p += gamma * a.part[(int64_t)n * a.C + c];
-        q += gamma * a.part[(int64_t)(a.N + n) * a.C + c];
-    }
-    const float m1 = block_sum(p, red) / M, m2 = block_sum(q, red) / M;
-    int c;
-    for (int i = threadIdx.x; i < M; i += 256) {
-        const int64_t e = norm_elem(a, n, g, i, c);
+    float m1 = 0.f, m2 = 0.f;
+    for (int c = c0 + threadIdx.x; c < c0 + a.cpg; c += blockDim.x) {
         const float gamma = a.gamma ? a.gamma[c] : 1.f, beta = a.beta ? a.beta[c] : 0.f;
-        const float xh = (ld_elem(x, e) - mean) * rstd, dz = act_bwd(ld_elem(dy, e), gamma * xh + beta, a.act);
-        st_elem(dx, e, rstd * (gamma * dz - m1 - xh * m2));
+        float A = 0.f, B = 0.f;
+        for (int r = 0; r < a.S; ++r) {
+            const float xh = (ld_elem(x, r * a.C + c) - mean) * rstd;
+            const float dz = act_bwd(ld_elem(dy, r * a.C + c), gamma * xh + beta, a.act);
+            A += dz;
+            B += dz * xh;
+        }
+        a.part[(int64_t)n * a.C + c] = A;
+        a.part[((int64_t)a.part_rows + n) * a.C + c] = B;
+        m1 += gamma * A;
+        m2 += gamma * B;
     }
-}
-
-// sums over the samples, in order, a thread per channel
-__global__ void group_norm_bwd_finish(NormArgs a)
-{
-    const int c = blockIdx.x * blockDim.x + threadIdx.x;
-    if (c >= a.C) return;
-    float A = 0.f, B = 0.f;
-    for (int n = 0; n < a.N; ++n) {
-        A += a.part[(int64_t)n * a.C + c];
-        B += a.part[(int64_t)(a.N + n) * a.C + c];
+    m1 = block_sum(m1, red) * a.inv_m;
+    m2 = block_sum(m2, red) * a.inv_m;
+    for (int c = c0 + threadIdx.x; c < c0 + a.cpg; c += blockDim.x) {
+        const float gamma = a.gamma ? a.gamma[c] : 1.f, beta = a.beta ? a.beta[c] : 0.f;
+        for (int r = 0; r < a.S; ++r) {
+            const float xh = (ld_elem(x, r * a.C + c) - mean) * rstd;
+            const float dz = act_bwd(ld_elem(dy, r * a.C + c), gamma * xh + beta, a.act);
+            st_elem(dx, r * a.C + c, rstd * (gamma * dz - m1 - xh * m2));
+        }
     }
-    if (a.dbeta) a.dbeta[c] = A;
-    if (a.dgamma) a.dgamma[c] = B;
 }

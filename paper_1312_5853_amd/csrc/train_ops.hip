@@ -17,6 +17,7 @@ namespace {
 constexpr int kActNone = CONV_ACT_NONE, kActRelu = CONV_ACT_RELU, kActSilu = CONV_ACT_SILU;
 
 #include "elements.h"
+#include "vectors.h"
 #include "norm_kernels.h"
 #include "loss_kernels.h"
 
@@ -33,53 +34,286 @@ int norm_checks(int N, int C, int S, int groups, int layout, int dtype)
     return kStatusOk;
 }
 
-size_t norm_workspace(int op, int N, int C, int S, int groups, int layout, int dtype)
+int pow2_up(int v)
 {
-    if (norm_checks(N, C, S, groups, layout, dtype) != kStatusOk) return 0;
-    if (op != CONV_OP_BWD_DATA) return 0;
-    return (size_t)2 * N * C * 4;
+    int p = 1;
+    while (p < v) p <<= 1;
+    return p;
+}
+int pow2_down(int v)
+{
+    int p = 1;
+    while (2 * p <= v) p <<= 1;
+    return p;
 }
 
-int norm_common(NormArgs &a, int op, int N, int C, int S, int groups, int act, int layout, int dtype, void *ws,
-                size_t ws_bytes)
+constexpr int kMaxWaves = 16, kSplitWaves = 8, kSplitRun = 4;
+
+// How a call runs: which kernels, on what tiles, with how much scratch.
+struct NormPlan {
+    bool planes, wide, split, solo;
+    int threads, regs;               // vectors a lane keeps (of each input): the kernel's template argument
+    int64_t blocks;
+    size_t lds, part_bytes, sums_bytes, total;
+    NormArgs a;
+};
+
+int regs_for(int run, int most)
 {
+    return std::min(pow2_up(run), most);
+}
+
+void plan_planes(NormPlan &p, bool bwd, int V)
+{
+    NormArgs &a = p.a;
+    const int nv = (a.S + V - 1) / V;
+    a.lane_bits = 0;
+    while ((1 << a.lane_bits) < nv && a.lane_bits < 6) ++a.lane_bits;
+    a.chunks = (nv + 63) / 64;
+    a.channels = 64 >> a.lane_bits;
+    const int runs = ceil_div(a.cpg, a.channels);          // a plane's units, or a unit's planes
+    const int64_t units = (int64_t)runs * a.chunks;
+    const int most = 8;
+    const int64_t groups = (int64_t)a.N * a.groups;
+    a.tiles = 1;
+    if (units <= (int64_t)kMaxWaves * most && (!bwd || units * a.channels <= 8192)) {
+        a.units = (int)units;
+        p.solo = units <= 4 && groups >= 1024;
+        // a wave keeps up to four units while that leaves enough waves; few groups take a wave to a unit
+        const int want = groups >= 1024 ? 4 : 1;
+        const int waves = p.solo ? 1 : std::min(kMaxWaves, ceil_div(a.units, want));
+        a.run = ceil_div(a.units, waves);
+        p.threads = p.solo ? 256 : 64 * ceil_div(a.units, a.run);
+        p.blocks = p.solo ? (groups + 3) / 4 : groups;
+        p.regs = regs_for(a.run, most);
+        a.span = a.units;
+    } else {
+        p.split = true;
+        a.units = (int)units;
+        const int per = kSplitWaves * kSplitRun;
+        if (a.chunks > per) {
+            a.parts = ceil_div(a.chunks, per);
+            a.span = ceil_div(a.chunks, a.parts);
+            a.tiles = a.cpg * a.parts;
+        } else {
+            const int whole = std::max(1, per / a.chunks);
+            a.span = whole * a.chunks;
+            a.tiles = ceil_div(runs, whole);
+        }
+        p.threads = 64 * kSplitWaves;
+        a.run = kSplitRun;
+        p.regs = kSplitRun;
+        p.blocks = groups * a.tiles;
+    }
+    a.rows_per_sample = a.parts ? a.parts : 1;
+    p.lds = bwd ? (size_t)(p.solo ? 4 : 1) * 2 * a.span * a.channels * 4 : 0;
+    a.div_chunks = make_fastdiv(a.chunks);
+}
+
+void plan_last(NormPlan &p, bool bwd, int V, int eb)
+{
+    NormArgs &a = p.a;
+    const int most = bwd ? 8 : 16;
+    int best = 0;
+    double best_score = 0.0;
+    auto lanes_of = [&](int slab_groups) { return (int)(((int64_t)slab_groups * a.cpg + V - 1) / V); };
+    for (int j = 1; j <= a.groups; ++j) {
+        if (a.groups % j) continue;
+        const int64_t lanes64 = ((int64_t)j * a.cpg + V - 1) / V;
+        if (lanes64 > 1024) break;
+        const int rows = 1024 / (int)lanes64;
+        if (ceil_div(a.S, rows) > most) continue;
+        const double seg = (double)j * a.cpg * eb;
+        if (seg < 64 && j != a.groups) continue;
+        // lines that a slab shares with its neighbours are read by both; few work-groups leave the card idle
+        const double wgs = (double)a.N * (a.groups / j);
+        const double score = seg / (seg + 64) * std::min(1.0, wgs / 512);
+        if (score > best_score) { best_score = score; best = j; }
+    }
+    int threads;
+    if (best) {
+        a.slab_groups = best;
+        a.lanes = lanes_of(best);
+        const int want = 4;
+        threads = std::min<int64_t>(1024, round_up64((int64_t)a.lanes * ceil_div(a.S, want), 64));
+        a.rows = threads / a.lanes;
+        a.tile_rows = a.S;
+        a.tiles = 1;
+    } else {
+        p.split = true;
+        int j = 1;
+        for (int k = 1; k <= a.groups; ++k)
+            if (a.groups % k == 0 && lanes_of(k) <= 512) j = k;
+        a.slab_groups = j;
+        a.lanes = lanes_of(j);
+        threads = std::max(512, round_up(a.lanes, 64));
+        a.rows = threads / a.lanes;
+        a.tile_rows = std::min(a.S, a.rows * kSplitRun);
+        a.tiles = ceil_div(a.S, a.tile_rows);
+    }
+    a.cw = a.slab_groups * a.cpg;
+    a.slabs = a.groups / a.slab_groups;
+    p.threads = threads;
+    p.regs = regs_for(ceil_div(a.tile_rows, a.rows), most);
+    a.pitch = threads + 9;
+    a.group_lanes = std::min(64, pow2_down(std::max(1, threads / a.slab_groups)));
+    a.channel_lanes = std::min(64, pow2_down(std::max(1, threads / a.cw)));
+    a.work = a.N * a.tiles * a.slabs;
+    a.units_per_xcd = ceil_div(a.work, 8);
+    p.blocks = 8 * (int64_t)a.units_per_xcd;
+    p.lds = (size_t)(2 * V * a.pitch + 2 * a.slab_groups + (bwd ? 2 * a.cw : 0)) * 4;
+    a.rows_per_sample = a.tiles;
+    a.div_lanes = make_fastdiv(a.lanes);
+    a.div_slabs = make_fastdiv(a.slabs);
+}
+
+int plan_norm(NormPlan &p, int op, int N, int C, int S, int groups, int layout, int dtype)
+{
+    p = {};
     const int rc = norm_checks(N, C, S, groups, layout, dtype);
     if (rc != kStatusOk) return rc;
-    if (act != kActNone && act != kActRelu && act != kActSilu) return kErrInvalidArg;
+    if (op != CONV_OP_FWD && op != CONV_OP_BWD_DATA) return kErrInvalidArg;
+    const bool bwd = op == CONV_OP_BWD_DATA;
+    const int eb = glue_elem_bytes(dtype), V = 16 / eb;
+    NormArgs &a = p.a;
+    a.N = N; a.C = C; a.S = S; a.groups = groups; a.cpg = C / groups;
+    a.inv_m = (float)(1.0 / ((double)a.cpg * S));
+    a.div_groups = make_fastdiv(groups);
+    a.div_cpg = make_fastdiv(a.cpg);
+    // one channel, or one position: the same memory either way
+    p.planes = layout == CONV_LAYOUT_PLANES ? S > 1 : C == 1;
+    p.wide = !p.planes && a.cpg > 1024 * V;
+    if (p.wide) {
+        p.threads = 1024;
+        p.blocks = (int64_t)N * groups;
+        a.tiles = a.rows_per_sample = 1;
+    } else if (p.planes) {
+        plan_planes(p, bwd, V);
+    } else {
+        plan_last(p, bwd, V, eb);
+    }
+    a.div_tiles = make_fastdiv(a.tiles);
+    if ((int64_t)N * a.rows_per_sample >= ((int64_t)1 << 31) || p.blocks >= ((int64_t)1 << 31)) return kErrTooLarge;
+    a.part_rows = N * a.rows_per_sample;
+    const int64_t ng = (int64_t)N * groups;
+    if (bwd) p.part_bytes = (size_t)2 * a.part_rows * C * 4;
+    else if (p.split) p.part_bytes = (size_t)ng * a.tiles * 3 * 4;
+    if (p.split) p.sums_bytes = (size_t)ng * 2 * 4;
+    p.part_bytes = (size_t)round_up64(p.part_bytes, 256);
+    p.total = p.part_bytes + (size_t)round_up64(p.sums_bytes, 256);
+    return kStatusOk;
+}
+
+// a holds the call's pointers, act and eps; takes the plan's figures over
+int norm_common(NormPlan &p, const NormArgs &given, int op, int N, int C, int S, int groups, int layout, int dtype, void *ws,
+                size_t ws_bytes)
+{
+    const int rc = plan_norm(p, op, N, C, S, groups, layout, dtype);
+    if (rc != kStatusOk) return rc;
+    const NormArgs &a = given;
+    if (a.act != kActNone && a.act != kActRelu && a.act != kActSilu) return kErrInvalidArg;
     const size_t eb = glue_elem_bytes(dtype);
     if (!aligned(a.x, eb) || !aligned(a.dy, eb) || !aligned(a.out, eb)) return kErrMisaligned;
     if (!aligned(a.gamma, 4) || !aligned(a.beta, 4) || !aligned(a.mean, 4) || !aligned(a.rstd, 4) ||
         !aligned(a.dgamma, 4) || !aligned(a.dbeta, 4))
         return kErrMisaligned;
-    const size_t need = norm_workspace(op, N, C, S, groups, layout, dtype);
-    if (need) {
-        if (!ws || ws_bytes < need) return kErrWorkspace;
+    if (p.total) {
+        if (!ws || ws_bytes < p.total) return kErrWorkspace;
         if (!aligned(ws, 256)) return kErrMisaligned;
     }
-    a.part = static_cast<float *>(ws);
-    a.N = N; a.C = C; a.S = S; a.groups = groups; a.cpg = C / groups;
-    a.act = act; a.last = layout == CONV_LAYOUT_CHANNELS_LAST;
+    p.a.x = a.x; p.a.dy = a.dy; p.a.out = a.out; p.a.gamma = a.gamma; p.a.beta = a.beta;
+    p.a.mean = a.mean; p.a.rstd = a.rstd; p.a.dgamma = a.dgamma; p.a.dbeta = a.dbeta;
+    p.a.act = a.act; p.a.eps = a.eps;
+    p.a.part = static_cast<float *>(ws);
+    p.a.group_sums = reinterpret_cast<float *>(static_cast<char *>(ws) + p.part_bytes);
     return kStatusOk;
 }
 
-template <typename T>
-int run_norm_fwd(const NormArgs &a, hipStream_t st)
+template <typename Kern>
+void launch_norm(Kern kern, const NormPlan &p, size_t lds, hipStream_t st)
 {
-    hipLaunchKernelGGL(group_norm_fwd_kernel<T>, dim3(a.N * a.groups), dim3(256), 0, st, a);
+    if (lds > 64 * 1024)                             // more dynamic LDS than that has to be allowed per kernel
+        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    hipLaunchKernelGGL(kern, dim3((unsigned)p.blocks), dim3(p.threads), lds, st, p.a);
+}
+
+template <typename T, int MODE>
+void launch_norm_fwd(const NormPlan &p, hipStream_t st)
+{
+    if (p.planes) {
+        if constexpr (MODE != kWhole) launch_norm(group_norm_planes_fwd<T, kSplitRun, false, MODE>, p, 0, st);
+        else if (p.solo && p.regs == 1) launch_norm(group_norm_planes_fwd<T, 1, true, MODE>, p, 0, st);
+        else if (p.solo && p.regs == 2) launch_norm(group_norm_planes_fwd<T, 2, true, MODE>, p, 0, st);
+        else if (p.solo) launch_norm(group_norm_planes_fwd<T, 4, true, MODE>, p, 0, st);
+        else if (p.regs == 1) launch_norm(group_norm_planes_fwd<T, 1, false, MODE>, p, 0, st);
+        else if (p.regs == 2) launch_norm(group_norm_planes_fwd<T, 2, false, MODE>, p, 0, st);
+        else if (p.regs == 4) launch_norm(group_norm_planes_fwd<T, 4, false, MODE>, p, 0, st);
+        else launch_norm(group_norm_planes_fwd<T, 8, false, MODE>, p, 0, st);
+        return;
+    }
+    const size_t lds = MODE == kApply ? 0 : p.lds;
+    if constexpr (MODE != kWhole) launch_norm(group_norm_last_fwd<T, kSplitRun, MODE>, p, lds, st);
+    else if (p.regs <= 4) launch_norm(group_norm_last_fwd<T, 4, MODE>, p, lds, st);
+    else if (p.regs == 8) launch_norm(group_norm_last_fwd<T, 8, MODE>, p, lds, st);
+    else launch_norm(group_norm_last_fwd<T, 16, MODE>, p, lds, st);
+}
+
+template <typename T, int MODE>
+void launch_norm_bwd(const NormPlan &p, hipStream_t st)
+{
+    const size_t lds = MODE == kApply ? 0 : p.lds;
+    if (p.planes) {
+        if constexpr (MODE != kWhole) launch_norm(group_norm_planes_bwd<T, kSplitRun, false, MODE>, p, lds, st);
+        else if (p.solo && p.regs == 1) launch_norm(group_norm_planes_bwd<T, 1, true, MODE>, p, lds, st);
+        else if (p.solo && p.regs == 2) launch_norm(group_norm_planes_bwd<T, 2, true, MODE>, p, lds, st);
+        else if (p.solo) launch_norm(group_norm_planes_bwd<T, 4, true, MODE>, p, lds, st);
+        else if (p.regs == 1) launch_norm(group_norm_planes_bwd<T, 1, false, MODE>, p, lds, st);
+        else if (p.regs == 2) launch_norm(group_norm_planes_bwd<T, 2, false, MODE>, p, lds, st);
+        else if (p.regs == 4) launch_norm(group_norm_planes_bwd<T, 4, false, MODE>, p, lds, st);
+        else launch_norm(group_norm_planes_bwd<T, 8, false, MODE>, p, lds, st);
+        return;
+    }
+    if constexpr (MODE != kWhole) launch_norm(group_norm_last_bwd<T, kSplitRun, MODE>, p, lds, st);
+    else if (p.regs <= 4) launch_norm(group_norm_last_bwd<T, 4, MODE>, p, lds, st);
+    else launch_norm(group_norm_last_bwd<T, 8, MODE>, p, lds, st);
+}
+
+template <typename T>
+int run_norm_fwd(NormPlan &p, hipStream_t st)
+{
+    if (p.wide) {
+        launch_norm(group_norm_wide_fwd<T>, p, 0, st);
+    } else if (!p.split) {
+        launch_norm_fwd<T, kWhole>(p, st);
+    } else {
+        launch_norm_fwd<T, kSums>(p, st);
+        const int total = p.a.N * p.a.groups;
+        float *mean = p.a.group_sums, *rstd = mean + total;
+        hipLaunchKernelGGL(group_norm_join_stats, dim3((total + 3) / 4), dim3(256), 0, st, p.a.part, p.a.tiles, total,
+                           p.a.inv_m, p.a.eps, mean, rstd, p.a.mean, p.a.rstd);
+        p.a.mean = mean;
+        p.a.rstd = rstd;
+        launch_norm_fwd<T, kApply>(p, st);
+    }
     return check_launch();
 }
 
 template <typename T>
-int run_norm_bwd(const NormArgs &a, hipStream_t st)
+int run_norm_bwd(NormPlan &p, hipStream_t st)
 {
-    if (a.N > 0) {
-        hipLaunchKernelGGL(group_norm_bwd_sums<T>, dim3(a.N * a.C), dim3(256), 0, st, a);
-        hipLaunchKernelGGL(group_norm_bwd_kernel<T>, dim3(a.N * a.groups), dim3(256), 0, st, a);
-        const int rc = check_launch();
-        if (rc != kStatusOk) return rc;
+    if (p.a.N > 0) {
+        if (p.wide) {
+            launch_norm(group_norm_wide_bwd<T>, p, 0, st);
+        } else if (!p.split) {
+            launch_norm_bwd<T, kWhole>(p, st);
+        } else {
+            launch_norm_bwd<T, kSums>(p, st);
+            hipLaunchKernelGGL(group_norm_join_groups, dim3((p.a.N * p.a.groups + 3) / 4), dim3(256), 0, st, p.a);
+            launch_norm_bwd<T, kApply>(p, st);
+        }
     }
-    if (!a.dgamma && !a.dbeta) return kStatusOk;
-    hipLaunchKernelGGL(group_norm_bwd_finish, dim3((a.C + 63) / 64), dim3(64), 0, st, a);
+    if (p.a.dgamma || p.a.dbeta)
+        hipLaunchKernelGGL(group_norm_join_channels, dim3((p.a.C + 31) / 32), dim3(1024), 0, st, p.a);
     return check_launch();
 }
 
@@ -138,7 +372,8 @@ extern "C" {
 
 size_t group_norm_act_workspace_bytes(int op, int N, int C, int S, int groups, int layout, int dtype)
 {
-    return norm_workspace(op, N, C, S, groups, layout, dtype);
+    NormPlan p;
+    return plan_norm(p, op, N, C, S, groups, layout, dtype) == kStatusOk ? p.total : 0;
 }
 
 int group_norm_act_fwd(const void *x, const void *gamma, const void *beta, void *y, void *mean, void *rstd, int N, int C,
@@ -147,14 +382,15 @@ int group_norm_act_fwd(const void *x, const void *gamma, const void *beta, void 
 {
     if ((N != 0 && (!x || !y || x == y)) || !(eps > 0.f) || !isfinite(eps)) return kErrInvalidArg;
     NormArgs a = {};
-    a.x = x; a.out = y; a.eps = eps;
+    a.x = x; a.out = y; a.eps = eps; a.act = act;
     a.gamma = static_cast<const float *>(gamma); a.beta = static_cast<const float *>(beta);
     a.mean = static_cast<float *>(mean); a.rstd = static_cast<float *>(rstd);
-    const int rc = norm_common(a, CONV_OP_FWD, N, C, S, groups, act, layout, dtype, ws, ws_bytes);
+    NormPlan p;
+    const int rc = norm_common(p, a, CONV_OP_FWD, N, C, S, groups, layout, dtype, ws, ws_bytes);
     if (rc != kStatusOk) return rc;
     if (N == 0) return kStatusOk;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    return glue_elem_bytes(dtype) == 4 ? run_norm_fwd<float>(a, st) : run_norm_fwd<unsigned short>(a, st);
+    return glue_elem_bytes(dtype) == 4 ? run_norm_fwd<float>(p, st) : run_norm_fwd<unsigned short>(p, st);
 }
 
 int group_norm_act_bwd(const void *x, const void *dy, const void *gamma, const void *beta, const void *mean,
@@ -163,14 +399,15 @@ int group_norm_act_bwd(const void *x, const void *dy, const void *gamma, const v
 {
     if (N != 0 && (!x || !dy || !mean || !rstd || !dx || x == dx || dy == dx)) return kErrInvalidArg;
     NormArgs a = {};
-    a.x = x; a.dy = dy; a.out = dx;
+    a.x = x; a.dy = dy; a.out = dx; a.act = act;
     a.gamma = static_cast<const float *>(gamma); a.beta = static_cast<const float *>(beta);
     a.mean = static_cast<float *>(const_cast<void *>(mean)); a.rstd = static_cast<float *>(const_cast<void *>(rstd));
     a.dgamma = static_cast<float *>(dgamma); a.dbeta = static_cast<float *>(dbeta);
-    const int rc = norm_common(a, CONV_OP_BWD_DATA, N, C, S, groups, act, layout, dtype, ws, ws_bytes);
+    NormPlan p;
+    const int rc = norm_common(p, a, CONV_OP_BWD_DATA, N, C, S, groups, layout, dtype, ws, ws_bytes);
     if (rc != kStatusOk) return rc;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    return glue_elem_bytes(dtype) == 4 ? run_norm_bwd<float>(a, st) : run_norm_bwd<unsigned short>(a, st);
+    return glue_elem_bytes(dtype) == 4 ? run_norm_bwd<float>(p, st) : run_norm_bwd<unsigned short>(p, st);
 }
 
 size_t distill_loss_workspace_bytes(int N, int V, int K, int dtype)

@@ -138,7 +138,8 @@ SHAPES = [
     (2, 12, 2, 2, 4), (1, 7, 5, 1, 7), (2, 10, 1, 7, 5), (3, 24, 3, 3, 8), (2, 48, 4, 4, 3), (2, 40, 1, 17, 4), (1, 200, 6, 6, 2),
     (2, 6, 15, 17, 2), (2, 6, 16, 16, 2), (2, 6, 1, 257, 2), (3, 384, 13, 13, 32), (2, 256, 27, 27, 32),
     (2, 96, 55, 55, 32), (1, 33, 31, 45, 3), (2, 72, 31, 45, 8), (1, 62, 19, 23, 31), (1, 16, 64, 64, 1), (1, 5, 120, 130, 1),
-    (1, 64, 112, 113, 2), (2, 2, 224, 224, 1), (1, 1, 401, 399, 1),
+    (1, 64, 112, 113, 2), (2, 2, 224, 224, 1), (1, 1, 401, 399, 1), (2, 9001, 1, 2, 1), (1, 4100, 3, 3, 1), (2, 16500, 1, 1, 2),
+    (3, 3, 20, 30, 1), (2, 3, 200, 300, 3),
 ]
 
 

@@ -415,7 +415,7 @@ size_t group_norm_act_workspace_bytes(int op, int N, int C, int S, int groups, i
  * once); top_dtype: the same of top_val; index_bytes: 4 or 8, size of the signed integers in
  * labels and top_idx.  All arithmetic is fp32; results do not depend on the order of work.
  * Pointers aligned to their elements; rows may start anywhere.  dz [N][V], rows dz_stride apart,
- * may be z itself (same stride), and may not overlap it otherwise.  K <= CONV_DISTILL_MAX_TOP.
+ * may be z itself (same stride), and may not overlap it otherwise.  K <= CONV_DISTILL_MAX_TOP, V <= 2^30.
  * N = 0 is a no-op (pointers may be NULL).  Scratch: distill_loss_workspace_bytes bytes (fwd and fwd_bwd), 256-byte aligned.
  */
 #define CONV_DISTILL_MAX_TOP 1024

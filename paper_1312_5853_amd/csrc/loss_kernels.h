@@ -1,10 +1,19 @@
 // Loss of a row of logits against a label and a teacher's top logits, and its gradient.
-// Part of train_ops.hip: included there, inside its anonymous namespace.
+// Part of train_ops.hip: included there, inside its anonymous namespace, after vectors.h.
 //
 //   m = max z, sT = sum exp((z - m) / T), s1 = sum exp(z - m); p = softmax(t / T) over the row's entries
 //   loss = wk T^2 sum_k p_k (log p_k - (z_k - m) / T + log sT) + wl (log s1 - (z_label - m))
 //   dz = g [wk T (exp((z - m) / T) / sT - p scattered) + wl (exp(z - m) / s1 - onehot)]
-// A row's maximum is taken off before the division by T, so no finite logit overflows.
+// A row's maximum is taken off before the division by T, so no finite logit overflows.  exp(v) is taken as 2^(v log2 e).
+//
+// Bound by memory: z is read and dz written, once; two exponentials to a value and sum, and two more for the gradient, fit
+// beside that.  A row stays in the registers of a wave (SOLO) or a work-group between the reads and the result.  Rows that
+// do not fit, and rows too few to fill the card, are cut into parts: one launch leaves each part's m, sT and s1, another
+// joins them and writes the gradient, reading z again.
+//
+// The classes that a target names are written twice: the softmax's share with all the others, then, after a barrier, the
+// whole value by the first entry that names the class, which adds up the entries that name it too.  So no atomics, and an
+// order that does not change.
 
 struct LossArgs {
     const void *z;
@@ -14,8 +23,12 @@ struct LossArgs {
     float *loss, *stats;
     const float *row_stats;          // backward: what the forward call left
     const float *grad;
+    float *part, *named;             // parts: {m, sT, s1}; the logits that the row's targets name (K, then the label's)
     float grad_scale, T, inv_T, wk, wl;
+    float to_2T, to_21;              // log2 e / T, log2 e
     int N, V, K, wide_index, top_bf16;
+    int run, parts, part_chunks, chunks;      // vectors of 64 lanes: of a wave, (parts to a row), of a part, of a row
+    FastDiv div_parts;
 };
 
 // index i of an array of 4- or 8-byte integers; -1 where it names no class
@@ -31,107 +44,466 @@ __device__ __forceinline__ float teacher_logit(const LossArgs &a, int64_t i)
                       : ld_elem(static_cast<const float *>(a.top_val), i);
 }
 
-__device__ __forceinline__ float block_max(float v, float *red)
+__device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// ---------------------------------------------------------------------------
+// A row's vectors
+// ---------------------------------------------------------------------------
+// The last vector is moved back so that it ends where the row ends: its first k0 values are the vector's before it too.
+// Lanes past the end hold that vector with no value of their own (k0 = V).
+struct RowLane { int off, k0, k1; };
+
+template <int V>
+__device__ __forceinline__ RowLane row_lane(int width, int chunk, int lane)
 {
-    __syncthreads();
-    v = wave_max(v);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    RowLane l;
+    const int pos = (chunk * 64 + lane) * V;
+    if (width >= V) {
+        l.off = min(pos, width - V);
+        l.k0 = min(pos - l.off, V);
+        l.k1 = V;
+    } else {
+        l.off = 0;
+        l.k0 = 0;
+        l.k1 = pos == 0 ? width : 0;
+    }
+    return l;
 }
 
-// One work-group per row.  GRAD: dz too; the row's statistics are taken from the row, or from row_stats where given.
-template <typename T, bool GRAD>
-__global__ __launch_bounds__(256) void distill_rows_kernel(LossArgs a)
+template <typename T>
+__device__ __forceinline__ typename Vec<T>::Raw row_load(const T *z, int width, const RowLane &l)
 {
-    __shared__ float red[256];
-    __shared__ int idx[CONV_DISTILL_MAX_TOP];
-    __shared__ float prob[CONV_DISTILL_MAX_TOP], zk[CONV_DISTILL_MAX_TOP];
-    const int n = blockIdx.x, tid = threadIdx.x;
+    return width >= Vec<T>::V ? Vec<T>::load(z + l.off) : Vec<T>::some(z, width);
+}
+
+// Of a row in parts, the values before the moved-back vector may be another work-group's: they are left to it.
+template <typename T>
+__device__ __forceinline__ void row_store(const LossArgs &a, T *dz, const RowLane &l, const float (&v)[Vec<T>::V])
+{
+    if (a.V >= Vec<T>::V && (l.k0 == 0 || a.parts == 1)) {
+        if (l.k0 < Vec<T>::V) Vec<T>::store(dz + l.off, v);
+    } else {
+#pragma unroll
+        for (int k = 0; k < Vec<T>::V; ++k)
+            if (k >= l.k0 && k < l.k1) st_elem(dz, l.off + k, v[k]);
+    }
+}
+
+// the maximum of a lane's vectors (values that two vectors hold do no harm)
+template <typename T, int R>
+__device__ __forceinline__ float row_max(const typename Vec<T>::Raw (&raw)[R], int n, int width)
+{
+    constexpr int V = Vec<T>::V;
+    float m = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (r < n) {
+            float v[V];
+            Vec<T>::open(raw[r], v);
+#pragma unroll
+            for (int k = 0; k < V; ++k) m = fmaxf(m, width >= V || k < width ? v[k] : -INFINITY);
+        }
+    return m;
+}
+
+template <typename T, int R, bool TEMP, bool ONE>
+__device__ __forceinline__ void row_sums(const LossArgs &a, const typename Vec<T>::Raw (&raw)[R], int c0, int n, int lane, float m,
+                                         float &sT, float &s1)
+{
+    constexpr int V = Vec<T>::V;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (r < n) {
+            const RowLane l = row_lane<V>(a.V, c0 + r, lane);
+            float v[V];
+            Vec<T>::open(raw[r], v);
+            if (l.k0 == 0 && l.k1 == V) {
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const float d = v[k] - m;
+                    if (TEMP) sT += exp2_of(d * a.to_2T);
+                    if (ONE) s1 += exp2_of(d * a.to_21);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const float d = v[k] - m;
+                    const bool in = k >= l.k0 && k < l.k1;
+                    if (TEMP) sT += in ? exp2_of(d * a.to_2T) : 0.f;
+                    if (ONE) s1 += in ? exp2_of(d * a.to_21) : 0.f;
+                }
+            }
+        }
+}
+
+// dz without the targets: ck exp((z - m) / T) + cl exp(z - m)
+template <typename T, int R, bool TEMP, bool ONE>
+__device__ __forceinline__ void row_write(const LossArgs &a, const typename Vec<T>::Raw (&raw)[R], T *dz, int c0, int n, int lane,
+                                          float m, float ck, float cl)
+{
+    constexpr int V = Vec<T>::V;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (r < n) {
+            const RowLane l = row_lane<V>(a.V, c0 + r, lane);
+            float v[V];
+            Vec<T>::open(raw[r], v);
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const float d = v[k] - m;
+                float g = 0.f;
+                if (TEMP) g = exp2_of(d * a.to_2T) * ck;
+                if (ONE) g += exp2_of(d * a.to_21) * cl;
+                v[k] = g;
+            }
+            row_store(a, dz, l, v);
+        }
+}
+
+template <typename T, int R>
+__device__ __forceinline__ void row_gradient(const LossArgs &a, const typename Vec<T>::Raw (&raw)[R], T *dz, int c0, int n, int lane,
+                                             float m, float ck, float cl, bool temp, bool one)
+{
+    if (temp && one) row_write<T, R, true, true>(a, raw, dz, c0, n, lane, m, ck, cl);
+    else if (temp) row_write<T, R, true, false>(a, raw, dz, c0, n, lane, m, ck, cl);
+    else row_write<T, R, false, true>(a, raw, dz, c0, n, lane, m, ck, cl);
+}
+
+template <typename T, int R>
+__device__ __forceinline__ void row_clear(const LossArgs &a, T *dz, int c0, int n, int lane)
+{
+    constexpr int V = Vec<T>::V;
+    const float zero[V] = {};
+    for (int r = 0; r < n; ++r) row_store(a, dz, row_lane<V>(a.V, c0 + r, lane), zero);
+}
+
+// ---------------------------------------------------------------------------
+// The threads that work on a row: a wave (its LDS to itself, no barrier), or a work-group
+// ---------------------------------------------------------------------------
+template <bool SOLO>
+struct RowTeam {
+    int lane, wave, waves, id, size;
+    __device__ __forceinline__ RowTeam()
+    {
+        lane = threadIdx.x & 63;
+        wave = SOLO ? 0 : uniform((int)(threadIdx.x >> 6));
+        waves = SOLO ? 1 : (int)(blockDim.x >> 6);
+        id = SOLO ? lane : (int)threadIdx.x;
+        size = waves * 64;
+    }
+    // what a lane has written to LDS or memory is there for the others of the team afterwards
+    __device__ __forceinline__ void sync() const
+    {
+        if (SOLO) {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        } else {
+            __syncthreads();
+        }
+    }
+    // `red`: one float per wave, used by one call between two barriers; a barrier is in the call
+    template <int COUNT>
+    __device__ __forceinline__ void max_of(float (&v)[COUNT], float (*red)[16]) const
+    {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) v[i] = wave_max(v[i]);
+        if (SOLO) return;
+        if (lane == 0)
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) red[i][wave] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            v[i] = red[i][0];
+            for (int w = 1; w < waves; ++w) v[i] = fmaxf(v[i], red[i][w]);
+        }
+    }
+    template <int COUNT>
+    __device__ __forceinline__ void sum_of(float (&v)[COUNT], float (*red)[16]) const
+    {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) v[i] = wave_sum(v[i]);
+        if (SOLO) return;
+        if (lane == 0)
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) red[i][wave] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) {
+            v[i] = red[i][0];
+            for (int w = 1; w < waves; ++w) v[i] += red[i][w];
+        }
+    }
+};
+
+// The row's entries in LDS: classes, probabilities (up to 1 / sum), logits of the student there.
+struct Entries { int *idx; float *prob, *zk; };
+
+__device__ __forceinline__ Entries entries_at(float *lds, int K)
+{
+    return {reinterpret_cast<int *>(lds), lds + K, lds + 2 * K};
+}
+
+// Reads a thread's share of the entries; has: whether one names a class; returns the largest of the teacher's logits.
+// zk: the student's logit where the class lies in [lo, hi).
+template <typename T, bool SOLO>
+__device__ __forceinline__ float read_entries(const LossArgs &a, const RowTeam<SOLO> &team, const Entries &e, const T *z, int n, int lo,
+                                              int hi, float &has)
+{
+    float tm = -INFINITY;
+    has = 0.f;
+    for (int k = team.id; k < a.K; k += team.size) {
+        const int64_t i = (int64_t)n * a.K + k;
+        const int v = class_at(a.top_idx, i, a.wide_index, a.V);
+        const float t = teacher_logit(a, i);
+        e.idx[k] = v;
+        e.prob[k] = v >= 0 ? t : -INFINITY;
+        e.zk[k] = v >= lo && v < hi ? ld_elem(z, v) : 0.f;
+        if (v >= 0) {
+            has = 1.f;
+            tm = fmaxf(tm, t);
+        }
+    }
+    return tm;
+}
+
+// exp((t - tm) / T) of a thread's share, into prob; returns their sum
+template <bool SOLO>
+__device__ __forceinline__ float weigh_entries(const LossArgs &a, const RowTeam<SOLO> &team, const Entries &e, float tm)
+{
+    float ts = 0.f;
+    for (int k = team.id; k < a.K; k += team.size) {
+        const float p = e.idx[k] >= 0 ? exp2_of((e.prob[k] - tm) * a.to_2T) : 0.f;
+        e.prob[k] = p;
+        ts += p;
+    }
+    return ts;
+}
+
+// sum_k p_k (log p_k - log q_k) over a thread's share; zk from `named` where given
+template <bool SOLO>
+__device__ __forceinline__ float divergence(const LossArgs &a, const RowTeam<SOLO> &team, const Entries &e, const float *named,
+                                            float inv_ts, float m, float sT)
+{
+    float kd = 0.f;
+    const float log_sT = logf(sT);
+    for (int k = team.id; k < a.K; k += team.size) {
+        const float p = e.prob[k] * inv_ts;
+        if (e.idx[k] >= 0 && !(p <= 0.f)) kd += p * (logf(p) - (((named ? named[k] : e.zk[k]) - m) * a.inv_T - log_sT));
+    }
+    return kd;
+}
+
+// the classes in [lo, hi) that the targets name, whole
+template <typename T, bool SOLO>
+__device__ __forceinline__ void write_named(const LossArgs &a, const RowTeam<SOLO> &team, const Entries &e, T *dz, int label, float zl,
+                                            int lo, int hi, float m, float ck, float cl, float share, float gl)
+{
+    for (int k = team.id; k <= a.K; k += team.size) {
+        const int v = k < a.K ? e.idx[k] : label;
+        if (v < lo || v >= hi) continue;
+        float p = 0.f;
+        bool first = true;
+        for (int j = 0; j < a.K; ++j)
+            if (e.idx[j] == v) {
+                p += e.prob[j];
+                if (j < k) first = false;
+            }
+        if (!first) continue;
+        const float d = (k < a.K ? e.zk[k] : zl) - m;
+        float g = 0.f;
+        if (share != 0.f) g = exp2_of(d * a.to_2T) * ck - share * p;
+        if (gl != 0.f) g += exp2_of(d * a.to_21) * cl - (v == label ? gl : 0.f);
+        st_elem(dz, v, g);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Whole rows: loss (and statistics), and with GRAD the gradient
+// ---------------------------------------------------------------------------
+template <typename T, int R, bool SOLO, bool GRAD>
+__global__ __launch_bounds__(SOLO ? 256 : 1024) void distill_rows(LossArgs a)
+{
+    extern __shared__ float lds[];
+    __shared__ float red[7][16];
+    const RowTeam<SOLO> team;
+    const int n = SOLO ? uniform((int)(blockIdx.x * 4 + (threadIdx.x >> 6))) : (int)blockIdx.x;
+    if (SOLO && n >= a.N) return;
     const T *z = static_cast<const T *>(a.z) + n * a.z_stride;
     T *dz = static_cast<T *>(a.dz) + n * a.dz_stride;
+    const int c0 = team.wave * a.run, cn = min(a.run, a.chunks - c0);
+    typename Vec<T>::Raw raw[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (r < cn) raw[r] = row_load(z, a.V, row_lane<Vec<T>::V>(a.V, c0 + r, team.lane));
     const int label = a.labels ? class_at(a.labels, n, a.wide_index, a.V) : -1;
-    // the teacher's softmax over the entries that name a class
-    float tm = -INFINITY, has = 0.f;
-    for (int k = tid; k < a.K; k += 256) {
-        const int64_t e = (int64_t)n * a.K + k;
-        const int v = class_at(a.top_idx, e, a.wide_index, a.V);
-        idx[k] = v;
-        zk[k] = v >= 0 ? ld_elem(z, v) : 0.f;
-        prob[k] = v >= 0 ? teacher_logit(a, e) : -INFINITY;
-        if (v >= 0) { has = 1.f; tm = fmaxf(tm, prob[k]); }
-    }
-    has = block_max(has, red);
-    tm = block_max(tm, red);
     const float zl = label >= 0 ? ld_elem(z, label) : 0.f;
-    if (has == 0.f && label < 0) {                       // nothing to learn from: the logits are not looked at
-        if (a.loss && tid == 0) a.loss[n] = 0.f;
-        if (a.stats && tid < 3) a.stats[(int64_t)n * 3 + tid] = 0.f;
-        if (GRAD)
-            for (int v = tid; v < a.V; v += 256) st_elem(dz, v, 0.f);
+    const Entries e = entries_at(lds + (SOLO ? (int)(threadIdx.x >> 6) * 3 * a.K : 0), a.K);
+    float most[3];
+    most[1] = read_entries(a, team, e, z, n, 0, a.V, most[2]);
+    most[0] = row_max<T, R>(raw, cn, a.V);
+    team.max_of(most, red);
+    const float m = most[0], tm = most[1];
+    const bool has = most[2] > 0.f;
+    if (!has && label < 0) {                              // nothing to learn from, whatever the logits are
+        if (team.id == 0) a.loss[n] = 0.f;
+        if (a.stats && team.id < 3) a.stats[(int64_t)n * 3 + team.id] = 0.f;
+        if (GRAD) row_clear<T, R>(a, dz, c0, cn, team.lane);
         return;
     }
-    float ts = 0.f;
-    for (int k = tid; k < a.K; k += 256) {
-        prob[k] = idx[k] >= 0 ? expf((prob[k] - tm) * a.inv_T) : 0.f;
-        ts += prob[k];
+    float sums[3] = {0.f, 0.f, 0.f};
+    sums[2] = weigh_entries(a, team, e, tm);
+    // statistics are asked for whole; without them a term without target needs no sum
+    const bool temp = a.K > 0 && (has || a.stats), one = label >= 0 || a.stats;
+    if (temp && one) row_sums<T, R, true, true>(a, raw, c0, cn, team.lane, m, sums[0], sums[1]);
+    else if (temp) row_sums<T, R, true, false>(a, raw, c0, cn, team.lane, m, sums[0], sums[1]);
+    else row_sums<T, R, false, true>(a, raw, c0, cn, team.lane, m, sums[0], sums[1]);
+    team.sum_of(sums, red + 3);
+    const float s1 = sums[1], sT = a.K ? sums[0] : s1, inv_ts = has ? 1.f / sums[2] : 0.f;
+    if (a.stats && team.id == 0) {
+        a.stats[(int64_t)n * 3] = m;
+        a.stats[(int64_t)n * 3 + 1] = sT;
+        a.stats[(int64_t)n * 3 + 2] = s1;
     }
-    ts = block_sum(ts, red);
-    for (int k = tid; k < a.K; k += 256) prob[k] = idx[k] >= 0 ? prob[k] / ts : 0.f;
+    float gk = 0.f, gl = 0.f, ck = 0.f, cl = 0.f;
+    if (GRAD) {
+        const float g = a.grad_scale * (a.grad ? a.grad[n] : 1.f);
+        if (has) { gk = g * a.wk * a.T; ck = gk / sT; }
+        if (label >= 0) { gl = g * a.wl; cl = gl / s1; }
+        row_gradient<T, R>(a, raw, dz, c0, cn, team.lane, m, ck, cl, has, label >= 0);
+    }
+    float kd[1] = {has ? divergence(a, team, e, nullptr, inv_ts, m, sT) : 0.f};
+    team.sum_of(kd, red + 6);
+    if (team.id == 0)
+        a.loss[n] = (has ? a.wk * a.T * a.T * kd[0] : 0.f) + (label >= 0 ? a.wl * (logf(s1) - (zl - m)) : 0.f);
+    if (GRAD) {
+        team.sync();
+        write_named(a, team, e, dz, label, zl, 0, a.V, m, ck, cl, gk * inv_ts, gl);
+    }
+}
 
+// ---------------------------------------------------------------------------
+// Parts of rows
+// ---------------------------------------------------------------------------
+// m, sT and s1 of a part; the first part's work-group also puts aside the logits that the targets name, as the gradient
+// may take their place.
+template <typename T, int R>
+__global__ __launch_bounds__(512) void distill_part_sums(LossArgs a)
+{
+    __shared__ float red[3][16];
+    const RowTeam<false> team;
+    const int n = fastdiv(blockIdx.x, a.div_parts), part = blockIdx.x - n * a.parts;
+    const T *z = static_cast<const T *>(a.z) + n * a.z_stride;
+    const int first = part * a.part_chunks, last = min(first + a.part_chunks, a.chunks);
+    const int c0 = first + team.wave * a.run, cn = min(a.run, last - c0);
+    typename Vec<T>::Raw raw[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (r < cn) raw[r] = row_load(z, a.V, row_lane<Vec<T>::V>(a.V, c0 + r, team.lane));
+    if (part == 0) {
+        float *named = a.named + (int64_t)n * (a.K + 1);
+        for (int k = team.id; k <= a.K; k += team.size) {
+            const int v = k < a.K ? class_at(a.top_idx, (int64_t)n * a.K + k, a.wide_index, a.V)
+                                  : a.labels ? class_at(a.labels, n, a.wide_index, a.V) : -1;
+            named[k] = v >= 0 ? ld_elem(z, v) : 0.f;
+        }
+    }
+    float m[1] = {row_max<T, R>(raw, cn, a.V)};
+    team.max_of(m, red);
+    float s[2] = {0.f, 0.f};
+    // of a part without any class left the sums are 0
+    const float top = m[0] == -INFINITY ? 0.f : m[0];
+    if (a.K) row_sums<T, R, true, true>(a, raw, c0, cn, team.lane, top, s[0], s[1]);
+    else row_sums<T, R, false, true>(a, raw, c0, cn, team.lane, top, s[0], s[1]);
+    team.sum_of(s, red + 1);
+    if (team.id == 0) {
+        float *p = a.part + (int64_t)blockIdx.x * 3;
+        p[0] = m[0];
+        p[1] = s[0];
+        p[2] = s[1];
+    }
+}
+
+// Joins the parts (or takes the statistics given).  GRAD: a work-group writes its part's gradient, and the first part's
+// also the row's loss where asked for; otherwise one work-group per row writes the loss.
+template <typename T, int R, bool GRAD>
+__global__ __launch_bounds__(512) void distill_part_apply(LossArgs a)
+{
+    constexpr int V = Vec<T>::V;
+    extern __shared__ float lds[];
+    __shared__ float red[4][16];
+    const RowTeam<false> team;
+    const int n = GRAD ? fastdiv(blockIdx.x, a.div_parts) : (int)blockIdx.x, part = GRAD ? blockIdx.x - n * a.parts : 0;
+    const T *z = static_cast<const T *>(a.z) + n * a.z_stride;
+    T *dz = static_cast<T *>(a.dz) + n * a.dz_stride;
+    const int first = part * a.part_chunks, last = min(first + a.part_chunks, a.chunks);
+    const int c0 = first + team.wave * a.run, cn = min(a.run, last - c0);
+    typename Vec<T>::Raw raw[R];
+    if (GRAD)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (r < cn) raw[r] = row_load(z, a.V, row_lane<V>(a.V, c0 + r, team.lane));
+    // classes [lo, hi) are this work-group's to write
+    const int lo = first * 64 * V, hi = (int)min((int64_t)last * 64 * V, (int64_t)a.V);
+    const int label = a.labels ? class_at(a.labels, n, a.wide_index, a.V) : -1;
+    const float zl = GRAD && label >= lo && label < hi ? ld_elem(z, label) : 0.f;
+    const Entries e = entries_at(lds, a.K);
+    float most[2];
+    most[0] = read_entries(a, team, e, z, n, GRAD ? lo : 0, GRAD ? hi : 0, most[1]);
+    team.max_of(most, red);
+    const bool has = most[1] > 0.f;
+    const bool lead = part == 0 && a.loss;
+    if (!has && label < 0) {
+        if (lead && team.id == 0) a.loss[n] = 0.f;
+        if (lead && a.stats && team.id < 3) a.stats[(int64_t)n * 3 + team.id] = 0.f;
+        if (GRAD) row_clear<T, R>(a, dz, c0, cn, team.lane);
+        return;
+    }
     float m, sT, s1;
     if (a.row_stats) {
         m = a.row_stats[(int64_t)n * 3];
         sT = a.row_stats[(int64_t)n * 3 + 1];
         s1 = a.row_stats[(int64_t)n * 3 + 2];
     } else {
+        const float *p = a.part + (int64_t)n * a.parts * 3;
         m = -INFINITY;
-        for (int v = tid; v < a.V; v += 256) m = fmaxf(m, ld_elem(z, v));
-        m = block_max(m, red);
+        for (int i = team.lane; i < a.parts; i += 64) m = fmaxf(m, p[3 * i]);
+        m = wave_max(m);
         sT = s1 = 0.f;
-        for (int v = tid; v < a.V; v += 256) {
-            const float d = ld_elem(z, v) - m, e = expf(d);
-            s1 += e;
-            sT += a.K ? expf(d * a.inv_T) : e;
+        for (int i = team.lane; i < a.parts; i += 64) {
+            const float d = p[3 * i] - m;
+            sT += p[3 * i + 1] * exp2_of(d * a.to_2T);
+            s1 += p[3 * i + 2] * exp2_of(d * a.to_21);
         }
-        sT = block_sum(sT, red);
-        s1 = block_sum(s1, red);
+        sT = wave_sum(sT);
+        s1 = wave_sum(s1);
+        if (!a.K) sT = s1;
     }
-    if (a.stats && tid == 0) {
-        a.stats[(int64_t)n * 3] = m;
-        a.stats[(int64_t)n * 3 + 1] = sT;
-        a.stats[(int64_t)n * 3 + 2] = s1;
-    }
-    if (a.loss) {
-        const float lT = logf(sT);
-        float kd = 0.f;
-        __syncthreads();
-        for (int k = tid; k < a.K; k += 256)
-            if (idx[k] >= 0 && !(prob[k] <= 0.f)) kd += prob[k] * (logf(prob[k]) - ((zk[k] - m) * a.inv_T - lT));
-        kd = block_sum(kd, red);
-        if (tid == 0)
-            a.loss[n] = (has > 0.f ? a.wk * a.T * a.T * kd : 0.f) + (label >= 0 ? a.wl * (logf(s1) - (zl - m)) : 0.f);
-    }
+    float ts[1] = {weigh_entries(a, team, e, most[0])};
+    team.sum_of(ts, red + 2);
+    const float inv_ts = has ? 1.f / ts[0] : 0.f;
+    float gk = 0.f, gl = 0.f, ck = 0.f, cl = 0.f;
     if (GRAD) {
         const float g = a.grad_scale * (a.grad ? a.grad[n] : 1.f);
-        const float gk = has > 0.f ? g * a.wk * a.T : 0.f, gl = label >= 0 ? g * a.wl : 0.f;
-        const float ck = gk / sT, cl = gl / s1;
-        auto soft = [&](float d) { return (gk != 0.f ? expf(d * a.inv_T) * ck : 0.f) + (gl != 0.f ? expf(d) * cl : 0.f); };
-        for (int v = tid; v < a.V; v += 256) st_elem(dz, v, soft(ld_elem(z, v) - m));
-        __syncthreads();
-        // classes with a target are written again; the first entry that names a class writes it
-        for (int k = tid; k <= a.K; k += 256) {
-            const int v = k < a.K ? idx[k] : label;
-            if (v < 0) continue;
-            float p = 0.f;
-            bool first = true;
-            for (int j = 0; j < a.K; ++j)
-                if (idx[j] == v) {
-                    p += prob[j];
-                    if (j < k) first = false;
-                }
-            if (!first) continue;
-            st_elem(dz, v, soft((k < a.K ? zk[k] : zl) - m) - gk * p - (v == label ? gl : 0.f));
+        if (has) { gk = g * a.wk * a.T; ck = gk / sT; }
+        if (label >= 0) { gl = g * a.wl; cl = gl / s1; }
+        row_gradient<T, R>(a, raw, dz, c0, cn, team.lane, m, ck, cl, has, label >= 0);
+    }
+    if (lead) {
+        const float *named = a.named + (int64_t)n * (a.K + 1);
+        float kd[1] = {has ? divergence(a, team, e, named, inv_ts, m, sT) : 0.f};
+        team.sum_of(kd, red + 3);
+        if (team.id == 0) {
+            a.loss[n] = (has ? a.wk * a.T * a.T * kd[0] : 0.f) + (label >= 0 ? a.wl * (logf(s1) - (named[a.K] - m)) : 0.f);
+            if (a.stats) {
+                a.stats[(int64_t)n * 3] = m;
+                a.stats[(int64_t)n * 3 + 1] = sT;
+                a.stats[(int64_t)n * 3 + 2] = s1;
+            }
         }
+    }
+    if (GRAD) {
+        team.sync();
+        write_named(a, team, e, dz, label, zl, lo, hi, m, ck, cl, gk * inv_ts, gl);
     }
 }

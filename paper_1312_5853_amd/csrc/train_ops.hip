@@ -320,24 +320,74 @@ int run_norm_bwd(NormPlan &p, hipStream_t st)
 // ---------------------------------------------------------------------------
 // Loss
 // ---------------------------------------------------------------------------
-int loss_checks(int N, int V, int K, int dtype)
+// How a call runs: a wave or a work-group to a row, or several work-groups.
+struct LossPlan {
+    bool solo;
+    int chunks, run, parts, part_chunks, threads, regs;
+    int64_t blocks;
+    size_t part_bytes, total;
+};
+
+constexpr int kPartWaves = 8, kPartRun = 4;
+
+int plan_loss(LossPlan &p, int N, int V, int K, int dtype, bool from_stats)
 {
+    p = {};
     if (N < 0 || V <= 0 || K < 0) return kErrInvalidArg;
-    if (!glue_elem_bytes(dtype)) return kErrBadDtype;
-    if (K > CONV_DISTILL_MAX_TOP) return kErrTooLarge;
-    return kStatusOk;
+    const int eb = glue_elem_bytes(dtype);
+    if (!eb) return kErrBadDtype;
+    if (K > CONV_DISTILL_MAX_TOP || V > (1 << 30)) return kErrTooLarge;
+    const int vec = 16 / eb, nv = (V + vec - 1) / vec;
+    p.chunks = ceil_div(nv, 64);
+    p.parts = 1;
+    if (from_stats) {
+        // nothing to join: parts of a row are work of their own
+        const int per = std::min(p.chunks, kPartWaves * kPartRun);
+        p.run = std::min(kPartRun, p.chunks);
+        p.threads = 64 * ceil_div(per, p.run);
+        p.part_chunks = per;
+        p.parts = ceil_div(p.chunks, per);
+        p.blocks = (int64_t)N * p.parts;
+        return p.blocks < ((int64_t)1 << 31) ? kStatusOk : kErrTooLarge;
+    }
+    p.solo = p.chunks <= 4 && N >= 1024;
+    if (p.solo) {
+        p.run = p.chunks;
+        p.threads = 256;
+        p.blocks = ((int64_t)N + 3) / 4;
+    } else if (p.chunks <= 16 || (p.chunks <= 16 * 8 && N >= 128)) {
+        const int want = N >= 512 ? 4 : 1;
+        p.run = ceil_div(p.chunks, std::min(16, ceil_div(p.chunks, want)));
+        p.threads = 64 * ceil_div(p.chunks, p.run);
+        p.blocks = N;
+    } else {
+        const int most = kPartWaves * kPartRun;
+        p.parts = ceil_div(p.chunks, most);
+        p.part_chunks = ceil_div(p.chunks, p.parts);
+        p.parts = ceil_div(p.chunks, p.part_chunks);
+        p.run = ceil_div(p.part_chunks, kPartWaves);
+        p.threads = 64 * ceil_div(p.part_chunks, p.run);
+        p.blocks = (int64_t)N * p.parts;
+        p.part_bytes = (size_t)round_up64(p.blocks * 3 * 4, 256);
+        p.total = p.part_bytes + (size_t)round_up64((int64_t)N * (K + 1) * 4, 256);
+    }
+    p.regs = std::min(pow2_up(p.run), 8);
+    return p.blocks < ((int64_t)1 << 31) ? kStatusOk : kErrTooLarge;
 }
 
 // a: pointers, strides and scalars of the call are set; the rest is checked and filled in
-int loss_common(LossArgs &a, bool dz, int N, int V, int K, float temperature, int index_bytes, int top_dtype, int dtype)
+int loss_common(LossArgs &a, LossPlan &p, bool dz, int N, int V, int K, float temperature, int index_bytes, int top_dtype,
+                int dtype, void *ws, size_t ws_bytes)
 {
     if (N != 0 && (!a.z || (dz && !a.dz) || (!a.labels && K == 0) || (K > 0 && (!a.top_idx || !a.top_val))))
         return kErrInvalidArg;
     if (a.z_stride < V || (dz && a.dz_stride < V) || (index_bytes != 4 && index_bytes != 8)) return kErrInvalidArg;
-    if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(a.wk) || !isfinite(a.wl) || !isfinite(a.grad_scale))
+    const float log2e = 1.44269504088896340736f;
+    if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(log2e / temperature) || !isfinite(a.wk) ||
+        !isfinite(a.wl) || !isfinite(a.grad_scale))
         return kErrInvalidArg;
     if (N != 0 && dz && a.z == a.dz && a.z_stride != a.dz_stride) return kErrInvalidArg;
-    const int rc = loss_checks(N, V, K, dtype);
+    const int rc = plan_loss(p, N, V, K, dtype, a.row_stats != nullptr);
     if (rc != kStatusOk) return rc;
     const int tb = K ? glue_elem_bytes(top_dtype) : 4;
     if (!tb) return kErrBadDtype;
@@ -346,24 +396,64 @@ int loss_common(LossArgs &a, bool dz, int N, int V, int K, float temperature, in
         !aligned(a.top_val, tb) || !aligned(a.loss, 4) || !aligned(a.stats, 4) || !aligned(a.row_stats, 4) ||
         !aligned(a.grad, 4))
         return kErrMisaligned;
+    if (p.total) {
+        if (!ws || ws_bytes < p.total) return kErrWorkspace;
+        if (!aligned(ws, 256)) return kErrMisaligned;
+    }
     a.N = N; a.V = V; a.K = K;
     a.T = temperature; a.inv_T = 1.f / temperature;
+    a.to_21 = log2e; a.to_2T = log2e / temperature;
     a.wide_index = index_bytes == 8; a.top_bf16 = tb == 2;
     if (a.wk == 0.f) a.K = 0;                            // a term of weight 0 is absent
     if (a.wl == 0.f) a.labels = nullptr;
+    a.chunks = p.chunks; a.run = p.run; a.parts = p.parts; a.part_chunks = p.part_chunks;
+    a.div_parts = make_fastdiv(p.parts);
+    a.part = static_cast<float *>(ws);
+    a.named = reinterpret_cast<float *>(static_cast<char *>(ws) + p.part_bytes);
     return kStatusOk;
 }
 
+template <typename Kern>
+void launch_loss(Kern kern, const LossArgs &a, int64_t blocks, int threads, size_t lds, hipStream_t st)
+{
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(threads), lds, st, a);
+}
+
+template <typename T, bool GRAD>
+int run_loss_typed(const LossArgs &a, const LossPlan &p, hipStream_t st)
+{
+    const size_t lds = (size_t)(p.solo ? 4 : 1) * 3 * a.K * 4;
+    if constexpr (GRAD)
+        if (a.row_stats) {
+            launch_loss(distill_part_apply<T, kPartRun, true>, a, p.blocks, p.threads, lds, st);
+            return check_launch();
+        }
+    if (p.parts > 1) {
+        launch_loss(distill_part_sums<T, kPartRun>, a, p.blocks, p.threads, 0, st);
+        launch_loss(distill_part_apply<T, kPartRun, GRAD>, a, GRAD ? p.blocks : a.N, GRAD ? p.threads : 256, lds, st);
+    } else if (p.solo && p.regs == 1) {
+        launch_loss(distill_rows<T, 1, true, GRAD>, a, p.blocks, p.threads, lds, st);
+    } else if (p.solo && p.regs == 2) {
+        launch_loss(distill_rows<T, 2, true, GRAD>, a, p.blocks, p.threads, lds, st);
+    } else if (p.solo) {
+        launch_loss(distill_rows<T, 4, true, GRAD>, a, p.blocks, p.threads, lds, st);
+    } else if (p.regs == 1) {
+        launch_loss(distill_rows<T, 1, false, GRAD>, a, p.blocks, p.threads, lds, st);
+    } else if (p.regs <= 4) {
+        launch_loss(distill_rows<T, 4, false, GRAD>, a, p.blocks, p.threads, lds, st);
+    } else {
+        launch_loss(distill_rows<T, 8, false, GRAD>, a, p.blocks, p.threads, lds, st);
+    }
+    return check_launch();
+}
+
 template <bool GRAD>
-int run_loss(const LossArgs &a, int dtype, void *stream)
+int run_loss(const LossArgs &a, const LossPlan &p, int dtype, void *stream)
 {
     if (a.N == 0) return kStatusOk;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (glue_elem_bytes(dtype) == 4)
-        hipLaunchKernelGGL((distill_rows_kernel<float, GRAD>), dim3(a.N), dim3(256), 0, st, a);
-    else
-        hipLaunchKernelGGL((distill_rows_kernel<unsigned short, GRAD>), dim3(a.N), dim3(256), 0, st, a);
-    return check_launch();
+    return glue_elem_bytes(dtype) == 4 ? run_loss_typed<float, GRAD>(a, p, st)
+                                       : run_loss_typed<unsigned short, GRAD>(a, p, st);
 }
 
 }  // namespace
@@ -412,8 +502,8 @@ int group_norm_act_bwd(const void *x, const void *dy, const void *gamma, const v
 
 size_t distill_loss_workspace_bytes(int N, int V, int K, int dtype)
 {
-    (void)N; (void)V; (void)K; (void)dtype;
-    return 0;
+    LossPlan p;
+    return plan_loss(p, N, V, K, dtype, false) == kStatusOk ? p.total : 0;
 }
 
 int distill_loss_fwd(const void *z, int64_t z_stride, const void *labels, const void *top_idx, const void *top_val,
@@ -421,14 +511,14 @@ int distill_loss_fwd(const void *z, int64_t z_stride, const void *labels, const 
                      float label_weight, int index_bytes, int top_dtype, int dtype, void *ws, size_t ws_bytes,
                      void *stream)
 {
-    (void)ws; (void)ws_bytes;
     if (N != 0 && !loss) return kErrInvalidArg;
     LossArgs a = {};
     a.z = z; a.z_stride = z_stride; a.labels = labels; a.top_idx = top_idx; a.top_val = top_val;
     a.loss = static_cast<float *>(loss); a.stats = static_cast<float *>(stats);
     a.wk = kd_weight; a.wl = label_weight;
-    const int rc = loss_common(a, false, N, V, K, temperature, index_bytes, top_dtype, dtype);
-    return rc != kStatusOk ? rc : run_loss<false>(a, dtype, stream);
+    LossPlan p;
+    const int rc = loss_common(a, p, false, N, V, K, temperature, index_bytes, top_dtype, dtype, ws, ws_bytes);
+    return rc != kStatusOk ? rc : run_loss<false>(a, p, dtype, stream);
 }
 
 int distill_loss_bwd(const void *z, int64_t z_stride, const void *labels, const void *top_idx, const void *top_val,
@@ -442,8 +532,9 @@ int distill_loss_bwd(const void *z, int64_t z_stride, const void *labels, const 
     a.dz = dz; a.dz_stride = dz_stride; a.row_stats = static_cast<const float *>(stats);
     a.grad = static_cast<const float *>(grad); a.grad_scale = grad_scale;
     a.wk = kd_weight; a.wl = label_weight;
-    const int rc = loss_common(a, true, N, V, K, temperature, index_bytes, top_dtype, dtype);
-    return rc != kStatusOk ? rc : run_loss<true>(a, dtype, stream);
+    LossPlan p;
+    const int rc = loss_common(a, p, true, N, V, K, temperature, index_bytes, top_dtype, dtype, nullptr, 0);
+    return rc != kStatusOk ? rc : run_loss<true>(a, p, dtype, stream);
 }
 
 int distill_loss_fwd_bwd(const void *z, int64_t z_stride, const void *labels, const void *top_idx, const void *top_val,
@@ -451,15 +542,15 @@ int distill_loss_fwd_bwd(const void *z, int64_t z_stride, const void *labels, co
                          int K, float temperature, float kd_weight, float label_weight, int index_bytes, int top_dtype,
                          int dtype, void *ws, size_t ws_bytes, void *stream)
 {
-    (void)ws; (void)ws_bytes;
     if (N != 0 && !loss) return kErrInvalidArg;
     LossArgs a = {};
     a.z = z; a.z_stride = z_stride; a.labels = labels; a.top_idx = top_idx; a.top_val = top_val;
     a.dz = dz; a.dz_stride = dz_stride; a.loss = static_cast<float *>(loss);
     a.grad = static_cast<const float *>(grad); a.grad_scale = grad_scale;
     a.wk = kd_weight; a.wl = label_weight;
-    const int rc = loss_common(a, true, N, V, K, temperature, index_bytes, top_dtype, dtype);
-    return rc != kStatusOk ? rc : run_loss<true>(a, dtype, stream);
+    LossPlan p;
+    const int rc = loss_common(a, p, true, N, V, K, temperature, index_bytes, top_dtype, dtype, ws, ws_bytes);
+    return rc != kStatusOk ? rc : run_loss<true>(a, p, dtype, stream);
 }
 
 }  // extern "C"

@@ -24,7 +24,7 @@ struct LossArgs {
     const float *row_stats;          // backward: what the forward call left
     const float *grad;
     float *part, *named;             // parts: {m, sT, s1}; the logits that the row's targets name (K, then the label's)
-    float grad_scale, T, inv_T, wk, wl;
+    float grad_scale, T, wk, wl;
     float to_2T, to_21;              // log2 e / T, log2 e
     int N, V, K, wide_index, top_bf16;
     int run, parts, part_chunks, chunks;      // vectors of 64 lanes: of a wave, (parts to a row), of a part, of a row
@@ -106,9 +106,41 @@ __device__ __forceinline__ float row_max(const typename Vec<T>::Raw (&raw)[R], i
     return m;
 }
 
-template <typename T, int R, bool TEMP, bool ONE>
-__device__ __forceinline__ void row_sums(const LossArgs &a, const typename Vec<T>::Raw (&raw)[R], int c0, int n, int lane, float m,
-                                         float &sT, float &s1)
+// The exponentials of a row, relative to its maximum m.  exp((z - m) / T) is 2^(z c - m c) with c = log2 e / T.  m c is
+// rounded to `mc`, so that one multiply-add gives the exponent; what that leaves out, m c - mc, is the same for every value,
+// and a factor 2^-(m c - mc) on their sum puts it right.  (`fix` is that factor.)
+struct Scale { float c, mc, fix; };
+
+__device__ __forceinline__ Scale scale_of(float c, float m)
+{
+    const float mc = m * c;
+    return {c, mc, exp2_of(-fmaf(m, c, -mc))};
+}
+
+// Which exponentials a row needs: kOne: one of them (only one term has a target, or T = 1: they are the same); kTwo: both;
+// kSquare, kFourth: both, with T = 2 or 4: exp(z - m) is then the second or fourth power of exp((z - m) / T), one
+// exponential (four times a vector operation) and a multiplication or two instead of two exponentials.  kFar: both, the
+// maximum taken off first; for maxima whose product with c leaves the range (a row of the type's lowest values, say).
+enum { kOne, kTwo, kSquare, kFourth, kFar };
+
+template <int HOW>
+__device__ __forceinline__ void add_exps(float v, const Scale &t, const Scale &o, float &sT, float &s1)
+{
+    if (HOW == kFar) {
+        sT += exp2_of((v - t.mc) * t.c);
+        s1 += exp2_of((v - t.mc) * o.c);
+        return;
+    }
+    const float e = exp2_of(fmaf(v, t.c, -t.mc));
+    sT += e;
+    if (HOW == kTwo) s1 += exp2_of(fmaf(v, o.c, -o.mc));
+    if (HOW == kSquare) s1 = fmaf(e, e, s1);
+    if (HOW == kFourth) s1 = fmaf(e * e, e * e, s1);
+}
+
+template <typename T, int R, int HOW>
+__device__ __forceinline__ void row_sums(const LossArgs &a, const typename Vec<T>::Raw (&raw)[R], int c0, int n, int lane,
+                                         const Scale &t, const Scale &o, float &sT, float &s1)
 {
     constexpr int V = Vec<T>::V;
 #pragma unroll
@@ -119,55 +151,109 @@ __device__ __forceinline__ void row_sums(const LossArgs &a, const typename Vec<T
             Vec<T>::open(raw[r], v);
             if (l.k0 == 0 && l.k1 == V) {
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    const float d = v[k] - m;
-                    if (TEMP) sT += exp2_of(d * a.to_2T);
-                    if (ONE) s1 += exp2_of(d * a.to_21);
-                }
+                for (int k = 0; k < V; ++k) add_exps<HOW>(v[k], t, o, sT, s1);
             } else {
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    const float d = v[k] - m;
-                    const bool in = k >= l.k0 && k < l.k1;
-                    if (TEMP) sT += in ? exp2_of(d * a.to_2T) : 0.f;
-                    if (ONE) s1 += in ? exp2_of(d * a.to_21) : 0.f;
-                }
+                for (int k = 0; k < V; ++k)
+                    if (k >= l.k0 && k < l.k1) add_exps<HOW>(v[k], t, o, sT, s1);
             }
         }
 }
 
 // dz without the targets: ck exp((z - m) / T) + cl exp(z - m)
-template <typename T, int R, bool TEMP, bool ONE>
+template <int HOW>
+__device__ __forceinline__ float mix_exps(float v, const Scale &t, const Scale &o, float ck, float cl)
+{
+    if (HOW == kFar) return exp2_of((v - t.mc) * t.c) * ck + exp2_of((v - t.mc) * o.c) * cl;
+    const float e = exp2_of(fmaf(v, t.c, -t.mc));
+    if (HOW == kOne) return e * ck;
+    if (HOW == kTwo) return fmaf(exp2_of(fmaf(v, o.c, -o.mc)), cl, e * ck);
+    if (HOW == kSquare) return e * fmaf(e, cl, ck);
+    return e * fmaf(e * e * e, cl, ck);
+}
+
+template <typename T, int R, int HOW>
 __device__ __forceinline__ void row_write(const LossArgs &a, const typename Vec<T>::Raw (&raw)[R], T *dz, int c0, int n, int lane,
-                                          float m, float ck, float cl)
+                                          const Scale &t, const Scale &o, float ck, float cl)
 {
     constexpr int V = Vec<T>::V;
 #pragma unroll
     for (int r = 0; r < R; ++r)
         if (r < n) {
-            const RowLane l = row_lane<V>(a.V, c0 + r, lane);
             float v[V];
             Vec<T>::open(raw[r], v);
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const float d = v[k] - m;
-                float g = 0.f;
-                if (TEMP) g = exp2_of(d * a.to_2T) * ck;
-                if (ONE) g += exp2_of(d * a.to_21) * cl;
-                v[k] = g;
-            }
-            row_store(a, dz, l, v);
+            for (int k = 0; k < V; ++k) v[k] = mix_exps<HOW>(v[k], t, o, ck, cl);
+            row_store(a, dz, row_lane<V>(a.V, c0 + r, lane), v);
         }
 }
 
-template <typename T, int R>
-__device__ __forceinline__ void row_gradient(const LossArgs &a, const typename Vec<T>::Raw (&raw)[R], T *dz, int c0, int n, int lane,
-                                             float m, float ck, float cl, bool temp, bool one)
-{
-    if (temp && one) row_write<T, R, true, true>(a, raw, dz, c0, n, lane, m, ck, cl);
-    else if (temp) row_write<T, R, true, false>(a, raw, dz, c0, n, lane, m, ck, cl);
-    else row_write<T, R, false, true>(a, raw, dz, c0, n, lane, m, ck, cl);
-}
+// A row's exponentials as its targets need them: sums, gradient of a lane's vectors, and of one value.  temp, one: whether
+// exp((z - m) / T), exp(z - m) is needed.
+struct RowExps {
+    Scale t, o;
+    int how;
+    bool temp;
+    __device__ __forceinline__ RowExps(const LossArgs &a, float m, bool temp_needed, bool one_needed) : temp(temp_needed)
+    {
+        t = scale_of(temp ? a.to_2T : a.to_21, m);
+        o = scale_of(a.to_21, m);
+        const bool both = temp_needed && one_needed && a.T != 1.f;
+        how = !both ? kOne : a.T == 2.f ? kSquare : a.T == 4.f ? kFourth : kTwo;
+        if (!(fabsf(t.mc) < 1e30f && fabsf(o.mc) < 1e30f)) {
+            how = kFar;
+            t.mc = m;
+            t.fix = o.fix = 1.f;
+        }
+    }
+    template <typename T, int R>
+    __device__ __forceinline__ void sums(const LossArgs &a, const typename Vec<T>::Raw (&raw)[R], int c0, int n, int lane, float &sT,
+                                         float &s1) const
+    {
+        if (how == kOne) row_sums<T, R, kOne>(a, raw, c0, n, lane, t, o, sT, s1);
+        else if (how == kTwo) row_sums<T, R, kTwo>(a, raw, c0, n, lane, t, o, sT, s1);
+        else if (how == kSquare) row_sums<T, R, kSquare>(a, raw, c0, n, lane, t, o, sT, s1);
+        else if (how == kFourth) row_sums<T, R, kFourth>(a, raw, c0, n, lane, t, o, sT, s1);
+        else row_sums<T, R, kFar>(a, raw, c0, n, lane, t, o, sT, s1);
+    }
+    __device__ __forceinline__ float one_fix() const
+    {
+        const float f2 = t.fix * t.fix;
+        return how == kSquare ? f2 : how == kFourth ? f2 * f2 : o.fix;
+    }
+    // the factors of 2^-(m c - mc), on sums of all lanes
+    __device__ __forceinline__ void finish(float &sT, float &s1) const
+    {
+        sT *= t.fix;
+        s1 = how == kOne ? sT : s1 * one_fix();
+    }
+    // ck / sT and cl / s1 as factors of the raw exponentials
+    __device__ __forceinline__ void factors(float &ck, float &cl) const
+    {
+        if (how == kOne) {
+            ck = (ck + cl) * t.fix;
+            return;
+        }
+        ck *= t.fix;
+        cl *= one_fix();
+    }
+    template <typename T, int R>
+    __device__ __forceinline__ void write(const LossArgs &a, const typename Vec<T>::Raw (&raw)[R], T *dz, int c0, int n, int lane,
+                                          float ck, float cl) const
+    {
+        if (how == kOne) row_write<T, R, kOne>(a, raw, dz, c0, n, lane, t, o, ck, cl);
+        else if (how == kTwo) row_write<T, R, kTwo>(a, raw, dz, c0, n, lane, t, o, ck, cl);
+        else if (how == kSquare) row_write<T, R, kSquare>(a, raw, dz, c0, n, lane, t, o, ck, cl);
+        else if (how == kFourth) row_write<T, R, kFourth>(a, raw, dz, c0, n, lane, t, o, ck, cl);
+        else row_write<T, R, kFar>(a, raw, dz, c0, n, lane, t, o, ck, cl);
+    }
+    __device__ __forceinline__ float mix(float v, float ck, float cl) const
+    {
+        return how == kOne ? mix_exps<kOne>(v, t, o, ck, cl) : how == kTwo ? mix_exps<kTwo>(v, t, o, ck, cl)
+             : how == kSquare ? mix_exps<kSquare>(v, t, o, ck, cl) : how == kFourth ? mix_exps<kFourth>(v, t, o, ck, cl)
+             : mix_exps<kFar>(v, t, o, ck, cl);
+    }
+};
 
 template <typename T, int R>
 __device__ __forceinline__ void row_clear(const LossArgs &a, T *dz, int c0, int n, int lane)
@@ -280,7 +366,8 @@ __device__ __forceinline__ float weigh_entries(const LossArgs &a, const RowTeam<
     return ts;
 }
 
-// sum_k p_k (log p_k - log q_k) over a thread's share; zk from `named` where given
+// T sum_k p_k (log p_k - log q_k) over a thread's share, as sum_k p_k (T (log p_k + log sT) - (z_k - m)), in which no
+// distance is divided by a small T; zk from `named` where given
 template <bool SOLO>
 __device__ __forceinline__ float divergence(const LossArgs &a, const RowTeam<SOLO> &team, const Entries &e, const float *named,
                                             float inv_ts, float m, float sT)
@@ -289,7 +376,7 @@ __device__ __forceinline__ float divergence(const LossArgs &a, const RowTeam<SOL
     const float log_sT = logf(sT);
     for (int k = team.id; k < a.K; k += team.size) {
         const float p = e.prob[k] * inv_ts;
-        if (e.idx[k] >= 0 && !(p <= 0.f)) kd += p * (logf(p) - (((named ? named[k] : e.zk[k]) - m) * a.inv_T - log_sT));
+        if (e.idx[k] >= 0 && !(p <= 0.f)) kd += p * (a.T * (logf(p) + log_sT) - ((named ? named[k] : e.zk[k]) - m));
     }
     return kd;
 }
@@ -297,7 +384,7 @@ __device__ __forceinline__ float divergence(const LossArgs &a, const RowTeam<SOL
 // the classes in [lo, hi) that the targets name, whole
 template <typename T, bool SOLO>
 __device__ __forceinline__ void write_named(const LossArgs &a, const RowTeam<SOLO> &team, const Entries &e, T *dz, int label, float zl,
-                                            int lo, int hi, float m, float ck, float cl, float share, float gl)
+                                            int lo, int hi, const RowExps &x, float ck, float cl, float share, float gl)
 {
     for (int k = team.id; k <= a.K; k += team.size) {
         const int v = k < a.K ? e.idx[k] : label;
@@ -309,12 +396,7 @@ __device__ __forceinline__ void write_named(const LossArgs &a, const RowTeam<SOL
                 p += e.prob[j];
                 if (j < k) first = false;
             }
-        if (!first) continue;
-        const float d = (k < a.K ? e.zk[k] : zl) - m;
-        float g = 0.f;
-        if (share != 0.f) g = exp2_of(d * a.to_2T) * ck - share * p;
-        if (gl != 0.f) g += exp2_of(d * a.to_21) * cl - (v == label ? gl : 0.f);
-        st_elem(dz, v, g);
+        if (first) st_elem(dz, v, x.mix(k < a.K ? e.zk[k] : zl, ck, cl) - (share * p + (v == label ? gl : 0.f)));
     }
 }
 
@@ -322,7 +404,7 @@ __device__ __forceinline__ void write_named(const LossArgs &a, const RowTeam<SOL
 // Whole rows: loss (and statistics), and with GRAD the gradient
 // ---------------------------------------------------------------------------
 template <typename T, int R, bool SOLO, bool GRAD>
-__global__ __launch_bounds__(SOLO ? 256 : 1024) void distill_rows(LossArgs a)
+__global__ __launch_bounds__(SOLO ? 256 : 1024, 8) void distill_rows(LossArgs a)
 {
     extern __shared__ float lds[];
     __shared__ float red[7][16];
@@ -351,15 +433,15 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void distill_rows(LossArgs a)
         if (GRAD) row_clear<T, R>(a, dz, c0, cn, team.lane);
         return;
     }
+    // statistics are asked for whole; without them a term without target needs no sum
+    const RowExps x(a, m, a.K > 0 && (has || a.stats), label >= 0 || a.stats);
     float sums[3] = {0.f, 0.f, 0.f};
     sums[2] = weigh_entries(a, team, e, tm);
-    // statistics are asked for whole; without them a term without target needs no sum
-    const bool temp = a.K > 0 && (has || a.stats), one = label >= 0 || a.stats;
-    if (temp && one) row_sums<T, R, true, true>(a, raw, c0, cn, team.lane, m, sums[0], sums[1]);
-    else if (temp) row_sums<T, R, true, false>(a, raw, c0, cn, team.lane, m, sums[0], sums[1]);
-    else row_sums<T, R, false, true>(a, raw, c0, cn, team.lane, m, sums[0], sums[1]);
+    x.template sums<T, R>(a, raw, c0, cn, team.lane, sums[0], sums[1]);
     team.sum_of(sums, red + 3);
-    const float s1 = sums[1], sT = a.K ? sums[0] : s1, inv_ts = has ? 1.f / sums[2] : 0.f;
+    float sT = sums[0], s1 = sums[1];
+    x.finish(sT, s1);
+    const float inv_ts = has ? 1.f / sums[2] : 0.f;
     if (a.stats && team.id == 0) {
         a.stats[(int64_t)n * 3] = m;
         a.stats[(int64_t)n * 3 + 1] = sT;
@@ -370,15 +452,16 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void distill_rows(LossArgs a)
         const float g = a.grad_scale * (a.grad ? a.grad[n] : 1.f);
         if (has) { gk = g * a.wk * a.T; ck = gk / sT; }
         if (label >= 0) { gl = g * a.wl; cl = gl / s1; }
-        row_gradient<T, R>(a, raw, dz, c0, cn, team.lane, m, ck, cl, has, label >= 0);
+        x.factors(ck, cl);
+        x.template write<T, R>(a, raw, dz, c0, cn, team.lane, ck, cl);
     }
     float kd[1] = {has ? divergence(a, team, e, nullptr, inv_ts, m, sT) : 0.f};
     team.sum_of(kd, red + 6);
     if (team.id == 0)
-        a.loss[n] = (has ? a.wk * a.T * a.T * kd[0] : 0.f) + (label >= 0 ? a.wl * (logf(s1) - (zl - m)) : 0.f);
+        a.loss[n] = (has ? a.wk * a.T * kd[0] : 0.f) + (label >= 0 ? a.wl * (logf(s1) - (zl - m)) : 0.f);
     if (GRAD) {
         team.sync();
-        write_named(a, team, e, dz, label, zl, 0, a.V, m, ck, cl, gk * inv_ts, gl);
+        write_named(a, team, e, dz, label, zl, 0, a.V, x, ck, cl, gk * inv_ts, gl);
     }
 }
 
@@ -413,9 +496,10 @@ __global__ __launch_bounds__(512) void distill_part_sums(LossArgs a)
     float s[2] = {0.f, 0.f};
     // of a part without any class left the sums are 0
     const float top = m[0] == -INFINITY ? 0.f : m[0];
-    if (a.K) row_sums<T, R, true, true>(a, raw, c0, cn, team.lane, top, s[0], s[1]);
-    else row_sums<T, R, false, true>(a, raw, c0, cn, team.lane, top, s[0], s[1]);
+    const RowExps x(a, top, a.K > 0, true);
+    x.template sums<T, R>(a, raw, c0, cn, team.lane, s[0], s[1]);
     team.sum_of(s, red + 1);
+    x.finish(s[0], s[1]);
     if (team.id == 0) {
         float *p = a.part + (int64_t)blockIdx.x * 3;
         p[0] = m[0];
@@ -431,7 +515,7 @@ __global__ __launch_bounds__(512) void distill_part_apply(LossArgs a)
 {
     constexpr int V = Vec<T>::V;
     extern __shared__ float lds[];
-    __shared__ float red[4][16];
+    __shared__ float red[3][16];
     const RowTeam<false> team;
     const int n = GRAD ? fastdiv(blockIdx.x, a.div_parts) : (int)blockIdx.x, part = GRAD ? blockIdx.x - n * a.parts : 0;
     const T *z = static_cast<const T *>(a.z) + n * a.z_stride;
@@ -448,10 +532,12 @@ __global__ __launch_bounds__(512) void distill_part_apply(LossArgs a)
     const int label = a.labels ? class_at(a.labels, n, a.wide_index, a.V) : -1;
     const float zl = GRAD && label >= lo && label < hi ? ld_elem(z, label) : 0.f;
     const Entries e = entries_at(lds, a.K);
-    float most[2];
-    most[0] = read_entries(a, team, e, z, n, GRAD ? lo : 0, GRAD ? hi : 0, most[1]);
-    team.max_of(most, red);
-    const bool has = most[1] > 0.f;
+    float most[1], dummy;
+    most[0] = read_entries(a, team, e, z, n, GRAD ? lo : 0, GRAD ? hi : 0, dummy);
+    // every wave for itself: whether an entry names a class
+    bool has = false;
+    for (int k = team.lane; k < a.K; k += 64) has |= class_at(a.top_idx, (int64_t)n * a.K + k, a.wide_index, a.V) >= 0;
+    has = __any(has);
     const bool lead = part == 0 && a.loss;
     if (!has && label < 0) {
         if (lead && team.id == 0) a.loss[n] = 0.f;
@@ -479,22 +565,25 @@ __global__ __launch_bounds__(512) void distill_part_apply(LossArgs a)
         s1 = wave_sum(s1);
         if (!a.K) sT = s1;
     }
-    float ts[1] = {weigh_entries(a, team, e, most[0])};
-    team.sum_of(ts, red + 2);
-    const float inv_ts = has ? 1.f / ts[0] : 0.f;
+    const RowExps x(a, m, has, label >= 0);
+    team.max_of(most, red);                  // (a barrier: the logits that targets name are read, their places may be written)
     float gk = 0.f, gl = 0.f, ck = 0.f, cl = 0.f;
     if (GRAD) {
         const float g = a.grad_scale * (a.grad ? a.grad[n] : 1.f);
         if (has) { gk = g * a.wk * a.T; ck = gk / sT; }
         if (label >= 0) { gl = g * a.wl; cl = gl / s1; }
-        row_gradient<T, R>(a, raw, dz, c0, cn, team.lane, m, ck, cl, has, label >= 0);
+        x.factors(ck, cl);
+        x.template write<T, R>(a, raw, dz, c0, cn, team.lane, ck, cl);
     }
+    float ts[1] = {weigh_entries(a, team, e, most[0])};
+    team.sum_of(ts, red + 1);                // (a barrier: the softmax's share is written, targets may be written over it)
+    const float inv_ts = has ? 1.f / ts[0] : 0.f;
     if (lead) {
         const float *named = a.named + (int64_t)n * (a.K + 1);
         float kd[1] = {has ? divergence(a, team, e, named, inv_ts, m, sT) : 0.f};
-        team.sum_of(kd, red + 3);
+        team.sum_of(kd, red + 2);
         if (team.id == 0) {
-            a.loss[n] = (has ? a.wk * a.T * a.T * kd[0] : 0.f) + (label >= 0 ? a.wl * (logf(s1) - (named[a.K] - m)) : 0.f);
+            a.loss[n] = (has ? a.wk * a.T * kd[0] : 0.f) + (label >= 0 ? a.wl * (logf(s1) - (named[a.K] - m)) : 0.f);
             if (a.stats) {
                 a.stats[(int64_t)n * 3] = m;
                 a.stats[(int64_t)n * 3 + 1] = sT;
@@ -502,8 +591,5 @@ __global__ __launch_bounds__(512) void distill_part_apply(LossArgs a)
             }
         }
     }
-    if (GRAD) {
-        team.sync();
-        write_named(a, team, e, dz, label, zl, lo, hi, m, ck, cl, gk * inv_ts, gl);
-    }
+    if (GRAD) write_named(a, team, e, dz, label, zl, lo, hi, x, ck, cl, gk * inv_ts, gl);
 }

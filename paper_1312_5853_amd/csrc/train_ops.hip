@@ -401,7 +401,7 @@ int loss_common(LossArgs &a, LossPlan &p, bool dz, int N, int V, int K, float te
         if (!aligned(ws, 256)) return kErrMisaligned;
     }
     a.N = N; a.V = V; a.K = K;
-    a.T = temperature; a.inv_T = 1.f / temperature;
+    a.T = temperature;
     a.to_21 = log2e; a.to_2T = log2e / temperature;
     a.wide_index = index_bytes == 8; a.top_bf16 = tb == 2;
     if (a.wk == 0.f) a.K = 0;                            // a term of weight 0 is absent

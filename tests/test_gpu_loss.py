@@ -69,12 +69,16 @@ def bounds(z, lab, idx, val, T, wk, wl, grad, dtype):
                 bl[n] += E * wk * T * T * (1 + (p * (1 + np.abs(np.where(use, t, 0))) * (1 + np.where(use, lq, 0) + np.abs(np.log(np.where(use, p, 1)))))[use].sum())
                 bz[n] += E * wk * T * abs(grad[n]) * np.where(eT > 0, eT / eT.sum() * (1 - np.maximum(d, -1e30) / T), 0)
                 np.add.at(bz[n], idx[n][held], E * wk * T * abs(grad[n]) * p * (1 + np.abs(np.where(use, t, 0))))
+    bl += U * np.abs(loss)
+    bz += U * np.abs(dz)                                              # `want` is compared as fp32
     bz += np.abs(dz) * (2.0 ** -8 if dtype == "bf16" else U) + 1e-37
     return loss, dz, bl + 1e-37, bz
 
 
 def close(got, want, bound):
     got = got.float().cpu().numpy().astype(np.float64) if isinstance(got, torch.Tensor) else got
+    with np.errstate(over="ignore"):
+        want = want.astype(np.float32).astype(np.float64)           # what fp32 cannot hold is infinite
     bad = np.isnan(want)
     assert (np.isnan(got) == bad).all()
     inf = np.isinf(want)
@@ -182,6 +186,29 @@ def test_rows_that_a_mask_leaves_empty_and_targets_left_out(V):
     l = loss.cpu().numpy()
     assert np.isnan(l[0]) and l[1] == INF and l[2] == INF and np.isfinite(l[3]) and np.isfinite(l[4])
     assert torch.isnan(dz[0]).all() and torch.isfinite(dz[1:]).all()
+
+
+@pytest.mark.parametrize("V", [40, 5003, 70001])
+@pytest.mark.parametrize("value", [-3.4028234663852886e38, 3.4028234663852886e38, 1e37, -2e30])
+def test_rows_of_extreme_finite_logits(V, value):
+    """A row of nothing but the type's lowest (or largest) value is an even distribution; one class above it takes all."""
+    z, lab, idx, val = inputs(4, V, 4, "f32", 13)
+    z[:2] = value
+    z[1, 2] = value / 2 if value < 0 else value
+    lab[:], idx[:] = 2, [0, 1, 2, 3]
+    for T in (1.0, 2.0, 3.0, 4.0, 0.25):
+        run_case(z, lab, idx, val, T)
+
+
+@pytest.mark.parametrize("T", [1.0, 2.0, 4.0, 2.5])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_logits_far_from_zero(T, dtype):
+    """A maximum of some thousands is taken off before anything is rounded away."""
+    z, lab, idx, val = inputs(5, 3001, 6, "f32", 14)
+    z = (z + np.array([[5000.0], [-5000.0], [1e6], [-3e7], [123.4]])).astype(np.float32)
+    if dtype == "bf16":
+        z, val = oracle.bf16_round(z), oracle.bf16_round(val)
+    run_case(z, lab, idx, val, T, dtype=dtype)
 
 
 @pytest.mark.parametrize("V", [40, 5003, 70001])

@@ -28,6 +28,7 @@ struct NormArgs {
     float *mean, *rstd;              // forward: results (nullptr: not wanted); backward and kApply: read
     float *part;                     // sums of tiles.  forward: {mean, sum of squares, count}; backward: A, then B, of a row of C
     float *group_sums;               // backward kApply: {m1, m2} of every sample and group
+    float *sample_sums;              // backward: A, then B, of every sample and channel (`part` itself where a sample has one row)
     float *dgamma, *dbeta;
     int N, C, S, groups, cpg, act;
     float eps, inv_m;                // inv_m: 1 / M
@@ -37,11 +38,11 @@ struct NormArgs {
     int units, chunks, lane_bits, channels;   // of a group; chunks to a plane; lanes to a plane (log2); planes to a unit
     int run;                                  // units to a wave
     int tiles, parts, span;                   // of a group; of a plane (0: a tile is whole planes); units of a tile
-    FastDiv div_chunks, div_tiles;
+    FastDiv div_chunks, div_tiles, div_slots;  // slots: of a plane's sums in LDS (backward)
     // channels last
     int cw, slab_groups, slabs, lanes, rows;  // channels, groups of a slab; slabs; lanes to a row; rows at a time
     int tile_rows, pitch, group_lanes, channel_lanes, units_per_xcd, work;
-    FastDiv div_lanes, div_slabs;
+    FastDiv div_lanes, div_slabs, div_width;  // width: sums of a group in a thread row (forward)
 };
 
 __device__ __forceinline__ float act_fwd(float z, int act)
@@ -235,23 +236,25 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_fwd(NormA
 #pragma unroll
     for (int r = 0; r < R; ++r)
         if (r < n && t.live) {
-            const float scale = rstd * (a.gamma ? a.gamma[c0 + pl[r].c] : 1.f), shift = a.beta ? a.beta[c0 + pl[r].c] : 0.f;
+            const float scale = rstd * (a.gamma ? a.gamma[c0 + pl[r].c] : 1.f);
+            const float shift = fmaf(-mean, scale, a.beta ? a.beta[c0 + pl[r].c] : 0.f);
             float v[V];
             Vec<T>::open(raw[r], v);
 #pragma unroll
-            for (int k = 0; k < V; ++k) v[k] = act_fwd((v[k] - mean) * scale + shift, a.act);
+            for (int k = 0; k < V; ++k) v[k] = act_fwd(fmaf(v[k], scale, shift), a.act);
             plane_store(a, y, pl[r], v);
         }
 }
 
 // With d = x - mean: z = gamma rstd d + beta, B = rstd sum dz d, dx = gamma rstd dz - rstd m1 - d rstd^2 m2.
-// Sums per channel: of a unit over its lanes.  Consecutive units of a wave that lie in one plane are added before that.
+// Sums per channel: of a unit over the runs of lanes that share a plane, at most 16 lanes (what the moves within a row of
+// lanes reach), each run's in a slot of LDS.  Consecutive units of a wave that lie in one plane are added before that.
 template <typename T, int R, bool SOLO, int MODE>
 __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_bwd(NormArgs a)
 {
     constexpr int V = Vec<T>::V;
-    constexpr bool kKeep = sizeof(T) == 4;       // fp32: d and dz take the place of x and dy
-    extern __shared__ float slots[];             // A of every unit's planes, then B
+    constexpr bool kKeep = MODE == kWhole && (sizeof(T) == 4 || R <= 4);       // dz stays in registers, else it is computed twice
+    extern __shared__ float slots[];             // A of every unit's runs, then B
     const int lane = threadIdx.x & 63, wave = SOLO ? 0 : uniform((int)(threadIdx.x >> 6));
     const PlaneTile t = plane_tile<SOLO, MODE>(a);
     const int64_t base = t.group * a.cpg * a.S;
@@ -259,6 +262,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_bwd(NormA
     typename Vec<T>::Raw rx[R], rd[R];
     PlaneLane pl[R];
     float scale[R], shift[R];                    // gamma rstd, beta
+    float dz[kKeep ? R : 1][V];
     const int u0 = t.u0 + wave * a.run, n = min(a.run, t.u1 - u0);
     const int c0 = t.g * a.cpg;
 #pragma unroll
@@ -279,7 +283,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_bwd(NormA
         m1 = a.group_sums[2 * t.group];
         m2 = a.group_sums[2 * t.group + 1];
     } else {
-        const int count = (t.u1 - t.u0) * a.channels;                          // slots of the tile
+        const int bits = min(a.lane_bits, 4), slots_of_unit = 64 >> bits, count = (t.u1 - t.u0) * slots_of_unit;
         float *slot_a = slots + (SOLO ? (int)(threadIdx.x >> 6) * 2 * count : 0), *slot_b = slot_a + count;
         float A = 0.f, B = 0.f;
 #pragma unroll
@@ -309,42 +313,30 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_bwd(NormA
                 }
                 if constexpr (kKeep) {
 #pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        rx[r][k] = xv[k];
-                        rd[r][k] = dv[k];
-                    }
+                    for (int k = 0; k < V; ++k) dz[r][k] = dv[k];
                 }
-                const int u = u0 + r, slot = (u - t.u0) * a.channels;
-                if (a.lane_bits == 6) {
-                    // a wave's last unit in a plane gets the sum of those before it there
-                    const bool flush = r + 1 == n || (int)fastdiv(u + 1, a.div_chunks) != (int)fastdiv(u, a.div_chunks);
-                    float ta = 0.f, tb = 0.f;
-                    if (flush) {
-                        ta = wave_sum(A);
-                        tb = wave_sum(B) * rstd;
-                        A = B = 0.f;
-                    }
-                    if (lane == 0) {
-                        slot_a[slot] = ta;
-                        slot_b[slot] = tb;
-                    }
-                } else {
-                    A = run_sum(A, 1 << a.lane_bits);
-                    B = run_sum(B, 1 << a.lane_bits) * rstd;
-                    if ((lane & ((1 << a.lane_bits) - 1)) == 0) {
-                        slot_a[slot + (lane >> a.lane_bits)] = A;
-                        slot_b[slot + (lane >> a.lane_bits)] = B;
-                    }
+                // a wave's last unit in a plane gets the sum of those before it there
+                const int u = u0 + r, slot = (u - t.u0) * slots_of_unit + (lane >> bits);
+                const bool flush = a.lane_bits < 6 || r + 1 == n ||
+                                   (int)fastdiv(u + 1, a.div_chunks) != (int)fastdiv(u, a.div_chunks);
+                float ta = 0.f, tb = 0.f;
+                if (flush) {
+                    ta = run_sum(A, 1 << bits);
+                    tb = run_sum(B, 1 << bits) * rstd;
                     A = B = 0.f;
+                }
+                if ((lane & ((1 << bits) - 1)) == 0) {
+                    slot_a[slot] = ta;
+                    slot_b[slot] = tb;
                 }
             }
         __syncthreads();
-        // the tile's channels: from the first unit's (there is one chunk to a plane wherever a unit holds several)
+        // the tile's planes, from the first unit's on
         const int first = fastdiv(t.u0, a.div_chunks) * a.channels;
         if (MODE == kWhole) {
             float p = 0.f, q = 0.f;
             for (int i = lane; i < count; i += 64) {
-                const int c = fastdiv(i, a.div_chunks);
+                const int c = fastdiv(i, a.div_slots);
                 const float gamma = c < a.cpg && a.gamma ? a.gamma[c0 + c] : 1.f;
                 p += gamma * slot_a[i];
                 q += gamma * slot_b[i];
@@ -354,7 +346,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_bwd(NormA
         }
         const int64_t n_group = fastdiv((uint32_t)t.group, a.div_groups);
         const int64_t row = n_group * a.rows_per_sample + (a.parts ? t.tile - t.tile / a.parts * a.parts : 0);
-        const int planes = a.parts ? 1 : (count + a.chunks - 1) / a.chunks, per = a.parts ? count : a.chunks;
+        const int per = a.parts ? count : (int)a.div_slots.d, planes = a.parts ? 1 : (count + per - 1) / per;
         for (int j = SOLO ? lane : (int)threadIdx.x; j < planes; j += SOLO ? 64 : (int)blockDim.x)
             if (first + j < a.cpg && t.live) {
                 float sa = 0.f, sb = 0.f;
@@ -375,15 +367,13 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_bwd(NormA
             float xv[V], dv[V];
             Vec<T>::open(rx[r], xv);
             Vec<T>::open(rd[r], dv);
-            if (!kKeep || MODE == kApply) {
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    xv[k] -= mean;
-                    dv[k] = act_bwd(dv[k], scale[r] * xv[k] + shift[r], a.act);
-                }
+            for (int k = 0; k < V; ++k) {
+                xv[k] -= mean;
+                if constexpr (kKeep) dv[k] = dz[r][k];
+                else dv[k] = act_bwd(dv[k], scale[r] * xv[k] + shift[r], a.act);
+                dv[k] = (scale[r] * dv[k] - c1) - xv[k] * c2;
             }
-#pragma unroll
-            for (int k = 0; k < V; ++k) dv[k] = (scale[r] * dv[k] - c1) - xv[k] * c2;
             plane_store(a, dx, pl[r], dv);
         }
 }
@@ -455,12 +445,13 @@ __device__ __forceinline__ int slab_slot(const NormArgs &a, int p, int c)
     return (c - q) * a.pitch + p * a.lanes + j;
 }
 
-template <typename T, int R, int MODE>
+// ONE: every vector lies in one group (C / groups a multiple of the vector): a thread then has one sum, not one per value.
+template <typename T, int R, int MODE, bool ONE>
 __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
 {
-    constexpr int V = Vec<T>::V;
+    constexpr int V = Vec<T>::V, W = ONE ? 1 : V;      // W sums to a thread, of V / W values a row each
     extern __shared__ float lds[];
-    float *sum = lds, *dev = lds + V * a.pitch, *gmean = dev + V * a.pitch, *grstd = gmean + a.slab_groups;
+    float *sum = lds, *dev = lds + W * a.pitch, *gmean = dev + W * a.pitch, *grstd = gmean + a.slab_groups;
     const SlabTile t = slab_tile<V>(a);
     if (!t.live) return;
     const int64_t base = ((int64_t)t.n * a.S + t.s0) * a.C + t.slab * a.cw + t.q;
@@ -473,21 +464,21 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
     }
     const int64_t group0 = (int64_t)t.n * a.groups + t.slab * a.slab_groups;
     if (MODE != kApply) {
-        // every thread's sums and squared distances from its own mean, channel by channel
+        // every thread's sums, and squared distances from its own means
         const int whole = t.count / a.rows, extra = t.count - whole * a.rows;       // rows of a thread: whole (+ 1)
         if (t.on) {
             const int cnt = whole + (t.p < extra);
-            const float inv = cnt ? 1.f / cnt : 0.f;
-            float s[V], d[V];
+            const float inv = cnt ? 1.f / (cnt * (V / W)) : 0.f;
+            float s[W], d[W];
 #pragma unroll
-            for (int k = 0; k < V; ++k) s[k] = d[k] = 0.f;
+            for (int k = 0; k < W; ++k) s[k] = d[k] = 0.f;
 #pragma unroll
             for (int r = 0; r < R; ++r)
                 if (t.p + r * a.rows < t.count) {
                     float v[V];
                     Vec<T>::open(raw[r], v);
 #pragma unroll
-                    for (int k = 0; k < V; ++k) s[k] += v[k];
+                    for (int k = 0; k < V; ++k) s[k % W] += v[k];
                 }
 #pragma unroll
             for (int r = 0; r < R; ++r)
@@ -496,38 +487,43 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
                     Vec<T>::open(raw[r], v);
 #pragma unroll
                     for (int k = 0; k < V; ++k) {
-                        const float e = v[k] - s[k] * inv;
-                        d[k] += e * e;
+                        const float e = v[k] - s[k % W] * inv;
+                        d[k % W] += e * e;
                     }
                 }
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
+            for (int k = 0; k < W; ++k) {
                 sum[k * a.pitch + threadIdx.x] = s[k];
                 dev[k * a.pitch + threadIdx.x] = d[k];
             }
         }
         __syncthreads();
         // a group's sum, then its squared distances: those of the parts, and the parts' means' own
-        const int lane = threadIdx.x & (a.group_lanes - 1), entries = a.rows * a.cpg;
+        const int width = ONE ? a.cpg / V : a.cpg;                                  // sums of a group in a thread row
+        const int lane = threadIdx.x & (a.group_lanes - 1), entries = a.rows * width;
         const int at = threadIdx.x / a.group_lanes, step = blockDim.x / a.group_lanes;
         const float total = (float)t.count * a.cpg, inv_total = 1.f / total;
-        const float inv_whole = whole ? 1.f / whole : 0.f, inv_more = 1.f / (whole + 1);
+        const float n_whole = whole * (V / W), n_more = (whole + 1) * (V / W);
+        const float inv_whole = whole ? 1.f / n_whole : 0.f, inv_more = 1.f / n_more;
+        auto slot = [&](int p, int g, int i) {
+            return ONE ? p * a.lanes + g * width + i : slab_slot<V>(a, p, g * width + i);
+        };
         for (int g0 = 0; g0 < a.slab_groups; g0 += step) {
             const int g = g0 + at;
             const bool some = g < a.slab_groups;
             float s = 0.f, d = 0.f;
             if (some)
                 for (int e = lane; e < entries; e += a.group_lanes) {
-                    const int p = fastdiv(e, a.div_cpg);
-                    s += sum[slab_slot<V>(a, p, g * a.cpg + e - p * a.cpg)];
+                    const int p = fastdiv(e, a.div_width);
+                    s += sum[slot(p, g, e - p * width)];
                 }
             const float mean = run_sum(s, a.group_lanes) * inv_total;
             if (some)
                 for (int e = lane; e < entries; e += a.group_lanes) {
-                    const int p = fastdiv(e, a.div_cpg), at2 = slab_slot<V>(a, p, g * a.cpg + e - p * a.cpg);
+                    const int p = fastdiv(e, a.div_width), i = slot(p, g, e - p * width);
                     const bool more = p < extra;
-                    const float diff = sum[at2] * (more ? inv_more : inv_whole) - mean;
-                    if (more || whole) d += dev[at2] + (float)(whole + more) * diff * diff;
+                    const float diff = sum[i] * (more ? inv_more : inv_whole) - mean;
+                    if (more || whole) d += dev[i] + (more ? n_more : n_whole) * diff * diff;
                 }
             d = run_sum(d, a.group_lanes);
             if (some && lane == 0) {
@@ -549,13 +545,12 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
         __syncthreads();
     }
     if (!t.on) return;
-    float mean[V], scale[V], shift[V];
+    float scale[V], shift[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         const int c = min(t.q + k, a.cw - 1), g = fastdiv(c, a.div_cpg), ch = t.slab * a.cw + c;
-        mean[k] = MODE == kApply ? a.mean[group0 + g] : gmean[g];
         scale[k] = (MODE == kApply ? a.rstd[group0 + g] : grstd[g]) * (a.gamma ? a.gamma[ch] : 1.f);
-        shift[k] = a.beta ? a.beta[ch] : 0.f;
+        shift[k] = fmaf(-(MODE == kApply ? a.mean[group0 + g] : gmean[g]), scale[k], a.beta ? a.beta[ch] : 0.f);
     }
     T *y = static_cast<T *>(a.out) + base;
 #pragma unroll
@@ -565,7 +560,7 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
             float v[V];
             Vec<T>::open(raw[r], v);
 #pragma unroll
-            for (int k = 0; k < V; ++k) v[k] = act_fwd((v[k] - mean[k]) * scale[k] + shift[k], a.act);
+            for (int k = 0; k < V; ++k) v[k] = act_fwd(fmaf(v[k], scale[k], shift[k]), a.act);
             slab_store(a, y + s * a.C, t, v);
         }
     }
@@ -575,7 +570,7 @@ template <typename T, int R, int MODE>
 __global__ __launch_bounds__(1024) void group_norm_last_bwd(NormArgs a)
 {
     constexpr int V = Vec<T>::V;
-    constexpr bool kKeep = sizeof(T) == 4;
+    constexpr bool kKeep = MODE == kWhole && sizeof(T) == 4;     // d and dz take the place of x and dy
     extern __shared__ float lds[];
     float *sa = lds, *sb = lds + V * a.pitch, *ca = sb + V * a.pitch, *cb = ca + a.cw, *g1 = cb + a.cw, *g2 = g1 + a.slab_groups;
     const SlabTile t = slab_tile<V>(a);
@@ -698,7 +693,7 @@ __global__ __launch_bounds__(1024) void group_norm_last_bwd(NormArgs a)
             Vec<T>::open(rd[r], dv);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                if (!kKeep || MODE == kApply) {
+                if (!kKeep) {
                     xv[k] -= mean[k];
                     dv[k] = act_bwd(dv[k], scale[k] * xv[k] + shift[k], a.act);
                 }
@@ -731,46 +726,56 @@ __global__ __launch_bounds__(256) void group_norm_join_stats(const float *part, 
     }
 }
 
-// A wave per sample and group: {m1, m2} from the rows of channel sums.
+// A wave per sample and group: its channels' sums over the sample's rows, and {m1, m2} from them.
 __global__ __launch_bounds__(256) void group_norm_join_groups(NormArgs a)
 {
     const int lane = threadIdx.x & 63, total = a.N * a.groups, i = blockIdx.x * 4 + (threadIdx.x >> 6);
     const int grp = min(i, total - 1), n = fastdiv(grp, a.div_groups), c0 = (grp - n * a.groups) * a.cpg;
-    float p = 0.f, q = 0.f;
-    for (int e = lane; e < a.rows_per_sample * a.cpg; e += 64) {
-        const int t = fastdiv(e, a.div_cpg), c = c0 + e - t * a.cpg;
-        const int64_t row = (int64_t)n * a.rows_per_sample + t;
-        const float gamma = a.gamma ? a.gamma[c] : 1.f;
-        p += gamma * a.part[row * a.C + c];
-        q += gamma * a.part[((int64_t)a.part_rows + row) * a.C + c];
+    const float *pa = a.part + (int64_t)n * a.rows_per_sample * a.C + c0, *pb = pa + (int64_t)a.part_rows * a.C;
+    float m1 = 0.f, m2 = 0.f;
+    for (int c = 0; c < a.cpg; ++c) {
+        float A = 0.f, B = 0.f;
+        for (int t = lane; t < a.rows_per_sample; t += 64) {
+            A += pa[(int64_t)t * a.C + c];
+            B += pb[(int64_t)t * a.C + c];
+        }
+        A = wave_sum(A);
+        B = wave_sum(B);
+        const float gamma = a.gamma ? a.gamma[c0 + c] : 1.f;
+        m1 += gamma * A;
+        m2 += gamma * B;
+        if (lane == 0 && i < total) {
+            a.sample_sums[(int64_t)n * a.C + c0 + c] = A;
+            a.sample_sums[(int64_t)(a.N + n) * a.C + c0 + c] = B;
+        }
     }
-    p = wave_sum(p) * a.inv_m;
-    q = wave_sum(q) * a.inv_m;
     if (lane == 0 && i < total) {
-        a.group_sums[2 * i] = p;
-        a.group_sums[2 * i + 1] = q;
+        a.group_sums[2 * i] = m1 * a.inv_m;
+        a.group_sums[2 * i + 1] = m2 * a.inv_m;
     }
 }
 
-// Gradients of gamma and beta: a work-group adds the rows of 32 channels, 32 rows at a time, then in a tree.
+// Gradients of gamma and beta: a work-group adds the samples' sums of 16 channels, 64 samples at a time, then in a tree.
 __global__ __launch_bounds__(1024) void group_norm_join_channels(NormArgs a)
 {
-    __shared__ float red[2][32][33];
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
+    __shared__ float red[2][16][65];
+    const int x = threadIdx.x & 15, y = threadIdx.x >> 4, c = blockIdx.x * 16 + x;
     float A = 0.f, B = 0.f;
-    if (c < a.C)
-        for (int r = y; r < a.part_rows; r += 32) {
-            A += a.part[(int64_t)r * a.C + c];
-            B += a.part[((int64_t)a.part_rows + r) * a.C + c];
+    if (c < a.C) {
+#pragma unroll 4
+        for (int n = y; n < a.N; n += 64) {
+            A += a.sample_sums[(int64_t)n * a.C + c];
+            B += a.sample_sums[(int64_t)(a.N + n) * a.C + c];
         }
-    red[0][y][x] = A;
-    red[1][y][x] = B;
+    }
+    red[0][x][y] = A;
+    red[1][x][y] = B;
     __syncthreads();
-    // half a wave per channel: lane x of row y holds row x of channel y
-    A = run_sum(red[0][x][y], 32);
-    B = run_sum(red[1][x][y], 32);
-    const int ch = blockIdx.x * 32 + y;
-    if (x == 0 && ch < a.C) {
+    // a wave to a channel
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, ch = blockIdx.x * 16 + w;
+    A = wave_sum(red[0][w][lane]);
+    B = wave_sum(red[1][w][lane]);
+    if (lane == 0 && ch < a.C) {
         if (a.dbeta) a.dbeta[ch] = A;
         if (a.dgamma) a.dgamma[ch] = B;
     }

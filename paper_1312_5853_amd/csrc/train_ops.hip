@@ -51,7 +51,7 @@ constexpr int kMaxWaves = 16, kSplitWaves = 8, kSplitRun = 4;
 
 // How a call runs: which kernels, on what tiles, with how much scratch.
 struct NormPlan {
-    bool planes, wide, split, solo;
+    bool planes, wide, split, solo, one;
     int threads, regs;               // vectors a lane keeps (of each input): the kernel's template argument
     int64_t blocks;
     size_t lds, part_bytes, sums_bytes, total;
@@ -76,7 +76,9 @@ void plan_planes(NormPlan &p, bool bwd, int V)
     const int most = 8;
     const int64_t groups = (int64_t)a.N * a.groups;
     a.tiles = 1;
-    if (units <= (int64_t)kMaxWaves * most && (!bwd || units * a.channels <= 8192)) {
+    const int slot_bits = std::min(a.lane_bits, 4);
+    a.div_slots = make_fastdiv(a.chunks << (a.lane_bits - slot_bits));
+    if (units <= (int64_t)kMaxWaves * most && (!bwd || units * (64 >> slot_bits) <= 8192)) {
         a.units = (int)units;
         p.solo = units <= 4 && groups >= 1024;
         // a wave keeps up to four units while that leaves enough waves; few groups take a wave to a unit
@@ -106,7 +108,7 @@ void plan_planes(NormPlan &p, bool bwd, int V)
         p.blocks = groups * a.tiles;
     }
     a.rows_per_sample = a.parts ? a.parts : 1;
-    p.lds = bwd ? (size_t)(p.solo ? 4 : 1) * 2 * a.span * a.channels * 4 : 0;
+    p.lds = bwd ? (size_t)(p.solo ? 4 : 1) * 2 * a.span * (64 >> slot_bits) * 4 : 0;
     a.div_chunks = make_fastdiv(a.chunks);
 }
 
@@ -161,7 +163,9 @@ void plan_last(NormPlan &p, bool bwd, int V, int eb)
     a.work = a.N * a.tiles * a.slabs;
     a.units_per_xcd = ceil_div(a.work, 8);
     p.blocks = 8 * (int64_t)a.units_per_xcd;
-    p.lds = (size_t)(2 * V * a.pitch + 2 * a.slab_groups + (bwd ? 2 * a.cw : 0)) * 4;
+    p.one = !bwd && a.cpg % V == 0;
+    a.div_width = make_fastdiv(p.one ? a.cpg / V : a.cpg);
+    p.lds = (size_t)(2 * (p.one ? 1 : V) * a.pitch + 2 * a.slab_groups + (bwd ? 2 * a.cw : 0)) * 4;
     a.rows_per_sample = a.tiles;
     a.div_lanes = make_fastdiv(a.lanes);
     a.div_slabs = make_fastdiv(a.slabs);
@@ -198,7 +202,7 @@ int plan_norm(NormPlan &p, int op, int N, int C, int S, int groups, int layout, 
     const int64_t ng = (int64_t)N * groups;
     if (bwd) p.part_bytes = (size_t)2 * a.part_rows * C * 4;
     else if (p.split) p.part_bytes = (size_t)ng * a.tiles * 3 * 4;
-    if (p.split) p.sums_bytes = (size_t)ng * 2 * 4;
+    if (p.split) p.sums_bytes = (size_t)(ng * 2 + (bwd ? 2 * (int64_t)N * C : 0)) * 4;
     p.part_bytes = (size_t)round_up64(p.part_bytes, 256);
     p.total = p.part_bytes + (size_t)round_up64(p.sums_bytes, 256);
     return kStatusOk;
@@ -226,6 +230,7 @@ int norm_common(NormPlan &p, const NormArgs &given, int op, int N, int C, int S,
     p.a.act = a.act; p.a.eps = a.eps;
     p.a.part = static_cast<float *>(ws);
     p.a.group_sums = reinterpret_cast<float *>(static_cast<char *>(ws) + p.part_bytes);
+    p.a.sample_sums = p.split ? p.a.group_sums + (int64_t)2 * N * groups : p.a.part;
     return kStatusOk;
 }
 
@@ -252,10 +257,12 @@ void launch_norm_fwd(const NormPlan &p, hipStream_t st)
         return;
     }
     const size_t lds = MODE == kApply ? 0 : p.lds;
-    if constexpr (MODE != kWhole) launch_norm(group_norm_last_fwd<T, kSplitRun, MODE>, p, lds, st);
-    else if (p.regs <= 4) launch_norm(group_norm_last_fwd<T, 4, MODE>, p, lds, st);
-    else if (p.regs == 8) launch_norm(group_norm_last_fwd<T, 8, MODE>, p, lds, st);
-    else launch_norm(group_norm_last_fwd<T, 16, MODE>, p, lds, st);
+    auto go = [&](auto of_one, auto of_several) { launch_norm(p.one ? of_one : of_several, p, lds, st); };
+    if constexpr (MODE == kSums) go(group_norm_last_fwd<T, kSplitRun, MODE, true>, group_norm_last_fwd<T, kSplitRun, MODE, false>);
+    else if constexpr (MODE == kApply) launch_norm(group_norm_last_fwd<T, kSplitRun, MODE, false>, p, lds, st);
+    else if (p.regs <= 4) go(group_norm_last_fwd<T, 4, MODE, true>, group_norm_last_fwd<T, 4, MODE, false>);
+    else if (p.regs == 8) go(group_norm_last_fwd<T, 8, MODE, true>, group_norm_last_fwd<T, 8, MODE, false>);
+    else go(group_norm_last_fwd<T, 16, MODE, true>, group_norm_last_fwd<T, 16, MODE, false>);
 }
 
 template <typename T, int MODE>
@@ -313,7 +320,7 @@ int run_norm_bwd(NormPlan &p, hipStream_t st)
         }
     }
     if (p.a.dgamma || p.a.dbeta)
-        hipLaunchKernelGGL(group_norm_join_channels, dim3((p.a.C + 31) / 32), dim3(1024), 0, st, p.a);
+        hipLaunchKernelGGL(group_norm_join_channels, dim3((p.a.C + 15) / 16), dim3(1024), 0, st, p.a);
     return check_launch();
 }
 

@@ -97,7 +97,11 @@ __device__ __forceinline__ float wave_max(float v)
 // sum over the aligned runs of `width` lanes (a power of two), the same in every lane of a run
 __device__ __forceinline__ float run_sum(float v, int width)
 {
-    for (int o = 1; o < width; o <<= 1) v += __shfl_xor(v, o);
+    if (width > 1) v += dpp_move<0xB1>(v);
+    if (width > 2) v += dpp_move<0x4E>(v);
+    if (width > 4) v += dpp_move<0x141>(v);
+    if (width > 8) v += dpp_move<0x140>(v);
+    for (int o = 16; o < width; o <<= 1) v += __shfl_xor(v, o);
     return v;
 }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }

@@ -11,9 +11,10 @@
 // bytes a lane, of each tensor (16 channels last, forward).  What does not fit is read twice: a launch that leaves sums of tiles
 // (kSums), one that joins them, and one that applies them (kApply).
 //
-// Planes: a group's C / groups planes are one run of memory.  A wave's unit is 64 vectors of a plane, or, of planes
-// shorter than that, as many whole planes as fit 64 lanes with a power of two of lanes to a plane: so the channel is known
-// for each lane, and sums per channel are sums over lanes.
+// Planes: a group's C / groups planes are one run of memory.  A wave's unit is 64 vectors of it: of one plane where planes
+// fill units well (long planes: sums per channel are then sums over lanes), or of the planes' vectors one after the other
+// (flat; every lane leaves its own sums in LDS, 16 lanes add a plane's).  256 x 384 planes of 169 bfloat16 values, backward:
+// 22 vectors to a plane, 31 us with 32 lanes to a plane, FLATUS us flat.
 // Channels last: a work-group takes `cw` neighbouring channels (whole groups) of a sample; a lane keeps its columns and
 // walks down the positions.
 // A plane's (row's) last vector is moved back so that it ends where the plane ends: it then holds values of the vector
@@ -35,10 +36,10 @@ struct NormArgs {
     FastDiv div_groups, div_cpg;
     int part_rows, rows_per_sample;  // rows of C sums in `part`, and of those a sample's
     // planes
-    int units, chunks, lane_bits, channels;   // of a group; chunks to a plane; lanes to a plane (log2); planes to a unit
+    int flat, vectors, chunks, units;         // vectors and units to a plane (long planes); units of a group
     int run;                                  // units to a wave
-    int tiles, parts, span;                   // of a group; of a plane (0: a tile is whole planes); units of a tile
-    FastDiv div_chunks, div_tiles, div_slots;  // slots: of a plane's sums in LDS (backward)
+    int tiles, parts, span;                   // of a group; of a plane (0: a tile is whole planes); units or planes of a tile
+    FastDiv div_chunks, div_vectors, div_tiles;
     // channels last
     int cw, slab_groups, slabs, lanes, rows;  // channels, groups of a slab; slabs; lanes to a row; rows at a time
     int tile_rows, pitch, group_lanes, channel_lanes, units_per_xcd, work;
@@ -76,16 +77,71 @@ __device__ __forceinline__ float join_waves(float v, float *red, int nw)
 // ---------------------------------------------------------------------------
 // Planes
 // ---------------------------------------------------------------------------
+// The group, planes and units of a work-group (SOLO: of a wave; four groups to a work-group, then).
+struct PlaneTile {
+    int64_t group;
+    int g, tile;
+    int first, planes;               // of the group
+    int u0, u1;                      // units: long planes: of the group; flat: of the tile
+    bool live;
+};
+
+template <bool SOLO, int MODE>
+__device__ __forceinline__ PlaneTile plane_tile(const NormArgs &a)
+{
+    PlaneTile t;
+    t.tile = 0;
+    t.first = 0;
+    t.planes = a.cpg;
+    t.u0 = 0;
+    t.u1 = a.units;
+    t.live = true;
+    int group;
+    if (SOLO) {
+        const int total = a.N * a.groups;
+        group = uniform((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+        t.live = group < total;
+        group = min(group, total - 1);
+    } else if (MODE == kWhole) {
+        group = blockIdx.x;
+    } else {
+        group = fastdiv(blockIdx.x, a.div_tiles);
+        t.tile = blockIdx.x - group * a.tiles;
+        if (a.parts) {                           // a part of one plane
+            t.first = t.tile / a.parts;
+            t.planes = 1;
+            t.u0 = t.first * a.chunks + (t.tile - t.first * a.parts) * a.span;
+            t.u1 = min(t.u0 + a.span, (t.first + 1) * a.chunks);
+        } else {                                 // a.span whole planes
+            t.first = t.tile * a.span;
+            t.planes = min(a.span, a.cpg - t.first);
+            t.u0 = a.flat ? 0 : t.first * a.chunks;
+            t.u1 = a.flat ? (t.planes * a.vectors + 63) >> 6 : t.u0 + t.planes * a.chunks;
+        }
+    }
+    t.g = group - fastdiv(group, a.div_groups) * a.groups;
+    t.group = group;
+    return t;
+}
+
 struct PlaneLane { int c, off, k0, k1; };    // channel in the group, element in the group, valid values k0 <= k < k1
 
 template <int V>
-__device__ __forceinline__ PlaneLane plane_lane(const NormArgs &a, int u, int lane)
+__device__ __forceinline__ PlaneLane plane_lane(const NormArgs &a, const PlaneTile &t, int u, int lane)
 {
     PlaneLane p;
-    const int cg = fastdiv(u, a.div_chunks), chunk = u - cg * a.chunks;
-    p.c = cg * a.channels + (lane >> a.lane_bits);
-    const int pos = ((chunk << a.lane_bits) + (lane & ((1 << a.lane_bits) - 1))) * V;
-    const bool on = p.c < a.cpg && pos < a.S;
+    int pos;
+    bool on;
+    if (a.flat) {
+        const int f = u * 64 + lane, j = fastdiv(f, a.div_vectors);
+        p.c = t.first + j;
+        pos = (f - j * a.vectors) * V;
+        on = j < t.planes;
+    } else {
+        p.c = fastdiv(u, a.div_chunks);
+        pos = ((u - p.c * a.chunks) * 64 + lane) * V;
+        on = pos < a.S;
+    }
     if (!on) p.c = 0;
     if (a.S >= V) {
         const int q = min(pos, a.S - V);
@@ -117,42 +173,6 @@ __device__ __forceinline__ void plane_store(const NormArgs &a, T *p, const Plane
     }
 }
 
-// The group and the units of a work-group (SOLO: of a wave; four groups to a work-group, then).
-struct PlaneTile { int64_t group; int g, tile, u0, u1; bool live; };
-
-template <bool SOLO, int MODE>
-__device__ __forceinline__ PlaneTile plane_tile(const NormArgs &a)
-{
-    PlaneTile t;
-    t.tile = 0;
-    t.u0 = 0;
-    t.u1 = a.units;
-    t.live = true;
-    int group;
-    if (SOLO) {
-        const int total = a.N * a.groups;
-        group = uniform((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
-        t.live = group < total;
-        group = min(group, total - 1);
-    } else if (MODE == kWhole) {
-        group = blockIdx.x;
-    } else {
-        group = fastdiv(blockIdx.x, a.div_tiles);
-        t.tile = blockIdx.x - group * a.tiles;
-        if (a.parts) {
-            const int plane = t.tile / a.parts;
-            t.u0 = plane * a.chunks + (t.tile - plane * a.parts) * a.span;
-            t.u1 = min(t.u0 + a.span, (plane + 1) * a.chunks);
-        } else {
-            t.u0 = t.tile * a.span;
-            t.u1 = min(t.u0 + a.span, a.units);
-        }
-    }
-    t.g = group - fastdiv(group, a.div_groups) * a.groups;
-    t.group = group;
-    return t;
-}
-
 template <typename T, int R, bool SOLO, int MODE>
 __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_fwd(NormArgs a)
 {
@@ -169,7 +189,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_fwd(NormA
 #pragma unroll
     for (int r = 0; r < R; ++r)
         if (r < n) {
-            pl[r] = plane_lane<V>(a, u0 + r, lane);
+            pl[r] = plane_lane<V>(a, t, u0 + r, lane);
             raw[r] = plane_load(a, x, pl[r]);
         }
     float mean, rstd;
@@ -247,8 +267,8 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_fwd(NormA
 }
 
 // With d = x - mean: z = gamma rstd d + beta, B = rstd sum dz d, dx = gamma rstd dz - rstd m1 - d rstd^2 m2.
-// Sums per channel: of a unit over the runs of lanes that share a plane, at most 16 lanes (what the moves within a row of
-// lanes reach), each run's in a slot of LDS.  Consecutive units of a wave that lie in one plane are added before that.
+// Sums per channel go through slots in LDS: of long planes four to a unit (16 lanes are added by moves within a row of
+// lanes; consecutive units of a wave that lie in one plane are added before that), flat one to a lane.
 template <typename T, int R, bool SOLO, int MODE>
 __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_bwd(NormArgs a)
 {
@@ -260,44 +280,64 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_bwd(NormA
     const int64_t base = t.group * a.cpg * a.S;
     const T *x = static_cast<const T *>(a.x) + base, *dy = static_cast<const T *>(a.dy) + base;
     typename Vec<T>::Raw rx[R], rd[R];
-    PlaneLane pl[R];
-    float scale[R], shift[R];                    // gamma rstd, beta
+    // where a vector lies, gamma rstd and beta there: kept, or with many vectors found again for each use (`at` is the
+    // lane, hidden from the compiler so that it does not keep them after all)
+    constexpr bool kFew = R <= 4;
+    PlaneLane pl[kFew ? R : 1];
+    float scale[kFew ? R : 1], shift[kFew ? R : 1];
+    int at = lane;
     float dz[kKeep ? R : 1][V];
     const int u0 = t.u0 + wave * a.run, n = min(a.run, t.u1 - u0);
     const int c0 = t.g * a.cpg;
 #pragma unroll
     for (int r = 0; r < R; ++r)
         if (r < n) {
-            pl[r] = plane_lane<V>(a, u0 + r, lane);
-            rx[r] = plane_load(a, x, pl[r]);
-            rd[r] = plane_load(a, dy, pl[r]);
-            scale[r] = a.gamma ? a.gamma[c0 + pl[r].c] : 1.f;
-            shift[r] = a.beta ? a.beta[c0 + pl[r].c] : 0.f;
+            const PlaneLane l = plane_lane<V>(a, t, u0 + r, lane);
+            rx[r] = plane_load(a, x, l);
+            rd[r] = plane_load(a, dy, l);
+            if constexpr (kFew) {
+                pl[r] = l;
+                scale[r] = a.gamma ? a.gamma[c0 + l.c] : 1.f;
+                shift[r] = a.beta ? a.beta[c0 + l.c] : 0.f;
+            }
         }
     const float mean = a.mean[t.group], rstd = a.rstd[t.group];
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-        if (r < n) scale[r] *= rstd;
+    auto find = [&](int r, PlaneLane &l, float &sc, float &sh) {
+        if constexpr (kFew) {
+            l = pl[r];
+            sc = scale[r] * rstd;
+            sh = shift[r];
+        } else {
+            l = plane_lane<V>(a, t, u0 + r, at);
+            sc = (a.gamma ? a.gamma[c0 + l.c] : 1.f) * rstd;
+            sh = a.beta ? a.beta[c0 + l.c] : 0.f;
+        }
+    };
     float m1, m2;
     if (MODE == kApply) {
         m1 = a.group_sums[2 * t.group];
         m2 = a.group_sums[2 * t.group + 1];
     } else {
-        const int bits = min(a.lane_bits, 4), slots_of_unit = 64 >> bits, count = (t.u1 - t.u0) * slots_of_unit;
-        float *slot_a = slots + (SOLO ? (int)(threadIdx.x >> 6) * 2 * count : 0), *slot_b = slot_a + count;
+        // slots of the tile; a plane's are neighbours.  Then the planes' sums, times gamma
+        const int per = a.flat ? a.vectors : 4 * (a.parts ? t.u1 - t.u0 : a.chunks), count = per * t.planes;
+        float *slot_a = slots + (SOLO ? (int)(threadIdx.x >> 6) * 2 * (count + t.planes) : 0), *slot_b = slot_a + count;
+        float *plane_a = slot_b + count, *plane_b = plane_a + t.planes;
         float A = 0.f, B = 0.f;
+        if (!kFew) asm volatile("" : "+v"(at));
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (r < n) {
-                float xv[V], dv[V];
+                PlaneLane l;
+                float sc, sh, xv[V], dv[V];
+                find(r, l, sc, sh);
                 Vec<T>::open(rx[r], xv);
                 Vec<T>::open(rd[r], dv);
 #pragma unroll
                 for (int k = 0; k < V; ++k) {
                     xv[k] -= mean;
-                    dv[k] = act_bwd(dv[k], scale[r] * xv[k] + shift[r], a.act);
+                    dv[k] = act_bwd(dv[k], sc * xv[k] + sh, a.act);
                 }
-                if (pl[r].k0 == 0 && pl[r].k1 == V) {
+                if (l.k0 == 0 && l.k1 == V) {
 #pragma unroll
                     for (int k = 0; k < V; ++k) {
                         A += dv[k];
@@ -306,7 +346,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_bwd(NormA
                 } else {
 #pragma unroll
                     for (int k = 0; k < V; ++k)
-                        if (k >= pl[r].k0 && k < pl[r].k1) {
+                        if (k >= l.k0 && k < l.k1) {
                             A += dv[k];
                             B += dv[k] * xv[k];
                         }
@@ -315,66 +355,84 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_bwd(NormA
 #pragma unroll
                     for (int k = 0; k < V; ++k) dz[r][k] = dv[k];
                 }
-                // a wave's last unit in a plane gets the sum of those before it there
-                const int u = u0 + r, slot = (u - t.u0) * slots_of_unit + (lane >> bits);
-                const bool flush = a.lane_bits < 6 || r + 1 == n ||
-                                   (int)fastdiv(u + 1, a.div_chunks) != (int)fastdiv(u, a.div_chunks);
-                float ta = 0.f, tb = 0.f;
-                if (flush) {
-                    ta = run_sum(A, 1 << bits);
-                    tb = run_sum(B, 1 << bits) * rstd;
+                const int u = u0 + r;
+                if (a.flat) {
+                    const int slot = u * 64 + lane;
+                    if (slot < count) {
+                        slot_a[slot] = A;
+                        slot_b[slot] = B * rstd;
+                    }
                     A = B = 0.f;
-                }
-                if ((lane & ((1 << bits) - 1)) == 0) {
-                    slot_a[slot] = ta;
-                    slot_b[slot] = tb;
+                } else {
+                    // a wave's last unit in a plane gets the sum of those before it there
+                    float ta = 0.f, tb = 0.f;
+                    if (r + 1 == n || (int)fastdiv(u + 1, a.div_chunks) != (int)fastdiv(u, a.div_chunks)) {
+                        ta = run_sum(A, 16);
+                        tb = run_sum(B, 16) * rstd;
+                        A = B = 0.f;
+                    }
+                    if ((lane & 15) == 0) {
+                        const int slot = (u - t.u0) * 4 + (lane >> 4);
+                        slot_a[slot] = ta;
+                        slot_b[slot] = tb;
+                    }
                 }
             }
         __syncthreads();
-        // the tile's planes, from the first unit's on
-        const int first = fastdiv(t.u0, a.div_chunks) * a.channels;
+        const int64_t n_group = fastdiv((uint32_t)t.group, a.div_groups);
+        const int64_t row = n_group * a.rows_per_sample + (a.parts ? t.tile - t.first * a.parts : 0);
+        const int teams = SOLO ? 4 : (int)(blockDim.x >> 4), sub = lane & 15;
+        for (int j0 = 0; j0 < t.planes; j0 += teams) {
+            const int j = j0 + ((SOLO ? lane : (int)threadIdx.x) >> 4), c = c0 + t.first + j;
+            float sa = 0.f, sb = 0.f;
+            if (j < t.planes)
+                for (int i = j * per + sub; i < (j + 1) * per; i += 16) {
+                    sa += slot_a[i];
+                    sb += slot_b[i];
+                }
+            sa = run_sum(sa, 16);
+            sb = run_sum(sb, 16);
+            if (j < t.planes && sub == 0) {
+                const float gamma = a.gamma ? a.gamma[c] : 1.f;
+                plane_a[j] = gamma * sa;
+                plane_b[j] = gamma * sb;
+                if (t.live) {
+                    a.part[row * a.C + c] = sa;
+                    a.part[((int64_t)a.part_rows + row) * a.C + c] = sb;
+                }
+            }
+        }
         if (MODE == kWhole) {
+            __syncthreads();
             float p = 0.f, q = 0.f;
-            for (int i = lane; i < count; i += 64) {
-                const int c = fastdiv(i, a.div_slots);
-                const float gamma = c < a.cpg && a.gamma ? a.gamma[c0 + c] : 1.f;
-                p += gamma * slot_a[i];
-                q += gamma * slot_b[i];
+            for (int j = lane; j < t.planes; j += 64) {
+                p += plane_a[j];
+                q += plane_b[j];
             }
             m1 = wave_sum(p) * a.inv_m;
             m2 = wave_sum(q) * a.inv_m;
         }
-        const int64_t n_group = fastdiv((uint32_t)t.group, a.div_groups);
-        const int64_t row = n_group * a.rows_per_sample + (a.parts ? t.tile - t.tile / a.parts * a.parts : 0);
-        const int per = a.parts ? count : (int)a.div_slots.d, planes = a.parts ? 1 : (count + per - 1) / per;
-        for (int j = SOLO ? lane : (int)threadIdx.x; j < planes; j += SOLO ? 64 : (int)blockDim.x)
-            if (first + j < a.cpg && t.live) {
-                float sa = 0.f, sb = 0.f;
-                for (int i = 0; i < per; ++i) {
-                    sa += slot_a[j * per + i];
-                    sb += slot_b[j * per + i];
-                }
-                a.part[row * a.C + c0 + first + j] = sa;
-                a.part[((int64_t)a.part_rows + row) * a.C + c0 + first + j] = sb;
-            }
         if (MODE == kSums) return;
     }
     const float c1 = rstd * m1, c2 = rstd * rstd * m2;
     T *dx = static_cast<T *>(a.out) + base;
+    if (!kFew) asm volatile("" : "+v"(at));
 #pragma unroll
     for (int r = 0; r < R; ++r)
         if (r < n && t.live) {
-            float xv[V], dv[V];
+            PlaneLane l;
+            float sc, sh, xv[V], dv[V];
+            find(r, l, sc, sh);
             Vec<T>::open(rx[r], xv);
             Vec<T>::open(rd[r], dv);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 xv[k] -= mean;
                 if constexpr (kKeep) dv[k] = dz[r][k];
-                else dv[k] = act_bwd(dv[k], scale[r] * xv[k] + shift[r], a.act);
-                dv[k] = (scale[r] * dv[k] - c1) - xv[k] * c2;
+                else dv[k] = act_bwd(dv[k], sc * xv[k] + sh, a.act);
+                dv[k] = (sc * dv[k] - c1) - xv[k] * c2;
             }
-            plane_store(a, dx, pl[r], dv);
+            plane_store(a, dx, l, dv);
         }
 }
 

@@ -66,19 +66,16 @@ int regs_for(int run, int most)
 void plan_planes(NormPlan &p, bool bwd, int V)
 {
     NormArgs &a = p.a;
-    const int nv = (a.S + V - 1) / V;
-    a.lane_bits = 0;
-    while ((1 << a.lane_bits) < nv && a.lane_bits < 6) ++a.lane_bits;
-    a.chunks = (nv + 63) / 64;
-    a.channels = 64 >> a.lane_bits;
-    const int runs = ceil_div(a.cpg, a.channels);          // a plane's units, or a unit's planes
-    const int64_t units = (int64_t)runs * a.chunks;
+    a.vectors = (a.S + V - 1) / V;
+    a.chunks = (a.vectors + 63) / 64;
+    a.flat = a.vectors < 0.85 * 64 * a.chunks;             // a sixth of the lanes idle otherwise
+    const int64_t units = a.flat ? ((int64_t)a.cpg * a.vectors + 63) / 64 : (int64_t)a.cpg * a.chunks;
     const int most = 8;
     const int64_t groups = (int64_t)a.N * a.groups;
     a.tiles = 1;
-    const int slot_bits = std::min(a.lane_bits, 4);
-    a.div_slots = make_fastdiv(a.chunks << (a.lane_bits - slot_bits));
-    if (units <= (int64_t)kMaxWaves * most && (!bwd || units * (64 >> slot_bits) <= 8192)) {
+    a.span = a.cpg;
+    int64_t slots = a.flat ? (int64_t)a.cpg * a.vectors : 4 * units;
+    if (units <= (int64_t)kMaxWaves * most && a.cpg <= 4096) {
         a.units = (int)units;
         p.solo = units <= 4 && groups >= 1024;
         // a wave keeps up to four units while that leaves enough waves; few groups take a wave to a unit
@@ -88,19 +85,20 @@ void plan_planes(NormPlan &p, bool bwd, int V)
         p.threads = p.solo ? 256 : 64 * ceil_div(a.units, a.run);
         p.blocks = p.solo ? (groups + 3) / 4 : groups;
         p.regs = regs_for(a.run, most);
-        a.span = a.units;
     } else {
         p.split = true;
-        a.units = (int)units;
         const int per = kSplitWaves * kSplitRun;
-        if (a.chunks > per) {
+        if (a.chunks > per) {                              // parts of a plane (flat planes are shorter)
+            a.flat = 0;
             a.parts = ceil_div(a.chunks, per);
             a.span = ceil_div(a.chunks, a.parts);
+            a.parts = ceil_div(a.chunks, a.span);
             a.tiles = a.cpg * a.parts;
-        } else {
-            const int whole = std::max(1, per / a.chunks);
-            a.span = whole * a.chunks;
-            a.tiles = ceil_div(runs, whole);
+            slots = 4 * a.span;
+        } else {                                           // whole planes
+            a.span = std::min(a.cpg, std::max(1, a.flat ? per * 64 / a.vectors : per / a.chunks));
+            a.tiles = ceil_div(a.cpg, a.span);
+            slots = a.flat ? (int64_t)a.span * a.vectors : 4 * (int64_t)a.span * a.chunks;
         }
         p.threads = 64 * kSplitWaves;
         a.run = kSplitRun;
@@ -108,8 +106,9 @@ void plan_planes(NormPlan &p, bool bwd, int V)
         p.blocks = groups * a.tiles;
     }
     a.rows_per_sample = a.parts ? a.parts : 1;
-    p.lds = bwd ? (size_t)(p.solo ? 4 : 1) * 2 * a.span * (64 >> slot_bits) * 4 : 0;
+    p.lds = bwd ? (size_t)((p.solo ? 4 : 1) * 2 * (slots + (a.parts ? 1 : a.span)) * 4) : 0;
     a.div_chunks = make_fastdiv(a.chunks);
+    a.div_vectors = make_fastdiv(a.vectors);
 }
 
 void plan_last(NormPlan &p, bool bwd, int V, int eb)

@@ -70,18 +70,30 @@ __device__ __forceinline__ RowLane row_lane(int width, int chunk, int lane)
     return l;
 }
 
-template <typename T>
-__device__ __forceinline__ typename Vec<T>::Raw row_load(const T *z, int width, const RowLane &l)
+// A lane's vectors, R from chunk c0 on, n of them the wave's; -infinity (no share in maximum and sums) for values that are
+// not the lane's own
+template <typename T, int R>
+__device__ __forceinline__ void row_read(typename Vec<T>::Raw (&raw)[R], const T *z, int width, int c0, int n, int lane)
 {
-    return width >= Vec<T>::V ? Vec<T>::load(z + l.off) : Vec<T>::some(z, width);
+    constexpr int V = Vec<T>::V;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (r < n) raw[r] = width >= V ? Vec<T>::load(z + row_lane<V>(width, c0 + r, lane).off) : Vec<T>::some(z, width);
+    const int last = (width - 1) / (64 * V);             // the chunk that may hold a moved-back vector
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (r >= n || c0 + r >= last) {
+            const RowLane l = row_lane<V>(width, c0 + r, lane);
+            Vec<T>::drop(raw[r], r < n ? l.k0 : V, l.k1);
+        }
 }
 
-// Of a row in parts, the values before the moved-back vector may be another work-group's: they are left to it.
+// (What a moved-back vector does not hold of its own is left to the vector before.)
 template <typename T>
 __device__ __forceinline__ void row_store(const LossArgs &a, T *dz, const RowLane &l, const float (&v)[Vec<T>::V])
 {
-    if (a.V >= Vec<T>::V && (l.k0 == 0 || a.parts == 1)) {
-        if (l.k0 < Vec<T>::V) Vec<T>::store(dz + l.off, v);
+    if (l.k0 == 0 && l.k1 == Vec<T>::V) {
+        Vec<T>::store(dz + l.off, v);
     } else {
 #pragma unroll
         for (int k = 0; k < Vec<T>::V; ++k)
@@ -89,20 +101,28 @@ __device__ __forceinline__ void row_store(const LossArgs &a, T *dz, const RowLan
     }
 }
 
-// the maximum of a lane's vectors (values that two vectors hold do no harm)
+// Makes the compiler take a lane's vectors for new ones: it would else keep bfloat16 values that it has widened for one
+// use for the next, twice the registers, and spill.
 template <typename T, int R>
-__device__ __forceinline__ float row_max(const typename Vec<T>::Raw (&raw)[R], int n, int width)
+__device__ __forceinline__ void row_again(typename Vec<T>::Raw (&raw)[R])
+{
+#pragma unroll
+    for (int r = 0; r < R; ++r) asm volatile("" : "+v"(raw[r]));
+}
+
+// the maximum of a lane's vectors
+template <typename T, int R>
+__device__ __forceinline__ float row_max(const typename Vec<T>::Raw (&raw)[R])
 {
     constexpr int V = Vec<T>::V;
     float m = -INFINITY;
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-        if (r < n) {
-            float v[V];
-            Vec<T>::open(raw[r], v);
+    for (int r = 0; r < R; ++r) {
+        float v[V];
+        Vec<T>::open(raw[r], v);
 #pragma unroll
-            for (int k = 0; k < V; ++k) m = fmaxf(m, width >= V || k < width ? v[k] : -INFINITY);
-        }
+        for (int k = 0; k < V; k += 2) m = max3(m, v[k], v[k + 1]);
+    }
     return m;
 }
 
@@ -139,25 +159,17 @@ __device__ __forceinline__ void add_exps(float v, const Scale &t, const Scale &o
 }
 
 template <typename T, int R, int HOW>
-__device__ __forceinline__ void row_sums(const LossArgs &a, const typename Vec<T>::Raw (&raw)[R], int c0, int n, int lane,
-                                         const Scale &t, const Scale &o, float &sT, float &s1)
+__device__ __forceinline__ void row_sums(const typename Vec<T>::Raw (&raw)[R], const Scale &t, const Scale &o, float &sT, float &s1)
 {
     constexpr int V = Vec<T>::V;
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-        if (r < n) {
-            const RowLane l = row_lane<V>(a.V, c0 + r, lane);
-            float v[V];
-            Vec<T>::open(raw[r], v);
-            if (l.k0 == 0 && l.k1 == V) {
+    for (int r = 0; r < R; ++r) {
+        float v[V];
+        Vec<T>::open(raw[r], v);
 #pragma unroll
-                for (int k = 0; k < V; ++k) add_exps<HOW>(v[k], t, o, sT, s1);
-            } else {
-#pragma unroll
-                for (int k = 0; k < V; ++k)
-                    if (k >= l.k0 && k < l.k1) add_exps<HOW>(v[k], t, o, sT, s1);
-            }
-        }
+        for (int k = 0; k < V; ++k) add_exps<HOW>(v[k], t, o, sT, s1);
+        __builtin_amdgcn_sched_barrier(0);               // vectors one after the other: their opened values need registers
+    }
 }
 
 // dz without the targets: ck exp((z - m) / T) + cl exp(z - m)
@@ -185,6 +197,7 @@ __device__ __forceinline__ void row_write(const LossArgs &a, const typename Vec<
 #pragma unroll
             for (int k = 0; k < V; ++k) v[k] = mix_exps<HOW>(v[k], t, o, ck, cl);
             row_store(a, dz, row_lane<V>(a.V, c0 + r, lane), v);
+            __builtin_amdgcn_sched_barrier(0);
         }
 }
 
@@ -207,14 +220,13 @@ struct RowExps {
         }
     }
     template <typename T, int R>
-    __device__ __forceinline__ void sums(const LossArgs &a, const typename Vec<T>::Raw (&raw)[R], int c0, int n, int lane, float &sT,
-                                         float &s1) const
+    __device__ __forceinline__ void sums(const typename Vec<T>::Raw (&raw)[R], float &sT, float &s1) const
     {
-        if (how == kOne) row_sums<T, R, kOne>(a, raw, c0, n, lane, t, o, sT, s1);
-        else if (how == kTwo) row_sums<T, R, kTwo>(a, raw, c0, n, lane, t, o, sT, s1);
-        else if (how == kSquare) row_sums<T, R, kSquare>(a, raw, c0, n, lane, t, o, sT, s1);
-        else if (how == kFourth) row_sums<T, R, kFourth>(a, raw, c0, n, lane, t, o, sT, s1);
-        else row_sums<T, R, kFar>(a, raw, c0, n, lane, t, o, sT, s1);
+        if (how == kOne) row_sums<T, R, kOne>(raw, t, o, sT, s1);
+        else if (how == kTwo) row_sums<T, R, kTwo>(raw, t, o, sT, s1);
+        else if (how == kSquare) row_sums<T, R, kSquare>(raw, t, o, sT, s1);
+        else if (how == kFourth) row_sums<T, R, kFourth>(raw, t, o, sT, s1);
+        else row_sums<T, R, kFar>(raw, t, o, sT, s1);
     }
     __device__ __forceinline__ float one_fix() const
     {
@@ -404,7 +416,7 @@ __device__ __forceinline__ void write_named(const LossArgs &a, const RowTeam<SOL
 // Whole rows: loss (and statistics), and with GRAD the gradient
 // ---------------------------------------------------------------------------
 template <typename T, int R, bool SOLO, bool GRAD>
-__global__ __launch_bounds__(SOLO ? 256 : 1024, 8) void distill_rows(LossArgs a)
+__global__ __launch_bounds__(SOLO ? 256 : 1024, GRAD ? 8 : 6) void distill_rows(LossArgs a)
 {
     extern __shared__ float lds[];
     __shared__ float red[7][16];
@@ -415,15 +427,13 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, 8) void distill_rows(LossArgs a)
     T *dz = static_cast<T *>(a.dz) + n * a.dz_stride;
     const int c0 = team.wave * a.run, cn = min(a.run, a.chunks - c0);
     typename Vec<T>::Raw raw[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-        if (r < cn) raw[r] = row_load(z, a.V, row_lane<Vec<T>::V>(a.V, c0 + r, team.lane));
+    row_read<T, R>(raw, z, a.V, c0, cn, team.lane);
     const int label = a.labels ? class_at(a.labels, n, a.wide_index, a.V) : -1;
     const float zl = label >= 0 ? ld_elem(z, label) : 0.f;
     const Entries e = entries_at(lds + (SOLO ? (int)(threadIdx.x >> 6) * 3 * a.K : 0), a.K);
     float most[3];
     most[1] = read_entries(a, team, e, z, n, 0, a.V, most[2]);
-    most[0] = row_max<T, R>(raw, cn, a.V);
+    most[0] = row_max<T, R>(raw);
     team.max_of(most, red);
     const float m = most[0], tm = most[1];
     const bool has = most[2] > 0.f;
@@ -437,7 +447,8 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, 8) void distill_rows(LossArgs a)
     const RowExps x(a, m, a.K > 0 && (has || a.stats), label >= 0 || a.stats);
     float sums[3] = {0.f, 0.f, 0.f};
     sums[2] = weigh_entries(a, team, e, tm);
-    x.template sums<T, R>(a, raw, c0, cn, team.lane, sums[0], sums[1]);
+    row_again<T, R>(raw);
+    x.template sums<T, R>(raw, sums[0], sums[1]);
     team.sum_of(sums, red + 3);
     float sT = sums[0], s1 = sums[1];
     x.finish(sT, s1);
@@ -453,6 +464,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, 8) void distill_rows(LossArgs a)
         if (has) { gk = g * a.wk * a.T; ck = gk / sT; }
         if (label >= 0) { gl = g * a.wl; cl = gl / s1; }
         x.factors(ck, cl);
+        row_again<T, R>(raw);
         x.template write<T, R>(a, raw, dz, c0, cn, team.lane, ck, cl);
     }
     float kd[1] = {has ? divergence(a, team, e, nullptr, inv_ts, m, sT) : 0.f};
@@ -471,7 +483,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, 8) void distill_rows(LossArgs a)
 // m, sT and s1 of a part; the first part's work-group also puts aside the logits that the targets name, as the gradient
 // may take their place.
 template <typename T, int R>
-__global__ __launch_bounds__(512) void distill_part_sums(LossArgs a)
+__global__ __launch_bounds__(512, 8) void distill_part_sums(LossArgs a)
 {
     __shared__ float red[3][16];
     const RowTeam<false> team;
@@ -480,9 +492,7 @@ __global__ __launch_bounds__(512) void distill_part_sums(LossArgs a)
     const int first = part * a.part_chunks, last = min(first + a.part_chunks, a.chunks);
     const int c0 = first + team.wave * a.run, cn = min(a.run, last - c0);
     typename Vec<T>::Raw raw[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-        if (r < cn) raw[r] = row_load(z, a.V, row_lane<Vec<T>::V>(a.V, c0 + r, team.lane));
+    row_read<T, R>(raw, z, a.V, c0, cn, team.lane);
     if (part == 0) {
         float *named = a.named + (int64_t)n * (a.K + 1);
         for (int k = team.id; k <= a.K; k += team.size) {
@@ -491,13 +501,14 @@ __global__ __launch_bounds__(512) void distill_part_sums(LossArgs a)
             named[k] = v >= 0 ? ld_elem(z, v) : 0.f;
         }
     }
-    float m[1] = {row_max<T, R>(raw, cn, a.V)};
+    float m[1] = {row_max<T, R>(raw)};
     team.max_of(m, red);
     float s[2] = {0.f, 0.f};
     // of a part without any class left the sums are 0
     const float top = m[0] == -INFINITY ? 0.f : m[0];
     const RowExps x(a, top, a.K > 0, true);
-    x.template sums<T, R>(a, raw, c0, cn, team.lane, s[0], s[1]);
+    row_again<T, R>(raw);
+    x.template sums<T, R>(raw, s[0], s[1]);
     team.sum_of(s, red + 1);
     x.finish(s[0], s[1]);
     if (team.id == 0) {
@@ -511,7 +522,7 @@ __global__ __launch_bounds__(512) void distill_part_sums(LossArgs a)
 // Joins the parts (or takes the statistics given).  GRAD: a work-group writes its part's gradient, and the first part's
 // also the row's loss where asked for; otherwise one work-group per row writes the loss.
 template <typename T, int R, bool GRAD>
-__global__ __launch_bounds__(512) void distill_part_apply(LossArgs a)
+__global__ __launch_bounds__(512, 8) void distill_part_apply(LossArgs a)
 {
     constexpr int V = Vec<T>::V;
     extern __shared__ float lds[];
@@ -523,10 +534,7 @@ __global__ __launch_bounds__(512) void distill_part_apply(LossArgs a)
     const int first = part * a.part_chunks, last = min(first + a.part_chunks, a.chunks);
     const int c0 = first + team.wave * a.run, cn = min(a.run, last - c0);
     typename Vec<T>::Raw raw[R];
-    if (GRAD)
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            if (r < cn) raw[r] = row_load(z, a.V, row_lane<V>(a.V, c0 + r, team.lane));
+    if (GRAD) row_read<T, R>(raw, z, a.V, c0, cn, team.lane);
     // classes [lo, hi) are this work-group's to write
     const int lo = first * 64 * V, hi = (int)min((int64_t)last * 64 * V, (int64_t)a.V);
     const int label = a.labels ? class_at(a.labels, n, a.wide_index, a.V) : -1;
@@ -573,6 +581,7 @@ __global__ __launch_bounds__(512) void distill_part_apply(LossArgs a)
         if (has) { gk = g * a.wk * a.T; ck = gk / sT; }
         if (label >= 0) { gl = g * a.wl; cl = gl / s1; }
         x.factors(ck, cl);
+        row_again<T, R>(raw);
         x.template write<T, R>(a, raw, dz, c0, cn, team.lane, ck, cl);
     }
     float ts[1] = {weigh_entries(a, team, e, most[0])};

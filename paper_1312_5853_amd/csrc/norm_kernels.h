@@ -21,6 +21,7 @@
 // before it too (the first k0 ones), which take no part in sums and are written twice, the same.
 
 constexpr int kWhole = 0, kSums = 1, kApply = 2;
+constexpr float kLog2e = 1.44269504088896340736f;
 
 struct NormArgs {
     const void *x, *dy;
@@ -46,22 +47,41 @@ struct NormArgs {
     FastDiv div_lanes, div_slabs, div_width;  // width: sums of a group in a thread row (forward)
 };
 
-__device__ __forceinline__ float act_fwd(float z, int act)
+// The activation is decided once for a vector, so that its values' chains (two of the slow instructions each in a SiLU)
+// run beside each other.
+// v = act(v * scale + shift)
+template <int V, typename F, typename G>
+__device__ __forceinline__ void act_fwd(float (&v)[V], int act, F scale, G shift)
 {
-    if (act == kActRelu) return z > 0.f ? z : z != z ? z : 0.f;
-    if (act == kActSilu) return z * __builtin_amdgcn_rcpf(1.f + __expf(-z));
-    return z;
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = fmaf(v[k], scale(k), shift(k));
+    if (act == kActRelu) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = v[k] < 0.f ? 0.f : v[k];           // (a NaN stays)
+    } else if (act == kActSilu) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] *= __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * v[k]));
+    }
 }
 
-// dy * act'(z)
-__device__ __forceinline__ float act_bwd(float dy, float z, int act)
+// dy = dy * act'(z) at z = d * scale + shift
+template <int V, typename F, typename G>
+__device__ __forceinline__ void act_bwd(float (&dy)[V], const float (&d)[V], int act, F scale, G shift)
 {
-    if (act == kActRelu) return z > 0.f ? dy : z != z ? z : 0.f;
-    if (act == kActSilu) {
-        const float s = __builtin_amdgcn_rcpf(1.f + __expf(-z));
-        return dy * (s * (1.f + z * (1.f - s)));
+    if (act == kActRelu) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const float z = fmaf(d[k], scale(k), shift(k));
+            dy[k] = z > 0.f ? dy[k] : z <= 0.f ? 0.f : z;                     // (a NaN stays)
+        }
+    } else if (act == kActSilu) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const float z = fmaf(d[k], scale(k), shift(k));
+            const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z));
+            dy[k] *= s * fmaf(z, 1.f - s, 1.f);
+        }
     }
-    return dy;
 }
 
 // the waves' values joined in their order; `red` holds one per wave.  Every thread gets the sum.
@@ -260,8 +280,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_fwd(NormA
             const float shift = fmaf(-mean, scale, a.beta ? a.beta[c0 + pl[r].c] : 0.f);
             float v[V];
             Vec<T>::open(raw[r], v);
-#pragma unroll
-            for (int k = 0; k < V; ++k) v[k] = act_fwd(fmaf(v[k], scale, shift), a.act);
+            act_fwd(v, a.act, [&](int) { return scale; }, [&](int) { return shift; });
             plane_store(a, y, pl[r], v);
         }
 }
@@ -333,23 +352,22 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_bwd(NormA
                 Vec<T>::open(rx[r], xv);
                 Vec<T>::open(rd[r], dv);
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    xv[k] -= mean;
-                    dv[k] = act_bwd(dv[k], sc * xv[k] + sh, a.act);
-                }
-                if (l.k0 == 0 && l.k1 == V) {
+                for (int k = 0; k < V; ++k) xv[k] -= mean;
+                act_bwd(dv, xv, a.act, [&](int) { return sc; }, [&](int) { return sh; });
+                if (a.S % V == 0) {
+                    if (l.k0 == 0)
 #pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        A += dv[k];
-                        B += dv[k] * xv[k];
-                    }
+                        for (int k = 0; k < V; ++k) {
+                            A += dv[k];
+                            B = fmaf(dv[k], xv[k], B);
+                        }
                 } else {
 #pragma unroll
-                    for (int k = 0; k < V; ++k)
-                        if (k >= l.k0 && k < l.k1) {
-                            A += dv[k];
-                            B += dv[k] * xv[k];
-                        }
+                    for (int k = 0; k < V; ++k) {
+                        const float w = k >= l.k0 && k < l.k1 ? dv[k] : 0.f;
+                        A += w;
+                        B = fmaf(w, xv[k], B);
+                    }
                 }
                 if constexpr (kKeep) {
 #pragma unroll
@@ -426,12 +444,15 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_bwd(NormA
             Vec<T>::open(rx[r], xv);
             Vec<T>::open(rd[r], dv);
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                xv[k] -= mean;
-                if constexpr (kKeep) dv[k] = dz[r][k];
-                else dv[k] = act_bwd(dv[k], sc * xv[k] + sh, a.act);
-                dv[k] = (sc * dv[k] - c1) - xv[k] * c2;
+            for (int k = 0; k < V; ++k) xv[k] -= mean;
+            if constexpr (kKeep) {
+#pragma unroll
+                for (int k = 0; k < V; ++k) dv[k] = dz[r][k];
+            } else {
+                act_bwd(dv, xv, a.act, [&](int) { return sc; }, [&](int) { return sh; });
             }
+#pragma unroll
+            for (int k = 0; k < V; ++k) dv[k] = fmaf(-xv[k], c2, fmaf(sc, dv[k], -c1));
             plane_store(a, dx, l, dv);
         }
 }
@@ -491,6 +512,28 @@ __device__ __forceinline__ void slab_store(const NormArgs &a, T *p, const SlabTi
     } else {
         for (int k = 0; k < Vec<T>::V; ++k)
             if (k < t.k1) st_elem(p, k, v[k]);
+    }
+}
+
+// V neighbouring channels' values of a vector over the channels (nullptr: `none`); a slab of fewer channels than a vector
+// repeats its last
+template <int V>
+__device__ __forceinline__ void slab_params(const NormArgs &a, const SlabTile &t, const float *p, float none, float (&v)[V])
+{
+    const int ch = t.slab * a.cw + t.q;
+    if (!p) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = none;
+    } else if (a.cw >= V) {
+#pragma unroll
+        for (int k = 0; k < V; k += 4) {
+            const f32x4 q = *reinterpret_cast<const f32x4_any *>(p + ch + k);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[k + i] = q[i];
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = p[ch + min(k, a.cw - 1)];
     }
 }
 
@@ -604,11 +647,18 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
     }
     if (!t.on) return;
     float scale[V], shift[V];
+    slab_params<V>(a, t, a.gamma, 1.f, scale);
+    slab_params<V>(a, t, a.beta, 0.f, shift);
+    float mean = 0.f, rstd = 0.f;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-        const int c = min(t.q + k, a.cw - 1), g = fastdiv(c, a.div_cpg), ch = t.slab * a.cw + c;
-        scale[k] = (MODE == kApply ? a.rstd[group0 + g] : grstd[g]) * (a.gamma ? a.gamma[ch] : 1.f);
-        shift[k] = fmaf(-(MODE == kApply ? a.mean[group0 + g] : gmean[g]), scale[k], a.beta ? a.beta[ch] : 0.f);
+        if (!ONE || k == 0) {
+            const int g = fastdiv(min(t.q + k, a.cw - 1), a.div_cpg);
+            mean = MODE == kApply ? a.mean[group0 + g] : gmean[g];
+            rstd = MODE == kApply ? a.rstd[group0 + g] : grstd[g];
+        }
+        scale[k] *= rstd;
+        shift[k] = fmaf(-mean, scale[k], shift[k]);
     }
     T *y = static_cast<T *>(a.out) + base;
 #pragma unroll
@@ -617,17 +667,16 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
         if (s < t.count) {
             float v[V];
             Vec<T>::open(raw[r], v);
-#pragma unroll
-            for (int k = 0; k < V; ++k) v[k] = act_fwd(fmaf(v[k], scale[k], shift[k]), a.act);
+            act_fwd(v, a.act, [&](int k) { return scale[k]; }, [&](int k) { return shift[k]; });
             slab_store(a, y + s * a.C, t, v);
         }
     }
 }
 
-template <typename T, int R, int MODE>
+template <typename T, int R, int MODE, bool ONE>
 __global__ __launch_bounds__(1024) void group_norm_last_bwd(NormArgs a)
 {
-    constexpr int V = Vec<T>::V;
+    constexpr int V = Vec<T>::V, W = ONE ? 1 : V;      // W groups to a vector at most
     constexpr bool kKeep = MODE == kWhole && sizeof(T) == 4;     // d and dz take the place of x and dy
     extern __shared__ float lds[];
     float *sa = lds, *sb = lds + V * a.pitch, *ca = sb + V * a.pitch, *cb = ca + a.cw, *g1 = cb + a.cw, *g2 = g1 + a.slab_groups;
@@ -645,14 +694,18 @@ __global__ __launch_bounds__(1024) void group_norm_last_bwd(NormArgs a)
         }
     }
     const int64_t group0 = (int64_t)t.n * a.groups + t.slab * a.slab_groups;
-    float mean[V], scale[V], shift[V];
+    float mean[W], scale[V], shift[V];
+    slab_params<V>(a, t, a.gamma, 1.f, scale);
+    slab_params<V>(a, t, a.beta, 0.f, shift);
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-        const int c = min(t.q + k, a.cw - 1), ch = t.slab * a.cw + c;
-        const int64_t g = group0 + fastdiv(c, a.div_cpg);
-        mean[k] = a.mean[g];
-        scale[k] = a.rstd[g] * (a.gamma ? a.gamma[ch] : 1.f);
-        shift[k] = a.beta ? a.beta[ch] : 0.f;
+    for (int k = 0; k < W; ++k) mean[k] = a.mean[group0 + fastdiv(min(t.q + k, a.cw - 1), a.div_cpg)];
+    {
+        float rstd = 0.f;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            if (k < W) rstd = a.rstd[group0 + fastdiv(min(t.q + k, a.cw - 1), a.div_cpg)];
+            scale[k] *= rstd;
+        }
     }
     if (MODE != kApply) {
         if (t.on) {
@@ -666,11 +719,12 @@ __global__ __launch_bounds__(1024) void group_norm_last_bwd(NormArgs a)
                     Vec<T>::open(rx[r], xv);
                     Vec<T>::open(rd[r], dv);
 #pragma unroll
+                    for (int k = 0; k < V; ++k) xv[k] -= mean[k % W];
+                    act_bwd(dv, xv, a.act, [&](int k) { return scale[k]; }, [&](int k) { return shift[k]; });
+#pragma unroll
                     for (int k = 0; k < V; ++k) {
-                        xv[k] -= mean[k];
-                        dv[k] = act_bwd(dv[k], scale[k] * xv[k] + shift[k], a.act);
                         A[k] += dv[k];
-                        B[k] += dv[k] * xv[k];
+                        B[k] = fmaf(dv[k], xv[k], B[k]);
                         if constexpr (kKeep) {
                             rx[r][k] = xv[k];
                             rd[r][k] = dv[k];
@@ -733,9 +787,9 @@ __global__ __launch_bounds__(1024) void group_norm_last_bwd(NormArgs a)
         __syncthreads();
     }
     if (!t.on) return;
-    float c1[V], c2[V];
+    float c1[W], c2[W];
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
+    for (int k = 0; k < W; ++k) {
         const int g = fastdiv(min(t.q + k, a.cw - 1), a.div_cpg);
         const float rstd = a.rstd[group0 + g];
         c1[k] = rstd * (MODE == kApply ? a.group_sums[2 * (group0 + g)] : g1[g]);
@@ -749,14 +803,13 @@ __global__ __launch_bounds__(1024) void group_norm_last_bwd(NormArgs a)
             float xv[V], dv[V];
             Vec<T>::open(rx[r], xv);
             Vec<T>::open(rd[r], dv);
+            if (!kKeep) {
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                if (!kKeep) {
-                    xv[k] -= mean[k];
-                    dv[k] = act_bwd(dv[k], scale[k] * xv[k] + shift[k], a.act);
-                }
-                dv[k] = (scale[k] * dv[k] - c1[k]) - xv[k] * c2[k];
+                for (int k = 0; k < V; ++k) xv[k] -= mean[k % W];
+                act_bwd(dv, xv, a.act, [&](int k) { return scale[k]; }, [&](int k) { return shift[k]; });
             }
+#pragma unroll
+            for (int k = 0; k < V; ++k) dv[k] = fmaf(-xv[k], c2[k % W], fmaf(scale[k], dv[k], -c1[k % W]));
             slab_store(a, dx + s * a.C, t, dv);
         }
     }
@@ -874,8 +927,11 @@ __global__ __launch_bounds__(1024) void group_norm_wide_fwd(NormArgs a)
     }
     for (int c = c0 + threadIdx.x; c < c0 + a.cpg; c += blockDim.x) {
         const float scale = rstd * (a.gamma ? a.gamma[c] : 1.f), shift = a.beta ? a.beta[c] : 0.f;
-        for (int r = 0; r < a.S; ++r)
-            st_elem(y, r * a.C + c, act_fwd((ld_elem(x, r * a.C + c) - mean) * scale + shift, a.act));
+        for (int r = 0; r < a.S; ++r) {
+            float v[1] = {ld_elem(x, r * a.C + c) - mean};
+            act_fwd(v, a.act, [&](int) { return scale; }, [&](int) { return shift; });
+            st_elem(y, r * a.C + c, v[0]);
+        }
     }
 }
 
@@ -892,10 +948,11 @@ __global__ __launch_bounds__(1024) void group_norm_wide_bwd(NormArgs a)
         const float gamma = a.gamma ? a.gamma[c] : 1.f, beta = a.beta ? a.beta[c] : 0.f;
         float A = 0.f, B = 0.f;
         for (int r = 0; r < a.S; ++r) {
-            const float xh = (ld_elem(x, r * a.C + c) - mean) * rstd;
-            const float dz = act_bwd(ld_elem(dy, r * a.C + c), gamma * xh + beta, a.act);
-            A += dz;
-            B += dz * xh;
+            const float xh[1] = {(ld_elem(x, r * a.C + c) - mean) * rstd};
+            float dz[1] = {ld_elem(dy, r * a.C + c)};
+            act_bwd(dz, xh, a.act, [&](int) { return gamma; }, [&](int) { return beta; });
+            A += dz[0];
+            B += dz[0] * xh[0];
         }
         a.part[(int64_t)n * a.C + c] = A;
         a.part[((int64_t)a.part_rows + n) * a.C + c] = B;
@@ -907,9 +964,10 @@ __global__ __launch_bounds__(1024) void group_norm_wide_bwd(NormArgs a)
     for (int c = c0 + threadIdx.x; c < c0 + a.cpg; c += blockDim.x) {
         const float gamma = a.gamma ? a.gamma[c] : 1.f, beta = a.beta ? a.beta[c] : 0.f;
         for (int r = 0; r < a.S; ++r) {
-            const float xh = (ld_elem(x, r * a.C + c) - mean) * rstd;
-            const float dz = act_bwd(ld_elem(dy, r * a.C + c), gamma * xh + beta, a.act);
-            st_elem(dx, r * a.C + c, rstd * (gamma * dz - m1 - xh * m2));
+            const float xh[1] = {(ld_elem(x, r * a.C + c) - mean) * rstd};
+            float dz[1] = {ld_elem(dy, r * a.C + c)};
+            act_bwd(dz, xh, a.act, [&](int) { return gamma; }, [&](int) { return beta; });
+            st_elem(dx, r * a.C + c, rstd * (gamma * dz[0] - m1 - xh[0] * m2));
         }
     }
 }

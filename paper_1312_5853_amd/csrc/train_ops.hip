@@ -78,8 +78,9 @@ void plan_planes(NormPlan &p, bool bwd, int V)
     if (units <= (int64_t)kMaxWaves * most && a.cpg <= 4096) {
         a.units = (int)units;
         p.solo = units <= 4 && groups >= 1024;
-        // a wave keeps up to four units while that leaves enough waves; few groups take a wave to a unit
-        const int want = groups >= 1024 ? 4 : 1;
+        // units to a wave, of one tensor or of two: 2, 4, 8 units of it measured (forward 60, 59, 69 us on 128 x 96 planes of
+        // 3025 fp32, backward 54, 55, 64 us on 128 x 256 planes of 729); few groups take a wave to a unit
+        const int want = groups < 1024 ? 1 : bwd ? 2 : 4;
         const int waves = p.solo ? 1 : std::min(kMaxWaves, ceil_div(a.units, want));
         a.run = ceil_div(a.units, waves);
         p.threads = p.solo ? 256 : 64 * ceil_div(a.units, a.run);
@@ -162,9 +163,9 @@ void plan_last(NormPlan &p, bool bwd, int V, int eb)
     a.work = a.N * a.tiles * a.slabs;
     a.units_per_xcd = ceil_div(a.work, 8);
     p.blocks = 8 * (int64_t)a.units_per_xcd;
-    p.one = !bwd && a.cpg % V == 0;
+    p.one = a.cpg % V == 0;
     a.div_width = make_fastdiv(p.one ? a.cpg / V : a.cpg);
-    p.lds = (size_t)(2 * (p.one ? 1 : V) * a.pitch + 2 * a.slab_groups + (bwd ? 2 * a.cw : 0)) * 4;
+    p.lds = (size_t)(2 * (p.one && !bwd ? 1 : V) * a.pitch + 2 * a.slab_groups + (bwd ? 2 * a.cw : 0)) * 4;
     a.rows_per_sample = a.tiles;
     a.div_lanes = make_fastdiv(a.lanes);
     a.div_slabs = make_fastdiv(a.slabs);
@@ -257,8 +258,7 @@ void launch_norm_fwd(const NormPlan &p, hipStream_t st)
     }
     const size_t lds = MODE == kApply ? 0 : p.lds;
     auto go = [&](auto of_one, auto of_several) { launch_norm(p.one ? of_one : of_several, p, lds, st); };
-    if constexpr (MODE == kSums) go(group_norm_last_fwd<T, kSplitRun, MODE, true>, group_norm_last_fwd<T, kSplitRun, MODE, false>);
-    else if constexpr (MODE == kApply) launch_norm(group_norm_last_fwd<T, kSplitRun, MODE, false>, p, lds, st);
+    if constexpr (MODE != kWhole) go(group_norm_last_fwd<T, kSplitRun, MODE, true>, group_norm_last_fwd<T, kSplitRun, MODE, false>);
     else if (p.regs <= 4) go(group_norm_last_fwd<T, 4, MODE, true>, group_norm_last_fwd<T, 4, MODE, false>);
     else if (p.regs == 8) go(group_norm_last_fwd<T, 8, MODE, true>, group_norm_last_fwd<T, 8, MODE, false>);
     else go(group_norm_last_fwd<T, 16, MODE, true>, group_norm_last_fwd<T, 16, MODE, false>);
@@ -279,9 +279,10 @@ void launch_norm_bwd(const NormPlan &p, hipStream_t st)
         else launch_norm(group_norm_planes_bwd<T, 8, false, MODE>, p, lds, st);
         return;
     }
-    if constexpr (MODE != kWhole) launch_norm(group_norm_last_bwd<T, kSplitRun, MODE>, p, lds, st);
-    else if (p.regs <= 4) launch_norm(group_norm_last_bwd<T, 4, MODE>, p, lds, st);
-    else launch_norm(group_norm_last_bwd<T, 8, MODE>, p, lds, st);
+    auto go = [&](auto of_one, auto of_several) { launch_norm(p.one ? of_one : of_several, p, lds, st); };
+    if constexpr (MODE != kWhole) go(group_norm_last_bwd<T, kSplitRun, MODE, true>, group_norm_last_bwd<T, kSplitRun, MODE, false>);
+    else if (p.regs <= 4) go(group_norm_last_bwd<T, 4, MODE, true>, group_norm_last_bwd<T, 4, MODE, false>);
+    else go(group_norm_last_bwd<T, 8, MODE, true>, group_norm_last_bwd<T, 8, MODE, false>);
 }
 
 template <typename T>

@@ -25,6 +25,12 @@ struct Vec<float> {
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[k] = r[k];
     }
+    static __device__ __forceinline__ void drop(Raw &r, int k0, int k1)      // -infinity in place of values before k0, from k1 on
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k < k0 || k >= k1) r[k] = -INFINITY;
+    }
     static __device__ __forceinline__ Raw some(const float *p, int n)        // the first n values, zeros after them
     {
         Raw r = {0.f, 0.f, 0.f, 0.f};
@@ -58,6 +64,14 @@ struct Vec<unsigned short> {
             v[2 * k + 1] = __uint_as_float(r[k] & 0xFFFF0000u);
         }
     }
+    static __device__ __forceinline__ void drop(Raw &r, int k0, int k1)
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (2 * k < k0 || 2 * k >= k1) r[k] = (r[k] & 0xFFFF0000u) | 0xFF80u;
+            if (2 * k + 1 < k0 || 2 * k + 1 >= k1) r[k] = (r[k] & 0xFFFFu) | 0xFF800000u;
+        }
+    }
     static __device__ __forceinline__ Raw some(const unsigned short *p, int n)
     {
         Raw r = {0u, 0u, 0u, 0u};
@@ -69,6 +83,13 @@ struct Vec<unsigned short> {
 
 // Sum and maximum over the 64 lanes, the same in every lane: within the rows of 16 lanes by data-parallel-primitive
 // moves, then the four row results by scalar reads.
+__device__ __forceinline__ float max3(float a, float b, float c)          // the largest; a NaN is passed over
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 template <int CTRL>
 __device__ __forceinline__ float dpp_move(float v)
 {

@@ -598,24 +598,28 @@ def _loss_workspace_bytes(N, V, K, dtype):
     return int(lib().distill_loss_workspace_bytes(N, V, K, dtype))
 
 
-def _norm_layout(x, *others):
+# The checks of the calls below are written out for speed: the smallest of these calls take the GPU about as long as
+# Python needs for their arguments.
+def _norm_layout(*tensors):
     """The memory order that all of a call's [N,C,H,W] tensors have: NCHW, or channels last."""
-    for layout, order in ((LAYOUT_PLANES, torch.contiguous_format), (LAYOUT_CHANNELS_LAST, torch.channels_last)):
-        if all(t.is_contiguous(memory_format=order) for t in (x,) + others):
-            return layout
-    raise ValueError("the tensors of a normalisation must be dense, all NCHW or all channels last")
+    for t in tensors:
+        if not t.is_contiguous():
+            break
+    else:
+        return LAYOUT_PLANES
+    for t in tensors:
+        if not t.is_contiguous(memory_format=torch.channels_last):
+            raise ValueError("the tensors of a normalisation must be dense, all NCHW or all channels last")
+    return LAYOUT_CHANNELS_LAST
 
 
-def _per_channel(C, **vectors):
-    for name, v in vectors.items():
-        if v is not None and (v.dtype != torch.float32 or v.numel() != C or not v.is_contiguous()):
-            raise ValueError("%s must hold one fp32 value per channel" % name)
+_F32 = torch.float32
 
 
-def _row_stats_of(N, groups, **tensors):
-    for name, v in tensors.items():
-        if v.dtype != torch.float32 or tuple(v.shape) != (N, groups) or not v.is_contiguous():
-            raise ValueError("%s must be a dense fp32 tensor [N, groups]" % name)
+def _dense_f32(t, shape, what):
+    """A dense fp32 tensor of this shape (None passes)."""
+    if t is not None and (t.dtype is not _F32 or t.shape != shape or not t.is_contiguous()):
+        raise ValueError("%s must be a dense fp32 tensor %s" % (what, list(shape)))
 
 
 def _opt(t):
@@ -623,8 +627,11 @@ def _opt(t):
 
 
 def _on_device(first, *others):
-    for t in (first,) + others:
-        if t is not None and (not t.is_cuda or t.device != first.device):
+    d = first.get_device()
+    if d < 0:
+        raise ValueError("the tensors of a call must be on one GPU")
+    for t in others:
+        if t is not None and t.get_device() != d:
             raise ValueError("the tensors of a call must be on one GPU")
 
 
@@ -635,19 +642,20 @@ def group_norm_act_fwd(x, groups, gamma=None, beta=None, eps=1e-5, act="relu", y
     gamma and beta: fp32 [C], or None."""
     if type(groups) is not int:
         groups, = _whole(groups)
-    N, C, H, W = x.shape
+    N, C, H, W = shape = x.shape
     if act not in ACTIVATIONS:
         raise ValueError("unknown activation %r" % (act,))
-    _per_channel(C, gamma=gamma, beta=beta)
+    _dense_f32(gamma, (C,), "gamma")
+    _dense_f32(beta, (C,), "beta")
     if y is None:
         y = torch.empty_like(x)
-    if y.shape != x.shape:
+    elif y.shape != shape:
         raise ValueError("y must have the shape of x")
     if groups > 0:
-        f = dict(dtype=torch.float32, device=x.device)
-        mean = torch.empty((N, groups), **f) if mean is None else mean
-        rstd = torch.empty((N, groups), **f) if rstd is None else rstd
-        _row_stats_of(N, groups, mean=mean, rstd=rstd)
+        mean = torch.empty((N, groups), dtype=_F32, device=x.device) if mean is None else mean
+        rstd = torch.empty((N, groups), dtype=_F32, device=x.device) if rstd is None else rstd
+        _dense_f32(mean, (N, groups), "mean")
+        _dense_f32(rstd, (N, groups), "rstd")
     dtype, layout = _glue_dtype(x, y), _norm_layout(x, y)
     _on_device(x, y, gamma, beta, mean, rstd)
     buf, nbytes = _ws(ws).get(_norm_workspace_bytes(OP_FWD, N, C, H * W, groups, layout, dtype))
@@ -661,19 +669,20 @@ def group_norm_act_fwd(x, groups, gamma=None, beta=None, eps=1e-5, act="relu", y
 def group_norm_act_bwd(x, dy, mean, rstd, gamma=None, beta=None, act="relu", dx=None, dgamma=None, dbeta=None, ws=None,
                        stream=None):
     """(dx, dgamma [C], dbeta [C]) from the forward call's x, mean and rstd and the gradient dy of its y."""
-    N, C, H, W = x.shape
+    N, C, H, W = shape = x.shape
     if act not in ACTIVATIONS:
         raise ValueError("unknown activation %r" % (act,))
     groups = mean.shape[1]
-    _row_stats_of(N, groups, mean=mean, rstd=rstd)
+    _dense_f32(mean, (N, groups), "mean")
+    _dense_f32(rstd, (N, groups), "rstd")
     if dx is None:
         dx = torch.empty_like(x)
-    if dy.shape != x.shape or dx.shape != x.shape:
+    if dy.shape != shape or dx.shape != shape:
         raise ValueError("dy and dx must have the shape of x")
-    f = dict(dtype=torch.float32, device=x.device)
-    dgamma = torch.empty((C,), **f) if dgamma is None else dgamma
-    dbeta = torch.empty((C,), **f) if dbeta is None else dbeta
-    _per_channel(C, gamma=gamma, beta=beta, dgamma=dgamma, dbeta=dbeta)
+    dgamma = torch.empty((C,), dtype=_F32, device=x.device) if dgamma is None else dgamma
+    dbeta = torch.empty((C,), dtype=_F32, device=x.device) if dbeta is None else dbeta
+    for what, v in (("gamma", gamma), ("beta", beta), ("dgamma", dgamma), ("dbeta", dbeta)):
+        _dense_f32(v, (C,), what)
     dtype, layout = _glue_dtype(x, dy, dx), _norm_layout(x, dy, dx)
     _on_device(x, dy, dx, mean, rstd, gamma, beta, dgamma, dbeta)
     buf, nbytes = _ws(ws).get(_norm_workspace_bytes(OP_BWD_DATA, N, C, H * W, groups, layout, dtype))
@@ -686,36 +695,36 @@ def group_norm_act_bwd(x, dy, mean, rstd, gamma=None, beta=None, act="relu", dx=
 
 
 def _rows_of(t, what):
-    """Row stride of a [N,V] tensor whose rows are dense."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+    """(N, V, row stride) of a [N,V] tensor whose rows are dense."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1) or (shape[0] > 1 and stride[0] < shape[1]):
         raise ValueError("%s must be [N, V] with dense rows" % what)
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return shape[0], shape[1], (stride[0] if shape[0] > 1 else shape[1])
 
 
-def _fp32_rows(N, width, **tensors):
-    for name, v in tensors.items():
-        if v is not None and (v.dtype != torch.float32 or v.numel() != N * width or v.shape[0] != N
-                              or not v.is_contiguous()):
-            raise ValueError("%s must be a dense fp32 tensor with %d value(s) per row" % (name, width))
+_INDEX_BYTES = {torch.int32: 4, torch.int64: 8}
 
 
-def _targets(z, labels, top_idx, top_val):
+def _targets(N, labels, top_idx, top_val):
     """(K, bytes of an index, dtype code of the teacher's logits) of a loss call, its target tensors checked."""
-    N = z.shape[0]
     if (top_idx is None) != (top_val is None):
         raise ValueError("top_idx and top_val come together")
-    index = {t.dtype for t in (labels, top_idx) if t is not None}
-    if len(index) > 1 or not index <= {torch.int32, torch.int64}:
+    index = 4
+    if labels is not None:
+        index = _INDEX_BYTES.get(labels.dtype)
+        if labels.shape != (N,) or not labels.is_contiguous():
+            raise ValueError("labels must be a dense tensor with one class per row")
+    if top_idx is None:
+        if index is None:
+            raise TypeError("labels must be int32 or int64")
+        return 0, index, DTYPE_F32
+    of_top = _INDEX_BYTES.get(top_idx.dtype)
+    if of_top is None or (labels is not None and of_top != index):
         raise TypeError("labels and top_idx must have one type, int32 or int64")
-    if labels is not None and (tuple(labels.shape) != (N,) or not labels.is_contiguous()):
-        raise ValueError("labels must be a dense tensor with one class per row")
-    K = 0
-    if top_idx is not None:
-        K = top_idx.shape[-1]
-        if tuple(top_idx.shape) != (N, K) or top_val.shape != top_idx.shape:
-            raise ValueError("top_idx and top_val must be [N, K]")
-        _dense(top_idx, top_val)
-    return K, 8 if torch.int64 in index else 4, DTYPE_F32 if K == 0 else _dtype_of(top_val)
+    shape = top_idx.shape
+    if len(shape) != 2 or shape[0] != N or top_val.shape != shape or not top_idx.is_contiguous() or not top_val.is_contiguous():
+        raise ValueError("top_idx and top_val must be dense tensors [N, K]")
+    return shape[1], of_top, _dtype_of(top_val)
 
 
 def distill_loss_fwd(z, labels=None, top_idx=None, top_val=None, temperature=1.0, kd_weight=1.0, label_weight=1.0,
@@ -723,14 +732,12 @@ def distill_loss_fwd(z, labels=None, top_idx=None, top_val=None, temperature=1.0
     """Losses of the logits z [N,V] (fp32 or bfloat16, rows may be apart) against labels [N] and / or a teacher's top
     logits (classes top_idx [N,K], logits top_val [N,K]); indexes int32 or int64, one outside 0..V-1 for none.  Returns
     (loss [N], stats [N,3]); stats is what distill_loss_bwd takes."""
-    zs = _rows_of(z, "z")
-    N, V = z.shape
-    K, ib, td = _targets(z, labels, top_idx, top_val)
-    f = dict(dtype=torch.float32, device=z.device)
-    loss = torch.empty((N,), **f) if loss is None else loss
-    stats = torch.empty((N, 3), **f) if stats is None else stats
-    _fp32_rows(N, 1, loss=loss)
-    _fp32_rows(N, 3, stats=stats)
+    N, V, zs = _rows_of(z, "z")
+    K, ib, td = _targets(N, labels, top_idx, top_val)
+    loss = torch.empty((N,), dtype=_F32, device=z.device) if loss is None else loss
+    stats = torch.empty((N, 3), dtype=_F32, device=z.device) if stats is None else stats
+    _dense_f32(loss, (N,), "loss")
+    _dense_f32(stats, (N, 3), "stats")
     dtype = _dtype_of(z)
     _on_device(z, labels, top_idx, top_val, loss, stats)
     buf, nbytes = _ws(ws).get(_loss_workspace_bytes(N, V, K, dtype))
@@ -744,18 +751,18 @@ def distill_loss_bwd(z, stats, labels=None, top_idx=None, top_val=None, temperat
                      grad=None, grad_scale=1.0, dz=None, stream=None):
     """dz = grad_scale * grad[n] * d loss[n] / d z (grad [N] fp32, or None for ones) from the forward call's arguments and
     statistics.  dz has z's element type and may be z itself."""
-    zs = _rows_of(z, "z")
-    N, V = z.shape
-    K, ib, td = _targets(z, labels, top_idx, top_val)
-    _fp32_rows(N, 1, grad=grad)
-    _fp32_rows(N, 3, stats=stats)
+    N, V, zs = _rows_of(z, "z")
+    K, ib, td = _targets(N, labels, top_idx, top_val)
+    _dense_f32(grad, (N,), "grad")
+    _dense_f32(stats, (N, 3), "stats")
     dz = torch.empty((N, V), dtype=z.dtype, device=z.device) if dz is None else dz
-    if dz.shape != z.shape:
+    dN, dV, dzs = _rows_of(dz, "dz")
+    if dN != N or dV != V:
         raise ValueError("dz must have the shape of z")
     dtype = _glue_dtype(z, dz)
     _on_device(z, labels, top_idx, top_val, stats, grad, dz)
     _check(lib().distill_loss_bwd(_ptr(z), zs, _opt(labels), _opt(top_idx), _opt(top_val), _ptr(stats), _opt(grad),
-                                  grad_scale, _ptr(dz), _rows_of(dz, "dz"), N, V, K, temperature, kd_weight,
+                                  grad_scale, _ptr(dz), dzs, N, V, K, temperature, kd_weight,
                                   label_weight, ib, td, dtype, _stream_handle(stream)), "distill_loss_bwd")
     return dz
 
@@ -763,19 +770,20 @@ def distill_loss_bwd(z, stats, labels=None, top_idx=None, top_val=None, temperat
 def distill_loss_fwd_bwd(z, labels=None, top_idx=None, top_val=None, temperature=1.0, kd_weight=1.0, label_weight=1.0,
                          grad=None, grad_scale=1.0, loss=None, dz=None, ws=None, stream=None):
     """(loss [N], dz [N,V]) of distill_loss_fwd and distill_loss_bwd in one call."""
-    zs = _rows_of(z, "z")
-    N, V = z.shape
-    K, ib, td = _targets(z, labels, top_idx, top_val)
-    loss = torch.empty((N,), dtype=torch.float32, device=z.device) if loss is None else loss
-    _fp32_rows(N, 1, grad=grad, loss=loss)
+    N, V, zs = _rows_of(z, "z")
+    K, ib, td = _targets(N, labels, top_idx, top_val)
+    loss = torch.empty((N,), dtype=_F32, device=z.device) if loss is None else loss
+    _dense_f32(grad, (N,), "grad")
+    _dense_f32(loss, (N,), "loss")
     dz = torch.empty((N, V), dtype=z.dtype, device=z.device) if dz is None else dz
-    if dz.shape != z.shape:
+    dN, dV, dzs = _rows_of(dz, "dz")
+    if dN != N or dV != V:
         raise ValueError("dz must have the shape of z")
     dtype = _glue_dtype(z, dz)
     _on_device(z, labels, top_idx, top_val, grad, loss, dz)
     buf, nbytes = _ws(ws).get(_loss_workspace_bytes(N, V, K, dtype))
     _check(lib().distill_loss_fwd_bwd(_ptr(z), zs, _opt(labels), _opt(top_idx), _opt(top_val), _opt(grad), grad_scale,
-                                      _ptr(loss), _ptr(dz), _rows_of(dz, "dz"), N, V, K, temperature, kd_weight,
+                                      _ptr(loss), _ptr(dz), dzs, N, V, K, temperature, kd_weight,
                                       label_weight, ib, td, dtype, _opt(buf), nbytes, _stream_handle(stream)),
            "distill_loss_fwd_bwd")
     return loss, dz

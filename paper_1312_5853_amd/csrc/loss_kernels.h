@@ -101,15 +101,6 @@ __device__ __forceinline__ void row_store(const LossArgs &a, T *dz, const RowLan
     }
 }
 
-// Makes the compiler take a lane's vectors for new ones: it would else keep bfloat16 values that it has widened for one
-// use for the next, twice the registers, and spill.
-template <typename T, int R>
-__device__ __forceinline__ void row_again(typename Vec<T>::Raw (&raw)[R])
-{
-#pragma unroll
-    for (int r = 0; r < R; ++r) asm volatile("" : "+v"(raw[r]));
-}
-
 // the maximum of a lane's vectors
 template <typename T, int R>
 __device__ __forceinline__ float row_max(const typename Vec<T>::Raw (&raw)[R])
@@ -447,7 +438,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, GRAD ? 8 : 6) void distill_rows(
     const RowExps x(a, m, a.K > 0 && (has || a.stats), label >= 0 || a.stats);
     float sums[3] = {0.f, 0.f, 0.f};
     sums[2] = weigh_entries(a, team, e, tm);
-    row_again<T, R>(raw);
+    open_again(raw);
     x.template sums<T, R>(raw, sums[0], sums[1]);
     team.sum_of(sums, red + 3);
     float sT = sums[0], s1 = sums[1];
@@ -464,7 +455,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, GRAD ? 8 : 6) void distill_rows(
         if (has) { gk = g * a.wk * a.T; ck = gk / sT; }
         if (label >= 0) { gl = g * a.wl; cl = gl / s1; }
         x.factors(ck, cl);
-        row_again<T, R>(raw);
+        open_again(raw);
         x.template write<T, R>(a, raw, dz, c0, cn, team.lane, ck, cl);
     }
     float kd[1] = {has ? divergence(a, team, e, nullptr, inv_ts, m, sT) : 0.f};
@@ -507,7 +498,7 @@ __global__ __launch_bounds__(512, 8) void distill_part_sums(LossArgs a)
     // of a part without any class left the sums are 0
     const float top = m[0] == -INFINITY ? 0.f : m[0];
     const RowExps x(a, top, a.K > 0, true);
-    row_again<T, R>(raw);
+    open_again(raw);
     x.template sums<T, R>(raw, s[0], s[1]);
     team.sum_of(s, red + 1);
     x.finish(s[0], s[1]);
@@ -581,7 +572,7 @@ __global__ __launch_bounds__(512, 8) void distill_part_apply(LossArgs a)
         if (has) { gk = g * a.wk * a.T; ck = gk / sT; }
         if (label >= 0) { gl = g * a.wl; cl = gl / s1; }
         x.factors(ck, cl);
-        row_again<T, R>(raw);
+        open_again(raw);
         x.template write<T, R>(a, raw, dz, c0, cn, team.lane, ck, cl);
     }
     float ts[1] = {weigh_entries(a, team, e, most[0])};

@@ -72,7 +72,7 @@ __device__ __forceinline__ void act_bwd(float (&dy)[V], const float (&d)[V], int
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             const float z = fmaf(d[k], scale(k), shift(k));
-            dy[k] = z > 0.f ? dy[k] : z <= 0.f ? 0.f : z;                     // (a NaN stays)
+            dy[k] = z > 0.f ? dy[k] : 0.f;
         }
     } else if (act == kActSilu) {
 #pragma unroll
@@ -537,6 +537,25 @@ __device__ __forceinline__ void slab_params(const NormArgs &a, const SlabTile &t
     }
 }
 
+// the group (in the slab) of a vector's values one after the other, from one division
+struct GroupWalk {
+    int g, left;
+    __device__ __forceinline__ GroupWalk(const NormArgs &a, const SlabTile &t)
+    {
+        g = fastdiv(t.q, a.div_cpg);
+        left = a.cpg * (g + 1) - t.q;
+    }
+    __device__ __forceinline__ int next(const NormArgs &a)
+    {
+        const int now = g;
+        if (--left == 0) {
+            left = a.cpg;
+            g = min(g + 1, a.slab_groups - 1);       // (past the slab: a vector's values that do not exist)
+        }
+        return now;
+    }
+};
+
 // where the sums of channel c of the slab over the rows of thread row p lie: [value of the vector][thread], so that the
 // lanes of a wave write neighbouring words
 template <int V>
@@ -547,6 +566,7 @@ __device__ __forceinline__ int slab_slot(const NormArgs &a, int p, int c)
 }
 
 // ONE: every vector lies in one group (C / groups a multiple of the vector): a thread then has one sum, not one per value.
+// A thread of kSums and kApply takes R rows after R rows of its tile.
 template <typename T, int R, int MODE, bool ONE>
 __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
 {
@@ -558,40 +578,63 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
     const int64_t base = ((int64_t)t.n * a.S + t.s0) * a.C + t.slab * a.cw + t.q;
     const T *x = static_cast<const T *>(a.x) + base;
     typename Vec<T>::Raw raw[R];
+    auto load = [&](int p) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int s = t.p + r * a.rows;
-        if (t.on && s < t.count) raw[r] = slab_load(a, x + s * a.C, t);
-    }
+        for (int r = 0; r < R; ++r)
+            if (t.on && p + r * a.rows < t.count) raw[r] = slab_load(a, x + (p + r * a.rows) * a.C, t);
+    };
+    if (MODE == kWhole) load(t.p);
     const int64_t group0 = (int64_t)t.n * a.groups + t.slab * a.slab_groups;
     if (MODE != kApply) {
         // every thread's sums, and squared distances from its own means
         const int whole = t.count / a.rows, extra = t.count - whole * a.rows;       // rows of a thread: whole (+ 1)
+        const int mine = whole + (t.p < extra);
         if (t.on) {
-            const int cnt = whole + (t.p < extra);
-            const float inv = cnt ? 1.f / (cnt * (V / W)) : 0.f;
             float s[W], d[W];
 #pragma unroll
             for (int k = 0; k < W; ++k) s[k] = d[k] = 0.f;
+            int done = 0;
+            do {
+                const int p = t.p + done * a.rows;
+                if (MODE != kWhole) load(p);
+                const int cnt = min(R, mine - done);
+                const float inv = cnt > 0 ? 1.f / (cnt * (V / W)) : 0.f;
+                float bs[W], bd[W];
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-                if (t.p + r * a.rows < t.count) {
-                    float v[V];
-                    Vec<T>::open(raw[r], v);
+                for (int k = 0; k < W; ++k) bs[k] = bd[k] = 0.f;
 #pragma unroll
-                    for (int k = 0; k < V; ++k) s[k % W] += v[k];
-                }
+                for (int r = 0; r < R; ++r)
+                    if (r < cnt) {
+                        float v[V];
+                        Vec<T>::open(raw[r], v);
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-                if (t.p + r * a.rows < t.count) {
-                    float v[V];
-                    Vec<T>::open(raw[r], v);
-#pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        const float e = v[k] - s[k % W] * inv;
-                        d[k % W] += e * e;
+                        for (int k = 0; k < V; ++k) bs[k % W] += v[k];
                     }
+                open_again(raw);
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    if (r < cnt) {
+                        float v[V];
+                        Vec<T>::open(raw[r], v);
+#pragma unroll
+                        for (int k = 0; k < V; ++k) {
+                            const float e = v[k] - bs[k % W] * inv;
+                            bd[k % W] = fmaf(e, e, bd[k % W]);
+                        }
+                    }
+                // joined with the rows before: n1 n2 / (n1 + n2) times the square of the means' distance comes on top
+                const float n1 = done * (V / W), n2 = cnt * (V / W), inv1 = done ? 1.f / n1 : 0.f, both = n1 * n2 / (n1 + n2);
+#pragma unroll
+                for (int k = 0; k < W; ++k) {
+                    if (MODE != kWhole && done) {
+                        const float gap = bs[k] * inv - s[k] * inv1;
+                        d[k] += gap * gap * both;
+                    }
+                    s[k] += bs[k];
+                    d[k] += bd[k];
                 }
+                done += R;
+            } while (MODE != kWhole && done < mine);
 #pragma unroll
             for (int k = 0; k < W; ++k) {
                 sum[k * a.pitch + threadIdx.x] = s[k];
@@ -650,10 +693,11 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
     slab_params<V>(a, t, a.gamma, 1.f, scale);
     slab_params<V>(a, t, a.beta, 0.f, shift);
     float mean = 0.f, rstd = 0.f;
+    GroupWalk walk(a, t);
 #pragma unroll
     for (int k = 0; k < V; ++k) {
         if (!ONE || k == 0) {
-            const int g = fastdiv(min(t.q + k, a.cw - 1), a.div_cpg);
+            const int g = walk.next(a);
             mean = MODE == kApply ? a.mean[group0 + g] : gmean[g];
             rstd = MODE == kApply ? a.rstd[group0 + g] : grstd[g];
         }
@@ -661,23 +705,30 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
         shift[k] = fmaf(-mean, scale[k], shift[k]);
     }
     T *y = static_cast<T *>(a.out) + base;
+    if (MODE == kWhole) open_again(raw);
+    int p = t.p;
+    do {
+        if (MODE == kApply) load(p);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int s = t.p + r * a.rows;
-        if (s < t.count) {
-            float v[V];
-            Vec<T>::open(raw[r], v);
-            act_fwd(v, a.act, [&](int k) { return scale[k]; }, [&](int k) { return shift[k]; });
-            slab_store(a, y + s * a.C, t, v);
+        for (int r = 0; r < R; ++r) {
+            const int s = p + r * a.rows;
+            if (s < t.count) {
+                float v[V];
+                Vec<T>::open(raw[r], v);
+                act_fwd(v, a.act, [&](int k) { return scale[k]; }, [&](int k) { return shift[k]; });
+                slab_store(a, y + s * a.C, t, v);
+            }
         }
-    }
+        p += R * a.rows;
+    } while (MODE != kWhole && p < t.count);
 }
 
 template <typename T, int R, int MODE, bool ONE>
 __global__ __launch_bounds__(1024) void group_norm_last_bwd(NormArgs a)
 {
     constexpr int V = Vec<T>::V, W = ONE ? 1 : V;      // W groups to a vector at most
-    constexpr bool kKeep = MODE == kWhole && sizeof(T) == 4;     // d and dz take the place of x and dy
+    // d and dz stay in registers, in fp32 in the places of x and dy; with many bfloat16 vectors they are computed twice
+    constexpr bool kInPlace = MODE == kWhole && sizeof(T) == 4, kKeep = MODE == kWhole && sizeof(T) == 2 && R <= 4 && ONE;
     extern __shared__ float lds[];
     float *sa = lds, *sb = lds + V * a.pitch, *ca = sb + V * a.pitch, *cb = ca + a.cw, *g1 = cb + a.cw, *g2 = g1 + a.slab_groups;
     const SlabTile t = slab_tile<V>(a);
@@ -685,52 +736,67 @@ __global__ __launch_bounds__(1024) void group_norm_last_bwd(NormArgs a)
     const int64_t base = ((int64_t)t.n * a.S + t.s0) * a.C + t.slab * a.cw + t.q;
     const T *x = static_cast<const T *>(a.x) + base, *dy = static_cast<const T *>(a.dy) + base;
     typename Vec<T>::Raw rx[R], rd[R];
+    float dz[kKeep ? R : 1][V];
+    auto load = [&](int p) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int s = t.p + r * a.rows;
-        if (t.on && s < t.count) {
-            rx[r] = slab_load(a, x + s * a.C, t);
-            rd[r] = slab_load(a, dy + s * a.C, t);
-        }
-    }
+        for (int r = 0; r < R; ++r)
+            if (t.on && p + r * a.rows < t.count) {
+                rx[r] = slab_load(a, x + (p + r * a.rows) * a.C, t);
+                rd[r] = slab_load(a, dy + (p + r * a.rows) * a.C, t);
+            }
+    };
+    if (MODE == kWhole) load(t.p);
     const int64_t group0 = (int64_t)t.n * a.groups + t.slab * a.slab_groups;
     float mean[W], scale[V], shift[V];
     slab_params<V>(a, t, a.gamma, 1.f, scale);
     slab_params<V>(a, t, a.beta, 0.f, shift);
-#pragma unroll
-    for (int k = 0; k < W; ++k) mean[k] = a.mean[group0 + fastdiv(min(t.q + k, a.cw - 1), a.div_cpg)];
     {
         float rstd = 0.f;
+        GroupWalk walk(a, t);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            if (k < W) rstd = a.rstd[group0 + fastdiv(min(t.q + k, a.cw - 1), a.div_cpg)];
+            if (k < W) {
+                const int64_t g = group0 + walk.next(a);
+                mean[k] = a.mean[g];
+                rstd = a.rstd[g];
+            }
             scale[k] *= rstd;
         }
     }
+    // d = x - mean and dz of a vector
+    auto slopes = [&](int r, float (&xv)[V], float (&dv)[V]) {
+        Vec<T>::open(rx[r], xv);
+        Vec<T>::open(rd[r], dv);
+#pragma unroll
+        for (int k = 0; k < V; ++k) xv[k] -= mean[k % W];
+        act_bwd(dv, xv, a.act, [&](int k) { return scale[k]; }, [&](int k) { return shift[k]; });
+    };
     if (MODE != kApply) {
         if (t.on) {
             float A[V], B[V];
 #pragma unroll
             for (int k = 0; k < V; ++k) A[k] = B[k] = 0.f;
+            int p = t.p;
+            do {
+                if (MODE == kSums) load(p);
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-                if (t.p + r * a.rows < t.count) {
-                    float xv[V], dv[V];
-                    Vec<T>::open(rx[r], xv);
-                    Vec<T>::open(rd[r], dv);
+                for (int r = 0; r < R; ++r)
+                    if (p + r * a.rows < t.count) {
+                        float xv[V], dv[V];
+                        slopes(r, xv, dv);
 #pragma unroll
-                    for (int k = 0; k < V; ++k) xv[k] -= mean[k % W];
-                    act_bwd(dv, xv, a.act, [&](int k) { return scale[k]; }, [&](int k) { return shift[k]; });
-#pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        A[k] += dv[k];
-                        B[k] = fmaf(dv[k], xv[k], B[k]);
-                        if constexpr (kKeep) {
-                            rx[r][k] = xv[k];
-                            rd[r][k] = dv[k];
+                        for (int k = 0; k < V; ++k) {
+                            A[k] += dv[k];
+                            B[k] = fmaf(dv[k], xv[k], B[k]);
+                            if constexpr (kKeep) dz[r][k] = dv[k];
+                            if constexpr (kInPlace) {
+                                rx[r][k] = xv[k];
+                                rd[r][k] = dv[k];
+                            }
                         }
                     }
-                }
+                p += R * a.rows;
+            } while (MODE != kWhole && p < t.count);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 sa[k * a.pitch + threadIdx.x] = A[k];
@@ -788,31 +854,47 @@ __global__ __launch_bounds__(1024) void group_norm_last_bwd(NormArgs a)
     }
     if (!t.on) return;
     float c1[W], c2[W];
+    GroupWalk walk(a, t);
 #pragma unroll
     for (int k = 0; k < W; ++k) {
-        const int g = fastdiv(min(t.q + k, a.cw - 1), a.div_cpg);
+        const int g = walk.next(a);
         const float rstd = a.rstd[group0 + g];
         c1[k] = rstd * (MODE == kApply ? a.group_sums[2 * (group0 + g)] : g1[g]);
         c2[k] = rstd * rstd * (MODE == kApply ? a.group_sums[2 * (group0 + g) + 1] : g2[g]);
     }
     T *dx = static_cast<T *>(a.out) + base;
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int s = t.p + r * a.rows;
-        if (s < t.count) {
-            float xv[V], dv[V];
-            Vec<T>::open(rx[r], xv);
-            Vec<T>::open(rd[r], dv);
-            if (!kKeep) {
-#pragma unroll
-                for (int k = 0; k < V; ++k) xv[k] -= mean[k % W];
-                act_bwd(dv, xv, a.act, [&](int k) { return scale[k]; }, [&](int k) { return shift[k]; });
-            }
-#pragma unroll
-            for (int k = 0; k < V; ++k) dv[k] = fmaf(-xv[k], c2[k % W], fmaf(scale[k], dv[k], -c1[k % W]));
-            slab_store(a, dx + s * a.C, t, dv);
-        }
+    if (MODE == kWhole) {
+        open_again(rx);
+        open_again(rd);
     }
+    int p = t.p;
+    do {
+        if (MODE == kApply) load(p);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int s = p + r * a.rows;
+            if (s < t.count) {
+                float xv[V], dv[V];
+                if constexpr (kKeep) {
+                    Vec<T>::open(rx[r], xv);
+#pragma unroll
+                    for (int k = 0; k < V; ++k) {
+                        xv[k] -= mean[k % W];
+                        dv[k] = dz[r][k];
+                    }
+                } else if constexpr (kInPlace) {
+                    Vec<T>::open(rx[r], xv);
+                    Vec<T>::open(rd[r], dv);
+                } else {
+                    slopes(r, xv, dv);
+                }
+#pragma unroll
+                for (int k = 0; k < V; ++k) dv[k] = fmaf(-xv[k], c2[k % W], fmaf(scale[k], dv[k], -c1[k % W]));
+                slab_store(a, dx + s * a.C, t, dv);
+            }
+        }
+        p += R * a.rows;
+    } while (MODE != kWhole && p < t.count);
 }
 
 // ---------------------------------------------------------------------------

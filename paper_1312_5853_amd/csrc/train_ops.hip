@@ -115,7 +115,7 @@ void plan_planes(NormPlan &p, bool bwd, int V)
 void plan_last(NormPlan &p, bool bwd, int V, int eb)
 {
     NormArgs &a = p.a;
-    const int most = bwd ? 8 : 16;
+    const int most = !bwd ? 16 : eb == 4 ? 10 : 8;
     int best = 0;
     double best_score = 0.0;
     auto lanes_of = [&](int slab_groups) { return (int)(((int64_t)slab_groups * a.cpg + V - 1) / V); };
@@ -126,7 +126,7 @@ void plan_last(NormPlan &p, bool bwd, int V, int eb)
         const int rows = 1024 / (int)lanes64;
         if (ceil_div(a.S, rows) > most) continue;
         const double seg = (double)j * a.cpg * eb;
-        if (seg < 64 && j != a.groups) continue;
+        if (seg < (bwd ? 48 : 64) && j != a.groups) continue;
         // lines that a slab shares with its neighbours are read by both; few work-groups leave the card idle
         const double wgs = (double)a.N * (a.groups / j);
         const double score = seg / (seg + 64) * std::min(1.0, wgs / 512);
@@ -136,7 +136,7 @@ void plan_last(NormPlan &p, bool bwd, int V, int eb)
     if (best) {
         a.slab_groups = best;
         a.lanes = lanes_of(best);
-        const int want = 4;
+        const int want = bwd ? 6 : 8;
         threads = std::min<int64_t>(1024, round_up64((int64_t)a.lanes * ceil_div(a.S, want), 64));
         a.rows = threads / a.lanes;
         a.tile_rows = a.S;
@@ -150,13 +150,17 @@ void plan_last(NormPlan &p, bool bwd, int V, int eb)
         a.lanes = lanes_of(j);
         threads = std::max(512, round_up(a.lanes, 64));
         a.rows = threads / a.lanes;
-        a.tile_rows = std::min(a.S, a.rows * kSplitRun);
+        const int64_t N_slabs = (int64_t)a.N * (a.groups / j);
+        // as many rows to a thread as leave 1024 work-groups, 32 at most
+        const int most_rows = (int)std::max<int64_t>(4, std::min<int64_t>(32, (int64_t)N_slabs * ceil_div(a.S, a.rows) / 1024));
+        a.tile_rows = std::min(a.S, a.rows * most_rows);
         a.tiles = ceil_div(a.S, a.tile_rows);
+        a.tile_rows = ceil_div(a.S, a.tiles);
     }
     a.cw = a.slab_groups * a.cpg;
     a.slabs = a.groups / a.slab_groups;
     p.threads = threads;
-    p.regs = regs_for(ceil_div(a.tile_rows, a.rows), most);
+    p.regs = ceil_div(a.tile_rows, a.rows);
     a.pitch = threads + 9;
     a.group_lanes = std::min(64, pow2_down(std::max(1, threads / a.slab_groups)));
     a.channel_lanes = std::min(64, pow2_down(std::max(1, threads / a.cw)));
@@ -260,7 +264,7 @@ void launch_norm_fwd(const NormPlan &p, hipStream_t st)
     auto go = [&](auto of_one, auto of_several) { launch_norm(p.one ? of_one : of_several, p, lds, st); };
     if constexpr (MODE != kWhole) go(group_norm_last_fwd<T, kSplitRun, MODE, true>, group_norm_last_fwd<T, kSplitRun, MODE, false>);
     else if (p.regs <= 4) go(group_norm_last_fwd<T, 4, MODE, true>, group_norm_last_fwd<T, 4, MODE, false>);
-    else if (p.regs == 8) go(group_norm_last_fwd<T, 8, MODE, true>, group_norm_last_fwd<T, 8, MODE, false>);
+    else if (p.regs <= 8) go(group_norm_last_fwd<T, 8, MODE, true>, group_norm_last_fwd<T, 8, MODE, false>);
     else go(group_norm_last_fwd<T, 16, MODE, true>, group_norm_last_fwd<T, 16, MODE, false>);
 }
 
@@ -282,7 +286,9 @@ void launch_norm_bwd(const NormPlan &p, hipStream_t st)
     auto go = [&](auto of_one, auto of_several) { launch_norm(p.one ? of_one : of_several, p, lds, st); };
     if constexpr (MODE != kWhole) go(group_norm_last_bwd<T, kSplitRun, MODE, true>, group_norm_last_bwd<T, kSplitRun, MODE, false>);
     else if (p.regs <= 4) go(group_norm_last_bwd<T, 4, MODE, true>, group_norm_last_bwd<T, 4, MODE, false>);
-    else go(group_norm_last_bwd<T, 8, MODE, true>, group_norm_last_bwd<T, 8, MODE, false>);
+    else if (p.regs <= 6) go(group_norm_last_bwd<T, 6, MODE, true>, group_norm_last_bwd<T, 6, MODE, false>);
+    else if (p.regs <= 8) go(group_norm_last_bwd<T, 8, MODE, true>, group_norm_last_bwd<T, 8, MODE, false>);
+    else if constexpr (sizeof(T) == 4) go(group_norm_last_bwd<T, 10, MODE, true>, group_norm_last_bwd<T, 10, MODE, false>);
 }
 
 template <typename T>

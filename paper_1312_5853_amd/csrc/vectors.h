@@ -81,6 +81,15 @@ struct Vec<unsigned short> {
     }
 };
 
+// Makes the compiler take vectors for new ones.  It would else keep values that it has opened for one use, bfloat16 ones
+// in twice the registers, for the next, and spill; opening them again is one instruction.
+template <typename Raw, int R>
+__device__ __forceinline__ void open_again(Raw (&raw)[R])
+{
+#pragma unroll
+    for (int r = 0; r < R; ++r) asm volatile("" : "+v"(raw[r]));
+}
+
 // Sum and maximum over the 64 lanes, the same in every lane: within the rows of 16 lanes by data-parallel-primitive
 // moves, then the four row results by scalar reads.
 __device__ __forceinline__ float max3(float a, float b, float c)          // the largest; a NaN is passed over

@@ -267,7 +267,7 @@ __device__ __forceinline__ void row_clear(const LossArgs &a, T *dz, int c0, int 
 }
 
 // ---------------------------------------------------------------------------
-// The threads that work on a row: a wave (its LDS to itself, no barrier), or a work-group
+// The threads that work on a row: a wave (SOLO: four rows to a work-group, LDS to each, no barrier), or a work-group
 // ---------------------------------------------------------------------------
 template <bool SOLO>
 struct RowTeam {
@@ -280,7 +280,7 @@ struct RowTeam {
         id = SOLO ? lane : (int)threadIdx.x;
         size = waves * 64;
     }
-    // what a lane has written to LDS or memory is there for the others of the team afterwards
+    // what a lane has read or written before, in LDS or memory, is done for the others of the team afterwards
     __device__ __forceinline__ void sync() const
     {
         if (SOLO) {
@@ -290,117 +290,130 @@ struct RowTeam {
             __syncthreads();
         }
     }
-    // `red`: one float per wave, used by one call between two barriers; a barrier is in the call
-    template <int COUNT>
-    __device__ __forceinline__ void max_of(float (&v)[COUNT], float (*red)[16]) const
-    {
-#pragma unroll
-        for (int i = 0; i < COUNT; ++i) v[i] = wave_max(v[i]);
-        if (SOLO) return;
-        if (lane == 0)
-#pragma unroll
-            for (int i = 0; i < COUNT; ++i) red[i][wave] = v[i];
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < COUNT; ++i) {
-            v[i] = red[i][0];
-            for (int w = 1; w < waves; ++w) v[i] = fmaxf(v[i], red[i][w]);
-        }
-    }
-    template <int COUNT>
-    __device__ __forceinline__ void sum_of(float (&v)[COUNT], float (*red)[16]) const
-    {
-#pragma unroll
-        for (int i = 0; i < COUNT; ++i) v[i] = wave_sum(v[i]);
-        if (SOLO) return;
-        if (lane == 0)
-#pragma unroll
-            for (int i = 0; i < COUNT; ++i) red[i][wave] = v[i];
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < COUNT; ++i) {
-            v[i] = red[i][0];
-            for (int w = 1; w < waves; ++w) v[i] += red[i][w];
-        }
-    }
 };
 
-// The row's entries in LDS: classes, probabilities (up to 1 / sum), logits of the student there.
-struct Entries { int *idx; float *prob, *zk; };
+// The row's entries in LDS: classes and probabilities, by fours (class -1, probability 0 after the last), then the
+// student's logits there.
+struct Entries {
+    int *idx;
+    float *prob, *zk;
+};
+
+__device__ __forceinline__ int entry_floats(int K) { return 3 * ((K + 3) & ~3); }
 
 __device__ __forceinline__ Entries entries_at(float *lds, int K)
 {
-    return {reinterpret_cast<int *>(lds), lds + K, lds + 2 * K};
+    const int k4 = (K + 3) & ~3;
+    return {reinterpret_cast<int *>(lds), lds + k4, lds + 2 * k4};
 }
 
-// Reads a thread's share of the entries; has: whether one names a class; returns the largest of the teacher's logits.
-// zk: the student's logit where the class lies in [lo, hi).
-template <typename T, bool SOLO>
-__device__ __forceinline__ float read_entries(const LossArgs &a, const RowTeam<SOLO> &team, const Entries &e, const T *z, int n, int lo,
-                                              int hi, float &has)
+// Whether an entry of the row names a class; every wave finds out for itself.
+__device__ __forceinline__ bool row_has_entry(const LossArgs &a, int n, int lane)
 {
+    bool has = false;
+    for (int k = lane; k < a.K; k += 64) has |= class_at(a.top_idx, (int64_t)n * a.K + k, a.wide_index, a.V) >= 0;
+    return __any(has);
+}
+
+// One wave fills the entries in and takes the teacher's softmax.  zk: the student's logit where the class lies in [lo, hi).
+template <typename T>
+__device__ __forceinline__ void read_entries(const LossArgs &a, const Entries &e, const T *z, int n, int lo, int hi, int lane)
+{
+    const int k4 = (a.K + 3) & ~3;
     float tm = -INFINITY;
-    has = 0.f;
-    for (int k = team.id; k < a.K; k += team.size) {
-        const int64_t i = (int64_t)n * a.K + k;
-        const int v = class_at(a.top_idx, i, a.wide_index, a.V);
-        const float t = teacher_logit(a, i);
-        e.idx[k] = v;
-        e.prob[k] = v >= 0 ? t : -INFINITY;
-        e.zk[k] = v >= lo && v < hi ? ld_elem(z, v) : 0.f;
-        if (v >= 0) {
-            has = 1.f;
-            tm = fmaxf(tm, t);
+    for (int k = lane; k < k4; k += 64) {
+        int v = -1;
+        float t = -INFINITY;
+        if (k < a.K) {
+            const int64_t i = (int64_t)n * a.K + k;
+            v = class_at(a.top_idx, i, a.wide_index, a.V);
+            if (v >= 0) t = teacher_logit(a, i);
+            e.zk[k] = v >= lo && v < hi ? ld_elem(z, v) : 0.f;
         }
+        e.idx[k] = v;
+        e.prob[k] = t;
+        tm = fmaxf(tm, t);
     }
-    return tm;
-}
-
-// exp((t - tm) / T) of a thread's share, into prob; returns their sum
-template <bool SOLO>
-__device__ __forceinline__ float weigh_entries(const LossArgs &a, const RowTeam<SOLO> &team, const Entries &e, float tm)
-{
+    tm = wave_max(tm);
     float ts = 0.f;
-    for (int k = team.id; k < a.K; k += team.size) {
+    for (int k = lane; k < k4; k += 64) {
         const float p = e.idx[k] >= 0 ? exp2_of((e.prob[k] - tm) * a.to_2T) : 0.f;
         e.prob[k] = p;
         ts += p;
     }
-    return ts;
+    ts = wave_sum(ts);
+    for (int k = lane; k < k4; k += 64)
+        if (e.idx[k] >= 0) e.prob[k] /= ts;
 }
 
-// T sum_k p_k (log p_k - log q_k) over a thread's share, as sum_k p_k (T (log p_k + log sT) - (z_k - m)), in which no
-// distance is divided by a small T; zk from `named` where given
-template <bool SOLO>
-__device__ __forceinline__ float divergence(const LossArgs &a, const RowTeam<SOLO> &team, const Entries &e, const float *named,
-                                            float inv_ts, float m, float sT)
+// The wave that has filled the entries in: T sum_k p_k (log p_k - log q_k), as sum_k p_k (T (log p_k + log sT) - (z_k - m)),
+// in which no distance is divided by a small T; zk from `named` where given.
+__device__ __forceinline__ float divergence(const LossArgs &a, const Entries &e, const float *named, float m, float sT, int lane)
 {
     float kd = 0.f;
     const float log_sT = logf(sT);
-    for (int k = team.id; k < a.K; k += team.size) {
-        const float p = e.prob[k] * inv_ts;
+    for (int k = lane; k < a.K; k += 64) {
+        const float p = e.prob[k];
         if (e.idx[k] >= 0 && !(p <= 0.f)) kd += p * (a.T * (logf(p) + log_sT) - ((named ? named[k] : e.zk[k]) - m));
     }
-    return kd;
+    return wave_sum(kd);
 }
 
 // the classes in [lo, hi) that the targets name, whole
 template <typename T, bool SOLO>
-__device__ __forceinline__ void write_named(const LossArgs &a, const RowTeam<SOLO> &team, const Entries &e, T *dz, int label, float zl,
-                                            int lo, int hi, const RowExps &x, float ck, float cl, float share, float gl)
+__device__ __forceinline__ void write_named(const RowTeam<SOLO> &team, const Entries &e, int K, T *dz, int label, float zl, int lo,
+                                            int hi, const RowExps &x, float ck, float cl, float share, float gl)
 {
-    for (int k = team.id; k <= a.K; k += team.size) {
-        const int v = k < a.K ? e.idx[k] : label;
+    typedef int i32x4 __attribute__((ext_vector_type(4)));
+    for (int k = team.id; k <= K; k += team.size) {
+        const int v = k < K ? e.idx[k] : label;
         if (v < lo || v >= hi) continue;
         float p = 0.f;
         bool first = true;
-        for (int j = 0; j < a.K; ++j)
-            if (e.idx[j] == v) {
-                p += e.prob[j];
-                if (j < k) first = false;
+#pragma unroll 4
+        for (int j = 0; j < K; j += 4) {
+            const i32x4 i4 = *reinterpret_cast<const i32x4 *>(e.idx + j);
+            const f32x4 p4 = *reinterpret_cast<const f32x4 *>(e.prob + j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p += i4[i] == v ? p4[i] : 0.f;
+                first &= i4[i] != v || j + i >= k;
             }
-        if (first) st_elem(dz, v, x.mix(k < a.K ? e.zk[k] : zl, ck, cl) - (share * p + (v == label ? gl : 0.f)));
+        }
+        if (first) st_elem(dz, v, x.mix(k < K ? e.zk[k] : zl, ck, cl) - (share * p + (v == label ? gl : 0.f)));
     }
+}
+
+// Joins m, sT and s1 of `count` parts (three floats each at p) over the lanes of a wave; sums relative to the maximum of all.
+__device__ __forceinline__ void join_parts(const LossArgs &a, const float *p, int count, int lane, float &m, float &sT, float &s1)
+{
+    m = -INFINITY;
+    for (int i = lane; i < count; i += 64) m = fmaxf(m, p[3 * i]);
+    m = wave_max(m);
+    sT = s1 = 0.f;
+    for (int i = lane; i < count; i += 64) {
+        const float d = p[3 * i] - m;
+        sT += p[3 * i + 1] * exp2_of(d * a.to_2T);
+        s1 += p[3 * i + 2] * exp2_of(d * a.to_21);
+    }
+    sT = wave_sum(sT);
+    s1 = wave_sum(s1);
+}
+
+// A wave's share of a row, relative to its own maximum (so no barrier stands between maximum and sums).  A share without any
+// class has sums of 0.
+template <typename T, int R>
+__device__ __forceinline__ void share_sums(const LossArgs &a, typename Vec<T>::Raw (&raw)[R], bool temp, bool one, float &m, float &sT,
+                                           float &s1)
+{
+    m = wave_max(row_max<T, R>(raw));
+    const RowExps x(a, m == -INFINITY ? 0.f : m, temp, one);
+    sT = s1 = 0.f;
+    open_again(raw);
+    x.template sums<T, R>(raw, sT, s1);
+    sT = wave_sum(sT);
+    s1 = wave_sum(s1);
+    x.finish(sT, s1);
 }
 
 // ---------------------------------------------------------------------------
@@ -410,7 +423,7 @@ template <typename T, int R, bool SOLO, bool GRAD>
 __global__ __launch_bounds__(SOLO ? 256 : 1024, GRAD ? 8 : 6) void distill_rows(LossArgs a)
 {
     extern __shared__ float lds[];
-    __shared__ float red[7][16];
+    __shared__ float shares[16 * 3];
     const RowTeam<SOLO> team;
     const int n = SOLO ? uniform((int)(blockIdx.x * 4 + (threadIdx.x >> 6))) : (int)blockIdx.x;
     if (SOLO && n >= a.N) return;
@@ -420,35 +433,34 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, GRAD ? 8 : 6) void distill_rows(
     typename Vec<T>::Raw raw[R];
     row_read<T, R>(raw, z, a.V, c0, cn, team.lane);
     const int label = a.labels ? class_at(a.labels, n, a.wide_index, a.V) : -1;
-    const float zl = label >= 0 ? ld_elem(z, label) : 0.f;
-    const Entries e = entries_at(lds + (SOLO ? (int)(threadIdx.x >> 6) * 3 * a.K : 0), a.K);
-    float most[3];
-    most[1] = read_entries(a, team, e, z, n, 0, a.V, most[2]);
-    most[0] = row_max<T, R>(raw);
-    team.max_of(most, red);
-    const float m = most[0], tm = most[1];
-    const bool has = most[2] > 0.f;
+    const bool has = row_has_entry(a, n, team.lane);
     if (!has && label < 0) {                              // nothing to learn from, whatever the logits are
         if (team.id == 0) a.loss[n] = 0.f;
         if (a.stats && team.id < 3) a.stats[(int64_t)n * 3 + team.id] = 0.f;
         if (GRAD) row_clear<T, R>(a, dz, c0, cn, team.lane);
         return;
     }
+    const float zl = label >= 0 ? ld_elem(z, label) : 0.f;
+    const Entries e = entries_at(lds + (SOLO ? (int)(threadIdx.x >> 6) * entry_floats(a.K) : 0), a.K);
+    if (has && team.wave == 0) read_entries(a, e, z, n, 0, a.V, team.lane);
     // statistics are asked for whole; without them a term without target needs no sum
-    const RowExps x(a, m, a.K > 0 && (has || a.stats), label >= 0 || a.stats);
-    float sums[3] = {0.f, 0.f, 0.f};
-    sums[2] = weigh_entries(a, team, e, tm);
-    open_again(raw);
-    x.template sums<T, R>(raw, sums[0], sums[1]);
-    team.sum_of(sums, red + 3);
-    float sT = sums[0], s1 = sums[1];
-    x.finish(sT, s1);
-    const float inv_ts = has ? 1.f / sums[2] : 0.f;
-    if (a.stats && team.id == 0) {
-        a.stats[(int64_t)n * 3] = m;
-        a.stats[(int64_t)n * 3 + 1] = sT;
-        a.stats[(int64_t)n * 3 + 2] = s1;
+    const bool temp = a.K > 0 && (has || a.stats), one = label >= 0 || a.stats;
+    float m, sT, s1;
+    share_sums<T, R>(a, raw, temp, one, m, sT, s1);
+    if (!SOLO) {
+        if (team.lane == 0) {
+            shares[3 * team.wave] = m;
+            shares[3 * team.wave + 1] = sT;
+            shares[3 * team.wave + 2] = s1;
+        }
+        __syncthreads();                                  // also: the row is read, the entries are there
+        join_parts(a, shares, team.waves, team.lane, m, sT, s1);
+    } else {
+        if (m == -INFINITY) sT = s1 = NAN;                // no class left
+        team.sync();
     }
+    if (!a.K) sT = s1;
+    const RowExps x(a, m, has, label >= 0);
     float gk = 0.f, gl = 0.f, ck = 0.f, cl = 0.f;
     if (GRAD) {
         const float g = a.grad_scale * (a.grad ? a.grad[n] : 1.f);
@@ -458,13 +470,20 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, GRAD ? 8 : 6) void distill_rows(
         open_again(raw);
         x.template write<T, R>(a, raw, dz, c0, cn, team.lane, ck, cl);
     }
-    float kd[1] = {has ? divergence(a, team, e, nullptr, inv_ts, m, sT) : 0.f};
-    team.sum_of(kd, red + 6);
-    if (team.id == 0)
-        a.loss[n] = (has ? a.wk * a.T * kd[0] : 0.f) + (label >= 0 ? a.wl * (logf(s1) - (zl - m)) : 0.f);
+    if (team.wave == 0) {
+        const float kd = has ? divergence(a, e, nullptr, m, sT, team.lane) : 0.f;
+        if (team.lane == 0) {
+            a.loss[n] = (has ? a.wk * a.T * kd : 0.f) + (label >= 0 ? a.wl * (logf(s1) - (zl - m)) : 0.f);
+            if (a.stats) {
+                a.stats[(int64_t)n * 3] = m;
+                a.stats[(int64_t)n * 3 + 1] = sT;
+                a.stats[(int64_t)n * 3 + 2] = s1;
+            }
+        }
+    }
     if (GRAD) {
-        team.sync();
-        write_named(a, team, e, dz, label, zl, 0, a.V, x, ck, cl, gk * inv_ts, gl);
+        team.sync();                                      // the softmax's share is written: the targets' classes may be again
+        write_named(team, e, has ? a.K : 0, dz, label, zl, 0, a.V, x, ck, cl, gk, gl);
     }
 }
 
@@ -476,7 +495,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, GRAD ? 8 : 6) void distill_rows(
 template <typename T, int R>
 __global__ __launch_bounds__(512, 8) void distill_part_sums(LossArgs a)
 {
-    __shared__ float red[3][16];
+    __shared__ float shares[8 * 3];
     const RowTeam<false> team;
     const int n = fastdiv(blockIdx.x, a.div_parts), part = blockIdx.x - n * a.parts;
     const T *z = static_cast<const T *>(a.z) + n * a.z_stride;
@@ -492,21 +511,26 @@ __global__ __launch_bounds__(512, 8) void distill_part_sums(LossArgs a)
             named[k] = v >= 0 ? ld_elem(z, v) : 0.f;
         }
     }
-    float m[1] = {row_max<T, R>(raw)};
-    team.max_of(m, red);
-    float s[2] = {0.f, 0.f};
-    // of a part without any class left the sums are 0
-    const float top = m[0] == -INFINITY ? 0.f : m[0];
-    const RowExps x(a, top, a.K > 0, true);
-    open_again(raw);
-    x.template sums<T, R>(raw, s[0], s[1]);
-    team.sum_of(s, red + 1);
-    x.finish(s[0], s[1]);
-    if (team.id == 0) {
+    float m, sT, s1;
+    share_sums<T, R>(a, raw, a.K > 0, true, m, sT, s1);
+    if (team.lane == 0) {
+        shares[3 * team.wave] = m;
+        shares[3 * team.wave + 1] = sT;
+        shares[3 * team.wave + 2] = s1;
+    }
+    __syncthreads();
+    if (team.wave > 0) return;
+    join_parts(a, shares, team.waves, team.lane, m, sT, s1);
+    if (m == -INFINITY && sT != sT) {                    // no class in the part (or a NaN in it, which the sums of a wave tell)
+        bool nan = false;
+        for (int i = team.lane; i < team.waves; i += 64) nan |= shares[3 * i + 2] != shares[3 * i + 2];
+        if (!__any(nan)) sT = s1 = 0.f;
+    }
+    if (team.lane == 0) {
         float *p = a.part + (int64_t)blockIdx.x * 3;
-        p[0] = m[0];
-        p[1] = s[0];
-        p[2] = s[1];
+        p[0] = m;
+        p[1] = sT;
+        p[2] = s1;
     }
 }
 
@@ -517,7 +541,6 @@ __global__ __launch_bounds__(512, 8) void distill_part_apply(LossArgs a)
 {
     constexpr int V = Vec<T>::V;
     extern __shared__ float lds[];
-    __shared__ float red[3][16];
     const RowTeam<false> team;
     const int n = GRAD ? fastdiv(blockIdx.x, a.div_parts) : (int)blockIdx.x, part = GRAD ? blockIdx.x - n * a.parts : 0;
     const T *z = static_cast<const T *>(a.z) + n * a.z_stride;
@@ -529,14 +552,7 @@ __global__ __launch_bounds__(512, 8) void distill_part_apply(LossArgs a)
     // classes [lo, hi) are this work-group's to write
     const int lo = first * 64 * V, hi = (int)min((int64_t)last * 64 * V, (int64_t)a.V);
     const int label = a.labels ? class_at(a.labels, n, a.wide_index, a.V) : -1;
-    const float zl = GRAD && label >= lo && label < hi ? ld_elem(z, label) : 0.f;
-    const Entries e = entries_at(lds, a.K);
-    float most[1], dummy;
-    most[0] = read_entries(a, team, e, z, n, GRAD ? lo : 0, GRAD ? hi : 0, dummy);
-    // every wave for itself: whether an entry names a class
-    bool has = false;
-    for (int k = team.lane; k < a.K; k += 64) has |= class_at(a.top_idx, (int64_t)n * a.K + k, a.wide_index, a.V) >= 0;
-    has = __any(has);
+    const bool has = row_has_entry(a, n, team.lane);
     const bool lead = part == 0 && a.loss;
     if (!has && label < 0) {
         if (lead && team.id == 0) a.loss[n] = 0.f;
@@ -544,46 +560,33 @@ __global__ __launch_bounds__(512, 8) void distill_part_apply(LossArgs a)
         if (GRAD) row_clear<T, R>(a, dz, c0, cn, team.lane);
         return;
     }
+    const float zl = GRAD && label >= lo && label < hi ? ld_elem(z, label) : 0.f;
+    const Entries e = entries_at(lds, a.K);
+    if (has && team.wave == 0) read_entries(a, e, z, n, GRAD ? lo : 0, GRAD ? hi : 0, team.lane);
     float m, sT, s1;
     if (a.row_stats) {
         m = a.row_stats[(int64_t)n * 3];
         sT = a.row_stats[(int64_t)n * 3 + 1];
         s1 = a.row_stats[(int64_t)n * 3 + 2];
     } else {
-        const float *p = a.part + (int64_t)n * a.parts * 3;
-        m = -INFINITY;
-        for (int i = team.lane; i < a.parts; i += 64) m = fmaxf(m, p[3 * i]);
-        m = wave_max(m);
-        sT = s1 = 0.f;
-        for (int i = team.lane; i < a.parts; i += 64) {
-            const float d = p[3 * i] - m;
-            sT += p[3 * i + 1] * exp2_of(d * a.to_2T);
-            s1 += p[3 * i + 2] * exp2_of(d * a.to_21);
-        }
-        sT = wave_sum(sT);
-        s1 = wave_sum(s1);
+        join_parts(a, a.part + (int64_t)n * a.parts * 3, a.parts, team.lane, m, sT, s1);
         if (!a.K) sT = s1;
     }
     const RowExps x(a, m, has, label >= 0);
-    team.max_of(most, red);                  // (a barrier: the logits that targets name are read, their places may be written)
     float gk = 0.f, gl = 0.f, ck = 0.f, cl = 0.f;
     if (GRAD) {
         const float g = a.grad_scale * (a.grad ? a.grad[n] : 1.f);
         if (has) { gk = g * a.wk * a.T; ck = gk / sT; }
         if (label >= 0) { gl = g * a.wl; cl = gl / s1; }
         x.factors(ck, cl);
-        open_again(raw);
+        __syncthreads();                                  // the logits that targets name are read: their places may be written
         x.template write<T, R>(a, raw, dz, c0, cn, team.lane, ck, cl);
     }
-    float ts[1] = {weigh_entries(a, team, e, most[0])};
-    team.sum_of(ts, red + 1);                // (a barrier: the softmax's share is written, targets may be written over it)
-    const float inv_ts = has ? 1.f / ts[0] : 0.f;
-    if (lead) {
+    if (lead && team.wave == 0) {
         const float *named = a.named + (int64_t)n * (a.K + 1);
-        float kd[1] = {has ? divergence(a, team, e, named, inv_ts, m, sT) : 0.f};
-        team.sum_of(kd, red + 2);
-        if (team.id == 0) {
-            a.loss[n] = (has ? a.wk * a.T * kd[0] : 0.f) + (label >= 0 ? a.wl * (logf(s1) - (named[a.K] - m)) : 0.f);
+        const float kd = has ? divergence(a, e, named, m, sT, team.lane) : 0.f;
+        if (team.lane == 0) {
+            a.loss[n] = (has ? a.wk * a.T * kd : 0.f) + (label >= 0 ? a.wl * (logf(s1) - (named[a.K] - m)) : 0.f);
             if (a.stats) {
                 a.stats[(int64_t)n * 3] = m;
                 a.stats[(int64_t)n * 3 + 1] = sT;
@@ -591,5 +594,8 @@ __global__ __launch_bounds__(512, 8) void distill_part_apply(LossArgs a)
             }
         }
     }
-    if (GRAD) write_named(a, team, e, dz, label, zl, lo, hi, x, ck, cl, gk * inv_ts, gl);
+    if (GRAD) {
+        __syncthreads();                                  // the softmax's share is written: the targets' classes may be again
+        write_named(team, e, has ? a.K : 0, dz, label, zl, lo, hi, x, ck, cl, gk, gl);
+    }
 }

@@ -435,7 +435,7 @@ void launch_loss(Kern kern, const LossArgs &a, int64_t blocks, int threads, size
 template <typename T, bool GRAD>
 int run_loss_typed(const LossArgs &a, const LossPlan &p, hipStream_t st)
 {
-    const size_t lds = (size_t)(p.solo ? 4 : 1) * 3 * a.K * 4;
+    const size_t lds = (size_t)(p.solo ? 4 : 1) * 3 * round_up(a.K, 4) * 4;
     if constexpr (GRAD)
         if (a.row_stats) {
             launch_loss(distill_part_apply<T, kPartRun, true>, a, p.blocks, p.threads, lds, st);

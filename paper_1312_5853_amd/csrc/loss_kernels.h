@@ -307,29 +307,49 @@ __device__ __forceinline__ Entries entries_at(float *lds, int K)
     return {reinterpret_cast<int *>(lds), lds + k4, lds + 2 * k4};
 }
 
-// Whether an entry of the row names a class; every wave finds out for itself.
-__device__ __forceinline__ bool row_has_entry(const LossArgs &a, int n, int lane)
-{
-    bool has = false;
-    for (int k = lane; k < a.K; k += 64) has |= class_at(a.top_idx, (int64_t)n * a.K + k, a.wide_index, a.V) >= 0;
-    return __any(has);
-}
+// A row's label and the first 64 entries, one to a lane.  Read before the row, as loads come back in order and what the
+// entries name is read next.
+struct Targets {
+    int label, v;                    // classes, or -1
+    float t;                         // the teacher's logit
+    __device__ __forceinline__ Targets(const LossArgs &a, int n, int lane)
+    {
+        label = a.labels ? class_at(a.labels, n, a.wide_index, a.V) : -1;
+        v = -1;
+        t = -INFINITY;
+        if (lane < a.K) {
+            v = class_at(a.top_idx, (int64_t)n * a.K + lane, a.wide_index, a.V);
+            t = teacher_logit(a, (int64_t)n * a.K + lane);
+        }
+    }
+    // whether an entry of the row names a class; every wave finds out for itself
+    __device__ __forceinline__ bool any(const LossArgs &a, int n, int lane) const
+    {
+        bool has = v >= 0;
+        for (int k = lane + 64; k < a.K; k += 64) has |= class_at(a.top_idx, (int64_t)n * a.K + k, a.wide_index, a.V) >= 0;
+        return __any(has);
+    }
+};
 
 // One wave fills the entries in and takes the teacher's softmax.  zk: the student's logit where the class lies in [lo, hi).
 template <typename T>
-__device__ __forceinline__ void read_entries(const LossArgs &a, const Entries &e, const T *z, int n, int lo, int hi, int lane)
+__device__ __forceinline__ void read_entries(const LossArgs &a, const Entries &e, const Targets &first, const T *z, int n, int lo, int hi,
+                                             int lane)
 {
     const int k4 = (a.K + 3) & ~3;
     float tm = -INFINITY;
+    int v = first.v;
+    float t = first.t;
     for (int k = lane; k < k4; k += 64) {
-        int v = -1;
-        float t = -INFINITY;
-        if (k < a.K) {
-            const int64_t i = (int64_t)n * a.K + k;
-            v = class_at(a.top_idx, i, a.wide_index, a.V);
-            if (v >= 0) t = teacher_logit(a, i);
-            e.zk[k] = v >= lo && v < hi ? ld_elem(z, v) : 0.f;
+        if (k >= 64) {
+            v = -1;
+            if (k < a.K) {
+                v = class_at(a.top_idx, (int64_t)n * a.K + k, a.wide_index, a.V);
+                t = teacher_logit(a, (int64_t)n * a.K + k);
+            }
         }
+        if (v < 0) t = -INFINITY;
+        e.zk[k] = v >= lo && v < hi ? ld_elem(z, v) : 0.f;
         e.idx[k] = v;
         e.prob[k] = t;
         tm = fmaxf(tm, t);
@@ -347,14 +367,15 @@ __device__ __forceinline__ void read_entries(const LossArgs &a, const Entries &e
 }
 
 // The wave that has filled the entries in: T sum_k p_k (log p_k - log q_k), as sum_k p_k (T (log p_k + log sT) - (z_k - m)),
-// in which no distance is divided by a small T; zk from `named` where given.
-__device__ __forceinline__ float divergence(const LossArgs &a, const Entries &e, const float *named, float m, float sT, int lane)
+// in which no distance is divided by a small T; zk from `named` where given (the first 64 in `early`).
+__device__ __forceinline__ float divergence(const LossArgs &a, const Entries &e, const float *named, float early, float m, float sT,
+                                            int lane)
 {
     float kd = 0.f;
     const float log_sT = logf(sT);
     for (int k = lane; k < a.K; k += 64) {
-        const float p = e.prob[k];
-        if (e.idx[k] >= 0 && !(p <= 0.f)) kd += p * (a.T * (logf(p) + log_sT) - ((named ? named[k] : e.zk[k]) - m));
+        const float p = e.prob[k], zk = !named ? e.zk[k] : k < 64 ? early : named[k];
+        if (e.idx[k] >= 0 && !(p <= 0.f)) kd += p * (a.T * (logf(p) + log_sT) - (zk - m));
     }
     return wave_sum(kd);
 }
@@ -430,10 +451,11 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, GRAD ? 8 : 6) void distill_rows(
     const T *z = static_cast<const T *>(a.z) + n * a.z_stride;
     T *dz = static_cast<T *>(a.dz) + n * a.dz_stride;
     const int c0 = team.wave * a.run, cn = min(a.run, a.chunks - c0);
+    const Targets targets(a, n, team.lane);
     typename Vec<T>::Raw raw[R];
     row_read<T, R>(raw, z, a.V, c0, cn, team.lane);
-    const int label = a.labels ? class_at(a.labels, n, a.wide_index, a.V) : -1;
-    const bool has = row_has_entry(a, n, team.lane);
+    const int label = targets.label;
+    const bool has = targets.any(a, n, team.lane);
     if (!has && label < 0) {                              // nothing to learn from, whatever the logits are
         if (team.id == 0) a.loss[n] = 0.f;
         if (a.stats && team.id < 3) a.stats[(int64_t)n * 3 + team.id] = 0.f;
@@ -442,7 +464,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, GRAD ? 8 : 6) void distill_rows(
     }
     const float zl = label >= 0 ? ld_elem(z, label) : 0.f;
     const Entries e = entries_at(lds + (SOLO ? (int)(threadIdx.x >> 6) * entry_floats(a.K) : 0), a.K);
-    if (has && team.wave == 0) read_entries(a, e, z, n, 0, a.V, team.lane);
+    if (has && team.wave == 0) read_entries(a, e, targets, z, n, 0, a.V, team.lane);
     // statistics are asked for whole; without them a term without target needs no sum
     const bool temp = a.K > 0 && (has || a.stats), one = label >= 0 || a.stats;
     float m, sT, s1;
@@ -471,7 +493,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, GRAD ? 8 : 6) void distill_rows(
         x.template write<T, R>(a, raw, dz, c0, cn, team.lane, ck, cl);
     }
     if (team.wave == 0) {
-        const float kd = has ? divergence(a, e, nullptr, m, sT, team.lane) : 0.f;
+        const float kd = has ? divergence(a, e, nullptr, 0.f, m, sT, team.lane) : 0.f;
         if (team.lane == 0) {
             a.loss[n] = (has ? a.wk * a.T * kd : 0.f) + (label >= 0 ? a.wl * (logf(s1) - (zl - m)) : 0.f);
             if (a.stats) {
@@ -493,9 +515,9 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, GRAD ? 8 : 6) void distill_rows(
 // m, sT and s1 of a part; the first part's work-group also puts aside the logits that the targets name, as the gradient
 // may take their place.
 template <typename T, int R>
-__global__ __launch_bounds__(512, 8) void distill_part_sums(LossArgs a)
+__global__ __launch_bounds__(256, 8) void distill_part_sums(LossArgs a)
 {
-    __shared__ float shares[8 * 3];
+    __shared__ float shares[4 * 3];
     const RowTeam<false> team;
     const int n = fastdiv(blockIdx.x, a.div_parts), part = blockIdx.x - n * a.parts;
     const T *z = static_cast<const T *>(a.z) + n * a.z_stride;
@@ -537,7 +559,7 @@ __global__ __launch_bounds__(512, 8) void distill_part_sums(LossArgs a)
 // Joins the parts (or takes the statistics given).  GRAD: a work-group writes its part's gradient, and the first part's
 // also the row's loss where asked for; otherwise one work-group per row writes the loss.
 template <typename T, int R, bool GRAD>
-__global__ __launch_bounds__(512, 8) void distill_part_apply(LossArgs a)
+__global__ __launch_bounds__(256, 8) void distill_part_apply(LossArgs a)
 {
     constexpr int V = Vec<T>::V;
     extern __shared__ float lds[];
@@ -547,22 +569,10 @@ __global__ __launch_bounds__(512, 8) void distill_part_apply(LossArgs a)
     T *dz = static_cast<T *>(a.dz) + n * a.dz_stride;
     const int first = part * a.part_chunks, last = min(first + a.part_chunks, a.chunks);
     const int c0 = first + team.wave * a.run, cn = min(a.run, last - c0);
-    typename Vec<T>::Raw raw[R];
-    if (GRAD) row_read<T, R>(raw, z, a.V, c0, cn, team.lane);
-    // classes [lo, hi) are this work-group's to write
-    const int lo = first * 64 * V, hi = (int)min((int64_t)last * 64 * V, (int64_t)a.V);
-    const int label = a.labels ? class_at(a.labels, n, a.wide_index, a.V) : -1;
-    const bool has = row_has_entry(a, n, team.lane);
     const bool lead = part == 0 && a.loss;
-    if (!has && label < 0) {
-        if (lead && team.id == 0) a.loss[n] = 0.f;
-        if (lead && a.stats && team.id < 3) a.stats[(int64_t)n * 3 + team.id] = 0.f;
-        if (GRAD) row_clear<T, R>(a, dz, c0, cn, team.lane);
-        return;
-    }
-    const float zl = GRAD && label >= lo && label < hi ? ld_elem(z, label) : 0.f;
-    const Entries e = entries_at(lds, a.K);
-    if (has && team.wave == 0) read_entries(a, e, z, n, GRAD ? lo : 0, GRAD ? hi : 0, team.lane);
+    const float *named = a.named + (int64_t)n * (a.K + 1);
+    const Targets targets(a, n, team.lane);
+    const float early = lead && team.lane < a.K ? named[team.lane] : 0.f, named_label = lead ? named[a.K] : 0.f;
     float m, sT, s1;
     if (a.row_stats) {
         m = a.row_stats[(int64_t)n * 3];
@@ -572,6 +582,21 @@ __global__ __launch_bounds__(512, 8) void distill_part_apply(LossArgs a)
         join_parts(a, a.part + (int64_t)n * a.parts * 3, a.parts, team.lane, m, sT, s1);
         if (!a.K) sT = s1;
     }
+    typename Vec<T>::Raw raw[R];
+    if (GRAD) row_read<T, R>(raw, z, a.V, c0, cn, team.lane);
+    // classes [lo, hi) are this work-group's to write
+    const int lo = first * 64 * V, hi = (int)min((int64_t)last * 64 * V, (int64_t)a.V);
+    const int label = targets.label;
+    const bool has = targets.any(a, n, team.lane);
+    if (!has && label < 0) {
+        if (lead && team.id == 0) a.loss[n] = 0.f;
+        if (lead && a.stats && team.id < 3) a.stats[(int64_t)n * 3 + team.id] = 0.f;
+        if (GRAD) row_clear<T, R>(a, dz, c0, cn, team.lane);
+        return;
+    }
+    const float zl = GRAD && label >= lo && label < hi ? ld_elem(z, label) : 0.f;
+    const Entries e = entries_at(lds, a.K);
+    if (has && team.wave == 0) read_entries(a, e, targets, z, n, GRAD ? lo : 0, GRAD ? hi : 0, team.lane);
     const RowExps x(a, m, has, label >= 0);
     float gk = 0.f, gl = 0.f, ck = 0.f, cl = 0.f;
     if (GRAD) {
@@ -583,10 +608,9 @@ __global__ __launch_bounds__(512, 8) void distill_part_apply(LossArgs a)
         x.template write<T, R>(a, raw, dz, c0, cn, team.lane, ck, cl);
     }
     if (lead && team.wave == 0) {
-        const float *named = a.named + (int64_t)n * (a.K + 1);
-        const float kd = has ? divergence(a, e, named, m, sT, team.lane) : 0.f;
+        const float kd = has ? divergence(a, e, named, early, m, sT, team.lane) : 0.f;
         if (team.lane == 0) {
-            a.loss[n] = (has ? a.wk * a.T * kd : 0.f) + (label >= 0 ? a.wl * (logf(s1) - (named[a.K] - m)) : 0.f);
+            a.loss[n] = (has ? a.wk * a.T * kd : 0.f) + (label >= 0 ? a.wl * (logf(s1) - (named_label - m)) : 0.f);
             if (a.stats) {
                 a.stats[(int64_t)n * 3] = m;
                 a.stats[(int64_t)n * 3 + 1] = sT;

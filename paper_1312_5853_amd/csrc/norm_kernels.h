@@ -29,10 +29,11 @@ struct NormArgs {
     const float *gamma, *beta;       // nullptr: ones, zeros
     float *mean, *rstd;              // forward: results (nullptr: not wanted); backward and kApply: read
     float *part;                     // sums of tiles.  forward: {mean, sum of squares, count}; backward: A, then B, of a row of C
+    float *joined;                   // forward kApply, unless it joins the tiles itself (join): means, then rstds
     float *group_sums;               // backward kApply: {m1, m2} of every sample and group
     float *sample_sums;              // backward: A, then B, of every sample and channel (`part` itself where a sample has one row)
     float *dgamma, *dbeta;
-    int N, C, S, groups, cpg, act;
+    int N, C, S, groups, cpg, act, join;
     float eps, inv_m;                // inv_m: 1 / M
     FastDiv div_groups, div_cpg;
     int part_rows, rows_per_sample;  // rows of C sums in `part`, and of those a sample's
@@ -92,6 +93,36 @@ __device__ __forceinline__ float join_waves(float v, float *red, int nw)
     float s = red[0];
     for (int i = 1; i < nw; ++i) s += red[i];
     return s;
+}
+
+// The tiles' means and squared distances of a group, joined to the group's over the lanes of a wave: four tiles of a lane
+// at a time (their loads in flight together), these with the lane's others, then the lanes.
+__device__ __forceinline__ void join_tiles(const NormArgs &a, int64_t group, int lane, float &mean, float &rstd)
+{
+    const float *p = a.part + group * a.tiles * 3;
+    float n = 0.f, m = 0.f, d = 0.f;
+    for (int t0 = lane; t0 < a.tiles; t0 += 256) {
+        float tm[4], td[4], tn[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int t = min(t0 + 64 * u, a.tiles - 1);
+            tm[u] = p[3 * t];
+            td[u] = p[3 * t + 1];
+            tn[u] = t0 + 64 * u < a.tiles ? p[3 * t + 2] : 0.f;
+        }
+        const float cn = (tn[0] + tn[1]) + (tn[2] + tn[3]);
+        const float cm = (tm[0] * tn[0] + tm[1] * tn[1] + (tm[2] * tn[2] + tm[3] * tn[3])) / cn;
+        float cd = 0.f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) cd += tn[u] > 0.f ? td[u] + tn[u] * (tm[u] - cm) * (tm[u] - cm) : 0.f;
+        const float gap = cm - m, all = n + cn;
+        d += cd + gap * gap * n * cn / all;
+        m = n > 0.f ? m + gap * cn / all : cm;
+        n = all;
+    }
+    mean = wave_sum(n > 0.f ? m * n : 0.f) * a.inv_m;
+    d = wave_sum(n > 0.f ? d + n * (m - mean) * (m - mean) : 0.f);
+    rstd = 1.f / sqrtf(d * a.inv_m + a.eps);
 }
 
 // ---------------------------------------------------------------------------
@@ -214,8 +245,16 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_fwd(NormA
         }
     float mean, rstd;
     if (MODE == kApply) {
-        mean = a.mean[t.group];
-        rstd = a.rstd[t.group];
+        if (a.join) {
+            join_tiles(a, t.group, lane, mean, rstd);
+            if (t.tile == 0 && threadIdx.x == 0) {
+                if (a.mean) a.mean[t.group] = mean;
+                if (a.rstd) a.rstd[t.group] = rstd;
+            }
+        } else {
+            mean = a.joined[t.group];
+            rstd = a.joined[a.N * a.groups + t.group];
+        }
     } else {
         float s = 0.f, cnt = 0.f;
 #pragma unroll
@@ -686,8 +725,28 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
             }
         }
         if (MODE == kSums) return;
-        __syncthreads();
+    } else {
+        load(t.p);
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+        if (a.join) {
+            for (int g = wave; g < a.slab_groups; g += waves) {
+                float mean, rstd;
+                join_tiles(a, group0 + g, lane, mean, rstd);
+                if (lane == 0) {
+                    gmean[g] = mean;
+                    grstd[g] = rstd;
+                    if (t.tile == 0 && a.mean) a.mean[group0 + g] = mean;
+                    if (t.tile == 0 && a.rstd) a.rstd[group0 + g] = rstd;
+                }
+            }
+        } else {
+            for (int g = threadIdx.x; g < a.slab_groups; g += blockDim.x) {
+                gmean[g] = a.joined[group0 + g];
+                grstd[g] = a.joined[a.N * a.groups + group0 + g];
+            }
+        }
     }
+    __syncthreads();
     if (!t.on) return;
     float scale[V], shift[V];
     slab_params<V>(a, t, a.gamma, 1.f, scale);
@@ -698,8 +757,8 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
     for (int k = 0; k < V; ++k) {
         if (!ONE || k == 0) {
             const int g = walk.next(a);
-            mean = MODE == kApply ? a.mean[group0 + g] : gmean[g];
-            rstd = MODE == kApply ? a.rstd[group0 + g] : grstd[g];
+            mean = gmean[g];
+            rstd = grstd[g];
         }
         scale[k] *= rstd;
         shift[k] = fmaf(-mean, scale[k], shift[k]);
@@ -708,7 +767,7 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
     if (MODE == kWhole) open_again(raw);
     int p = t.p;
     do {
-        if (MODE == kApply) load(p);
+        if (MODE == kApply && p != t.p) load(p);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int s = p + r * a.rows;
@@ -900,22 +959,17 @@ __global__ __launch_bounds__(1024) void group_norm_last_bwd(NormArgs a)
 // ---------------------------------------------------------------------------
 // Joining the tiles
 // ---------------------------------------------------------------------------
-// A wave per sample and group: the tiles' means and squared distances, joined to the group's.
-__global__ __launch_bounds__(256) void group_norm_join_stats(const float *part, int tiles, int total, float inv_m, float eps,
-                                                             float *mean, float *rstd, float *mean_out, float *rstd_out)
+// A wave per sample and group, where the tiles are too many for every work-group to join them again.
+__global__ __launch_bounds__(256) void group_norm_join_stats(NormArgs a)
 {
-    const int lane = threadIdx.x & 63, i = blockIdx.x * 4 + (threadIdx.x >> 6);
-    const float *p = part + (int64_t)min(i, total - 1) * tiles * 3;
-    float s = 0.f, d = 0.f;
-    for (int t = lane; t < tiles; t += 64) s += p[3 * t] * p[3 * t + 2];
-    const float m = wave_sum(s) * inv_m;
-    for (int t = lane; t < tiles; t += 64) d += p[3 * t + 1] + p[3 * t + 2] * (p[3 * t] - m) * (p[3 * t] - m);
-    const float r = 1.f / sqrtf(wave_sum(d) * inv_m + eps);
+    const int lane = threadIdx.x & 63, total = a.N * a.groups, i = blockIdx.x * 4 + (threadIdx.x >> 6);
+    float mean, rstd;
+    join_tiles(a, min(i, total - 1), lane, mean, rstd);
     if (lane == 0 && i < total) {
-        mean[i] = m;
-        rstd[i] = r;
-        if (mean_out) mean_out[i] = m;
-        if (rstd_out) rstd_out[i] = r;
+        a.joined[i] = mean;
+        a.joined[total + i] = rstd;
+        if (a.mean) a.mean[i] = mean;
+        if (a.rstd) a.rstd[i] = rstd;
     }
 }
 
@@ -926,20 +980,29 @@ __global__ __launch_bounds__(256) void group_norm_join_groups(NormArgs a)
     const int grp = min(i, total - 1), n = fastdiv(grp, a.div_groups), c0 = (grp - n * a.groups) * a.cpg;
     const float *pa = a.part + (int64_t)n * a.rows_per_sample * a.C + c0, *pb = pa + (int64_t)a.part_rows * a.C;
     float m1 = 0.f, m2 = 0.f;
-    for (int c = 0; c < a.cpg; ++c) {
-        float A = 0.f, B = 0.f;
-        for (int t = lane; t < a.rows_per_sample; t += 64) {
-            A += pa[(int64_t)t * a.C + c];
-            B += pb[(int64_t)t * a.C + c];
-        }
-        A = wave_sum(A);
-        B = wave_sum(B);
-        const float gamma = a.gamma ? a.gamma[c0 + c] : 1.f;
-        m1 += gamma * A;
-        m2 += gamma * B;
-        if (lane == 0 && i < total) {
-            a.sample_sums[(int64_t)n * a.C + c0 + c] = A;
-            a.sample_sums[(int64_t)(a.N + n) * a.C + c0 + c] = B;
+    for (int c1 = 0; c1 < a.cpg; c1 += 4) {              // four channels at a time, their loads in flight together
+        float A[4] = {0.f, 0.f, 0.f, 0.f}, B[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int t = lane; t < a.rows_per_sample; t += 64)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int c = min(c1 + u, a.cpg - 1);
+                A[u] += pa[(int64_t)t * a.C + c];
+                B[u] += pb[(int64_t)t * a.C + c];
+            }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int c = c0 + c1 + u;
+            A[u] = wave_sum(A[u]);
+            B[u] = wave_sum(B[u]);
+            if (c1 + u < a.cpg) {
+                const float gamma = a.gamma ? a.gamma[c] : 1.f;
+                m1 += gamma * A[u];
+                m2 += gamma * B[u];
+                if (lane == 0 && i < total) {
+                    a.sample_sums[(int64_t)n * a.C + c] = A[u];
+                    a.sample_sums[(int64_t)(a.N + n) * a.C + c] = B[u];
+                }
+            }
         }
     }
     if (lane == 0 && i < total) {
@@ -948,27 +1011,36 @@ __global__ __launch_bounds__(256) void group_norm_join_groups(NormArgs a)
     }
 }
 
-// Gradients of gamma and beta: a work-group adds the samples' sums of 16 channels, 64 samples at a time, then in a tree.
-__global__ __launch_bounds__(1024) void group_norm_join_channels(NormArgs a)
+// Gradients of gamma and beta: a work-group adds the samples' sums of 16 channels; 16 threads to a channel, eight loads of
+// each kind in flight at once.
+__global__ __launch_bounds__(256) void group_norm_join_channels(NormArgs a)
 {
-    __shared__ float red[2][16][65];
-    const int x = threadIdx.x & 15, y = threadIdx.x >> 4, c = blockIdx.x * 16 + x;
+    __shared__ float red[2][16][17];
+    const int x = threadIdx.x & 15, y = threadIdx.x >> 4, c = min((int)(blockIdx.x * 16) + x, a.C - 1);
+    const float *pa = a.sample_sums + c, *pb = pa + (int64_t)a.N * a.C;
     float A = 0.f, B = 0.f;
-    if (c < a.C) {
-#pragma unroll 4
-        for (int n = y; n < a.N; n += 64) {
-            A += a.sample_sums[(int64_t)n * a.C + c];
-            B += a.sample_sums[(int64_t)(a.N + n) * a.C + c];
+    for (int n0 = y; n0 < a.N; n0 += 128) {
+        float va[8], vb[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int64_t n = min(n0 + 16 * u, a.N - 1);
+            va[u] = pa[n * a.C];
+            vb[u] = pb[n * a.C];
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            A += n0 + 16 * u < a.N ? va[u] : 0.f;
+            B += n0 + 16 * u < a.N ? vb[u] : 0.f;
         }
     }
     red[0][x][y] = A;
     red[1][x][y] = B;
     __syncthreads();
-    // a wave to a channel
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, ch = blockIdx.x * 16 + w;
-    A = wave_sum(red[0][w][lane]);
-    B = wave_sum(red[1][w][lane]);
-    if (lane == 0 && ch < a.C) {
+    // 16 lanes to a channel
+    const int ch = blockIdx.x * 16 + y;
+    A = run_sum(red[0][y][x], 16);
+    B = run_sum(red[1][y][x], 16);
+    if (x == 0 && ch < a.C) {
         if (a.dbeta) a.dbeta[ch] = A;
         if (a.dgamma) a.dgamma[ch] = B;
     }

@@ -151,8 +151,8 @@ void plan_last(NormPlan &p, bool bwd, int V, int eb)
         threads = std::max(512, round_up(a.lanes, 64));
         a.rows = threads / a.lanes;
         const int64_t N_slabs = (int64_t)a.N * (a.groups / j);
-        // as many rows to a thread as leave 1024 work-groups, 32 at most
-        const int most_rows = (int)std::max<int64_t>(4, std::min<int64_t>(32, (int64_t)N_slabs * ceil_div(a.S, a.rows) / 1024));
+        // as many rows to a thread as leave 512 work-groups, 32 at most
+        const int most_rows = (int)std::max<int64_t>(4, std::min<int64_t>(32, (int64_t)N_slabs * ceil_div(a.S, a.rows) / 512));
         a.tile_rows = std::min(a.S, a.rows * most_rows);
         a.tiles = ceil_div(a.S, a.tile_rows);
         a.tile_rows = ceil_div(a.S, a.tiles);
@@ -201,6 +201,7 @@ int plan_norm(NormPlan &p, int op, int N, int C, int S, int groups, int layout, 
         plan_last(p, bwd, V, eb);
     }
     a.div_tiles = make_fastdiv(a.tiles);
+    a.join = (int64_t)a.tiles * (p.planes ? 1 : a.slab_groups) <= 2048;
     if ((int64_t)N * a.rows_per_sample >= ((int64_t)1 << 31) || p.blocks >= ((int64_t)1 << 31)) return kErrTooLarge;
     a.part_rows = N * a.rows_per_sample;
     const int64_t ng = (int64_t)N * groups;
@@ -234,6 +235,7 @@ int norm_common(NormPlan &p, const NormArgs &given, int op, int N, int C, int S,
     p.a.act = a.act; p.a.eps = a.eps;
     p.a.part = static_cast<float *>(ws);
     p.a.group_sums = reinterpret_cast<float *>(static_cast<char *>(ws) + p.part_bytes);
+    p.a.joined = p.a.group_sums;
     p.a.sample_sums = p.split ? p.a.group_sums + (int64_t)2 * N * groups : p.a.part;
     return kStatusOk;
 }
@@ -260,8 +262,7 @@ void launch_norm_fwd(const NormPlan &p, hipStream_t st)
         else launch_norm(group_norm_planes_fwd<T, 8, false, MODE>, p, 0, st);
         return;
     }
-    const size_t lds = MODE == kApply ? 0 : p.lds;
-    auto go = [&](auto of_one, auto of_several) { launch_norm(p.one ? of_one : of_several, p, lds, st); };
+    auto go = [&](auto of_one, auto of_several) { launch_norm(p.one ? of_one : of_several, p, p.lds, st); };
     if constexpr (MODE != kWhole) go(group_norm_last_fwd<T, kSplitRun, MODE, true>, group_norm_last_fwd<T, kSplitRun, MODE, false>);
     else if (p.regs <= 4) go(group_norm_last_fwd<T, 4, MODE, true>, group_norm_last_fwd<T, 4, MODE, false>);
     else if (p.regs <= 8) go(group_norm_last_fwd<T, 8, MODE, true>, group_norm_last_fwd<T, 8, MODE, false>);
@@ -301,11 +302,8 @@ int run_norm_fwd(NormPlan &p, hipStream_t st)
     } else {
         launch_norm_fwd<T, kSums>(p, st);
         const int total = p.a.N * p.a.groups;
-        float *mean = p.a.group_sums, *rstd = mean + total;
-        hipLaunchKernelGGL(group_norm_join_stats, dim3((total + 3) / 4), dim3(256), 0, st, p.a.part, p.a.tiles, total,
-                           p.a.inv_m, p.a.eps, mean, rstd, p.a.mean, p.a.rstd);
-        p.a.mean = mean;
-        p.a.rstd = rstd;
+        if (!p.a.join)
+            hipLaunchKernelGGL(group_norm_join_stats, dim3((total + 3) / 4), dim3(256), 0, st, p.a);
         launch_norm_fwd<T, kApply>(p, st);
     }
     return check_launch();
@@ -326,7 +324,7 @@ int run_norm_bwd(NormPlan &p, hipStream_t st)
         }
     }
     if (p.a.dgamma || p.a.dbeta)
-        hipLaunchKernelGGL(group_norm_join_channels, dim3((p.a.C + 15) / 16), dim3(1024), 0, st, p.a);
+        hipLaunchKernelGGL(group_norm_join_channels, dim3((p.a.C + 15) / 16), dim3(256), 0, st, p.a);
     return check_launch();
 }
 

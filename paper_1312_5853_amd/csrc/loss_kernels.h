@@ -97,7 +97,7 @@ __device__ __forceinline__ void row_store(const LossArgs &a, T *dz, const RowLan
     } else {
 #pragma unroll
         for (int k = 0; k < Vec<T>::V; ++k)
-            if (k >= l.k0 && k < l.k1) st_elem(dz, l.off + k, v[k]);
+            if (k >= l.k0 && k < l.k1) Vec<T>::put(dz, l.off + k, v[k]);
     }
 }
 
@@ -401,7 +401,7 @@ __device__ __forceinline__ void write_named(const RowTeam<SOLO> &team, const Ent
                 first &= i4[i] != v || j + i >= k;
             }
         }
-        if (first) st_elem(dz, v, x.mix(k < K ? e.zk[k] : zl, ck, cl) - (share * p + (v == label ? gl : 0.f)));
+        if (first) Vec<T>::put(dz, v, x.mix(k < K ? e.zk[k] : zl, ck, cl) - (share * p + (v == label ? gl : 0.f)));
     }
 }
 

@@ -17,8 +17,10 @@
 // 22 vectors to a plane, 31 us with 32 lanes to a plane, FLATUS us flat.
 // Channels last: a work-group takes `cw` neighbouring channels (whole groups) of a sample; a lane keeps its columns and
 // walks down the positions.
-// A plane's (row's) last vector is moved back so that it ends where the plane ends: it then holds values of the vector
-// before it too (the first k0 ones), which take no part in sums and are written twice, the same.
+// A plane's last vector is moved back so that it ends where the plane ends; the values of the vector before that it holds
+// then are replaced by its last one, which leaves the sums with a known number of copies of one value to take off: two
+// operations to a vector, where a mask takes one or two to each value.  A slab's last vector is moved back too; its first
+// values are the ones of the vector before it, are left out of the sums and written twice, the same.
 
 constexpr int kWhole = 0, kSums = 1, kApply = 2;
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -41,7 +43,8 @@ struct NormArgs {
     int flat, vectors, chunks, units;         // vectors and units to a plane (long planes); units of a group
     int run;                                  // units to a wave
     int tiles, parts, span;                   // of a group; of a plane (0: a tile is whole planes); units or planes of a tile
-    FastDiv div_chunks, div_vectors, div_tiles;
+    float inv_vectors, half_vectors;          // 1 / vectors, and half of that
+    FastDiv div_chunks, div_tiles;
     // channels last
     int cw, slab_groups, slabs, lanes, rows;  // channels, groups of a slab; slabs; lanes to a row; rows at a time
     int tile_rows, pitch, group_lanes, channel_lanes, units_per_xcd, work;
@@ -175,57 +178,59 @@ __device__ __forceinline__ PlaneTile plane_tile(const NormArgs &a)
     return t;
 }
 
-struct PlaneLane { int c, off, k0, k1; };    // channel in the group, element in the group, valid values k0 <= k < k1
+// A lane's vector: channel in the group, first value in the group (before the plane if it is shorter than a vector), and
+// whether there is one and it is moved back.
+struct PlaneLane {
+    int c, off;
+    bool on, tail;
+};
 
 template <int V>
 __device__ __forceinline__ PlaneLane plane_lane(const NormArgs &a, const PlaneTile &t, int u, int lane)
 {
     PlaneLane p;
     int pos;
-    bool on;
     if (a.flat) {
-        const int f = u * 64 + lane, j = fastdiv(f, a.div_vectors);
+        // f / vectors: f is below 2^16 here, and (f + 1/2) / vectors in fp32 is far enough from a whole number.  Full-rate
+        // operations; a division by multiplication of integers takes four times as long, and so do their products.
+        const int f = u * 64 + lane, j = (int)fmaf((float)f, a.inv_vectors, a.half_vectors);
         p.c = t.first + j;
-        pos = (f - j * a.vectors) * V;
-        on = j < t.planes;
+        pos = (f - __mul24(j, a.vectors)) * V;
+        p.on = j < t.planes;
+        p.off = __mul24(p.c, a.S) + min(pos, a.S - V);
     } else {
         p.c = fastdiv(u, a.div_chunks);
         pos = ((u - p.c * a.chunks) * 64 + lane) * V;
-        on = pos < a.S;
+        p.on = pos < a.S;
+        p.off = p.c * a.S + min(pos, a.S - V);
     }
-    if (!on) p.c = 0;
-    if (a.S >= V) {
-        const int q = min(pos, a.S - V);
-        p.off = on ? p.c * a.S + q : 0;
-        p.k0 = on ? pos - q : V;
-        p.k1 = V;
-    } else {
-        p.off = p.c * a.S;
-        p.k0 = 0;
-        p.k1 = on ? a.S : 0;
+    p.tail = pos > a.S - V;
+    if (!p.on) {
+        p.c = 0;
+        p.off = 0;
     }
     return p;
 }
 
 template <typename T>
-__device__ __forceinline__ typename Vec<T>::Raw plane_load(const NormArgs &a, const T *p, const PlaneLane &l)
+__device__ __forceinline__ typename Vec<T>::Raw plane_load(const NormArgs &a, const T *p, const PlaneLane &l, int moved)
 {
-    return a.S >= Vec<T>::V ? Vec<T>::load(p + l.off) : Vec<T>::some(p + l.off, l.k1);
+    if (a.S >= Vec<T>::V) return Vec<T>::load(p + l.off);
+    return Vec<T>::ends(p + l.off, l.on ? moved : Vec<T>::V);
 }
 
 template <typename T>
-__device__ __forceinline__ void plane_store(const NormArgs &a, T *p, const PlaneLane &l, const float (&v)[Vec<T>::V])
+__device__ __forceinline__ void plane_store(T *p, const PlaneLane &l, int moved, const float (&v)[Vec<T>::V])
 {
-    if (a.S >= Vec<T>::V) {
-        if (l.k0 < Vec<T>::V) Vec<T>::store(p + l.off, v);
-    } else {
-        for (int k = 0; k < Vec<T>::V; ++k)
-            if (k < l.k1) st_elem(p, l.off + k, v[k]);
-    }
+    if (l.on && !l.tail) Vec<T>::store(p + l.off, v);
+    if (moved == 0) return;
+#pragma unroll
+    for (int k = 0; k < Vec<T>::V; ++k)
+        if (k >= moved && l.on && l.tail) Vec<T>::put(p, l.off + k, v[k]);
 }
 
 template <typename T, int R, bool SOLO, int MODE>
-__global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_fwd(NormArgs a)
+__global__ __launch_bounds__(SOLO ? 256 : 1024, R <= 4 ? 8 : 6) void group_norm_planes_fwd(NormArgs a)
 {
     constexpr int V = Vec<T>::V;
     __shared__ float red[3][16];
@@ -237,11 +242,12 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_fwd(NormA
     typename Vec<T>::Raw raw[R];
     PlaneLane pl[R];
     const int u0 = t.u0 + wave * a.run, n = min(a.run, t.u1 - u0);
+    const int moved = (V - a.S % V) % V;         // values of a moved-back vector that are the vector's before it
 #pragma unroll
     for (int r = 0; r < R; ++r)
         if (r < n) {
             pl[r] = plane_lane<V>(a, t, u0 + r, lane);
-            raw[r] = plane_load(a, x, pl[r]);
+            raw[r] = plane_load(a, x, pl[r], moved);
         }
     float mean, rstd;
     if (MODE == kApply) {
@@ -260,16 +266,15 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_fwd(NormA
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (r < n) {
+                if (moved && pl[r].tail) Vec<T>::repeat_last(raw[r], moved);
                 float v[V];
                 Vec<T>::open(raw[r], v);
-                if (pl[r].k0 == 0 && pl[r].k1 == V) {
+                if (pl[r].on) {
 #pragma unroll
                     for (int k = 0; k < V; ++k) s += v[k];
-                } else {
-#pragma unroll
-                    for (int k = 0; k < V; ++k) s += k >= pl[r].k0 && k < pl[r].k1 ? v[k] : 0.f;
+                    if (moved) s = fmaf(pl[r].tail ? -(float)moved : 0.f, v[V - 1], s);
+                    if (MODE == kSums) cnt += pl[r].tail ? V - moved : V;
                 }
-                if (MODE == kSums) cnt += max(0, pl[r].k1 - pl[r].k0);
             }
         s = wave_sum(s);
         if (!SOLO) s = join_waves(s, red[0], nw);
@@ -280,17 +285,19 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_fwd(NormA
         }
         mean = s * inv;
         s = 0.f;
+        if (MODE == kWhole) open_again(raw);
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (r < n) {
                 float v[V];
                 Vec<T>::open(raw[r], v);
-                if (pl[r].k0 == 0 && pl[r].k1 == V) {
+                if (pl[r].on) {
 #pragma unroll
-                    for (int k = 0; k < V; ++k) s += (v[k] - mean) * (v[k] - mean);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < V; ++k) s += k >= pl[r].k0 && k < pl[r].k1 ? (v[k] - mean) * (v[k] - mean) : 0.f;
+                    for (int k = 0; k < V; ++k) {
+                        v[k] -= mean;
+                        s = fmaf(v[k], v[k], s);
+                    }
+                    if (moved) s = fmaf((pl[r].tail ? -(float)moved : 0.f) * v[V - 1], v[V - 1], s);
                 }
             }
         s = wave_sum(s);
@@ -310,6 +317,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_fwd(NormA
             if (a.rstd) a.rstd[t.group] = rstd;
         }
     }
+    if (MODE == kWhole) open_again(raw);
     T *y = static_cast<T *>(a.out) + base;
     const int c0 = t.g * a.cpg;
 #pragma unroll
@@ -320,7 +328,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_fwd(NormA
             float v[V];
             Vec<T>::open(raw[r], v);
             act_fwd(v, a.act, [&](int) { return scale; }, [&](int) { return shift; });
-            plane_store(a, y, pl[r], v);
+            plane_store(y, pl[r], moved, v);
         }
 }
 
@@ -328,7 +336,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_fwd(NormA
 // Sums per channel go through slots in LDS: of long planes four to a unit (16 lanes are added by moves within a row of
 // lanes; consecutive units of a wave that lie in one plane are added before that), flat one to a lane.
 template <typename T, int R, bool SOLO, int MODE>
-__global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_bwd(NormArgs a)
+__global__ __launch_bounds__(SOLO ? 256 : 1024, R <= 2 ? 8 : R <= 4 ? 5 : 4) void group_norm_planes_bwd(NormArgs a)
 {
     constexpr int V = Vec<T>::V;
     constexpr bool kKeep = MODE == kWhole && (sizeof(T) == 4 || R <= 4);       // dz stays in registers, else it is computed twice
@@ -347,12 +355,13 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_bwd(NormA
     float dz[kKeep ? R : 1][V];
     const int u0 = t.u0 + wave * a.run, n = min(a.run, t.u1 - u0);
     const int c0 = t.g * a.cpg;
+    const int moved = (V - a.S % V) % V;         // values of a moved-back vector that are the vector's before it
 #pragma unroll
     for (int r = 0; r < R; ++r)
         if (r < n) {
             const PlaneLane l = plane_lane<V>(a, t, u0 + r, lane);
-            rx[r] = plane_load(a, x, l);
-            rd[r] = plane_load(a, dy, l);
+            rx[r] = plane_load(a, x, l, moved);
+            rd[r] = plane_load(a, dy, l, moved);
             if constexpr (kFew) {
                 pl[r] = l;
                 scale[r] = a.gamma ? a.gamma[c0 + l.c] : 1.f;
@@ -388,24 +397,25 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_bwd(NormA
                 PlaneLane l;
                 float sc, sh, xv[V], dv[V];
                 find(r, l, sc, sh);
+                if (moved && l.tail) {
+                    Vec<T>::repeat_last(rx[r], moved);
+                    Vec<T>::repeat_last(rd[r], moved);
+                }
                 Vec<T>::open(rx[r], xv);
                 Vec<T>::open(rd[r], dv);
 #pragma unroll
                 for (int k = 0; k < V; ++k) xv[k] -= mean;
                 act_bwd(dv, xv, a.act, [&](int) { return sc; }, [&](int) { return sh; });
-                if (a.S % V == 0) {
-                    if (l.k0 == 0)
-#pragma unroll
-                        for (int k = 0; k < V; ++k) {
-                            A += dv[k];
-                            B = fmaf(dv[k], xv[k], B);
-                        }
-                } else {
+                if (l.on) {
 #pragma unroll
                     for (int k = 0; k < V; ++k) {
-                        const float w = k >= l.k0 && k < l.k1 ? dv[k] : 0.f;
-                        A += w;
-                        B = fmaf(w, xv[k], B);
+                        A += dv[k];
+                        B = fmaf(dv[k], xv[k], B);
+                    }
+                    if (moved) {
+                        const float off = (l.tail ? -(float)moved : 0.f) * dv[V - 1];
+                        A += off;
+                        B = fmaf(off, xv[V - 1], B);
                     }
                 }
                 if constexpr (kKeep) {
@@ -492,7 +502,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024) void group_norm_planes_bwd(NormA
             }
 #pragma unroll
             for (int k = 0; k < V; ++k) dv[k] = fmaf(-xv[k], c2, fmaf(sc, dv[k], -c1));
-            plane_store(a, dx, l, dv);
+            plane_store(dx, l, moved, dv);
         }
 }
 
@@ -550,7 +560,7 @@ __device__ __forceinline__ void slab_store(const NormArgs &a, T *p, const SlabTi
         Vec<T>::store(p, v);
     } else {
         for (int k = 0; k < Vec<T>::V; ++k)
-            if (k < t.k1) st_elem(p, k, v[k]);
+            if (k < t.k1) Vec<T>::put(p, k, v[k]);
     }
 }
 

@@ -109,7 +109,8 @@ void plan_planes(NormPlan &p, bool bwd, int V)
     a.rows_per_sample = a.parts ? a.parts : 1;
     p.lds = bwd ? (size_t)((p.solo ? 4 : 1) * 2 * (slots + (a.parts ? 1 : a.span)) * 4) : 0;
     a.div_chunks = make_fastdiv(a.chunks);
-    a.div_vectors = make_fastdiv(a.vectors);
+    a.inv_vectors = (float)(1.0 / a.vectors);
+    a.half_vectors = (float)(0.5 / a.vectors);
 }
 
 void plan_last(NormPlan &p, bool bwd, int V, int eb)

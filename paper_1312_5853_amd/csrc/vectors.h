@@ -20,6 +20,7 @@ struct Vec<float> {
     {
         *reinterpret_cast<f32x4_any *>(p) = f32x4{v[0], v[1], v[2], v[3]};
     }
+    static __device__ __forceinline__ void put(float *p, int i, float v) { p[i] = v; }
     static __device__ __forceinline__ void open(const Raw &r, float (&v)[4])
     {
 #pragma unroll
@@ -38,6 +39,19 @@ struct Vec<float> {
             if (k < n) r[k] = p[k];
         return r;
     }
+    static __device__ __forceinline__ Raw ends(const float *p, int n)        // the values from the n-th on, zeros before them
+    {
+        Raw r = {0.f, 0.f, 0.f, 0.f};
+        for (int k = 0; k < 4; ++k)
+            if (k >= n) r[k] = p[k];
+        return r;
+    }
+    static __device__ __forceinline__ void repeat_last(Raw &r, int n)        // the last value in place of the first n
+    {
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            if (k < n) r[k] = r[3];
+    }
 };
 
 template <>
@@ -55,6 +69,10 @@ struct Vec<unsigned short> {
         for (int k = 0; k < 4; ++k)          // both at once, to nearest even (v_cvt_pk_bf16_f32)
             q[k] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2){v[2 * k], v[2 * k + 1]}, bf16x2));
         *reinterpret_cast<u32x4_any *>(p) = q;
+    }
+    static __device__ __forceinline__ void put(unsigned short *p, int i, float v)
+    {
+        p[i] = __builtin_bit_cast(unsigned short, (__bf16)v);
     }
     static __device__ __forceinline__ void open(const Raw &r, float (&v)[8])
     {
@@ -78,6 +96,22 @@ struct Vec<unsigned short> {
         for (int k = 0; k < 8; ++k)
             if (k < n) r[k >> 1] |= (unsigned)p[k] << (16 * (k & 1));
         return r;
+    }
+    static __device__ __forceinline__ Raw ends(const unsigned short *p, int n)
+    {
+        Raw r = {0u, 0u, 0u, 0u};
+        for (int k = 0; k < 8; ++k)
+            if (k >= n) r[k >> 1] |= (unsigned)p[k] << (16 * (k & 1));
+        return r;
+    }
+    static __device__ __forceinline__ void repeat_last(Raw &r, int n)
+    {
+        const unsigned last = r[3] >> 16, both = last | (r[3] & 0xFFFF0000u);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (2 * k + 1 < n) r[k] = both;
+            else if (2 * k < n) r[k] = (r[k] & 0xFFFF0000u) | last;
+        }
     }
 };
 

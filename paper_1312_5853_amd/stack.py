@@ -187,8 +187,16 @@ class FullNetwork(ConvStack):
                        + [(self.fc_b[n], self.fc_db[n]) for n, _, _ in FC_LAYERS])
         self.vel = [torch.zeros_like(p) for p, _ in self.params]
 
+    def conv_forward(self):
+        """The convolutional part of forward(): the last pooling output."""
+        return ConvStack.forward(self)
+
+    def conv_backward(self):
+        """The convolutional part of backward(), from the gradient g5 of the last pooling output."""
+        return ConvStack.backward(self)
+
     def forward(self):
-        a = super().forward().view(self.N, -1)
+        a = self.conv_forward().view(self.N, -1)
         ws = self.ws
         for name, _, _ in FC_LAYERS:
             a = hp.fc_fwd(a, self.fc_w[name], self.fc_b[name], relu=name != "fc8", y=self.fc_y[name], ws=ws)
@@ -206,7 +214,7 @@ class FullNetwork(ConvStack):
             hp.bias_bwd(d.view(N, -1, 1, 1), db=self.fc_db[name], ws=ws)
             dx = self.fc_dy[FC_LAYERS[idx - 1][0]] if idx > 0 else self.g5.view(N, -1)
             d = hp.fc_bwd_data(d, self.fc_w[name], dx=dx, ws=ws)
-        return super().backward()
+        return self.conv_backward()
 
     def update(self):
         """Mean gradient over this shard's N samples (a data-parallel job would first sum the shards' gradients)."""

@@ -39,6 +39,7 @@ struct NormArgs {
     float eps, inv_m;                // inv_m: 1 / M
     FastDiv div_groups, div_cpg;
     int part_rows, rows_per_sample;  // rows of C sums in `part`, and of those a sample's
+    int join_lanes;                  // threads to channels where a group's sums are joined
     // planes
     int flat, vectors, chunks, units;         // vectors and units to a plane (long planes); units of a group
     int run;                                  // units to a wave
@@ -197,7 +198,7 @@ __device__ __forceinline__ PlaneLane plane_lane(const NormArgs &a, const PlaneTi
         p.c = t.first + j;
         pos = (f - __mul24(j, a.vectors)) * V;
         p.on = j < t.planes;
-        p.off = __mul24(p.c, a.S) + min(pos, a.S - V);
+        p.off = t.first * a.S + __mul24(j, a.S) + min(pos, a.S - V);
     } else {
         p.c = fastdiv(u, a.div_chunks);
         pos = ((u - p.c * a.chunks) * 64 + lane) * V;
@@ -983,41 +984,58 @@ __global__ __launch_bounds__(256) void group_norm_join_stats(NormArgs a)
     }
 }
 
-// A wave per sample and group: its channels' sums over the sample's rows, and {m1, m2} from them.
-__global__ __launch_bounds__(256) void group_norm_join_groups(NormArgs a)
+// A work-group per sample and group: its channels' sums over the sample's rows, and {m1, m2} from them.  join_lanes threads
+// to neighbouring channels (so that a wave reads runs of memory), the others to the rows, four loads of each kind in flight
+// at once.
+__global__ __launch_bounds__(1024) void group_norm_join_groups(NormArgs a)
 {
-    const int lane = threadIdx.x & 63, total = a.N * a.groups, i = blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int grp = min(i, total - 1), n = fastdiv(grp, a.div_groups), c0 = (grp - n * a.groups) * a.cpg;
-    const float *pa = a.part + (int64_t)n * a.rows_per_sample * a.C + c0, *pb = pa + (int64_t)a.part_rows * a.C;
+    __shared__ float red[2][1024], shares[2][16];
+    const int n = fastdiv(blockIdx.x, a.div_groups), c0 = (blockIdx.x - n * a.groups) * a.cpg, rows = a.rows_per_sample;
+    const float *pa = a.part + (int64_t)n * rows * a.C + c0, *pb = pa + (int64_t)a.part_rows * a.C;
+    const int i = threadIdx.x, x = i & (a.join_lanes - 1), sub = i / a.join_lanes, subs = blockDim.x / a.join_lanes;
     float m1 = 0.f, m2 = 0.f;
-    for (int c1 = 0; c1 < a.cpg; c1 += 4) {              // four channels at a time, their loads in flight together
-        float A[4] = {0.f, 0.f, 0.f, 0.f}, B[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int t = lane; t < a.rows_per_sample; t += 64)
+    for (int c1 = 0; c1 < a.cpg; c1 += a.join_lanes) {
+        const int own = min(c1 + x, a.cpg - 1), c = c0 + own;
+        float A = 0.f, B = 0.f;
+        for (int t0 = sub; t0 < rows; t0 += 4 * subs) {
+            float va[4], vb[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int c = min(c1 + u, a.cpg - 1);
-                A[u] += pa[(int64_t)t * a.C + c];
-                B[u] += pb[(int64_t)t * a.C + c];
+                const int64_t at = (int64_t)min(t0 + u * subs, rows - 1) * a.C + own;
+                va[u] = pa[at];
+                vb[u] = pb[at];
             }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int c = c0 + c1 + u;
-            A[u] = wave_sum(A[u]);
-            B[u] = wave_sum(B[u]);
-            if (c1 + u < a.cpg) {
-                const float gamma = a.gamma ? a.gamma[c] : 1.f;
-                m1 += gamma * A[u];
-                m2 += gamma * B[u];
-                if (lane == 0 && i < total) {
-                    a.sample_sums[(int64_t)n * a.C + c] = A[u];
-                    a.sample_sums[(int64_t)(a.N + n) * a.C + c] = B[u];
+            for (int u = 0; u < 4; ++u) {
+                A += t0 + u * subs < rows ? va[u] : 0.f;
+                B += t0 + u * subs < rows ? vb[u] : 0.f;
+            }
+        }
+        if (subs > 1) {
+            __syncthreads();                             // the channels before are read
+            red[0][i] = A;
+            red[1][i] = B;
+            for (int s = subs >> 1; s > 0; s >>= 1) {
+                __syncthreads();
+                if (sub < s) {
+                    red[0][i] = A += red[0][i + s * a.join_lanes];
+                    red[1][i] = B += red[1][i + s * a.join_lanes];
                 }
             }
         }
+        if (sub == 0 && c1 + x < a.cpg) {
+            const float gamma = a.gamma ? a.gamma[c] : 1.f;
+            m1 += gamma * A;
+            m2 += gamma * B;
+            a.sample_sums[(int64_t)n * a.C + c] = A;
+            a.sample_sums[(int64_t)(a.N + n) * a.C + c] = B;
+        }
     }
-    if (lane == 0 && i < total) {
-        a.group_sums[2 * i] = m1 * a.inv_m;
-        a.group_sums[2 * i + 1] = m2 * a.inv_m;
+    m1 = join_waves(wave_sum(m1), shares[0], (int)(blockDim.x >> 6));
+    m2 = join_waves(wave_sum(m2), shares[1], (int)(blockDim.x >> 6));
+    if (i == 0) {
+        a.group_sums[2 * (int64_t)blockIdx.x] = m1 * a.inv_m;
+        a.group_sums[2 * (int64_t)blockIdx.x + 1] = m2 * a.inv_m;
     }
 }
 

@@ -31,6 +31,8 @@ int norm_checks(int N, int C, int S, int groups, int layout, int dtype)
     if (!glue_elem_bytes(dtype)) return kErrBadDtype;
     const int64_t limit = (int64_t)1 << 31;
     if ((int64_t)C * S >= limit || (int64_t)N * C >= limit) return kErrTooLarge;
+    // more than the card holds; keeps the numbers of tiles and rows of sums in their 32 bits
+    if ((int64_t)N * C * S >= (int64_t)1 << 40) return kErrTooLarge;
     return kStatusOk;
 }
 
@@ -46,6 +48,13 @@ int pow2_down(int v)
     while (2 * p <= v) p <<= 1;
     return p;
 }
+
+// a launch has fewer than 2^32 threads
+bool launchable(int64_t blocks, int threads) { return blocks * threads < (int64_t)1 << 32; }
+
+// Threads that join a group's sums: 1 to 32 rows of 64 to 512 channels take 4 to 5 us, the launch; 8 x 512 channels of 64 rows
+// 15 us, and 38 us with 256 threads, 480 us with a wave.
+constexpr int kJoinThreads = 1024;
 
 constexpr int kMaxWaves = 16, kSplitWaves = 8, kSplitRun = 4;
 
@@ -203,9 +212,13 @@ int plan_norm(NormPlan &p, int op, int N, int C, int S, int groups, int layout, 
     }
     a.div_tiles = make_fastdiv(a.tiles);
     a.join = (int64_t)a.tiles * (p.planes ? 1 : a.slab_groups) <= 2048;
-    if ((int64_t)N * a.rows_per_sample >= ((int64_t)1 << 31) || p.blocks >= ((int64_t)1 << 31)) return kErrTooLarge;
+    if ((int64_t)N * a.rows_per_sample >= ((int64_t)1 << 31) || !launchable(p.blocks, p.threads)) return kErrTooLarge;
     a.part_rows = N * a.rows_per_sample;
     const int64_t ng = (int64_t)N * groups;
+    if (p.split) {
+        a.join_lanes = std::min(pow2_up(std::min(a.cpg, kJoinThreads)), kJoinThreads / pow2_up(std::min(16, a.rows_per_sample)));
+        if (!launchable(ng, kJoinThreads)) return kErrTooLarge;
+    }
     if (bwd) p.part_bytes = (size_t)2 * a.part_rows * C * 4;
     else if (p.split) p.part_bytes = (size_t)ng * a.tiles * 3 * 4;
     if (p.split) p.sums_bytes = (size_t)(ng * 2 + (bwd ? 2 * (int64_t)N * C : 0)) * 4;
@@ -320,7 +333,7 @@ int run_norm_bwd(NormPlan &p, hipStream_t st)
             launch_norm_bwd<T, kWhole>(p, st);
         } else {
             launch_norm_bwd<T, kSums>(p, st);
-            hipLaunchKernelGGL(group_norm_join_groups, dim3((p.a.N * p.a.groups + 3) / 4), dim3(256), 0, st, p.a);
+            hipLaunchKernelGGL(group_norm_join_groups, dim3(p.a.N * p.a.groups), dim3(kJoinThreads), 0, st, p.a);
             launch_norm_bwd<T, kApply>(p, st);
         }
     }
@@ -366,7 +379,7 @@ int plan_loss(LossPlan &p, int N, int V, int K, int dtype, bool from_stats)
         p.threads = 64 * ceil_div(p.part_chunks, p.run);
         p.parts = ceil_div(p.chunks, p.part_chunks);
         p.blocks = (int64_t)N * p.parts;
-        return p.blocks < ((int64_t)1 << 31) ? kStatusOk : kErrTooLarge;
+        return launchable(p.blocks, p.threads) ? kStatusOk : kErrTooLarge;
     }
     p.solo = p.chunks <= 4 && N >= 1024;
     if (p.solo) {
@@ -390,7 +403,7 @@ int plan_loss(LossPlan &p, int N, int V, int K, int dtype, bool from_stats)
         p.total = p.part_bytes + (size_t)round_up64((int64_t)N * (K + 1) * 4, 256);
     }
     p.regs = std::min(pow2_up(p.run), 8);
-    return p.blocks < ((int64_t)1 << 31) ? kStatusOk : kErrTooLarge;
+    return launchable(p.blocks, p.threads) ? kStatusOk : kErrTooLarge;
 }
 
 // a: pointers, strides and scalars of the call are set; the rest is checked and filled in

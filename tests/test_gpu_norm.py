@@ -250,7 +250,7 @@ def test_same_bits_every_time(shape, layout):
 
 
 def test_a_sample_is_normalised_alone():
-    """Results of a sample are the same bits in whatever batch it stands: a shard needs no exchange."""
+    """Results of a sample are its own in whatever batch it stands (up to the order of sums): a shard needs no exchange."""
     _, (xd, _), gamma, beta = _tensors(9, 48, 13, 13, "planes", "f32", 11)
     ga, be = _cuda(gamma), _cuda(beta)
     whole = hp.group_norm_act_fwd(xd, 16, ga, be)[0]
@@ -297,3 +297,23 @@ def test_offsets_past_32_bits():
     dx = hp.group_norm_act_bwd(x, dy, mean, rstd, ga, be, dx=y)[0]
     dx2 = hp.group_norm_act_bwd(x[-2:].clone(), dy[-2:].clone(), mean2, rstd2, ga, be)[0]
     assert torch.allclose(dx[-2:], dx2, rtol=1e-4, atol=1e-4)
+
+
+def test_groups_of_millions_of_channels():
+    """More channels to a group than 24-bit products of their number hold.  Sums run over chains of up to 2^15 here, so the
+    gradient's means may be off by 2^15 u of the mean magnitude, 1.6e-3 and 6 times that with |xh| up to 6."""
+    C, S = (1 << 23) + 3000, 2
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x, dy = (torch.randn((1, C, 1, S), device="cuda", generator=g) for _ in range(2))
+    y, mean, rstd = hp.group_norm_act_fwd(x, 1, act="none")
+    xd, dyd = x.double(), dy.double()
+    m = xd.mean()
+    r = (xd.sub(m).square().mean() + 1e-5).rsqrt()
+    xh = (xd - m) * r
+    assert abs(float(mean - m)) < 1e-4 and abs(float(rstd / r - 1)) < 1e-4
+    assert float((y - xh).abs().max()) < 1e-3
+    dx, dgamma, dbeta = hp.group_norm_act_bwd(x, dy, mean, rstd, act="none")
+    want = r * (dyd - dyd.mean() - xh * (dyd * xh).mean())
+    assert float((dx - want).abs().max()) < 0.02
+    assert float((dbeta - dyd.sum((0, 2, 3))).abs().max()) < 1e-4
+    assert float((dgamma - (dyd * xh).sum((0, 2, 3))).abs().max()) < 1e-2

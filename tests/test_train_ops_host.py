@@ -149,6 +149,17 @@ def test_norm_backward_argument_checks(lib):
     assert lib.group_norm_act_workspace_bytes(9, 2, 8, 9, 4, 0, 0) == 0
 
 
+def test_sizes_past_what_a_launch_or_its_counters_hold(lib):
+    from paper_1312_5853_amd import binding as b
+    big = dict(N=1 << 14, C=1 << 16, S=1 << 14, groups=1 << 5)                     # 2^44 values
+    for layout in (0, 1):
+        assert lib.group_norm_act_fwd(*_norm_args(layout=layout, **big)) == b.ERR_TOO_LARGE
+        assert lib.group_norm_act_bwd(*_norm_bwd_args(layout=layout, **big)) == b.ERR_TOO_LARGE
+    many = dict(N=1 << 25, C=8, S=200, groups=8)                                   # 2^28 groups of a wavefront each
+    assert lib.group_norm_act_fwd(*_norm_args(**many)) == b.ERR_TOO_LARGE
+    assert lib.distill_loss_fwd(*_loss_args(N=1 << 27)) == b.ERR_TOO_LARGE         # 2^27 rows of a wavefront each
+
+
 def _loss_args(**kw):
     a = dict(z=PTR, z_stride=10, labels=PTR, top_idx=PTR, top_val=PTR, loss=PTR, stats=PTR, N=2, V=10, K=3, T=2.0, wk=1.0,
              wl=1.0, ib=4, td=0, dtype=0, ws=PTR, ws_bytes=1 << 30, stream=None)

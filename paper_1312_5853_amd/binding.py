@@ -598,41 +598,57 @@ def _loss_workspace_bytes(N, V, K, dtype):
     return int(lib().distill_loss_workspace_bytes(N, V, K, dtype))
 
 
-# The checks of the calls below are written out for speed: the smallest of these calls take the GPU about as long as
-# Python needs for their arguments.
-def _norm_layout(*tensors):
-    """The memory order that all of a call's [N,C,H,W] tensors have: NCHW, or channels last."""
-    for t in tensors:
-        if not t.is_contiguous():
-            break
-    else:
-        return LAYOUT_PLANES
+# The checks of the calls below are written out for speed: the smallest of these calls take the GPU less time than Python
+# needs for their arguments.
+_F32 = torch.float32
+_GLUE_CODES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
+
+
+def _glue_code(t):
+    code = _GLUE_CODES.get(t.dtype)
+    if code is None:
+        raise TypeError("unsupported tensor dtype %s" % t.dtype)
+    return code
+
+
+def _on_gpu(d):
+    if d < 0:
+        raise ValueError("the tensors of a call must be on one GPU")
+
+
+def _like(t, x, shape, d, what):
+    """A tensor of x's shape, element type and GPU."""
+    if t.shape != shape:
+        raise ValueError("%s must have the shape of its input" % what)
+    if t.dtype is not x.dtype:
+        raise TypeError("the tensors of a glue call must have one dtype")
+    if t.get_device() != d:
+        raise ValueError("the tensors of a call must be on one GPU")
+
+
+def _dense_f32(t, shape, d, what):
+    """A dense fp32 tensor of this shape on GPU d; its address."""
+    if t.dtype is not _F32 or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be a dense fp32 tensor %s" % (what, list(shape)))
+    if t.get_device() != d:
+        raise ValueError("the tensors of a call must be on one GPU")
+    return t.data_ptr()
+
+
+def _new_f32(shape, like):
+    return torch.empty(shape, dtype=_F32, device=like.device)
+
+
+def _current_stream(stream):
+    """_stream_handle for a call whose tensors are on a GPU, so that the GPU's state is there (1 us less)."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream.cuda_stream
+
+
+def _channels_last(*tensors):
     for t in tensors:
         if not t.is_contiguous(memory_format=torch.channels_last):
             raise ValueError("the tensors of a normalisation must be dense, all NCHW or all channels last")
     return LAYOUT_CHANNELS_LAST
-
-
-_F32 = torch.float32
-
-
-def _dense_f32(t, shape, what):
-    """A dense fp32 tensor of this shape (None passes)."""
-    if t is not None and (t.dtype is not _F32 or t.shape != shape or not t.is_contiguous()):
-        raise ValueError("%s must be a dense fp32 tensor %s" % (what, list(shape)))
-
-
-def _opt(t):
-    return 0 if t is None else t.data_ptr()
-
-
-def _on_device(first, *others):
-    d = first.get_device()
-    if d < 0:
-        raise ValueError("the tensors of a call must be on one GPU")
-    for t in others:
-        if t is not None and t.get_device() != d:
-            raise ValueError("the tensors of a call must be on one GPU")
 
 
 def group_norm_act_fwd(x, groups, gamma=None, beta=None, eps=1e-5, act="relu", y=None, mean=None, rstd=None, ws=None,
@@ -643,24 +659,30 @@ def group_norm_act_fwd(x, groups, gamma=None, beta=None, eps=1e-5, act="relu", y
     if type(groups) is not int:
         groups, = _whole(groups)
     N, C, H, W = shape = x.shape
-    if act not in ACTIVATIONS:
+    code = ACTIVATIONS.get(act)
+    if code is None:
         raise ValueError("unknown activation %r" % (act,))
-    _dense_f32(gamma, (C,), "gamma")
-    _dense_f32(beta, (C,), "beta")
     if y is None:
         y = torch.empty_like(x)
-    elif y.shape != shape:
-        raise ValueError("y must have the shape of x")
+    dtype = _glue_code(x)
+    layout = LAYOUT_PLANES if x.is_contiguous() and y.is_contiguous() else _channels_last(x, y)
+    d = x.get_device()
+    _like(y, x, shape, d, "y")
+    _on_gpu(d)
+    gp = 0 if gamma is None else _dense_f32(gamma, (C,), d, "gamma")
+    bp = 0 if beta is None else _dense_f32(beta, (C,), d, "beta")
+    mp = rp = 0
     if groups > 0:
-        mean = torch.empty((N, groups), dtype=_F32, device=x.device) if mean is None else mean
-        rstd = torch.empty((N, groups), dtype=_F32, device=x.device) if rstd is None else rstd
-        _dense_f32(mean, (N, groups), "mean")
-        _dense_f32(rstd, (N, groups), "rstd")
-    dtype, layout = _glue_dtype(x, y), _norm_layout(x, y)
-    _on_device(x, y, gamma, beta, mean, rstd)
-    buf, nbytes = _ws(ws).get(_norm_workspace_bytes(OP_FWD, N, C, H * W, groups, layout, dtype))
-    rc = lib().group_norm_act_fwd(_ptr(x), _opt(gamma), _opt(beta), _ptr(y), _opt(mean), _opt(rstd), N, C, H * W, groups,
-                                  eps, ACTIVATIONS[act], layout, dtype, _opt(buf), nbytes, _stream_handle(stream))
+        per = (N, groups)
+        mean = _new_f32(per, x) if mean is None else mean
+        rstd = _new_f32(per, x) if rstd is None else rstd
+        mp, rp = _dense_f32(mean, per, d, "mean"), _dense_f32(rstd, per, d, "rstd")
+    need, wsp = _norm_workspace_bytes(OP_FWD, N, C, H * W, groups, layout, dtype), 0
+    if need:
+        buf, need = _ws(ws).get(need)
+        wsp = buf.data_ptr()
+    rc = lib().group_norm_act_fwd(x.data_ptr(), gp, bp, y.data_ptr(), mp, rp, N, C, H * W, groups, eps, code, layout, dtype,
+                                  wsp, need, _current_stream(stream))
     if rc != OK:
         raise ConvError(rc, "group_norm_act_fwd")
     return y, mean, rstd
@@ -670,25 +692,34 @@ def group_norm_act_bwd(x, dy, mean, rstd, gamma=None, beta=None, act="relu", dx=
                        stream=None):
     """(dx, dgamma [C], dbeta [C]) from the forward call's x, mean and rstd and the gradient dy of its y."""
     N, C, H, W = shape = x.shape
-    if act not in ACTIVATIONS:
+    code = ACTIVATIONS.get(act)
+    if code is None:
         raise ValueError("unknown activation %r" % (act,))
     groups = mean.shape[1]
-    _dense_f32(mean, (N, groups), "mean")
-    _dense_f32(rstd, (N, groups), "rstd")
+    if rstd.shape != mean.shape:
+        raise ValueError("mean and rstd must have one shape")
     if dx is None:
         dx = torch.empty_like(x)
-    if dy.shape != shape or dx.shape != shape:
-        raise ValueError("dy and dx must have the shape of x")
-    dgamma = torch.empty((C,), dtype=_F32, device=x.device) if dgamma is None else dgamma
-    dbeta = torch.empty((C,), dtype=_F32, device=x.device) if dbeta is None else dbeta
-    for what, v in (("gamma", gamma), ("beta", beta), ("dgamma", dgamma), ("dbeta", dbeta)):
-        _dense_f32(v, (C,), what)
-    dtype, layout = _glue_dtype(x, dy, dx), _norm_layout(x, dy, dx)
-    _on_device(x, dy, dx, mean, rstd, gamma, beta, dgamma, dbeta)
-    buf, nbytes = _ws(ws).get(_norm_workspace_bytes(OP_BWD_DATA, N, C, H * W, groups, layout, dtype))
-    rc = lib().group_norm_act_bwd(_ptr(x), _ptr(dy), _opt(gamma), _opt(beta), _ptr(mean), _ptr(rstd), _ptr(dx),
-                                  _ptr(dgamma), _ptr(dbeta), N, C, H * W, groups, ACTIVATIONS[act], layout, dtype,
-                                  _opt(buf), nbytes, _stream_handle(stream))
+    dtype = _glue_code(x)
+    layout = (LAYOUT_PLANES if x.is_contiguous() and dy.is_contiguous() and dx.is_contiguous()
+              else _channels_last(x, dy, dx))
+    d = x.get_device()
+    _like(dy, x, shape, d, "dy")
+    _like(dx, x, shape, d, "dx")
+    _on_gpu(d)
+    per, chan = (N, groups), (C,)
+    mp, rp = _dense_f32(mean, per, d, "mean"), _dense_f32(rstd, per, d, "rstd")
+    gp = 0 if gamma is None else _dense_f32(gamma, chan, d, "gamma")
+    bp = 0 if beta is None else _dense_f32(beta, chan, d, "beta")
+    dgamma = _new_f32(chan, x) if dgamma is None else dgamma
+    dbeta = _new_f32(chan, x) if dbeta is None else dbeta
+    dgp, dbp = _dense_f32(dgamma, chan, d, "dgamma"), _dense_f32(dbeta, chan, d, "dbeta")
+    need, wsp = _norm_workspace_bytes(OP_BWD_DATA, N, C, H * W, groups, layout, dtype), 0
+    if need:
+        buf, need = _ws(ws).get(need)
+        wsp = buf.data_ptr()
+    rc = lib().group_norm_act_bwd(x.data_ptr(), dy.data_ptr(), gp, bp, mp, rp, dx.data_ptr(), dgp, dbp, N, C, H * W, groups,
+                                  code, layout, dtype, wsp, need, _current_stream(stream))
     if rc != OK:
         raise ConvError(rc, "group_norm_act_bwd")
     return dx, dgamma, dbeta
@@ -705,26 +736,46 @@ def _rows_of(t, what):
 _INDEX_BYTES = {torch.int32: 4, torch.int64: 8}
 
 
-def _targets(N, labels, top_idx, top_val):
-    """(K, bytes of an index, dtype code of the teacher's logits) of a loss call, its target tensors checked."""
-    if (top_idx is None) != (top_val is None):
-        raise ValueError("top_idx and top_val come together")
-    index = 4
+def _targets(N, labels, top_idx, top_val, d):
+    """(addresses of the three, K, bytes of an index, dtype code of the teacher's logits) of a loss call, its targets
+    checked."""
+    lp, index = 0, 4
     if labels is not None:
         index = _INDEX_BYTES.get(labels.dtype)
-        if labels.shape != (N,) or not labels.is_contiguous():
-            raise ValueError("labels must be a dense tensor with one class per row")
-    if top_idx is None:
         if index is None:
             raise TypeError("labels must be int32 or int64")
-        return 0, index, DTYPE_F32
+        if labels.shape != (N,) or not labels.is_contiguous() or labels.get_device() != d:
+            raise ValueError("labels must be a dense tensor with one class per row on the logits' GPU")
+        lp = labels.data_ptr()
+    if top_idx is None:
+        if top_val is not None:
+            raise ValueError("top_idx and top_val come together")
+        return lp, 0, 0, 0, index, DTYPE_F32
+    if top_val is None:
+        raise ValueError("top_idx and top_val come together")
     of_top = _INDEX_BYTES.get(top_idx.dtype)
     if of_top is None or (labels is not None and of_top != index):
         raise TypeError("labels and top_idx must have one type, int32 or int64")
+    td = _glue_code(top_val)
     shape = top_idx.shape
-    if len(shape) != 2 or shape[0] != N or top_val.shape != shape or not top_idx.is_contiguous() or not top_val.is_contiguous():
-        raise ValueError("top_idx and top_val must be dense tensors [N, K]")
-    return shape[1], of_top, _dtype_of(top_val)
+    if (len(shape) != 2 or shape[0] != N or top_val.shape != shape or not top_idx.is_contiguous()
+            or not top_val.is_contiguous() or top_idx.get_device() != d or top_val.get_device() != d):
+        raise ValueError("top_idx and top_val must be dense tensors [N, K] on the logits' GPU")
+    return lp, top_idx.data_ptr(), top_val.data_ptr(), shape[1], of_top, td
+
+
+def _gradient_rows(dz, z, N, V, d):
+    """dz (a new one for None) and its row stride."""
+    if dz is None:
+        return torch.empty((N, V), dtype=z.dtype, device=z.device), V
+    dN, dV, stride = _rows_of(dz, "dz")
+    if dN != N or dV != V:
+        raise ValueError("dz must have the shape of z")
+    if dz.dtype is not z.dtype:
+        raise TypeError("dz must have the element type of z")
+    if dz.get_device() != d:
+        raise ValueError("the tensors of a call must be on one GPU")
+    return dz, stride
 
 
 def distill_loss_fwd(z, labels=None, top_idx=None, top_val=None, temperature=1.0, kd_weight=1.0, label_weight=1.0,
@@ -733,17 +784,20 @@ def distill_loss_fwd(z, labels=None, top_idx=None, top_val=None, temperature=1.0
     logits (classes top_idx [N,K], logits top_val [N,K]); indexes int32 or int64, one outside 0..V-1 for none.  Returns
     (loss [N], stats [N,3]); stats is what distill_loss_bwd takes."""
     N, V, zs = _rows_of(z, "z")
-    K, ib, td = _targets(N, labels, top_idx, top_val)
-    loss = torch.empty((N,), dtype=_F32, device=z.device) if loss is None else loss
-    stats = torch.empty((N, 3), dtype=_F32, device=z.device) if stats is None else stats
-    _dense_f32(loss, (N,), "loss")
-    _dense_f32(stats, (N, 3), "stats")
-    dtype = _dtype_of(z)
-    _on_device(z, labels, top_idx, top_val, loss, stats)
-    buf, nbytes = _ws(ws).get(_loss_workspace_bytes(N, V, K, dtype))
-    _check(lib().distill_loss_fwd(_ptr(z), zs, _opt(labels), _opt(top_idx), _opt(top_val), _ptr(loss), _ptr(stats), N, V,
-                                  K, temperature, kd_weight, label_weight, ib, td, dtype, _opt(buf), nbytes,
-                                  _stream_handle(stream)), "distill_loss_fwd")
+    dtype, d = _glue_code(z), z.get_device()
+    lp, ip, vp, K, ib, td = _targets(N, labels, top_idx, top_val, d)
+    _on_gpu(d)
+    loss = _new_f32((N,), z) if loss is None else loss
+    stats = _new_f32((N, 3), z) if stats is None else stats
+    op, sp = _dense_f32(loss, (N,), d, "loss"), _dense_f32(stats, (N, 3), d, "stats")
+    need, wsp = _loss_workspace_bytes(N, V, K, dtype), 0
+    if need:
+        buf, need = _ws(ws).get(need)
+        wsp = buf.data_ptr()
+    rc = lib().distill_loss_fwd(z.data_ptr(), zs, lp, ip, vp, op, sp, N, V, K, temperature, kd_weight, label_weight, ib, td,
+                                dtype, wsp, need, _current_stream(stream))
+    if rc != OK:
+        raise ConvError(rc, "distill_loss_fwd")
     return loss, stats
 
 
@@ -752,18 +806,16 @@ def distill_loss_bwd(z, stats, labels=None, top_idx=None, top_val=None, temperat
     """dz = grad_scale * grad[n] * d loss[n] / d z (grad [N] fp32, or None for ones) from the forward call's arguments and
     statistics.  dz has z's element type and may be z itself."""
     N, V, zs = _rows_of(z, "z")
-    K, ib, td = _targets(N, labels, top_idx, top_val)
-    _dense_f32(grad, (N,), "grad")
-    _dense_f32(stats, (N, 3), "stats")
-    dz = torch.empty((N, V), dtype=z.dtype, device=z.device) if dz is None else dz
-    dN, dV, dzs = _rows_of(dz, "dz")
-    if dN != N or dV != V:
-        raise ValueError("dz must have the shape of z")
-    dtype = _glue_dtype(z, dz)
-    _on_device(z, labels, top_idx, top_val, stats, grad, dz)
-    _check(lib().distill_loss_bwd(_ptr(z), zs, _opt(labels), _opt(top_idx), _opt(top_val), _ptr(stats), _opt(grad),
-                                  grad_scale, _ptr(dz), dzs, N, V, K, temperature, kd_weight,
-                                  label_weight, ib, td, dtype, _stream_handle(stream)), "distill_loss_bwd")
+    dtype, d = _glue_code(z), z.get_device()
+    lp, ip, vp, K, ib, td = _targets(N, labels, top_idx, top_val, d)
+    dz, dzs = _gradient_rows(dz, z, N, V, d)
+    _on_gpu(d)
+    gp = 0 if grad is None else _dense_f32(grad, (N,), d, "grad")
+    sp = _dense_f32(stats, (N, 3), d, "stats")
+    rc = lib().distill_loss_bwd(z.data_ptr(), zs, lp, ip, vp, sp, gp, grad_scale, dz.data_ptr(), dzs, N, V, K, temperature,
+                                kd_weight, label_weight, ib, td, dtype, _current_stream(stream))
+    if rc != OK:
+        raise ConvError(rc, "distill_loss_bwd")
     return dz
 
 
@@ -771,19 +823,19 @@ def distill_loss_fwd_bwd(z, labels=None, top_idx=None, top_val=None, temperature
                          grad=None, grad_scale=1.0, loss=None, dz=None, ws=None, stream=None):
     """(loss [N], dz [N,V]) of distill_loss_fwd and distill_loss_bwd in one call."""
     N, V, zs = _rows_of(z, "z")
-    K, ib, td = _targets(N, labels, top_idx, top_val)
-    loss = torch.empty((N,), dtype=_F32, device=z.device) if loss is None else loss
-    _dense_f32(grad, (N,), "grad")
-    _dense_f32(loss, (N,), "loss")
-    dz = torch.empty((N, V), dtype=z.dtype, device=z.device) if dz is None else dz
-    dN, dV, dzs = _rows_of(dz, "dz")
-    if dN != N or dV != V:
-        raise ValueError("dz must have the shape of z")
-    dtype = _glue_dtype(z, dz)
-    _on_device(z, labels, top_idx, top_val, grad, loss, dz)
-    buf, nbytes = _ws(ws).get(_loss_workspace_bytes(N, V, K, dtype))
-    _check(lib().distill_loss_fwd_bwd(_ptr(z), zs, _opt(labels), _opt(top_idx), _opt(top_val), _opt(grad), grad_scale,
-                                      _ptr(loss), _ptr(dz), dzs, N, V, K, temperature, kd_weight,
-                                      label_weight, ib, td, dtype, _opt(buf), nbytes, _stream_handle(stream)),
-           "distill_loss_fwd_bwd")
+    dtype, d = _glue_code(z), z.get_device()
+    lp, ip, vp, K, ib, td = _targets(N, labels, top_idx, top_val, d)
+    dz, dzs = _gradient_rows(dz, z, N, V, d)
+    _on_gpu(d)
+    loss = _new_f32((N,), z) if loss is None else loss
+    op = _dense_f32(loss, (N,), d, "loss")
+    gp = 0 if grad is None else _dense_f32(grad, (N,), d, "grad")
+    need, wsp = _loss_workspace_bytes(N, V, K, dtype), 0
+    if need:
+        buf, need = _ws(ws).get(need)
+        wsp = buf.data_ptr()
+    rc = lib().distill_loss_fwd_bwd(z.data_ptr(), zs, lp, ip, vp, gp, grad_scale, op, dz.data_ptr(), dzs, N, V, K,
+                                    temperature, kd_weight, label_weight, ib, td, dtype, wsp, need, _current_stream(stream))
+    if rc != OK:
+        raise ConvError(rc, "distill_loss_fwd_bwd")
     return loss, dz

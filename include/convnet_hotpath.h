@@ -373,8 +373,9 @@ int sgd_update_multi(void *const *w, const void *const *dw, void *const *vel, co
  * 4-byte aligned, bfloat16 2-byte aligned): values are read exactly, all
  * arithmetic is fp32, the squares are taken of distances from a mean, and a bfloat16 result is
  * rounded once.  eps > 0.  N = 0 is allowed (tensors over it may be NULL; dgamma and
- * dbeta become 0); C * S and N * C must stay below 2^31.  Outputs must not overlap
- * inputs.  Scratch:
+ * dbeta become 0); C * S and N * C must stay below 2^31, N * C * S below 2^40, and
+ * a launch's threads (64 to a group at least) below 2^32.
+ * Outputs must not overlap inputs.  Scratch:
  * group_norm_act_workspace_bytes(op, ...) bytes, 256-byte aligned (op = CONV_OP_FWD or
  * CONV_OP_BWD_DATA; 0 bytes for invalid arguments and where none is needed).
  */
@@ -415,7 +416,8 @@ size_t group_norm_act_workspace_bytes(int op, int N, int C, int S, int groups, i
  * once); top_dtype: the same of top_val; index_bytes: 4 or 8, size of the signed integers in
  * labels and top_idx.  All arithmetic is fp32; results do not depend on the order of work.
  * Pointers aligned to their elements; rows may start anywhere.  dz [N][V], rows dz_stride apart,
- * may be z itself (same stride), and may not overlap it otherwise.  K <= CONV_DISTILL_MAX_TOP, V <= 2^30.
+ * may be z itself (same stride), and may not overlap it otherwise.  K <= CONV_DISTILL_MAX_TOP, V <= 2^30,
+ * and a launch's threads (64 to a row at least) below 2^32.
  * N = 0 is a no-op (pointers may be NULL).  Scratch: distill_loss_workspace_bytes bytes (fwd and fwd_bwd), 256-byte aligned.
  */
 #define CONV_DISTILL_MAX_TOP 1024

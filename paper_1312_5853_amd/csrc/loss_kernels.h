@@ -9,7 +9,10 @@
 // Bound by memory: z is read and dz written, once; two exponentials to a value and sum, and two more for the gradient, fit
 // beside that.  A row stays in the registers of a wave (SOLO) or a work-group between the reads and the result.  Rows that
 // do not fit, and rows too few to fill the card, are cut into parts: one launch leaves each part's m, sT and s1, another
-// joins them and writes the gradient, reading z again.
+// joins them and writes the gradient, reading z again.  A large copy moves 5.0 TB/s on this card: both on 2048 x 65536 bf16
+// take 111 us, 4.8 TB/s, the gradient alone on 700 x 32003 fp32 39 us, 4.6 TB/s.  Smaller calls are bound by latency: targets
+// and row, then what the targets name, then the joins; 4096 x 1000 bf16, loss alone, 7 us, 128 x 1000 fp32, both, 5.4 us,
+// 33 x 50021 fp32, both, 4.2 us for the sums and 7.9 for the rest.
 //
 // The classes that a target names are written twice: the softmax's share with all the others, then, after a barrier, the
 // whole value by the first entry that names the class, which adds up the entries that name it too.  So no atomics, and an
@@ -271,7 +274,7 @@ __device__ __forceinline__ void row_clear(const LossArgs &a, T *dz, int c0, int 
 // ---------------------------------------------------------------------------
 template <bool SOLO>
 struct RowTeam {
-    int lane, wave, waves, id, size;
+    int lane, wave, waves, id, size;        // id, size: the thread in the team, its threads
     __device__ __forceinline__ RowTeam()
     {
         lane = threadIdx.x & 63;
@@ -556,6 +559,8 @@ __global__ __launch_bounds__(256, 8) void distill_part_sums(LossArgs a)
     }
 }
 
+// With dz in z's place another part's work-group may have written over what a part's moved-back last vector reads of that
+// part; those values are dropped, and no other value is read that another work-group writes.
 // Joins the parts (or takes the statistics given).  GRAD: a work-group writes its part's gradient, and the first part's
 // also the row's loss where asked for; otherwise one work-group per row writes the loss.
 template <typename T, int R, bool GRAD>

@@ -77,7 +77,10 @@ void plan_planes(NormPlan &p, bool bwd, int V)
     NormArgs &a = p.a;
     a.vectors = (a.S + V - 1) / V;
     a.chunks = (a.vectors + 63) / 64;
-    a.flat = a.vectors < 0.85 * 64 * a.chunks;             // a sixth of the lanes idle otherwise
+    // flat where a plane of its own would leave a sixth of the lanes idle: backward on 256 x 384 planes of 169 bfloat16 (22
+    // vectors) 28 us, and 50 with a unit to a plane; on 128 x 256 planes of 729 (92) 36.2 and 37.1.  Longer planes gain
+    // nothing by it: 128 x 256 planes of 729 fp32 (183 of 192) backward 57.1 us, and 58.8 flat
+    a.flat = a.vectors < 0.85 * 64 * a.chunks;
     const int64_t units = a.flat ? ((int64_t)a.cpg * a.vectors + 63) / 64 : (int64_t)a.cpg * a.chunks;
     const int most = 8;
     const int64_t groups = (int64_t)a.N * a.groups;
@@ -86,9 +89,13 @@ void plan_planes(NormPlan &p, bool bwd, int V)
     int64_t slots = a.flat ? (int64_t)a.cpg * a.vectors : 4 * units;
     if (units <= (int64_t)kMaxWaves * most && a.cpg <= 4096) {
         a.units = (int)units;
-        p.solo = units <= 4 && groups >= 1024;
+        // a wave to a group, four to a work-group and no barrier, for many small groups: 1024 x 64 planes of 16 fp32 in 64
+        // groups 16.8 us forward and 30.3 backward, 19.1 and 31.1 with a work-group to each; at 4 units it loses (bfloat16
+        // backward on 512 x 256 planes of 196 in 32 groups: 44 us, and 38)
+        p.solo = units <= 2 && groups >= 1024;
         // units to a wave, of one tensor or of two: 2, 4, 8 units of it measured (forward 60, 59, 69 us on 128 x 96 planes of
-        // 3025 fp32, backward 54, 55, 64 us on 128 x 256 planes of 729); few groups take a wave to a unit
+        // 3025 fp32, backward 54, 55, 64 us on 128 x 256 planes of 729); few groups take a wave to a unit (one sample of 256
+        // planes of 169 fp32, which 32 work-groups of a wave or eleven take: latency alone)
         const int want = groups < 1024 ? 1 : bwd ? 2 : 4;
         const int waves = p.solo ? 1 : std::min(kMaxWaves, ceil_div(a.units, want));
         a.run = ceil_div(a.units, waves);
@@ -136,6 +143,10 @@ void plan_last(NormPlan &p, bool bwd, int V, int eb)
         const int rows = 1024 / (int)lanes64;
         if (ceil_div(a.S, rows) > most) continue;
         const double seg = (double)j * a.cpg * eb;
+        // Columns of fewer bytes cost more lines than tiles and their joins cost launches: backward 64 x 96 x 55 x 55 fp32 76 us
+        // in one pass of 48-byte columns, and 107 in tiles; forward in columns of 16 or 24 bytes 4 x 256 x 112 x 112 bf16 34 us
+        // and 32 x 64 x 112 x 112 bf16 56, in tiles 22.5 and 42.  At 48 bytes forward goes either way (64 x 192 x 48 x 48 bf16 48
+        // us in one pass and 36 in tiles, 32 x 96 x 55 x 55 bf16 20 and 26).
         if (seg < (bwd ? 48 : 64) && j != a.groups) continue;
         // lines that a slab shares with its neighbours are read by both; few work-groups leave the card idle
         const double wgs = (double)a.N * (a.groups / j);
@@ -146,6 +157,8 @@ void plan_last(NormPlan &p, bool bwd, int V, int eb)
     if (best) {
         a.slab_groups = best;
         a.lanes = lanes_of(best);
+        // rows to a thread.  Forward 4, 8, 16: 26.1, 21.1, 24.0 us on 128 x 256 x 27 x 27 bf16, 26.0, 19.9, 19.6 us on
+        // 256 x 384 x 13 x 13; backward 4 to 10 are within 3 %, and 6 leaves more work-groups to a CU than 10
         const int want = bwd ? 6 : 8;
         threads = std::min<int64_t>(1024, round_up64((int64_t)a.lanes * ceil_div(a.S, want), 64));
         a.rows = threads / a.lanes;
@@ -161,7 +174,8 @@ void plan_last(NormPlan &p, bool bwd, int V, int eb)
         threads = std::max(512, round_up(a.lanes, 64));
         a.rows = threads / a.lanes;
         const int64_t N_slabs = (int64_t)a.N * (a.groups / j);
-        // as many rows to a thread as leave 512 work-groups, 32 at most
+        // as many rows to a thread as leave 512 work-groups, 32 at most: forward 4 x 256 x 112 x 112 bf16 22.5 us, 27.9 with
+        // 128 work-groups and 22.2 with 2048; 32 x 64 x 112 x 112 bf16 42, 40 and 49 us
         const int most_rows = (int)std::max<int64_t>(4, std::min<int64_t>(32, (int64_t)N_slabs * ceil_div(a.S, a.rows) / 512));
         a.tile_rows = std::min(a.S, a.rows * most_rows);
         a.tiles = ceil_div(a.S, a.tile_rows);
@@ -211,6 +225,8 @@ int plan_norm(NormPlan &p, int op, int N, int C, int S, int groups, int layout, 
         plan_last(p, bwd, V, eb);
     }
     a.div_tiles = make_fastdiv(a.tiles);
+    // forward: every work-group joins its group's tiles itself where these are few, which saves a launch of 4 us; past that
+    // the joins' reads (12 bytes to a tile and work-group) would come to a part of the tensor's own
     a.join = (int64_t)a.tiles * (p.planes ? 1 : a.slab_groups) <= 2048;
     if ((int64_t)N * a.rows_per_sample >= ((int64_t)1 << 31) || !launchable(p.blocks, p.threads)) return kErrTooLarge;
     a.part_rows = N * a.rows_per_sample;
@@ -268,8 +284,7 @@ void launch_norm_fwd(const NormPlan &p, hipStream_t st)
     if (p.planes) {
         if constexpr (MODE != kWhole) launch_norm(group_norm_planes_fwd<T, kSplitRun, false, MODE>, p, 0, st);
         else if (p.solo && p.regs == 1) launch_norm(group_norm_planes_fwd<T, 1, true, MODE>, p, 0, st);
-        else if (p.solo && p.regs == 2) launch_norm(group_norm_planes_fwd<T, 2, true, MODE>, p, 0, st);
-        else if (p.solo) launch_norm(group_norm_planes_fwd<T, 4, true, MODE>, p, 0, st);
+        else if (p.solo) launch_norm(group_norm_planes_fwd<T, 2, true, MODE>, p, 0, st);
         else if (p.regs == 1) launch_norm(group_norm_planes_fwd<T, 1, false, MODE>, p, 0, st);
         else if (p.regs == 2) launch_norm(group_norm_planes_fwd<T, 2, false, MODE>, p, 0, st);
         else if (p.regs == 4) launch_norm(group_norm_planes_fwd<T, 4, false, MODE>, p, 0, st);
@@ -290,8 +305,7 @@ void launch_norm_bwd(const NormPlan &p, hipStream_t st)
     if (p.planes) {
         if constexpr (MODE != kWhole) launch_norm(group_norm_planes_bwd<T, kSplitRun, false, MODE>, p, lds, st);
         else if (p.solo && p.regs == 1) launch_norm(group_norm_planes_bwd<T, 1, true, MODE>, p, lds, st);
-        else if (p.solo && p.regs == 2) launch_norm(group_norm_planes_bwd<T, 2, true, MODE>, p, lds, st);
-        else if (p.solo) launch_norm(group_norm_planes_bwd<T, 4, true, MODE>, p, lds, st);
+        else if (p.solo) launch_norm(group_norm_planes_bwd<T, 2, true, MODE>, p, lds, st);
         else if (p.regs == 1) launch_norm(group_norm_planes_bwd<T, 1, false, MODE>, p, lds, st);
         else if (p.regs == 2) launch_norm(group_norm_planes_bwd<T, 2, false, MODE>, p, lds, st);
         else if (p.regs == 4) launch_norm(group_norm_planes_bwd<T, 4, false, MODE>, p, lds, st);
@@ -381,13 +395,16 @@ int plan_loss(LossPlan &p, int N, int V, int K, int dtype, bool from_stats)
         p.blocks = (int64_t)N * p.parts;
         return launchable(p.blocks, p.threads) ? kStatusOk : kErrTooLarge;
     }
+    // a wave to a row: 4096 x 1000 bf16, loss 7.2 us, both 11.1; with a work-group to a row 9.2 and 13.1
     p.solo = p.chunks <= 4 && N >= 1024;
     if (p.solo) {
         p.run = p.chunks;
         p.threads = 256;
         p.blocks = ((int64_t)N + 3) / 4;
     } else if (p.chunks <= 16 * 4 || (p.chunks <= 16 * 8 && N >= 128)) {
-        // few rows: 64 x 10007 fp32, both, takes 6.0 us this way, 8.6 in parts
+        // A work-group to a row.  Few rows, both: 64 x 10007 fp32 7.5 us this way, 10.0 in parts, 1 x 16000 6.3 and 8.2; up to
+        // twice as long ones where they occupy half of the card: 128 x 32003 fp32 13.1 us, 15.3 in parts, 33 x 32003 10.4 and 9.9.
+        // Vectors of a lane: many rows 2048 x 5000 fp32 20.7 us with four, 28.5 with one; few 128 x 1000 6.3 and 5.5.
         const int want = N >= 512 ? 4 : 1;
         p.run = ceil_div(p.chunks, std::min(16, ceil_div(p.chunks, want)));
         p.threads = 64 * ceil_div(p.chunks, p.run);

@@ -517,7 +517,8 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, R <= 2 ? 8 : R <= 4 ? 5 : 4) voi
 // Forward 128 x 256 x 27 x 27 bf16 in 32 groups 22 us, 4.3 TB/s.  4 x 256 x 112 x 112 bf16, in tiles: 8.9 us for the sums and 13.3
 // for the rest, 2.3 TB/s counting x once, 3.5 as it is read.  Backward 64 x 96 x 55 x 55 fp32 70 us, 3.2 TB/s: columns of 48
 // bytes in the registers of 1008 threads, so that one work-group lives on a CU and its reads, sums and writes do not overlap
-// with another's; in tiles, which do overlap but read x and dy twice, 107 us.
+// with another's; in tiles, which do overlap but read x and dy twice, 84 us (and
+// 5 for their join).
 struct SlabTile {
     int n, slab, tile, s0, count;    // sample, slab, tile of positions [s0, s0 + count)
     int j, p;                        // this thread's column vector and first row

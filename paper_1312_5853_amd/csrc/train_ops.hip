@@ -52,16 +52,12 @@ int pow2_down(int v)
 // a launch has fewer than 2^32 threads
 bool launchable(int64_t blocks, int threads) { return blocks * threads < (int64_t)1 << 32; }
 
-// Threads that join a group's sums: 1 to 32 rows of 64 to 512 channels take 4 to 5 us, the launch; 8 x 512 channels of 64 rows
-// 15 us, and 38 us with 256 threads, 480 us with a wave.
-constexpr int kJoinThreads = 1024;
-
 constexpr int kMaxWaves = 16, kSplitWaves = 8, kSplitRun = 4;
 
 // How a call runs: which kernels, on what tiles, with how much scratch.
 struct NormPlan {
     bool planes, wide, split, solo, one;
-    int threads, regs;               // vectors a lane keeps (of each input): the kernel's template argument
+    int threads, join_threads, regs;  // regs: vectors a lane keeps (of each input): the kernel's template argument
     int64_t blocks;
     size_t lds, part_bytes, sums_bytes, total;
     NormArgs a;
@@ -144,7 +140,7 @@ void plan_last(NormPlan &p, bool bwd, int V, int eb)
         if (ceil_div(a.S, rows) > most) continue;
         const double seg = (double)j * a.cpg * eb;
         // Columns of fewer bytes cost more lines than tiles and their joins cost launches: backward 64 x 96 x 55 x 55 fp32 76 us
-        // in one pass of 48-byte columns, and 107 in tiles; forward in columns of 16 or 24 bytes 4 x 256 x 112 x 112 bf16 34 us
+        // in one pass of 48-byte columns, and 94 in tiles; forward in columns of 16 or 24 bytes 4 x 256 x 112 x 112 bf16 34 us
         // and 32 x 64 x 112 x 112 bf16 56, in tiles 22.5 and 42.  At 48 bytes forward goes either way (64 x 192 x 48 x 48 bf16 48
         // us in one pass and 36 in tiles, 32 x 96 x 55 x 55 bf16 20 and 26).
         if (seg < (bwd ? 48 : 64) && j != a.groups) continue;
@@ -232,8 +228,12 @@ int plan_norm(NormPlan &p, int op, int N, int C, int S, int groups, int layout, 
     a.part_rows = N * a.rows_per_sample;
     const int64_t ng = (int64_t)N * groups;
     if (p.split) {
-        a.join_lanes = std::min(pow2_up(std::min(a.cpg, kJoinThreads)), kJoinThreads / pow2_up(std::min(16, a.rows_per_sample)));
-        if (!launchable(ng, kJoinThreads)) return kErrTooLarge;
+        // threads that join a group's sums, a channel of a row to each: 128 x 96 x 55 x 55 bf16 in 32 groups, channels last,
+        // 4.8 us, 8.0 with 256 threads at least and 32 with 1024; 8 x 512 x 56 x 56 bf16 in one group 15.5 us, 38 with 256
+        const int64_t loads = (int64_t)a.cpg * a.rows_per_sample;
+        p.join_threads = std::min(1024, std::max(64, pow2_up((int)std::min<int64_t>(loads, 1024))));
+        a.join_lanes = std::min(pow2_up(std::min(a.cpg, p.join_threads)), p.join_threads / pow2_up(std::min(16, a.rows_per_sample)));
+        if (!launchable(ng, p.join_threads)) return kErrTooLarge;
     }
     if (bwd) p.part_bytes = (size_t)2 * a.part_rows * C * 4;
     else if (p.split) p.part_bytes = (size_t)ng * a.tiles * 3 * 4;
@@ -347,7 +347,7 @@ int run_norm_bwd(NormPlan &p, hipStream_t st)
             launch_norm_bwd<T, kWhole>(p, st);
         } else {
             launch_norm_bwd<T, kSums>(p, st);
-            hipLaunchKernelGGL(group_norm_join_groups, dim3(p.a.N * p.a.groups), dim3(kJoinThreads), 0, st, p.a);
+            hipLaunchKernelGGL(group_norm_join_groups, dim3(p.a.N * p.a.groups), dim3(p.join_threads), 0, st, p.a);
             launch_norm_bwd<T, kApply>(p, st);
         }
     }

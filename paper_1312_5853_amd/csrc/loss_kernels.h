@@ -341,21 +341,38 @@ __device__ __forceinline__ void read_entries(const LossArgs &a, const Entries &e
 {
     const int k4 = (a.K + 3) & ~3;
     float tm = -INFINITY;
-    int v = first.v;
-    float t = first.t;
-    for (int k = lane; k < k4; k += 64) {
-        if (k >= 64) {
-            v = -1;
-            if (k < a.K) {
-                v = class_at(a.top_idx, (int64_t)n * a.K + k, a.wide_index, a.V);
-                t = teacher_logit(a, (int64_t)n * a.K + k);
+    if (a.K <= 64 && lane < k4) {
+        tm = first.v < 0 ? -INFINITY : first.t;
+        e.zk[lane] = first.v >= lo && first.v < hi ? ld_elem(z, first.v) : 0.f;
+        e.idx[lane] = first.v;
+        e.prob[lane] = tm;
+    }
+    for (int k0 = lane; k0 < k4 && a.K > 64; k0 += 256) {    // four entries of a lane at a time, their loads in flight together
+        int v[4];
+        float t[4], zk[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int k = k0 + 64 * u;
+            v[u] = k < 64 ? first.v : -1;
+            t[u] = k < 64 ? first.t : -INFINITY;
+            if (k >= 64 && k < a.K) {
+                v[u] = class_at(a.top_idx, (int64_t)n * a.K + k, a.wide_index, a.V);
+                t[u] = teacher_logit(a, (int64_t)n * a.K + k);
             }
         }
-        if (v < 0) t = -INFINITY;
-        e.zk[k] = v >= lo && v < hi ? ld_elem(z, v) : 0.f;
-        e.idx[k] = v;
-        e.prob[k] = t;
-        tm = fmaxf(tm, t);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) zk[u] = v[u] >= lo && v[u] < hi ? ld_elem(z, v[u]) : 0.f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int k = k0 + 64 * u;
+            if (v[u] < 0) t[u] = -INFINITY;
+            if (k < k4) {
+                e.zk[k] = zk[u];
+                e.idx[k] = v[u];
+                e.prob[k] = t[u];
+                tm = fmaxf(tm, t[u]);
+            }
+        }
     }
     tm = wave_max(tm);
     float ts = 0.f;

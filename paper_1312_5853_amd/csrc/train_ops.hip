@@ -52,6 +52,9 @@ int pow2_down(int v)
 // a launch has fewer than 2^32 threads
 bool launchable(int64_t blocks, int threads) { return blocks * threads < (int64_t)1 << 32; }
 
+constexpr size_t kMaxLds = 160 * 1024;
+int pitch_of(int threads) { return threads + 9; }        // words between a thread's sums, channels last
+
 constexpr int kMaxWaves = 16, kSplitWaves = 8, kSplitRun = 4;
 
 // How a call runs: which kernels, on what tiles, with how much scratch.
@@ -131,11 +134,16 @@ void plan_last(NormPlan &p, bool bwd, int V, int eb)
     const int most = !bwd ? 16 : eb == 4 ? 10 : 8;
     int best = 0;
     double best_score = 0.0;
+    p.one = a.cpg % V == 0;
+    auto lds_of = [&](int threads, int64_t slab_groups) {
+        const int64_t of_channels = bwd ? 2 * slab_groups * a.cpg : 0;
+        return (size_t)(2 * (p.one && !bwd ? 1 : V) * pitch_of(threads) + 2 * slab_groups + of_channels) * 4;
+    };
     auto lanes_of = [&](int slab_groups) { return (int)(((int64_t)slab_groups * a.cpg + V - 1) / V); };
     for (int j = 1; j <= a.groups; ++j) {
         if (a.groups % j) continue;
         const int64_t lanes64 = ((int64_t)j * a.cpg + V - 1) / V;
-        if (lanes64 > 1024) break;
+        if (lanes64 > 1024 || lds_of(1024, j) > kMaxLds) break;
         const int rows = 1024 / (int)lanes64;
         if (ceil_div(a.S, rows) > most) continue;
         const double seg = (double)j * a.cpg * eb;
@@ -181,15 +189,14 @@ void plan_last(NormPlan &p, bool bwd, int V, int eb)
     a.slabs = a.groups / a.slab_groups;
     p.threads = threads;
     p.regs = ceil_div(a.tile_rows, a.rows);
-    a.pitch = threads + 9;
+    a.pitch = pitch_of(threads);
     a.group_lanes = std::min(64, pow2_down(std::max(1, threads / a.slab_groups)));
     a.channel_lanes = std::min(64, pow2_down(std::max(1, threads / a.cw)));
     a.work = a.N * a.tiles * a.slabs;
     a.units_per_xcd = ceil_div(a.work, 8);
     p.blocks = 8 * (int64_t)a.units_per_xcd;
-    p.one = a.cpg % V == 0;
     a.div_width = make_fastdiv(p.one ? a.cpg / V : a.cpg);
-    p.lds = (size_t)(2 * (p.one && !bwd ? 1 : V) * a.pitch + 2 * a.slab_groups + (bwd ? 2 * a.cw : 0)) * 4;
+    p.lds = lds_of(threads, a.slab_groups);
     a.rows_per_sample = a.tiles;
     a.div_lanes = make_fastdiv(a.lanes);
     a.div_slabs = make_fastdiv(a.slabs);
@@ -274,7 +281,7 @@ template <typename Kern>
 void launch_norm(Kern kern, const NormPlan &p, size_t lds, hipStream_t st)
 {
     if (lds > 64 * 1024)                             // more dynamic LDS than that has to be allowed per kernel
-        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kMaxLds);
     hipLaunchKernelGGL(kern, dim3((unsigned)p.blocks), dim3(p.threads), lds, st, p.a);
 }
 

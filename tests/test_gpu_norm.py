@@ -317,3 +317,10 @@ def test_groups_of_millions_of_channels():
     assert float((dx - want).abs().max()) < 0.02
     assert float((dbeta - dyd.sum((0, 2, 3))).abs().max()) < 1e-4
     assert float((dgamma - (dyd * xh).sum((0, 2, 3))).abs().max()) < 1e-2
+
+
+@pytest.mark.parametrize("shape", [(512, 8192, 1, 1, 4096), (512, 8190, 1, 2, 8190)])
+def test_thousands_of_small_groups_channels_last(shape):
+    """The widest slabs: their channels' and groups' sums have to fit beside the threads' own."""
+    N, C, H, W, G = shape
+    run_case(N, C, H, W, G, "none", "last", "bf16", seed=14)

@@ -122,7 +122,8 @@ __device__ __forceinline__ float row_max(const typename Vec<T>::Raw (&raw)[R])
 
 // The exponentials of a row, relative to its maximum m.  exp((z - m) / T) is 2^(z c - m c) with c = log2 e / T.  m c is
 // rounded to `mc`, so that one multiply-add gives the exponent; what that leaves out, m c - mc, is the same for every value,
-// and a factor 2^-(m c - mc) on their sum puts it right.  (`fix` is that factor.)
+// and a factor 2^-(m c - mc) on their sum puts it right.  (`fix` is that factor.)  It is half an ulp of mc at most, and has
+// to stay small for that: see kFar.
 struct Scale { float c, mc, fix; };
 
 __device__ __forceinline__ Scale scale_of(float c, float m)
@@ -134,8 +135,11 @@ __device__ __forceinline__ Scale scale_of(float c, float m)
 // Which exponentials a row needs: kOne: one of them (only one term has a target, or T = 1: they are the same); kTwo: both;
 // kSquare, kFourth: both, with T = 2 or 4: exp(z - m) is then the second or fourth power of exp((z - m) / T), one
 // exponential (four times a vector operation) and a multiplication or two instead of two exponentials.  kFar: both, the
-// maximum taken off first; for maxima whose product with c leaves the range (a row of the type's lowest values, say).
+// maximum taken off first; for maxima whose product with c is kFarFrom or more (a share of a row at a mask's -1e9 or at the
+// type's lowest value, say).  Below that m c - mc is 1/4 at most, so that the exponentials, their fourth powers and `fix`'s
+// stay within a factor of 2 of those relative to m; at 2^32 the difference passes 128 and an exponential the range.
 enum { kOne, kTwo, kSquare, kFourth, kFar };
+constexpr float kFarFrom = 8388608.f;                    // 2^23
 
 template <int HOW>
 __device__ __forceinline__ void add_exps(float v, const Scale &t, const Scale &o, float &sT, float &s1)
@@ -207,7 +211,7 @@ struct RowExps {
         o = scale_of(a.to_21, m);
         const bool both = temp_needed && one_needed && a.T != 1.f;
         how = !both ? kOne : a.T == 2.f ? kSquare : a.T == 4.f ? kFourth : kTwo;
-        if (!(fabsf(t.mc) < 1e30f && fabsf(o.mc) < 1e30f)) {
+        if (!(fabsf(t.mc) < kFarFrom && fabsf(o.mc) < kFarFrom)) {
             how = kFar;
             t.mc = m;
             t.fix = o.fix = 1.f;

@@ -329,3 +329,32 @@ def test_offsets_past_32_bits():
     loss, dz = hp.distill_loss_fwd_bwd(z, labels=lab, dz=z)
     assert not loss[:-3].any() and not dz[:-3].any()
     assert torch.allclose(loss[-3:], want[0], rtol=1e-6) and torch.allclose(dz[-3:], want[1], rtol=1e-4, atol=1e-9)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [40, 5003, 70001])
+@pytest.mark.parametrize("value", [1e8, 1e9, -1e9, 1e10, -1e10, 1e12, -1e15, 1e20, -1e20, 1e28, -1e28])
+def test_even_rows_of_large_logits(V, value, dtype):
+    """Rows of one value, with and without a class above it, at magnitudes whose products with log2 e have no small rounding."""
+    z, lab, idx, val = inputs(4, V, 4, "f32", 15)
+    z[:2] = value
+    z[1, 2] = value + abs(value) / 2
+    lab[:], idx[:] = 2, [0, 1, 2, 3]
+    if dtype == "bf16":
+        z, val = oracle.bf16_round(z), oracle.bf16_round(val)
+    for T in (1.0, 1.5, 2.0, 4.0, 0.05, 0.01):
+        run_case(z, lab, idx, val, T, dtype=dtype)
+
+
+@pytest.mark.parametrize("V,first,last", [(5003, 0, 4200), (5003, 900, 5003), (70001, 0, 40000), (70001, 20000, 70001)])
+@pytest.mark.parametrize("low", [-1e9, -1e10, -1e20, -1e28])
+def test_classes_left_out_side_by_side(V, first, last, low):
+    """Whole wavefronts and parts of a row at a large negative value, beside ordinary logits."""
+    z, lab, idx, val = inputs(5, V, 4, "f32", 16)
+    z[:, first:last] = low
+    free = np.setdiff1d(np.arange(V), np.arange(first, last))
+    idx = np.where(idx >= 0, free[idx % free.size], -1)
+    lab = np.where(lab >= 0, free[lab % free.size], -1)
+    for T in (1.0, 2.0, 4.0, 0.7):
+        stats, loss, dz, _ = run_case(z, lab, idx, val, T)
+        assert torch.isfinite(loss).all() and not dz[:, first:last].any()

@@ -358,3 +358,20 @@ def test_classes_left_out_side_by_side(V, first, last, low):
     for T in (1.0, 2.0, 4.0, 0.7):
         stats, loss, dz, _ = run_case(z, lab, idx, val, T)
         assert torch.isfinite(loss).all() and not dz[:, first:last].any()
+
+
+@pytest.mark.parametrize("V", [40, 5003, 70001])
+def test_a_term_of_weight_zero_is_absent_whatever_its_logits(V):
+    """Classes at -infinity that only the term of weight zero names: the other term is what it is without that one."""
+    z, lab, idx, val = inputs(5, V, 4, "f32", 17)
+    lab[:], idx[:] = [1, 2, 3, V - 1, 1], [5, 6, 7, 8]
+    for out, wk, wl in (([5, 8], 0.0, 0.6), ([1, 2, 3, V - 1], 0.6, 0.0)):
+        y = z.copy()
+        y[:, out] = -INF
+        alone = (lab, None, None) if wk == 0.0 else (None, idx, val)
+        _, loss, dz, _ = run_case(y, *alone, 2.0, wk, wl)
+        args = dict(labels=dev(lab), top_idx=dev(idx), top_val=dev(val), temperature=2.0, kd_weight=wk, label_weight=wl)
+        both = hp.distill_loss_fwd_bwd(dev(y), **args)
+        got, stats = hp.distill_loss_fwd(dev(y), **args)
+        assert torch.equal(got, loss) and torch.equal(both[0], loss)
+        assert torch.equal(hp.distill_loss_bwd(dev(y), stats, **args), dz) and torch.isfinite(dz).all()

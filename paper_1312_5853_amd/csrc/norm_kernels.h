@@ -17,10 +17,11 @@
 // (flat; every lane leaves its own sums in LDS, 16 lanes add a plane's).
 // Channels last: a work-group takes `cw` neighbouring channels (whole groups) of a sample; a lane keeps its columns and
 // walks down the positions.
-// A plane's last vector is moved back so that it ends where the plane ends; the values of the vector before that it holds
-// then are replaced by its last one, which leaves the sums with a known number of copies of one value to take off: two
-// operations to a vector, where a mask takes one or two to each value.  A slab's last vector is moved back too; its first
-// values are the ones of the vector before it, are left out of the sums and written twice, the same.
+// A plane's last vector is moved back so that it ends where the plane ends.  The values of the vector before that it holds
+// then are zeros for the sums: of x, then of the distances from the mean (forward), and of dy (backward), whose share in
+// every sum is then 0.  Only the lanes with such a vector spend operations on it.  (Sums that take in copies of a value and
+// take them off again turn an infinity into a NaN.)  A slab's last vector is moved back too; its first values are the ones
+// of the vector before it, are left out of the sums and written twice, the same.
 
 constexpr int kWhole = 0, kSums = 1, kApply = 2;
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -36,7 +37,8 @@ struct NormArgs {
     float *sample_sums;              // backward: A, then B, of every sample and channel (`part` itself where a sample has one row)
     float *dgamma, *dbeta;
     int N, C, S, groups, cpg, act, join;
-    float eps, inv_m;                // inv_m: 1 / M
+    double inv_m;                    // 1 / M
+    float eps;
     FastDiv div_groups, div_cpg;
     int part_rows, rows_per_sample;  // rows of C sums in `part`, and of those a sample's
     int join_lanes;                  // threads to channels where a group's sums are joined
@@ -99,12 +101,15 @@ __device__ __forceinline__ float join_waves(float v, float *red, int nw)
     return s;
 }
 
-// The tiles' means and squared distances of a group, joined to the group's over the lanes of a wave: four tiles of a lane
-// at a time (their loads in flight together), these with the lane's others, then the lanes.
+// The tiles' means and squared distances of a group, joined to the group's over the lanes of a wave, four loads of each
+// kind in flight at once.  In 64 bits, as distances from the first tile's mean r0: sum n (m_t - r0) and
+// sum (d_t + n (m_t - r0)^2).  The variance is then a difference, but of terms that r0's own tile bounds by the number of tiles
+// times the variance, below 2^20 of them; tiles of one mean have exactly that mean; and an infinite one stays infinite.
 __device__ __forceinline__ void join_tiles(const NormArgs &a, int64_t group, int lane, float &mean, float &rstd)
 {
     const float *p = a.part + group * a.tiles * 3;
-    float n = 0.f, m = 0.f, d = 0.f;
+    const double r0 = __builtin_isfinite(p[0]) ? p[0] : 0.;
+    double s = 0., d = 0.;
     for (int t0 = lane; t0 < a.tiles; t0 += 256) {
         float tm[4], td[4], tn[4];
 #pragma unroll
@@ -112,21 +117,19 @@ __device__ __forceinline__ void join_tiles(const NormArgs &a, int64_t group, int
             const int t = min(t0 + 64 * u, a.tiles - 1);
             tm[u] = p[3 * t];
             td[u] = p[3 * t + 1];
-            tn[u] = t0 + 64 * u < a.tiles ? p[3 * t + 2] : 0.f;
+            tn[u] = p[3 * t + 2];
         }
-        const float cn = (tn[0] + tn[1]) + (tn[2] + tn[3]);
-        const float cm = (tm[0] * tn[0] + tm[1] * tn[1] + (tm[2] * tn[2] + tm[3] * tn[3])) / cn;
-        float cd = 0.f;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) cd += tn[u] > 0.f ? td[u] + tn[u] * (tm[u] - cm) * (tm[u] - cm) : 0.f;
-        const float gap = cm - m, all = n + cn;
-        d += cd + gap * gap * n * cn / all;
-        m = n > 0.f ? m + gap * cn / all : cm;
-        n = all;
+        for (int u = 0; u < 4; ++u)
+            if (t0 + 64 * u < a.tiles) {
+                const double gap = tm[u] - r0, w = tn[u] * gap;
+                s += w;
+                d += fma(w, gap, (double)td[u]);
+            }
     }
-    mean = wave_sum(n > 0.f ? m * n : 0.f) * a.inv_m;
-    d = wave_sum(n > 0.f ? d + n * (m - mean) * (m - mean) : 0.f);
-    rstd = 1.f / sqrtf(d * a.inv_m + a.eps);
+    const double shift = wave_sum(s) * a.inv_m;
+    mean = (float)(r0 + shift);
+    rstd = 1.f / sqrtf((float)(wave_sum(d) * a.inv_m - shift * shift) + a.eps);
 }
 
 // ---------------------------------------------------------------------------
@@ -271,19 +274,18 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, R <= 4 ? 8 : 6) void group_norm_
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (r < n) {
-                if (moved && pl[r].tail) Vec<T>::repeat_last(raw[r], moved);
+                if (moved && pl[r].tail) Vec<T>::clear_first(raw[r], moved);
                 float v[V];
                 Vec<T>::open(raw[r], v);
                 if (pl[r].on) {
 #pragma unroll
                     for (int k = 0; k < V; ++k) s += v[k];
-                    if (moved) s = fmaf(pl[r].tail ? -(float)moved : 0.f, v[V - 1], s);
                     if (MODE == kSums) cnt += pl[r].tail ? V - moved : V;
                 }
             }
         s = wave_sum(s);
         if (!SOLO) s = join_waves(s, red[0], nw);
-        float inv = a.inv_m;
+        float inv = (float)a.inv_m;
         if (MODE == kSums) {
             cnt = join_waves(wave_sum(cnt), red[2], nw);       // at most 2^16 values to a tile: exact
             inv = 1.f / cnt;
@@ -298,11 +300,14 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, R <= 4 ? 8 : 6) void group_norm_
                 Vec<T>::open(raw[r], v);
                 if (pl[r].on) {
 #pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        v[k] -= mean;
-                        s = fmaf(v[k], v[k], s);
+                    for (int k = 0; k < V; ++k) v[k] -= mean;
+                    if (moved && pl[r].tail) {
+#pragma unroll
+                        for (int k = 0; k < V - 1; ++k)
+                            if (k < moved) v[k] = 0.f;
                     }
-                    if (moved) s = fmaf((pl[r].tail ? -(float)moved : 0.f) * v[V - 1], v[V - 1], s);
+#pragma unroll
+                    for (int k = 0; k < V; ++k) s = fmaf(v[k], v[k], s);
                 }
             }
         s = wave_sum(s);
@@ -402,10 +407,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, R <= 2 ? 8 : R <= 4 ? 5 : 4) voi
                 PlaneLane l;
                 float sc, sh, xv[V], dv[V];
                 find(r, l, sc, sh);
-                if (moved && l.tail) {
-                    Vec<T>::repeat_last(rx[r], moved);
-                    Vec<T>::repeat_last(rd[r], moved);
-                }
+                if (moved && l.tail) Vec<T>::clear_first(rd[r], moved);
                 Vec<T>::open(rx[r], xv);
                 Vec<T>::open(rd[r], dv);
 #pragma unroll
@@ -416,11 +418,6 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, R <= 2 ? 8 : R <= 4 ? 5 : 4) voi
                     for (int k = 0; k < V; ++k) {
                         A += dv[k];
                         B = fmaf(dv[k], xv[k], B);
-                    }
-                    if (moved) {
-                        const float off = (l.tail ? -(float)moved : 0.f) * dv[V - 1];
-                        A += off;
-                        B = fmaf(off, xv[V - 1], B);
                     }
                 }
                 if constexpr (kKeep) {

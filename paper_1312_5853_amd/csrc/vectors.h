@@ -46,11 +46,11 @@ struct Vec<float> {
             if (k >= n) r[k] = p[k];
         return r;
     }
-    static __device__ __forceinline__ void repeat_last(Raw &r, int n)        // the last value in place of the first n
+    static __device__ __forceinline__ void clear_first(Raw &r, int n)        // zeros in place of the first n values, n < V
     {
 #pragma unroll
         for (int k = 0; k < 3; ++k)
-            if (k < n) r[k] = r[3];
+            if (k < n) r[k] = 0.f;
     }
 };
 
@@ -104,13 +104,12 @@ struct Vec<unsigned short> {
             if (k >= n) r[k >> 1] |= (unsigned)p[k] << (16 * (k & 1));
         return r;
     }
-    static __device__ __forceinline__ void repeat_last(Raw &r, int n)
+    static __device__ __forceinline__ void clear_first(Raw &r, int n)
     {
-        const unsigned last = r[3] >> 16, both = last | (r[3] & 0xFFFF0000u);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            if (2 * k + 1 < n) r[k] = both;
-            else if (2 * k < n) r[k] = (r[k] & 0xFFFF0000u) | last;
+            if (2 * k + 1 < n) r[k] = 0u;
+            else if (2 * k < n) r[k] &= 0xFFFF0000u;
         }
     }
 };
@@ -157,6 +156,25 @@ __device__ __forceinline__ float wave_max(float v)
     v = fmaxf(v, dpp_move<0x141>(v));
     v = fmaxf(v, dpp_move<0x140>(v));
     return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
+}
+template <int CTRL>
+__device__ __forceinline__ double dpp_move(double v)
+{
+    return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xF, 0xF, false),
+                            __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xF, 0xF, false));
+}
+__device__ __forceinline__ double lane_value(double v, int lane)
+{
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane),
+                            __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
+__device__ __forceinline__ double wave_sum(double v)
+{
+    v += dpp_move<0xB1>(v);
+    v += dpp_move<0x4E>(v);
+    v += dpp_move<0x141>(v);
+    v += dpp_move<0x140>(v);
+    return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
 }
 // sum over the aligned runs of `width` lanes (a power of two), the same in every lane of a run
 __device__ __forceinline__ float run_sum(float v, int width)

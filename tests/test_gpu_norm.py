@@ -324,3 +324,58 @@ def test_thousands_of_small_groups_channels_last(shape):
     """The widest slabs: their channels' and groups' sums have to fit beside the threads' own."""
     N, C, H, W, G = shape
     run_case(N, C, H, W, G, "none", "last", "bf16", seed=14)
+
+
+# Kernels of every plan: a wavefront to a group, a work-group to a group (one run of memory, planes of their own), tiles of
+# planes and of parts of a plane; slabs of whole groups and of groups that share vectors, tiles of slabs, very wide groups
+PLANS = [(1030, 4, 3, 7, 2), (3, 24, 13, 13, 4), (2, 6, 31, 45, 2), (1, 5, 120, 130, 1), (1, 2, 401, 399, 1), (2, 48, 9, 11, 3),
+         (2, 64, 27, 27, 8), (1, 70, 112, 113, 2), (1, 9000, 1, 7, 1), (2, 3, 2, 1, 3)]
+
+
+@pytest.mark.parametrize("act", ["none", "silu"])
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", PLANS)
+def test_an_infinite_gradient_wherever_it_stands(shape, layout, dtype, act):
+    """Sums with one infinite term are that infinity, in the channel that holds it; the other groups do not see it."""
+    N, C, H, W, G = shape
+    (x, _), (xd, dyd), gamma, beta = _tensors(N, C, H, W, layout, dtype, 30)
+    ga, be = _cuda(gamma), _cuda(beta)
+    _, mean, rstd = hp.group_norm_act_fwd(xd, G, ga, be, act=act)
+    want = hp.group_norm_act_bwd(xd, dyd, mean, rstd, ga, be, act=act)
+    S, c = H * W, C // 2
+    other = torch.ones(C, dtype=torch.bool, device="cuda")
+    other[c] = False
+    for s in sorted({p for p in (*range(9), *range(S - 18, S)) if 0 <= p < S}):
+        dyi = dyd.clone(memory_format=torch.preserve_format)
+        dyi[N - 1, c, s // W, s % W] = float("inf")
+        dx, dgamma, dbeta = hp.group_norm_act_bwd(xd, dyi, mean, rstd, ga, be, act=act)
+        xi, m, r = (float(v) for v in (xd[N - 1, c, s // W, s % W], mean[N - 1, c * G // C], rstd[N - 1, c * G // C]))
+        z = float(ga[c]) * (xi - m) * r + float(be[c])
+        slope = 1.0 if act == "none" else (1 + z / (1 + np.exp(z))) / (1 + np.exp(-z))
+        assert float(dbeta[c]) == np.copysign(np.inf, slope), s
+        assert float(dgamma[c]) == np.copysign(np.inf, slope * (xi - m)), s
+        assert torch.equal(dbeta[other], want[2][other]) and torch.equal(dgamma[other], want[1][other])
+        per = C // G
+        same = torch.ones(N, C, dtype=torch.bool, device="cuda")
+        same[N - 1, c // per * per:(c // per + 1) * per] = False
+        assert torch.equal(dx[same], want[0][same])
+
+
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", PLANS)
+def test_the_mean_of_an_infinite_value_wherever_it_stands(shape, layout, dtype):
+    N, C, H, W, G = shape
+    (x, _), (xd, _), gamma, beta = _tensors(N, C, H, W, layout, dtype, 31)
+    S, c = H * W, C // 2
+    want = hp.group_norm_act_fwd(xd, G, act="relu")[1]
+    for sign in (1.0, -1.0):
+        for s in sorted({p for p in (*range(9), *range(S - 18, S)) if 0 <= p < S}):
+            xi = xd.clone(memory_format=torch.preserve_format)
+            xi[N - 1, c, s // W, s % W] = sign * float("inf")
+            y, mean, rstd = hp.group_norm_act_fwd(xi, G, act="relu")
+            here = (N - 1, c * G // C)
+            assert float(mean[here]) == sign * float("inf") and torch.isnan(rstd[here]), s
+            mean[here] = want[here]
+            assert torch.equal(mean, want)

@@ -37,8 +37,8 @@ struct NormArgs {
     float *sample_sums;              // backward: A, then B, of every sample and channel (`part` itself where a sample has one row)
     float *dgamma, *dbeta;
     int N, C, S, groups, cpg, act, join;
-    double inv_m;                    // 1 / M
-    float eps;
+    double inv_m64;                  // 1 / M, also as inv_m
+    float eps, inv_m;
     FastDiv div_groups, div_cpg;
     int part_rows, rows_per_sample;  // rows of C sums in `part`, and of those a sample's
     int join_lanes;                  // threads to channels where a group's sums are joined
@@ -53,6 +53,9 @@ struct NormArgs {
     int tile_rows, pitch, group_lanes, channel_lanes, units_per_xcd, work;
     FastDiv div_lanes, div_slabs, div_width;  // width: sums of a group in a thread row (forward)
 };
+
+// z is taken the same way everywhere, d = x - mean first and then one multiply-add with gamma rstd and beta: exact at the
+// mean however far from zero that is, and the same bits backward as forward, so that both agree on the side of a ReLU.
 
 // The activation is decided once for a vector, so that its values' chains (two of the slow instructions each in a SiLU)
 // run beside each other.
@@ -91,6 +94,13 @@ __device__ __forceinline__ void act_bwd(float (&dy)[V], const float (&d)[V], int
     }
 }
 
+// s / n, with n's reciprocal at hand: the remainder of the first quotient corrects it (a group of one value has that mean)
+__device__ __forceinline__ float quotient(float s, float n, float inv)
+{
+    const float q = s * inv;
+    return fmaf(fmaf(-q, n, s), inv, q);
+}
+
 // the waves' values joined in their order; `red` holds one per wave.  Every thread gets the sum.
 __device__ __forceinline__ float join_waves(float v, float *red, int nw)
 {
@@ -127,9 +137,9 @@ __device__ __forceinline__ void join_tiles(const NormArgs &a, int64_t group, int
                 d += fma(w, gap, (double)td[u]);
             }
     }
-    const double shift = wave_sum(s) * a.inv_m;
+    const double shift = wave_sum(s) * a.inv_m64;
     mean = (float)(r0 + shift);
-    rstd = 1.f / sqrtf((float)(wave_sum(d) * a.inv_m - shift * shift) + a.eps);
+    rstd = 1.f / sqrtf((float)(wave_sum(d) * a.inv_m64 - shift * shift) + a.eps);
 }
 
 // ---------------------------------------------------------------------------
@@ -274,7 +284,10 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, R <= 4 ? 8 : 6) void group_norm_
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (r < n) {
-                if (moved && pl[r].tail) Vec<T>::clear_first(raw[r], moved);
+                if (moved && pl[r].tail) {
+                    as_branch();
+                    Vec<T>::clear_first(raw[r], moved);
+                }
                 float v[V];
                 Vec<T>::open(raw[r], v);
                 if (pl[r].on) {
@@ -285,12 +298,11 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, R <= 4 ? 8 : 6) void group_norm_
             }
         s = wave_sum(s);
         if (!SOLO) s = join_waves(s, red[0], nw);
-        float inv = (float)a.inv_m;
+        mean = (float)(s * a.inv_m64);
         if (MODE == kSums) {
             cnt = join_waves(wave_sum(cnt), red[2], nw);       // at most 2^16 values to a tile: exact
-            inv = 1.f / cnt;
+            mean = s / cnt;
         }
-        mean = s * inv;
         s = 0.f;
         if (MODE == kWhole) open_again(raw);
 #pragma unroll
@@ -302,6 +314,7 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, R <= 4 ? 8 : 6) void group_norm_
 #pragma unroll
                     for (int k = 0; k < V; ++k) v[k] -= mean;
                     if (moved && pl[r].tail) {
+                        as_branch();
 #pragma unroll
                         for (int k = 0; k < V - 1; ++k)
                             if (k < moved) v[k] = 0.f;
@@ -334,9 +347,11 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, R <= 4 ? 8 : 6) void group_norm_
     for (int r = 0; r < R; ++r)
         if (r < n && t.live) {
             const float scale = rstd * (a.gamma ? a.gamma[c0 + pl[r].c] : 1.f);
-            const float shift = fmaf(-mean, scale, a.beta ? a.beta[c0 + pl[r].c] : 0.f);
+            const float shift = a.beta ? a.beta[c0 + pl[r].c] : 0.f;
             float v[V];
             Vec<T>::open(raw[r], v);
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] -= mean;
             act_fwd(v, a.act, [&](int) { return scale; }, [&](int) { return shift; });
             plane_store(y, pl[r], moved, v);
         }
@@ -407,7 +422,10 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, R <= 2 ? 8 : R <= 4 ? 5 : 4) voi
                 PlaneLane l;
                 float sc, sh, xv[V], dv[V];
                 find(r, l, sc, sh);
-                if (moved && l.tail) Vec<T>::clear_first(rd[r], moved);
+                if (moved && l.tail) {
+                    as_branch();
+                    Vec<T>::clear_first(rd[r], moved);
+                }
                 Vec<T>::open(rx[r], xv);
                 Vec<T>::open(rd[r], dv);
 #pragma unroll
@@ -654,8 +672,8 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
                 const int p = t.p + done * a.rows;
                 if (MODE != kWhole) load(p);
                 const int cnt = min(R, mine - done);
-                const float inv = cnt > 0 ? 1.f / (cnt * (V / W)) : 0.f;
-                float bs[W], bd[W];
+                const float n2 = cnt * (V / W), inv = cnt > 0 ? 1.f / n2 : 0.f;
+                float bs[W], bd[W], bm[W];
 #pragma unroll
                 for (int k = 0; k < W; ++k) bs[k] = bd[k] = 0.f;
 #pragma unroll
@@ -666,6 +684,8 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
 #pragma unroll
                         for (int k = 0; k < V; ++k) bs[k % W] += v[k];
                     }
+#pragma unroll
+                for (int k = 0; k < W; ++k) bm[k] = quotient(bs[k], n2, inv);
                 open_again(raw);
 #pragma unroll
                 for (int r = 0; r < R; ++r)
@@ -674,16 +694,16 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
                         Vec<T>::open(raw[r], v);
 #pragma unroll
                         for (int k = 0; k < V; ++k) {
-                            const float e = v[k] - bs[k % W] * inv;
+                            const float e = v[k] - bm[k % W];
                             bd[k % W] = fmaf(e, e, bd[k % W]);
                         }
                     }
                 // joined with the rows before: n1 n2 / (n1 + n2) times the square of the means' distance comes on top
-                const float n1 = done * (V / W), n2 = cnt * (V / W), inv1 = done ? 1.f / n1 : 0.f, both = n1 * n2 / (n1 + n2);
+                const float n1 = done * (V / W), inv1 = done ? 1.f / n1 : 0.f, both = n1 * n2 / (n1 + n2);
 #pragma unroll
                 for (int k = 0; k < W; ++k) {
                     if (MODE != kWhole && done) {
-                        const float gap = bs[k] * inv - s[k] * inv1;
+                        const float gap = bm[k] - quotient(s[k], n1, inv1);
                         d[k] += gap * gap * both;
                     }
                     s[k] += bs[k];
@@ -702,7 +722,7 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
         const int width = ONE ? a.cpg / V : a.cpg;                                  // sums of a group in a thread row
         const int lane = threadIdx.x & (a.group_lanes - 1), entries = a.rows * width;
         const int at = threadIdx.x / a.group_lanes, step = blockDim.x / a.group_lanes;
-        const float total = (float)t.count * a.cpg, inv_total = 1.f / total;
+        const float total = (float)t.count * a.cpg;                                 // below 2^24: exact
         const float n_whole = whole * (V / W), n_more = (whole + 1) * (V / W);
         const float inv_whole = whole ? 1.f / n_whole : 0.f, inv_more = 1.f / n_more;
         auto slot = [&](int p, int g, int i) {
@@ -717,12 +737,12 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
                     const int p = fastdiv(e, a.div_width);
                     s += sum[slot(p, g, e - p * width)];
                 }
-            const float mean = run_sum(s, a.group_lanes) * inv_total;
+            const float mean = run_sum(s, a.group_lanes) / total;
             if (some)
                 for (int e = lane; e < entries; e += a.group_lanes) {
                     const int p = fastdiv(e, a.div_width), i = slot(p, g, e - p * width);
                     const bool more = p < extra;
-                    const float diff = sum[i] * (more ? inv_more : inv_whole) - mean;
+                    const float diff = quotient(sum[i], more ? n_more : n_whole, more ? inv_more : inv_whole) - mean;
                     if (more || whole) d += dev[i] + (more ? n_more : n_whole) * diff * diff;
                 }
             d = run_sum(d, a.group_lanes);
@@ -768,17 +788,16 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
     float scale[V], shift[V];
     slab_params<V>(a, t, a.gamma, 1.f, scale);
     slab_params<V>(a, t, a.beta, 0.f, shift);
-    float mean = 0.f, rstd = 0.f;
+    float mean[W], rstd = 0.f;
     GroupWalk walk(a, t);
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-        if (!ONE || k == 0) {
+        if (k < W) {
             const int g = walk.next(a);
-            mean = gmean[g];
+            mean[k] = gmean[g];
             rstd = grstd[g];
         }
         scale[k] *= rstd;
-        shift[k] = fmaf(-mean, scale[k], shift[k]);
     }
     T *y = static_cast<T *>(a.out) + base;
     if (MODE == kWhole) open_again(raw);
@@ -791,6 +810,8 @@ __global__ __launch_bounds__(1024) void group_norm_last_fwd(NormArgs a)
             if (s < t.count) {
                 float v[V];
                 Vec<T>::open(raw[r], v);
+#pragma unroll
+                for (int k = 0; k < V; ++k) v[k] -= mean[k % W];
                 act_fwd(v, a.act, [&](int k) { return scale[k]; }, [&](int k) { return shift[k]; });
                 slab_store(a, y + s * a.C, t, v);
             }
@@ -1133,14 +1154,14 @@ __global__ __launch_bounds__(1024) void group_norm_wide_bwd(NormArgs a)
     const float mean = a.mean[blockIdx.x], rstd = a.rstd[blockIdx.x];
     float m1 = 0.f, m2 = 0.f;
     for (int c = c0 + threadIdx.x; c < c0 + a.cpg; c += blockDim.x) {
-        const float gamma = a.gamma ? a.gamma[c] : 1.f, beta = a.beta ? a.beta[c] : 0.f;
+        const float gamma = a.gamma ? a.gamma[c] : 1.f, beta = a.beta ? a.beta[c] : 0.f, scale = rstd * gamma;
         float A = 0.f, B = 0.f;
         for (int r = 0; r < a.S; ++r) {
-            const float xh[1] = {(ld_elem(x, r * a.C + c) - mean) * rstd};
+            const float d[1] = {ld_elem(x, r * a.C + c) - mean};
             float dz[1] = {ld_elem(dy, r * a.C + c)};
-            act_bwd(dz, xh, a.act, [&](int) { return gamma; }, [&](int) { return beta; });
+            act_bwd(dz, d, a.act, [&](int) { return scale; }, [&](int) { return beta; });
             A += dz[0];
-            B += dz[0] * xh[0];
+            B += dz[0] * (d[0] * rstd);
         }
         a.part[(int64_t)n * a.C + c] = A;
         a.part[((int64_t)a.part_rows + n) * a.C + c] = B;
@@ -1150,12 +1171,12 @@ __global__ __launch_bounds__(1024) void group_norm_wide_bwd(NormArgs a)
     m1 = block_sum(m1, red) * a.inv_m;
     m2 = block_sum(m2, red) * a.inv_m;
     for (int c = c0 + threadIdx.x; c < c0 + a.cpg; c += blockDim.x) {
-        const float gamma = a.gamma ? a.gamma[c] : 1.f, beta = a.beta ? a.beta[c] : 0.f;
+        const float gamma = a.gamma ? a.gamma[c] : 1.f, beta = a.beta ? a.beta[c] : 0.f, scale = rstd * gamma;
         for (int r = 0; r < a.S; ++r) {
-            const float xh[1] = {(ld_elem(x, r * a.C + c) - mean) * rstd};
+            const float d[1] = {ld_elem(x, r * a.C + c) - mean};
             float dz[1] = {ld_elem(dy, r * a.C + c)};
-            act_bwd(dz, xh, a.act, [&](int) { return gamma; }, [&](int) { return beta; });
-            st_elem(dx, r * a.C + c, rstd * (gamma * dz[0] - m1 - xh[0] * m2));
+            act_bwd(dz, d, a.act, [&](int) { return scale; }, [&](int) { return beta; });
+            st_elem(dx, r * a.C + c, rstd * (gamma * dz[0] - m1 - d[0] * rstd * m2));
         }
     }
 }

@@ -212,7 +212,8 @@ int plan_norm(NormPlan &p, int op, int N, int C, int S, int groups, int layout, 
     const int eb = glue_elem_bytes(dtype), V = 16 / eb;
     NormArgs &a = p.a;
     a.N = N; a.C = C; a.S = S; a.groups = groups; a.cpg = C / groups;
-    a.inv_m = 1.0 / ((double)a.cpg * S);
+    a.inv_m64 = 1.0 / ((double)a.cpg * S);
+    a.inv_m = (float)a.inv_m64;
     a.div_groups = make_fastdiv(groups);
     a.div_cpg = make_fastdiv(a.cpg);
     // one channel, or one position: the same memory either way

@@ -123,6 +123,10 @@ __device__ __forceinline__ void open_again(Raw (&raw)[R])
     for (int r = 0; r < R; ++r) asm volatile("" : "+v"(raw[r]));
 }
 
+// In a branch that few wavefronts take: keeps it one.  The compiler would else compute both sides and select (1024 x 64 planes
+// of 16 fp32 in 64 groups, none of which needs the branch: 16.1 us, and 15.1).
+__device__ __forceinline__ void as_branch() { asm volatile(""); }
+
 // Sum and maximum over the 64 lanes, the same in every lane: within the rows of 16 lanes by data-parallel-primitive
 // moves, then the four row results by scalar reads.
 __device__ __forceinline__ float max3(float a, float b, float c)          // the largest; a NaN is passed over

@@ -379,3 +379,35 @@ def test_the_mean_of_an_infinite_value_wherever_it_stands(shape, layout, dtype):
             assert float(mean[here]) == sign * float("inf") and torch.isnan(rstd[here]), s
             mean[here] = want[here]
             assert torch.equal(mean, want)
+
+
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", PLANS)
+def test_a_group_of_one_value_gives_its_shift(shape, layout, dtype):
+    """Every distance from the mean is zero, however large the mean: sums of up to 2^21 times 1536 = 3 * 2^9 are exact in
+    fp32, and so is their quotient."""
+    N, C, H, W, G = shape
+    for value in (1536.0, -96.0):
+        x = _dev(np.full((N, C, H, W), value), layout, dtype)
+        gamma, beta = torch.full((C,), 1.7, device="cuda"), torch.linspace(-2, 3, C, device="cuda")
+        y, mean, rstd = hp.group_norm_act_fwd(x, G, gamma, beta, act="none")
+        assert bool((mean == value).all())
+        assert torch.allclose(rstd, torch.full_like(rstd, 1e-5 ** -0.5), rtol=1e-6)
+        assert torch.equal(y, beta.to(y.dtype)[None, :, None, None].expand_as(y))
+
+
+@pytest.mark.parametrize("layout", ["planes", "last"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", PLANS)
+def test_forward_and_backward_agree_where_a_relu_is_open(shape, layout, dtype):
+    """With a gradient of one everywhere dbeta counts the values that pass; these are the ones that forward leaves positive,
+    and gamma's gradient has the sign that follows.  Means of 1 to 1000 deviations."""
+    N, C, H, W, G = shape
+    for k, level in enumerate((1.0, 30.0, 1000.0)):
+        _, (xd, _), gamma, beta = _tensors(N, C, H, W, layout, dtype, 20 + k, mean=level)
+        ga, be = _cuda(gamma), _cuda(0.1 * beta)
+        y, mean, rstd = hp.group_norm_act_fwd(xd, G, ga, be, act="relu")
+        ones = torch.ones_like(xd)
+        _, _, dbeta = hp.group_norm_act_bwd(xd, ones, mean, rstd, ga, be, act="relu")
+        assert torch.equal(dbeta.double(), (y > 0).double().sum((0, 2, 3)))         # counts below 2^24: exact

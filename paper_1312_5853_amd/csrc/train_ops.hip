@@ -74,7 +74,7 @@ int regs_for(int run, int most)
 void plan_planes(NormPlan &p, bool bwd, int V)
 {
     NormArgs &a = p.a;
-    a.vectors = (a.S + V - 1) / V;
+    a.vectors = (a.S - 1) / V + 1;
     a.chunks = (a.vectors + 63) / 64;
     // flat where a plane of its own would leave a sixth of the lanes idle: backward on 256 x 384 planes of 169 bfloat16 (22
     // vectors) 28 us, and 50 with a unit to a plane; on 128 x 256 planes of 729 (92) 36.2 and 37.1.  Longer planes gain

@@ -411,3 +411,22 @@ def test_forward_and_backward_agree_where_a_relu_is_open(shape, layout, dtype):
         ones = torch.ones_like(xd)
         _, _, dbeta = hp.group_norm_act_bwd(xd, ones, mean, rstd, ga, be, act="relu")
         assert torch.equal(dbeta.double(), (y > 0).double().sum((0, 2, 3)))         # counts below 2^24: exact
+
+
+def test_the_longest_plane():
+    """2^31 - 1 positions, of which the last vector holds seven of its eight."""
+    S = (1 << 31) - 1
+    x = torch.empty((1, 1, 1, S), dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(6))
+    x += 0.5
+    y, mean, rstd = hp.group_norm_act_fwd(x, 1, act="none")
+    dx, dgamma, dbeta = hp.group_norm_act_bwd(x, y, mean, rstd, act="none")
+    m = sum(p.double().sum().item() for p in x.view(-1).split(1 << 28)) / S
+    var = sum((p.double() - m).square().sum().item() for p in x.view(-1).split(1 << 28)) / S
+    assert abs(mean.item() - m) <= SUM and abs(rstd.item() * (var + 1e-5) ** 0.5 - 1) <= SUM
+    for at in (slice(0, 5000), slice(S // 2, S // 2 + 5000), slice(S - 5000, S)):
+        want = (x[0, 0, 0, at].double() - m) * (var + 1e-5) ** -0.5
+        assert bool(((y[0, 0, 0, at].double() - want).abs() <= 2.0 ** -8 * want.abs() + SUM).all())
+        # dy = y is xh up to its rounding: what is left of it after the share of xh
+        left = rstd.double().item() * (y[0, 0, 0, at].double() - dbeta.item() / S - want * dgamma.item() / S)
+        assert bool(((dx[0, 0, 0, at].double() - left).abs() <= 2.0 ** -8 * left.abs() + 16 * U * (1 + want.abs())).all())
+    assert abs(dgamma.item() / S - 1) <= 2.0 ** -8 and abs(dbeta.item() / S) <= 2.0 ** -8

@@ -243,3 +243,17 @@ def test_binding_refuses_what_the_library_cannot_see(lib):
         b.distill_loss_fwd_bwd(z, labels=lab, dz=torch.zeros(3, 8))
     with pytest.raises(TypeError):
         b.distill_loss_fwd_bwd(z.cuda() if torch.cuda.is_available() else z, labels=lab, dz=torch.zeros(3, 7, dtype=torch.bfloat16))
+
+
+@pytest.mark.parametrize("dtype,per_tile", [(0, 8192), (1, 16384)])
+def test_the_longest_plane(lib, dtype, per_tile):
+    """C * S of 2^31 - 1 is within the limits: tiles of a plane, three sums each, then the group's two."""
+    from paper_1312_5853_amd import binding as b
+    for S in ((1 << 31) - 1, (1 << 31) - 3, (1 << 31) - 16):
+        tiles = -(-S // per_tile)
+        need = lib.group_norm_act_workspace_bytes(b.OP_FWD, 1, 1, S, 1, 0, dtype)
+        assert need == -(-12 * tiles // 256) * 256 + 256
+        assert lib.group_norm_act_fwd(*_norm_args(N=1, C=1, S=S, groups=1, dtype=dtype, ws_bytes=need - 1)) == b.ERR_WORKSPACE
+        need = lib.group_norm_act_workspace_bytes(b.OP_BWD_DATA, 1, 1, S, 1, 0, dtype)
+        assert need == -(-8 * tiles // 256) * 256 + 256
+        assert lib.group_norm_act_bwd(*_norm_bwd_args(N=1, C=1, S=S, groups=1, dtype=dtype, ws_bytes=need - 1)) == b.ERR_WORKSPACE

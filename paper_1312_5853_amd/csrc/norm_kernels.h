@@ -102,11 +102,12 @@ __device__ __forceinline__ float quotient(float s, float n, float inv)
 }
 
 // the waves' values joined in their order; `red` holds one per wave.  Every thread gets the sum.
-__device__ __forceinline__ float join_waves(float v, float *red, int nw)
+template <typename F>
+__device__ __forceinline__ F join_waves(F v, F *red, int nw)
 {
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
-    float s = red[0];
+    F s = red[0];
     for (int i = 1; i < nw; ++i) s += red[i];
     return s;
 }
@@ -997,6 +998,9 @@ __global__ __launch_bounds__(1024) void group_norm_last_bwd(NormArgs a)
 // ---------------------------------------------------------------------------
 // Joining the tiles
 // ---------------------------------------------------------------------------
+// A thread's sums here and in the wide kernels below run over as many tiles, samples or channels as a call has, so they are
+// kept in 64 bits (a chain of 4096 like terms in fp32 is off by 600 of its roundings, and all threads' the same way).
+
 // A wave per sample and group, where the tiles are too many for every work-group to join them again.
 __global__ __launch_bounds__(256) void group_norm_join_stats(NormArgs a)
 {
@@ -1016,14 +1020,15 @@ __global__ __launch_bounds__(256) void group_norm_join_stats(NormArgs a)
 // at once.
 __global__ __launch_bounds__(1024) void group_norm_join_groups(NormArgs a)
 {
-    __shared__ float red[2][1024], shares[2][16];
+    __shared__ float red[2][1024];
+    __shared__ double shares[2][16];
     const int n = fastdiv(blockIdx.x, a.div_groups), c0 = (blockIdx.x - n * a.groups) * a.cpg, rows = a.rows_per_sample;
     const float *pa = a.part + (int64_t)n * rows * a.C + c0, *pb = pa + (int64_t)a.part_rows * a.C;
     const int i = threadIdx.x, x = i & (a.join_lanes - 1), sub = i / a.join_lanes, subs = blockDim.x / a.join_lanes;
-    float m1 = 0.f, m2 = 0.f;
+    double m1 = 0., m2 = 0.;
     for (int c1 = 0; c1 < a.cpg; c1 += a.join_lanes) {
         const int own = min(c1 + x, a.cpg - 1), c = c0 + own;
-        float A = 0.f, B = 0.f;
+        double A64 = 0., B64 = 0.;
         for (int t0 = sub; t0 < rows; t0 += 4 * subs) {
             float va[4], vb[4];
 #pragma unroll
@@ -1033,11 +1038,12 @@ __global__ __launch_bounds__(1024) void group_norm_join_groups(NormArgs a)
                 vb[u] = pb[at];
             }
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                A += t0 + u * subs < rows ? va[u] : 0.f;
-                B += t0 + u * subs < rows ? vb[u] : 0.f;
-            }
+            for (int u = 1; u < 4; ++u)
+                if (t0 + u * subs >= rows) va[u] = vb[u] = 0.f;
+            A64 += (va[0] + va[1]) + (va[2] + va[3]);
+            B64 += (vb[0] + vb[1]) + (vb[2] + vb[3]);
         }
+        float A = (float)A64, B = (float)B64;
         if (subs > 1) {
             __syncthreads();                             // the channels before are read
             red[0][i] = A;
@@ -1051,7 +1057,7 @@ __global__ __launch_bounds__(1024) void group_norm_join_groups(NormArgs a)
             }
         }
         if (sub == 0 && c1 + x < a.cpg) {
-            const float gamma = a.gamma ? a.gamma[c] : 1.f;
+            const double gamma = a.gamma ? a.gamma[c] : 1.f;
             m1 += gamma * A;
             m2 += gamma * B;
             a.sample_sums[(int64_t)n * a.C + c] = A;
@@ -1061,8 +1067,8 @@ __global__ __launch_bounds__(1024) void group_norm_join_groups(NormArgs a)
     m1 = join_waves(wave_sum(m1), shares[0], (int)(blockDim.x >> 6));
     m2 = join_waves(wave_sum(m2), shares[1], (int)(blockDim.x >> 6));
     if (i == 0) {
-        a.group_sums[2 * (int64_t)blockIdx.x] = m1 * a.inv_m;
-        a.group_sums[2 * (int64_t)blockIdx.x + 1] = m2 * a.inv_m;
+        a.group_sums[2 * (int64_t)blockIdx.x] = (float)(m1 * a.inv_m64);
+        a.group_sums[2 * (int64_t)blockIdx.x + 1] = (float)(m2 * a.inv_m64);
     }
 }
 
@@ -1073,7 +1079,7 @@ __global__ __launch_bounds__(256) void group_norm_join_channels(NormArgs a)
     __shared__ float red[2][16][17];
     const int x = threadIdx.x & 15, y = threadIdx.x >> 4, c = min((int)(blockIdx.x * 16) + x, a.C - 1);
     const float *pa = a.sample_sums + c, *pb = pa + (int64_t)a.N * a.C;
-    float A = 0.f, B = 0.f;
+    double A64 = 0., B64 = 0.;
     for (int n0 = y; n0 < a.N; n0 += 128) {
         float va[8], vb[8];
 #pragma unroll
@@ -1083,18 +1089,17 @@ __global__ __launch_bounds__(256) void group_norm_join_channels(NormArgs a)
             vb[u] = pb[n * a.C];
         }
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            A += n0 + 16 * u < a.N ? va[u] : 0.f;
-            B += n0 + 16 * u < a.N ? vb[u] : 0.f;
-        }
+        for (int u = 1; u < 8; ++u)
+            if (n0 + 16 * u >= a.N) va[u] = vb[u] = 0.f;
+        A64 += ((va[0] + va[1]) + (va[2] + va[3])) + ((va[4] + va[5]) + (va[6] + va[7]));
+        B64 += ((vb[0] + vb[1]) + (vb[2] + vb[3])) + ((vb[4] + vb[5]) + (vb[6] + vb[7]));
     }
-    red[0][x][y] = A;
-    red[1][x][y] = B;
+    red[0][x][y] = (float)A64;
+    red[1][x][y] = (float)B64;
     __syncthreads();
     // 16 lanes to a channel
     const int ch = blockIdx.x * 16 + y;
-    A = run_sum(red[0][y][x], 16);
-    B = run_sum(red[1][y][x], 16);
+    const float A = run_sum(red[0][y][x], 16), B = run_sum(red[1][y][x], 16);
     if (x == 0 && ch < a.C) {
         if (a.dbeta) a.dbeta[ch] = A;
         if (a.dgamma) a.dgamma[ch] = B;
@@ -1105,31 +1110,30 @@ __global__ __launch_bounds__(256) void group_norm_join_channels(NormArgs a)
 // Groups of very many channels, channels last (a row of a group is more than a work-group's vectors): one work-group per
 // sample and group, a pass over memory for every step, a thread to a channel
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ float block_sum(float v, float *red)
+__device__ __forceinline__ double block_sum(double v, double *red)
 {
     __syncthreads();
-    const float s = join_waves(wave_sum(v), red, (int)(blockDim.x >> 6));
-    return s;
+    return join_waves(wave_sum(v), red, (int)(blockDim.x >> 6));
 }
 
 template <typename T>
 __global__ __launch_bounds__(1024) void group_norm_wide_fwd(NormArgs a)
 {
-    __shared__ float red[16];
+    __shared__ double red[16];
     const int n = fastdiv(blockIdx.x, a.div_groups), c0 = (blockIdx.x - n * a.groups) * a.cpg;
     const T *x = static_cast<const T *>(a.x) + (int64_t)n * a.S * a.C;
     T *y = static_cast<T *>(a.out) + (int64_t)n * a.S * a.C;
-    float s = 0.f;
+    double s = 0.;
     for (int r = 0; r < a.S; ++r)
         for (int c = c0 + threadIdx.x; c < c0 + a.cpg; c += blockDim.x) s += ld_elem(x, r * a.C + c);
-    const float mean = block_sum(s, red) * a.inv_m;
-    s = 0.f;
+    const float mean = (float)(block_sum(s, red) * a.inv_m64);
+    s = 0.;
     for (int r = 0; r < a.S; ++r)
         for (int c = c0 + threadIdx.x; c < c0 + a.cpg; c += blockDim.x) {
-            const float d = ld_elem(x, r * a.C + c) - mean;
-            s += d * d;
+            const double d = ld_elem(x, r * a.C + c) - mean;
+            s = fma(d, d, s);
         }
-    const float rstd = 1.f / sqrtf(block_sum(s, red) * a.inv_m + a.eps);
+    const float rstd = 1.f / sqrtf((float)(block_sum(s, red) * a.inv_m64) + a.eps);
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[blockIdx.x] = mean;
         if (a.rstd) a.rstd[blockIdx.x] = rstd;
@@ -1147,36 +1151,36 @@ __global__ __launch_bounds__(1024) void group_norm_wide_fwd(NormArgs a)
 template <typename T>
 __global__ __launch_bounds__(1024) void group_norm_wide_bwd(NormArgs a)
 {
-    __shared__ float red[16];
+    __shared__ double red[16];
     const int n = fastdiv(blockIdx.x, a.div_groups), c0 = (blockIdx.x - n * a.groups) * a.cpg;
     const T *x = static_cast<const T *>(a.x) + (int64_t)n * a.S * a.C, *dy = static_cast<const T *>(a.dy) + (int64_t)n * a.S * a.C;
     T *dx = static_cast<T *>(a.out) + (int64_t)n * a.S * a.C;
     const float mean = a.mean[blockIdx.x], rstd = a.rstd[blockIdx.x];
-    float m1 = 0.f, m2 = 0.f;
+    double m1 = 0., m2 = 0.;
     for (int c = c0 + threadIdx.x; c < c0 + a.cpg; c += blockDim.x) {
         const float gamma = a.gamma ? a.gamma[c] : 1.f, beta = a.beta ? a.beta[c] : 0.f, scale = rstd * gamma;
-        float A = 0.f, B = 0.f;
+        double A = 0., B = 0.;
         for (int r = 0; r < a.S; ++r) {
             const float d[1] = {ld_elem(x, r * a.C + c) - mean};
             float dz[1] = {ld_elem(dy, r * a.C + c)};
             act_bwd(dz, d, a.act, [&](int) { return scale; }, [&](int) { return beta; });
             A += dz[0];
-            B += dz[0] * (d[0] * rstd);
+            B = fma((double)dz[0], (double)d[0], B);
         }
-        a.part[(int64_t)n * a.C + c] = A;
-        a.part[((int64_t)a.part_rows + n) * a.C + c] = B;
+        B *= rstd;
+        a.part[(int64_t)n * a.C + c] = (float)A;
+        a.part[((int64_t)a.part_rows + n) * a.C + c] = (float)B;
         m1 += gamma * A;
         m2 += gamma * B;
     }
-    m1 = block_sum(m1, red) * a.inv_m;
-    m2 = block_sum(m2, red) * a.inv_m;
+    const float mean1 = (float)(block_sum(m1, red) * a.inv_m64), mean2 = (float)(block_sum(m2, red) * a.inv_m64);
     for (int c = c0 + threadIdx.x; c < c0 + a.cpg; c += blockDim.x) {
         const float gamma = a.gamma ? a.gamma[c] : 1.f, beta = a.beta ? a.beta[c] : 0.f, scale = rstd * gamma;
         for (int r = 0; r < a.S; ++r) {
             const float d[1] = {ld_elem(x, r * a.C + c) - mean};
             float dz[1] = {ld_elem(dy, r * a.C + c)};
             act_bwd(dz, d, a.act, [&](int) { return scale; }, [&](int) { return beta; });
-            st_elem(dx, r * a.C + c, rstd * (gamma * dz[0] - m1 - d[0] * rstd * m2));
+            st_elem(dx, r * a.C + c, rstd * (gamma * dz[0] - mean1 - d[0] * rstd * mean2));
         }
     }
 }

@@ -430,3 +430,53 @@ def test_the_longest_plane():
         left = rstd.double().item() * (y[0, 0, 0, at].double() - dbeta.item() / S - want * dgamma.item() / S)
         assert bool(((dx[0, 0, 0, at].double() - left).abs() <= 2.0 ** -8 * left.abs() + 16 * U * (1 + want.abs())).all())
     assert abs(dgamma.item() / S - 1) <= 2.0 ** -8 and abs(dbeta.item() / S) <= 2.0 ** -8
+
+
+@pytest.mark.parametrize("layout,shape", [("last", (1, 4104, 64, 64, 1)), ("last", (1, 8200, 40, 40, 1)), ("planes", (1, 12, 90, 91, 3)),
+                                          ("last", (200000, 4, 1, 1, 2)), ("planes", (30000, 3, 1, 5, 3))])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_long_sums_of_like_terms(shape, layout, dtype):
+    """Terms of one sign and size, whose roundings in a long fp32 chain all go the same way (a chain of 10^4 of 0.1: 10^3 u):
+    the bounds of a few hundred hold for very wide groups and for many samples as well."""
+    N, C, H, W, G = shape
+    g = np.random.Generator(np.random.Philox(40))
+    x = 0.1 + 1e-3 * g.standard_normal((N, C, H * W))
+    dy = np.full((N, C, H * W), 0.1) + 1e-4 * (g.random((N, C, H * W)) < 0.01)
+    gamma, beta = np.ones(C, np.float32), np.zeros(C, np.float32)
+    rnd = oracle.bf16_round if dtype == "bf16" else (lambda a: a)
+    x, dy = (rnd(v.astype(np.float32)).astype(np.float64) for v in (x, dy))
+    xd, dyd = (_dev(v.reshape(N, C, H, W), layout, dtype) for v in (x, dy))
+    got = hp.group_norm_act_fwd(xd, G, _cuda(gamma), _cuda(beta), act="none")
+    check_fwd(got, x, G, gamma, beta, 1e-5, "none", dtype)
+    m, r = (v.astype(np.float32).astype(np.float64) for v in oracle.group_norm_stats(x, G, 1e-5))
+    got = hp.group_norm_act_bwd(xd, dyd, _cuda(m), _cuda(r), _cuda(gamma), _cuda(beta), act="none")
+    check_bwd(got, x, dy, m, r, gamma, beta, "none", dtype)
+
+
+@pytest.mark.parametrize("layout", ["planes", "last"])
+def test_gradient_means_of_millions_of_channels(layout):
+    """dy with a mean and a share of xh, so that dx takes off two terms of the size of dy itself: rstd (64 u of the terms'
+    mean magnitudes, 0.8 and 0.8 |xh| with |xh| below 6, and 8 u of what is subtracted) is below 4e-5."""
+    C, S = (1 << 22) + 1500, 2
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn((1, C, 1, S), device="cuda", generator=g)
+    if layout == "last":
+        x = x.contiguous(memory_format=torch.channels_last)
+    y, mean, rstd = hp.group_norm_act_fwd(x, 1, act="none")
+    xd = x.double()
+    m, r = mean.double().item(), rstd.double().item()
+    assert abs(m - xd.mean().item()) <= 64 * U and abs(r * (xd.var(correction=0).item() + 1e-5) ** 0.5 - 1) <= 64 * U
+    xh = (xd - m) * r
+    dy = (0.3 + 0.5 * xh + 0.2 * torch.randn(x.shape, device="cuda", generator=g, dtype=torch.float64)).float()
+    dy = dy.contiguous(memory_format=torch.channels_last) if layout == "last" else dy.contiguous()
+    dx, dgamma, dbeta = hp.group_norm_act_bwd(x, dy, mean, rstd, act="none")
+    dyd = dy.double()
+    m1, m2 = dyd.mean().item(), (dyd * xh).mean().item()
+    assert m1 > 0.25 and m2 > 0.4
+    assert float((dx - r * (dyd - m1 - xh * m2)).abs().max()) <= 4e-5
+    assert float((dbeta - dyd.sum((0, 2, 3))).abs().max()) <= 1e-6 and float((dgamma - (dyd * xh).sum((0, 2, 3))).abs().max()) <= 2e-5
+    # like terms: what is left of 0.1 - m1 is the error of m1 (xh's share: of sums of both signs)
+    one = torch.full_like(x, 0.1)
+    left = hp.group_norm_act_bwd(x, one, mean, rstd, act="none")[0].double()
+    ref = 0.1 * (xh.mean().item() * xh)
+    assert float((left + r * ref).abs().max()) <= r * (64 * U * 0.1 * (1 + 6 * 0.8) + 8 * U * 0.3)

@@ -187,7 +187,9 @@ def _dtype_of(t):
 
 
 class Workspace:
-    """A growable device scratch buffer handed to the library as `ws`."""
+    """A growable device scratch buffer handed to the library as `ws`: for the calls of one stream and one thread (calls
+    that overlap would take their sums from each other), and, where a call is captured in a graph, grown to its size
+    before that."""
 
     def __init__(self, device="cuda"):
         self.device = device
@@ -201,21 +203,36 @@ class Workspace:
         return self.buf, self.buf.numel()
 
 
-_default_ws = None
+class _CallScratch:
+    """Scratch of a call without a `ws`: its own, from PyTorch's allocator, on the stream that the call runs on, so that the
+    memory can be given out again when that stream has passed the call (1.2 us a call).  The caller holds the buffer until
+    the library has returned."""
+    __slots__ = ("stream",)
+
+    def __init__(self, stream):
+        self.stream = stream
+
+    def get(self, nbytes):
+        if nbytes == 0:
+            return None, 0
+        if self.stream is None:
+            return torch.empty(nbytes, dtype=torch.uint8, device="cuda"), nbytes
+        with torch.cuda.stream(self.stream):
+            return torch.empty(nbytes, dtype=torch.uint8, device="cuda"), nbytes
 
 
-def _ws(ws):
-    global _default_ws
+_on_current_stream = _CallScratch(None)
+
+
+def _ws(ws, stream):
     if ws is not None:
         return ws
-    if _default_ws is None:
-        _default_ws = Workspace()
-    return _default_ws
+    return _on_current_stream if stream is None else _CallScratch(stream)
 
 
 def _run(name, op, a, b, out, dims, x_bs, y_bs, dtype, ws, stream):
     need = _workspace_bytes(op, *dims, dtype)
-    buf, nbytes = _ws(ws).get(need)
+    buf, nbytes = _ws(ws, stream).get(need)
     wsp = buf.data_ptr() if buf is not None else 0
     if x_bs or y_bs:
         rc = getattr(lib(), name + "_ex")(_ptr(a), _ptr(b), _ptr(out), *dims, int(x_bs), int(y_bs), dtype,
@@ -302,7 +319,7 @@ def conv_fwd_bias_relu(x, w, bias, stride, pad, relu=True, y=None, ws=None, stre
     _dense(x, w, bias, y)
     dims = (N, C, H, W, K, R, S, stride, pad)
     dtype = _io_dtype(x, y)
-    buf, nbytes = _ws(ws).get(_workspace_bytes(OP_FWD, *dims, dtype))
+    buf, nbytes = _ws(ws, stream).get(_workspace_bytes(OP_FWD, *dims, dtype))
     wsp = buf.data_ptr() if buf is not None else 0
     bp = _ptr(bias) if bias is not None else 0
     rc = lib().conv_fwd_bias_relu(_ptr(x), _ptr(w), bp, _ptr(y), *dims, 1 if relu else 0, dtype, wsp, nbytes,
@@ -328,7 +345,7 @@ def conv_bwd_data_relu(dy, w, act, stride, pad, dx=None, ws=None, stream=None):
     _dense(dy, w, act, dx)
     dims = (N, C, H, W, K, R, S, stride, pad)
     dtype = _io_dtype(dy, dx)
-    buf, nbytes = _ws(ws).get(_workspace_bytes(OP_BWD_DATA, *dims, dtype))
+    buf, nbytes = _ws(ws, stream).get(_workspace_bytes(OP_BWD_DATA, *dims, dtype))
     wsp = buf.data_ptr() if buf is not None else 0
     rc = lib().conv_bwd_data_relu(_ptr(dy), _ptr(w), _ptr(act), _ptr(dx), *dims, dtype, wsp, nbytes,
                                   _stream_handle(stream))
@@ -370,7 +387,7 @@ def _run_grouped(name, op, a, b, out, dims, groups, dtype, ws, stream):
         if not t.is_contiguous():
             raise ValueError("grouped calls take dense tensors")
     need = int(lib().conv_workspace_bytes_grouped(op, *dims, groups, dtype))
-    buf, nbytes = _ws(ws).get(need)
+    buf, nbytes = _ws(ws, stream).get(need)
     wsp = buf.data_ptr() if buf is not None else 0
     rc = getattr(lib(), name)(_ptr(a), _ptr(b), _ptr(out), *dims, groups, dtype, wsp, nbytes, _stream_handle(stream))
     if rc != OK:
@@ -494,7 +511,7 @@ def bias_bwd(dy, db=None, ws=None, stream=None):
         raise ValueError("bias_bwd takes a dense dy")
     if db is None:
         db = torch.empty((K,), dtype=torch.float32, device=dy.device)
-    buf, nbytes = _ws(ws).get(int(lib().bias_bwd_workspace_bytes(N, K)))
+    buf, nbytes = _ws(ws, stream).get(int(lib().bias_bwd_workspace_bytes(N, K)))
     _check(lib().bias_bwd(_ptr(dy), _ptr(db), N, K, P * Q, _dtype_of(dy), ctypes.c_void_p(buf.data_ptr()), nbytes,
                           _stream_handle(stream)), "bias_bwd")
     return db
@@ -510,9 +527,10 @@ def convert_f32_to_bf16(src, dst=None, stream=None):
     return dst
 
 
-def _fc_ws(op, N, I, O, ws):
-    buf, nbytes = _ws(ws).get(int(lib().fc_workspace_bytes(op, N, I, O, DTYPE_F32)))
-    return (buf.data_ptr() if buf is not None else 0), nbytes
+def _fc_ws(op, N, I, O, ws, stream):
+    """(buffer, its address, its size)"""
+    buf, nbytes = _ws(ws, stream).get(int(lib().fc_workspace_bytes(op, N, I, O, DTYPE_F32)))
+    return buf, (buf.data_ptr() if buf is not None else 0), nbytes
 
 
 def fc_fwd(x, w, bias=None, relu=False, y=None, ws=None, stream=None):
@@ -524,7 +542,7 @@ def fc_fwd(x, w, bias=None, relu=False, y=None, ws=None, stream=None):
     if y is None:
         y = torch.empty((N, O), dtype=torch.float32, device=x.device)
     _dense(x, w, bias, y)
-    wsp, nbytes = _fc_ws(OP_FWD, N, I, O, ws)
+    buf, wsp, nbytes = _fc_ws(OP_FWD, N, I, O, ws, stream)
     bp = _ptr(bias) if bias is not None else 0
     _check(lib().fc_fwd(_ptr(x), _ptr(w), bp, _ptr(y), N, I, O, 1 if relu else 0, _dtype_of(x), wsp, nbytes,
                         _stream_handle(stream)), "fc_fwd")
@@ -540,7 +558,7 @@ def fc_bwd_data(dy, w, dx=None, ws=None, stream=None):
     if dx is None:
         dx = torch.empty((N, I), dtype=torch.float32, device=dy.device)
     _dense(dy, w, dx)
-    wsp, nbytes = _fc_ws(OP_BWD_DATA, N, I, O, ws)
+    buf, wsp, nbytes = _fc_ws(OP_BWD_DATA, N, I, O, ws, stream)
     _check(lib().fc_bwd_data(_ptr(dy), _ptr(w), _ptr(dx), N, I, O, _dtype_of(dy), wsp, nbytes,
                              _stream_handle(stream)), "fc_bwd_data")
     return dx
@@ -555,7 +573,7 @@ def fc_bwd_filter(x, dy, dw=None, ws=None, stream=None):
     if dw is None:
         dw = torch.empty((O, I), dtype=torch.float32, device=x.device)
     _dense(x, dy, dw)
-    wsp, nbytes = _fc_ws(OP_BWD_FILTER, N, I, O, ws)
+    buf, wsp, nbytes = _fc_ws(OP_BWD_FILTER, N, I, O, ws, stream)
     _check(lib().fc_bwd_filter(_ptr(x), _ptr(dy), _ptr(dw), N, I, O, _dtype_of(x), wsp, nbytes,
                                _stream_handle(stream)), "fc_bwd_filter")
     return dw
@@ -679,7 +697,7 @@ def group_norm_act_fwd(x, groups, gamma=None, beta=None, eps=1e-5, act="relu", y
         mp, rp = _dense_f32(mean, per, d, "mean"), _dense_f32(rstd, per, d, "rstd")
     need, wsp = _norm_workspace_bytes(OP_FWD, N, C, H * W, groups, layout, dtype), 0
     if need:
-        buf, need = _ws(ws).get(need)
+        buf, need = _ws(ws, stream).get(need)
         wsp = buf.data_ptr()
     rc = lib().group_norm_act_fwd(x.data_ptr(), gp, bp, y.data_ptr(), mp, rp, N, C, H * W, groups, eps, code, layout, dtype,
                                   wsp, need, _current_stream(stream))
@@ -716,7 +734,7 @@ def group_norm_act_bwd(x, dy, mean, rstd, gamma=None, beta=None, act="relu", dx=
     dgp, dbp = _dense_f32(dgamma, chan, d, "dgamma"), _dense_f32(dbeta, chan, d, "dbeta")
     need, wsp = _norm_workspace_bytes(OP_BWD_DATA, N, C, H * W, groups, layout, dtype), 0
     if need:
-        buf, need = _ws(ws).get(need)
+        buf, need = _ws(ws, stream).get(need)
         wsp = buf.data_ptr()
     rc = lib().group_norm_act_bwd(x.data_ptr(), dy.data_ptr(), gp, bp, mp, rp, dx.data_ptr(), dgp, dbp, N, C, H * W, groups,
                                   code, layout, dtype, wsp, need, _current_stream(stream))
@@ -792,7 +810,7 @@ def distill_loss_fwd(z, labels=None, top_idx=None, top_val=None, temperature=1.0
     op, sp = _dense_f32(loss, (N,), d, "loss"), _dense_f32(stats, (N, 3), d, "stats")
     need, wsp = _loss_workspace_bytes(N, V, K, dtype), 0
     if need:
-        buf, need = _ws(ws).get(need)
+        buf, need = _ws(ws, stream).get(need)
         wsp = buf.data_ptr()
     rc = lib().distill_loss_fwd(z.data_ptr(), zs, lp, ip, vp, op, sp, N, V, K, temperature, kd_weight, label_weight, ib, td,
                                 dtype, wsp, need, _current_stream(stream))
@@ -832,7 +850,7 @@ def distill_loss_fwd_bwd(z, labels=None, top_idx=None, top_val=None, temperature
     gp = 0 if grad is None else _dense_f32(grad, (N,), d, "grad")
     need, wsp = _loss_workspace_bytes(N, V, K, dtype), 0
     if need:
-        buf, need = _ws(ws).get(need)
+        buf, need = _ws(ws, stream).get(need)
         wsp = buf.data_ptr()
     rc = lib().distill_loss_fwd_bwd(z.data_ptr(), zs, lp, ip, vp, gp, grad_scale, op, dz.data_ptr(), dzs, N, V, K,
                                     temperature, kd_weight, label_weight, ib, td, dtype, wsp, need, _current_stream(stream))

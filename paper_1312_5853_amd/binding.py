@@ -657,9 +657,11 @@ def _new_f32(shape, like):
     return torch.empty(shape, dtype=_F32, device=like.device)
 
 
-def _current_stream(stream):
-    """_stream_handle for a call whose tensors are on a GPU, so that the GPU's state is there (1 us less)."""
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream.cuda_stream
+def _current_stream(stream, d):
+    """_stream_handle for a call whose tensors are on GPU d (whose state is there, then: 1 us less)."""
+    if torch._C._cuda_getDevice() != d or (stream is not None and stream.device_index != d):
+        raise ValueError("the tensors of a call must be on the current GPU, and its stream too")
+    return torch._C._cuda_getCurrentRawStream(d) if stream is None else stream.cuda_stream
 
 
 def _channels_last(*tensors):
@@ -700,7 +702,7 @@ def group_norm_act_fwd(x, groups, gamma=None, beta=None, eps=1e-5, act="relu", y
         buf, need = _ws(ws, stream).get(need)
         wsp = buf.data_ptr()
     rc = lib().group_norm_act_fwd(x.data_ptr(), gp, bp, y.data_ptr(), mp, rp, N, C, H * W, groups, eps, code, layout, dtype,
-                                  wsp, need, _current_stream(stream))
+                                  wsp, need, _current_stream(stream, d))
     if rc != OK:
         raise ConvError(rc, "group_norm_act_fwd")
     return y, mean, rstd
@@ -737,7 +739,7 @@ def group_norm_act_bwd(x, dy, mean, rstd, gamma=None, beta=None, act="relu", dx=
         buf, need = _ws(ws, stream).get(need)
         wsp = buf.data_ptr()
     rc = lib().group_norm_act_bwd(x.data_ptr(), dy.data_ptr(), gp, bp, mp, rp, dx.data_ptr(), dgp, dbp, N, C, H * W, groups,
-                                  code, layout, dtype, wsp, need, _current_stream(stream))
+                                  code, layout, dtype, wsp, need, _current_stream(stream, d))
     if rc != OK:
         raise ConvError(rc, "group_norm_act_bwd")
     return dx, dgamma, dbeta
@@ -813,7 +815,7 @@ def distill_loss_fwd(z, labels=None, top_idx=None, top_val=None, temperature=1.0
         buf, need = _ws(ws, stream).get(need)
         wsp = buf.data_ptr()
     rc = lib().distill_loss_fwd(z.data_ptr(), zs, lp, ip, vp, op, sp, N, V, K, temperature, kd_weight, label_weight, ib, td,
-                                dtype, wsp, need, _current_stream(stream))
+                                dtype, wsp, need, _current_stream(stream, d))
     if rc != OK:
         raise ConvError(rc, "distill_loss_fwd")
     return loss, stats
@@ -831,7 +833,7 @@ def distill_loss_bwd(z, stats, labels=None, top_idx=None, top_val=None, temperat
     gp = 0 if grad is None else _dense_f32(grad, (N,), d, "grad")
     sp = _dense_f32(stats, (N, 3), d, "stats")
     rc = lib().distill_loss_bwd(z.data_ptr(), zs, lp, ip, vp, sp, gp, grad_scale, dz.data_ptr(), dzs, N, V, K, temperature,
-                                kd_weight, label_weight, ib, td, dtype, _current_stream(stream))
+                                kd_weight, label_weight, ib, td, dtype, _current_stream(stream, d))
     if rc != OK:
         raise ConvError(rc, "distill_loss_bwd")
     return dz
@@ -853,7 +855,7 @@ def distill_loss_fwd_bwd(z, labels=None, top_idx=None, top_val=None, temperature
         buf, need = _ws(ws, stream).get(need)
         wsp = buf.data_ptr()
     rc = lib().distill_loss_fwd_bwd(z.data_ptr(), zs, lp, ip, vp, gp, grad_scale, op, dz.data_ptr(), dzs, N, V, K,
-                                    temperature, kd_weight, label_weight, ib, td, dtype, wsp, need, _current_stream(stream))
+                                    temperature, kd_weight, label_weight, ib, td, dtype, wsp, need, _current_stream(stream, d))
     if rc != OK:
         raise ConvError(rc, "distill_loss_fwd_bwd")
     return loss, dz

@@ -257,3 +257,18 @@ def test_the_longest_plane(lib, dtype, per_tile):
         need = lib.group_norm_act_workspace_bytes(b.OP_BWD_DATA, 1, 1, S, 1, 0, dtype)
         assert need == -(-8 * tiles // 256) * 256 + 256
         assert lib.group_norm_act_bwd(*_norm_bwd_args(N=1, C=1, S=S, groups=1, dtype=dtype, ws_bytes=need - 1)) == b.ERR_WORKSPACE
+
+
+def test_tensors_of_another_gpu_than_the_current_one(monkeypatch):
+    """A launch goes to the current GPU, whose kernels may not reach another one's memory."""
+    from paper_1312_5853_amd import binding as b
+
+    class Stream:
+        device_index, cuda_stream = 1, 77
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: 55 + d, raising=False)
+    assert b._current_stream(None, 1) == 56 and b._current_stream(Stream, 1) == 77
+    for stream, d in ((None, 0), (Stream, 0), (type("S", (Stream,), dict(device_index=0)), 1)):
+        with pytest.raises(ValueError):
+            b._current_stream(stream, d)

@@ -205,8 +205,8 @@ class Workspace:
 
 class _CallScratch:
     """Scratch of a call without a `ws`: its own, from PyTorch's allocator, on the stream that the call runs on, so that the
-    memory can be given out again when that stream has passed the call (1.2 us a call).  The caller holds the buffer until
-    the library has returned."""
+    memory can be given out again when that stream has passed the call.  The caller holds the buffer until the library has
+    returned."""
     __slots__ = ("stream",)
 
     def __init__(self, stream):
@@ -664,6 +664,11 @@ def _current_stream(stream, d):
     return torch._C._cuda_getCurrentRawStream(d) if stream is None else stream.cuda_stream
 
 
+# Scratch of a call without a `ws`, as _CallScratch has it, without a tensor around it (0.5 us instead of 1.2)
+_take_scratch = torch._C._cuda_cudaCachingAllocator_raw_alloc
+_give_scratch = torch._C._cuda_cudaCachingAllocator_raw_delete
+
+
 def _channels_last(*tensors):
     for t in tensors:
         if not t.is_contiguous(memory_format=torch.channels_last):
@@ -698,11 +703,19 @@ def group_norm_act_fwd(x, groups, gamma=None, beta=None, eps=1e-5, act="relu", y
         rstd = _new_f32(per, x) if rstd is None else rstd
         mp, rp = _dense_f32(mean, per, d, "mean"), _dense_f32(rstd, per, d, "rstd")
     need, wsp = _norm_workspace_bytes(OP_FWD, N, C, H * W, groups, layout, dtype), 0
+    handle, own = _current_stream(stream, d), 0
     if need:
-        buf, need = _ws(ws, stream).get(need)
-        wsp = buf.data_ptr()
-    rc = lib().group_norm_act_fwd(x.data_ptr(), gp, bp, y.data_ptr(), mp, rp, N, C, H * W, groups, eps, code, layout, dtype,
-                                  wsp, need, _current_stream(stream, d))
+        if ws is None:
+            own = wsp = _take_scratch(need, handle)
+        else:
+            buf, need = ws.get(need)
+            wsp = buf.data_ptr()
+    try:
+        rc = lib().group_norm_act_fwd(x.data_ptr(), gp, bp, y.data_ptr(), mp, rp, N, C, H * W, groups, eps, code, layout, dtype,
+                                      wsp, need, handle)
+    finally:
+        if own:
+            _give_scratch(own)
     if rc != OK:
         raise ConvError(rc, "group_norm_act_fwd")
     return y, mean, rstd
@@ -735,11 +748,19 @@ def group_norm_act_bwd(x, dy, mean, rstd, gamma=None, beta=None, act="relu", dx=
     dbeta = _new_f32(chan, x) if dbeta is None else dbeta
     dgp, dbp = _dense_f32(dgamma, chan, d, "dgamma"), _dense_f32(dbeta, chan, d, "dbeta")
     need, wsp = _norm_workspace_bytes(OP_BWD_DATA, N, C, H * W, groups, layout, dtype), 0
+    handle, own = _current_stream(stream, d), 0
     if need:
-        buf, need = _ws(ws, stream).get(need)
-        wsp = buf.data_ptr()
-    rc = lib().group_norm_act_bwd(x.data_ptr(), dy.data_ptr(), gp, bp, mp, rp, dx.data_ptr(), dgp, dbp, N, C, H * W, groups,
-                                  code, layout, dtype, wsp, need, _current_stream(stream, d))
+        if ws is None:
+            own = wsp = _take_scratch(need, handle)
+        else:
+            buf, need = ws.get(need)
+            wsp = buf.data_ptr()
+    try:
+        rc = lib().group_norm_act_bwd(x.data_ptr(), dy.data_ptr(), gp, bp, mp, rp, dx.data_ptr(), dgp, dbp, N, C, H * W, groups,
+                                      code, layout, dtype, wsp, need, handle)
+    finally:
+        if own:
+            _give_scratch(own)
     if rc != OK:
         raise ConvError(rc, "group_norm_act_bwd")
     return dx, dgamma, dbeta
@@ -811,11 +832,19 @@ def distill_loss_fwd(z, labels=None, top_idx=None, top_val=None, temperature=1.0
     stats = _new_f32((N, 3), z) if stats is None else stats
     op, sp = _dense_f32(loss, (N,), d, "loss"), _dense_f32(stats, (N, 3), d, "stats")
     need, wsp = _loss_workspace_bytes(N, V, K, dtype), 0
+    handle, own = _current_stream(stream, d), 0
     if need:
-        buf, need = _ws(ws, stream).get(need)
-        wsp = buf.data_ptr()
-    rc = lib().distill_loss_fwd(z.data_ptr(), zs, lp, ip, vp, op, sp, N, V, K, temperature, kd_weight, label_weight, ib, td,
-                                dtype, wsp, need, _current_stream(stream, d))
+        if ws is None:
+            own = wsp = _take_scratch(need, handle)
+        else:
+            buf, need = ws.get(need)
+            wsp = buf.data_ptr()
+    try:
+        rc = lib().distill_loss_fwd(z.data_ptr(), zs, lp, ip, vp, op, sp, N, V, K, temperature, kd_weight, label_weight, ib, td,
+                                    dtype, wsp, need, handle)
+    finally:
+        if own:
+            _give_scratch(own)
     if rc != OK:
         raise ConvError(rc, "distill_loss_fwd")
     return loss, stats
@@ -851,11 +880,19 @@ def distill_loss_fwd_bwd(z, labels=None, top_idx=None, top_val=None, temperature
     op = _dense_f32(loss, (N,), d, "loss")
     gp = 0 if grad is None else _dense_f32(grad, (N,), d, "grad")
     need, wsp = _loss_workspace_bytes(N, V, K, dtype), 0
+    handle, own = _current_stream(stream, d), 0
     if need:
-        buf, need = _ws(ws, stream).get(need)
-        wsp = buf.data_ptr()
-    rc = lib().distill_loss_fwd_bwd(z.data_ptr(), zs, lp, ip, vp, gp, grad_scale, op, dz.data_ptr(), dzs, N, V, K,
-                                    temperature, kd_weight, label_weight, ib, td, dtype, wsp, need, _current_stream(stream, d))
+        if ws is None:
+            own = wsp = _take_scratch(need, handle)
+        else:
+            buf, need = ws.get(need)
+            wsp = buf.data_ptr()
+    try:
+        rc = lib().distill_loss_fwd_bwd(z.data_ptr(), zs, lp, ip, vp, gp, grad_scale, op, dz.data_ptr(), dzs, N, V, K,
+                                        temperature, kd_weight, label_weight, ib, td, dtype, wsp, need, handle)
+    finally:
+        if own:
+            _give_scratch(own)
     if rc != OK:
         raise ConvError(rc, "distill_loss_fwd_bwd")
     return loss, dz

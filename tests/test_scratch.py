@@ -53,9 +53,12 @@ def test_calls_that_overlap_share_no_scratch(name, monkeypatch):
         monkeypatch.setattr(hp, "_norm_workspace_bytes", lambda *a: 4096)
         monkeypatch.setattr(hp, "_loss_workspace_bytes", lambda *a: 4096)
         monkeypatch.setattr(torch, "empty", lambda *a, **k: _empty(*a, **dict(k, device="cpu")))
+        held = {}
+        monkeypatch.setattr(hp, "_take_scratch", lambda n, stream: held.setdefault((t := _empty(n, dtype=torch.uint8)).data_ptr(), t).data_ptr())
+        monkeypatch.setattr(hp, "_give_scratch", held.pop)
         _calls()[name]()
         first, second = lib.seen
-        assert first and second and abs(first - second) >= 4096
+        assert first and second and abs(first - second) >= 4096 and not held
 
 
 def _norm_case(seed, N):

@@ -272,3 +272,59 @@ def test_tensors_of_another_gpu_than_the_current_one(monkeypatch):
     for stream, d in ((None, 0), (Stream, 0), (type("S", (Stream,), dict(device_index=0)), 1)):
         with pytest.raises(ValueError):
             b._current_stream(stream, d)
+
+
+def test_the_oracle_against_loops():
+    """Both operators written out value by value, from the definitions, on sizes with several groups and entries."""
+    g = RNG(9)
+    N, C, S, G, eps = 2, 6, 5, 3, 1e-2
+    x, dy = g.normal(size=(N, C, S)).tolist(), g.normal(size=(N, C, S)).tolist()
+    gamma, beta = g.normal(1.0, 0.3, C).tolist(), g.normal(0, 0.3, C).tolist()
+    y, dx = np.zeros((N, C, S)), np.zeros((N, C, S))
+    dgamma, dbeta = np.zeros(C), np.zeros(C)
+    means, rstds = np.zeros((N, G)), np.zeros((N, G))
+    for n in range(N):
+        for k in range(G):
+            chans = [c for c in range(C) if c // (C // G) == k]
+            M = len(chans) * S
+            m = sum(x[n][c][s] for c in chans for s in range(S)) / M
+            r = (sum((x[n][c][s] - m) ** 2 for c in chans for s in range(S)) / M + eps) ** -0.5
+            means[n, k], rstds[n, k] = m, r
+            m1 = m2 = 0.0
+            dz = {}
+            for c in chans:
+                for s in range(S):
+                    xh = (x[n][c][s] - m) * r
+                    z = gamma[c] * xh + beta[c]
+                    sig = 1 / (1 + np.exp(-z))
+                    y[n, c, s] = z * sig
+                    dz[c, s] = dy[n][c][s] * (sig + z * sig * (1 - sig))
+                    dgamma[c] += dz[c, s] * xh
+                    dbeta[c] += dz[c, s]
+                    m1 += gamma[c] * dz[c, s] / M
+                    m2 += gamma[c] * dz[c, s] * xh / M
+            for c in chans:
+                for s in range(S):
+                    dx[n, c, s] = r * (gamma[c] * dz[c, s] - m1 - (x[n][c][s] - m) * r * m2)
+    got = oracle.group_norm_act_fwd(np.array(x), G, gamma, beta, eps, "silu")
+    assert all(np.abs(a - b).max() < 1e-13 for a, b in zip(got, (y, means, rstds)))
+    got = oracle.group_norm_act_bwd(np.array(x), np.array(dy), means, rstds, gamma, beta, "silu")
+    assert all(np.abs(a - b).max() < 1e-13 for a, b in zip(got, (dx, dgamma, dbeta)))
+    V, T, wk, wl = 7, 1.6, 0.7, 0.3
+    z, lab, w = g.normal(size=(4, V)), [2, -1, 6, 7], [1.0, 0.5, -2.0, 3.0]
+    idx, val = [[1, 1, -1], [0, 6, 3], [9, -2, 5], [-1, 7, -1]], g.normal(size=(4, 3))
+    loss, dz = np.zeros(4), np.zeros((4, V))
+    for n in range(4):
+        held = [k for k in range(3) if 0 <= idx[n][k] < V]
+        e = {k: np.exp(val[n, k] / T) for k in held}
+        for t, weight, targets in ((T, wk * T * T, {k: (idx[n][k], e[k] / sum(e.values())) for k in held}),
+                                   (1.0, wl, {0: (lab[n], 1.0)} if 0 <= lab[n] < V else {})):
+            total = sum(np.exp(z[n, v] / t) for v in range(V))
+            for v, p in targets.values():
+                loss[n] += weight * p * (np.log(p) - z[n, v] / t + np.log(total))
+                dz[n, v] -= w[n] * weight / t * p
+            if targets:
+                for v in range(V):
+                    dz[n, v] += w[n] * weight / t * np.exp(z[n, v] / t) / total
+    got = oracle.distill_loss(z, np.array(lab), np.array(idx), val, T, wk, wl, w)
+    assert np.abs(got[0] - loss).max() < 1e-13 and np.abs(got[1] - dz).max() < 1e-13

@@ -203,36 +203,37 @@ class Workspace:
         return self.buf, self.buf.numel()
 
 
-class _CallScratch:
-    """Scratch of a call without a `ws`: its own, from PyTorch's allocator, on the stream that the call runs on, so that the
-    memory can be given out again when that stream has passed the call.  The caller holds the buffer until the library has
-    returned."""
-    __slots__ = ("stream",)
-
-    def __init__(self, stream):
-        self.stream = stream
-
-    def get(self, nbytes):
-        if nbytes == 0:
-            return None, 0
-        if self.stream is None:
-            return torch.empty(nbytes, dtype=torch.uint8, device="cuda"), nbytes
-        with torch.cuda.stream(self.stream):
-            return torch.empty(nbytes, dtype=torch.uint8, device="cuda"), nbytes
+# Scratch of a call without a `ws` is its own, from PyTorch's allocator, on the stream that the call runs on, so that the
+# memory can be given out again when that stream has passed the call; it is held until the library has returned.
+_take_scratch = torch._C._cuda_cudaCachingAllocator_raw_alloc
+_give_scratch = torch._C._cuda_cudaCachingAllocator_raw_delete
 
 
-_on_current_stream = _CallScratch(None)
+class _Scratch:
+    __slots__ = ("at",)
+
+    def __init__(self, nbytes, handle):
+        self.at = 0
+        self.at = _take_scratch(nbytes, handle)
+
+    def data_ptr(self):
+        return self.at
+
+    def __del__(self):
+        if self.at:
+            _give_scratch(self.at)
 
 
-def _ws(ws, stream):
-    if ws is not None:
-        return ws
-    return _on_current_stream if stream is None else _CallScratch(stream)
+def _scratch(ws, nbytes, stream):
+    """(buffer, its size) for a call that needs so many bytes: of `ws`, or one of its own; (None, 0) for none."""
+    if nbytes == 0:
+        return None, 0
+    return ws.get(nbytes) if ws is not None else (_Scratch(nbytes, _stream_handle(stream)), nbytes)
 
 
 def _run(name, op, a, b, out, dims, x_bs, y_bs, dtype, ws, stream):
     need = _workspace_bytes(op, *dims, dtype)
-    buf, nbytes = _ws(ws, stream).get(need)
+    buf, nbytes = _scratch(ws, need, stream)
     wsp = buf.data_ptr() if buf is not None else 0
     if x_bs or y_bs:
         rc = getattr(lib(), name + "_ex")(_ptr(a), _ptr(b), _ptr(out), *dims, int(x_bs), int(y_bs), dtype,
@@ -319,7 +320,7 @@ def conv_fwd_bias_relu(x, w, bias, stride, pad, relu=True, y=None, ws=None, stre
     _dense(x, w, bias, y)
     dims = (N, C, H, W, K, R, S, stride, pad)
     dtype = _io_dtype(x, y)
-    buf, nbytes = _ws(ws, stream).get(_workspace_bytes(OP_FWD, *dims, dtype))
+    buf, nbytes = _scratch(ws, _workspace_bytes(OP_FWD, *dims, dtype), stream)
     wsp = buf.data_ptr() if buf is not None else 0
     bp = _ptr(bias) if bias is not None else 0
     rc = lib().conv_fwd_bias_relu(_ptr(x), _ptr(w), bp, _ptr(y), *dims, 1 if relu else 0, dtype, wsp, nbytes,
@@ -345,7 +346,7 @@ def conv_bwd_data_relu(dy, w, act, stride, pad, dx=None, ws=None, stream=None):
     _dense(dy, w, act, dx)
     dims = (N, C, H, W, K, R, S, stride, pad)
     dtype = _io_dtype(dy, dx)
-    buf, nbytes = _ws(ws, stream).get(_workspace_bytes(OP_BWD_DATA, *dims, dtype))
+    buf, nbytes = _scratch(ws, _workspace_bytes(OP_BWD_DATA, *dims, dtype), stream)
     wsp = buf.data_ptr() if buf is not None else 0
     rc = lib().conv_bwd_data_relu(_ptr(dy), _ptr(w), _ptr(act), _ptr(dx), *dims, dtype, wsp, nbytes,
                                   _stream_handle(stream))
@@ -387,7 +388,7 @@ def _run_grouped(name, op, a, b, out, dims, groups, dtype, ws, stream):
         if not t.is_contiguous():
             raise ValueError("grouped calls take dense tensors")
     need = int(lib().conv_workspace_bytes_grouped(op, *dims, groups, dtype))
-    buf, nbytes = _ws(ws, stream).get(need)
+    buf, nbytes = _scratch(ws, need, stream)
     wsp = buf.data_ptr() if buf is not None else 0
     rc = getattr(lib(), name)(_ptr(a), _ptr(b), _ptr(out), *dims, groups, dtype, wsp, nbytes, _stream_handle(stream))
     if rc != OK:
@@ -511,7 +512,7 @@ def bias_bwd(dy, db=None, ws=None, stream=None):
         raise ValueError("bias_bwd takes a dense dy")
     if db is None:
         db = torch.empty((K,), dtype=torch.float32, device=dy.device)
-    buf, nbytes = _ws(ws, stream).get(int(lib().bias_bwd_workspace_bytes(N, K)))
+    buf, nbytes = _scratch(ws, int(lib().bias_bwd_workspace_bytes(N, K)), stream)
     _check(lib().bias_bwd(_ptr(dy), _ptr(db), N, K, P * Q, _dtype_of(dy), ctypes.c_void_p(buf.data_ptr()), nbytes,
                           _stream_handle(stream)), "bias_bwd")
     return db
@@ -529,7 +530,7 @@ def convert_f32_to_bf16(src, dst=None, stream=None):
 
 def _fc_ws(op, N, I, O, ws, stream):
     """(buffer, its address, its size)"""
-    buf, nbytes = _ws(ws, stream).get(int(lib().fc_workspace_bytes(op, N, I, O, DTYPE_F32)))
+    buf, nbytes = _scratch(ws, int(lib().fc_workspace_bytes(op, N, I, O, DTYPE_F32)), stream)
     return buf, (buf.data_ptr() if buf is not None else 0), nbytes
 
 
@@ -616,8 +617,8 @@ def _loss_workspace_bytes(N, V, K, dtype):
     return int(lib().distill_loss_workspace_bytes(N, V, K, dtype))
 
 
-# The checks of the calls below are written out for speed: the smallest of these calls take the GPU less time than Python
-# needs for their arguments.
+# The checks of the calls below, and the handling of their scratch, are written out for speed: the smallest of these calls
+# take the GPU less time than Python needs for their arguments.
 _F32 = torch.float32
 _GLUE_CODES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16}
 
@@ -662,11 +663,6 @@ def _current_stream(stream, d):
     if torch._C._cuda_getDevice() != d or (stream is not None and stream.device_index != d):
         raise ValueError("the tensors of a call must be on the current GPU, and its stream too")
     return torch._C._cuda_getCurrentRawStream(d) if stream is None else stream.cuda_stream
-
-
-# Scratch of a call without a `ws`, as _CallScratch has it, without a tensor around it (0.5 us instead of 1.2)
-_take_scratch = torch._C._cuda_cudaCachingAllocator_raw_alloc
-_give_scratch = torch._C._cuda_cudaCachingAllocator_raw_delete
 
 
 def _channels_last(*tensors):

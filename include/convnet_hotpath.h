@@ -370,9 +370,9 @@ int sgd_update_multi(void *const *w, const void *const *dw, void *const *vel, co
  *   dx = rstd * (gamma[c] * dz - m1 - xh * m2), m1 and m2 the group's means of
  *        gamma[c] * dz and gamma[c] * dz * xh
  * `dtype` names the element type of x, y, dy and dx as for the glue layers (fp32
- * 4-byte aligned, bfloat16 2-byte aligned): values are read exactly, all
- * arithmetic is fp32, the squares are taken of distances from a mean, and a bfloat16 result is
- * rounded once.  eps > 0.  N = 0 is allowed (tensors over it may be NULL; dgamma and
+ * 4-byte aligned, bfloat16 2-byte aligned): values are read exactly, arithmetic is
+ * fp32 (long sums 64 bits), the squares are taken of distances from a mean, z is taken as
+ * (gamma * rstd) * (x - mean) + beta by both calls, and a bfloat16 result is rounded once.  eps > 0.  N = 0 is allowed (tensors over it may be NULL; dgamma and
  * dbeta become 0); C * S and N * C must stay below 2^31, N * C * S below 2^40, and
  * a launch's threads (64 to a group at least) below 2^32.
  * Outputs must not overlap inputs.  Scratch:

@@ -314,8 +314,9 @@ __device__ __forceinline__ Entries entries_at(float *lds, int K)
     return {reinterpret_cast<int *>(lds), lds + k4, lds + 2 * k4};
 }
 
-// A row's label and the first 64 entries, one to a lane.  Read before the row, as loads come back in order and what the
-// entries name is read next.
+// A row's label and the first 64 entries, one to a lane.  Asked for before the row, as loads come back in order and what the
+// entries name is read next.  (The width of an index and the type of a teacher's logit are known at run time only, and behind
+// each such branch its load is waited for: the index, and a bfloat16 teacher's logit, are there before the row is asked for.)
 struct Targets {
     int label, v;                    // classes, or -1
     float t;                         // the teacher's logit
@@ -464,6 +465,8 @@ __device__ __forceinline__ void share_sums(const LossArgs &a, typename Vec<T>::R
 // ---------------------------------------------------------------------------
 // Whole rows: loss (and statistics), and with GRAD the gradient
 // ---------------------------------------------------------------------------
+// The bound on the registers, for as many wavefronts as hide the reads, costs the instances with 8 vectors two registers (fp32
+// with a gradient four) that go to memory and back.
 template <typename T, int R, bool SOLO, bool GRAD>
 __global__ __launch_bounds__(SOLO ? 256 : 1024, GRAD ? 8 : 6) void distill_rows(LossArgs a)
 {
@@ -583,7 +586,8 @@ __global__ __launch_bounds__(256, 8) void distill_part_sums(LossArgs a)
 // With dz in z's place another part's work-group may have written over what a part's moved-back last vector reads of that
 // part; those values are dropped, and no other value is read that another work-group writes.
 // Joins the parts (or takes the statistics given).  GRAD: a work-group writes its part's gradient, and the first part's
-// also the row's loss where asked for; otherwise one work-group per row writes the loss.
+// also the row's loss where asked for; otherwise one work-group per row writes the loss.  The targets and the parts' maxima
+// and sums, which come before the row, are three trips to memory one after the other.
 template <typename T, int R, bool GRAD>
 __global__ __launch_bounds__(256, 8) void distill_part_apply(LossArgs a)
 {

@@ -69,6 +69,8 @@ __device__ __forceinline__ void act_fwd(float (&v)[V], int act, F scale, G shift
 #pragma unroll
         for (int k = 0; k < V; ++k) v[k] = v[k] < 0.f ? 0.f : v[k];           // (a NaN stays)
     } else if (act == kActSilu) {
+        // exp2's argument and the reciprocal are rounded: a relative error of about (|z| + 2) 2^-23 below zero, where y is
+        // smaller than 2^-24 |z| from z = -17 on
 #pragma unroll
         for (int k = 0; k < V; ++k) v[k] *= __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * v[k]));
     }
@@ -148,8 +150,10 @@ __device__ __forceinline__ void join_tiles(const NormArgs &a, int64_t group, int
 // ---------------------------------------------------------------------------
 // Forward 128 x 96 planes of 3025 fp32 in 32 groups 58 us, 5.1 TB/s: at the copy's rate.  One sample of 256 planes of 169: 3.7
 // us, the launch and one trip to memory.  Backward 128 x 256 planes of 729 fp32 53 us, 5.4 TB/s (part of it stays in the
-// last cache), and 4.7 us for the gradients of gamma and beta, a launch; 256 x 384 planes of 169 bfloat16 with a SiLU 27 us,
-// 3.7 TB/s: two quarter-rate operations and some 25 others to a value, and the reads do not overlap with them enough.
+// last cache), and 4.8 us for the gradients of gamma and beta, a launch.  Bfloat16 is bound by the vector units, which are
+// busy for 91 % of the cycles of CUs that hold work in backward on 256 x 384 planes of 169 with a SiLU (26 us, 3.9 TB/s; two
+// quarter-rate operations and some 25 others to a value), and for 85 % in forward with a ReLU there (18 to 20 us, 3.6 TB/s).
+// (The bound on the registers costs the sums of bfloat16 tiles one spilt register.)
 // The group, planes and units of a work-group (SOLO: of a wave; four groups to a work-group, then).
 struct PlaneTile {
     int64_t group;
@@ -530,11 +534,15 @@ __global__ __launch_bounds__(SOLO ? 256 : 1024, R <= 2 ? 8 : R <= 4 ? 5 : 4) voi
 // ---------------------------------------------------------------------------
 // Channels last
 // ---------------------------------------------------------------------------
-// Forward 128 x 256 x 27 x 27 bf16 in 32 groups 22 us, 4.3 TB/s.  4 x 256 x 112 x 112 bf16, in tiles: 8.9 us for the sums and 13.3
-// for the rest, 2.3 TB/s counting x once, 3.5 as it is read.  Backward 64 x 96 x 55 x 55 fp32 70 us, 3.2 TB/s: columns of 48
-// bytes in the registers of 1008 threads, so that one work-group lives on a CU and its reads, sums and writes do not overlap
-// with another's; in tiles, which do overlap but read x and dy twice, 84 us (and
-// 5 for their join).
+// Forward 128 x 256 x 27 x 27 bf16 in 32 groups 23 us, 4.2 TB/s (vector units busy for 72 % of the cycles of CUs that hold
+// work).  4 x 64 x 224 x 224 bf16 in 8 groups, in tiles: 9.0 us for the sums and 13.9 for the rest, 2.2 TB/s counting x once, 3.4
+// as it is read.  Backward 64 x 96 x 55 x 55 fp32 70 us, 3.2 TB/s: columns of 48 bytes in the registers of 1008 threads, so
+// that one work-group lives on a CU, two of them one after the other, and the reads, sums and writes of one do not overlap
+// with another's; and parts of lines are written, 110 MB in place of 74.  In tiles, which do overlap but read x and dy twice,
+// 84 us (and 5 for their join).
+//
+// Backward on bfloat16 has eight fp32 sums of each kind to a thread beside its vectors, and with 6 or 8 vectors of several
+// groups 7 and 24 registers go to memory and back (8 vectors of one group: 3), 4 waves to a SIMD as it is.
 struct SlabTile {
     int n, slab, tile, s0, count;    // sample, slab, tile of positions [s0, s0 + count)
     int j, p;                        // this thread's column vector and first row

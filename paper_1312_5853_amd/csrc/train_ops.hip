@@ -77,8 +77,8 @@ void plan_planes(NormPlan &p, bool bwd, int V)
     a.vectors = (a.S - 1) / V + 1;
     a.chunks = (a.vectors + 63) / 64;
     // flat where a plane of its own would leave a sixth of the lanes idle: backward on 256 x 384 planes of 169 bfloat16 (22
-    // vectors) 28 us, and 50 with a unit to a plane; on 128 x 256 planes of 729 (92) 36.2 and 37.1.  Longer planes gain
-    // nothing by it: 128 x 256 planes of 729 fp32 (183 of 192) backward 57.1 us, and 58.8 flat
+    // vectors) 28 us, and 50 with a unit to a plane; on 128 x 256 planes of 729 (92) 36.4 and 37.3.  Longer planes gain
+    // nothing by it: 128 x 256 planes of 729 fp32 (183 of 192) backward 56.6 us, and 58.6 flat
     a.flat = a.vectors < 0.85 * 64 * a.chunks;
     const int64_t units = a.flat ? ((int64_t)a.cpg * a.vectors + 63) / 64 : (int64_t)a.cpg * a.chunks;
     const int most = 8;
@@ -89,11 +89,11 @@ void plan_planes(NormPlan &p, bool bwd, int V)
     if (units <= (int64_t)kMaxWaves * most && a.cpg <= 4096) {
         a.units = (int)units;
         // a wave to a group, four to a work-group and no barrier, for many small groups: 1024 x 64 planes of 16 fp32 in 64
-        // groups 16.8 us forward and 30.3 backward, 19.1 and 31.1 with a work-group to each; at 4 units it loses (bfloat16
+        // groups 16.4 us forward and 28.7 backward, 18.9 and 29.9 with a work-group to each; at 4 units it loses (bfloat16
         // backward on 512 x 256 planes of 196 in 32 groups: 44 us, and 38)
         p.solo = units <= 2 && groups >= 1024;
-        // units to a wave, of one tensor or of two: 2, 4, 8 units of it measured (forward 60, 59, 69 us on 128 x 96 planes of
-        // 3025 fp32, backward 54, 55, 64 us on 128 x 256 planes of 729); few groups take a wave to a unit (one sample of 256
+        // units to a wave, of one tensor or of two: 2, 4, 8 units of it measured (forward 58, 58, 60 us on 128 x 96 planes of
+        // 3025 fp32, backward 52, 53, 61 us on 128 x 256 planes of 729); few groups take a wave to a unit (one sample of 256
         // planes of 169 fp32, which 32 work-groups of a wave or eleven take: latency alone)
         const int want = groups < 1024 ? 1 : bwd ? 2 : 4;
         const int waves = p.solo ? 1 : std::min(kMaxWaves, ceil_div(a.units, want));
@@ -147,10 +147,10 @@ void plan_last(NormPlan &p, bool bwd, int V, int eb)
         const int rows = 1024 / (int)lanes64;
         if (ceil_div(a.S, rows) > most) continue;
         const double seg = (double)j * a.cpg * eb;
-        // Columns of fewer bytes cost more lines than tiles and their joins cost launches: backward 64 x 96 x 55 x 55 fp32 76 us
-        // in one pass of 48-byte columns, and 94 in tiles; forward in columns of 16 or 24 bytes 4 x 256 x 112 x 112 bf16 34 us
-        // and 32 x 64 x 112 x 112 bf16 56, in tiles 22.5 and 42.  At 48 bytes forward goes either way (64 x 192 x 48 x 48 bf16 48
-        // us in one pass and 36 in tiles, 32 x 96 x 55 x 55 bf16 20 and 26).
+        // Columns of fewer bytes cost more lines than tiles and their joins cost launches: backward 64 x 96 x 55 x 55 fp32 74 us
+        // in one pass of 48-byte columns, and 93 in tiles; forward in columns of 16 or 24 bytes 4 x 256 x 112 x 112 bf16 34 us
+        // and 32 x 64 x 112 x 112 bf16 57, in tiles 23 and 44.  At 48 bytes forward goes either way (64 x 192 x 48 x 48 bf16 48
+        // us in one pass of 48 bytes, 45 in tiles, and 37 in the 96 bytes that it takes; 32 x 96 x 55 x 55 bf16 20 and 25).
         if (seg < (bwd ? 48 : 64) && j != a.groups) continue;
         // lines that a slab shares with its neighbours are read by both; few work-groups leave the card idle
         const double wgs = (double)a.N * (a.groups / j);
@@ -161,7 +161,7 @@ void plan_last(NormPlan &p, bool bwd, int V, int eb)
     if (best) {
         a.slab_groups = best;
         a.lanes = lanes_of(best);
-        // rows to a thread.  Forward 4, 8, 16: 26.1, 21.1, 24.0 us on 128 x 256 x 27 x 27 bf16, 26.0, 19.9, 19.6 us on
+        // rows to a thread.  Forward 4, 8, 16: 25.8, 22.1, 24.3 us on 128 x 256 x 27 x 27 bf16, 25.6, 19.9, 19.5 us on
         // 256 x 384 x 13 x 13; backward 4 to 10 are within 3 %, and 6 leaves more work-groups to a CU than 10
         const int want = bwd ? 6 : 8;
         threads = std::min<int64_t>(1024, round_up64((int64_t)a.lanes * ceil_div(a.S, want), 64));
@@ -178,8 +178,9 @@ void plan_last(NormPlan &p, bool bwd, int V, int eb)
         threads = std::max(512, round_up(a.lanes, 64));
         a.rows = threads / a.lanes;
         const int64_t N_slabs = (int64_t)a.N * (a.groups / j);
-        // as many rows to a thread as leave 512 work-groups, 32 at most: forward 4 x 256 x 112 x 112 bf16 22.5 us, 27.9 with
-        // 128 work-groups and 22.2 with 2048; 32 x 64 x 112 x 112 bf16 42, 40 and 49 us
+        // as many rows to a thread as leave 512 work-groups, 32 at most: forward 4 x 256 x 112 x 112 bf16 23.0 us, 28.5 with
+        // 128 work-groups and 22.5 with 2048; 32 x 64 x 112 x 112 bf16 44, 40 and 52 us.  (A thread holds kSplitRun of them at
+        // a time: 6 rows, say, are a full and a half-empty trip to memory.)
         const int most_rows = (int)std::max<int64_t>(4, std::min<int64_t>(32, (int64_t)N_slabs * ceil_div(a.S, a.rows) / 512));
         a.tile_rows = std::min(a.S, a.rows * most_rows);
         a.tiles = ceil_div(a.S, a.tile_rows);

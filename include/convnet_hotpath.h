@@ -436,6 +436,74 @@ int distill_loss_fwd_bwd(const void *z, int64_t z_stride, const void *labels, co
                          void *ws, size_t ws_bytes, void *stream);
 size_t distill_loss_workspace_bytes(int N, int V, int K, int dtype);
 
+/*
+ * Tensors held in blocks.  32 neighbouring values of a row share a power of two, and each is a small floating-point
+ * number times it:
+ *   CONV_BLOCKS_E4M3: 8 bits, sign, 4 of exponent, 3 of mantissa, largest 448 (the format without infinities)
+ *   CONV_BLOCKS_E2M1: 4 bits, magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * A block's power is 2^e with e the smallest integer from -117 (E4M3) or -125 (E2M1) on under which its largest magnitude is
+ * at most 448 or 6 times it; x / 2^e is rounded to the nearest number of the format, to the even code where two are as near.
+ * So a value comes back within 2^-4 (E4M3) of itself or, below, half the format's least step times 2^e.  A block that holds an
+ * infinity or a NaN is all NaN.  (A value within 7 % (E4M3) or 13 % (E2M1) of 2^128 can come back as infinity.)
+ *   codes:  [N][P] (E4M3) or [N][P / 2] bytes (E2M1: two to a byte, the first in the low bits), P = C rounded up to a multiple
+ *           of 128, codes past C zero; 16-byte aligned
+ *   scales: [N][P / 32] bytes, e + 127, 255 for a block of NaN; 4-byte aligned
+ *   quantize_blocks:   codes and scales of x [N][C], rows x_stride elements apart (>= C)
+ *   dequantize_blocks: x from codes and scales as quantize_blocks writes them; exact in both types
+ * dtype: element type of x as for the glue layers.  C <= 2^30, N * P <= 2^34.  N = 0 is a no-op (pointers may be NULL).  The
+ * tensors of a call must not overlap.
+ */
+enum { CONV_BLOCKS_E4M3 = 0, CONV_BLOCKS_E2M1 = 1 };
+int quantize_blocks(const void *x, int64_t x_stride, void *codes, void *scales, int N, int C, int format, int dtype, void *stream);
+int dequantize_blocks(const void *codes, const void *scales, void *x, int64_t x_stride, int N, int C, int format, int dtype,
+                      void *stream);
+
+/*
+ * Layer normalisation: every row of x [N][C] by itself, for use in front of or behind a fully connected layer.
+ *   mean = sum x / C,   var = sum (x - mean)^2 / C,   rstd = 1 / sqrt(var + eps)
+ *   xh = (x - mean) * rstd,   y = gamma[c] * xh + beta[c]
+ *   gamma, beta: fp32 [C] on the device, or NULL for ones / zeros
+ *   mean, rstd:  fp32 [N]; layer_norm_fwd writes them where they are not NULL, the others read them
+ * layer_norm_bwd, with g = gamma[c] * dy:
+ *   dx = rstd * (g - mean(g) - xh * mean(g * xh)),   dgamma[c] = sum_n dy * xh,   dbeta[c] = sum_n dy  (fp32; each may be NULL)
+ * layer_norm_bwd_kept: the same from x as it was kept in E4M3 blocks (codes, scales of C values to a row); mean and rstd are
+ * those of the forward pass.
+ * `dtype` names the element type of x, y, dy and dx as for the glue layers; arithmetic is fp32 (sums of more than 32 values to a
+ * thread, and the join of a column's sums, in 64 bits), a bfloat16 result is rounded once.  Rows lie x_stride, y_stride, ... elements apart (>= C) and
+ * may start anywhere.  eps > 0.  C <= 2^27, N * C < 2^40.  N = 0 is allowed (tensors over it may be NULL; dgamma and dbeta
+ * become 0).  Outputs must not overlap inputs.  Scratch of the backward calls: layer_norm_workspace_bytes(CONV_OP_BWD_DATA, ...)
+ * bytes, 256-byte aligned (0 for invalid arguments; none is needed without dgamma and dbeta).
+ */
+int layer_norm_fwd(const void *x, int64_t x_stride, const void *gamma, const void *beta, void *y, int64_t y_stride, void *mean,
+                   void *rstd, int N, int C, float eps, int dtype, void *stream);
+int layer_norm_bwd(const void *x, int64_t x_stride, const void *dy, int64_t dy_stride, const void *gamma, const void *mean,
+                   const void *rstd, void *dx, int64_t dx_stride, void *dgamma, void *dbeta, int N, int C, int dtype, void *ws,
+                   size_t ws_bytes, void *stream);
+int layer_norm_bwd_kept(const void *codes, const void *scales, const void *dy, int64_t dy_stride, const void *gamma,
+                        const void *mean, const void *rstd, void *dx, int64_t dx_stride, void *dgamma, void *dbeta, int N, int C,
+                        int dtype, void *ws, size_t ws_bytes, void *stream);
+size_t layer_norm_workspace_bytes(int op, int N, int C, int dtype);
+
+/*
+ * Fully connected passes on tensors held in blocks; x [N][I], w and dw [O][I], y and dy [N][O] as for fc_fwd and
+ * fc_bwd_filter, dense, any I and O, each tensor (rows of codes filled up) below 2^31 elements.
+ *   fc_bwd_filter_kept: dw[o][i] = sum_n dy[n][o] * x[n][i] with x as it was kept in E4M3 blocks.  dtype: element type of dy
+ *                       (as for the glue layers); dw is fp32.  Products are exact in both types (of an fp32 dy below 2^-110
+ *                       less than 2^-133 is cut off), sums fp32.  N = 0: dw = 0.
+ *   fc_fwd_q4:          y[n][o] = f(sum_i x4[n][i] * w[o][i] + bias[o]) with w in E2M1 blocks, made once by quantize_blocks,
+ *                       and x4 what quantize_blocks makes of x in E2M1 (within the call).  bias fp32 [O] or NULL; f = max(., 0) if
+ *                       relu = 1, identity if relu = 0; NaN stays NaN.  dtype as for a convolution: CONV_DTYPE_F32 x and y
+ *                       fp32, CONV_DTYPE_BF16 x bfloat16 and y fp32, CONV_DTYPE_BF16_OUT_BF16 both bfloat16, y rounded
+ *                       once.  Sums fp32.  N = 0 is a no-op.
+ * Scratch: fc_kept_workspace_bytes / fc_q4_workspace_bytes bytes (0 for invalid arguments), 256-byte aligned.
+ */
+int fc_bwd_filter_kept(const void *codes, const void *scales, const void *dy, void *dw, int N, int I, int O, int dtype, void *ws,
+                       size_t ws_bytes, void *stream);
+size_t fc_kept_workspace_bytes(int N, int I, int O, int dtype);
+int fc_fwd_q4(const void *x, const void *w_codes, const void *w_scales, const void *bias, void *y, int N, int I, int O, int relu,
+              int dtype, void *ws, size_t ws_bytes, void *stream);
+size_t fc_q4_workspace_bytes(int N, int I, int O, int dtype);
+
 #ifdef __cplusplus
 }
 #endif

@@ -38,6 +38,11 @@ from .oracle import (  # noqa: F401
     group_norm_act_fwd,
     group_norm_act_bwd,
     distill_loss,
+    block_magnitudes,
+    quantize_blocks,
+    dequantize_blocks,
+    layer_norm_fwd,
+    layer_norm_bwd,
     bf16_bits,
     bf16_round,
     num_threads,

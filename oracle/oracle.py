@@ -403,3 +403,79 @@ def distill_loss(z, labels=None, top_idx=None, top_val=None, temperature=1.0, kd
             dz[n] += grad[n] * label_weight * np.exp(lq)
             dz[n, labels[n]] -= grad[n] * label_weight
     return loss, dz
+
+
+# ---------------------------------------------------------------------------
+# Tensors [N, C] held in blocks of 32 values with a shared power of two, and layer normalisation of rows.
+# ---------------------------------------------------------------------------
+BLOCK_LEAST = {"e4m3": -117, "e2m1": -125}
+
+
+def block_magnitudes(form):
+    """The format's magnitudes in the order of their codes, from sign, exponent and mantissa bits."""
+    exp_bits, man_bits, bias, count = {"e4m3": (4, 3, 7, 127), "e2m1": (2, 1, 1, 8)}[form]
+    out = []
+    for code in range(count):
+        e, m = code >> man_bits, code & ((1 << man_bits) - 1)
+        out.append((m / 2 ** man_bits if e == 0 else 1 + m / 2 ** man_bits) * 2.0 ** (max(e, 1) - bias))
+    return np.array(out)
+
+
+def quantize_blocks(x, form):
+    """(codes, scales) as bytes, rows filled up to a multiple of 128 values."""
+    x = _f64(x)
+    N, C = x.shape
+    pitch = -(-C // 128) * 128
+    v = np.zeros((N, pitch))
+    v[:, :C] = x
+    v = v.reshape(N, -1, 32)
+    mags = block_magnitudes(form)
+    amax = np.abs(v).max(axis=2)
+    bad = ~np.isfinite(v).all(axis=2)
+    amax = np.where(bad, 0.0, amax)
+    m, e = np.frexp(amax / mags[-1])                      # amax / M = m 2^e, m in [1/2, 1): 2^e is enough, 2^(e-1) if m = 1/2
+    e = np.where(m == 0.5, e - 1, e)
+    e = np.where(amax == 0, BLOCK_LEAST[form], np.maximum(e, BLOCK_LEAST[form]))
+    w = np.where(bad[:, :, None], 0.0, v) / np.exp2(e.astype(np.float64))[:, :, None]
+    mid = (mags[:-1] + mags[1:]) / 2
+    a = np.abs(w)
+    lo = np.searchsorted(mid, a, side="left")             # ties go down ...
+    hi = np.searchsorted(mid, a, side="right")            # ... or up, to the even one of the two codes
+    code = np.where(lo == hi, lo, np.where(lo % 2 == 0, lo, hi))
+    code = code + np.where(np.signbit(w), 128 if form == "e4m3" else 8, 0)
+    code = code.reshape(N, pitch).astype(np.uint8)
+    if form == "e2m1":
+        code = code[:, 0::2] | (code[:, 1::2] << 4)
+    return code, np.where(bad, 255, e + 127).astype(np.uint8)
+
+
+def dequantize_blocks(codes, scales, C, form):
+    """The values [N, C]."""
+    mags = block_magnitudes(form)
+    if form == "e4m3":
+        sign, mag = codes >> 7, codes & 127
+        v = np.append(mags, np.nan)[mag]
+    else:
+        both = np.stack([codes & 15, codes >> 4], axis=2).reshape(codes.shape[0], -1)
+        sign, mag = both >> 3, both & 7
+        v = mags[mag]
+    s = np.where(scales == 255, np.nan, np.exp2(scales.astype(np.float64) - 127))
+    return (np.where(sign == 1, -v, v) * np.repeat(s, 32, axis=1))[:, :C]
+
+
+def layer_norm_fwd(x, gamma, beta, eps):
+    """(y, mean, rstd)"""
+    x = _f64(x)
+    mean = x.mean(axis=1)
+    d = x - mean[:, None]
+    rstd = 1.0 / np.sqrt((d ** 2).mean(axis=1) + eps)
+    return d * rstd[:, None] * _f64(gamma) + _f64(beta), mean, rstd
+
+
+def layer_norm_bwd(x, dy, mean, rstd, gamma):
+    """(dx, dgamma, dbeta) for the statistics given."""
+    x, dy, mean, rstd = _f64(x), _f64(dy), _f64(mean)[:, None], _f64(rstd)[:, None]
+    xh = (x - mean) * rstd
+    g = dy * _f64(gamma)
+    dx = rstd * (g - g.mean(axis=1, keepdims=True) - xh * (g * xh).mean(axis=1, keepdims=True))
+    return dx, (dy * xh).sum(axis=0), dy.sum(axis=0)

@@ -24,6 +24,8 @@ DTYPE_F32, DTYPE_BF16, DTYPE_BF16_OUT_BF16 = 0, 1, 2
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2}
 LAYOUT_PLANES, LAYOUT_CHANNELS_LAST = 0, 1
 DISTILL_MAX_TOP = 1024
+BLOCK_FORMATS = {"e4m3": 0, "e2m1": 1}
+BLOCK_VALUES, BLOCK_ROW_FILL = 32, 128
 OP_FWD, OP_BWD_DATA, OP_BWD_FILTER = 0, 1, 2
 
 EXPORTS = (
@@ -37,6 +39,8 @@ EXPORTS = (
     "fc_fwd", "fc_bwd_data", "fc_bwd_filter", "fc_workspace_bytes", "sgd_update", "sgd_update_multi",
     "group_norm_act_fwd", "group_norm_act_bwd", "group_norm_act_workspace_bytes",
     "distill_loss_fwd", "distill_loss_bwd", "distill_loss_fwd_bwd", "distill_loss_workspace_bytes",
+    "quantize_blocks", "dequantize_blocks", "layer_norm_fwd", "layer_norm_bwd", "layer_norm_bwd_kept",
+    "layer_norm_workspace_bytes", "fc_bwd_filter_kept", "fc_kept_workspace_bytes", "fc_fwd_q4", "fc_q4_workspace_bytes",
 )
 
 _lib = None
@@ -128,6 +132,19 @@ def lib():
                  "distill_loss_fwd_bwd"):
         getattr(L, name).restype = i
     for name in ("group_norm_act_workspace_bytes", "distill_loss_workspace_bytes"):
+        getattr(L, name).restype = sz
+    L.quantize_blocks.argtypes = [vp, i64, vp, vp, i, i, i, i, vp]
+    L.dequantize_blocks.argtypes = [vp, vp, vp, i64, i, i, i, i, vp]
+    L.layer_norm_fwd.argtypes = [vp, i64, vp, vp, vp, i64, vp, vp, i, i, f32, i, vp]
+    L.layer_norm_bwd.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, i, i, i, vp, sz, vp]
+    L.layer_norm_bwd_kept.argtypes = [vp, vp, vp, i64, vp, vp, vp, vp, i64, vp, vp, i, i, i, vp, sz, vp]
+    L.fc_bwd_filter_kept.argtypes = [vp, vp, vp, vp, i, i, i, i, vp, sz, vp]
+    L.fc_fwd_q4.argtypes = [vp, vp, vp, vp, vp, i, i, i, i, i, vp, sz, vp]
+    for name in ("quantize_blocks", "dequantize_blocks", "layer_norm_fwd", "layer_norm_bwd", "layer_norm_bwd_kept",
+                 "fc_bwd_filter_kept", "fc_fwd_q4"):
+        getattr(L, name).restype = i
+    for name in ("layer_norm_workspace_bytes", "fc_kept_workspace_bytes", "fc_q4_workspace_bytes"):
+        getattr(L, name).argtypes = [i] * 4
         getattr(L, name).restype = sz
     _lib = L
     return L
@@ -892,3 +909,268 @@ def distill_loss_fwd_bwd(z, labels=None, top_idx=None, top_val=None, temperature
     if rc != OK:
         raise ConvError(rc, "distill_loss_fwd_bwd")
     return loss, dz
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# Tensors held in blocks, layer normalisation, and the fully connected passes on such tensors
+# ---------------------------------------------------------------------------------------------------------------
+@functools.lru_cache(maxsize=1024, typed=True)
+def _layer_norm_workspace_bytes(N, C, dtype):
+    return int(lib().layer_norm_workspace_bytes(OP_BWD_DATA, N, C, dtype))
+
+
+@functools.lru_cache(maxsize=1024, typed=True)
+def _fc_kept_workspace_bytes(N, I, O, dtype):
+    return int(lib().fc_kept_workspace_bytes(N, I, O, dtype))
+
+
+@functools.lru_cache(maxsize=1024, typed=True)
+def _fc_q4_workspace_bytes(N, I, O, dtype):
+    return int(lib().fc_q4_workspace_bytes(N, I, O, dtype))
+
+
+class Blocks:
+    """A tensor [N, cols] held in blocks of 32 values with a shared power of two: `codes` and `scales` (uint8, rows filled up
+    to a multiple of 128 values) and the format's name, "e4m3" (8 bits) or "e2m1" (4 bits).  quantize_blocks makes one."""
+    __slots__ = ("codes", "scales", "cols", "format")
+
+    def __init__(self, codes, scales, cols, format):
+        if type(cols) is not int:
+            cols, = _whole(cols)
+        if format not in BLOCK_FORMATS:
+            raise ValueError("unknown block format %r" % (format,))
+        pitch = -(-cols // BLOCK_ROW_FILL) * BLOCK_ROW_FILL
+        shape = codes.shape
+        if codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8:
+            raise TypeError("codes and scales are bytes")
+        if (cols < 1 or len(shape) != 2 or shape[1] != (pitch if format == "e4m3" else pitch // 2)
+                or scales.shape != (shape[0], pitch // BLOCK_VALUES) or not codes.is_contiguous() or not scales.is_contiguous()):
+            raise ValueError("codes and scales must be dense, with rows of %d values and their exponents" % pitch)
+        if codes.get_device() != scales.get_device():
+            raise ValueError("the tensors of a call must be on one GPU")
+        self.codes, self.scales, self.cols, self.format = codes, scales, cols, format
+
+    @classmethod
+    def empty(cls, N, cols, format, device="cuda"):
+        """Room for N rows of `cols` values."""
+        if format not in BLOCK_FORMATS:
+            raise ValueError("unknown block format %r" % (format,))
+        N, cols = _whole(N, cols)
+        pitch = -(-cols // BLOCK_ROW_FILL) * BLOCK_ROW_FILL
+        byte = dict(dtype=torch.uint8, device=device)
+        return cls(torch.empty((N, pitch if format == "e4m3" else pitch // 2), **byte),
+                   torch.empty((N, pitch // BLOCK_VALUES), **byte), cols, format)
+
+    @property
+    def shape(self):
+        return torch.Size((self.codes.shape[0], self.cols))
+
+    @property
+    def nbytes(self):
+        return self.codes.numel() + self.scales.numel()
+
+
+def _held(q, format, what):
+    if type(q) is not Blocks:
+        raise TypeError("%s must be a tensor held in blocks" % what)
+    if q.format != format:
+        raise ValueError("%s must be held as %s" % (what, format))
+
+
+def quantize_blocks(x, format, out=None, stream=None):
+    """x [N,C] (fp32 or bfloat16, rows may be apart) in blocks of `format`, "e4m3" or "e2m1"."""
+    N, C, xs = _rows_of(x, "x")
+    dtype, d = _glue_code(x), x.get_device()
+    if format not in BLOCK_FORMATS:
+        raise ValueError("unknown block format %r" % (format,))
+    _on_gpu(d)
+    if out is None:
+        out = Blocks.empty(N, C, format, x.device)
+    else:
+        _held(out, format, "out")
+        if out.cols != C or out.codes.shape[0] != N:
+            raise ValueError("out must have the shape of x")
+        if out.codes.get_device() != d:
+            raise ValueError("the tensors of a call must be on one GPU")
+    rc = lib().quantize_blocks(x.data_ptr(), xs, out.codes.data_ptr(), out.scales.data_ptr(), N, C, BLOCK_FORMATS[format], dtype,
+                               _current_stream(stream, d))
+    if rc != OK:
+        raise ConvError(rc, "quantize_blocks")
+    return out
+
+
+def dequantize_blocks(q, x=None, dtype=torch.float32, stream=None):
+    """The values [N,C] of a tensor held in blocks, as fp32 or bfloat16 (exact in both), into x (its type decides) or a new
+    tensor of `dtype`."""
+    if type(q) is not Blocks:
+        raise TypeError("q must be a tensor held in blocks")
+    N, C = q.codes.shape[0], q.cols
+    d = q.codes.get_device()
+    if x is None:
+        x = torch.empty((N, C), dtype=dtype, device=q.codes.device)
+    xN, xC, xs = _rows_of(x, "x")
+    code = _glue_code(x)
+    if xN != N or xC != C:
+        raise ValueError("x must have the shape of the tensor in blocks")
+    if x.get_device() != d:
+        raise ValueError("the tensors of a call must be on one GPU")
+    _on_gpu(d)
+    rc = lib().dequantize_blocks(q.codes.data_ptr(), q.scales.data_ptr(), x.data_ptr(), xs, N, C, BLOCK_FORMATS[q.format], code,
+                                 _current_stream(stream, d))
+    if rc != OK:
+        raise ConvError(rc, "dequantize_blocks")
+    return x
+
+
+def _rows_like(t, x, N, C, d, what):
+    """Row stride of t, a tensor of x's shape [N,C], element type and GPU."""
+    tN, tC, stride = _rows_of(t, what)
+    if tN != N or tC != C:
+        raise ValueError("%s must have the shape [%d, %d]" % (what, N, C))
+    if t.dtype is not x.dtype:
+        raise TypeError("%s must have the element type of the call's other tensors" % what)
+    if t.get_device() != d:
+        raise ValueError("the tensors of a call must be on one GPU")
+    return stride
+
+
+def layer_norm_fwd(x, gamma=None, beta=None, eps=1e-5, y=None, mean=None, rstd=None, stream=None):
+    """y = (x - mean) * rstd * gamma + beta for every row of x [N,C] (fp32 or bfloat16, rows may be apart), and the statistics
+    that the backward pass needs: (y, mean [N], rstd [N]).  gamma and beta: fp32 [C], or None."""
+    N, C, xs = _rows_of(x, "x")
+    dtype, d = _glue_code(x), x.get_device()
+    _on_gpu(d)
+    if y is None:
+        y, ys = torch.empty((N, C), dtype=x.dtype, device=x.device), C
+    else:
+        ys = _rows_like(y, x, N, C, d, "y")
+    gp = 0 if gamma is None else _dense_f32(gamma, (C,), d, "gamma")
+    bp = 0 if beta is None else _dense_f32(beta, (C,), d, "beta")
+    mean = _new_f32((N,), x) if mean is None else mean
+    rstd = _new_f32((N,), x) if rstd is None else rstd
+    mp, rp = _dense_f32(mean, (N,), d, "mean"), _dense_f32(rstd, (N,), d, "rstd")
+    rc = lib().layer_norm_fwd(x.data_ptr(), xs, gp, bp, y.data_ptr(), ys, mp, rp, N, C, eps, dtype, _current_stream(stream, d))
+    if rc != OK:
+        raise ConvError(rc, "layer_norm_fwd")
+    return y, mean, rstd
+
+
+def _layer_norm_bwd(name, source, dy, N, C, mean, rstd, gamma, dx, dgamma, dbeta, ws, stream):
+    dyN, dyC, dys = _rows_of(dy, "dy")
+    if dyN != N or dyC != C:
+        raise ValueError("dy must have the shape [%d, %d]" % (N, C))
+    dtype, d = _glue_code(dy), dy.get_device()
+    _on_gpu(d)
+    if dx is None:
+        dx, dxs = torch.empty((N, C), dtype=dy.dtype, device=dy.device), C
+    else:
+        dxs = _rows_like(dx, dy, N, C, d, "dx")
+    mp, rp = _dense_f32(mean, (N,), d, "mean"), _dense_f32(rstd, (N,), d, "rstd")
+    gp = 0 if gamma is None else _dense_f32(gamma, (C,), d, "gamma")
+    dgamma = _new_f32((C,), dy) if dgamma is None else dgamma
+    dbeta = _new_f32((C,), dy) if dbeta is None else dbeta
+    dgp, dbp = _dense_f32(dgamma, (C,), d, "dgamma"), _dense_f32(dbeta, (C,), d, "dbeta")
+    need, wsp = _layer_norm_workspace_bytes(N, C, dtype), 0
+    handle, own = _current_stream(stream, d), 0
+    if need:
+        if ws is None:
+            own = wsp = _take_scratch(need, handle)
+        else:
+            buf, need = ws.get(need)
+            wsp = buf.data_ptr()
+    try:
+        rc = getattr(lib(), name)(*source, dy.data_ptr(), dys, gp, mp, rp, dx.data_ptr(), dxs, dgp, dbp, N, C, dtype, wsp, need,
+                                  handle)
+    finally:
+        if own:
+            _give_scratch(own)
+    if rc != OK:
+        raise ConvError(rc, name)
+    return dx, dgamma, dbeta
+
+
+def layer_norm_bwd(x, dy, mean, rstd, gamma=None, dx=None, dgamma=None, dbeta=None, ws=None, stream=None):
+    """(dx, dgamma [C], dbeta [C]) from the forward call's x, mean and rstd and the gradient dy of its y."""
+    N, C, xs = _rows_of(x, "x")
+    if dy.dtype is not x.dtype:
+        raise TypeError("dy must have the element type of x")
+    if dy.get_device() != x.get_device():
+        raise ValueError("the tensors of a call must be on one GPU")
+    return _layer_norm_bwd("layer_norm_bwd", (x.data_ptr(), xs), dy, N, C, mean, rstd, gamma, dx, dgamma, dbeta, ws, stream)
+
+
+def layer_norm_bwd_kept(q, dy, mean, rstd, gamma=None, dx=None, dgamma=None, dbeta=None, ws=None, stream=None):
+    """layer_norm_bwd from x as it was kept in blocks of 8 bits; dx has dy's element type."""
+    _held(q, "e4m3", "q")
+    if dy.get_device() != q.codes.get_device():
+        raise ValueError("the tensors of a call must be on one GPU")
+    return _layer_norm_bwd("layer_norm_bwd_kept", (q.codes.data_ptr(), q.scales.data_ptr()), dy, q.codes.shape[0], q.cols, mean,
+                           rstd, gamma, dx, dgamma, dbeta, ws, stream)
+
+
+def fc_bwd_filter_kept(q, dy, dw=None, ws=None, stream=None):
+    """q: x [N,I] as it was kept in blocks of 8 bits, dy [N,O] (fp32 or bfloat16) -> dw [O,I] fp32."""
+    _held(q, "e4m3", "q")
+    N, I = q.codes.shape[0], q.cols
+    shape = dy.shape
+    if len(shape) != 2 or shape[0] != N or not dy.is_contiguous():
+        raise ValueError("dy must be a dense tensor with the rows of q")
+    O, dtype, d = shape[1], _glue_code(dy), dy.get_device()
+    if q.codes.get_device() != d:
+        raise ValueError("the tensors of a call must be on one GPU")
+    _on_gpu(d)
+    dw = _new_f32((O, I), dy) if dw is None else dw
+    wp = _dense_f32(dw, (O, I), d, "dw")
+    need, wsp = _fc_kept_workspace_bytes(N, I, O, dtype), 0
+    handle, own = _current_stream(stream, d), 0
+    if need:
+        if ws is None:
+            own = wsp = _take_scratch(need, handle)
+        else:
+            buf, need = ws.get(need)
+            wsp = buf.data_ptr()
+    try:
+        rc = lib().fc_bwd_filter_kept(q.codes.data_ptr(), q.scales.data_ptr(), dy.data_ptr(), wp, N, I, O, dtype, wsp, need, handle)
+    finally:
+        if own:
+            _give_scratch(own)
+    if rc != OK:
+        raise ConvError(rc, "fc_bwd_filter_kept")
+    return dw
+
+
+def fc_fwd_q4(x, w, bias=None, relu=False, y=None, ws=None, stream=None, out_bf16=False):
+    """x [N,I] (fp32 or bfloat16), w [O,I] held in blocks of 4 bits -> y [N,O] = f(x w^T + bias), fp32 (or bfloat16: pass a
+    bfloat16 y, or out_bf16=True, with a bfloat16 x).  x is put into blocks of 4 bits within the call."""
+    _held(w, "e2m1", "w")
+    O, I = w.codes.shape[0], w.cols
+    shape = x.shape
+    if len(shape) != 2 or shape[1] != I or not x.is_contiguous():
+        raise ValueError("x must be a dense tensor with rows of %d values" % I)
+    N, dtype, d = shape[0], _glue_code(x), x.get_device()
+    if w.codes.get_device() != d:
+        raise ValueError("the tensors of a call must be on one GPU")
+    _on_gpu(d)
+    if y is None:
+        y = torch.empty((N, O), dtype=torch.bfloat16 if out_bf16 else _F32, device=x.device)
+    elif y.shape != (N, O) or not y.is_contiguous() or y.get_device() != d:
+        raise ValueError("y must be a dense tensor [%d, %d] on the GPU of x" % (N, O))
+    code = _io_dtype(x, y)
+    bp = 0 if bias is None else _dense_f32(bias, (O,), d, "bias")
+    need, wsp = _fc_q4_workspace_bytes(N, I, O, code), 0
+    handle, own = _current_stream(stream, d), 0
+    if need:
+        if ws is None:
+            own = wsp = _take_scratch(need, handle)
+        else:
+            buf, need = ws.get(need)
+            wsp = buf.data_ptr()
+    try:
+        rc = lib().fc_fwd_q4(x.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(), bp, y.data_ptr(), N, I, O, 1 if relu else 0, code,
+                             wsp, need, handle)
+    finally:
+        if own:
+            _give_scratch(own)
+    if rc != OK:
+        raise ConvError(rc, "fc_fwd_q4")
+    return y

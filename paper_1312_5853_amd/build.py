@@ -11,15 +11,17 @@ import tempfile
 _HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(_HERE, "csrc", "convnet_hotpath.hip")
 TRAIN_SRC = os.path.join(_HERE, "csrc", "train_ops.hip")
-SOURCES = (SRC, TRAIN_SRC)
+BLOCK_SRC = os.path.join(_HERE, "csrc", "block_ops.hip")
+SOURCES = (SRC, TRAIN_SRC, BLOCK_SRC)
 LIB = os.path.join(_HERE, "libconvnet_hotpath.so")
 CEILING_SRC = os.path.join(_HERE, "csrc", "mfma_ceiling.hip")
 CEILING_EXE = os.path.join(_HERE, "mfma_ceiling")
-DEPS = [SRC, TRAIN_SRC] + [os.path.join(_HERE, "csrc", h) for h in (
+DEPS = list(SOURCES) + [os.path.join(_HERE, "csrc", h) for h in (
     "plan.h", "fastdiv.h", "device_common.h", "conv_colgemm_kernels.h", "conv_bf16_dma_kernels.h",
     "conv_bf16_window_kernels.h", "conv_split_kernels.h", "conv_wgrad_split_kernels.h", "conv_direct_kernels.h",
     "conv_wgrad_rows_kernels.h", "conv_wgrad_kernels.h", "fc_kernels.h", "glue_kernels.h",
-    "host_status.h", "elements.h", "vectors.h", "norm_kernels.h", "loss_kernels.h")] + [os.path.join(os.path.dirname(_HERE), "include", "convnet_hotpath.h")]
+    "host_status.h", "elements.h", "vectors.h", "norm_kernels.h", "loss_kernels.h",
+    "block_formats.h", "block_kernels.h", "layer_norm_kernels.h", "fc_kept_kernels.h", "fc_q4_kernels.h")] + [os.path.join(os.path.dirname(_HERE), "include", "convnet_hotpath.h")]
 
 # no packed-fp32 instruction selection
 DEVICE_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

@@ -1,0 +1,394 @@
+// HIP kernels (gfx950 / CDNA4) and C-ABI entry points of the fully connected part of a network: layer normalisation, tensors
+// held in blocks of 8 or 4 bits with a shared power of two, the filter gradient from 8 bits and the forward pass in 4 bits.
+// Signatures and conventions are documented in include/convnet_hotpath.h.
+#include <hip/hip_runtime.h>
+
+#include <math.h>
+
+#include <algorithm>
+
+#include "../../include/convnet_hotpath.h"
+#include "host_status.h"
+
+using namespace convnet;
+
+namespace {
+
+#include "elements.h"
+#include "vectors.h"
+#include "block_formats.h"
+#include "layer_norm_kernels.h"
+#include "block_kernels.h"
+#include "fc_kept_kernels.h"
+#include "fc_q4_kernels.h"
+
+typedef unsigned short Bf16;
+
+int pow2_up(int v)
+{
+    int p = 1;
+    while (p < v) p <<= 1;
+    return p;
+}
+
+constexpr int64_t kMaxElements = (int64_t)1 << 31;       // of a fully connected layer's tensors
+constexpr size_t kMaxLds = 160 * 1024;
+
+int64_t pitch_of(int C) { return round_up64(C, kRowFill); }
+
+// codes are read and written 16 bytes at a time, exponents four
+bool blocks_aligned(const void *codes, const void *scales) { return aligned(codes, 16) && aligned(scales, 4); }
+
+template <typename Kern, typename Args>
+void launch(Kern kern, int64_t blocks, int threads, size_t lds, hipStream_t st, const Args &a)
+{
+    if (lds > 64 * 1024)                                 // more dynamic LDS than that has to be allowed per kernel
+        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kMaxLds);
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(threads), lds, st, a);
+}
+
+// ---------------------------------------------------------------------------
+// Blocks
+// ---------------------------------------------------------------------------
+int blocks_common(BlockArgs &a, int N, int C, int form, int dtype, const void *values, const void *codes)
+{
+    if (N < 0 || C <= 0 || a.stride < C || (form != kE4M3 && form != kE2M1)) return kErrInvalidArg;
+    if (N != 0 && (!values || !codes || !a.scales || values == codes || values == a.scales || codes == a.scales)) return kErrInvalidArg;
+    const int eb = glue_elem_bytes(dtype);
+    if (!eb) return kErrBadDtype;
+    if (C > (1 << 30) || N * pitch_of(C) > (int64_t)1 << 34) return kErrTooLarge;       // a thread to eight values
+    if (!aligned(values, eb) || !blocks_aligned(codes, a.scales)) return kErrMisaligned;
+    a.C = C;
+    a.per_row = (int)(pitch_of(C) / 8);
+    a.total = (int64_t)N * a.per_row;
+    a.div = make_fastdiv(a.per_row);
+    return kStatusOk;
+}
+
+template <typename T>
+void run_quantize(const BlockArgs &a, int form, hipStream_t st)
+{
+    const int64_t blocks = (a.total + 255) / 256;
+    if (form == kE4M3) launch(quantize_blocks_kernel<T, kE4M3>, blocks, 256, 0, st, a);
+    else launch(quantize_blocks_kernel<T, kE2M1>, blocks, 256, 0, st, a);
+}
+
+template <typename T>
+void run_dequantize(const BlockArgs &a, int form, hipStream_t st)
+{
+    const int64_t blocks = (a.total + 255) / 256;
+    if (form == kE4M3) launch(dequantize_blocks_kernel<T, kE4M3>, blocks, 256, 0, st, a);
+    else launch(dequantize_blocks_kernel<T, kE2M1>, blocks, 256, 0, st, a);
+}
+
+// ---------------------------------------------------------------------------
+// Layer normalisation
+// ---------------------------------------------------------------------------
+struct LayerNormPlan {
+    bool wide;                    // rows longer than a work-group keeps
+    int regs, threads;
+    int64_t blocks;
+    size_t lds, part_bytes;
+    LayerNormArgs a;
+};
+
+int plan_layer_norm(LayerNormPlan &p, int op, int N, int C, int dtype)
+{
+    p = {};
+    if (N < 0 || C <= 0 || (op != CONV_OP_FWD && op != CONV_OP_BWD_DATA)) return kErrInvalidArg;
+    const int eb = glue_elem_bytes(dtype);
+    if (!eb) return kErrBadDtype;
+    if (C > (1 << 27) || (int64_t)N * C >= (int64_t)1 << 40) return kErrTooLarge;
+    const bool bwd = op == CONV_OP_BWD_DATA;
+    const int V = 16 / eb;
+    LayerNormArgs &a = p.a;
+    a.N = N; a.C = C;
+    a.vectors = (C - 1) / V + 1;
+    a.pitch = pitch_of(C);
+    a.inv_c = (float)(1.0 / C);
+    // values to a thread: 16 or, forward, 32 where a work-group of 1024 threads needs them
+    const int few = 16 / V, most = bwd ? few : 2 * few;
+    const int chunks = (a.vectors + 63) / 64;
+    p.wide = chunks > 16 * most;
+    if (p.wide) {
+        a.waves = 16; a.groups = 1;
+        p.threads = 1024;
+        p.blocks = std::min(N, 1 << 16);
+        if (bwd) {
+            const int tiles = (C + 63) / 64;
+            a.part_rows = std::max(1, std::min(ceil_div(N, 256), 2048 / tiles));
+            a.rows_per_part = std::max(1, ceil_div(N, a.part_rows));
+            a.part_rows = std::max(1, ceil_div(N, a.rows_per_part));
+        }
+    } else {
+        a.waves = std::min(16, ceil_div(chunks, few));
+        p.regs = pow2_up(ceil_div(chunks, a.waves));
+        a.groups = std::max(1, 8 / a.waves);
+        p.threads = a.waves * a.groups * 64;
+        const int rounds = ceil_div(N, a.groups);
+        // a column's sum in a thread runs over at most 256 rows
+        p.blocks = std::min<int64_t>(rounds, std::max(512, ceil_div(rounds, 256)));
+        if (bwd) {
+            a.part_rows = (int)p.blocks;
+            p.lds = a.groups > 1 ? (size_t)a.groups * 2 * a.vectors * V * 4 : 0;
+        }
+    }
+    if (bwd) p.part_bytes = (size_t)round_up64((int64_t)a.part_rows * 2 * C * 4, 256);
+    return kStatusOk;
+}
+
+template <typename T>
+int run_layer_norm_fwd(const LayerNormPlan &p, hipStream_t st)
+{
+    if (p.wide) launch(layer_norm_fwd_wide<T>, p.blocks, p.threads, 0, st, p.a);
+    else if (p.regs == 1) launch(layer_norm_fwd_rows<T, 1>, p.blocks, p.threads, 0, st, p.a);
+    else if (p.regs == 2) launch(layer_norm_fwd_rows<T, 2>, p.blocks, p.threads, 0, st, p.a);
+    else if (p.regs == 4) launch(layer_norm_fwd_rows<T, 4>, p.blocks, p.threads, 0, st, p.a);
+    else if constexpr (sizeof(T) == 4) launch(layer_norm_fwd_rows<T, 8>, p.blocks, p.threads, 0, st, p.a);
+    return check_launch();
+}
+
+template <typename T, bool HELD>
+int run_layer_norm_bwd(const LayerNormPlan &p, hipStream_t st)
+{
+    const LayerNormArgs &a = p.a;
+    if (a.N > 0) {
+        if (p.wide) {
+            launch(layer_norm_bwd_wide<T, HELD>, p.blocks, p.threads, 0, st, a);
+            if (a.part) launch(layer_norm_columns<T, HELD>, (int64_t)a.part_rows * ((a.C + 63) / 64), 1024, 0, st, a);
+        } else if (p.regs == 1) {
+            launch(layer_norm_bwd_rows<T, HELD, 1>, p.blocks, p.threads, p.lds, st, a);
+        } else if (p.regs == 2) {
+            launch(layer_norm_bwd_rows<T, HELD, 2>, p.blocks, p.threads, p.lds, st, a);
+        } else if constexpr (sizeof(T) == 4) {
+            launch(layer_norm_bwd_rows<T, HELD, 4>, p.blocks, p.threads, p.lds, st, a);
+        }
+    }
+    if (a.dgamma || a.dbeta) launch(layer_norm_join, (a.C + 63) / 64, 1024, 0, st, a);
+    return check_launch();
+}
+
+// a: the call's pointers and strides
+int layer_norm_bwd_common(const LayerNormArgs &given, bool held, int N, int C, int dtype, void *ws, size_t ws_bytes, void *stream)
+{
+    const LayerNormArgs &g = given;
+    if (g.dy_stride < C || g.out_stride < C || (!held && g.x_stride < C)) return kErrInvalidArg;
+    LayerNormPlan p;
+    const int rc = plan_layer_norm(p, CONV_OP_BWD_DATA, N, C, dtype);
+    if (rc != kStatusOk) return rc;
+    const size_t eb = glue_elem_bytes(dtype);
+    if (!aligned(g.x, eb) || !aligned(g.dy, eb) || !aligned(g.out, eb) || !blocks_aligned(g.codes, g.scales) || !aligned(g.gamma, 4) ||
+        !aligned(g.mean, 4) || !aligned(g.rstd, 4) || !aligned(g.dgamma, 4) || !aligned(g.dbeta, 4))
+        return kErrMisaligned;
+    const bool sums = g.dgamma || g.dbeta;
+    if (sums && p.part_bytes) {
+        if (!ws || ws_bytes < p.part_bytes) return kErrWorkspace;
+        if (!aligned(ws, 256)) return kErrMisaligned;
+    }
+    LayerNormArgs &a = p.a;
+    a.x = g.x; a.codes = g.codes; a.scales = g.scales; a.dy = g.dy; a.out = g.out;
+    a.gamma = g.gamma; a.mean = g.mean; a.rstd = g.rstd; a.dgamma = g.dgamma; a.dbeta = g.dbeta;
+    a.x_stride = g.x_stride; a.dy_stride = g.dy_stride; a.out_stride = g.out_stride;
+    a.part = sums ? static_cast<float *>(ws) : nullptr;
+    if (N == 0) a.part_rows = 0;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (held) return eb == 4 ? run_layer_norm_bwd<float, true>(p, st) : run_layer_norm_bwd<Bf16, true>(p, st);
+    return eb == 4 ? run_layer_norm_bwd<float, false>(p, st) : run_layer_norm_bwd<Bf16, false>(p, st);
+}
+
+// ---------------------------------------------------------------------------
+// Fully connected layers
+// ---------------------------------------------------------------------------
+struct KeptGradPlan {
+    KeptGradArgs a;
+    int64_t blocks;
+    size_t part_bytes;
+};
+
+int plan_kept_grad(KeptGradPlan &p, int N, int I, int O, int dtype)
+{
+    p = {};
+    if (N < 0 || I <= 0 || O <= 0) return kErrInvalidArg;
+    if (!glue_elem_bytes(dtype)) return kErrBadDtype;
+    if (N * pitch_of(I) >= kMaxElements || (int64_t)N * O >= kMaxElements || (int64_t)I * O >= kMaxElements) return kErrTooLarge;
+    KeptGradArgs &a = p.a;
+    a.N = N; a.I = I; a.O = O;
+    a.pitch = pitch_of(I);
+    a.dy_stride = O;
+    a.itiles = ceil_div(I, kGradTile);
+    a.otiles = ceil_div(O, kGradTile);
+    const int64_t tiles = (int64_t)a.itiles * a.otiles;
+    const int steps = std::max(1, ceil_div(N, kGradStep));
+    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, steps / 4));
+    const int per = ceil_div(steps, a.splits);
+    a.rows_per_split = per * kGradStep;
+    a.splits = ceil_div(steps, per);
+    p.blocks = tiles * a.splits;
+    if (a.splits > 1) p.part_bytes = (size_t)round_up64((int64_t)a.splits * I * O * 4, 256);
+    return kStatusOk;
+}
+
+int check_q4(int N, int I, int O, int dtype)
+{
+    if (N < 0 || I <= 0 || O <= 0) return kErrInvalidArg;
+    if (!glue_elem_bytes(dtype)) return kErrBadDtype;
+    if (N * pitch_of(I) >= kMaxElements || O * pitch_of(I) >= kMaxElements || (int64_t)N * O >= kMaxElements) return kErrTooLarge;
+    return kStatusOk;
+}
+size_t q4_codes_bytes(int N, int I) { return (size_t)round_up64(N * pitch_of(I) / 2, 256); }
+size_t q4_bytes(int N, int I) { return q4_codes_bytes(N, I) + (size_t)round_up64(N * pitch_of(I) / kBlock, 256); }
+
+template <typename T>
+int run_q4(const Q4Args &a, hipStream_t st)
+{
+    launch(fc_q4_tiles<T>, (int64_t)a.ntiles * a.otiles, 256, 0, st, a);
+    return check_launch();
+}
+
+}  // namespace
+
+extern "C" {
+
+int quantize_blocks(const void *x, int64_t x_stride, void *codes, void *scales, int N, int C, int format, int dtype, void *stream)
+{
+    BlockArgs a = {};
+    a.in = x; a.out = codes; a.scales = static_cast<unsigned char *>(scales); a.stride = x_stride;
+    const int rc = blocks_common(a, N, C, format, dtype, x, codes);
+    if (rc != kStatusOk || N == 0) return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (glue_elem_bytes(dtype) == 4) run_quantize<float>(a, format, st);
+    else run_quantize<Bf16>(a, format, st);
+    return check_launch();
+}
+
+int dequantize_blocks(const void *codes, const void *scales, void *x, int64_t x_stride, int N, int C, int format, int dtype,
+                      void *stream)
+{
+    BlockArgs a = {};
+    a.in = codes; a.out = x; a.scales = static_cast<unsigned char *>(const_cast<void *>(scales)); a.stride = x_stride;
+    const int rc = blocks_common(a, N, C, format, dtype, x, codes);
+    if (rc != kStatusOk || N == 0) return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (glue_elem_bytes(dtype) == 4) run_dequantize<float>(a, format, st);
+    else run_dequantize<Bf16>(a, format, st);
+    return check_launch();
+}
+
+size_t layer_norm_workspace_bytes(int op, int N, int C, int dtype)
+{
+    LayerNormPlan p;
+    return plan_layer_norm(p, op, N, C, dtype) == kStatusOk ? p.part_bytes : 0;
+}
+
+int layer_norm_fwd(const void *x, int64_t x_stride, const void *gamma, const void *beta, void *y, int64_t y_stride, void *mean,
+                   void *rstd, int N, int C, float eps, int dtype, void *stream)
+{
+    if ((N != 0 && (!x || !y || x == y)) || !(eps > 0.f) || !isfinite(eps) || x_stride < C || y_stride < C) return kErrInvalidArg;
+    LayerNormPlan p;
+    const int rc = plan_layer_norm(p, CONV_OP_FWD, N, C, dtype);
+    if (rc != kStatusOk) return rc;
+    const size_t eb = glue_elem_bytes(dtype);
+    if (!aligned(x, eb) || !aligned(y, eb) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) || !aligned(rstd, 4))
+        return kErrMisaligned;
+    if (N == 0) return kStatusOk;
+    LayerNormArgs &a = p.a;
+    a.x = x; a.x_stride = x_stride; a.out = y; a.out_stride = y_stride; a.eps = eps;
+    a.gamma = static_cast<const float *>(gamma); a.beta = static_cast<const float *>(beta);
+    a.mean = static_cast<float *>(mean); a.rstd = static_cast<float *>(rstd);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return eb == 4 ? run_layer_norm_fwd<float>(p, st) : run_layer_norm_fwd<Bf16>(p, st);
+}
+
+int layer_norm_bwd(const void *x, int64_t x_stride, const void *dy, int64_t dy_stride, const void *gamma, const void *mean,
+                   const void *rstd, void *dx, int64_t dx_stride, void *dgamma, void *dbeta, int N, int C, int dtype, void *ws,
+                   size_t ws_bytes, void *stream)
+{
+    if (N != 0 && (!x || !dy || !mean || !rstd || !dx || x == dx || dy == dx)) return kErrInvalidArg;
+    LayerNormArgs a = {};
+    a.x = x; a.x_stride = x_stride; a.dy = dy; a.dy_stride = dy_stride; a.out = dx; a.out_stride = dx_stride;
+    a.gamma = static_cast<const float *>(gamma);
+    a.mean = static_cast<float *>(const_cast<void *>(mean)); a.rstd = static_cast<float *>(const_cast<void *>(rstd));
+    a.dgamma = static_cast<float *>(dgamma); a.dbeta = static_cast<float *>(dbeta);
+    return layer_norm_bwd_common(a, false, N, C, dtype, ws, ws_bytes, stream);
+}
+
+int layer_norm_bwd_kept(const void *codes, const void *scales, const void *dy, int64_t dy_stride, const void *gamma,
+                        const void *mean, const void *rstd, void *dx, int64_t dx_stride, void *dgamma, void *dbeta, int N, int C,
+                        int dtype, void *ws, size_t ws_bytes, void *stream)
+{
+    if (N != 0 && (!codes || !scales || !dy || !mean || !rstd || !dx || dy == dx || codes == dx || scales == dx)) return kErrInvalidArg;
+    LayerNormArgs a = {};
+    a.codes = static_cast<const unsigned char *>(codes); a.scales = static_cast<const unsigned char *>(scales);
+    a.dy = dy; a.dy_stride = dy_stride; a.out = dx; a.out_stride = dx_stride;
+    a.gamma = static_cast<const float *>(gamma);
+    a.mean = static_cast<float *>(const_cast<void *>(mean)); a.rstd = static_cast<float *>(const_cast<void *>(rstd));
+    a.dgamma = static_cast<float *>(dgamma); a.dbeta = static_cast<float *>(dbeta);
+    return layer_norm_bwd_common(a, true, N, C, dtype, ws, ws_bytes, stream);
+}
+
+size_t fc_kept_workspace_bytes(int N, int I, int O, int dtype)
+{
+    KeptGradPlan p;
+    return plan_kept_grad(p, N, I, O, dtype) == kStatusOk ? p.part_bytes : 0;
+}
+
+int fc_bwd_filter_kept(const void *codes, const void *scales, const void *dy, void *dw, int N, int I, int O, int dtype, void *ws,
+                       size_t ws_bytes, void *stream)
+{
+    if (!dw || (N != 0 && (!codes || !scales || !dy || dw == dy || dw == codes || dw == scales))) return kErrInvalidArg;
+    KeptGradPlan p;
+    const int rc = plan_kept_grad(p, N, I, O, dtype);
+    if (rc != kStatusOk) return rc;
+    const size_t eb = glue_elem_bytes(dtype);
+    if (!blocks_aligned(codes, scales) || !aligned(dy, eb) || !aligned(dw, 4)) return kErrMisaligned;
+    if (p.part_bytes) {
+        if (!ws || ws_bytes < p.part_bytes) return kErrWorkspace;
+        if (!aligned(ws, 256)) return kErrMisaligned;
+    }
+    KeptGradArgs &a = p.a;
+    a.codes = static_cast<const unsigned char *>(codes); a.scales = static_cast<const unsigned char *>(scales);
+    a.dy = dy;
+    a.dw = static_cast<float *>(a.splits > 1 ? ws : dw);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (eb == 4) launch(fc_grad_kept_kernel<float>, p.blocks, 256, 0, st, a);
+    else launch(fc_grad_kept_kernel<Bf16>, p.blocks, 256, 0, st, a);
+    if (a.splits > 1) {
+        const int64_t count = (int64_t)I * O;
+        hipLaunchKernelGGL(fc_grad_join, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, a.dw, static_cast<float *>(dw),
+                           count, a.splits);
+    }
+    return check_launch();
+}
+
+size_t fc_q4_workspace_bytes(int N, int I, int O, int dtype)
+{
+    return check_q4(N, I, O, dtype) == kStatusOk ? q4_bytes(N, I) : 0;
+}
+
+int fc_fwd_q4(const void *x, const void *w_codes, const void *w_scales, const void *bias, void *y, int N, int I, int O, int relu,
+              int dtype, void *ws, size_t ws_bytes, void *stream)
+{
+    if (N != 0 && (!x || !w_codes || !w_scales || !y || x == y || w_codes == y || w_scales == y)) return kErrInvalidArg;
+    const int rc = check_q4(N, I, O, dtype);
+    if (rc != kStatusOk) return rc;
+    const size_t eb = glue_elem_bytes(dtype);
+    if (!aligned(x, eb) || !blocks_aligned(w_codes, w_scales) || !aligned(bias, 4) || !aligned(y, dtype == kDtypeBf16OutBf16 ? 2 : 4))
+        return kErrMisaligned;
+    if (N == 0) return kStatusOk;
+    if (!ws || ws_bytes < q4_bytes(N, I)) return kErrWorkspace;
+    if (!aligned(ws, 256)) return kErrMisaligned;
+    unsigned char *const xc = static_cast<unsigned char *>(ws), *const xs = xc + q4_codes_bytes(N, I);
+    const int made = quantize_blocks(x, I, xc, xs, N, I, kE2M1, dtype, stream);
+    if (made != kStatusOk) return made;
+    Q4Args a = {};
+    a.xc = xc; a.xs = xs;
+    a.wc = static_cast<const unsigned char *>(w_codes); a.ws = static_cast<const unsigned char *>(w_scales);
+    a.bias = static_cast<const float *>(bias);
+    a.y = y;
+    a.N = N; a.I = I; a.O = O; a.steps = (int)(pitch_of(I) / 128); a.relu = relu;
+    a.ntiles = ceil_div(N, 128); a.otiles = ceil_div(O, 128);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return dtype == kDtypeBf16OutBf16 ? run_q4<Bf16>(a, st) : run_q4<float>(a, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,268 @@
+"""Tensors held in blocks of 8 and 4 bits on the GPU, the filter gradient and the forward pass of a fully connected layer on
+them, against the oracle in 64 bits.
+
+Codes, exponents and the values read back are compared bit for bit.  The bounds of the products: u = 2^-24 is one fp32
+rounding; every single product is exact, and a sum of n of them, in whatever order the matrix instructions take it, with every
+addition rounded or cut off (2 u), is within 2 u n of the sum of magnitudes.  A result stored as bfloat16 adds 2^-8 of itself."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_1312_5853_amd import binding as hp
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+FORMS = ["e4m3", "e2m1"]
+RNG = lambda s: np.random.Generator(np.random.Philox(s))
+
+
+def _values(shape, dtype, seed, std=1.0):
+    g = RNG(seed)
+    a = (std * g.standard_normal(shape) * np.exp2(g.integers(-6, 6, (shape[0], 1)))).astype(np.float32)
+    a[g.random(shape) < 0.2] = 0.0
+    return oracle.bf16_round(a) if dtype == "bf16" else a
+
+
+def _dev(a, dtype="f32", pitch=0, off=0):
+    N, C = a.shape
+    pitch = pitch or C
+    buf = torch.full((off + max(N, 1) * pitch,), 77.0, dtype=DTYPES[dtype], device="cuda")
+    t = buf[off:off + N * pitch].view(N, pitch)[:, :C]
+    t.copy_(torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)))
+    return t
+
+
+def _held(a, form):
+    """An array in blocks on the GPU, made by the oracle, and its values."""
+    codes, scales = oracle.quantize_blocks(a, form)
+    q = hp.Blocks(torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), a.shape[1], form)
+    return q, oracle.dequantize_blocks(codes, scales, a.shape[1], form)
+
+
+def _host(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+def check_blocks(x, form, dtype, **place):
+    N, C = x.shape
+    q = hp.Blocks.empty(N, C, form)
+    q.codes.fill_(0xA5)
+    q.scales.fill_(0xA5)
+    assert hp.quantize_blocks(_dev(x, dtype, **place), form, out=q) is q
+    codes, scales = oracle.quantize_blocks(x, form)
+    assert np.array_equal(q.scales.cpu().numpy(), scales)
+    assert np.array_equal(q.codes.cpu().numpy(), codes)
+    want = oracle.dequantize_blocks(codes, scales, C, form)
+    for d in ("f32", "bf16"):
+        out = _dev(np.full((N, C), 5.0), d, **place)
+        assert hp.dequantize_blocks(q, x=out) is out
+        with np.errstate(over="ignore"):
+            assert np.array_equal(_host(out), want.astype(np.float32).astype(np.float64), equal_nan=True)
+    return q
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("N,C", [(1, 1), (3, 2), (2, 7), (5, 8), (4, 31), (3, 32), (2, 33), (7, 100), (2, 127), (9, 128), (3, 129), (1, 2048),
+                                 (2, 2049), (130, 40), (33, 1000), (17, 4097), (1, 70001)])
+def test_blocks_bit_for_bit(N, C, form, dtype):
+    check_blocks(_values((N, C), dtype, N * 1000 + C), form, dtype)
+    if C > 4:
+        check_blocks(_values((N, C), dtype, N * 1000 + C), form, dtype, pitch=C + 3, off=1)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_every_magnitude(form):
+    """Every exponent of fp32, normal and not, ties, zeros of both signs, the largest finite values, infinities and NaN."""
+    g = RNG(1)
+    x = (g.uniform(1, 2, (255, 96)) * np.where(g.random((255, 96)) < 0.5, -1, 1)).astype(np.float32)
+    x = np.ldexp(x, np.arange(-127, 128)[:, None] + g.integers(-14, 1, (255, 96))).astype(np.float32)
+    x[:, 5], x[:, 40] = 0.0, -0.0
+    check_blocks(x, form, "f32")
+    steps = np.concatenate([oracle.block_magnitudes(form), (oracle.block_magnitudes(form)[1:] + oracle.block_magnitudes(form)[:-1]) / 2])
+    ties = np.zeros((len(steps), 64), np.float32)
+    ties[:, 0], ties[:, 1], ties[:, 2] = oracle.block_magnitudes(form)[-1], steps, -steps
+    ties[:, 32:] = np.ldexp(ties[:, :32], -30)
+    check_blocks(ties, form, "f32")
+    odd = np.ones((8, 40), np.float32)
+    odd[0, 3], odd[1, 35], odd[2, 0], odd[3, 39] = np.inf, np.nan, -np.inf, np.nan
+    odd[4, 1], odd[5, 33], odd[6, :], odd[7, 2] = 3.4028235e38, -3.4028235e38, 1e-45, np.float32(2.0 ** 126)
+    check_blocks(odd, form, "f32")
+
+
+def test_empty_and_untouched():
+    for form in FORMS:
+        q = hp.quantize_blocks(torch.zeros((0, 9), device="cuda"), form)
+        assert q.shape == (0, 9) and hp.dequantize_blocks(q).shape == (0, 9)
+        x = torch.full((4, 50), 7.0, device="cuda")
+        hp.dequantize_blocks(hp.quantize_blocks(torch.ones((4, 45), device="cuda"), form), x=x[:, :45])
+        assert (x[:, :45] == 1.0).all() and (x[:, 45:] == 7.0).all()
+
+
+# --------------------------------------------------------- the filter gradient
+def check_grad(x, dy, dtype):
+    q, held = _held(x, "e4m3")
+    dw = torch.full((dy.shape[1], x.shape[1]), float("nan"), device="cuda")
+    got = _host(hp.fc_bwd_filter_kept(q, _dev(dy, dtype), dw=dw))
+    dy = dy.astype(np.float64)
+    want, size = dy.T @ held, np.abs(dy).T @ np.abs(held)
+    n = len(x) * (3 if dtype == "f32" else 1) + 64                   # products, and the joins of the sum's parts
+    err = np.abs(got - want)
+    assert (err <= 2 * U * n * size + 1e-37).all(), (err / (2 * U * n * size + 1e-37)).max()
+    return got
+
+
+GRADS = [(1, 1, 1), (1, 130, 5), (2, 32, 33), (3, 7, 300), (15, 127, 31), (16, 128, 128), (17, 129, 127), (31, 64, 129), (32, 300, 257),
+         (33, 255, 256), (64, 256, 255), (65, 520, 100), (128, 384, 640), (129, 1000, 70), (500, 40, 24), (1000, 96, 1000), (3000, 130, 130),
+         (9001, 33, 5)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,I,O", GRADS)
+def test_filter_gradient(N, I, O, dtype):
+    check_grad(_values((N, I), dtype, N + I), _values((N, O), dtype, N + O, 1e-3), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,I,O", [(5, 40, 9), (130, 300, 260), (4100, 64, 100)])
+def test_filter_gradient_of_whole_numbers_is_exact(N, I, O, dtype):
+    """Sums of products of small whole numbers are whole numbers below 2^24."""
+    g = RNG(N)
+    x, dy = g.integers(-8, 9, (N, I)).astype(np.float32), g.integers(-16, 17, (N, O)).astype(np.float32)
+    q, held = _held(x, "e4m3")
+    assert np.array_equal(held, x)
+    assert np.array_equal(_host(hp.fc_bwd_filter_kept(q, _dev(dy, dtype))), dy.astype(np.float64).T @ x)
+
+
+def test_filter_gradient_keeps_every_bit_of_fp32():
+    """One sample of ones: dw is dy, whatever its magnitude; 24 bits of it, far ones too.  The last of the three parts holds
+    what lies 2^-23 of a value's leading bit and above in steps of 2^-133 at least, bfloat16's least: values from 2^-110 on
+    (2^-110 2^-23 = 2^-133) are held exactly, and of smaller ones less than 2^-133 is cut off."""
+    g = RNG(2)
+    dy = np.ldexp(g.uniform(1, 2, (1, 254)), np.arange(-126, 128)).astype(np.float32)
+    dy[0, :3] = 3.4028235e38, -3.4028235e38, 1.1754944e-38
+    q, _ = _held(np.ones((1, 70), np.float32), "e4m3")
+    got = hp.fc_bwd_filter_kept(q, _dev(dy)).cpu().numpy()
+    far = np.abs(dy[0]) >= 2.0 ** -110
+    assert np.array_equal(got[far], np.repeat(dy.T[far], 70, axis=1))
+    assert (np.abs(got.astype(np.float64) - dy.T.astype(np.float64)) < 2.0 ** -133).all(axis=1)[~far].all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_values_that_are_no_numbers_in_the_gradient(dtype):
+    x, dy = np.ones((70, 200), np.float32), np.ones((70, 90), np.float32)
+    dy[3, 5], dy[60, 7], dy[1, 80] = np.inf, -np.inf, np.nan
+    got = _host(hp.fc_bwd_filter_kept(_held(x, "e4m3")[0], _dev(dy, dtype)))
+    assert (got[5] == np.inf).all() and (got[7] == -np.inf).all() and np.isnan(got[80]).all()
+    rest = [o for o in range(90) if o not in (5, 7, 80)]
+    assert (got[rest] == 70).all()
+    x[9, 40] = np.nan                                              # block 1 of sample 9 is no number
+    got = _host(hp.fc_bwd_filter_kept(_held(x, "e4m3")[0], _dev(np.ones((70, 90), np.float32), dtype)))
+    assert np.isnan(got[:, 32:64]).all() and (got[:, :32] == 70).all() and (got[:, 64:] == 70).all()
+
+
+def test_filter_gradient_of_no_samples():
+    dw = torch.full((7, 40), 3.0, device="cuda")
+    hp.fc_bwd_filter_kept(hp.Blocks.empty(0, 40, "e4m3"), torch.zeros((0, 7), device="cuda"), dw=dw)
+    assert not dw.any()
+
+
+# --------------------------------------------------------- the forward pass in 4 bits
+def check_prod(x, w, bias, relu, dtype, out_bf16=False):
+    q, held = _held(w, "e2m1")
+    xv = oracle.dequantize_blocks(*oracle.quantize_blocks(x, "e2m1"), x.shape[1], "e2m1")
+    N, O = len(x), len(w)
+    y = torch.full((N, O), float("nan"), device="cuda", dtype=torch.bfloat16 if out_bf16 else torch.float32)
+    b = None if bias is None else torch.from_numpy(bias).cuda()
+    got = _host(hp.fc_fwd_q4(_dev(x, dtype), q, b, relu=relu, y=y))
+    want, size = xv @ held.T, np.abs(xv) @ np.abs(held).T
+    if bias is not None:
+        want, size = want + bias.astype(np.float64), size + np.abs(bias)
+    if relu:
+        want = np.maximum(want, 0.0)
+    bound = 2 * U * (x.shape[1] + 64) * size + (2.0 ** -8 * np.abs(want) if out_bf16 else 0.0) + 1e-37
+    if out_bf16:
+        bound = bound * (1 + 2.0 ** -8)                            # of a sum that is itself off by as much
+    err = np.abs(got - want)
+    assert (err <= bound).all(), (err / bound).max()
+    return got
+
+
+PRODS = [(1, 1, 1), (1, 128, 16), (1, 4096, 40), (2, 33, 100), (3, 1000, 17), (4, 129, 31), (7, 256, 1000), (8, 640, 33), (15, 127, 300),
+         (16, 384, 64), (17, 512, 129), (31, 40, 48), (32, 2000, 65), (33, 96, 257), (64, 128, 128), (65, 260, 127), (100, 1025, 70),
+         (128, 512, 256), (129, 300, 384), (257, 900, 130), (300, 640, 513), (1000, 64, 24)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,I,O", PRODS)
+def test_forward_in_four_bits(N, I, O, dtype):
+    g = RNG(N + I + O)
+    x, w, bias = _values((N, I), dtype, N + I), _values((O, I), "f32", I + O, 0.05), g.normal(size=O).astype(np.float32)
+    check_prod(x, w, bias, (N + I) % 2 == 0, dtype)
+    check_prod(x, w, None, False, dtype, out_bf16=dtype == "bf16")
+
+
+@pytest.mark.parametrize("N,I,O", [(1, 100, 20), (5, 1000, 70), (16, 4096, 33), (40, 300, 60), (260, 520, 300)])
+def test_forward_of_whole_numbers_is_exact(N, I, O):
+    g = RNG(N)
+    x = g.choice([0, 1, 2, 3, 4, 6, -1, -2, -3, -4, -6], (N, I)).astype(np.float32)
+    w = g.choice([0, 1, 2, 3, 4, 6, -1, -2, -3, -4, -6], (O, I)).astype(np.float32)
+    x[:, ::32] = 6.0
+    w[:, ::32] = -6.0
+    q, held = _held(w, "e2m1")
+    assert np.array_equal(held, w)
+    bias = g.integers(-9, 9, O).astype(np.float32)
+    want = x.astype(np.float64) @ w.T + bias
+    assert np.array_equal(_host(hp.fc_fwd_q4(_dev(x), q, torch.from_numpy(bias).cuda())), want)
+    assert np.array_equal(_host(hp.fc_fwd_q4(_dev(x), q, torch.from_numpy(bias).cuda(), relu=True)), np.maximum(want, 0))
+
+
+@pytest.mark.parametrize("N", [1, 3, 40, 200])
+def test_values_that_are_no_numbers_in_the_forward_pass(N):
+    """A sample's make its own outputs NaN, a filter's its own output; ReLU keeps them."""
+    x, w = np.ones((N, 300), np.float32), np.ones((70, 300), np.float32)
+    x[N - 1, 290], w[33, 5] = np.inf, np.nan
+    got = _host(hp.fc_fwd_q4(_dev(x), _held(w, "e2m1")[0], relu=True))
+    assert np.isnan(got[N - 1]).all() and np.isnan(got[:, 33]).all()
+    rest = [o for o in range(70) if o != 33]
+    assert (got[:N - 1][:, rest] == 300).all()
+
+
+def test_forward_of_far_exponents():
+    """Products whose factors are far apart in size."""
+    x, w = np.full((3, 64), 2.0 ** 100, np.float32), np.full((5, 64), 2.0 ** -100, np.float32)
+    x[:, 32:] = 2.0 ** -90
+    w[:, 32:] = 2.0 ** 80
+    got = _host(hp.fc_fwd_q4(_dev(x), _held(w, "e2m1")[0]))
+    assert np.array_equal(got, np.full((3, 5), 32 + 32 * 2.0 ** -10))
+
+
+def test_forward_of_no_samples():
+    assert hp.fc_fwd_q4(torch.zeros((0, 40), device="cuda"), hp.Blocks.empty(9, 40, "e2m1")).shape == (0, 9)
+
+
+@pytest.mark.parametrize("N,I,O", [(1, 300, 50), (9, 2000, 40), (130, 300, 260)])
+def test_nothing_outside_the_outputs_is_written(N, I, O):
+    w, _ = _held(_values((O, I), "f32", 3), "e2m1")
+    q, _ = _held(_values((N, I), "f32", 4), "e4m3")
+    x, dy = _dev(_values((N, I), "f32", 5)), _dev(_values((N, O), "f32", 6))
+    for count, shape, call in ((N * O, (N, O), lambda o: hp.fc_fwd_q4(x, w, y=o)), (O * I, (O, I), lambda o: hp.fc_bwd_filter_kept(q, dy, dw=o))):
+        buf = torch.full((count + 131,), 7.0, device="cuda")
+        out = buf[3:3 + count].view(shape)
+        out.fill_(float("nan"))
+        call(out)
+        assert not torch.isnan(out).any()
+        out.fill_(7.0)
+        assert (buf == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_same_bits_every_time(dtype):
+    q, _ = _held(_values((900, 200), dtype, 7), "e4m3")
+    w, _ = _held(_values((300, 1500), "f32", 8), "e2m1")
+    dy, x, few = _dev(_values((900, 170), dtype, 9), dtype), _dev(_values((200, 1500), dtype, 10), dtype), _dev(_values((2, 1500), dtype, 11), dtype)
+    first = [hp.fc_bwd_filter_kept(q, dy), hp.fc_fwd_q4(x, w), hp.fc_fwd_q4(few, w)]
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(first, [hp.fc_bwd_filter_kept(q, dy), hp.fc_fwd_q4(x, w), hp.fc_fwd_q4(few, w)]))

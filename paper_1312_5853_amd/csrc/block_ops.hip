@@ -235,13 +235,39 @@ int check_q4(int N, int I, int O, int dtype)
     if (N * pitch_of(I) >= kMaxElements || O * pitch_of(I) >= kMaxElements || (int64_t)N * O >= kMaxElements) return kErrTooLarge;
     return kStatusOk;
 }
-size_t q4_codes_bytes(int N, int I) { return (size_t)round_up64(N * pitch_of(I) / 2, 256); }
-size_t q4_bytes(int N, int I) { return q4_codes_bytes(N, I) + (size_t)round_up64(N * pitch_of(I) / kBlock, 256); }
+
+constexpr int kQ4Tile = 256;                         // outputs, and samples, of a tile
+
+// Where a call's scratch lies: x's codes, and the exponents of both operands by steps.
+struct Q4Plan {
+    int steps, nrows, orows;
+    size_t xs, ws, total;
+};
+
+Q4Plan plan_q4(int N, int I, int O)
+{
+    Q4Plan p;
+    p.steps = (int)(pitch_of(I) / kRowFill);
+    p.nrows = round_up(N, kQ4Tile);
+    p.orows = round_up(O, kQ4Tile);
+    p.xs = (size_t)round_up64((int64_t)N * p.steps * 64, 256);
+    p.ws = p.xs + (size_t)p.steps * p.nrows * 4;
+    p.total = p.ws + (size_t)p.steps * p.orows * 4;
+    return p;
+}
 
 template <typename T>
-int run_q4(const Q4Args &a, hipStream_t st)
+void run_q4_prepare(const Q4PrepArgs &p, hipStream_t st)
 {
-    launch(fc_q4_tiles<T>, (int64_t)a.ntiles * a.otiles, 256, 0, st, a);
+    launch(q4_prepare<T>, (int64_t)p.x_blocks + (int64_t)p.s_tiles * ceil_div(p.O, 32), 256, 0, st, p);
+}
+
+template <typename T>
+int run_q4(Q4TileArgs &a, hipStream_t st)
+{
+    a.ntiles = ceil_div(a.N, kQ4Tile); a.otiles = ceil_div(a.O, kQ4Tile);
+    a.per_xcd = ceil_div(a.ntiles * a.otiles, 8);
+    launch(fc_q4_tiles<T, 4, 4, 2, 2>, (int64_t)8 * a.per_xcd, 256, kQ4Stages * 2 * kQ4Tile * 68, st, a);
     return check_launch();
 }
 
@@ -362,7 +388,7 @@ int fc_bwd_filter_kept(const void *codes, const void *scales, const void *dy, vo
 
 size_t fc_q4_workspace_bytes(int N, int I, int O, int dtype)
 {
-    return check_q4(N, I, O, dtype) == kStatusOk ? q4_bytes(N, I) : 0;
+    return check_q4(N, I, O, dtype) == kStatusOk ? plan_q4(N, I, O).total : 0;
 }
 
 int fc_fwd_q4(const void *x, const void *w_codes, const void *w_scales, const void *bias, void *y, int N, int I, int O, int relu,
@@ -375,19 +401,30 @@ int fc_fwd_q4(const void *x, const void *w_codes, const void *w_scales, const vo
     if (!aligned(x, eb) || !blocks_aligned(w_codes, w_scales) || !aligned(bias, 4) || !aligned(y, dtype == kDtypeBf16OutBf16 ? 2 : 4))
         return kErrMisaligned;
     if (N == 0) return kStatusOk;
-    if (!ws || ws_bytes < q4_bytes(N, I)) return kErrWorkspace;
+    const Q4Plan plan = plan_q4(N, I, O);
+    if (!ws || ws_bytes < plan.total) return kErrWorkspace;
     if (!aligned(ws, 256)) return kErrMisaligned;
-    unsigned char *const xc = static_cast<unsigned char *>(ws), *const xs = xc + q4_codes_bytes(N, I);
-    const int made = quantize_blocks(x, I, xc, xs, N, I, kE2M1, dtype, stream);
-    if (made != kStatusOk) return made;
-    Q4Args a = {};
-    a.xc = xc; a.xs = xs;
-    a.wc = static_cast<const unsigned char *>(w_codes); a.ws = static_cast<const unsigned char *>(w_scales);
+    unsigned char *const scratch = static_cast<unsigned char *>(ws);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    Q4PrepArgs p = {};
+    p.x.in = x; p.x.out = scratch; p.x.stride = I; p.x.C = I;
+    p.x.per_row = plan.steps * 16;
+    p.x.total = (int64_t)N * p.x.per_row;
+    p.x.div = make_fastdiv(p.x.per_row);
+    p.w_scales = static_cast<const unsigned *>(w_scales);
+    p.xs = reinterpret_cast<unsigned *>(scratch + plan.xs); p.ws = reinterpret_cast<unsigned *>(scratch + plan.ws);
+    p.O = O; p.steps = plan.steps; p.nrows = plan.nrows; p.orows = plan.orows;
+    p.x_blocks = (int)((p.x.total + 255) / 256);
+    p.s_tiles = ceil_div(plan.steps, 32);
+    if (eb == 4) run_q4_prepare<float>(p, st);
+    else run_q4_prepare<Bf16>(p, st);
+    Q4TileArgs a = {};
+    a.xc = scratch; a.xs = scratch + plan.xs;
+    a.wc = static_cast<const unsigned char *>(w_codes); a.ws = scratch + plan.ws;
     a.bias = static_cast<const float *>(bias);
     a.y = y;
-    a.N = N; a.I = I; a.O = O; a.steps = (int)(pitch_of(I) / 128); a.relu = relu;
-    a.ntiles = ceil_div(N, 128); a.otiles = ceil_div(O, 128);
-    hipStream_t st = static_cast<hipStream_t>(stream);
+    a.N = N; a.O = O; a.steps = plan.steps; a.relu = relu;
+    a.nrows = plan.nrows; a.orows = plan.orows;
     return dtype == kDtypeBf16OutBf16 ? run_q4<Bf16>(a, st) : run_q4<float>(a, st);
 }
 

@@ -24,8 +24,8 @@ __device__ __forceinline__ f32x4 mfma_q4(const i32x4 &w, const i32x4 &x, const f
 }
 
 // four neighbouring outputs of sample n
-template <typename T>
-__device__ __forceinline__ void store_q4(const Q4Args &a, int n, int o, const f32x4 &s)
+template <typename T, typename Args>
+__device__ __forceinline__ void store_q4(const Args &a, int n, int o, const f32x4 &s)
 {
     if (n >= a.N) return;
     T *const y = static_cast<T *>(a.y) + (int64_t)n * a.O;
@@ -38,44 +38,187 @@ __device__ __forceinline__ void store_q4(const Q4Args &a, int n, int o, const f3
         }
 }
 
-// 128 x 128 outputs to a work-group, 64 x 64 to a wavefront, operands straight from memory
-template <typename T>
-__global__ __launch_bounds__(256) void fc_q4_tiles(const Q4Args a)
+// ---------------------------------------------------------------------------
+// Many samples: tiles of TM WM 32 outputs x TN WN 32 samples
+// ---------------------------------------------------------------------------
+// v_mfma_scale_f32_32x32x64_f8f6f4: lane l has row l % 32 and the 32 values of block l / 32.  Both operands go from global memory
+// straight into LDS, a row's 64 bytes of a step as four pieces of 16, the piece c of row r at place c ^ (r / 4 % 4): the rows are
+// 64 bytes apart, and the 16 lanes of a phase of ds_read_b128 then cover all banks.  The exponents of a step lie together (see
+// q4_prepare), four bytes to a row; a lane shifts its block's to the low byte.
+//
+// LDS: kQ4Stages buffers; step s is multiplied while those of s + 1 .. s + kQ4Stages - 1 are on their way.
+struct Q4TileArgs {
+    const unsigned char *xc, *wc;                // codes, rows of 64 steps bytes
+    const unsigned char *xs, *ws;                // exponents [steps][rows filled up][4]
+    const float *bias;
+    void *y;
+    int N, O, steps, relu;
+    int nrows, orows;                            // rows of the exponents, multiples of the tile
+    int ntiles, otiles, per_xcd;
+};
+
+constexpr int kQ4Stages = 4;
+
+__device__ __forceinline__ void dma16(const void *base, unsigned offset, unsigned lds)       // 16 bytes to a lane, at lds + 16 lane
 {
-    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-    const int nt = blockIdx.x % a.ntiles, ot = blockIdx.x / a.ntiles;
-    const int n0 = nt * 128 + (wave & 1) * 64, o0 = ot * 128 + (wave >> 1) * 64;
-    const int r = lane & 15, g = lane >> 4;
-    const int64_t cpitch = (int64_t)a.steps * 64, spitch = (int64_t)a.steps * 4;
-    const unsigned char *xc[4], *wc[4], *xs[4], *ws[4];
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds), "v"(offset), "s"(base) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
+
+__device__ __forceinline__ f32x16 mfma_q4_wide(const i32x4 &w, const i32x4 &x, const f32x16 &c, unsigned ws, unsigned xs, int second)
+{
+    const i32x8 a = {w[0], w[1], w[2], w[3], 0, 0, 0, 0}, b = {x[0], x[1], x[2], x[3], 0, 0, 0, 0};
+    return second ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 4, 2, (int)ws, 2, (int)xs)
+                  : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 4, 0, (int)ws, 0, (int)xs);
+}
+
+template <typename T, int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64) void fc_q4_tiles(const Q4TileArgs a)
+{
+    constexpr int NT = WM * WN * 64, BM = TM * WM * 32, BN = TN * WN * 32;
+    constexpr int NA = BM * 4 / NT, NB = BN * 4 / NT;            // loads of codes to a thread and step
+    constexpr int CODES = (BM + BN) * 64, STAGE = CODES + (BM + BN) * 4;
+    constexpr int SL = (BM + BN) / 4 / (WM * WN);                // lanes of a wavefront that load exponents, 16 bytes each
+    constexpr int LOADS = NA + NB + 1;
+    static_assert(SL <= 64 && BM % (4 * SL) == 0, "exponents");
+    extern __shared__ __attribute__((aligned(16))) char lds_q4[];
+    const unsigned lds0 = (unsigned)(size_t)lds_q4;
+    const int unit = (blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
+    if (unit >= a.ntiles * a.otiles) return;
+    const int ot = unit % a.otiles, nt = unit / a.otiles;
+    const int o0 = ot * BM, n0 = nt * BN;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    const unsigned pitch = (unsigned)a.steps * 64;
+
+    // load u of a thread: piece q % 4 of row q / 4, q = (wave loads + u) 64 + lane; rows past the end read the last one
+    unsigned aoff[NA], boff[NB];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {                // rows past the end read the last one; their sums are not stored
-        const int64_t n = min(n0 + k * 16 + r, a.N - 1), o = min(o0 + k * 16 + r, a.O - 1);
-        xc[k] = a.xc + n * cpitch + g * 16; wc[k] = a.wc + o * cpitch + g * 16;
-        xs[k] = a.xs + n * spitch + g; ws[k] = a.ws + o * spitch + g;
+    for (int u = 0; u < NA; ++u) {
+        const int q = (wave * NA + u) * 64 + lane, row = q >> 2, c = (q & 3) ^ ((row >> 2) & 3);
+        aoff[u] = (unsigned)min(row, a.O - 1 - o0) * pitch + c * 16;
     }
-    f32x4 acc[4][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int u = 0; u < NB; ++u) {
+        const int q = (wave * NB + u) * 64 + lane, row = q >> 2, c = (q & 3) ^ ((row >> 2) & 3);
+        boff[u] = (unsigned)min(row, a.N - 1 - n0) * pitch + c * 16;
+    }
+    const unsigned char *wc = a.wc + (int64_t)o0 * pitch, *xc = a.xc + (int64_t)n0 * pitch;
+    // exponents: the wavefront's part of the stage's BM + BN words, w's first
+    const int sfirst = wave * SL * 4;
+    const bool of_w = sfirst < BM;
+    const unsigned char *sp = of_w ? a.ws + (int64_t)(o0 + sfirst) * 4 : a.xs + (int64_t)(n0 + sfirst - BM) * 4;
+    const int64_t s_step = (int64_t)(of_w ? a.orows : a.nrows) * 4;
+
+    auto load_step = [&](int buf) {
+        const unsigned l = lds0 + buf * STAGE;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.steps; ++s) {
-        i32x4 x[4], w[4];
-        unsigned sx[4], sw[4];
+        for (int u = 0; u < NA; ++u) dma16(wc, aoff[u], l + (wave * NA + u) * 1024);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            x[k] = *reinterpret_cast<const i32x4 *>(xc[k] + (int64_t)s * 64);
-            w[k] = *reinterpret_cast<const i32x4 *>(wc[k] + (int64_t)s * 64);
-            sx[k] = xs[k][(int64_t)s * 4];
-            sw[k] = ws[k][(int64_t)s * 4];
+        for (int u = 0; u < NB; ++u) dma16(xc, boff[u], l + BM * 64 + (wave * NB + u) * 1024);
+        if (lane < SL) dma16(sp, lane * 16, l + CODES + sfirst * 4);
+        wc += 64; xc += 64; sp += s_step;
+    };
+
+    f32x16 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+
+    const int r = lane & 31, half = lane >> 5, swz = (r >> 2) & 3;
+    const int arow = (wm * TM * 32 + r) * 64, brow = BM * 64 + (wn * TN * 32 + r) * 64;
+    const int sa = CODES + (wm * TM * 32 + r) * 4, sb = CODES + (BM + wn * TN * 32 + r) * 4;
+
+    const int steps = a.steps;
+#pragma unroll
+    for (int s = 0; s < kQ4Stages - 1; ++s)
+        if (s < steps) load_step(s);
+    int buf = 0;
+    for (int s = 0; s < steps; ++s) {
+        // this wavefront's loads of step s have landed when at most those of the steps after it are left
+        if (s + kQ4Stages - 2 < steps) wait_vmcnt<(kQ4Stages - 2) * LOADS>();
+        else wait_vmcnt<0>();
+        __syncthreads();
+        const int next = buf == 0 ? kQ4Stages - 1 : buf - 1;      // step s - 1's buffer: every wavefront is past it
+        if (s + kQ4Stages - 1 < steps) load_step(next);
+        const char *const p = lds_q4 + buf * STAGE;
+        unsigned es[TM], ex[TN];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) es[i] = *reinterpret_cast<const unsigned *>(p + sa + i * 128) >> (8 * half);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) ex[j] = *reinterpret_cast<const unsigned *>(p + sb + j * 128) >> (8 * half);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            i32x4 w[TM], x[TN];
+            const int at = ((2 * k + half) ^ swz) * 16;
+#pragma unroll
+            for (int i = 0; i < TM; ++i) w[i] = *reinterpret_cast<const i32x4 *>(p + arow + i * 2048 + at);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) x[j] = *reinterpret_cast<const i32x4 *>(p + brow + j * 2048 + at);
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j] = mfma_q4_wide(w[i], x[j], acc[i][j], es[i], ex[j], k);
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = mfma_q4(w[i], x[j], acc[i][j], sw[i], sx[j]);
+        buf = buf == kQ4Stages - 1 ? 0 : buf + 1;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) store_q4<T>(a, n0 + j * 16 + r, o0 + i * 16 + g * 4, acc[i][j]);
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                store_q4<T>(a, n0 + (wn * TN + j) * 32 + r, o0 + (wm * TM + i) * 32 + q * 8 + half * 4,
+                            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
+}
+
+// Before the tiles: x in blocks, and the exponents of both operands as the tiles load them, [step][row][4 bytes], in one launch.
+struct Q4PrepArgs {
+    BlockArgs x;                                 // total, per_row and so on; scales unused
+    const unsigned *w_scales;                    // [O][steps] words
+    unsigned *xs, *ws;                           // [steps][nrows], [steps][orows]
+    int O, steps, nrows, orows;
+    int x_blocks, s_tiles;                       // work-groups that take x; tiles of 32 steps to a row of tiles
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void q4_prepare(const Q4PrepArgs p)
+{
+    if ((int)blockIdx.x < p.x_blocks) {
+        const BlockArgs &a = p.x;
+        const int64_t base = (int64_t)blockIdx.x * 256, i = base + threadIdx.x;
+        const int64_t row0 = base / a.per_row;
+        const unsigned at = (unsigned)(base - row0 * a.per_row) + threadIdx.x;
+        const unsigned down = fastdiv(at, a.div);
+        const int64_t row = row0 + down;
+        const int v8 = (int)(at - down * a.per_row);
+        if (i >= a.total) return;
+        float v[8];
+        load8(static_cast<const T *>(a.in) + row * a.stride + v8 * 8, a.C - v8 * 8, v);
+        unsigned word[2];
+        const int byte = into_codes<kE2M1>(v, word);
+        static_cast<unsigned *>(a.out)[i] = word[0];
+        if (v8 % 4 == 0) reinterpret_cast<unsigned char *>(p.xs)[((int64_t)(v8 >> 4) * p.nrows + row) * 4 + ((v8 >> 2) & 3)] = (unsigned char)byte;
+        return;
+    }
+    // 32 x 32 words of w's exponents turned round
+    __shared__ unsigned turned[32][33];
+    const int b = blockIdx.x - p.x_blocks;
+    const int rt = b / p.s_tiles, st = b - rt * p.s_tiles;
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+#pragma unroll
+    for (int k = 0; k < 32; k += 8) {
+        const int o = rt * 32 + ty + k, s = st * 32 + tx;
+        if (o < p.O && s < p.steps) turned[ty + k][tx] = p.w_scales[(int64_t)o * p.steps + s];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 32; k += 8) {
+        const int s = st * 32 + ty + k, o = rt * 32 + tx;
+        if (o < p.O && s < p.steps) p.ws[(int64_t)s * p.orows + o] = turned[tx][ty + k];
+    }
 }

@@ -23,19 +23,61 @@ __device__ __forceinline__ f32x4 mfma_q4(const i32x4 &w, const i32x4 &x, const f
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 4, 0, (int)ws, 0, (int)xs);
 }
 
-// four neighbouring outputs of sample n
-template <typename T, typename Args>
-__device__ __forceinline__ void store_q4(const Args &a, int n, int o, const f32x4 &s)
+// f(s + bias); NaN stays
+__device__ __forceinline__ float finish_q4(float s, float bias, int relu)
 {
-    if (n >= a.N) return;
+    s += bias;
+    return relu && s < 0.f ? 0.f : s;
+}
+
+// 32 outputs from o0 on of sample n, as v_mfma_scale_f32_32x32x64 leaves them: value 4 q + k of a lane is output 8 q + 4 half + k.
+// fp32: four neighbouring ones are 16 bytes.  bfloat16: the lanes of the two halves trade what makes eight of them (a lane of the
+// lower half gets those from 8 q on, its partner those from 8 (q + 1) on), 16 bytes as well; with a store to every value, 256
+// instructions to a wavefront that each touch 64 rows, the stores of a tile took as long as 40 of its steps.
+template <typename T, typename Args>
+__device__ __forceinline__ void store_block_q4(const Args &a, int n, int o0, int half, const f32x16 &s)
+{
     T *const y = static_cast<T *>(a.y) + (int64_t)n * a.O;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (o + k < a.O) {
-            float v = s[k] + (a.bias ? a.bias[o + k] : 0.f);
-            if (a.relu) v = v > 0.f ? v : (v != v ? v : 0.f);
-            st_elem(y, o + k, v);
+    for (int q = 0; q < 4; q += 2) {
+        float v[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int o = o0 + 8 * (q + h) + 4 * half;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                v[h][k] = finish_q4(s[4 * (q + h) + k], a.bias && o + k < a.O ? a.bias[o + k] : 0.f, a.relu);
         }
+        if constexpr (sizeof(T) == 2) {
+            unsigned w[2][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    w[h][k] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2){v[h][2 * k], v[h][2 * k + 1]}, bf16x2));
+            const auto p0 = __builtin_amdgcn_permlane32_swap(w[0][0], w[1][0], false, false);
+            const auto p1 = __builtin_amdgcn_permlane32_swap(w[0][1], w[1][1], false, false);
+            const int o = o0 + 8 * (q + half);
+            const u32x4 r = {p0[0], p1[0], p0[1], p1[1]};
+            if (n >= a.N) continue;
+            if (o + 8 <= a.O) *reinterpret_cast<u32x4_any *>(y + o) = r;
+            else
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (o + k < a.O) y[o + k] = (T)(r[k >> 1] >> (16 * (k & 1)));
+        } else {
+            if (n >= a.N) continue;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int o = o0 + 8 * (q + h) + 4 * half;
+                if (o + 4 <= a.O) *reinterpret_cast<f32x4_any *>(y + o) = f32x4{v[h][0], v[h][1], v[h][2], v[h][3]};
+                else
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (o + k < a.O) y[o + k] = v[h][k];
+            }
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -63,6 +105,10 @@ __device__ __forceinline__ void dma16(const void *base, unsigned offset, unsigne
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds), "v"(offset), "s"(base) : "memory");
 }
+__device__ __forceinline__ void dma4(const void *base, unsigned offset, unsigned lds)        // 4 bytes to a lane, at lds + 4 lane
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" :: "s"(lds), "v"(offset), "s"(base) : "memory");
+}
 template <int N>
 __device__ __forceinline__ void wait_vmcnt() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
 
@@ -79,14 +125,16 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_q4_tiles(const Q4TileArgs a)
     constexpr int NT = WM * WN * 64, BM = TM * WM * 32, BN = TN * WN * 32;
     constexpr int NA = BM * 4 / NT, NB = BN * 4 / NT;            // loads of codes to a thread and step
     constexpr int CODES = (BM + BN) * 64, STAGE = CODES + (BM + BN) * 4;
-    constexpr int SL = (BM + BN) / 4 / (WM * WN);                // lanes of a wavefront that load exponents, 16 bytes each
-    constexpr int LOADS = NA + NB + 1;
-    static_assert(SL <= 64 && BM % (4 * SL) == 0, "exponents");
+    constexpr int NE = (BM + BN) / NT;                           // ... of exponents
+    constexpr int LOADS = NA + NB + NE;
+    static_assert((BM + BN) % NT == 0 && BM % (64 * NE) == 0, "a wavefront's exponents are of one operand");
     extern __shared__ __attribute__((aligned(16))) char lds_q4[];
     const unsigned lds0 = (unsigned)(size_t)lds_q4;
     const int unit = (blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
     if (unit >= a.ntiles * a.otiles) return;
-    const int ot = unit % a.otiles, nt = unit / a.otiles;
+    // four rows of tiles at a time: the tiles that an XCD's work-groups take at once are 8 x 4, not 32 x 1
+    const int panel = uniform(unit / (4 * a.otiles)), in_panel = unit - panel * 4 * a.otiles, deep = min(4, a.ntiles - 4 * panel);
+    const int ot = uniform(in_panel / deep), nt = 4 * panel + in_panel - ot * deep;
     const int o0 = ot * BM, n0 = nt * BN;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
@@ -106,19 +154,15 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_q4_tiles(const Q4TileArgs a)
     }
     const unsigned char *wc = a.wc + (int64_t)o0 * pitch, *xc = a.xc + (int64_t)n0 * pitch;
     // exponents: the wavefront's part of the stage's BM + BN words, w's first
-    const int sfirst = wave * SL * 4;
+    const int sfirst = wave * NE * 64;
     const bool of_w = sfirst < BM;
     const unsigned char *sp = of_w ? a.ws + (int64_t)(o0 + sfirst) * 4 : a.xs + (int64_t)(n0 + sfirst - BM) * 4;
     const int64_t s_step = (int64_t)(of_w ? a.orows : a.nrows) * 4;
 
-    auto load_step = [&](int buf) {
-        const unsigned l = lds0 + buf * STAGE;
-#pragma unroll
-        for (int u = 0; u < NA; ++u) dma16(wc, aoff[u], l + (wave * NA + u) * 1024);
-#pragma unroll
-        for (int u = 0; u < NB; ++u) dma16(xc, boff[u], l + BM * 64 + (wave * NB + u) * 1024);
-        if (lane < SL) dma16(sp, lane * 16, l + CODES + sfirst * 4);
-        wc += 64; xc += 64; sp += s_step;
+    auto load_one = [&](int u, int s, unsigned l) {              // u < LOADS, known when unrolled; s: the step, l: its stage's place
+        if (u < NA) dma16(wc + s * 64, aoff[u], l + (wave * NA + u) * 1024);
+        else if (u < NA + NB) dma16(xc + s * 64, boff[u - NA], l + BM * 64 + (wave * NB + u - NA) * 1024);
+        else dma4(sp + s * s_step, (u - NA - NB) * 256 + lane * 4, l + CODES + sfirst * 4 + (u - NA - NB) * 256);
     };
 
     f32x16 acc[TM][TN];
@@ -133,47 +177,90 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_q4_tiles(const Q4TileArgs a)
     const int arow = (wm * TM * 32 + r) * 64, brow = BM * 64 + (wn * TN * 32 + r) * 64;
     const int sa = CODES + (wm * TM * 32 + r) * 4, sb = CODES + (BM + wn * TN * 32 + r) * 4;
 
+    i32x4 w[2][TM], x[2][TN];                                    // fragments of the two halves of a step
+    unsigned en[TM], fn[TN];                                     // exponents of the next step
+    auto read_exponents = [&](const char *p) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) en[i] = *reinterpret_cast<const unsigned *>(p + sa + i * 128);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) fn[j] = *reinterpret_cast<const unsigned *>(p + sb + j * 128);
+    };
+    auto read_codes = [&](const char *p, int k) {
+        const int at = ((2 * k + half) ^ swz) * 16;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) w[k][i] = *reinterpret_cast<const i32x4 *>(p + arow + i * 2048 + at);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) x[k][j] = *reinterpret_cast<const i32x4 *>(p + brow + j * 2048 + at);
+    };
+
     const int steps = a.steps;
 #pragma unroll
     for (int s = 0; s < kQ4Stages - 1; ++s)
-        if (s < steps) load_step(s);
-    int buf = 0;
-    for (int s = 0; s < steps; ++s) {
-        // this wavefront's loads of step s have landed when at most those of the steps after it are left
-        if (s + kQ4Stages - 2 < steps) wait_vmcnt<(kQ4Stages - 2) * LOADS>();
-        else wait_vmcnt<0>();
-        __syncthreads();
-        const int next = buf == 0 ? kQ4Stages - 1 : buf - 1;      // step s - 1's buffer: every wavefront is past it
-        if (s + kQ4Stages - 1 < steps) load_step(next);
-        const char *const p = lds_q4 + buf * STAGE;
-        unsigned es[TM], ex[TN];
+        if (s < steps) {
 #pragma unroll
-        for (int i = 0; i < TM; ++i) es[i] = *reinterpret_cast<const unsigned *>(p + sa + i * 128) >> (8 * half);
-#pragma unroll
-        for (int j = 0; j < TN; ++j) ex[j] = *reinterpret_cast<const unsigned *>(p + sb + j * 128) >> (8 * half);
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            i32x4 w[TM], x[TN];
-            const int at = ((2 * k + half) ^ swz) * 16;
-#pragma unroll
-            for (int i = 0; i < TM; ++i) w[i] = *reinterpret_cast<const i32x4 *>(p + arow + i * 2048 + at);
-#pragma unroll
-            for (int j = 0; j < TN; ++j) x[j] = *reinterpret_cast<const i32x4 *>(p + brow + j * 2048 + at);
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = mfma_q4_wide(w[i], x[j], acc[i][j], es[i], ex[j], k);
+            for (int u = 0; u < LOADS; ++u) load_one(u, s, lds0 + s * STAGE);
         }
-        buf = buf == kQ4Stages - 1 ? 0 : buf + 1;
-    }
+    // this wavefront's loads of step 0 have landed
+    if (kQ4Stages - 1 <= steps) wait_vmcnt<(kQ4Stages - 2) * LOADS>();
+    else wait_vmcnt<0>();
+    __syncthreads();
+    read_exponents(lds_q4);
+    read_codes(lds_q4, 0);
+    int buf = 0;
+    // One step, in two halves of 64 values.  While the first is multiplied, the second one's fragments are read and the step
+    // kQ4Stages - 1 on is sent for, into the buffer of the step before this one: every wavefront is past that.  Before the second
+    // is multiplied the next step has to have landed; its first half's fragments and exponents are read meanwhile.
+    auto do_step = [&](int s, auto more_c, auto next_c) {        // more: there is a step to send for; next: there is a next one
+        constexpr bool more = decltype(more_c)::value, has_next = decltype(next_c)::value;
+        const char *const p = lds_q4 + buf * STAGE;
+        const int next = buf == kQ4Stages - 1 ? 0 : buf + 1, free = buf == 0 ? kQ4Stages - 1 : buf - 1;
+        const unsigned to = lds0 + free * STAGE;
+        unsigned es[TM], ex[TN];
+        read_codes(p, 1);
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
+        for (int i = 0; i < TM; ++i) es[i] = en[i] >> (8 * half);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) ex[j] = fn[j] >> (8 * half);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                store_q4<T>(a, n0 + (wn * TN + j) * 32 + r, o0 + (wm * TM + i) * 32 + q * 8 + half * 4,
-                            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]});
+            for (int j = 0; j < TN; ++j) {
+                acc[i][j] = mfma_q4_wide(w[0][i], x[0][j], acc[i][j], es[i], ex[j], 0);
+                const int m = i * TN + j;
+                if (more && m < LOADS) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    load_one(m, s + kQ4Stages - 1, to);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        __builtin_amdgcn_sched_barrier(0);
+        if (has_next) {
+            if (more) wait_vmcnt<(kQ4Stages - 2) * LOADS>();
+            else wait_vmcnt<0>();
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __syncthreads();
+            read_exponents(lds_q4 + next * STAGE);
+            read_codes(lds_q4 + next * STAGE, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = mfma_q4_wide(w[1][i], x[1][j], acc[i][j], es[i], ex[j], 1);
+        __builtin_amdgcn_sched_barrier(0);
+        buf = next;
+    };
+    static_assert(LOADS <= TM * TN, "a load to a matrix instruction");
+    int s = 0;
+    for (; s + kQ4Stages - 1 < steps; ++s) do_step(s, std::true_type{}, std::true_type{});
+    for (; s + 1 < steps; ++s) do_step(s, std::false_type{}, std::true_type{});
+    do_step(s, std::false_type{}, std::false_type{});
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+            store_block_q4<T>(a, n0 + (wn * TN + j) * 32 + r, o0 + (wm * TM + i) * 32, half, acc[i][j]);
 }
 
 // Before the tiles: x in blocks, and the exponents of both operands as the tiles load them, [step][row][4 bytes], in one launch.

@@ -268,7 +268,7 @@ int run_q4(Q4TileArgs &a, hipStream_t st)
 {
     a.ntiles = ceil_div(a.N, kQ4Tile); a.otiles = ceil_div(a.O, kQ4Tile);
     a.per_xcd = ceil_div(a.ntiles * a.otiles, 8);
-    launch(fc_q4_tiles<T, 4, 4, 2, 2>, (int64_t)8 * a.per_xcd, 256, kQ4Stages * 2 * kQ4Tile * 68, st, a);
+    launch(fc_q4_tiles<T, 4, 4, 2, 2>, (int64_t)8 * a.per_xcd, 256, kQ4Stages * 2 * kQ4Tile * 68 + kQ4Tile * 4, st, a);
     return check_launch();
 }
 

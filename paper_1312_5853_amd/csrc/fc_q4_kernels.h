@@ -34,8 +34,9 @@ __device__ __forceinline__ float finish_q4(float s, float bias, int relu)
 // fp32: four neighbouring ones are 16 bytes.  bfloat16: the lanes of the two halves trade what makes eight of them (a lane of the
 // lower half gets those from 8 q on, its partner those from 8 (q + 1) on), 16 bytes as well; with a store to every value, 256
 // instructions to a wavefront that each touch 64 rows, the stores of a tile took as long as 40 of its steps.
+// bias: those of the block's outputs, zeros past the last one.
 template <typename T, typename Args>
-__device__ __forceinline__ void store_block_q4(const Args &a, int n, int o0, int half, const f32x16 &s)
+__device__ __forceinline__ void store_block_q4(const Args &a, const float *bias, int n, int o0, int half, const f32x16 &s)
 {
     T *const y = static_cast<T *>(a.y) + (int64_t)n * a.O;
 #pragma unroll
@@ -43,10 +44,9 @@ __device__ __forceinline__ void store_block_q4(const Args &a, int n, int o0, int
         float v[2][4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int o = o0 + 8 * (q + h) + 4 * half;
+            const f32x4 b = *reinterpret_cast<const f32x4 *>(bias + 8 * (q + h) + 4 * half);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                v[h][k] = finish_q4(s[4 * (q + h) + k], a.bias && o + k < a.O ? a.bias[o + k] : 0.f, a.relu);
+            for (int k = 0; k < 4; ++k) v[h][k] = finish_q4(s[4 * (q + h) + k], b[k], a.relu);
         }
         if constexpr (sizeof(T) == 2) {
             unsigned w[2][2];
@@ -139,6 +139,8 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_q4_tiles(const Q4TileArgs a)
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const unsigned pitch = (unsigned)a.steps * 64;
+    float *const bias = reinterpret_cast<float *>(lds_q4 + kQ4Stages * STAGE);
+    for (int i = tid; i < BM; i += NT) bias[i] = a.bias && o0 + i < a.O ? a.bias[o0 + i] : 0.f;
 
     // load u of a thread: piece q % 4 of row q / 4, q = (wave loads + u) 64 + lane; rows past the end read the last one
     unsigned aoff[NA], boff[NB];
@@ -228,15 +230,15 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_q4_tiles(const Q4TileArgs a)
             for (int j = 0; j < TN; ++j) {
                 acc[i][j] = mfma_q4_wide(w[0][i], x[0][j], acc[i][j], es[i], ex[j], 0);
                 const int m = i * TN + j;
-                if (more && m < LOADS) {
+                if (more && m % 3 == 0) {
                     __builtin_amdgcn_sched_barrier(0);
-                    load_one(m, s + kQ4Stages - 1, to);
+                    load_one(m / 3, s + kQ4Stages - 1, to);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
         __builtin_amdgcn_sched_barrier(0);
         if (has_next) {
-            if (more) wait_vmcnt<(kQ4Stages - 2) * LOADS>();
+            if (more) wait_vmcnt<(kQ4Stages - 3) * LOADS + 6>();
             else wait_vmcnt<0>();
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __syncthreads();
@@ -247,7 +249,15 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_q4_tiles(const Q4TileArgs a)
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = mfma_q4_wide(w[1][i], x[1][j], acc[i][j], es[i], ex[j], 1);
+            for (int j = 0; j < TN; ++j) {
+                acc[i][j] = mfma_q4_wide(w[1][i], x[1][j], acc[i][j], es[i], ex[j], 1);
+                const int m = i * TN + j;
+                if (more && m % 4 == 0 && m / 4 + 6 < LOADS) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    load_one(m / 4 + 6, s + kQ4Stages - 1, to);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
         __builtin_amdgcn_sched_barrier(0);
         buf = next;
     };
@@ -260,7 +270,7 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_q4_tiles(const Q4TileArgs a)
     for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j)
-            store_block_q4<T>(a, n0 + (wn * TN + j) * 32 + r, o0 + (wm * TM + i) * 32, half, acc[i][j]);
+            store_block_q4<T>(a, bias + (wm * TM + i) * 32, n0 + (wn * TN + j) * 32 + r, o0 + (wm * TM + i) * 32, half, acc[i][j]);
 }
 
 // Before the tiles: x in blocks, and the exponents of both operands as the tiles load them, [step][row][4 bytes], in one launch.

@@ -239,19 +239,29 @@ int check_q4(int N, int I, int O, int dtype)
 
 constexpr int kQ4Tile = 256;                         // outputs, and samples, of a tile
 
-// Where a call's scratch lies: x's codes, and the exponents of both operands by steps.
+// How a call runs, and where its scratch lies: x's codes and exponents, by rows or (tiles, which take those of w so too) by steps.
 struct Q4Plan {
+    bool tiles, fused;
     int steps, nrows, orows;
+    int wide;                                        // blocks of 16 samples to a work-group of the kernel for few
     size_t xs, ws, total;
 };
 
 Q4Plan plan_q4(int N, int I, int O)
 {
-    Q4Plan p;
+    Q4Plan p = {};
     p.steps = (int)(pitch_of(I) / kRowFill);
+    p.tiles = N > 256;
+    p.fused = N <= 16 && (int64_t)N * p.steps * 128 <= 16384;
+    if (p.fused) return p;
+    p.wide = N <= 16 ? 1 : N <= 32 ? 2 : 4;
+    p.xs = (size_t)round_up64((int64_t)N * p.steps * 64, 256);
+    if (!p.tiles) {
+        p.total = p.xs + (size_t)round_up64((int64_t)N * p.steps * 4, 256);
+        return p;
+    }
     p.nrows = round_up(N, kQ4Tile);
     p.orows = round_up(O, kQ4Tile);
-    p.xs = (size_t)round_up64((int64_t)N * p.steps * 64, 256);
     p.ws = p.xs + (size_t)p.steps * p.nrows * 4;
     p.total = p.ws + (size_t)p.steps * p.orows * 4;
     return p;
@@ -264,12 +274,25 @@ void run_q4_prepare(const Q4PrepArgs &p, hipStream_t st)
 }
 
 template <typename T>
-int run_q4(Q4TileArgs &a, hipStream_t st)
+void run_q4_tiles(Q4TileArgs &a, hipStream_t st)
 {
     a.ntiles = ceil_div(a.N, kQ4Tile); a.otiles = ceil_div(a.O, kQ4Tile);
     a.per_xcd = ceil_div(a.ntiles * a.otiles, 8);
     launch(fc_q4_tiles<T, 4, 4, 2, 2>, (int64_t)8 * a.per_xcd, 256, kQ4Stages * 2 * kQ4Tile * 68 + kQ4Tile * 4, st, a);
-    return check_launch();
+}
+
+template <typename TX, typename TY>
+void run_q4_rows(Q4RowsArgs &a, const Q4Plan &plan, hipStream_t st)
+{
+    auto go = [&](auto kern, int AO, int J) {
+        a.ntiles = ceil_div(a.N, 16 * J);
+        const size_t sums = (size_t)kQ4Waves * AO * J * 1024, held = plan.fused ? (size_t)a.N * a.steps * 68 : 0;
+        launch(kern, (int64_t)a.ntiles * ceil_div(a.O, 16 * AO), kQ4Waves * 64, std::max(sums, held), st, a);
+    };
+    if (plan.fused) go(fc_q4_rows<TX, TY, 1, 1, true>, 1, 1);
+    else if (plan.wide == 1) go(fc_q4_rows<float, TY, 1, 1, false>, 1, 1);
+    else if (plan.wide == 2) go(fc_q4_rows<float, TY, 1, 2, false>, 1, 2);
+    else go(fc_q4_rows<float, TY, 2, 4, false>, 2, 4);
 }
 
 }  // namespace
@@ -403,30 +426,51 @@ int fc_fwd_q4(const void *x, const void *w_codes, const void *w_scales, const vo
         return kErrMisaligned;
     if (N == 0) return kStatusOk;
     const Q4Plan plan = plan_q4(N, I, O);
-    if (!ws || ws_bytes < plan.total) return kErrWorkspace;
-    if (!aligned(ws, 256)) return kErrMisaligned;
+    if (plan.total) {
+        if (!ws || ws_bytes < plan.total) return kErrWorkspace;
+        if (!aligned(ws, 256)) return kErrMisaligned;
+    }
     unsigned char *const scratch = static_cast<unsigned char *>(ws);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    Q4PrepArgs p = {};
-    p.x.in = x; p.x.out = scratch; p.x.stride = I; p.x.C = I;
-    p.x.per_row = plan.steps * 16;
-    p.x.total = (int64_t)N * p.x.per_row;
-    p.x.div = make_fastdiv(p.x.per_row);
-    p.w_scales = static_cast<const unsigned *>(w_scales);
-    p.xs = reinterpret_cast<unsigned *>(scratch + plan.xs); p.ws = reinterpret_cast<unsigned *>(scratch + plan.ws);
-    p.O = O; p.steps = plan.steps; p.nrows = plan.nrows; p.orows = plan.orows;
-    p.x_blocks = (int)((p.x.total + 255) / 256);
-    p.s_tiles = ceil_div(plan.steps, 32);
-    if (eb == 4) run_q4_prepare<float>(p, st);
-    else run_q4_prepare<Bf16>(p, st);
-    Q4TileArgs a = {};
-    a.xc = scratch; a.xs = scratch + plan.xs;
-    a.wc = static_cast<const unsigned char *>(w_codes); a.ws = scratch + plan.ws;
+    if (plan.tiles) {
+        Q4PrepArgs p = {};
+        p.x.in = x; p.x.out = scratch; p.x.stride = I; p.x.C = I;
+        p.x.per_row = plan.steps * 16;
+        p.x.total = (int64_t)N * p.x.per_row;
+        p.x.div = make_fastdiv(p.x.per_row);
+        p.w_scales = static_cast<const unsigned *>(w_scales);
+        p.xs = reinterpret_cast<unsigned *>(scratch + plan.xs); p.ws = reinterpret_cast<unsigned *>(scratch + plan.ws);
+        p.O = O; p.steps = plan.steps; p.nrows = plan.nrows; p.orows = plan.orows;
+        p.x_blocks = (int)((p.x.total + 255) / 256);
+        p.s_tiles = ceil_div(plan.steps, 32);
+        if (eb == 4) run_q4_prepare<float>(p, st);
+        else run_q4_prepare<Bf16>(p, st);
+        Q4TileArgs a = {};
+        a.xc = scratch; a.xs = scratch + plan.xs;
+        a.wc = static_cast<const unsigned char *>(w_codes); a.ws = scratch + plan.ws;
+        a.bias = static_cast<const float *>(bias);
+        a.y = y;
+        a.N = N; a.O = O; a.steps = plan.steps; a.relu = relu;
+        a.nrows = plan.nrows; a.orows = plan.orows;
+        if (dtype == kDtypeBf16OutBf16) run_q4_tiles<Bf16>(a, st);
+        else run_q4_tiles<float>(a, st);
+        return check_launch();
+    }
+    if (!plan.fused) {
+        const int made = quantize_blocks(x, I, scratch, scratch + plan.xs, N, I, kE2M1, dtype, stream);
+        if (made != kStatusOk) return made;
+    }
+    Q4RowsArgs a = {};
+    a.x = x; a.xc = scratch; a.xs = scratch + plan.xs;
+    a.wc = static_cast<const unsigned char *>(w_codes); a.ws = static_cast<const unsigned char *>(w_scales);
     a.bias = static_cast<const float *>(bias);
     a.y = y;
-    a.N = N; a.O = O; a.steps = plan.steps; a.relu = relu;
-    a.nrows = plan.nrows; a.orows = plan.orows;
-    return dtype == kDtypeBf16OutBf16 ? run_q4<Bf16>(a, st) : run_q4<float>(a, st);
+    a.N = N; a.I = I; a.O = O; a.steps = plan.steps; a.relu = relu;
+    a.div_row = make_fastdiv(plan.steps * 16);
+    if (dtype == kDtypeBf16OutBf16) run_q4_rows<Bf16, Bf16>(a, plan, st);
+    else if (eb == 2) run_q4_rows<Bf16, float>(a, plan, st);
+    else run_q4_rows<float, float>(a, plan, st);
+    return check_launch();
 }
 
 }  // extern "C"

@@ -2,26 +2,12 @@
 //   y[n][o] = f(sum_i x[n][i] w[o][i] + bias[o]),  x and w E2M1 numbers times a power of two for every 32 of i
 // Part of block_ops.hip: included there, inside its anonymous namespace, after block_formats.h.
 //
-// v_mfma_scale_f32_16x16x128_f8f6f4 multiplies them as they are: a lane holds 32 neighbouring values of a row (16 bytes), and
-// the byte of their exponent.  Rows are filled up to 128 values, so a step of the sum is one 64-byte piece and one 4-byte word
-// of exponents of every row.  w is the first operand: a lane then has four neighbouring outputs of one sample.
-struct Q4Args {
-    const unsigned char *xc, *xs, *wc, *ws;      // codes, exponents
-    const float *bias;
-    void *y;
-    int N, I, O, steps;                          // steps of 128
-    int relu;
-    int ntiles, otiles;
-};
+// The matrix instructions multiply them as they are: a lane holds 32 neighbouring values of a row (16 bytes), and the byte of
+// their exponent.  Rows are filled up to 128 values, so a step of the sum is one 64-byte piece and one 4-byte word of exponents of
+// every row.  w is the first operand: a lane then has four neighbouring outputs of one sample.
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-
-__device__ __forceinline__ f32x4 mfma_q4(const i32x4 &w, const i32x4 &x, const f32x4 &c, unsigned ws, unsigned xs)
-{
-    const i32x8 a = {w[0], w[1], w[2], w[3], 0, 0, 0, 0}, b = {x[0], x[1], x[2], x[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 4, 0, (int)ws, 0, (int)xs);
-}
 
 // f(s + bias); NaN stays
 __device__ __forceinline__ float finish_q4(float s, float bias, int relu)
@@ -317,5 +303,131 @@ __global__ __launch_bounds__(256) void q4_prepare(const Q4PrepArgs p)
     for (int k = 0; k < 32; k += 8) {
         const int s = st * 32 + ty + k, o = rt * 32 + tx;
         if (o < p.O && s < p.steps) p.ws[(int64_t)s * p.orows + o] = turned[tx][ty + k];
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Few samples: AO 16 outputs x J 16 samples to a work-group, whose eight wavefronts share the sum
+// ---------------------------------------------------------------------------
+// Bound by reading w once.  v_mfma_scale_f32_16x16x128_f8f6f4: lane l has row l % 16 and the 32 values of block l / 16, so a
+// wavefront reads 64 bytes of each of its rows to a step, straight into registers, kQ4Ahead steps ahead of their products; the
+// wavefronts' sums are joined through LDS.  FUSED: every work-group puts all of x into blocks itself, in LDS, while its first
+// loads of w are on their way: a launch less.
+struct Q4RowsArgs {
+    const void *x;                               // FUSED: the values
+    const unsigned char *xc, *xs;                // else their codes and exponents, rows of 64 and 4 bytes to a step
+    const unsigned char *wc, *ws;
+    const float *bias;
+    void *y;
+    int N, I, O, steps, relu;
+    int ntiles;
+    FastDiv div_row;                             // by 16 steps: eights of a row
+};
+
+constexpr int kQ4Waves = 8, kQ4Ahead = 3;
+
+__device__ __forceinline__ f32x4 mfma_q4(const i32x4 &w, const i32x4 &x, const f32x4 &c, unsigned ws, unsigned xs)
+{
+    const i32x8 a = {w[0], w[1], w[2], w[3], 0, 0, 0, 0}, b = {x[0], x[1], x[2], x[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 4, 0, (int)ws, 0, (int)xs);
+}
+
+template <typename TX, typename TY, int AO, int J, bool FUSED>
+__global__ __launch_bounds__(kQ4Waves * 64) void fc_q4_rows(const Q4RowsArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds_rows[];      // FUSED: x's codes and exponents; then the sums
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const int ot = blockIdx.x / a.ntiles, nt = blockIdx.x - ot * a.ntiles;
+    const int o0 = ot * AO * 16, n0 = nt * J * 16;
+    const int r = lane & 15, g = lane >> 4;
+    const int64_t cpitch = (int64_t)a.steps * 64, spitch = (int64_t)a.steps * 4;
+    const unsigned char *wc[AO], *ws[AO], *xc[J], *xs[J];                // rows past the end read the last one; not stored
+#pragma unroll
+    for (int i = 0; i < AO; ++i) {
+        const int64_t o = min(o0 + i * 16 + r, a.O - 1);
+        wc[i] = a.wc + o * cpitch + g * 16;
+        ws[i] = a.ws + o * spitch + g;
+    }
+    if constexpr (!FUSED) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int64_t n = min(n0 + j * 16 + r, a.N - 1);
+            xc[j] = a.xc + n * cpitch + g * 16;
+            xs[j] = a.xs + n * spitch + g;
+        }
+    }
+    const int first = (int)((int64_t)a.steps * wave / kQ4Waves), last = (int)((int64_t)a.steps * (wave + 1) / kQ4Waves);
+    i32x4 w[kQ4Ahead][AO], x[kQ4Ahead][J];
+    unsigned ew[kQ4Ahead][AO], ex[kQ4Ahead][J];
+    auto load = [&](int s, int slot) {                                   // nothing past the wavefront's part
+        if (s < last) {
+#pragma unroll
+            for (int i = 0; i < AO; ++i) {
+                w[slot][i] = *reinterpret_cast<const i32x4 *>(wc[i] + (int64_t)s * 64);
+                ew[slot][i] = ws[i][(int64_t)s * 4];
+            }
+            if constexpr (!FUSED) {
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    x[slot][j] = *reinterpret_cast<const i32x4 *>(xc[j] + (int64_t)s * 64);
+                    ex[slot][j] = xs[j][(int64_t)s * 4];
+                }
+            }
+        }
+    };
+#pragma unroll
+    for (int k = 0; k < kQ4Ahead; ++k) load(first + k, k);
+    const char *const fc = lds_rows + (int64_t)min(r, a.N - 1) * cpitch + g * 16;
+    const char *const fe = lds_rows + (int64_t)a.N * cpitch + (int64_t)min(r, a.N - 1) * spitch + g;
+    if constexpr (FUSED) {
+        const int per_row = a.steps * 16, total = a.N * per_row;         // a multiple of 16: blocks of lanes stay whole
+        for (int i = tid; i < total; i += kQ4Waves * 64) {
+            const int n = (int)fastdiv((unsigned)i, a.div_row), c = (i - n * per_row) * 8;
+            float v[8];
+            load8(static_cast<const TX *>(a.x) + (int64_t)n * a.I + c, a.I - c, v);
+            unsigned word[2];
+            const int byte = into_codes<kE2M1>(v, word);
+            *reinterpret_cast<unsigned *>(lds_rows + i * 4) = word[0];
+            if (i % 4 == 0) lds_rows[(int64_t)a.N * cpitch + (i >> 2)] = (char)byte;
+        }
+        __syncthreads();
+    }
+    f32x4 acc[AO][J];
+#pragma unroll
+    for (int i = 0; i < AO; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s = first; s < last; s += kQ4Ahead)
+#pragma unroll
+        for (int k = 0; k < kQ4Ahead; ++k)
+            if (s + k < last) {
+                if constexpr (FUSED) {
+                    x[k][0] = *reinterpret_cast<const i32x4 *>(fc + (s + k) * 64);
+                    ex[k][0] = static_cast<unsigned char>(fe[(s + k) * 4]);
+                }
+#pragma unroll
+                for (int i = 0; i < AO; ++i)
+#pragma unroll
+                    for (int j = 0; j < J; ++j) acc[i][j] = mfma_q4(w[k][i], x[k][j], acc[i][j], ew[k][i], ex[k][j]);
+                load(s + k + kQ4Ahead, k);
+            }
+    if constexpr (FUSED) __syncthreads();
+    f32x4 *const sums = reinterpret_cast<f32x4 *>(lds_rows);             // [wavefront][block of 16 x 16][lane]
+#pragma unroll
+    for (int i = 0; i < AO; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j) sums[(wave * AO * J + i * J + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    for (int t = tid; t < AO * J * 64; t += kQ4Waves * 64) {
+        f32x4 s = sums[t];
+#pragma unroll
+        for (int k = 1; k < kQ4Waves; ++k) s += sums[k * AO * J * 64 + t];
+        const int block = t >> 6, i = block / J, j = block - i * J;
+        const int n = n0 + j * 16 + (t & 15), o = o0 + i * 16 + ((t >> 4) & 3) * 4;
+        if (n >= a.N) continue;
+        TY *const y = static_cast<TY *>(a.y) + (int64_t)n * a.O;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (o + k < a.O) st_elem(y, o + k, finish_q4(s[k], a.bias ? a.bias[o + k] : 0.f, a.relu));
     }
 }

@@ -187,10 +187,12 @@ def test_fully_connected_argument_checks(lib):
     for bad in (dict(N=1 << 24), dict(O=1 << 24, N=1), dict(N=1 << 16, O=1 << 15)):
         assert f(**bad) == b.ERR_TOO_LARGE, bad
     for bad in (dict(x=PTR + 2), dict(x=PTR + 1, dtype=1), dict(codes=PTR + 8), dict(scales=PTR + 2), dict(bias=PTR + 2),
-                dict(y=PTR * 4 + 2), dict(y=PTR * 4 + 2, dtype=1), dict(y=PTR * 4 + 1, dtype=2), dict(ws=PTR + 16)):
+                dict(y=PTR * 4 + 2), dict(y=PTR * 4 + 2, dtype=1), dict(y=PTR * 4 + 1, dtype=2)):
         assert f(**bad) == b.ERR_MISALIGNED, bad
-    need = lib.fc_q4_workspace_bytes(4, 40, 24, 0)
-    assert need > 0 and f(ws_bytes=need - 1) == b.ERR_WORKSPACE and f(ws=None) == b.ERR_WORKSPACE
+    for N in (100, 1000):
+        need = lib.fc_q4_workspace_bytes(N, 40, 24, 0)
+        assert need > 0 and f(N=N, ws_bytes=need - 1) == b.ERR_WORKSPACE and f(N=N, ws=None) == b.ERR_WORKSPACE
+        assert f(N=N, ws=PTR + 16) == b.ERR_MISALIGNED
     assert f(N=0, x=None, codes=None, scales=None, y=None, ws=None, ws_bytes=0) == b.OK
     for bad in ((-1, 40, 24, 0), (4, 0, 24, 0), (4, 40, 0, 0), (4, 40, 24, 9)):
         assert lib.fc_kept_workspace_bytes(*bad) == 0 and lib.fc_q4_workspace_bytes(*bad) == 0

@@ -239,7 +239,7 @@ int check_q4(int N, int I, int O, int dtype)
 
 constexpr int kQ4Tile = 256;                         // outputs, and samples, of a tile
 
-// How a call runs, and where its scratch lies: x's codes and exponents, by rows or (tiles, which take those of w so too) by steps.
+// How a call runs, and where its scratch lies: x's codes, and the exponents of both operands by steps.
 struct Q4Plan {
     bool tiles, fused;
     int steps, nrows, orows;
@@ -256,10 +256,6 @@ Q4Plan plan_q4(int N, int I, int O)
     if (p.fused) return p;
     p.wide = N <= 16 ? 1 : N <= 32 ? 2 : 4;
     p.xs = (size_t)round_up64((int64_t)N * p.steps * 64, 256);
-    if (!p.tiles) {
-        p.total = p.xs + (size_t)round_up64((int64_t)N * p.steps * 4, 256);
-        return p;
-    }
     p.nrows = round_up(N, kQ4Tile);
     p.orows = round_up(O, kQ4Tile);
     p.ws = p.xs + (size_t)p.steps * p.nrows * 4;
@@ -284,15 +280,19 @@ void run_q4_tiles(Q4TileArgs &a, hipStream_t st)
 template <typename TX, typename TY>
 void run_q4_rows(Q4RowsArgs &a, const Q4Plan &plan, hipStream_t st)
 {
-    auto go = [&](auto kern, int AO, int J) {
+    // LDS: x's codes and exponents, if they are made there, and the rings; the sums of the wavefronts take their place
+    auto go = [&](auto kern, int AO, int J, int waves, int stages) {
         a.ntiles = ceil_div(a.N, 16 * J);
-        const size_t sums = (size_t)kQ4Waves * AO * J * 1024, held = plan.fused ? (size_t)a.N * a.steps * 68 : 0;
-        launch(kern, (int64_t)a.ntiles * ceil_div(a.O, 16 * AO), kQ4Waves * 64, std::max(sums, held), st, a);
+        a.units = a.ntiles * ceil_div(a.O, 16 * AO);
+        a.per_xcd = ceil_div(a.units, 8);
+        a.held = plan.fused ? round_up(a.N * a.steps * 68, 256) : 0;
+        const size_t rings = (size_t)a.held + waves * stages * q4_rows_stage(AO, J, plan.fused);
+        launch(kern, (int64_t)8 * a.per_xcd, waves * 64, std::max(rings, (size_t)waves * AO * J * 1024), st, a);
     };
-    if (plan.fused) go(fc_q4_rows<TX, TY, 1, 1, true>, 1, 1);
-    else if (plan.wide == 1) go(fc_q4_rows<float, TY, 1, 1, false>, 1, 1);
-    else if (plan.wide == 2) go(fc_q4_rows<float, TY, 1, 2, false>, 1, 2);
-    else go(fc_q4_rows<float, TY, 2, 4, false>, 2, 4);
+    if (plan.fused) go(fc_q4_rows<TX, TY, 1, 1, true, 8, 3>, 1, 1, 8, 3);
+    else if (plan.wide == 1) go(fc_q4_rows<float, TY, 1, 1, false, 8, 3>, 1, 1, 8, 3);
+    else if (plan.wide == 2) go(fc_q4_rows<float, TY, 1, 2, false, 8, 3>, 1, 2, 8, 3);
+    else go(fc_q4_rows<float, TY, 2, 4, false, 4, 3>, 2, 4, 4, 3);
 }
 
 }  // namespace
@@ -432,7 +432,7 @@ int fc_fwd_q4(const void *x, const void *w_codes, const void *w_scales, const vo
     }
     unsigned char *const scratch = static_cast<unsigned char *>(ws);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (plan.tiles) {
+    if (!plan.fused) {
         Q4PrepArgs p = {};
         p.x.in = x; p.x.out = scratch; p.x.stride = I; p.x.C = I;
         p.x.per_row = plan.steps * 16;
@@ -445,6 +445,8 @@ int fc_fwd_q4(const void *x, const void *w_codes, const void *w_scales, const vo
         p.s_tiles = ceil_div(plan.steps, 32);
         if (eb == 4) run_q4_prepare<float>(p, st);
         else run_q4_prepare<Bf16>(p, st);
+    }
+    if (plan.tiles) {
         Q4TileArgs a = {};
         a.xc = scratch; a.xs = scratch + plan.xs;
         a.wc = static_cast<const unsigned char *>(w_codes); a.ws = scratch + plan.ws;
@@ -456,16 +458,14 @@ int fc_fwd_q4(const void *x, const void *w_codes, const void *w_scales, const vo
         else run_q4_tiles<float>(a, st);
         return check_launch();
     }
-    if (!plan.fused) {
-        const int made = quantize_blocks(x, I, scratch, scratch + plan.xs, N, I, kE2M1, dtype, stream);
-        if (made != kStatusOk) return made;
-    }
     Q4RowsArgs a = {};
     a.x = x; a.xc = scratch; a.xs = scratch + plan.xs;
-    a.wc = static_cast<const unsigned char *>(w_codes); a.ws = static_cast<const unsigned char *>(w_scales);
+    a.wc = static_cast<const unsigned char *>(w_codes);
+    a.ws = plan.fused ? static_cast<const unsigned char *>(w_scales) : scratch + plan.ws;
     a.bias = static_cast<const float *>(bias);
     a.y = y;
     a.N = N; a.I = I; a.O = O; a.steps = plan.steps; a.relu = relu;
+    a.nrows = plan.nrows; a.orows = plan.orows;
     a.div_row = make_fastdiv(plan.steps * 16);
     if (dtype == kDtypeBf16OutBf16) run_q4_rows<Bf16, Bf16>(a, plan, st);
     else if (eb == 2) run_q4_rows<Bf16, float>(a, plan, st);

@@ -309,22 +309,25 @@ __global__ __launch_bounds__(256) void q4_prepare(const Q4PrepArgs p)
 // ---------------------------------------------------------------------------
 // Few samples: AO 16 outputs x J 16 samples to a work-group, whose eight wavefronts share the sum
 // ---------------------------------------------------------------------------
-// Bound by reading w once.  v_mfma_scale_f32_16x16x128_f8f6f4: lane l has row l % 16 and the 32 values of block l / 16, so a
-// wavefront reads 64 bytes of each of its rows to a step, straight into registers, kQ4Ahead steps ahead of their products; the
-// wavefronts' sums are joined through LDS.  FUSED: every work-group puts all of x into blocks itself, in LDS, while its first
-// loads of w are on their way: a launch less.
+// Bound by reading w once.  v_mfma_scale_f32_16x16x128_f8f6f4: lane l has row l % 16 and the 32 values of block l / 16.  The
+// wavefronts of a work-group take parts of the sum, each with a ring of STAGES buffers of its own in LDS, so that none waits for
+// another; their sums are joined through LDS.  A buffer holds 256 values of every row (128 bytes, a cache line), loaded directly,
+// the piece c of 16 bytes of row r at place c ^ (r / 2 % 8).  (Fragments loaded into registers take a cache line to every lane of
+// sixteen: 128 samples 9216 -> 4096 19 us.)
+// FUSED: every work-group puts all of x into blocks itself, in LDS, while its first loads of w are on their way: a launch less.
+// Else the exponents of both operands come by steps, as the tiles have them.
 struct Q4RowsArgs {
     const void *x;                               // FUSED: the values
-    const unsigned char *xc, *xs;                // else their codes and exponents, rows of 64 and 4 bytes to a step
-    const unsigned char *wc, *ws;
+    const unsigned char *xc, *xs;                // else their codes, and exponents [steps][nrows][4]
+    const unsigned char *wc, *ws;                // codes, and exponents: FUSED [O][steps][4], else [steps][orows][4]
     const float *bias;
     void *y;
     int N, I, O, steps, relu;
-    int ntiles;
+    int nrows, orows;
+    int ntiles, units, per_xcd;
+    int held;                                    // FUSED: bytes of x's codes and exponents, in front of the rings
     FastDiv div_row;                             // by 16 steps: eights of a row
 };
-
-constexpr int kQ4Waves = 8, kQ4Ahead = 3;
 
 __device__ __forceinline__ f32x4 mfma_q4(const i32x4 &w, const i32x4 &x, const f32x4 &c, unsigned ws, unsigned xs)
 {
@@ -332,56 +335,82 @@ __device__ __forceinline__ f32x4 mfma_q4(const i32x4 &w, const i32x4 &x, const f
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 4, 0, (int)ws, 0, (int)xs);
 }
 
-template <typename TX, typename TY, int AO, int J, bool FUSED>
-__global__ __launch_bounds__(kQ4Waves * 64) void fc_q4_rows(const Q4RowsArgs a)
+// a ring's buffer: codes of the rows, then words of exponents, by steps and rows (a load of 64 words at least)
+constexpr int q4_rows_stage(int AO, int J, bool fused)
 {
-    extern __shared__ __attribute__((aligned(16))) char lds_rows[];      // FUSED: x's codes and exponents; then the sums
+    const int rows = 16 * (fused ? AO : AO + J), words = 32 * AO < 64 ? 64 : 32 * AO;
+    return rows * 128 + 4 * (words + (fused ? 0 : 32 * J < 64 ? 64 : 32 * J));
+}
+
+template <typename TX, typename TY, int AO, int J, bool FUSED, int WAVES, int STAGES>
+__global__ __launch_bounds__(WAVES * 64) void fc_q4_rows(const Q4RowsArgs a)
+{
+    constexpr int RA = 16 * AO, RB = FUSED ? 0 : 16 * J;                 // rows of a buffer, w's first
+    constexpr int NA = RA / 8, NB = RB / 8;                              // loads of codes
+    constexpr int EA = RA * 2 < 64 ? 1 : RA * 2 / 64, EB = FUSED ? 0 : RB * 2 < 64 ? 1 : RB * 2 / 64;
+    constexpr int LOADS = NA + NB + EA + EB, STAGE = q4_rows_stage(AO, J, FUSED);
+    constexpr int EXPA = (RA + RB) * 128, EXPB = EXPA + EA * 256;
+    extern __shared__ __attribute__((aligned(16))) char lds_rows[];      // x's codes and exponents; rings; at last the sums
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-    const int ot = blockIdx.x / a.ntiles, nt = blockIdx.x - ot * a.ntiles;
-    const int o0 = ot * AO * 16, n0 = nt * J * 16;
+    const int unit = (blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);   // an XCD's work-groups share rows of w
+    if (unit >= a.units) return;
+    const int ot = uniform(unit / a.ntiles), nt = unit - ot * a.ntiles;
+    const int o0 = ot * RA, n0 = nt * J * 16;
     const int r = lane & 15, g = lane >> 4;
-    const int64_t cpitch = (int64_t)a.steps * 64, spitch = (int64_t)a.steps * 4;
-    const unsigned char *wc[AO], *ws[AO], *xc[J], *xs[J];                // rows past the end read the last one; not stored
+    const unsigned cpitch = (unsigned)a.steps * 64, spitch = (unsigned)a.steps * 4;
+
+    // load u of codes: rows 8 u .. 8 u + 7; rows past the end read the last one, not stored.  A last step of 128 values is read twice.
+    unsigned arow[NA], brow[NB + 1], aexp[EA], bexp[EB + 1];
+    const unsigned piece = ((lane & 7) ^ (lane >> 4)) * 16;
 #pragma unroll
-    for (int i = 0; i < AO; ++i) {
-        const int64_t o = min(o0 + i * 16 + r, a.O - 1);
-        wc[i] = a.wc + o * cpitch + g * 16;
-        ws[i] = a.ws + o * spitch + g;
+    for (int u = 0; u < NA; ++u) arow[u] = (unsigned)min(8 * u + (lane >> 3), a.O - 1 - o0) * cpitch;
+#pragma unroll
+    for (int u = 0; u < NB; ++u) brow[u] = (unsigned)min(8 * u + (lane >> 3), a.N - 1 - n0) * cpitch;
+    // load u of exponents: words 64 u .. of [step][row] (twice the same 32 where there are no more)
+    const int half_a = (lane / RA) & 1;
+#pragma unroll
+    for (int u = 0; u < EA; ++u) {
+        const int word = (64 * u + lane) % (2 * RA), row = word % RA;
+        aexp[u] = FUSED ? (unsigned)min(row, a.O - 1 - o0) * spitch : (unsigned)row * 4;
     }
-    if constexpr (!FUSED) {
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int64_t n = min(n0 + j * 16 + r, a.N - 1);
-            xc[j] = a.xc + n * cpitch + g * 16;
-            xs[j] = a.xs + n * spitch + g;
+    for (int u = 0; u < EB; ++u) bexp[u] = (unsigned)((64 * u + lane) % (16 * J)) * 4;
+    const unsigned char *const wc = a.wc + (int64_t)o0 * cpitch, *const xc = FUSED ? nullptr : a.xc + (int64_t)n0 * cpitch;
+    const unsigned char *const we = a.ws + (FUSED ? (int64_t)o0 * spitch : (int64_t)o0 * 4), *const xe = FUSED ? nullptr : a.xs + (int64_t)n0 * 4;
+    const int pairs = (a.steps + 1) >> 1;
+    const int first = (int)((int64_t)pairs * wave / WAVES), last = (int)((int64_t)pairs * (wave + 1) / WAVES);
+    char *const ring = lds_rows + a.held + wave * STAGES * STAGE;
+    const unsigned ring_at = (unsigned)(size_t)lds_rows + a.held + wave * STAGES * STAGE;
+    const unsigned w_step = FUSED ? 4 : (unsigned)a.orows * 4, x_step = (unsigned)a.nrows * 4;
+    auto load = [&](int p, int slot) {
+        const unsigned l = ring_at + slot * STAGE;
+        const bool whole = 2 * p + 1 < a.steps;
+        const unsigned keep = whole ? 127 : 63;
+#pragma unroll
+        for (int u = 0; u < NA; ++u) dma16(wc + p * 128, arow[u] + ((piece ^ (u & 1) * 64) & keep), l + u * 1024);
+#pragma unroll
+        for (int u = 0; u < NB; ++u) dma16(xc + p * 128, brow[u] + ((piece ^ (u & 1) * 64) & keep), l + RA * 128 + u * 1024);
+        // the second step's words; the first one's again where there is none
+        const unsigned second = whole ? 1 : 0;
+#pragma unroll
+        for (int u = 0; u < EA; ++u) {
+            const unsigned h = RA * 2 <= 64 ? half_a : 64 * u / RA;
+            dma4(we + (int64_t)2 * p * w_step, aexp[u] + (h & second) * w_step, l + EXPA + u * 256);
         }
-    }
-    const int first = (int)((int64_t)a.steps * wave / kQ4Waves), last = (int)((int64_t)a.steps * (wave + 1) / kQ4Waves);
-    i32x4 w[kQ4Ahead][AO], x[kQ4Ahead][J];
-    unsigned ew[kQ4Ahead][AO], ex[kQ4Ahead][J];
-    auto load = [&](int s, int slot) {                                   // nothing past the wavefront's part
-        if (s < last) {
 #pragma unroll
-            for (int i = 0; i < AO; ++i) {
-                w[slot][i] = *reinterpret_cast<const i32x4 *>(wc[i] + (int64_t)s * 64);
-                ew[slot][i] = ws[i][(int64_t)s * 4];
-            }
-            if constexpr (!FUSED) {
-#pragma unroll
-                for (int j = 0; j < J; ++j) {
-                    x[slot][j] = *reinterpret_cast<const i32x4 *>(xc[j] + (int64_t)s * 64);
-                    ex[slot][j] = xs[j][(int64_t)s * 4];
-                }
-            }
+        for (int u = 0; u < EB; ++u) {
+            const unsigned h = J <= 2 ? (lane / (16 * J)) & 1 : 64 * u / (16 * J);
+            dma4(xe + (int64_t)2 * p * x_step, bexp[u] + (h & second) * x_step, l + EXPB + u * 256);
         }
     };
 #pragma unroll
-    for (int k = 0; k < kQ4Ahead; ++k) load(first + k, k);
+    for (int k = 0; k < STAGES - 1; ++k)
+        if (first + k < last) load(first + k, k);
     const char *const fc = lds_rows + (int64_t)min(r, a.N - 1) * cpitch + g * 16;
     const char *const fe = lds_rows + (int64_t)a.N * cpitch + (int64_t)min(r, a.N - 1) * spitch + g;
     if constexpr (FUSED) {
         const int per_row = a.steps * 16, total = a.N * per_row;         // a multiple of 16: blocks of lanes stay whole
-        for (int i = tid; i < total; i += kQ4Waves * 64) {
+        for (int i = tid; i < total; i += WAVES * 64) {
             const int n = (int)fastdiv((unsigned)i, a.div_row), c = (i - n * per_row) * 8;
             float v[8];
             load8(static_cast<const TX *>(a.x) + (int64_t)n * a.I + c, a.I - c, v);
@@ -397,31 +426,57 @@ __global__ __launch_bounds__(kQ4Waves * 64) void fc_q4_rows(const Q4RowsArgs a)
     for (int i = 0; i < AO; ++i)
 #pragma unroll
         for (int j = 0; j < J; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int s = first; s < last; s += kQ4Ahead)
+    const int swz = (r >> 1) & 7;
+    int slot = 0;
+    for (int p = first; p < last; ++p) {
+        // the buffer of the pair before this one is sent for again: what was read of it has arrived
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (p + STAGES - 1 < last) {
+            load(p + STAGES - 1, slot == 0 ? STAGES - 1 : slot - 1);
+            wait_vmcnt<(STAGES - 1) * LOADS>();
+        } else {
+            wait_vmcnt<0>();
+        }
+        const char *const buf = ring + slot * STAGE;
 #pragma unroll
-        for (int k = 0; k < kQ4Ahead; ++k)
-            if (s + k < last) {
-                if constexpr (FUSED) {
-                    x[k][0] = *reinterpret_cast<const i32x4 *>(fc + (s + k) * 64);
-                    ex[k][0] = static_cast<unsigned char>(fe[(s + k) * 4]);
-                }
+        for (int h = 0; h < 2; ++h) {
+            if (h == 1 && 2 * p + 1 >= a.steps) break;
+            const int at = ((4 * h + g) ^ swz) * 16;
+            i32x4 w[AO], x[J];
+            unsigned ew[AO], ex[J];
 #pragma unroll
-                for (int i = 0; i < AO; ++i)
-#pragma unroll
-                    for (int j = 0; j < J; ++j) acc[i][j] = mfma_q4(w[k][i], x[k][j], acc[i][j], ew[k][i], ex[k][j]);
-                load(s + k + kQ4Ahead, k);
+            for (int i = 0; i < AO; ++i) {
+                w[i] = *reinterpret_cast<const i32x4 *>(buf + (16 * i + r) * 128 + at);
+                ew[i] = static_cast<unsigned char>(buf[EXPA + (h * RA + 16 * i + r) * 4 + g]);
             }
-    if constexpr (FUSED) __syncthreads();
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                if constexpr (FUSED) {
+                    x[j] = *reinterpret_cast<const i32x4 *>(fc + (2 * p + h) * 64);
+                    ex[j] = static_cast<unsigned char>(fe[(2 * p + h) * 4]);
+                } else {
+                    x[j] = *reinterpret_cast<const i32x4 *>(buf + (RA + 16 * j + r) * 128 + at);
+                    ex[j] = static_cast<unsigned char>(buf[EXPB + (h * RB + 16 * j + r) * 4 + g]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < AO; ++i)
+#pragma unroll
+                for (int j = 0; j < J; ++j) acc[i][j] = mfma_q4(w[i], x[j], acc[i][j], ew[i], ex[j]);
+        }
+        slot = slot == STAGES - 1 ? 0 : slot + 1;
+    }
+    __syncthreads();
     f32x4 *const sums = reinterpret_cast<f32x4 *>(lds_rows);             // [wavefront][block of 16 x 16][lane]
 #pragma unroll
     for (int i = 0; i < AO; ++i)
 #pragma unroll
         for (int j = 0; j < J; ++j) sums[(wave * AO * J + i * J + j) * 64 + lane] = acc[i][j];
     __syncthreads();
-    for (int t = tid; t < AO * J * 64; t += kQ4Waves * 64) {
+    for (int t = tid; t < AO * J * 64; t += WAVES * 64) {
         f32x4 s = sums[t];
 #pragma unroll
-        for (int k = 1; k < kQ4Waves; ++k) s += sums[k * AO * J * 64 + t];
+        for (int k = 1; k < WAVES; ++k) s += sums[k * AO * J * 64 + t];
         const int block = t >> 6, i = block / J, j = block - i * J;
         const int n = n0 + j * 16 + (t & 15), o = o0 + i * 16 + ((t >> 4) & 3) * 4;
         if (n >= a.N) continue;

@@ -252,7 +252,7 @@ Q4Plan plan_q4(int N, int I, int O)
     Q4Plan p = {};
     p.steps = (int)(pitch_of(I) / kRowFill);
     p.tiles = N > 256;
-    p.fused = N <= 16 && (int64_t)N * p.steps * 128 <= 16384;
+    p.fused = N <= 16 && (int64_t)N * p.steps * 128 <= 32768;
     if (p.fused) return p;
     p.wide = N <= 16 ? 1 : N <= 32 ? 2 : 4;
     p.xs = (size_t)round_up64((int64_t)N * p.steps * 64, 256);

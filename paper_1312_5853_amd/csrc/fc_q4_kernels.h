@@ -167,18 +167,21 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_q4_tiles(const Q4TileArgs a)
 
     i32x4 w[2][TM], x[2][TN];                                    // fragments of the two halves of a step
     unsigned en[TM], fn[TN];                                     // exponents of the next step
-    auto read_exponents = [&](const char *p) {
-#pragma unroll
-        for (int i = 0; i < TM; ++i) en[i] = *reinterpret_cast<const unsigned *>(p + sa + i * 128);
-#pragma unroll
-        for (int j = 0; j < TN; ++j) fn[j] = *reinterpret_cast<const unsigned *>(p + sb + j * 128);
+    constexpr int FRAGMENTS = TM + TN, EXPONENTS = (TM + TN) / 2;
+    auto read_exponents = [&](const char *p, int u) {            // two words, u < EXPONENTS
+        const int e = 2 * u;
+        if (e < TM) {
+            en[e] = *reinterpret_cast<const unsigned *>(p + sa + e * 128);
+            en[e + 1] = *reinterpret_cast<const unsigned *>(p + sa + e * 128 + 128);
+        } else {
+            fn[e - TM] = *reinterpret_cast<const unsigned *>(p + sb + (e - TM) * 128);
+            fn[e - TM + 1] = *reinterpret_cast<const unsigned *>(p + sb + (e - TM) * 128 + 128);
+        }
     };
-    auto read_codes = [&](const char *p, int k) {
+    auto read_codes = [&](const char *p, int k, int u) {         // fragment u < FRAGMENTS of half k
         const int at = ((2 * k + half) ^ swz) * 16;
-#pragma unroll
-        for (int i = 0; i < TM; ++i) w[k][i] = *reinterpret_cast<const i32x4 *>(p + arow + i * 2048 + at);
-#pragma unroll
-        for (int j = 0; j < TN; ++j) x[k][j] = *reinterpret_cast<const i32x4 *>(p + brow + j * 2048 + at);
+        if (u < TN) x[k][u] = *reinterpret_cast<const i32x4 *>(p + brow + u * 2048 + at);
+        else w[k][u - TN] = *reinterpret_cast<const i32x4 *>(p + arow + (u - TN) * 2048 + at);
     };
 
     const int steps = a.steps;
@@ -192,19 +195,24 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_q4_tiles(const Q4TileArgs a)
     if (kQ4Stages - 1 <= steps) wait_vmcnt<(kQ4Stages - 2) * LOADS>();
     else wait_vmcnt<0>();
     __syncthreads();
-    read_exponents(lds_q4);
-    read_codes(lds_q4, 0);
+#pragma unroll
+    for (int u = 0; u < EXPONENTS; ++u) read_exponents(lds_q4, u);
+#pragma unroll
+    for (int u = 0; u < FRAGMENTS; ++u) read_codes(lds_q4, 0, u);
     int buf = 0;
     // One step, in two halves of 64 values.  While the first is multiplied, the second one's fragments are read and the step
     // kQ4Stages - 1 on is sent for, into the buffer of the step before this one: every wavefront is past that.  Before the second
-    // is multiplied the next step has to have landed; its first half's fragments and exponents are read meanwhile.
+    // is multiplied the next step has to have landed; its first half's fragments and exponents are read meanwhile.  A read or a
+    // load follows each matrix instruction: eight reads at once, of four wavefronts, hold up the instructions behind them.
+    constexpr int PER = TM * TN, EARLY = PER - FRAGMENTS < LOADS ? PER - FRAGMENTS : LOADS;
+    static_assert(TM % 2 == 0 && TN % 2 == 0 && FRAGMENTS + EXPONENTS + LOADS - EARLY <= PER, "one to an instruction");
     auto do_step = [&](int s, auto more_c, auto next_c) {        // more: there is a step to send for; next: there is a next one
         constexpr bool more = decltype(more_c)::value, has_next = decltype(next_c)::value;
         const char *const p = lds_q4 + buf * STAGE;
         const int next = buf == kQ4Stages - 1 ? 0 : buf + 1, free = buf == 0 ? kQ4Stages - 1 : buf - 1;
+        const char *const after = lds_q4 + next * STAGE;
         const unsigned to = lds0 + free * STAGE;
         unsigned es[TM], ex[TN];
-        read_codes(p, 1);
 #pragma unroll
         for (int i = 0; i < TM; ++i) es[i] = en[i] >> (8 * half);
 #pragma unroll
@@ -216,20 +224,16 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_q4_tiles(const Q4TileArgs a)
             for (int j = 0; j < TN; ++j) {
                 acc[i][j] = mfma_q4_wide(w[0][i], x[0][j], acc[i][j], es[i], ex[j], 0);
                 const int m = i * TN + j;
-                if (more && m % 3 == 0) {
-                    __builtin_amdgcn_sched_barrier(0);
-                    load_one(m / 3, s + kQ4Stages - 1, to);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (m < FRAGMENTS) read_codes(p, 1, m);
+                else if (more && m - FRAGMENTS < EARLY) load_one(m - FRAGMENTS, s + kQ4Stages - 1, to);
+                __builtin_amdgcn_sched_barrier(0);
             }
-        __builtin_amdgcn_sched_barrier(0);
         if (has_next) {
-            if (more) wait_vmcnt<(kQ4Stages - 3) * LOADS + 6>();
+            if (more) wait_vmcnt<(kQ4Stages - 3) * LOADS + EARLY>();
             else wait_vmcnt<0>();
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __syncthreads();
-            read_exponents(lds_q4 + next * STAGE);
-            read_codes(lds_q4 + next * STAGE, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -238,16 +242,15 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_q4_tiles(const Q4TileArgs a)
             for (int j = 0; j < TN; ++j) {
                 acc[i][j] = mfma_q4_wide(w[1][i], x[1][j], acc[i][j], es[i], ex[j], 1);
                 const int m = i * TN + j;
-                if (more && m % 4 == 0 && m / 4 + 6 < LOADS) {
-                    __builtin_amdgcn_sched_barrier(0);
-                    load_one(m / 4 + 6, s + kQ4Stages - 1, to);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (has_next && m < FRAGMENTS) read_codes(after, 0, m);
+                else if (has_next && m - FRAGMENTS < EXPONENTS) read_exponents(after, m - FRAGMENTS);
+                else if (more && m - FRAGMENTS - EXPONENTS + EARLY < LOADS)
+                    load_one(m - FRAGMENTS - EXPONENTS + EARLY, s + kQ4Stages - 1, to);
+                __builtin_amdgcn_sched_barrier(0);
             }
-        __builtin_amdgcn_sched_barrier(0);
         buf = next;
     };
-    static_assert(LOADS <= TM * TN, "a load to a matrix instruction");
     int s = 0;
     for (; s + kQ4Stages - 1 < steps; ++s) do_step(s, std::true_type{}, std::true_type{});
     for (; s + 1 < steps; ++s) do_step(s, std::false_type{}, std::true_type{});

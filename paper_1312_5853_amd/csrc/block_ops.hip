@@ -237,11 +237,27 @@ int check_q4(int N, int I, int O, int dtype)
     return kStatusOk;
 }
 
-constexpr int kQ4Tile = 256;                         // outputs, and samples, of a tile
+constexpr int kQ4Tile = 256;                         // outputs, and samples, of a large tile
+
+// The kernel for N > 32 samples: 0 the one for few, else the edge of the tiles.  Large tiles feed the matrix units with half the
+// traffic, where there is one for most of the CUs and the sum is long (x and y bfloat16, us a call, tiles of 256 and of 128):
+// 2048 x 8192 -> 8192 78 and 99, 1024 x 8192 -> 8192 58 and 53, 4096 x 4096 -> 4096 50 and 58, 2048 x 4096 -> 4096 39 and 33,
+// 8192 x 1024 -> 8192 77 and 70.  Few samples: what the two would take in us, by fits to calls like these (for few, and tiles of
+// 128): 64 x 8192 -> 8192 15 and 24, 256 x 8192 -> 8192 39 and 27, 256 x 9216 -> 4096 26 and 29, 512 x 9216 -> 4096 44 and 31,
+// 256 x 4096 -> 4096 16.6 and 15.9, 512 x 4096 -> 1000 11 and 16, 1024 x 4096 -> 1000 19 and 17.
+int q4_tile(int N, int O, int steps)
+{
+    if ((int64_t)ceil_div(N, 256) * ceil_div(O, 256) >= 192 && steps >= 16) return 256;
+    const double units = (double)ceil_div(N, 64) * ceil_div(O, 32), tiles = (double)ceil_div(N, 128) * ceil_div(O, 128);
+    const double few = 5.0 + 2.0 * ceil(units / 256) + units * 96 * 64 * steps / 12e6;
+    const double many = 6.3 + 0.31 * steps * std::max(1.0, tiles / 240);
+    return few < many ? 0 : 128;
+}
 
 // How a call runs, and where its scratch lies: x's codes, and the exponents of both operands by steps.
 struct Q4Plan {
-    bool tiles, fused;
+    bool fused;
+    int tile;                                        // of the kernel for many samples, 0: the one for few
     int steps, nrows, orows;
     int wide;                                        // blocks of 16 samples to a work-group of the kernel for few
     size_t xs, ws, total;
@@ -251,7 +267,9 @@ Q4Plan plan_q4(int N, int I, int O)
 {
     Q4Plan p = {};
     p.steps = (int)(pitch_of(I) / kRowFill);
-    p.tiles = N > 256;
+    p.tile = N > 32 ? q4_tile(N, O, p.steps) : 0;
+    // a launch for x less (4 samples 4096 -> 4096 5.5 us, and 8.8), as long as every work-group's putting x into blocks takes less
+    // than that: 8 x 4096 -> 4096 7.2 and 8.9, 4 x 8192 -> 8192 11.7 and 12.4, 4 x 9216 -> 4096 8.3 and 8.0, 8 x 8192 -> 8192 21 and 13
     p.fused = N <= 16 && (int64_t)N * p.steps * 128 <= 32768;
     if (p.fused) return p;
     p.wide = N <= 16 ? 1 : N <= 32 ? 2 : 4;
@@ -270,11 +288,13 @@ void run_q4_prepare(const Q4PrepArgs &p, hipStream_t st)
 }
 
 template <typename T>
-void run_q4_tiles(Q4TileArgs &a, hipStream_t st)
+void run_q4_tiles(Q4TileArgs &a, int tile, hipStream_t st)
 {
-    a.ntiles = ceil_div(a.N, kQ4Tile); a.otiles = ceil_div(a.O, kQ4Tile);
+    a.ntiles = ceil_div(a.N, tile); a.otiles = ceil_div(a.O, tile);
     a.per_xcd = ceil_div(a.ntiles * a.otiles, 8);
-    launch(fc_q4_tiles<T, 4, 4, 2, 2>, (int64_t)8 * a.per_xcd, 256, kQ4Stages * 2 * kQ4Tile * 68 + kQ4Tile * 4, st, a);
+    const size_t lds = (size_t)kQ4Stages * 2 * tile * 68 + tile * 4;
+    if (tile == 256) launch(fc_q4_tiles<T, 4, 4, 2, 2, 1>, (int64_t)8 * a.per_xcd, 256, lds, st, a);
+    else launch(fc_q4_tiles<T, 2, 2, 2, 2, 2>, (int64_t)8 * a.per_xcd, 256, lds, st, a);
 }
 
 template <typename TX, typename TY>
@@ -446,7 +466,7 @@ int fc_fwd_q4(const void *x, const void *w_codes, const void *w_scales, const vo
         if (eb == 4) run_q4_prepare<float>(p, st);
         else run_q4_prepare<Bf16>(p, st);
     }
-    if (plan.tiles) {
+    if (plan.tile) {
         Q4TileArgs a = {};
         a.xc = scratch; a.xs = scratch + plan.xs;
         a.wc = static_cast<const unsigned char *>(w_codes); a.ws = scratch + plan.ws;
@@ -454,8 +474,8 @@ int fc_fwd_q4(const void *x, const void *w_codes, const void *w_scales, const vo
         a.y = y;
         a.N = N; a.O = O; a.steps = plan.steps; a.relu = relu;
         a.nrows = plan.nrows; a.orows = plan.orows;
-        if (dtype == kDtypeBf16OutBf16) run_q4_tiles<Bf16>(a, st);
-        else run_q4_tiles<float>(a, st);
+        if (dtype == kDtypeBf16OutBf16) run_q4_tiles<Bf16>(a, plan.tile, st);
+        else run_q4_tiles<float>(a, plan.tile, st);
         return check_launch();
     }
     Q4RowsArgs a = {};

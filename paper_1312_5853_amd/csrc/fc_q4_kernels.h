@@ -105,8 +105,8 @@ __device__ __forceinline__ f32x16 mfma_q4_wide(const i32x4 &w, const i32x4 &x, c
                   : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 4, 0, (int)ws, 0, (int)xs);
 }
 
-template <typename T, int TM, int TN, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * 64) void fc_q4_tiles(const Q4TileArgs a)
+template <typename T, int TM, int TN, int WM, int WN, int OCC>
+__global__ __launch_bounds__(WM * WN * 64, OCC) void fc_q4_tiles(const Q4TileArgs a)
 {
     constexpr int NT = WM * WN * 64, BM = TM * WM * 32, BN = TN * WN * 32;
     constexpr int NA = BM * 4 / NT, NB = BN * 4 / NT;            // loads of codes to a thread and step
@@ -202,10 +202,10 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_q4_tiles(const Q4TileArgs a)
     int buf = 0;
     // One step, in two halves of 64 values.  While the first is multiplied, the second one's fragments are read and the step
     // kQ4Stages - 1 on is sent for, into the buffer of the step before this one: every wavefront is past that.  Before the second
-    // is multiplied the next step has to have landed; its first half's fragments and exponents are read meanwhile.  A read or a
-    // load follows each matrix instruction: eight reads at once, of four wavefronts, hold up the instructions behind them.
-    constexpr int PER = TM * TN, EARLY = PER - FRAGMENTS < LOADS ? PER - FRAGMENTS : LOADS;
-    static_assert(TM % 2 == 0 && TN % 2 == 0 && FRAGMENTS + EXPONENTS + LOADS - EARLY <= PER, "one to an instruction");
+    // is multiplied the next step has to have landed; its first half's fragments and exponents are read meanwhile.  The reads and
+    // loads stand between the matrix instructions: eight reads at once, of four wavefronts, hold up the instructions behind them.
+    constexpr int PER = TM * TN, EARLY = LOADS - LOADS / 5, LATE = LOADS - EARLY;
+    static_assert(TM % 2 == 0 && TN % 2 == 0, "exponents are read in twos");
     auto do_step = [&](int s, auto more_c, auto next_c) {        // more: there is a step to send for; next: there is a next one
         constexpr bool more = decltype(more_c)::value, has_next = decltype(next_c)::value;
         const char *const p = lds_q4 + buf * STAGE;
@@ -225,8 +225,10 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_q4_tiles(const Q4TileArgs a)
                 acc[i][j] = mfma_q4_wide(w[0][i], x[0][j], acc[i][j], es[i], ex[j], 0);
                 const int m = i * TN + j;
                 __builtin_amdgcn_sched_barrier(0);
-                if (m < FRAGMENTS) read_codes(p, 1, m);
-                else if (more && m - FRAGMENTS < EARLY) load_one(m - FRAGMENTS, s + kQ4Stages - 1, to);
+#pragma unroll
+                for (int u = m * (FRAGMENTS + EARLY) / PER; u < (m + 1) * (FRAGMENTS + EARLY) / PER; ++u)
+                    if (u < FRAGMENTS) read_codes(p, 1, u);
+                    else if (more) load_one(u - FRAGMENTS, s + kQ4Stages - 1, to);
                 __builtin_amdgcn_sched_barrier(0);
             }
         if (has_next) {
@@ -243,10 +245,15 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_q4_tiles(const Q4TileArgs a)
                 acc[i][j] = mfma_q4_wide(w[1][i], x[1][j], acc[i][j], es[i], ex[j], 1);
                 const int m = i * TN + j;
                 __builtin_amdgcn_sched_barrier(0);
-                if (has_next && m < FRAGMENTS) read_codes(after, 0, m);
-                else if (has_next && m - FRAGMENTS < EXPONENTS) read_exponents(after, m - FRAGMENTS);
-                else if (more && m - FRAGMENTS - EXPONENTS + EARLY < LOADS)
-                    load_one(m - FRAGMENTS - EXPONENTS + EARLY, s + kQ4Stages - 1, to);
+                constexpr int READS = FRAGMENTS + EXPONENTS;
+#pragma unroll
+                for (int u = m * (READS + LATE) / PER; u < (m + 1) * (READS + LATE) / PER; ++u)
+                    if (u < READS) {
+                        if (has_next && u < FRAGMENTS) read_codes(after, 0, u);
+                        else if (has_next) read_exponents(after, u - FRAGMENTS);
+                    } else if (more) {
+                        load_one(u - READS + EARLY, s + kQ4Stages - 1, to);
+                    }
                 __builtin_amdgcn_sched_barrier(0);
             }
         buf = next;

@@ -202,7 +202,7 @@ int layer_norm_bwd_common(const LayerNormArgs &given, bool held, int N, int C, i
 // ---------------------------------------------------------------------------
 struct KeptGradPlan {
     KeptGradArgs a;
-    int64_t blocks;
+    int tile, step;               // outputs, and inputs, of a tile; rows of a step
     size_t part_bytes;
 };
 
@@ -216,17 +216,46 @@ int plan_kept_grad(KeptGradPlan &p, int N, int I, int O, int dtype)
     a.N = N; a.I = I; a.O = O;
     a.pitch = pitch_of(I);
     a.dy_stride = O;
-    a.itiles = ceil_div(I, kGradTile);
-    a.otiles = ceil_div(O, kGradTile);
+    // Large tiles, one work-group to a CU, feed the matrix units with half the traffic, where they fill the rounds of 256 that they
+    // run in: 8192 rows 4096 -> 4096 bfloat16 220 us, 288 in tiles of 128, fp32 635 and 767; 9216 -> 4096 (576 tiles, three rounds)
+    // 643 and 642, fp32 1716 and 1714
+    const int64_t large = (int64_t)ceil_div(I, 256) * ceil_div(O, 256);
+    p.tile = N >= 1024 && large >= 0.77 * round_up64(large, 256) ? 256 : 128;
+    // fp32 over few rows: shorter steps leave room for more work-groups, one of which stores while others multiply (128 rows
+    // 9216 -> 4096 49 us, and 58); over many the longer ones are faster (1024 rows 4096 -> 4096, large tiles, 100 and 106)
+    p.step = glue_elem_bytes(dtype) == 2 ? 64 : p.tile == 128 && N <= 256 ? 16 : 32;
+    a.itiles = ceil_div(I, p.tile);
+    a.otiles = ceil_div(O, p.tile);
     const int64_t tiles = (int64_t)a.itiles * a.otiles;
-    const int steps = std::max(1, ceil_div(N, kGradStep));
-    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / tiles, steps / 4));
+    const int steps = std::max(1, ceil_div(N, p.step));
+    // as many parts of the sum as fill the card, of 256 rows at least: each is written and read again
+    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>((p.tile == 256 ? 256 : 512) / tiles, N / 256));
     const int per = ceil_div(steps, a.splits);
-    a.rows_per_split = per * kGradStep;
+    a.rows_per_split = per * p.step;
     a.splits = ceil_div(steps, per);
-    p.blocks = tiles * a.splits;
+    a.units = (int)(tiles * a.splits);
+    a.per_xcd = ceil_div(a.units, 8);
     if (a.splits > 1) p.part_bytes = (size_t)round_up64((int64_t)a.splits * I * O * 4, 256);
     return kStatusOk;
+}
+
+template <typename T, int TILES, int KS, int OCC>
+void launch_kept_grad(const KeptGradPlan &p, hipStream_t st)
+{
+    launch(fc_grad_kept_kernel<T, TILES, TILES, KS, OCC>, (int64_t)8 * p.a.per_xcd, 256, grad_lds<T, TILES, TILES, KS>(), st, p.a);
+}
+
+template <typename T>
+void run_kept_grad(const KeptGradPlan &p, hipStream_t st)
+{
+    if constexpr (sizeof(T) == 4) {
+        if (p.tile == 256) launch_kept_grad<T, 4, 32, 1>(p, st);
+        else if (p.step == 32) launch_kept_grad<T, 2, 32, 2>(p, st);
+        else launch_kept_grad<T, 2, 16, 2>(p, st);
+    } else {
+        if (p.tile == 256) launch_kept_grad<T, 4, 64, 1>(p, st);
+        else launch_kept_grad<T, 2, 64, 2>(p, st);
+    }
 }
 
 int check_q4(int N, int I, int O, int dtype)
@@ -420,8 +449,8 @@ int fc_bwd_filter_kept(const void *codes, const void *scales, const void *dy, vo
     a.dy = dy;
     a.dw = static_cast<float *>(a.splits > 1 ? ws : dw);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (eb == 4) launch(fc_grad_kept_kernel<float>, p.blocks, 256, 0, st, a);
-    else launch(fc_grad_kept_kernel<Bf16>, p.blocks, 256, 0, st, a);
+    if (eb == 4) run_kept_grad<float>(p, st);
+    else run_kept_grad<Bf16>(p, st);
     if (a.splits > 1) {
         const int64_t count = (int64_t)I * O;
         hipLaunchKernelGGL(fc_grad_join, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, a.dw, static_cast<float *>(dw),

@@ -7,8 +7,12 @@
 // hold them exactly (from 2^-110 on; bfloat16 ends at 2^-133): three products instead of one, and no error but that of the sums.
 //
 // Both operands lie in memory with the sum's index n outermost.  They are staged in LDS as they lie, rows of n, and read
-// transposed (ds_read_b64_tr_b16: 16 lanes read a block of 4 n x 16 columns and get a column of it each).  A row of 128 values is
-// 256 bytes and 64 more, so that the four rows of such a block, and the two blocks that 32 lanes read, lie in different banks.
+// transposed (ds_read_b64_tr_b16: 16 lanes read a block of 4 n x 16 columns and get a column of it each).  The 16-byte piece c of
+// row n stands at place c ^ 4 (n % 4): the four rows of such a block, and the two blocks that 32 lanes read, lie in different banks.
+//
+// Tiles of 64 TM outputs x 64 TN inputs, a quarter to each of four wavefronts, KS rows of n to a step.  Two buffers: while a step is
+// multiplied, the next one's values, which have come into registers meanwhile, are converted and stored piece by piece, and each
+// piece of the step after it is sent for as its registers become free.
 struct KeptGradArgs {
     const unsigned char *codes, *scales;
     const void *dy;
@@ -16,13 +20,13 @@ struct KeptGradArgs {
     int64_t pitch, dy_stride;
     int N, I, O;
     int itiles, otiles, splits, rows_per_split;
+    int units, per_xcd;
 };
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kGradTile = 128, kGradStep = 32, kGradPitch = kGradTile * 2 + 64;     // bytes of a staged row
 
 // 16 codes with their exponent as bfloat16
 __device__ __forceinline__ void kept_to_bf16(const u32x4 &w, unsigned byte, u32x4 (&out)[2])
@@ -54,7 +58,7 @@ __device__ __forceinline__ void three_parts(const float (&v)[8], u32x4 (&part)[3
         for (int k = 0; k < 4; ++k) part[p][k] = __builtin_amdgcn_perm(u[p][2 * k + 1], u[p][2 * k], 0x07060302u);
 }
 
-__device__ __forceinline__ bf16x8 read_transposed(const char *p, int pitch)          // k 0..3 from p, 4..7 four rows on
+__device__ __forceinline__ bf16x8 read_transposed(const char *p, int pitch)          // n 0..3 from p, 4..7 four rows on
 {
     typedef __attribute__((address_space(3))) s16x4 *Lds;
     const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p));
@@ -63,83 +67,192 @@ __device__ __forceinline__ bf16x8 read_transposed(const char *p, int pitch)     
     return __builtin_bit_cast(bf16x8, r);
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void fc_grad_kept_kernel(const KeptGradArgs a)
+template <typename T, int TM, int TN, int KS>
+constexpr int grad_lds() { return 2 * KS * (64 * TN * 2 + 64 * TM * 2 * (sizeof(T) == 4 ? 3 : 1)); }
+
+template <typename T, int TM, int TN, int KS, int OCC>
+__global__ __launch_bounds__(256, OCC) void fc_grad_kept_kernel(const KeptGradArgs a)
 {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-    constexpr int BYTES = kGradStep * kGradPitch;
-    __shared__ __attribute__((aligned(16))) char lds[(PARTS + 1) * BYTES];
-    char *const xs = lds, *const ds = lds + BYTES;
+    constexpr int BO = 64 * TM, BI = 64 * TN;
+    constexpr int XP = BI * 2, DP = BO * 2;                              // bytes of a staged row
+    constexpr int XB = KS * XP, DB = KS * DP, STAGE = XB + PARTS * DB;
+    constexpr int NX = (KS * BI / 16 + 255) / 256, ND = KS * BO / 8 / 256;       // pieces of 16 codes, of 8 gradients, to a thread
+    constexpr int TX = KS * BI / 16 / NX;                                // (fewer pieces than threads: several take the same one)
+    extern __shared__ __attribute__((aligned(16))) char lds_grad[];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const int unit = (blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3);
+    if (unit >= a.units) return;
     const int tiles = a.itiles * a.otiles;
-    const int split = blockIdx.x / tiles, tile = blockIdx.x - split * tiles;
-    const int ot = tile / a.itiles, it = tile - ot * a.itiles;
-    const int o0 = ot * kGradTile, i0 = it * kGradTile;
-    const int wo = (wave >> 1) * 64, wi = (wave & 1) * 64;
+    const int split = uniform(unit / tiles), tile = unit - split * tiles;
+    // four columns of tiles at a time: what an XCD's work-groups take at once shares rows and columns
+    const int panel = uniform(tile / (4 * a.otiles)), in_panel = tile - panel * 4 * a.otiles, deep = min(4, a.itiles - 4 * panel);
+    const int ot = uniform(in_panel / deep), it = 4 * panel + in_panel - ot * deep;
+    const int o0 = ot * BO, i0 = it * BI;
     const int begin = split * a.rows_per_split, end = min(a.N, begin + a.rows_per_split);
+    const int steps = (end - begin + KS - 1) / KS, whole = (end - begin) / KS;         // the last step may be part of one
 
-    f32x16 acc[2][2];
+    // where this thread's pieces lie: rows of n and columns
+    const int xrow = tid % TX / (BI / 16), xcol = tid % (BI / 16);       // piece u: KS / NX rows on
+    const int drow = tid / (BO / 8), dcol = tid % (BO / 8);
+    // A piece past the last output is the row's first one; one that goes past it has values of the next row.  No output is there,
+    // but the last row of all has no next one: steps up to `full` are read without a look at rows and columns.
+    const int dat = o0 + dcol * 8 < a.O ? o0 + dcol * 8 : 0;
+    const int full = o0 + BO > a.O && a.O % 8 ? min(whole, (a.N - 1 - begin) / KS) : whole;
+    // columns past the end of a row of codes are read from its start: no input is there
+    const int64_t xat = i0 + xcol * 16 < a.pitch ? i0 + xcol * 16 : 0;
+    u32x4 xraw[NX];
+    unsigned xbyte[NX];
+    typename Vec<T>::Raw draw[ND][sizeof(T) / 2];
+    const unsigned char *const xp = a.codes + (int64_t)(begin + xrow) * a.pitch + xat;
+    const unsigned char *const ep = a.scales + ((int64_t)(begin + xrow) * a.pitch + xat) / kBlock;
+    const T *const dp = static_cast<const T *>(a.dy) + (int64_t)(begin + drow) * a.dy_stride + dat;
+    // piece u of step s: of the codes for u < NX, else of the gradients; all: every row, and see `full`
+    auto load_piece = [&](int u, int s, bool all) {
+        if (u < NX) {
+            const int row = s * KS + u * (KS / NX);
+            if (all || begin + row + xrow < end) {
+                xraw[u] = *reinterpret_cast<const u32x4 *>(xp + (int64_t)row * a.pitch);
+                xbyte[u] = ep[(int64_t)row * (a.pitch / kBlock)];
+            } else {
+                xraw[u] = u32x4{0u, 0u, 0u, 0u};
+                xbyte[u] = 127;
+            }
+            return;
+        }
+        const int v = u - NX, row = s * KS + v * (KS / ND), left = begin + row + drow < end ? a.O - dat : 0;
+        const T *const p = dp + (int64_t)row * a.dy_stride;
 #pragma unroll
-    for (int p = 0; p < 2; ++p)
+        for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+            if (all) draw[v][h] = Vec<T>::load(p + h * Vec<T>::V);
+            else draw[v][h] = Vec<T>::some(p + h * Vec<T>::V, left - h * Vec<T>::V);
+        }
+    };
+    auto store_piece = [&](int u, char *p) {
+        if (u < NX) {
+            const int row = u * (KS / NX) + xrow;
+            u32x4 v[2];
+            kept_to_bf16(xraw[u], xbyte[u], v);
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
+            for (int h = 0; h < 2; ++h) *reinterpret_cast<u32x4 *>(p + row * XP + (((2 * xcol + h) ^ (4 * (row & 3))) << 4)) = v[h];
+            return;
+        }
+        const int row = (u - NX) * (KS / ND) + drow;
+        char *const to = p + XB + row * DP + ((dcol ^ (4 * (row & 3))) << 4);
+        if constexpr (PARTS == 3) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = draw[u - NX][k >> 2][k & 3];
+            u32x4 part[3];
+            three_parts(v, part);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x4 *>(to + q * DB) = part[q];
+        } else {
+            *reinterpret_cast<u32x4 *>(to) = __builtin_bit_cast(u32x4, draw[u - NX][0]);
+        }
+    };
+
+    f32x16 acc[TM][TN];
+#pragma unroll
+    for (int p = 0; p < TM; ++p)
+#pragma unroll
+        for (int q = 0; q < TN; ++q)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[p][q][v] = 0.f;
 
-    const int row = tid >> 3, col = (tid & 7) * 16;
-    // of a fragment: lane's row of n within 8, its 4 columns of 32
-    const int fr = (lane >> 5) * 8 + ((lane & 15) >> 2), fc = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-    for (int n0 = begin; n0 < end; n0 += kGradStep) {
-        const int n = n0 + row;
-        u32x4 w = {0u, 0u, 0u, 0u}, xv[2];
-        unsigned byte = 127;
-        if (n < end) {
-            const int64_t at = (int64_t)n * a.pitch + i0 + col;
-            w = *reinterpret_cast<const u32x4 *>(a.codes + at);
-            byte = a.scales[at / kBlock];
+    // a lane's part of a fragment: row of n within 8 (and 4 more), 4 columns of 32
+    const int wo = (wave >> 1) * TM * 32, wi = (wave & 1) * TN * 32;
+    const int fr = (lane >> 5) * 8 + ((lane & 15) >> 2), sw = 4 * ((lane & 15) >> 2);
+    const int fc = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), within = (lane & 1) * 8;
+    int xf[TN], df[TM];
+#pragma unroll
+    for (int q = 0; q < TN; ++q) xf[q] = fr * XP + ((((wi >> 3) + 4 * q + fc) ^ sw) << 4) + within;
+#pragma unroll
+    for (int m = 0; m < TM; ++m) df[m] = XB + fr * DP + ((((wo >> 3) + 4 * m + fc) ^ sw) << 4) + within;
+    // A step is groups of TN products that share a fragment of dy: by 16 rows of n, parts (the small ones first) and blocks of outputs.
+    constexpr int ROUND = PARTS * TM, GROUPS = KS / 16 * ROUND, PIECES = NX + ND;
+    bf16x8 xq[2][TN], dq[2];
+    auto read_x = [&](const char *p, int round, int q) { xq[round & 1][q] = read_transposed(p + xf[q] + round * 16 * XP, XP); };
+    auto read_d = [&](const char *p, int g) {
+        dq[g & 1] = read_transposed(p + df[g % TM] + (PARTS - 1 - g % ROUND / TM) * DB + g / ROUND * 16 * DP, DP);
+    };
+    auto start = [&](const char *p) {
+#pragma unroll
+        for (int q = 0; q < TN; ++q) read_x(p, 0, q);
+        read_d(p, 0);
+    };
+    // One step.  PIPELINED: its first fragments have been read, the next two steps are there and whole, and everything else stands
+    // between the products: the next group's fragments, a piece of the next step into LDS, the same of the one after it sent for;
+    // all of them before the last group, at whose start the wavefronts meet, so that it covers the next step's first reads.
+    int buf = 0;
+    auto do_step = [&](int s, auto pipelined_c) {
+        constexpr bool PIPELINED = decltype(pipelined_c)::value;
+        char *const p = lds_grad + buf, *const other = lds_grad + (STAGE - buf);
+        if constexpr (!PIPELINED) {
+            if (s + 1 < steps)
+#pragma unroll
+                for (int u = 0; u < PIECES; ++u) store_piece(u, other);
+            if (s + 2 < steps)
+#pragma unroll
+                for (int u = 0; u < PIECES; ++u) load_piece(u, s + 2, s + 2 < (u < NX ? whole : full));
+            start(p);
         }
-        kept_to_bf16(w, byte, xv);
-        float d[2][8];
-        const T *const dy = static_cast<const T *>(a.dy) + (int64_t)n * a.dy_stride + o0 + col;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) load8(dy + 8 * h, n < end ? max(0, a.O - o0 - col - 8 * h) : 0, d[h]);
-        __syncthreads();
-        char *const at = xs + row * kGradPitch + col * 2, *const dat = ds + row * kGradPitch + col * 2;
-        *reinterpret_cast<u32x4 *>(at) = xv[0];
-        *reinterpret_cast<u32x4 *>(at + 16) = xv[1];
+        for (int g = 0; g < GROUPS; ++g) {
+            const int round = g / ROUND, in = g % ROUND;
+            if (PIPELINED && g == GROUPS - 1) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __syncthreads();
+            }
+            if constexpr (PIPELINED) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if constexpr (PARTS == 3) {
-                u32x4 part[3];
-                three_parts(d[h], part);
+            for (int q = 0; q < TN; ++q) {
+                acc[g % TM][q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dq[g & 1], xq[round & 1][q], acc[g % TM][q], 0, 0, 0);
+                if constexpr (PIPELINED) __builtin_amdgcn_sched_barrier(0);
+                if (q == 0) {
+                    if (g + 1 < GROUPS) read_d(p, g + 1);
+                    else if (PIPELINED) read_d(other, 0);
+                }
+                if (q == (TN > 2 ? 1 : 0)) {                             // the next sixteen rows' fragments of x, over this round's groups
 #pragma unroll
-                for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4 *>(dat + p * BYTES + 16 * h) = part[p];
-            } else {
-                Vec<unsigned short>::store(reinterpret_cast<unsigned short *>(dat + 16 * h), d[h]);
+                    for (int k = 0; k < TN; ++k)
+                        if (round + 1 < KS / 16 && k * ROUND / TN == in) read_x(p, round + 1, k);
+                }
+                if (PIPELINED && g == GROUPS - 1) read_x(other, 0, q);
+                if (PIPELINED && q == TN - 1) {
+#pragma unroll
+                    for (int u = 0; u < PIECES; ++u)
+                        if (u * (GROUPS - 1) / PIECES == g) {
+                            store_piece(u, other);
+                            load_piece(u, s + 2, true);
+                        }
+                }
+                if constexpr (PIPELINED) __builtin_amdgcn_sched_barrier(0);
             }
         }
+        if constexpr (!PIPELINED) __syncthreads();
+        buf = STAGE - buf;
+    };
+    if (steps > 0) {
+#pragma unroll
+        for (int u = 0; u < PIECES; ++u) load_piece(u, 0, 0 < (u < NX ? whole : full));
+#pragma unroll
+        for (int u = 0; u < PIECES; ++u) store_piece(u, lds_grad);
+        if (steps > 1)
+#pragma unroll
+            for (int u = 0; u < PIECES; ++u) load_piece(u, 1, 1 < (u < NX ? whole : full));
         __syncthreads();
-#pragma unroll
-        for (int s = 0; s < kGradStep; s += 16) {
-            const char *const xf = xs + (s + fr) * kGradPitch + (wi + fc) * 2, *const df = ds + (s + fr) * kGradPitch + (wo + fc) * 2;
-            bf16x8 xq[2];
-#pragma unroll
-            for (int q = 0; q < 2; ++q) xq[q] = read_transposed(xf + q * 64, kGradPitch);
-#pragma unroll
-            for (int p = PARTS - 1; p >= 0; --p)                             // the small parts first
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    const bf16x8 dq = read_transposed(df + p * BYTES + m * 64, kGradPitch);
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) acc[m][q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(dq, xq[q], acc[m][q], 0, 0, 0);
-                }
-        }
+        start(lds_grad);
+        __builtin_amdgcn_s_waitcnt(0x0F70);                              // vmcnt(0): the loop's waits then count its own loads alone
+        int s = 0;
+        for (; s + 2 < full; ++s) do_step(s, std::true_type{});
+        for (; s < steps; ++s) do_step(s, std::false_type{});
     }
     float *const dw = a.dw + (int64_t)split * a.O * a.I;
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int m = 0; m < TM; ++m)
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
+        for (int q = 0; q < TN; ++q)
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 const int o = o0 + wo + m * 32 + (lane >> 5) * 4 + (v >> 2) * 8 + (v & 3), i = i0 + wi + q * 32 + (lane & 31);

@@ -33,7 +33,6 @@ int pow2_up(int v)
 }
 
 constexpr int64_t kMaxElements = (int64_t)1 << 31;       // of a fully connected layer's tensors
-constexpr size_t kMaxLds = 160 * 1024;
 
 int64_t pitch_of(int C) { return round_up64(C, kRowFill); }
 
@@ -44,7 +43,7 @@ template <typename Kern, typename Args>
 void launch(Kern kern, int64_t blocks, int threads, size_t lds, hipStream_t st, const Args &a)
 {
     if (lds > 64 * 1024)                                 // more dynamic LDS than that has to be allowed per kernel
-        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kMaxLds);
+        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(threads), lds, st, a);
 }
 
@@ -87,6 +86,7 @@ void run_dequantize(const BlockArgs &a, int form, hipStream_t st)
 // ---------------------------------------------------------------------------
 struct LayerNormPlan {
     bool wide;                    // rows longer than a work-group keeps
+    bool columns;                 // backward: columns' sums by work-groups of their own in the same launch
     int regs, threads;
     int64_t blocks;
     size_t lds, part_bytes;
@@ -107,8 +107,8 @@ int plan_layer_norm(LayerNormPlan &p, int op, int N, int C, int dtype)
     a.vectors = (C - 1) / V + 1;
     a.pitch = pitch_of(C);
     a.inv_c = (float)(1.0 / C);
-    // values to a thread: 16 or, forward, 32 where a work-group of 1024 threads needs them
-    const int few = 16 / V, most = bwd ? few : 2 * few;
+    // values to a thread: forward 16, 32 where a work-group of 1024 threads needs them; backward 8, and 16
+    const int few = (bwd ? 8 : 16) / V, most = 2 * few;
     const int chunks = (a.vectors + 63) / 64;
     p.wide = chunks > 16 * most;
     if (p.wide) {
@@ -124,14 +124,20 @@ int plan_layer_norm(LayerNormPlan &p, int op, int N, int C, int dtype)
     } else {
         a.waves = std::min(16, ceil_div(chunks, few));
         p.regs = pow2_up(ceil_div(chunks, a.waves));
-        a.groups = std::max(1, 8 / a.waves);
+        // rows side by side in a work-group (backward their columns' sums are joined in LDS), as many as few rows leave for all CUs
+        a.groups = std::max(1, std::min((bwd ? 16 : 8) / a.waves, ceil_div(N, 256)));
         p.threads = a.waves * a.groups * 64;
-        const int rounds = ceil_div(N, a.groups);
-        // a column's sum in a thread runs over at most 256 rows
-        p.blocks = std::min<int64_t>(rounds, std::max(512, ceil_div(rounds, 256)));
+        const int rounds = ceil_div(N, a.groups), width = a.vectors * V;
         if (bwd) {
-            a.part_rows = (int)p.blocks;
-            p.lds = a.groups > 1 ? (size_t)a.groups * 2 * a.vectors * V * 4 : 0;
+            p.columns = N <= 256;
+            const int resident = std::max(1, 20 / (a.waves * a.groups));
+            // a column's sum in a thread runs over at most 256 rows
+            a.row_blocks = (int)std::min<int64_t>(rounds, std::max(256 * resident, ceil_div(rounds, 256)));
+            p.blocks = a.row_blocks;
+            a.part_rows = p.columns ? 0 : a.row_blocks;
+            p.lds = (size_t)std::max(width * (a.groups > 1 && !p.columns ? 2 * a.groups : 1), p.columns ? 2 * p.threads : 0) * 4;
+        } else {
+            p.blocks = std::min(rounds, p.regs * V <= 8 ? 1024 : 512);
         }
     }
     if (bwd) p.part_bytes = (size_t)round_up64((int64_t)a.part_rows * 2 * C * 4, 256);
@@ -149,23 +155,31 @@ int run_layer_norm_fwd(const LayerNormPlan &p, hipStream_t st)
     return check_launch();
 }
 
+template <typename T, bool HELD, bool SUMS>
+void launch_layer_norm_bwd(const LayerNormPlan &p, int64_t blocks, hipStream_t st)
+{
+    if (p.regs == 1) launch(layer_norm_bwd_rows<T, HELD, 1, SUMS>, blocks, p.threads, p.lds, st, p.a);
+    else if (p.regs == 2) launch(layer_norm_bwd_rows<T, HELD, 2, SUMS>, blocks, p.threads, p.lds, st, p.a);
+    else if constexpr (sizeof(T) == 4) launch(layer_norm_bwd_rows<T, HELD, 4, SUMS>, blocks, p.threads, p.lds, st, p.a);
+}
+
 template <typename T, bool HELD>
-int run_layer_norm_bwd(const LayerNormPlan &p, hipStream_t st)
+int run_layer_norm_bwd(LayerNormPlan &p, hipStream_t st)
 {
     const LayerNormArgs &a = p.a;
+    const bool sums = a.dgamma || a.dbeta;
+    const int tiles = (a.C + 63) / 64;
     if (a.N > 0) {
         if (p.wide) {
             launch(layer_norm_bwd_wide<T, HELD>, p.blocks, p.threads, 0, st, a);
-            if (a.part) launch(layer_norm_columns<T, HELD>, (int64_t)a.part_rows * ((a.C + 63) / 64), 1024, 0, st, a);
-        } else if (p.regs == 1) {
-            launch(layer_norm_bwd_rows<T, HELD, 1>, p.blocks, p.threads, p.lds, st, a);
-        } else if (p.regs == 2) {
-            launch(layer_norm_bwd_rows<T, HELD, 2>, p.blocks, p.threads, p.lds, st, a);
-        } else if constexpr (sizeof(T) == 4) {
-            launch(layer_norm_bwd_rows<T, HELD, 4>, p.blocks, p.threads, p.lds, st, a);
+            if (a.part) launch(layer_norm_columns<T, HELD>, (int64_t)a.part_rows * tiles, 1024, 0, st, a);
+        } else if (a.part) {
+            launch_layer_norm_bwd<T, HELD, true>(p, p.blocks, st);
+        } else {
+            launch_layer_norm_bwd<T, HELD, false>(p, p.blocks + (sums ? tiles : 0), st);
         }
     }
-    if (a.dgamma || a.dbeta) launch(layer_norm_join, (a.C + 63) / 64, 1024, 0, st, a);
+    if (sums && (a.N == 0 || !p.columns)) launch(layer_norm_join, 2 * tiles, 1024, 0, st, a);
     return check_launch();
 }
 
@@ -190,7 +204,7 @@ int layer_norm_bwd_common(const LayerNormArgs &given, bool held, int N, int C, i
     a.x = g.x; a.codes = g.codes; a.scales = g.scales; a.dy = g.dy; a.out = g.out;
     a.gamma = g.gamma; a.mean = g.mean; a.rstd = g.rstd; a.dgamma = g.dgamma; a.dbeta = g.dbeta;
     a.x_stride = g.x_stride; a.dy_stride = g.dy_stride; a.out_stride = g.out_stride;
-    a.part = sums ? static_cast<float *>(ws) : nullptr;
+    a.part = sums && !p.columns ? static_cast<float *>(ws) : nullptr;
     if (N == 0) a.part_rows = 0;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (held) return eb == 4 ? run_layer_norm_bwd<float, true>(p, st) : run_layer_norm_bwd<Bf16, true>(p, st);

@@ -5,8 +5,8 @@
 //   g = gamma dy,  dx = rstd (g - mean(g) - xh mean(g xh)),  dgamma = sum_rows dy xh,  dbeta = sum_rows dy
 //
 // A row is read once and kept in registers (R vectors to a thread) from its sums to its result.  `waves` wavefronts take a row,
-// as many rows as fit run side by side in a work-group, and a work-group goes through rows so far apart as there are: gamma,
-// beta and the sums of the columns stay in its registers.
+// as many rows as fit run side by side in a work-group, and a work-group goes through rows so far apart as there are, the next
+// one's values on their way while one is summed and written: backward, the sums of the columns stay in its registers.
 struct LayerNormArgs {
     const void *x, *dy;
     const unsigned char *codes, *scales;     // x in blocks
@@ -20,7 +20,7 @@ struct LayerNormArgs {
     int vectors;                             // of a row, the last one perhaps part of one
     int waves, groups;                       // wavefronts to a row, rows side by side
     int part_rows, rows_per_part;
-    int row_blocks;                          // work-groups that take rows; those after them take columns
+    int row_blocks;                          // backward: work-groups that take rows; those after them take columns
     float inv_c, eps;
 };
 
@@ -84,34 +84,59 @@ __device__ __forceinline__ float row_sum(float v, float *lds, int wave, int lane
     return wave_sum(lane < waves ? lds[first + lane] : 0.f);
 }
 
+// what a thread has of a vector's gamma or beta: the values, `rest` past the row's end or where there are none
+template <int V>
+__device__ __forceinline__ void load_affine(const float *p, int at, int left, float rest, float (&v)[V])
+{
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = rest;
+    if (!p) return;
+    if (left >= V) {
+#pragma unroll
+        for (int h = 0; h < V; h += 4) {
+            const f32x4 r = *reinterpret_cast<const f32x4_any *>(p + at + h);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[h + k] = r[k];
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            if (k < left) v[k] = p[at + k];
+    }
+}
+
+// Up to 16 values to a thread gamma and beta stay in registers; with 32 they are read again for every row, from the cache.
 template <typename T, int R>
 __global__ __launch_bounds__(1024) void layer_norm_fwd_rows(const LayerNormArgs a)
 {
     constexpr int V = Vec<T>::V;
+    constexpr bool STAY = R * V <= 16;
     __shared__ float lds[2][16];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int group = wave / a.waves, first = group * a.waves;
     const int t = (wave - first) * 64 + lane, step = a.waves * 64;
-    float gamma[R][V], beta[R][V];
+    float gamma[STAY ? R : 1][V], beta[STAY ? R : 1][V];
     int left[R];                                     // of the row's values, from this vector on
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int v = t + r * step;
         left[r] = v < a.vectors ? a.C - v * V : 0;
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            gamma[r][k] = k < left[r] && a.gamma ? a.gamma[v * V + k] : 1.f;
-            beta[r][k] = k < left[r] && a.beta ? a.beta[v * V + k] : 0.f;
+        if constexpr (STAY) {
+            load_affine(a.gamma, v * V, left[r], 1.f, gamma[r]);
+            load_affine(a.beta, v * V, left[r], 0.f, beta[r]);
         }
     }
     const int64_t rows = (int64_t)gridDim.x * a.groups;
+    typename Vec<T>::Raw raw[R], next[R];
+    auto load = [&](int64_t row, typename Vec<T>::Raw (&to)[R]) {
+        const RowSource<T, false> x(a, row);
+#pragma unroll
+        for (int r = 0; r < R; ++r) to[r] = x.load(t + r * step, row < a.N ? left[r] : 0);
+    };
+    load((int64_t)blockIdx.x * a.groups + group, raw);
     for (int64_t base = (int64_t)blockIdx.x * a.groups; base < a.N; base += rows) {
         const int64_t row = base + group;
-        const bool live = row < a.N;
-        const RowSource<T, false> x(a, row);
-        typename Vec<T>::Raw raw[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) raw[r] = x.load(t + r * step, live ? left[r] : 0);
+        load(row + rows, next);
         float s = 0.f;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -133,25 +158,33 @@ __global__ __launch_bounds__(1024) void layer_norm_fwd_rows(const LayerNormArgs 
             }
         }
         const float rstd = 1.f / sqrtf(row_sum(s, lds[1], wave, lane, first, a.waves) * a.inv_c + a.eps);
-        if (!live) continue;
-        T *const y = static_cast<T *>(a.out) + row * a.out_stride;
+        if (row < a.N) {
+            T *const y = static_cast<T *>(a.out) + row * a.out_stride;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int v = t + r * step;
-            float w[V];
-            Vec<T>::open(raw[r], w);
-#pragma unroll
-            for (int k = 0; k < V; ++k) w[k] = (w[k] - mean) * rstd * gamma[r][k] + beta[r][k];
-            if (left[r] >= V) Vec<T>::store(y + (int64_t)v * V, w);
-            else
+            for (int r = 0; r < R; ++r) {
+                const int v = t + r * step;
+                float w[V], ga[V], be[V];
+                Vec<T>::open(raw[r], w);
+                if constexpr (!STAY) {
+                    load_affine(a.gamma, v * V, left[r], 1.f, ga);
+                    load_affine(a.beta, v * V, left[r], 0.f, be);
+                }
 #pragma unroll
                 for (int k = 0; k < V; ++k)
-                    if (k < left[r]) Vec<T>::put(y + (int64_t)v * V, k, w[k]);
+                    w[k] = (w[k] - mean) * rstd * (STAY ? gamma[STAY ? r : 0][k] : ga[k]) + (STAY ? beta[STAY ? r : 0][k] : be[k]);
+                if (left[r] >= V) Vec<T>::store(y + (int64_t)v * V, w);
+                else
+#pragma unroll
+                    for (int k = 0; k < V; ++k)
+                        if (k < left[r]) Vec<T>::put(y + (int64_t)v * V, k, w[k]);
+            }
+            if (t == 0) {
+                if (a.mean) a.mean[row] = mean;
+                if (a.rstd) a.rstd[row] = rstd;
+            }
         }
-        if (t == 0) {
-            if (a.mean) a.mean[row] = mean;
-            if (a.rstd) a.rstd[row] = rstd;
-        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) raw[r] = next[r];
     }
 }
 
@@ -183,65 +216,129 @@ __global__ __launch_bounds__(1024) void layer_norm_fwd_wide(const LayerNormArgs 
     }
 }
 
-// dx, and every work-group's sums of the columns over its rows
-template <typename T, bool HELD, int R>
+// Sums of 64 columns over the rows from `begin` on, before `end`, by the work-group's wavefronts: a row to each at a time, four
+// rows' loads together.
+template <typename T, bool HELD>
+__device__ __forceinline__ void column_sums(const LayerNormArgs &a, int tile, int64_t begin, int64_t end, float *lds, float *dgamma,
+                                            float *dbeta)
+{
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int c = tile * 64 + lane;
+    float sg = 0.f, sb = 0.f;
+    if (c < a.C)
+        for (int64_t row = begin + wave; row < end; row += 4 * waves) {
+            float d[4], x[4], mean[4], rstd[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {            // past the end the last row again, times zero
+                const int64_t at = min(row + k * waves, end - 1);
+                d[k] = ld_elem(static_cast<const T *>(a.dy) + at * a.dy_stride, c);
+                x[k] = RowSource<T, HELD>(a, at).at(c);
+                mean[k] = a.mean[at];
+                rstd[k] = a.rstd[at];
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (row + k * waves < end) {
+                    sg += d[k] * ((x[k] - mean[k]) * rstd[k]);
+                    sb += d[k];
+                }
+        }
+    lds[wave * 64 + lane] = sg;
+    lds[(waves + wave) * 64 + lane] = sb;
+    __syncthreads();
+    if (wave < 2 && c < a.C) {                       // one wavefront, or two, join them
+        for (int which = wave; which < 2; which += waves > 1 ? 2 : 1) {
+            float s = 0.f;
+            for (int w = 0; w < waves; ++w) s += lds[(which * waves + w) * 64 + lane];
+            float *const out = which ? dbeta : dgamma;
+            if (out) out[c] = s;
+        }
+    }
+}
+
+// dx, and every work-group's sums of the columns over its rows (SUMS); or, over few rows, dgamma and dbeta by work-groups of their
+// own, which read the rows once more, from the cache, and save the launch that joins.  gamma lies in LDS.  With 8 values to a
+// thread the next row's are on their way (twice the wavefronts to a SIMD that 16 leave room for: 8192 x 4096 bfloat16 56 -> XX us).
+template <typename T, bool HELD, int R, bool SUMS>
 __global__ __launch_bounds__(1024) void layer_norm_bwd_rows(const LayerNormArgs a)
 {
     constexpr int V = Vec<T>::V;
+    constexpr bool AHEAD = SUMS && R * V <= 8;
     typedef RowSource<T, HELD> X;
-    extern __shared__ float joined[];                // [groups][2][vectors * V] when several rows run side by side
+    extern __shared__ __attribute__((aligned(16))) float shared[];       // gamma [vectors * V], then [groups][2][vectors * V]
     __shared__ float lds[2][2][16];
+    if (!SUMS && (int)blockIdx.x >= a.row_blocks) {
+        column_sums<T, HELD>(a, blockIdx.x - a.row_blocks, 0, a.N, shared, a.dgamma, a.dbeta);
+        return;
+    }
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int group = wave / a.waves, first = group * a.waves;
     const int t = (wave - first) * 64 + lane, step = a.waves * 64;
-    float gamma[R][V], dgamma[R][V], dbeta[R][V];
+    const int width = a.vectors * V;
+    for (int i = threadIdx.x; i < width; i += blockDim.x) shared[i] = a.gamma && i < a.C ? a.gamma[i] : 1.f;
+    float dgamma[SUMS ? R : 1][V], dbeta[SUMS ? R : 1][V];
     int left[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int v = t + r * step;
         left[r] = v < a.vectors ? a.C - v * V : 0;
+        if constexpr (SUMS)
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            gamma[r][k] = k < left[r] && a.gamma ? a.gamma[v * V + k] : 1.f;
-            dgamma[r][k] = dbeta[r][k] = 0.f;
-        }
+            for (int k = 0; k < V; ++k) dgamma[r][k] = dbeta[r][k] = 0.f;
     }
-    const int64_t rows = (int64_t)gridDim.x * a.groups;
+    const int64_t rows = (int64_t)a.row_blocks * a.groups;
+    struct Row {
+        typename X::Raw x[R];
+        typename Vec<T>::Raw d[R];
+        float mean, rstd;
+    } now, next;
+    auto load = [&](int64_t row, Row &to) {
+        const X x(a, row);
+        const T *const dy = static_cast<const T *>(a.dy) + row * a.dy_stride;
+        const bool live = row < a.N;
+        to.mean = live ? a.mean[row] : 0.f;
+        to.rstd = live ? a.rstd[row] : 0.f;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int v = t + r * step, n = live ? left[r] : 0;
+            if (n > 0) to.x[r] = x.load(v, n);
+            else to.x[r] = {};
+            to.d[r] = n >= V ? Vec<T>::load(dy + (int64_t)v * V) : Vec<T>::some(dy + (int64_t)v * V, n);
+        }
+    };
+    load((int64_t)blockIdx.x * a.groups + group, now);
+    __syncthreads();
+    auto gamma_of = [&](int r, float (&v)[V]) {      // (a thread without a vector reads the first one)
+        const float *const p = shared + (left[r] > 0 ? (t + r * step) * V : 0);
+#pragma unroll
+        for (int h = 0; h < V; h += 4) {
+            const f32x4 g = *reinterpret_cast<const f32x4 *>(p + h);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[h + k] = g[k];
+        }
+    };
     int turn = 0;
     for (int64_t base = (int64_t)blockIdx.x * a.groups; base < a.N; base += rows, turn ^= 1) {
         const int64_t row = base + group;
-        const bool live = row < a.N;
-        typename X::Raw xr[R];
-        typename Vec<T>::Raw dr[R];
-        float mean = 0.f, rstd = 0.f;
-        if (live) {
-            const X x(a, row);
-            const T *const dy = static_cast<const T *>(a.dy) + row * a.dy_stride;
-            mean = a.mean[row]; rstd = a.rstd[row];
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const int v = t + r * step;
-                if (left[r] > 0) xr[r] = x.load(v, left[r]);
-                else xr[r] = {};
-                dr[r] = left[r] >= V ? Vec<T>::load(dy + (int64_t)v * V) : Vec<T>::some(dy + (int64_t)v * V, left[r]);
-            }
-        } else {
-#pragma unroll
-            for (int r = 0; r < R; ++r) { xr[r] = {}; dr[r] = {}; }
-        }
+        if constexpr (AHEAD) load(row + rows, next);
+        const float mean = now.mean, rstd = now.rstd;
+        // past the row's end dy is zero, and so is what it adds
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            float x[V], d[V];
-            X::open(xr[r], x);
-            Vec<T>::open(dr[r], d);
+            float x[V], d[V], g[V];
+            X::open(now.x[r], x);
+            Vec<T>::open(now.d[r], d);
+            gamma_of(r, g);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                const float xh = k < left[r] ? (x[k] - mean) * rstd : 0.f;
-                s1 += d[k] * gamma[r][k];
-                s2 += d[k] * gamma[r][k] * xh;
-                dgamma[r][k] += d[k] * xh;
-                dbeta[r][k] += d[k];
+                const float xh = (x[k] - mean) * rstd, gd = d[k] * g[k];
+                s1 += gd;
+                s2 += gd * xh;
+                if constexpr (SUMS) {
+                    dgamma[r][k] += d[k] * xh;
+                    dbeta[r][k] += d[k];
+                }
             }
         }
         s1 = wave_sum(s1);
@@ -252,57 +349,62 @@ __global__ __launch_bounds__(1024) void layer_norm_bwd_rows(const LayerNormArgs 
             s1 = wave_sum(lane < a.waves ? lds[turn][0][first + lane] : 0.f);
             s2 = wave_sum(lane < a.waves ? lds[turn][1][first + lane] : 0.f);
         }
-        if (!live) continue;
-        s1 *= a.inv_c;
-        s2 *= a.inv_c;
-        T *const dx = static_cast<T *>(a.out) + row * a.out_stride;
+        if (row < a.N) {
+            s1 *= a.inv_c;
+            s2 *= a.inv_c;
+            T *const dx = static_cast<T *>(a.out) + row * a.out_stride;
+            open_again(now.d);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int v = t + r * step;
-            float x[V], d[V];
-            X::open(xr[r], x);
-            Vec<T>::open(dr[r], d);
+            for (int r = 0; r < R; ++r) {
+                const int v = t + r * step;
+                float x[V], d[V], g[V];
+                X::open(now.x[r], x);
+                Vec<T>::open(now.d[r], d);
+                gamma_of(r, g);
 #pragma unroll
-            for (int k = 0; k < V; ++k) d[k] = rstd * (d[k] * gamma[r][k] - s1 - (x[k] - mean) * rstd * s2);
-            if (left[r] >= V) Vec<T>::store(dx + (int64_t)v * V, d);
-            else
+                for (int k = 0; k < V; ++k) d[k] = rstd * (d[k] * g[k] - s1 - (x[k] - mean) * rstd * s2);
+                if (left[r] >= V) Vec<T>::store(dx + (int64_t)v * V, d);
+                else
 #pragma unroll
-                for (int k = 0; k < V; ++k)
-                    if (k < left[r]) Vec<T>::put(dx + (int64_t)v * V, k, d[k]);
-        }
-    }
-    if (!a.part) return;
-    const int width = a.vectors * V;
-    if (a.groups > 1) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int v = t + r * step;
-            if (v < a.vectors)
-#pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    joined[(2 * group) * width + v * V + k] = dgamma[r][k];
-                    joined[(2 * group + 1) * width + v * V + k] = dbeta[r][k];
-                }
-        }
-        __syncthreads();
-        float *const out = a.part + (int64_t)blockIdx.x * 2 * a.C;
-        for (int i = threadIdx.x; i < 2 * width; i += blockDim.x) {
-            const int c = i < width ? i : i - width;
-            float s = 0.f;
-            for (int g = 0; g < a.groups; ++g) s += joined[2 * g * width + i];
-            if (c < a.C) out[(i < width ? 0 : a.C) + c] = s;
-        }
-        return;
-    }
-    float *const out = a.part + (int64_t)blockIdx.x * 2 * a.C;
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int k = 0; k < V; ++k)
-            if (k < left[r]) {
-                out[(t + r * step) * V + k] = dgamma[r][k];
-                out[a.C + (t + r * step) * V + k] = dbeta[r][k];
+                    for (int k = 0; k < V; ++k)
+                        if (k < left[r]) Vec<T>::put(dx + (int64_t)v * V, k, d[k]);
             }
+        }
+        if constexpr (AHEAD) now = next;
+        else if (base + rows < a.N) load(row + rows, now);
+    }
+    if constexpr (SUMS) {
+        float *const out = a.part + (int64_t)blockIdx.x * 2 * a.C;
+        if (a.groups > 1) {
+            __syncthreads();                         // gamma is no longer needed
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int v = t + r * step;
+                if (v < a.vectors)
+#pragma unroll
+                    for (int k = 0; k < V; ++k) {
+                        shared[(2 * group) * width + v * V + k] = dgamma[r][k];
+                        shared[(2 * group + 1) * width + v * V + k] = dbeta[r][k];
+                    }
+            }
+            __syncthreads();
+            for (int i = threadIdx.x; i < 2 * width; i += blockDim.x) {
+                const int c = i < width ? i : i - width;
+                float s = 0.f;
+                for (int g = 0; g < a.groups; ++g) s += shared[2 * g * width + i];
+                if (c < a.C) out[(i < width ? 0 : a.C) + c] = s;
+            }
+            return;
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (k < left[r]) {
+                    out[(t + r * step) * V + k] = dgamma[r][k];
+                    out[a.C + (t + r * step) * V + k] = dbeta[r][k];
+                }
+    }
 }
 
 // dx of rows longer than a work-group keeps
@@ -332,50 +434,43 @@ __global__ __launch_bounds__(1024) void layer_norm_bwd_wide(const LayerNormArgs 
     }
 }
 
-// Sums of 64 columns over a part of the rows, a wavefront to a sixteenth of them: where the rows' own work-groups keep none.
+// Sums of the columns over a part of the rows, where the rows' own work-groups keep none
 template <typename T, bool HELD>
 __global__ __launch_bounds__(1024) void layer_norm_columns(const LayerNormArgs a)
 {
-    __shared__ float lds[2][16][64];
-    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-    const int tiles = (a.C + 63) / 64;
-    const int part = blockIdx.x / tiles, c = (blockIdx.x - part * tiles) * 64 + lane;
-    const int64_t end = min((int64_t)a.N, (int64_t)(part + 1) * a.rows_per_part);
-    float sg = 0.f, sb = 0.f;
-    if (c < a.C)
-        for (int64_t row = (int64_t)part * a.rows_per_part + wave; row < end; row += 16) {
-            const float d = ld_elem(static_cast<const T *>(a.dy) + row * a.dy_stride, c);
-            sg += d * ((RowSource<T, HELD>(a, row).at(c) - a.mean[row]) * a.rstd[row]);
-            sb += d;
-        }
-    lds[0][wave][lane] = sg;
-    lds[1][wave][lane] = sb;
-    __syncthreads();
-    if (wave < 2 && c < a.C) {
-        float s = 0.f;
-        for (int w = 0; w < 16; ++w) s += lds[wave][w][lane];
-        a.part[((int64_t)part * 2 + wave) * a.C + c] = s;
-    }
+    __shared__ float lds[2 * 16 * 64];
+    const int tiles = (a.C + 63) / 64, part = blockIdx.x / tiles;
+    const int64_t begin = (int64_t)part * a.rows_per_part;
+    float *const out = a.part + (int64_t)part * 2 * a.C;
+    column_sums<T, HELD>(a, blockIdx.x - part * tiles, begin, min((int64_t)a.N, begin + a.rows_per_part), lds, out, out + a.C);
 }
 
-// dgamma and dbeta from the parts' sums, in 64 bits: 64 columns to a work-group, a wavefront to a sixteenth of the parts
+// dgamma or dbeta from the parts' sums, in 64 bits: 64 columns to a work-group, a wavefront to a sixteenth of the parts
 __global__ __launch_bounds__(1024) void layer_norm_join(const LayerNormArgs a)
 {
     __shared__ double lds[16][64];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-    const int c = blockIdx.x * 64 + lane;
-    for (int which = 0; which < 2; ++which) {
-        float *const out = which ? a.dbeta : a.dgamma;
-        double s = 0.0;
-        if (c < a.C)
-            for (int p = wave; p < a.part_rows; p += 16) s += a.part[((int64_t)p * 2 + which) * a.C + c];
-        lds[wave][lane] = s;
-        __syncthreads();
-        if (wave == 0 && c < a.C && out) {
-            s = 0.0;
-            for (int w = 0; w < 16; ++w) s += lds[w][lane];
-            out[c] = (float)s;
+    const int which = blockIdx.x & 1, c = (blockIdx.x >> 1) * 64 + lane;
+    float *const out = which ? a.dbeta : a.dgamma;
+    if (!out) return;
+    double s = 0.0;
+    if (c < a.C) {
+        const float *p = a.part + (int64_t)which * a.C + c;
+        const int64_t pitch = 2 * (int64_t)a.C;
+        int i = wave;
+        for (; i + 48 < a.part_rows; i += 64) {
+            const float v[4] = {p[i * pitch], p[(i + 16) * pitch], p[(i + 32) * pitch], p[(i + 48) * pitch]};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s += v[k];
         }
-        __syncthreads();
+        for (; i < a.part_rows; i += 16) s += p[i * pitch];
+    }
+    lds[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < a.C) {
+        s = 0.0;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) s += lds[w][lane];
+        out[c] = (float)s;
     }
 }

@@ -144,7 +144,7 @@ def test_layer_norm_argument_checks(lib):
     rest = dict(dy=PTR * 2, dys=40, gamma=None, mean=PTR, rstd=PTR, dx=PTR * 3, dxs=40, dgamma=PTR * 4, dbeta=PTR * 5, N=2, C=40,
                 dtype=0, ws=PTR, ws_bytes=1 << 30, stream=None)
     plain, kept = dict(x=PTR, xs=40, **rest), dict(codes=PTR, scales=PTR * 6, **rest)
-    need = lib.layer_norm_workspace_bytes(b.OP_BWD_DATA, 2, 40, 0)
+    need = lib.layer_norm_workspace_bytes(b.OP_BWD_DATA, 1000, 40, 0)
     assert need > 0
     for f, own in ((_caller(lib.layer_norm_bwd, plain), (dict(x=None), dict(dx=PTR), dict(xs=39))),
                    (_caller(lib.layer_norm_bwd_kept, kept), (dict(codes=None), dict(scales=None), dict(dx=PTR), dict(dx=PTR * 6)))):
@@ -154,9 +154,9 @@ def test_layer_norm_argument_checks(lib):
         assert f(dtype=3) == b.ERR_BAD_DTYPE
         assert f(C=(1 << 27) + 1, dys=1 << 30, dxs=1 << 30, **({"xs": 1 << 30} if own[0].get("x", 1) is None else {})) == b.ERR_TOO_LARGE
         for bad in (dict(dy=PTR * 2 + 2), dict(dx=PTR * 3 + 1, dtype=2), dict(gamma=PTR + 2), dict(mean=PTR + 2), dict(rstd=PTR + 2),
-                    dict(dgamma=PTR + 2), dict(dbeta=PTR + 2), dict(ws=PTR + 8)):
+                    dict(dgamma=PTR + 2), dict(dbeta=PTR + 2), dict(N=1000, ws=PTR + 8)):
             assert f(**bad) == b.ERR_MISALIGNED, bad
-        assert f(ws_bytes=need - 1) == b.ERR_WORKSPACE and f(ws=None) == b.ERR_WORKSPACE
+        assert f(N=1000, ws_bytes=need - 1) == b.ERR_WORKSPACE and f(N=1000, ws=None) == b.ERR_WORKSPACE
     assert _caller(lib.layer_norm_bwd_kept, kept)(codes=PTR + 8) == b.ERR_MISALIGNED
     assert _caller(lib.layer_norm_bwd_kept, kept)(scales=PTR + 2) == b.ERR_MISALIGNED
     for bad in ((b.OP_BWD_DATA, -1, 40, 0), (b.OP_BWD_DATA, 2, 0, 0), (b.OP_BWD_DATA, 2, 40, 3), (9, 2, 40, 0), (b.OP_FWD, 2, 40, 0)):

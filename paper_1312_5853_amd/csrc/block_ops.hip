@@ -86,7 +86,7 @@ void run_dequantize(const BlockArgs &a, int form, hipStream_t st)
 // ---------------------------------------------------------------------------
 struct LayerNormPlan {
     bool wide;                    // rows longer than a work-group keeps
-    bool columns;                 // backward: columns' sums by work-groups of their own in the same launch
+    bool columns, apart;          // backward: columns' sums by work-groups of their own, in the same launch or in one of their own
     int regs, threads;
     int64_t blocks;
     size_t lds, part_bytes;
@@ -107,38 +107,46 @@ int plan_layer_norm(LayerNormPlan &p, int op, int N, int C, int dtype)
     a.vectors = (C - 1) / V + 1;
     a.pitch = pitch_of(C);
     a.inv_c = (float)(1.0 / C);
-    // values to a thread: forward 16, 32 where a work-group of 1024 threads needs them; backward 8, and 16
-    const int few = (bwd ? 8 : 16) / V, most = 2 * few;
+    // values to a thread: forward 16, 32 where a work-group of 1024 threads needs them; backward 8, and 16 or 24 in up to 768 threads,
+    // which have registers for their sums too
     const int chunks = (a.vectors + 63) / 64;
-    p.wide = chunks > 16 * most;
+    const int few = (bwd ? 8 : 16) / V, most_waves = bwd && chunks > 16 * few ? layer_norm_bwd_waves(16) : 16;
+    p.wide = chunks > most_waves * (bwd ? 3 : 2) * few;
     if (p.wide) {
         a.waves = 16; a.groups = 1;
         p.threads = 1024;
         p.blocks = std::min(N, 1 << 16);
-        if (bwd) {
-            const int tiles = (C + 63) / 64;
-            a.part_rows = std::max(1, std::min(ceil_div(N, 256), 2048 / tiles));
-            a.rows_per_part = std::max(1, ceil_div(N, a.part_rows));
-            a.part_rows = std::max(1, ceil_div(N, a.rows_per_part));
-        }
+        p.apart = bwd;
     } else {
-        a.waves = std::min(16, ceil_div(chunks, few));
-        p.regs = pow2_up(ceil_div(chunks, a.waves));
+        a.waves = std::min(most_waves, ceil_div(chunks, few));
+        const int runs = ceil_div(chunks, a.waves);
+        p.regs = runs <= 2 * few ? pow2_up(runs) : 3 * few;
+        // dgamma and dbeta by work-groups of their own, over few rows in the same launch (fp32, us: 512 x 1024 9.0 and 11.3, 512 x 9216
+        // 22.7 and 26.8, 768 x 1024 12.0 and 10.9), and where a thread has no registers left for sums (24 values; 3000 x 16384 fp32
+        // with them, spilt, 368 us)
+        p.columns = bwd && N <= 640;
+        p.apart = bwd && !p.columns && p.regs == 3 * few;
         // rows side by side in a work-group (backward their columns' sums are joined in LDS), as many as few rows leave for all CUs
-        a.groups = std::max(1, std::min((bwd ? 16 : 8) / a.waves, ceil_div(N, 256)));
+        const int beside = (bwd ? 16 : 8) / a.waves;
+        a.groups = std::max(1, p.columns ? beside : std::min(beside, ceil_div(N, 256)));
         p.threads = a.waves * a.groups * 64;
         const int rounds = ceil_div(N, a.groups), width = a.vectors * V;
         if (bwd) {
-            p.columns = N <= 256;
             const int resident = std::max(1, 20 / (a.waves * a.groups));
             // a column's sum in a thread runs over at most 256 rows
             a.row_blocks = (int)std::min<int64_t>(rounds, std::max(256 * resident, ceil_div(rounds, 256)));
             p.blocks = a.row_blocks;
             a.part_rows = p.columns ? 0 : a.row_blocks;
-            p.lds = (size_t)std::max(width * (a.groups > 1 && !p.columns ? 2 * a.groups : 1), p.columns ? 2 * p.threads : 0) * 4;
+            p.lds = (size_t)std::max(width * (a.groups > 1 && !p.columns && !p.apart ? 2 * a.groups : 1), p.columns ? 2 * p.threads : 0) * 4;
         } else {
             p.blocks = std::min(rounds, p.regs * V <= 8 ? 1024 : 512);
         }
+    }
+    if (p.apart) {
+        const int tiles = (C + 63) / 64;
+        a.part_rows = std::max(1, std::min(ceil_div(N, 256), 2048 / tiles));
+        a.rows_per_part = std::max(1, ceil_div(N, a.part_rows));
+        a.part_rows = std::max(1, ceil_div(N, a.rows_per_part));
     }
     if (bwd) p.part_bytes = (size_t)round_up64((int64_t)a.part_rows * 2 * C * 4, 256);
     return kStatusOk;
@@ -158,9 +166,11 @@ int run_layer_norm_fwd(const LayerNormPlan &p, hipStream_t st)
 template <typename T, bool HELD, bool SUMS>
 void launch_layer_norm_bwd(const LayerNormPlan &p, int64_t blocks, hipStream_t st)
 {
-    if (p.regs == 1) launch(layer_norm_bwd_rows<T, HELD, 1, SUMS>, blocks, p.threads, p.lds, st, p.a);
-    else if (p.regs == 2) launch(layer_norm_bwd_rows<T, HELD, 2, SUMS>, blocks, p.threads, p.lds, st, p.a);
-    else if constexpr (sizeof(T) == 4) launch(layer_norm_bwd_rows<T, HELD, 4, SUMS>, blocks, p.threads, p.lds, st, p.a);
+    constexpr int few = 8 * (int)sizeof(T) / 16;         // vectors of eight values
+    if (few > 1 && p.regs == 1) launch(layer_norm_bwd_rows<T, HELD, 1, SUMS>, blocks, p.threads, p.lds, st, p.a);
+    else if (p.regs == few) launch(layer_norm_bwd_rows<T, HELD, few, SUMS>, blocks, p.threads, p.lds, st, p.a);
+    else if (p.regs == 2 * few) launch(layer_norm_bwd_rows<T, HELD, 2 * few, SUMS>, blocks, p.threads, p.lds, st, p.a);
+    else if constexpr (!SUMS) launch(layer_norm_bwd_rows<T, HELD, 3 * few, SUMS>, blocks, p.threads, p.lds, st, p.a);
 }
 
 template <typename T, bool HELD>
@@ -172,12 +182,12 @@ int run_layer_norm_bwd(LayerNormPlan &p, hipStream_t st)
     if (a.N > 0) {
         if (p.wide) {
             launch(layer_norm_bwd_wide<T, HELD>, p.blocks, p.threads, 0, st, a);
-            if (a.part) launch(layer_norm_columns<T, HELD>, (int64_t)a.part_rows * tiles, 1024, 0, st, a);
-        } else if (a.part) {
+        } else if (a.part && !p.apart) {
             launch_layer_norm_bwd<T, HELD, true>(p, p.blocks, st);
         } else {
-            launch_layer_norm_bwd<T, HELD, false>(p, p.blocks + (sums ? tiles : 0), st);
+            launch_layer_norm_bwd<T, HELD, false>(p, p.blocks + (p.columns && sums ? tiles : 0), st);
         }
+        if (a.part && p.apart) launch(layer_norm_columns<T, HELD>, (int64_t)a.part_rows * tiles, 1024, 0, st, a);
     }
     if (sums && (a.N == 0 || !p.columns)) launch(layer_norm_join, 2 * tiles, 1024, 0, st, a);
     return check_launch();

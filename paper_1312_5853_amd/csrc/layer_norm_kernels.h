@@ -258,9 +258,11 @@ __device__ __forceinline__ void column_sums(const LayerNormArgs &a, int tile, in
 
 // dx, and every work-group's sums of the columns over its rows (SUMS); or, over few rows, dgamma and dbeta by work-groups of their
 // own, which read the rows once more, from the cache, and save the launch that joins.  gamma lies in LDS.  With 8 values to a
-// thread the next row's are on their way (twice the wavefronts to a SIMD that 16 leave room for: 8192 x 4096 bfloat16 56 -> XX us).
+// thread the next row's are on their way (8192 x 4096 bfloat16 43 us, 56 with 16 values, which leave room for half the wavefronts).
+constexpr int layer_norm_bwd_waves(int values) { return values <= 8 ? 16 : 12; }        // most to a row, by values to a thread
+
 template <typename T, bool HELD, int R, bool SUMS>
-__global__ __launch_bounds__(1024) void layer_norm_bwd_rows(const LayerNormArgs a)
+__global__ __launch_bounds__(64 * layer_norm_bwd_waves(R * Vec<T>::V)) void layer_norm_bwd_rows(const LayerNormArgs a)
 {
     constexpr int V = Vec<T>::V;
     constexpr bool AHEAD = SUMS && R * V <= 8;

@@ -132,9 +132,9 @@ int plan_layer_norm(LayerNormPlan &p, int op, int N, int C, int dtype)
         p.threads = a.waves * a.groups * 64;
         const int rounds = ceil_div(N, a.groups), width = a.vectors * V;
         if (bwd) {
-            const int resident = std::max(1, 20 / (a.waves * a.groups));
-            // a column's sum in a thread runs over at most 256 rows
-            a.row_blocks = (int)std::min<int64_t>(rounds, std::max(256 * resident, ceil_div(rounds, 256)));
+            // One to a CU, as every one's sums are written and read again (6001 x 5003 bfloat16 from 8 bits 52 us, 63 with two); but
+            // a column's sum in a thread runs over at most 256 rows.
+            a.row_blocks = std::min(rounds, std::max(256, ceil_div(rounds, 256)));
             p.blocks = a.row_blocks;
             a.part_rows = p.columns ? 0 : a.row_blocks;
             p.lds = (size_t)std::max(width * (a.groups > 1 && !p.columns && !p.apart ? 2 * a.groups : 1), p.columns ? 2 * p.threads : 0) * 4;

@@ -123,6 +123,37 @@ struct RowSource<T, true> {
     }
 };
 
+// Two sums over the 64 lanes: over the rows of 16, then from each row into the next (row_bcast), the last lane's at the end; the two
+// chains fill each other's wait states.  Half the instructions of two wave_sum.
+__device__ __forceinline__ void wave_sums(float &a, float &b)
+{
+    a += dpp_move<0xB1>(a);  b += dpp_move<0xB1>(b);
+    a += dpp_move<0x4E>(a);  b += dpp_move<0x4E>(b);
+    a += dpp_move<0x141>(a); b += dpp_move<0x141>(b);
+    a += dpp_move<0x140>(a); b += dpp_move<0x140>(b);
+    auto from_row = [](float v, auto ctrl, auto rows) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, decltype(rows)::value, 0xF, false));
+    };
+    typedef std::integral_constant<int, 0x142> Bcast15;
+    typedef std::integral_constant<int, 0x143> Bcast31;
+    a += from_row(a, Bcast15{}, std::integral_constant<int, 0xA>{});
+    b += from_row(b, Bcast15{}, std::integral_constant<int, 0xA>{});
+    a += from_row(a, Bcast31{}, std::integral_constant<int, 0xC>{});
+    b += from_row(b, Bcast31{}, std::integral_constant<int, 0xC>{});
+    a = lane_value(a, 63);
+    b = lane_value(b, 63);
+}
+// ... of up to 16 lanes, zeros in the others
+__device__ __forceinline__ void row_sums(float &a, float &b)
+{
+    a += dpp_move<0xB1>(a);  b += dpp_move<0xB1>(b);
+    a += dpp_move<0x4E>(a);  b += dpp_move<0x4E>(b);
+    a += dpp_move<0x141>(a); b += dpp_move<0x141>(b);
+    a += dpp_move<0x140>(a); b += dpp_move<0x140>(b);
+    a = lane_value(a, 0);
+    b = lane_value(b, 0);
+}
+
 // sum of every wavefront's v over the wavefronts of a row; all of the work-group take part (several of them to a row)
 __device__ __forceinline__ float row_sum(float v, float *lds, int wave, int lane, int first, int waves)
 {
@@ -402,13 +433,13 @@ __global__ __launch_bounds__(64 * layer_norm_bwd_waves(R * Vec<T>::V)) void laye
                 }
             }
         }
-        s1 = wave_sum(s1);
-        s2 = wave_sum(s2);
+        wave_sums(s1, s2);
         if (a.waves > 1) {
             if (lane == 0) { lds[turn][0][wave] = s1; lds[turn][1][wave] = s2; }
             __syncthreads();
-            s1 = wave_sum(lane < a.waves ? lds[turn][0][first + lane] : 0.f);
-            s2 = wave_sum(lane < a.waves ? lds[turn][1][first + lane] : 0.f);
+            s1 = lane < a.waves ? lds[turn][0][first + lane] : 0.f;
+            s2 = lane < a.waves ? lds[turn][1][first + lane] : 0.f;
+            row_sums(s1, s2);
         }
         if (row < a.N) {
             s1 *= a.inv_c;

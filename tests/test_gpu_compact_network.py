@@ -1,0 +1,136 @@
+"""The network with layer norm in front of its fully connected layers, activations kept in 8 bits and weights in 4: every call of
+a step against the oracle on that call's own inputs, its gradients against differences of its loss, and a step in a graph."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_1312_5853_amd import binding as hp
+from paper_1312_5853_amd import compact
+
+pytestmark = pytest.mark.gpu
+N = 6
+
+
+def _host(t):
+    return t.double().cpu().numpy()
+
+
+def _values(q):
+    return oracle.dequantize_blocks(q.codes.cpu().numpy(), q.scales.cpu().numpy(), q.cols, q.format)
+
+
+def _close(got, want, rel):
+    want = np.asarray(want)
+    assert np.abs(_host(got).reshape(want.shape) - want).max() <= rel * np.abs(want).max()
+
+
+@pytest.fixture(scope="module")
+def net():
+    n = compact.CompactNetwork(N)
+    n.targets()
+    return n
+
+
+def test_calls_of_a_step_against_the_oracle(net):
+    """fp32 results of sums of up to 9216 terms: 1e-5 of the largest."""
+    seen = {}
+    real = {k: getattr(hp, k) for k in ("layer_norm_fwd", "quantize_blocks", "layer_norm_bwd_kept", "fc_bwd_filter_kept")}
+
+    def watch(name, inputs):
+        def call(*a, **k):
+            before = [_host(v) if torch.is_tensor(v) else v for v in a]
+            out = real[name](*a, **k)
+            torch.cuda.synchronize()
+            got = tuple(_host(o) for o in out) if isinstance(out, tuple) else _values(out) if isinstance(out, hp.Blocks) else _host(out)
+            seen.setdefault(name, []).append((before, got))
+            return out
+        return call
+
+    update, net.update = net.update, lambda: None
+    for k in real:
+        setattr(hp, k, watch(k, None))
+    try:
+        net.step()
+    finally:
+        net.update = update
+        for k, f in real.items():
+            setattr(hp, k, f)
+    assert [len(seen[k]) for k in real] == [3, 6, 3, 3]
+    for (a, gamma, beta), got in seen["layer_norm_fwd"]:
+        for g, w in zip(got, oracle.layer_norm_fwd(a, gamma, beta, 1e-5)):
+            assert np.abs(g - w).max() <= 1e-5 * np.abs(w).max()
+    for (a, form), got in seen["quantize_blocks"]:
+        assert np.array_equal(got, oracle.dequantize_blocks(*oracle.quantize_blocks(a, form), a.shape[1], form))
+    for (q, d), got in seen["fc_bwd_filter_kept"]:
+        want = d.T @ _values(q)
+        assert np.abs(got - want).max() <= 1e-5 * np.abs(want).max()
+    for (q, dh, mean, rstd, gamma), got in seen["layer_norm_bwd_kept"]:
+        for g, w in zip(got, oracle.layer_norm_bwd(_values(q), dh, mean, rstd, gamma)):
+            assert np.abs(g - w).max() <= 1e-5 * np.abs(w).max()
+    # what the passes hand on to one another: h in blocks, the gradient of its layer, the ReLU below
+    d = seen["fc_bwd_filter_kept"]
+    assert np.array_equal(d[0][0][1], _host(net.g8))
+    for later, layer in ((0, 1), (1, 2)):
+        dx = seen["layer_norm_bwd_kept"][later][1][0]
+        a = _values(seen["layer_norm_bwd_kept"][later][0][0])
+        assert np.array_equal(d[layer][0][1], np.where(a > 0, dx, 0.0))
+
+
+def test_gradients_against_differences_of_the_loss(net):
+    """Along the gradient g itself the loss has slope |g|: a step that should change it by a hundredth, either way (differences of
+    sums known to 1e-6 of themselves).  The gradient is of values rounded to 8 bits, each off by 2^-4 of itself at most: so by
+    about that, and the layers above it double or treble it."""
+    hp.distill_loss_fwd_bwd(net.forward(), **net._terms(), dz=net.g8)
+    net.backward()
+    total = float(net.loss.double().sum())
+    for p, g in [(net.fc_w["fc7"], net.fc_dw["fc7"]), (net.ln_gamma["fc7"], net.ln_dgamma["fc7"]), (net.ln_beta["fc8"], net.ln_dbeta["fc8"])]:
+        grad, saved = g.double().clone(), p.clone()
+        norm = float(grad.norm())
+        step = 1e-2 * total / norm
+        ends = []
+        for sign in (1.0, -1.0):
+            p.copy_((saved.double() + sign * step * grad / norm).float())
+            ends.append(float(net.evaluate().double().sum()))
+        p.copy_(saved)
+        slope = (ends[0] - ends[1]) / (2 * step)
+        assert abs(slope - norm) <= 0.2 * norm, (slope, norm)
+
+
+def test_a_step_in_a_graph_is_the_step():
+    a, b = compact.CompactNetwork(4), compact.CompactNetwork(4)
+    a.targets(2)
+    b.targets(2)
+    graph = b.capture()                                   # runs one step itself
+    a.step()
+    for _ in range(3):
+        a.step()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(a.loss, b.loss)
+        for (p, _), (q, _) in zip(a.params, b.params):
+            assert torch.equal(p, q)
+
+
+def test_evaluation_in_four_bits(net):
+    with pytest.raises(RuntimeError):
+        compact.CompactNetwork.evaluate_q4(type("N", (), dict(w4=None))())
+    net.quantize()
+    loss = net.evaluate_q4().clone()
+    a = _host(net.a5).reshape(N, -1)
+    for name in compact.FC_NAMES:
+        h = _host(hp.layer_norm_fwd(torch.from_numpy(a).float().cuda(), net.ln_gamma[name], net.ln_beta[name])[0])
+        x = oracle.dequantize_blocks(*oracle.quantize_blocks(h, "e2m1"), h.shape[1], "e2m1")
+        w = oracle.dequantize_blocks(*oracle.quantize_blocks(_host(net.fc_w[name]), "e2m1"), h.shape[1], "e2m1")
+        y = x @ w.T + _host(net.fc_b[name])
+        a = np.maximum(y, 0.0) if name != "fc8" else y
+        a = a.astype(np.float32).astype(np.float64)
+    want = oracle.distill_loss(a, net.labels.cpu().numpy(), net.top_idx.cpu().numpy(), _host(net.top_val), 4.0, 0.7, 0.3)[0]
+    # values next to the border between two 4-bit numbers may fall on either side: a handful of a layer's thousands
+    assert np.abs(_host(loss) - want).max() <= 1e-2 * np.abs(want).max()
+    assert abs(float(loss.mean()) - float(net.evaluate().mean())) < 0.5 * float(net.evaluate().mean())
+
+
+def test_bytes_kept(net):
+    held, full = net.kept_bytes()
+    assert full == 2 * 4 * N * (9216 + 4096 + 4096) and held * 32 == full // 4 * 33

@@ -226,6 +226,7 @@ int layer_norm_bwd_common(const LayerNormArgs &given, bool held, int N, int C, i
 // ---------------------------------------------------------------------------
 struct KeptGradPlan {
     KeptGradArgs a;
+    int slices;                   // few samples: sixteens of them; 0: tiles
     int tile, step;               // outputs, and inputs, of a tile; rows of a step
     size_t part_bytes;
 };
@@ -240,6 +241,15 @@ int plan_kept_grad(KeptGradPlan &p, int N, int I, int O, int dtype)
     a.N = N; a.I = I; a.O = O;
     a.pitch = pitch_of(I);
     a.dy_stride = O;
+    if (N > 0 && N <= 128) {          // the gradients stay in registers: a work-group goes through its share of the inputs
+        p.slices = N <= 16 ? 1 : N <= 32 ? 2 : N <= 64 ? 4 : 8;
+        a.otiles = ceil_div(O, 128);
+        const int inputs = ceil_div(I, kFewInputs), shares = std::max(1, std::min(inputs, 768 / a.otiles));
+        a.rows_per_split = ceil_div(inputs, shares);
+        a.itiles = ceil_div(inputs, a.rows_per_split);
+        a.splits = 1;
+        return kStatusOk;
+    }
     // Large tiles, one work-group to a CU, feed the matrix units with half the traffic, where they fill the rounds of 256 that they
     // run in: 8192 rows 4096 -> 4096 bfloat16 220 us, 288 in tiles of 128, fp32 635 and 767; 9216 -> 4096 (576 tiles, three rounds)
     // 643 and 642, fp32 1716 and 1714
@@ -269,9 +279,19 @@ void launch_kept_grad(const KeptGradPlan &p, hipStream_t st)
     launch(fc_grad_kept_kernel<T, TILES, TILES, KS, OCC>, (int64_t)8 * p.a.per_xcd, 256, grad_lds<T, TILES, TILES, KS>(), st, p.a);
 }
 
+template <typename T, int SLICES, int OCC>
+void launch_few_grad(const KeptGradPlan &p, hipStream_t st)
+{
+    launch(fc_grad_few_kernel<T, SLICES, OCC>, (int64_t)p.a.otiles * p.a.itiles, 256, 0, st, p.a);
+}
+
 template <typename T>
 void run_kept_grad(const KeptGradPlan &p, hipStream_t st)
 {
+    if (p.slices == 1) return launch_few_grad<T, 1, 3>(p, st);
+    if (p.slices == 2) return launch_few_grad<T, 2, 3>(p, st);
+    if (p.slices == 4) return launch_few_grad<T, 4, 3>(p, st);
+    if (p.slices == 8) return launch_few_grad<T, 8, 3>(p, st);
     if constexpr (sizeof(T) == 4) {
         if (p.tile == 256) launch_kept_grad<T, 4, 32, 1>(p, st);
         else if (p.step == 32) launch_kept_grad<T, 2, 32, 2>(p, st);

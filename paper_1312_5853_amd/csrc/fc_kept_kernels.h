@@ -260,6 +260,123 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_kept_kernel(const KeptGradAr
             }
 }
 
+// ---------------------------------------------------------------------------
+// Few samples: up to 16 SLICES of them, at least one
+// ---------------------------------------------------------------------------
+// Bound by writing dw.  A work-group has 128 outputs, 32 to a wavefront, which keeps their gradients as fragments in registers, all
+// parts of all samples, made once; it goes through 64 inputs at a time, whose values alone pass through LDS, two buffers of them.
+// Nothing waits for a store: those of one 64 inputs drain while the next ones are multiplied.  (In tiles, whose work-groups load,
+// multiply and store all at the same time, 128 samples 9216 -> 4096 fp32 took 51 us.)
+constexpr int kFewInputs = 64;
+
+template <typename T, int SLICES, int OCC>
+__global__ __launch_bounds__(256, OCC) void fc_grad_few_kernel(const KeptGradArgs a)
+{
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
+    constexpr int ROWS = 16 * SLICES, XP = kFewInputs * 2, XB = ROWS * XP;
+    constexpr int NX = (ROWS * kFewInputs / 16 + 255) / 256, TX = ROWS * kFewInputs / 16 / NX;
+    __shared__ __attribute__((aligned(16))) char lds[2 * XB];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const int ot = blockIdx.x / a.itiles, first = (blockIdx.x - ot * a.itiles) * a.rows_per_split;         // (of inputs here)
+    const int count = min(a.rows_per_split, (a.I + kFewInputs - 1) / kFewInputs - first);
+    const int o0 = ot * 128 + wave * 32, o = o0 + (lane & 31);
+
+    // pieces of 16 codes: sample tid / 4, and 64 more for the second
+    const int xrow = tid % TX >> 2, xcol = (tid & 3) * 16;
+    u32x4 xraw[NX];
+    unsigned xbyte[NX];
+    auto load_x = [&](int j) {
+#pragma unroll
+        for (int u = 0; u < NX; ++u) {
+            const int n = u * (TX >> 2) + xrow;
+            xraw[u] = u32x4{0u, 0u, 0u, 0u};
+            xbyte[u] = 127;
+            if (n < a.N) {
+                const int64_t at = (int64_t)n * a.pitch + (int64_t)(first + j) * kFewInputs + xcol;
+                xraw[u] = *reinterpret_cast<const u32x4 *>(a.codes + at);
+                xbyte[u] = a.scales[at / kBlock];
+            }
+        }
+    };
+    // piece c of row n at place c ^ 4 (n / 2 % 2): rows of 128 bytes, four of them and 64 bytes of each to a read
+    auto store_x = [&](char *p) {
+#pragma unroll
+        for (int u = 0; u < NX; ++u) {
+            const int row = u * (TX >> 2) + xrow;
+            u32x4 v[2];
+            kept_to_bf16(xraw[u], xbyte[u], v);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                *reinterpret_cast<u32x4 *>(p + row * XP + ((((xcol >> 3) + h) ^ (4 * (row >> 1 & 1))) << 4)) = v[h];
+        }
+    };
+    if (count > 0) load_x(0);
+
+    // a lane has output o and samples 16 s + 8 (lane / 32) + 0 .. 7 of slice s
+    bf16x8 d[SLICES][PARTS];
+#pragma unroll
+    for (int s = 0; s < SLICES; ++s) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {                // all of them on their way; past the end the last one, which then is dropped
+            const int n = min(16 * s + 8 * (lane >> 5) + k, a.N - 1);
+            v[k] = ld_elem(static_cast<const T *>(a.dy) + (int64_t)n * a.dy_stride, min(o, a.O - 1));
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = 16 * s + 8 * (lane >> 5) + k < a.N && o < a.O ? v[k] : 0.f;
+        if constexpr (PARTS == 3) {
+            u32x4 part[3];
+            three_parts(v, part);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) d[s][p] = __builtin_bit_cast(bf16x8, part[p]);
+        } else {
+            u32x4 q;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) q[k] = __builtin_amdgcn_perm(__float_as_uint(v[2 * k + 1]), __float_as_uint(v[2 * k]), 0x07060302u);
+            d[s][0] = __builtin_bit_cast(bf16x8, q);
+        }
+    }
+    if (count > 0) store_x(lds);
+    if (count > 1) load_x(1);
+    __syncthreads();
+
+    const int fr = (lane >> 5) * 8 + ((lane & 15) >> 2), sw = 4 * ((lane & 15) >> 3);
+    const int fc = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), within = (lane & 1) * 8;
+    int xf[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) xf[q] = fr * XP + (((4 * q + fc) ^ sw) << 4) + within;
+    for (int j = 0; j < count; ++j) {
+        const char *const p = lds + (j & 1) * XB;
+        if (j + 1 < count) store_x(lds + ((j + 1) & 1) * XB);
+        if (j + 2 < count) load_x(j + 2);
+        f32x16 acc[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[q][v] = 0.f;
+#pragma unroll
+        for (int s = 0; s < SLICES; ++s) {
+            bf16x8 x[2];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) x[q] = read_transposed(p + xf[q] + s * 16 * XP, XP);
+#pragma unroll
+            for (int part = PARTS - 1; part >= 0; --part)                // the small parts first
+#pragma unroll
+                for (int q = 0; q < 2; ++q) acc[q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(d[s][part], x[q], acc[q], 0, 0, 0);
+        }
+        __syncthreads();
+        const int i0 = (first + j) * kFewInputs + (lane & 31);
+        float *const dw = a.dw + (int64_t)(o0 + (lane >> 5) * 4) * a.I;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int down = (v >> 2) * 8 + (v & 3);
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+                if (o0 + (lane >> 5) * 4 + down < a.O && i0 + 32 * q < a.I) dw[(int64_t)down * a.I + i0 + 32 * q] = acc[q][v];
+        }
+    }
+}
+
 // the splits' sums, one after the other
 __global__ __launch_bounds__(256) void fc_grad_join(const float *part, float *dw, int64_t count, int splits)
 {

@@ -241,7 +241,9 @@ int plan_kept_grad(KeptGradPlan &p, int N, int I, int O, int dtype)
     a.N = N; a.I = I; a.O = O;
     a.pitch = pitch_of(I);
     a.dy_stride = O;
-    if (N > 0 && N <= 128) {          // the gradients stay in registers: a work-group goes through its share of the inputs
+    // The gradients stay in registers, and a work-group goes through its share of the inputs: 128 rows 9216 -> 4096 fp32 39 us,
+    // 47 in tiles, bfloat16 30 and 36; one row 25 and 28, 25 and 35.
+    if (N > 0 && N <= 128) {
         p.slices = N <= 16 ? 1 : N <= 32 ? 2 : N <= 64 ? 4 : 8;
         a.otiles = ceil_div(O, 128);
         const int inputs = ceil_div(I, kFewInputs), shares = std::max(1, std::min(inputs, 768 / a.otiles));
@@ -255,8 +257,8 @@ int plan_kept_grad(KeptGradPlan &p, int N, int I, int O, int dtype)
     // 643 and 642, fp32 1716 and 1714
     const int64_t large = (int64_t)ceil_div(I, 256) * ceil_div(O, 256);
     p.tile = N >= 1024 && large >= 0.77 * round_up64(large, 256) ? 256 : 128;
-    // fp32 over few rows: shorter steps leave room for more work-groups, one of which stores while others multiply (128 rows
-    // 9216 -> 4096 49 us, and 58); over many the longer ones are faster (1024 rows 4096 -> 4096, large tiles, 100 and 106)
+    // fp32 over few rows: shorter steps leave room for more work-groups, one of which stores while others multiply (130 rows
+    // 9216 -> 4096 55 us, and 66; 256 rows 75 and 78); over many the longer ones are faster (1024 rows 4096 -> 4096 100 and 106)
     p.step = glue_elem_bytes(dtype) == 2 ? 64 : p.tile == 128 && N <= 256 ? 16 : 32;
     a.itiles = ceil_div(I, p.tile);
     a.otiles = ceil_div(O, p.tile);
@@ -310,8 +312,6 @@ int check_q4(int N, int I, int O, int dtype)
     return kStatusOk;
 }
 
-constexpr int kQ4Tile = 256;                         // outputs, and samples, of a large tile
-
 // The kernel for N > 32 samples: 0 the one for few, else the edge of the tiles.  Large tiles feed the matrix units with half the
 // traffic, where there is one for most of the CUs and the sum is long (x and y bfloat16, us a call, tiles of 256 and of 128):
 // 2048 x 8192 -> 8192 78 and 99, 1024 x 8192 -> 8192 58 and 53, 4096 x 4096 -> 4096 50 and 58, 2048 x 4096 -> 4096 39 and 33,
@@ -347,8 +347,8 @@ Q4Plan plan_q4(int N, int I, int O)
     if (p.fused) return p;
     p.wide = N <= 16 ? 1 : N <= 32 ? 2 : 4;
     p.xs = (size_t)round_up64((int64_t)N * p.steps * 64, 256);
-    p.nrows = round_up(N, kQ4Tile);
-    p.orows = round_up(O, kQ4Tile);
+    p.nrows = round_up(N, p.tile ? p.tile : 16 * p.wide);
+    p.orows = round_up(O, p.tile ? p.tile : 32);
     p.ws = p.xs + (size_t)p.steps * p.nrows * 4;
     p.total = p.ws + (size_t)p.steps * p.orows * 4;
     return p;

@@ -167,10 +167,14 @@ template <typename T, bool HELD, bool SUMS>
 void launch_layer_norm_bwd(const LayerNormPlan &p, int64_t blocks, hipStream_t st)
 {
     constexpr int few = 8 * (int)sizeof(T) / 16;         // vectors of eight values
-    if (few > 1 && p.regs == 1) launch(layer_norm_bwd_rows<T, HELD, 1, SUMS>, blocks, p.threads, p.lds, st, p.a);
-    else if (p.regs == few) launch(layer_norm_bwd_rows<T, HELD, few, SUMS>, blocks, p.threads, p.lds, st, p.a);
-    else if (p.regs == 2 * few) launch(layer_norm_bwd_rows<T, HELD, 2 * few, SUMS>, blocks, p.threads, p.lds, st, p.a);
-    else if constexpr (!SUMS) launch(layer_norm_bwd_rows<T, HELD, 3 * few, SUMS>, blocks, p.threads, p.lds, st, p.a);
+    if (few > 1 && p.regs == 1) return launch(layer_norm_bwd_rows<T, HELD, 1, SUMS, 1>, blocks, p.threads, p.lds, st, p.a);
+    // Two rows at a time in more than eight wavefronts of bfloat16 rows: 6001 x 5003 from 8 bits 47.5 us, and 50.8; with rows side
+    // by side it costs registers for nothing (8192 x 4096 39.0 us, and 37.4; 60000 x 300 31.7 and 28.5)
+    if constexpr (SUMS && few == 1)
+        if (p.regs == few && p.a.waves > 8) return launch(layer_norm_bwd_rows<T, HELD, few, true, 2>, blocks, p.threads, p.lds, st, p.a);
+    if (p.regs == few) return launch(layer_norm_bwd_rows<T, HELD, few, SUMS, 1>, blocks, p.threads, p.lds, st, p.a);
+    if (p.regs == 2 * few) return launch(layer_norm_bwd_rows<T, HELD, 2 * few, SUMS, 1>, blocks, p.threads, p.lds, st, p.a);
+    if constexpr (!SUMS) launch(layer_norm_bwd_rows<T, HELD, 3 * few, SUMS, 1>, blocks, p.threads, p.lds, st, p.a);
 }
 
 template <typename T, bool HELD>

@@ -342,16 +342,18 @@ __device__ __forceinline__ void column_sums(const LayerNormArgs &a, int tile, in
 // dx, and every work-group's sums of the columns over its rows (SUMS); or, over few rows, dgamma and dbeta by work-groups of their
 // own, which read the rows once more, from the cache, and save the launch that joins.  gamma lies in LDS.  With 8 values to a
 // thread the next row's are on their way (8192 x 4096 bfloat16 43 us, 56 with 16 values, which leave room for half the wavefronts).
+// U rows at a time, with one barrier to all, where a work-group has no more rows side by side.
 constexpr int layer_norm_bwd_waves(int values) { return values <= 8 ? 16 : 12; }        // most to a row, by values to a thread
 
-template <typename T, bool HELD, int R, bool SUMS>
+template <typename T, bool HELD, int R, bool SUMS, int U>
 __global__ __launch_bounds__(64 * layer_norm_bwd_waves(R * Vec<T>::V)) void layer_norm_bwd_rows(const LayerNormArgs a)
 {
     constexpr int V = Vec<T>::V;
     constexpr bool AHEAD = SUMS && R * V <= 8;
+    static_assert(U == 1 || AHEAD, "the next rows are on their way too");
     typedef RowSource<T, HELD> X;
     extern __shared__ __attribute__((aligned(16))) float shared[];       // gamma [vectors * V], then [groups][2][vectors * V]
-    __shared__ float lds[2][2][16];
+    __shared__ float lds[2][2 * U][16];
     if (!SUMS && (int)blockIdx.x >= a.row_blocks) {
         column_sums<T, HELD>(a, blockIdx.x - a.row_blocks, 0, a.N, shared, a.dgamma, a.dbeta);
         return;
@@ -371,12 +373,12 @@ __global__ __launch_bounds__(64 * layer_norm_bwd_waves(R * Vec<T>::V)) void laye
 #pragma unroll
             for (int k = 0; k < V; ++k) dgamma[r][k] = dbeta[r][k] = 0.f;
     }
-    const int64_t rows = (int64_t)a.row_blocks * a.groups;
+    const int64_t rows = (int64_t)a.row_blocks * a.groups * U;
     struct Row {
         typename X::Raw x[R];
         typename Vec<T>::Raw d[R];
         float mean, rstd;
-    } now, next;
+    } now[U], next[U];
     auto load = [&](int64_t row, Row &to) {
         const X x(a, row);
         const T *const dy = static_cast<const T *>(a.dy) + row * a.dy_stride;
@@ -394,7 +396,9 @@ __global__ __launch_bounds__(64 * layer_norm_bwd_waves(R * Vec<T>::V)) void laye
                 to.d[r] = {};
             }
     };
-    load((int64_t)blockIdx.x * a.groups + group, now);
+    const int64_t begin = (int64_t)blockIdx.x * a.groups * U;
+#pragma unroll
+    for (int u = 0; u < U; ++u) load(begin + u * a.groups + group, now[u]);
     __syncthreads();
     auto gamma_of = [&](int r, float (&v)[V]) {      // (a thread without a vector reads the first one)
         const float *const p = shared + (left[r] > 0 ? (t + r * step) * V : 0);
@@ -406,61 +410,79 @@ __global__ __launch_bounds__(64 * layer_norm_bwd_waves(R * Vec<T>::V)) void laye
         }
     };
     int turn = 0;
-    for (int64_t base = (int64_t)blockIdx.x * a.groups; base < a.N; base += rows, turn ^= 1) {
-        const int64_t row = base + group;
-        if constexpr (AHEAD) load(row + rows, next);
-        const float mean = now.mean, rstd = now.rstd;
+    for (int64_t base = begin; base < a.N; base += rows, turn ^= 1) {
+        if constexpr (AHEAD)
+#pragma unroll
+            for (int u = 0; u < U; ++u) load(base + rows + u * a.groups + group, next[u]);
         // past the row's end dy is zero, and so is what it adds
-        float s1 = 0.f, s2 = 0.f;
+        float s1[U], s2[U];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float x[V], d[V], g[V];
-            if (partial && left[r] > 0 && left[r] < V) {
-                X::settle(now.x[r], V - left[r]);
-                now.d[r] = move_down(now.d[r], V - left[r]);
-            }
-            X::open(now.x[r], x);
-            Vec<T>::open(now.d[r], d);
-            gamma_of(r, g);
+        for (int u = 0; u < U; ++u) {
+            Row &row = now[u];
+            s1[u] = s2[u] = 0.f;
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const float xh = (x[k] - mean) * rstd, gd = d[k] * g[k];
-                s1 += gd;
-                s2 += gd * xh;
-                if constexpr (SUMS) {
-                    dgamma[r][k] += d[k] * xh;
-                    dbeta[r][k] += d[k];
+            for (int r = 0; r < R; ++r) {
+                float x[V], d[V], g[V];
+                if (partial && left[r] > 0 && left[r] < V) {
+                    X::settle(row.x[r], V - left[r]);
+                    row.d[r] = move_down(row.d[r], V - left[r]);
+                }
+                X::open(row.x[r], x);
+                Vec<T>::open(row.d[r], d);
+                gamma_of(r, g);
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const float xh = (x[k] - row.mean) * row.rstd, gd = d[k] * g[k];
+                    s1[u] += gd;
+                    s2[u] += gd * xh;
+                    if constexpr (SUMS) {
+                        dgamma[r][k] += d[k] * xh;
+                        dbeta[r][k] += d[k];
+                    }
                 }
             }
         }
-        wave_sums(s1, s2);
+#pragma unroll
+        for (int u = 0; u < U; ++u) wave_sums(s1[u], s2[u]);
         if (a.waves > 1) {
-            if (lane == 0) { lds[turn][0][wave] = s1; lds[turn][1][wave] = s2; }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (lane == 0) { lds[turn][2 * u][wave] = s1[u]; lds[turn][2 * u + 1][wave] = s2[u]; }
             __syncthreads();
-            s1 = lane < a.waves ? lds[turn][0][first + lane] : 0.f;
-            s2 = lane < a.waves ? lds[turn][1][first + lane] : 0.f;
-            row_sums(s1, s2);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                s1[u] = lane < a.waves ? lds[turn][2 * u][first + lane] : 0.f;
+                s2[u] = lane < a.waves ? lds[turn][2 * u + 1][first + lane] : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) row_sums(s1[u], s2[u]);
         }
-        if (row < a.N) {
-            s1 *= a.inv_c;
-            s2 *= a.inv_c;
-            T *const dx = static_cast<T *>(a.out) + row * a.out_stride;
-            open_again(now.d);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = base + u * a.groups + group;
+            if (at >= a.N) continue;
+            Row &row = now[u];
+            const float m1 = s1[u] * a.inv_c, m2 = s2[u] * a.inv_c;
+            T *const dx = static_cast<T *>(a.out) + at * a.out_stride;
+            open_again(row.d);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const int v = t + r * step;
                 float x[V], d[V], g[V];
-                X::open(now.x[r], x);
-                Vec<T>::open(now.d[r], d);
+                X::open(row.x[r], x);
+                Vec<T>::open(row.d[r], d);
                 gamma_of(r, g);
 #pragma unroll
-                for (int k = 0; k < V; ++k) d[k] = rstd * (d[k] * g[k] - s1 - (x[k] - mean) * rstd * s2);
+                for (int k = 0; k < V; ++k) d[k] = row.rstd * (d[k] * g[k] - m1 - (x[k] - row.mean) * row.rstd * m2);
                 if (left[r] >= V) Vec<T>::store(dx + (int64_t)v * V, d);
                 else if (left[r] > 0) store_first(dx + (int64_t)v * V, d, left[r]);
             }
         }
-        if constexpr (AHEAD) now = next;
-        else if (base + rows < a.N) load(row + rows, now);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if constexpr (AHEAD) now[u] = next[u];
+            else if (base + rows < a.N) load(base + rows + u * a.groups + group, now[u]);
+        }
     }
     if constexpr (SUMS) {
         float *const out = a.part + (int64_t)blockIdx.x * 2 * a.C;

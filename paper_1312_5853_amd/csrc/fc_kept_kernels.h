@@ -27,7 +27,6 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-
 // 16 codes with their exponent as bfloat16
 __device__ __forceinline__ void kept_to_bf16(const u32x4 &w, unsigned byte, u32x4 (&out)[2])
 {
@@ -95,10 +94,11 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_kept_kernel(const KeptGradAr
     // where this thread's pieces lie: rows of n and columns
     const int xrow = tid % TX / (BI / 16), xcol = tid % (BI / 16);       // piece u: KS / NX rows on
     const int drow = tid / (BO / 8), dcol = tid % (BO / 8);
-    // A piece past the last output is the row's first one; one that goes past it has values of the next row.  No output is there,
-    // but the last row of all has no next one: steps up to `full` are read without a look at rows and columns.
+    // A piece past the last output is the row's first one; one that goes past it has values of the next row, or of up to seven of
+    // fewer than eight outputs.  No output is there, but the last rows of all have none behind them: steps up to `full` are read
+    // without a look at rows and columns.
     const int dat = o0 + dcol * 8 < a.O ? o0 + dcol * 8 : 0;
-    const int full = o0 + BO > a.O && a.O % 8 ? min(whole, (a.N - 1 - begin) / KS) : whole;
+    const int full = o0 + BO > a.O && a.O % 8 ? min(whole, (a.N - (a.O < 8 ? 7 : 1) - begin) / KS) : whole;
     // columns past the end of a row of codes are read from its start: no input is there
     const int64_t xat = i0 + xcol * 16 < a.pitch ? i0 + xcol * 16 : 0;
     u32x4 xraw[NX];

@@ -126,6 +126,13 @@ def test_filter_gradient(N, I, O, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("O", [1, 2, 3, 4, 7])
+@pytest.mark.parametrize("N", [129, 160, 263, 1280])
+def test_filter_gradient_of_fewer_outputs_than_a_load_takes(N, O, dtype):
+    check_grad(_values((N, 70), dtype, N + 70), _values((N, O), dtype, N + O, 1e-3), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("N,I,O", [(5, 40, 9), (130, 300, 260), (4100, 64, 100)])
 def test_filter_gradient_of_whole_numbers_is_exact(N, I, O, dtype):
     """Sums of products of small whole numbers are whole numbers below 2^24."""

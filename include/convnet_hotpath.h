@@ -468,11 +468,12 @@ int dequantize_blocks(const void *codes, const void *scales, void *x, int64_t x_
  *   dx = rstd * (g - mean(g) - xh * mean(g * xh)),   dgamma[c] = sum_n dy * xh,   dbeta[c] = sum_n dy  (fp32; each may be NULL)
  * layer_norm_bwd_kept: the same from x as it was kept in E4M3 blocks (codes, scales of C values to a row); mean and rstd are
  * those of the forward pass.
- * `dtype` names the element type of x, y, dy and dx as for the glue layers; arithmetic is fp32 (sums of more than 32 values to a
- * thread, and the join of a column's sums, in 64 bits), a bfloat16 result is rounded once.  Rows lie x_stride, y_stride, ... elements apart (>= C) and
- * may start anywhere.  eps > 0.  C <= 2^27, N * C < 2^40.  N = 0 is allowed (tensors over it may be NULL; dgamma and dbeta
- * become 0).  Outputs must not overlap inputs.  Scratch of the backward calls: layer_norm_workspace_bytes(CONV_OP_BWD_DATA, ...)
- * bytes, 256-byte aligned (0 for invalid arguments; none is needed without dgamma and dbeta).
+ * `dtype` names the element type of x, y, dy and dx as for the glue layers; arithmetic is fp32 (a row's sums over more than 32
+ * values to a thread in 64 bits, a column's over at most 256 rows to a thread in fp32, the parts' in 64 bits), a bfloat16 result is
+ * rounded once.  Rows lie x_stride, y_stride, ... elements apart (>= C) and may start anywhere.  eps > 0.  C <= 2^27,
+ * N * C < 2^40.  N = 0 is allowed (tensors over it may be NULL; dgamma and dbeta become 0).  Outputs must not overlap inputs.
+ * Scratch of the backward calls: layer_norm_workspace_bytes(CONV_OP_BWD_DATA, ...) bytes, 256-byte aligned (0 for invalid
+ * arguments; none is needed without dgamma and dbeta).
  */
 int layer_norm_fwd(const void *x, int64_t x_stride, const void *gamma, const void *beta, void *y, int64_t y_stride, void *mean,
                    void *rstd, int N, int C, float eps, int dtype, void *stream);

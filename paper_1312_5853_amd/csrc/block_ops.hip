@@ -34,6 +34,9 @@ int pow2_up(int v)
 
 constexpr int64_t kMaxElements = (int64_t)1 << 31;       // of a fully connected layer's tensors
 
+// of rows, whose number may be any that an int holds
+int parts_of(int n, int m) { return (n - 1) / m + 1; }
+
 int64_t pitch_of(int C) { return round_up64(C, kRowFill); }
 
 // codes are read and written 16 bytes at a time, exponents four
@@ -128,13 +131,13 @@ int plan_layer_norm(LayerNormPlan &p, int op, int N, int C, int dtype)
         p.apart = bwd && !p.columns && p.regs == 3 * few;
         // rows side by side in a work-group (backward their columns' sums are joined in LDS), as many as few rows leave for all CUs
         const int beside = (bwd ? 16 : 8) / a.waves;
-        a.groups = std::max(1, p.columns ? beside : std::min(beside, ceil_div(N, 256)));
+        a.groups = std::max(1, p.columns ? beside : std::min(beside, parts_of(N, 256)));
         p.threads = a.waves * a.groups * 64;
-        const int rounds = ceil_div(N, a.groups), width = a.vectors * V;
+        const int rounds = parts_of(N, a.groups), width = a.vectors * V;
         if (bwd) {
             // One to a CU, as every one's sums are written and read again (6001 x 5003 bfloat16 from 8 bits 52 us, 63 with two); but
             // a column's sum in a thread runs over at most 256 rows.
-            a.row_blocks = std::min(rounds, std::max(256, ceil_div(rounds, 256)));
+            a.row_blocks = std::min(rounds, std::max(256, parts_of(rounds, 256)));
             p.blocks = a.row_blocks;
             a.part_rows = p.columns ? 0 : a.row_blocks;
             p.lds = (size_t)std::max(width * (a.groups > 1 && !p.columns && !p.apart ? 2 * a.groups : 1), p.columns ? 2 * p.threads : 0) * 4;
@@ -144,9 +147,9 @@ int plan_layer_norm(LayerNormPlan &p, int op, int N, int C, int dtype)
     }
     if (p.apart) {
         const int tiles = (C + 63) / 64;
-        a.part_rows = std::max(1, std::min(ceil_div(N, 256), 2048 / tiles));
-        a.rows_per_part = std::max(1, ceil_div(N, a.part_rows));
-        a.part_rows = std::max(1, ceil_div(N, a.rows_per_part));
+        a.part_rows = std::max(1, std::min(parts_of(N, 256), 2048 / tiles));
+        a.rows_per_part = std::max(1, parts_of(N, a.part_rows));
+        a.part_rows = parts_of(N, a.rows_per_part);
     }
     if (bwd) p.part_bytes = (size_t)round_up64((int64_t)a.part_rows * 2 * C * 4, 256);
     return kStatusOk;

@@ -300,14 +300,14 @@ __global__ __launch_bounds__(1024) void layer_norm_fwd_wide(const LayerNormArgs 
 }
 
 // Sums of 64 columns over the rows from `begin` on, before `end`, by the work-group's wavefronts: a row to each at a time, four
-// rows' loads together.
+// rows' loads together, and a sum of four rows after the other in 64 bits, as a part may have any number of rows.
 template <typename T, bool HELD>
 __device__ __forceinline__ void column_sums(const LayerNormArgs &a, int tile, int64_t begin, int64_t end, float *lds, float *dgamma,
                                             float *dbeta)
 {
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int c = tile * 64 + lane;
-    float sg = 0.f, sb = 0.f;
+    double sg = 0.0, sb = 0.0;
     if (c < a.C)
         for (int64_t row = begin + wave; row < end; row += 4 * waves) {
             float d[4], x[4], mean[4], rstd[4];
@@ -319,22 +319,25 @@ __device__ __forceinline__ void column_sums(const LayerNormArgs &a, int tile, in
                 mean[k] = a.mean[at];
                 rstd[k] = a.rstd[at];
             }
+            float fg = 0.f, fb = 0.f;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (row + k * waves < end) {
-                    sg += d[k] * ((x[k] - mean[k]) * rstd[k]);
-                    sb += d[k];
+                    fg += d[k] * ((x[k] - mean[k]) * rstd[k]);
+                    fb += d[k];
                 }
+            sg += fg;
+            sb += fb;
         }
-    lds[wave * 64 + lane] = sg;
-    lds[(waves + wave) * 64 + lane] = sb;
+    lds[wave * 64 + lane] = (float)sg;
+    lds[(waves + wave) * 64 + lane] = (float)sb;
     __syncthreads();
     if (wave < 2 && c < a.C) {                       // one wavefront, or two, join them
         for (int which = wave; which < 2; which += waves > 1 ? 2 : 1) {
-            float s = 0.f;
+            double s = 0.0;
             for (int w = 0; w < waves; ++w) s += lds[(which * waves + w) * 64 + lane];
             float *const out = which ? dbeta : dgamma;
-            if (out) out[c] = s;
+            if (out) out[c] = (float)s;
         }
     }
 }

@@ -200,3 +200,14 @@ def test_columns_over_many_rows():
     mean, rstd = torch.zeros(N, device="cuda"), torch.ones(N, device="cuda")
     dx, dgamma, dbeta = hp.layer_norm_bwd(x, dy, mean, rstd)
     assert dbeta.tolist() == [N] * 4 and dgamma.tolist() == [N, 0, 0, 0]
+
+
+def test_columns_of_rows_longer_than_a_work_group_keeps_over_many():
+    """4096 times 1 + 0.75 2^-17, each sum of a thread over 256 of them: one after the other in fp32, from 128 on every one would lose
+    what it has behind the 1, 2^-18.7 of the result.  Four are summed in fp32 (3 u), then in 64 bits but for a rounding to a part's
+    32 bits, one to a work-group's and one of the result."""
+    N, C, v = 4096, 131072, 1 + 0.75 * 2.0 ** -17
+    x, dy = torch.zeros((N, C), device="cuda"), torch.full((N, C), v, device="cuda")
+    dx, dgamma, dbeta = hp.layer_norm_bwd(x, dy, torch.full((N,), -1.0, device="cuda"), torch.ones(N, device="cuda"))
+    for got in (dgamma, dbeta):
+        assert (np.abs(_host(got) - N * v) <= 6 * U * N * v).all()

@@ -929,6 +929,10 @@ def _fc_q4_workspace_bytes(N, I, O, dtype):
     return int(lib().fc_q4_workspace_bytes(N, I, O, dtype))
 
 
+_BLOCK_BYTES = {"e4m3": 32, "e2m1": 16}
+_ROW_BLOCKS = BLOCK_ROW_FILL // BLOCK_VALUES
+
+
 class Blocks:
     """A tensor [N, cols] held in blocks of 32 values with a shared power of two: `codes` and `scales` (uint8, rows filled up
     to a multiple of 128 values) and the format's name, "e4m3" (8 bits) or "e2m1" (4 bits).  quantize_blocks makes one."""
@@ -937,15 +941,15 @@ class Blocks:
     def __init__(self, codes, scales, cols, format):
         if type(cols) is not int:
             cols, = _whole(cols)
-        if format not in BLOCK_FORMATS:
+        bytes_to_32 = _BLOCK_BYTES.get(format)
+        if bytes_to_32 is None:
             raise ValueError("unknown block format %r" % (format,))
-        pitch = -(-cols // BLOCK_ROW_FILL) * BLOCK_ROW_FILL
-        shape = codes.shape
+        shape, blocks = codes.shape, (cols + BLOCK_ROW_FILL - 1) // BLOCK_ROW_FILL * _ROW_BLOCKS
         if codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8:
             raise TypeError("codes and scales are bytes")
-        if (cols < 1 or len(shape) != 2 or shape[1] != (pitch if format == "e4m3" else pitch // 2)
-                or scales.shape != (shape[0], pitch // BLOCK_VALUES) or not codes.is_contiguous() or not scales.is_contiguous()):
-            raise ValueError("codes and scales must be dense, with rows of %d values and their exponents" % pitch)
+        if (cols < 1 or len(shape) != 2 or shape[1] != blocks * bytes_to_32 or scales.shape != (shape[0], blocks)
+                or not codes.is_contiguous() or not scales.is_contiguous()):
+            raise ValueError("codes and scales must be dense, with rows of %d values and their exponents" % (blocks * BLOCK_VALUES))
         if codes.get_device() != scales.get_device():
             raise ValueError("the tensors of a call must be on one GPU")
         self.codes, self.scales, self.cols, self.format = codes, scales, cols, format

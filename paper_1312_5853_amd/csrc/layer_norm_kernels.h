@@ -365,7 +365,6 @@ __global__ __launch_bounds__(64 * layer_norm_bwd_waves(R * Vec<T>::V)) void laye
     const int group = wave / a.waves, first = group * a.waves;
     const int t = (wave - first) * 64 + lane, step = a.waves * 64;
     const int width = a.vectors * V;
-    for (int i = threadIdx.x; i < width; i += blockDim.x) shared[i] = a.gamma && i < a.C ? a.gamma[i] : 1.f;
     float dgamma[SUMS ? R : 1][V], dbeta[SUMS ? R : 1][V];
     int left[R];                                     // of the row's values, from this vector on
     const bool partial = a.C >= V && a.C % V;        // (the rows of fewer values are read as they are)
@@ -402,6 +401,16 @@ __global__ __launch_bounds__(64 * layer_norm_bwd_waves(R * Vec<T>::V)) void laye
     const int64_t begin = (int64_t)blockIdx.x * a.groups * U;
 #pragma unroll
     for (int u = 0; u < U; ++u) load(begin + u * a.groups + group, now[u]);
+    // every thread puts down what it will read itself (rows side by side the same), as loads that do not wait for each other
+    float own[R][V];
+#pragma unroll
+    for (int r = 0; r < R; ++r) load_affine(a.gamma, (t + r * step) * V, left[r], 1.f, own[r]);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (left[r] > 0)
+#pragma unroll
+            for (int h = 0; h < V; h += 4)
+                *reinterpret_cast<f32x4 *>(shared + (t + r * step) * V + h) = f32x4{own[r][h], own[r][h + 1], own[r][h + 2], own[r][h + 3]};
     __syncthreads();
     auto gamma_of = [&](int r, float (&v)[V]) {      // (a thread without a vector reads the first one)
         const float *const p = shared + (left[r] > 0 ? (t + r * step) * V : 0);
@@ -489,17 +498,25 @@ __global__ __launch_bounds__(64 * layer_norm_bwd_waves(R * Vec<T>::V)) void laye
     }
     if constexpr (SUMS) {
         float *const out = a.part + (int64_t)blockIdx.x * 2 * a.C;
+        auto put = [&](float *to, const float (&v)[V], int n) {
+            if (n >= V) {
+#pragma unroll
+                for (int h = 0; h < V; h += 4) *reinterpret_cast<f32x4_any *>(to + h) = f32x4{v[h], v[h + 1], v[h + 2], v[h + 3]};
+                return;
+            }
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (k < n) to[k] = v[k];
+        };
         if (a.groups > 1) {
             __syncthreads();                         // gamma is no longer needed
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const int v = t + r * step;
-                if (v < a.vectors)
-#pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        shared[(2 * group) * width + v * V + k] = dgamma[r][k];
-                        shared[(2 * group + 1) * width + v * V + k] = dbeta[r][k];
-                    }
+                if (v < a.vectors) {
+                    put(shared + 2 * group * width + v * V, dgamma[r], V);
+                    put(shared + (2 * group + 1) * width + v * V, dbeta[r], V);
+                }
             }
             __syncthreads();
             for (int i = threadIdx.x; i < 2 * width; i += blockDim.x) {
@@ -511,13 +528,10 @@ __global__ __launch_bounds__(64 * layer_norm_bwd_waves(R * Vec<T>::V)) void laye
             return;
         }
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int k = 0; k < V; ++k)
-                if (k < left[r]) {
-                    out[(t + r * step) * V + k] = dgamma[r][k];
-                    out[a.C + (t + r * step) * V + k] = dbeta[r][k];
-                }
+        for (int r = 0; r < R; ++r) {
+            put(out + (t + r * step) * V, dgamma[r], left[r]);
+            put(out + a.C + (t + r * step) * V, dbeta[r], left[r]);
+        }
     }
 }
 

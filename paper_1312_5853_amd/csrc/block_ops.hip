@@ -124,8 +124,8 @@ int plan_layer_norm(LayerNormPlan &p, int op, int N, int C, int dtype)
         a.waves = std::min(most_waves, ceil_div(chunks, few));
         const int runs = ceil_div(chunks, a.waves);
         p.regs = runs <= 2 * few ? pow2_up(runs) : 3 * few;
-        // dgamma and dbeta by work-groups of their own, over few rows in the same launch (fp32, us: 512 x 1024 9.0 and 11.3, 512 x 9216
-        // 22.7 and 26.8, 768 x 1024 12.0 and 10.9), and where a thread has no registers left for sums (24 values; 3000 x 16384 fp32
+        // dgamma and dbeta by work-groups of their own, over few rows in the same launch (us: 512 x 1024 fp32 9.2 and 10.9, 512 x 9216
+        // 22.2 and 22.1, bfloat16 14.4 and 20.1, 768 x 1024 fp32 11.9 and 10.5), and where a thread has no registers left for sums (24 values; 3000 x 16384 fp32
         // with them, spilt, 368 us)
         p.columns = bwd && N <= 640;
         p.apart = bwd && !p.columns && p.regs == 3 * few;
@@ -135,7 +135,7 @@ int plan_layer_norm(LayerNormPlan &p, int op, int N, int C, int dtype)
         p.threads = a.waves * a.groups * 64;
         const int rounds = parts_of(N, a.groups), width = a.vectors * V;
         if (bwd) {
-            // One to a CU, as every one's sums are written and read again (6001 x 5003 bfloat16 from 8 bits 52 us, 63 with two); but
+            // One to a CU, as every one's sums are written and read again (6001 x 5003 bfloat16 from 8 bits 43 us, 49 with two); but
             // a column's sum in a thread runs over at most 256 rows.
             a.row_blocks = std::min(rounds, std::max(256, parts_of(rounds, 256)));
             p.blocks = a.row_blocks;
@@ -171,8 +171,9 @@ void launch_layer_norm_bwd(const LayerNormPlan &p, int64_t blocks, hipStream_t s
 {
     constexpr int few = 8 * (int)sizeof(T) / 16;         // vectors of eight values
     if (few > 1 && p.regs == 1) return launch(layer_norm_bwd_rows<T, HELD, 1, SUMS, 1>, blocks, p.threads, p.lds, st, p.a);
-    // Two rows at a time in more than eight wavefronts of bfloat16 rows: 6001 x 5003 from 8 bits 47.5 us, and 50.8; with rows side
-    // by side it costs registers for nothing (8192 x 4096 39.0 us, and 37.4; 60000 x 300 31.7 and 28.5)
+    // Two rows at a time in more than eight wavefronts of bfloat16 rows, whose loads cover more of the memory's latency: 6001 x 5003
+    // from 8 bits 48.8 us, and 52.5, over inputs that the last cache no longer holds (43 both where it does); with rows side by side
+    // it costs registers for nothing (8192 x 4096 39.0 us, and 37.4; 60000 x 300 31.7 and 28.5)
     if constexpr (SUMS && few == 1)
         if (p.regs == few && p.a.waves > 8) return launch(layer_norm_bwd_rows<T, HELD, few, true, 2>, blocks, p.threads, p.lds, st, p.a);
     if (p.regs == few) return launch(layer_norm_bwd_rows<T, HELD, few, SUMS, 1>, blocks, p.threads, p.lds, st, p.a);

@@ -265,8 +265,10 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_kept_kernel(const KeptGradAr
 // ---------------------------------------------------------------------------
 // Bound by writing dw.  A work-group has 128 outputs, 32 to a wavefront, which keeps their gradients as fragments in registers, all
 // parts of all samples, made once; it goes through 64 inputs at a time, whose values alone pass through LDS, two buffers of them.
-// Nothing waits for a store: those of one 64 inputs drain while the next ones are multiplied.  (In tiles, whose work-groups load,
-// multiply and store all at the same time, 128 samples 9216 -> 4096 fp32 took 51 us.)
+// Nothing waits for a store: those of one 64 inputs drain while the next ones are multiplied.  They are marked as not read again
+// soon where they are whole cache lines (128 samples 9216 -> 4096 fp32 37 us, 40 without the mark, with an update that reads dw
+// behind it 178 and 183; of parts of lines it costs: 9217 -> 4096 92 and 63).  (In tiles, whose work-groups load, multiply and
+// store all at the same time, the first took 51 us.)
 constexpr int kFewInputs = 64;
 
 template <typename T, int SLICES, int OCC>
@@ -281,21 +283,20 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_few_kernel(const KeptGradArg
     const int count = min(a.rows_per_split, (a.I + kFewInputs - 1) / kFewInputs - first);
     const int o0 = ot * 128 + wave * 32, o = o0 + (lane & 31);
 
-    // pieces of 16 codes: sample tid / 4, and 64 more for the second
+    // Pieces of 16 codes: sample tid / 4, and 64 more for the second.  Past the last sample it is the last one again, times gradients
+    // of zero: where that is NaN, so is the sum with the last one itself.  (No branch, behind which each load would be waited for.)
     const int xrow = tid % TX >> 2, xcol = (tid & 3) * 16;
     u32x4 xraw[NX];
     unsigned xbyte[NX];
-    auto load_x = [&](int j) {
+    int64_t xat[NX];
+#pragma unroll
+    for (int u = 0; u < NX; ++u) xat[u] = (int64_t)min(u * (TX >> 2) + xrow, a.N - 1) * a.pitch + (int64_t)first * kFewInputs + xcol;
+    auto load_x = [&](int j) {                       // past the last step that one again
+        const int at = min(j, count - 1) * kFewInputs;
 #pragma unroll
         for (int u = 0; u < NX; ++u) {
-            const int n = u * (TX >> 2) + xrow;
-            xraw[u] = u32x4{0u, 0u, 0u, 0u};
-            xbyte[u] = 127;
-            if (n < a.N) {
-                const int64_t at = (int64_t)n * a.pitch + (int64_t)(first + j) * kFewInputs + xcol;
-                xraw[u] = *reinterpret_cast<const u32x4 *>(a.codes + at);
-                xbyte[u] = a.scales[at / kBlock];
-            }
+            xraw[u] = *reinterpret_cast<const u32x4 *>(a.codes + xat[u] + at);
+            xbyte[u] = a.scales[(xat[u] + at) / kBlock];
         }
     };
     // piece c of row n at place c ^ 4 (n / 2 % 2): rows of 128 bytes, four of them and 64 bytes of each to a read
@@ -310,17 +311,20 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_few_kernel(const KeptGradArg
                 *reinterpret_cast<u32x4 *>(p + row * XP + ((((xcol >> 3) + h) ^ (4 * (row >> 1 & 1))) << 4)) = v[h];
         }
     };
-    if (count > 0) load_x(0);
+    load_x(0);
 
-    // a lane has output o and samples 16 s + 8 (lane / 32) + 0 .. 7 of slice s
+    // a lane has output o and samples 16 s + 8 (lane / 32) + 0 .. 7 of slice s; past the end it reads its first one, or the last of
+    // all, which then is dropped
     bf16x8 d[SLICES][PARTS];
+    const int n0 = min(8 * (lane >> 5), a.N - 1);
+    const T *const dp = static_cast<const T *>(a.dy) + (int64_t)n0 * a.dy_stride + min(o, a.O - 1);
 #pragma unroll
     for (int s = 0; s < SLICES; ++s) {
         float v[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {                // all of them on their way; past the end the last one, which then is dropped
-            const int n = min(16 * s + 8 * (lane >> 5) + k, a.N - 1);
-            v[k] = ld_elem(static_cast<const T *>(a.dy) + (int64_t)n * a.dy_stride, min(o, a.O - 1));
+        for (int k = 0; k < 8; ++k) {                // (masks: a choice between addresses becomes branches, which wait for each load)
+            const int64_t there = (n0 + 16 * s + k - a.N) >> 31;
+            v[k] = ld_elem(dp + ((16 * s + k) * a.dy_stride & there), 0);
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = 16 * s + 8 * (lane >> 5) + k < a.N && o < a.O ? v[k] : 0.f;
@@ -336,8 +340,8 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_few_kernel(const KeptGradArg
             d[s][0] = __builtin_bit_cast(bf16x8, q);
         }
     }
-    if (count > 0) store_x(lds);
-    if (count > 1) load_x(1);
+    store_x(lds);
+    load_x(1);
     __syncthreads();
 
     const int fr = (lane >> 5) * 8 + ((lane & 15) >> 2), sw = 4 * ((lane & 15) >> 3);
@@ -345,10 +349,14 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_few_kernel(const KeptGradArg
     int xf[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) xf[q] = fr * XP + (((4 * q + fc) ^ sw) << 4) + within;
-    for (int j = 0; j < count; ++j) {
+    // One 64 inputs; lines: all of the wavefront's outputs and inputs are there, in whole cache lines.  Loads and stores are counted
+    // together, in their order: where every path stores as often, the wait for the next values leaves this step's stores under way.
+    auto do_step = [&](int j, auto lines_c) {
+        constexpr bool lines = decltype(lines_c)::value;
         const char *const p = lds + (j & 1) * XB;
-        if (j + 1 < count) store_x(lds + ((j + 1) & 1) * XB);
-        if (j + 2 < count) load_x(j + 2);
+        store_x(lds + ((j + 1) & 1) * XB);
+        load_x(j + 2);
+        __builtin_amdgcn_sched_barrier(0);
         f32x16 acc[2];
 #pragma unroll
         for (int q = 0; q < 2; ++q)
@@ -366,15 +374,22 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_few_kernel(const KeptGradArg
         }
         __syncthreads();
         const int i0 = (first + j) * kFewInputs + (lane & 31);
-        float *const dw = a.dw + (int64_t)(o0 + (lane >> 5) * 4) * a.I;
+        float *const dw = a.dw + (int64_t)(o0 + (lane >> 5) * 4) * a.I + i0;
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
             const int down = (v >> 2) * 8 + (v & 3);
 #pragma unroll
             for (int q = 0; q < 2; ++q)
-                if (o0 + (lane >> 5) * 4 + down < a.O && i0 + 32 * q < a.I) dw[(int64_t)down * a.I + i0 + 32 * q] = acc[q][v];
+                if (lines) __builtin_nontemporal_store(acc[q][v], dw + (int64_t)down * a.I + 32 * q);
+                else if (o0 + (lane >> 5) * 4 + down < a.O && i0 + 32 * q < a.I) dw[(int64_t)down * a.I + 32 * q] = acc[q][v];
         }
-    }
+    };
+    __builtin_amdgcn_s_waitcnt(0x0F70);                                  // vmcnt(0): the loop's waits then count its own alone
+    const bool lines = o0 + 32 <= a.O && a.I % 32 == 0 && (reinterpret_cast<uintptr_t>(a.dw) & 127) == 0;
+    const int whole = lines ? min(count, a.I / kFewInputs - first) : 0;
+    int j = 0;
+    for (; j < whole; ++j) do_step(j, std::true_type{});
+    for (; j < count; ++j) do_step(j, std::false_type{});
 }
 
 // the splits' sums, one after the other

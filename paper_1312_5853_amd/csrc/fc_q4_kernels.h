@@ -450,20 +450,23 @@ __global__ __launch_bounds__(WAVES * 64) void fc_q4_rows(const Q4RowsArgs a)
         const char *const buf = ring + slot * STAGE;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            if (h == 1 && 2 * p + 1 >= a.steps) break;
+            // Where there is no second step it is the first one again, times zero: a block that is NaN has made its sums NaN before.
+            // (A branch costs a copy of all sums, 32 instructions to 16 products.)
+            const int keep = 2 * p + h < a.steps ? -1 : 0;
             const int at = ((4 * h + g) ^ swz) * 16;
             i32x4 w[AO], x[J];
             unsigned ew[AO], ex[J];
 #pragma unroll
             for (int i = 0; i < AO; ++i) {
-                w[i] = *reinterpret_cast<const i32x4 *>(buf + (16 * i + r) * 128 + at);
+                w[i] = *reinterpret_cast<const i32x4 *>(buf + (16 * i + r) * 128 + at) & keep;
                 ew[i] = static_cast<unsigned char>(buf[EXPA + (h * RA + 16 * i + r) * 4 + g]);
             }
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 if constexpr (FUSED) {
-                    x[j] = *reinterpret_cast<const i32x4 *>(fc + (2 * p + h) * 64);
-                    ex[j] = static_cast<unsigned char>(fe[(2 * p + h) * 4]);
+                    const int step = 2 * p + (h & keep);
+                    x[j] = *reinterpret_cast<const i32x4 *>(fc + step * 64);
+                    ex[j] = static_cast<unsigned char>(fe[step * 4]);
                 } else {
                     x[j] = *reinterpret_cast<const i32x4 *>(buf + (RA + 16 * j + r) * 128 + at);
                     ex[j] = static_cast<unsigned char>(buf[EXPB + (h * RB + 16 * j + r) * 4 + g]);

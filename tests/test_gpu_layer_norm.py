@@ -211,3 +211,20 @@ def test_columns_of_rows_longer_than_a_work_group_keeps_over_many():
     dx, dgamma, dbeta = hp.layer_norm_bwd(x, dy, torch.full((N,), -1.0, device="cuda"), torch.ones(N, device="cuda"))
     for got in (dgamma, dbeta):
         assert (np.abs(_host(got) - N * v) <= 6 * U * N * v).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,C", [(3, 1), (3, 5), (2, 9), (4, 300), (2, 4096), (2, 4100), (3, 5003), (2, 9217), (2, 16001), (2, 33000),
+                                 (3, 33003), (700, 301), (700, 4099), (700, 9217), (700, 16001)])
+def test_rows_whose_mean_times_rstd_is_past_fp32(N, C, dtype):
+    """2^110 throughout, with the statistics of eps = 1e-12: every distance from the mean is zero and so is xh, whatever the threads
+    without a value of the row make of the mean, -2^110 1e6 = -1.3e39."""
+    g = np.random.Generator(np.random.Philox(C))
+    x, dy = np.full((N, C), 2.0 ** 110, np.float32), _values((N, C), dtype, g)
+    gamma = (1.0 + 0.3 * g.standard_normal(C)).astype(np.float32)
+    xd, dyd = _dev(x, dtype), _dev(dy, dtype)
+    _, m, r = hp.layer_norm_fwd(xd, eps=1e-12)
+    mean, rstd = _host(m).astype(np.float32), _host(r).astype(np.float32)
+    assert (mean == 2.0 ** 110).all() and (np.abs(rstd - 1e6) <= 1).all()
+    check_bwd(hp.layer_norm_bwd(xd, dyd, m, r, _vec(gamma)), x, dy, mean, rstd, gamma, dtype)
+    check_bwd(hp.layer_norm_bwd_kept(hp.quantize_blocks(xd, "e4m3"), dyd, m, r, _vec(gamma)), x, dy, mean, rstd, gamma, dtype)

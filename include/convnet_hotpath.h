@@ -444,7 +444,7 @@ size_t distill_loss_workspace_bytes(int N, int V, int K, int dtype);
  * A block's power is 2^e with e the smallest integer from -117 (E4M3) or -125 (E2M1) on under which its largest magnitude is
  * at most 448 or 6 times it; x / 2^e is rounded to the nearest number of the format, to the even code where two are as near.
  * So a value comes back within 2^-4 (E4M3) of itself or, below, half the format's least step times 2^e.  A block that holds an
- * infinity or a NaN is all NaN.  (A value within 7 % (E4M3) or 13 % (E2M1) of 2^128 can come back as infinity.)
+ * infinity or a NaN is all NaN.  (A value within 3.2 % (E4M3) or 13 % (E2M1) of 2^128 can come back as infinity.)
  *   codes:  [N][P] (E4M3) or [N][P / 2] bytes (E2M1: two to a byte, the first in the low bits), P = C rounded up to a multiple
  *           of 128, codes past C zero; 16-byte aligned
  *   scales: [N][P / 32] bytes, e + 127, 255 for a block of NaN; 4-byte aligned
@@ -490,7 +490,8 @@ size_t layer_norm_workspace_bytes(int op, int N, int C, int dtype);
  * fc_bwd_filter, dense, any I and O, each tensor (rows of codes filled up) below 2^31 elements.
  *   fc_bwd_filter_kept: dw[o][i] = sum_n dy[n][o] * x[n][i] with x as it was kept in E4M3 blocks.  dtype: element type of dy
  *                       (as for the glue layers); dw is fp32.  Products are exact in both types (of an fp32 dy below 2^-110
- *                       less than 2^-133 is cut off), sums fp32.  N = 0: dw = 0.
+ *                       less than 2^-133 is cut off), sums fp32; a value that comes back as infinity counts as one.
+ *                       N = 0: dw = 0.
  *   fc_fwd_q4:          y[n][o] = f(sum_i x4[n][i] * w[o][i] + bias[o]) with w in E2M1 blocks, made once by quantize_blocks,
  *                       and x4 what quantize_blocks makes of x in E2M1 (within the call).  bias fp32 [O] or NULL; f = max(., 0) if
  *                       relu = 1, identity if relu = 0; NaN stays NaN.  dtype as for a convolution: CONV_DTYPE_F32 x and y

@@ -58,6 +58,33 @@ __device__ __forceinline__ void three_parts(const float (&v)[8], u32x4 (&part)[3
         for (int k = 0; k < 4; ++k) part[p][k] = __builtin_amdgcn_perm(u[p][2 * k + 1], u[p][2 * k], 0x07060302u);
 }
 
+// A value read back from a block of this exponent may be infinite (448 2^119 is below 2^128, 256 2^120 is not); 255 holds no numbers.
+__device__ __forceinline__ bool may_be_infinite(unsigned byte) { return byte - 247u < 8u; }
+
+// Of fp32 gradients one infinite value times three parts is no number wherever a part is zero.  If input i has one in the samples begin
+// .. end - 1, its sums again, product by product: those of a lane's 16 outputs of a block of 32 (see the kernels) from `first` on.
+__device__ __forceinline__ void infinite_input(const KeptGradArgs &a, float *dw, int begin, int end, int i, int first)
+{
+    if (i >= a.I) return;
+    auto value = [&](int n) {
+        const int64_t at = (int64_t)n * a.pitch + i;
+        return __builtin_amdgcn_cvt_f32_fp8((int)a.codes[at], 0) * block_scale(a.scales[at / kBlock]);
+    };
+    bool infinite = false;
+#pragma unroll 1
+    for (int n = begin; n < end; ++n) infinite |= fabsf(value(n)) == INFINITY;
+    if (!infinite) return;
+#pragma unroll 1
+    for (int v = 0; v < 16; ++v) {
+        const int o = first + (v >> 2) * 8 + (v & 3);
+        if (o >= a.O) break;                         // (they ascend)
+        double s = 0.0;
+#pragma unroll 1
+        for (int n = begin; n < end; ++n) s += (double)static_cast<const float *>(a.dy)[(int64_t)n * a.dy_stride + o] * value(n);
+        dw[(int64_t)o * a.I + i] = (float)s;
+    }
+}
+
 __device__ __forceinline__ bf16x8 read_transposed(const char *p, int pitch)          // n 0..3 from p, 4..7 four rows on
 {
     typedef __attribute__((address_space(3))) s16x4 *Lds;
@@ -104,6 +131,7 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_kept_kernel(const KeptGradAr
     const int64_t xat = i0 + xcol * 16 < a.pitch ? i0 + xcol * 16 : 0;
     u32x4 xraw[NX];
     unsigned xbyte[NX];
+    int seen = 0;                                    // a value that may be infinite
     typename Vec<T>::Raw draw[ND][sizeof(T) / 2];
     const unsigned char *const xp = a.codes + (int64_t)(begin + xrow) * a.pitch + xat;
     const unsigned char *const ep = a.scales + ((int64_t)(begin + xrow) * a.pitch + xat) / kBlock;
@@ -134,6 +162,7 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_kept_kernel(const KeptGradAr
             const int row = u * (KS / NX) + xrow;
             u32x4 v[2];
             kept_to_bf16(xraw[u], xbyte[u], v);
+            if (PARTS == 3 && may_be_infinite(xbyte[u])) seen = 1;
 #pragma unroll
             for (int h = 0; h < 2; ++h) *reinterpret_cast<u32x4 *>(p + row * XP + (((2 * xcol + h) ^ (4 * (row & 3))) << 4)) = v[h];
             return;
@@ -249,6 +278,14 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_kept_kernel(const KeptGradAr
         for (; s + 2 < full; ++s) do_step(s, std::true_type{});
         for (; s < steps; ++s) do_step(s, std::false_type{});
     }
+    bool infinite = false;
+    if constexpr (PARTS == 3) {                      // of any thread; the last step has left LDS free
+        int *const all = reinterpret_cast<int *>(lds_grad);
+        const int any = __ballot(seen) != 0;
+        if (lane == 0) all[wave] = any;
+        __syncthreads();
+        infinite = uniform(all[0] | all[1] | all[2] | all[3]);
+    }
     float *const dw = a.dw + (int64_t)split * a.O * a.I;
 #pragma unroll
     for (int m = 0; m < TM; ++m)
@@ -259,6 +296,12 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_kept_kernel(const KeptGradAr
                 const int o = o0 + wo + m * 32 + (lane >> 5) * 4 + (v >> 2) * 8 + (v & 3), i = i0 + wi + q * 32 + (lane & 31);
                 if (o < a.O && i < a.I) dw[(int64_t)o * a.I + i] = acc[m][q][v];
             }
+    if (infinite) {
+        __threadfence();                             // behind this lane's own stores
+#pragma unroll 1
+        for (int b = 0; b < TM * TN; ++b)
+            infinite_input(a, dw, begin, end, i0 + wi + b % TN * 32 + (lane & 31), o0 + wo + b / TN * 32 + (lane >> 5) * 4);
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -279,19 +322,22 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_few_kernel(const KeptGradArg
     constexpr int ROWS = 16 * SLICES, XP = kFewInputs * 2, XB = ROWS * XP;
     constexpr int NX = (ROWS * kFewInputs / 16 + 255) / 256, TX = ROWS * kFewInputs / 16 / NX;
     __shared__ __attribute__((aligned(16))) char lds[2 * XB];
+    __shared__ int any[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int ot = blockIdx.x / a.itiles, first = (blockIdx.x - ot * a.itiles) * a.rows_per_split;         // (of inputs here)
     const int count = min(a.rows_per_split, (a.I + kFewInputs - 1) / kFewInputs - first);
     const int o0 = ot * 128 + wave * 32, o = o0 + (lane & 31);
 
     // Pieces of 16 codes: sample tid / 4, and 64 more for the second.  Past the last sample it is the last one again, times gradients
-    // of zero: where that is NaN, so is the sum with the last one itself.  (No branch, behind which each load would be waited for.)
+    // of zero: where that is NaN, so is the sum with the last one itself; where it is infinite, bfloat16 gradients take 2^-127 for its
+    // power of two, and for fp32 ones the sums are made again.  (No branch, behind which each load would be waited for.)
     const int xrow = tid % TX >> 2, xcol = (tid & 3) * 16;
     u32x4 xraw[NX];
     unsigned xbyte[NX];
-    int64_t xat[NX];
+    unsigned long long seen = 0;                     // lanes that have had a value that may be infinite
+    unsigned xat[NX];                                // (all codes are fewer than 2^31)
 #pragma unroll
-    for (int u = 0; u < NX; ++u) xat[u] = (int64_t)min(u * (TX >> 2) + xrow, a.N - 1) * a.pitch + (int64_t)first * kFewInputs + xcol;
+    for (int u = 0; u < NX; ++u) xat[u] = (unsigned)min(u * (TX >> 2) + xrow, a.N - 1) * (unsigned)a.pitch + first * kFewInputs + xcol;
     auto load_x = [&](int j) {                       // past the last step that one again
         const int at = min(j, count - 1) * kFewInputs;
 #pragma unroll
@@ -305,8 +351,10 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_few_kernel(const KeptGradArg
 #pragma unroll
         for (int u = 0; u < NX; ++u) {
             const int row = u * (TX >> 2) + xrow;
+            const unsigned byte = PARTS == 3 || row < a.N ? xbyte[u] : 0;
             u32x4 v[2];
-            kept_to_bf16(xraw[u], xbyte[u], v);
+            kept_to_bf16(xraw[u], byte, v);
+            if (PARTS == 3) seen |= __ballot(may_be_infinite(byte));
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 *reinterpret_cast<u32x4 *>(p + row * XP + ((((xcol >> 3) + h) ^ (4 * (row >> 1 & 1))) << 4)) = v[h];
@@ -391,6 +439,16 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_few_kernel(const KeptGradArg
     int j = 0;
     for (; j < whole; ++j) do_step(j, std::true_type{});
     for (; j < count; ++j) do_step(j, std::false_type{});
+    if constexpr (PARTS == 3) {
+        const int l = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));        // lane, which nothing has to hold until here
+        if (l == 0) any[wave] = seen != 0;
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // (the stores are not waited for)
+        if (any[0] | any[1] | any[2] | any[3]) {
+            __threadfence();                         // behind this lane's own stores
+#pragma unroll 1
+            for (int b = 0; b < 2 * count; ++b) infinite_input(a, a.dw, 0, a.N, first * kFewInputs + b * 32 + (l & 31), o0 + (l >> 5) * 4);
+        }
+    }
 }
 
 // the splits' sums, one after the other

@@ -183,6 +183,33 @@ def test_values_that_are_no_numbers_in_the_gradient(dtype):
     assert np.isnan(got[:, 32:64]).all() and (got[:, :32] == 70).all() and (got[:, 64:] == 70).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,I,O", [(1, 40, 33), (15, 70, 90), (16, 64, 32), (17, 130, 20), (100, 200, 40), (128, 64, 129), (129, 130, 70),
+                                   (160, 70, 7), (300, 150, 200), (3000, 130, 130), (1030, 4000, 4003)])
+def test_infinite_inputs_in_the_gradient(N, I, O, dtype):
+    """A value that comes back as an infinity (3.4e38 is past 248 2^120, half way to 2^128) makes its column what the formula makes
+    of it: an infinity of the gradient's sign, no number where the gradient is zero or two of them have different signs."""
+    g = RNG(N + I)
+    x, dy = _values((N, I), dtype, N + I), _values((N, O), dtype, N + O, 1e-3)
+    dy[:, ::3] = g.choice([0.0, 0.5, -1.0, 2.0, 3.0], (N, len(dy[0, ::3])))       # their second and third parts are zero
+    big = np.float32(3.4e38) if dtype == "f32" else oracle.bf16_round(np.float32([3.38e38]))[0]
+    x[N - 1, I // 2] = big
+    x[0, I - 1], x[N // 2, I - 1], x[N // 3, 3] = big, -big, -big
+    q, held = _held(x, "e4m3")
+    with np.errstate(over="ignore", invalid="ignore"):
+        held = held.astype(np.float32).astype(np.float64)
+        columns = np.flatnonzero(np.isinf(held).any(axis=0))
+        assert {3, I // 2, I - 1} == set(columns.tolist())
+        got = _host(hp.fc_bwd_filter_kept(q, _dev(dy, dtype)))
+        d = dy.astype(np.float64)
+        for i in columns:
+            want = (d * held[:, i:i + 1]).sum(axis=0)
+            assert not np.isfinite(want).any() and np.array_equal(got[:, i], want, equal_nan=True), i
+    rest = np.setdiff1d(np.arange(I), columns)
+    want, size = d.T @ held[:, rest], np.abs(d).T @ np.abs(held[:, rest])
+    assert (np.abs(got[:, rest] - want) <= 2 * U * (N * (3 if dtype == "f32" else 1) + 64) * size + 1e-37).all()
+
+
 def test_filter_gradient_of_no_samples():
     dw = torch.full((7, 40), 3.0, device="cuda")
     hp.fc_bwd_filter_kept(hp.Blocks.empty(0, 40, "e4m3"), torch.zeros((0, 7), device="cuda"), dw=dw)

@@ -21,7 +21,7 @@ DEPS = list(SOURCES) + [os.path.join(_HERE, "csrc", h) for h in (
     "conv_bf16_window_kernels.h", "conv_split_kernels.h", "conv_wgrad_split_kernels.h", "conv_direct_kernels.h",
     "conv_wgrad_rows_kernels.h", "conv_wgrad_kernels.h", "fc_kernels.h", "glue_kernels.h",
     "host_status.h", "elements.h", "vectors.h", "norm_kernels.h", "loss_kernels.h",
-    "block_formats.h", "block_kernels.h", "layer_norm_kernels.h", "fc_kept_kernels.h", "fc_q4_kernels.h")] + [os.path.join(os.path.dirname(_HERE), "include", "convnet_hotpath.h")]
+    "block_plan.h", "block_formats.h", "block_kernels.h", "layer_norm_kernels.h", "fc_kept_kernels.h", "fc_q4_kernels.h")] + [os.path.join(os.path.dirname(_HERE), "include", "convnet_hotpath.h")]
 
 # no packed-fp32 instruction selection
 DEVICE_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

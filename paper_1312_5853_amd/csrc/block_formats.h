@@ -5,7 +5,6 @@
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kBlock = 32;          // values to an exponent
-constexpr int kRowFill = 128;       // a row's codes are filled up with zeros to a multiple of this many values
 constexpr int kE4M3 = CONV_BLOCKS_E4M3, kE2M1 = CONV_BLOCKS_E2M1;
 
 // largest magnitude (mantissa bits of its fp32 form, exponent) and the least exponent of a block: from there on every value

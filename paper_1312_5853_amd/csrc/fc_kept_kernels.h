@@ -14,15 +14,6 @@
 // multiplied, the next one's values, which have come into registers meanwhile, are converted and stored piece by piece, and each
 // piece of the step after it is sent for as its registers become free.
 // Bound by the matrix units: 8192 rows 4096 -> 4096 bfloat16 220 us, 1250 TFLOP/s (a library product of bfloat16 tensors 1176).
-struct KeptGradArgs {
-    const unsigned char *codes, *scales;
-    const void *dy;
-    float *dw;                   // [O][I], or one such for every split
-    int64_t pitch, dy_stride;
-    int N, I, O;
-    int itiles, otiles, splits, rows_per_split;
-    int units, per_xcd;
-};
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -313,8 +304,6 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_kept_kernel(const KeptGradAr
 // soon where they are whole cache lines (128 samples 9216 -> 4096 fp32 37 us, 40 without the mark, with an update that reads dw
 // behind it 178 and 183; of parts of lines it costs: 9217 -> 4096 92 and 63).  (In tiles, whose work-groups load, multiply and
 // store all at the same time, the first took 51 us.)
-constexpr int kFewInputs = 64;
-
 template <typename T, int SLICES, int OCC>
 __global__ __launch_bounds__(256, OCC) void fc_grad_few_kernel(const KeptGradArgs a)
 {

@@ -28,14 +28,6 @@ inline int check_launch()
 
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
-// element type of the glue tensors: fp32 for kDtypeF32, bfloat16 for the two bf16 codes
-inline int glue_elem_bytes(int dtype)
-{
-    if (dtype == kDtypeF32) return 4;
-    if (dtype == kDtypeBf16 || dtype == kDtypeBf16OutBf16) return 2;
-    return 0;
-}
-
 }  // namespace convnet
 
 #endif

@@ -7,22 +7,6 @@
 // A row is read once and kept in registers (R vectors to a thread) from its sums to its result.  `waves` wavefronts take a row,
 // as many rows as fit run side by side in a work-group, and a work-group goes through rows so far apart as there are, the next
 // one's values on their way while one is summed and written: backward, the sums of the columns stay in its registers.
-struct LayerNormArgs {
-    const void *x, *dy;
-    const unsigned char *codes, *scales;     // x in blocks
-    void *out;                               // y or dx
-    const float *gamma, *beta;
-    float *mean, *rstd, *dgamma, *dbeta;
-    float *part;                             // [part_rows][2][C]: sums of columns over a part of the rows, dgamma's and dbeta's
-    int64_t x_stride, dy_stride, out_stride;
-    int64_t pitch;                           // values from row to row of the codes
-    int N, C;
-    int vectors;                             // of a row, the last one perhaps part of one
-    int waves, groups;                       // wavefronts to a row, rows side by side
-    int part_rows, rows_per_part;
-    int row_blocks;                          // backward: work-groups that take rows; those after them take columns
-    float inv_c, eps;
-};
 
 // The last vector of a row may be part of one.  It is read whole, as the row's last V values, and moved down when it is used, so
 // that no load is waited for at once (value by value 6001 x 5003 bfloat16 forward took 36 us, 28 with 5008); rows of fewer than V
@@ -315,7 +299,7 @@ __global__ __launch_bounds__(1024) void layer_norm_fwd_rows(const LayerNormArgs 
 // Rows longer than a work-group keeps: one of 1024 threads to a row, which goes through it three times, four vectors to a thread on
 // their way at a time; a vector is summed in fp32 and then in 64 bits, as a row may have any number of them.  Bound by memory and what
 // is read again: 2000 x 40000 fp32 218 us, 5.9 TB/s over three reads and a write, bfloat16 108 (value by value 250 and 184).
-constexpr int kWideThreads = 1024, kWideAhead = 4;
+constexpr int kWideAhead = 4;
 
 template <typename T>
 __global__ __launch_bounds__(kWideThreads) void layer_norm_fwd_wide(const LayerNormArgs a)
@@ -430,8 +414,6 @@ __device__ __forceinline__ void column_sums(const LayerNormArgs &a, int tile, in
 // U rows at a time, with one barrier to all, where a work-group has no more rows side by side.
 // Bound by memory between a start and an end of 10 us together, and for few rows by those: 6001 x 5003 bfloat16 from 8 bits 45 us,
 // 3.4 TB/s, from 3000 rows on another thousand takes what a copy of its bytes does; 128 x 9216 fp32 8.7 us.
-constexpr int layer_norm_bwd_waves(int values) { return values <= 8 ? 16 : 12; }        // most to a row, by values to a thread
-
 template <typename T, bool HELD, int R, bool SUMS, int U>
 __global__ __launch_bounds__(64 * layer_norm_bwd_waves(R * Vec<T>::V)) void layer_norm_bwd_rows(const LayerNormArgs a)
 {

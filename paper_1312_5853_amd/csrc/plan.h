@@ -26,6 +26,14 @@ constexpr int kErrScratchLimit = -7;
 constexpr int kOpFwd = 0, kOpBwdData = 1, kOpBwdFilter = 2;
 constexpr int kDtypeF32 = 0, kDtypeBf16 = 1, kDtypeBf16OutBf16 = 2;
 
+// element type of the glue tensors: fp32 for kDtypeF32, bfloat16 for the two bf16 codes
+inline int glue_elem_bytes(int dtype)
+{
+    if (dtype == kDtypeF32) return 4;
+    if (dtype == kDtypeBf16 || dtype == kDtypeBf16OutBf16) return 2;
+    return 0;
+}
+
 constexpr int kChunk = 16;            // reduction elements staged in LDS per step
 constexpr int kTapTablePad = 256;     // tap table length is rounded up to this
 constexpr int64_t kMaxSpanBytes = (int64_t)1 << 31;

@@ -3,6 +3,7 @@ import ctypes
 import os
 import subprocess
 import sys
+import types
 
 import pytest
 
@@ -59,6 +60,30 @@ def route(planner):
                      ctypes.c_longlong(-1 if workspace is None else workspace), out) == 0
         return Route(("fp32", "split", "direct", "window")[out[0]], *list(out)[1:])
     return ask
+
+
+@pytest.fixture(scope="session")
+def block_plans(tmp_path_factory):
+    """Plans of tests/block_plan_query.cpp as dicts: block_plans.layer_norm(op, N, C, dtype), .kept_grad(N, I, O, dtype) and
+    .q4(N, I, O): which kernel takes such a call, its grid and its steps, so that a test written for one of them can assert that it
+    reaches it.  A refused call gives its status."""
+    so = str(tmp_path_factory.mktemp("plan") / "block_plan_query.so")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-o", so, os.path.join(ROOT, "tests", "block_plan_query.cpp")],
+                   check=True)
+    query = ctypes.CDLL(so)
+
+    def ask(name, keys):
+        def call(*a):
+            out = (ctypes.c_longlong * len(keys))()
+            rc = getattr(query, name)(*a, out)
+            return rc if rc else dict(zip(keys, out))
+        return call
+
+    return types.SimpleNamespace(
+        layer_norm=ask("layer_norm_plan", "wide columns apart regs threads blocks lds waves groups rows_per_part part_rows "
+                                          "row_blocks bytes".split()),
+        kept_grad=ask("kept_grad_plan", "slices tile step itiles otiles splits rows_per_split blocks bytes".split()),
+        q4=ask("q4_plan", "fused tile steps wide nrows orows bytes".split()))
 
 
 # Normalised max errors the parity tests measured, printed once at the end of the run (also under -q).

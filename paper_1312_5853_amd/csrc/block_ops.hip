@@ -160,7 +160,14 @@ void launch_kept_grad(const KeptGradPlan &p, hipStream_t st)
 template <typename T, int SLICES, int OCC>
 void launch_few_grad(const KeptGradPlan &p, hipStream_t st)
 {
-    launch(fc_grad_few_kernel<T, SLICES, OCC>, p.blocks, 256, 0, st, p.a);
+    KeptGradArgs a = p.a;
+    for (int o = 0;; o += p.outputs) {
+        a.O = std::min(p.outputs, p.a.O - o);
+        launch(fc_grad_few_kernel<T, SLICES, OCC>, (int64_t)ceil_div(a.O, 128) * a.itiles, 256, 0, st, a);
+        if (a.O == p.a.O - o) return;
+        a.dy = static_cast<const T *>(a.dy) + a.O;
+        a.dw += (int64_t)a.O * a.I;
+    }
 }
 
 template <typename T>
@@ -319,12 +326,12 @@ int fc_bwd_filter_kept(const void *codes, const void *scales, const void *dy, vo
     a.dy = dy;
     a.dw = static_cast<float *>(a.splits > 1 ? ws : dw);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (eb == 4) run_kept_grad<float>(p, st);
-    else run_kept_grad<Bf16>(p, st);
-    if (a.splits > 1) {
+    if (N > 0 && eb == 4) run_kept_grad<float>(p, st);
+    else if (N > 0) run_kept_grad<Bf16>(p, st);
+    if (N == 0 || a.splits > 1) {
         const int64_t count = (int64_t)I * O;
         hipLaunchKernelGGL(fc_grad_join, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, a.dw, static_cast<float *>(dw),
-                           count, a.splits);
+                           count, N == 0 ? 0 : a.splits);
     }
     return check_launch();
 }

@@ -13,7 +13,7 @@ inline int pow2_up(int v)
 
 constexpr int64_t kMaxElements = (int64_t)1 << 31;       // of a fully connected layer's tensors
 
-// of rows, whose number may be any that an int holds
+// of rows or columns, whose number may be any that an int holds
 inline int parts_of(int n, int m) { return (n - 1) / m + 1; }
 
 inline int64_t pitch_of(int C) { return round_up64(C, kRowFill); }
@@ -126,7 +126,8 @@ struct KeptGradArgs {
 
 struct KeptGradPlan {
     KeptGradArgs a;
-    int slices;                   // few samples: sixteens of them; 0: tiles
+    int slices;                   // few samples: sixteens of them; 0: tiles, or no samples
+    int outputs;                  // to a launch
     int tile, step;               // outputs, and inputs, of a tile; rows of a step
     int64_t blocks;               // the grid
     size_t part_bytes;
@@ -142,15 +143,18 @@ inline int plan_kept_grad(KeptGradPlan &p, int N, int I, int O, int dtype)
     a.N = N; a.I = I; a.O = O;
     a.pitch = pitch_of(I);
     a.dy_stride = O;
+    a.splits = 1;
+    p.outputs = O;
+    if (N == 0) return kStatusOk;                            // dw is filled
     // The gradients stay in registers, and a work-group goes through its share of the inputs (9216 -> 4096, three states in turn): 128
     // rows fp32 37 us, 52 in tiles, bfloat16 34 and 40; one row 32 and 33, 32 and 38.
-    if (N > 0 && N <= 128) {
+    if (N <= 128) {
         p.slices = N <= 16 ? 1 : N <= 32 ? 2 : N <= 64 ? 4 : 8;
-        a.otiles = ceil_div(O, 128);
-        const int inputs = ceil_div(I, kFewInputs), shares = std::max(1, std::min(inputs, 768 / a.otiles));
+        p.outputs = std::min(O, 1 << 30);                    // (a launch has fewer than 2^32 threads)
+        a.otiles = parts_of(p.outputs, 128);
+        const int inputs = parts_of(I, kFewInputs), shares = std::max(1, std::min(inputs, 768 / a.otiles));
         a.rows_per_split = ceil_div(inputs, shares);
         a.itiles = ceil_div(inputs, a.rows_per_split);
-        a.splits = 1;
         p.blocks = (int64_t)a.otiles * a.itiles;
         return kStatusOk;
     }

@@ -254,7 +254,7 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_kept_kernel(const KeptGradAr
         if constexpr (!PIPELINED) __syncthreads();
         buf = STAGE - buf;
     };
-    if (steps > 0) {
+    if (steps > 0) {                                 // (always; without it the 256 x 256 tiles take 90 registers more and spill)
 #pragma unroll
         for (int u = 0; u < PIECES; ++u) load_piece(u, 0, 0 < (u < NX ? whole : full));
 #pragma unroll
@@ -440,12 +440,12 @@ __global__ __launch_bounds__(256, OCC) void fc_grad_few_kernel(const KeptGradArg
     }
 }
 
-// the splits' sums, one after the other
+// the splits' sums, one after the other; zeros for no splits
 __global__ __launch_bounds__(256) void fc_grad_join(const float *part, float *dw, int64_t count, int splits)
 {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= count) return;
-    float s = part[i];
+    float s = splits > 0 ? part[i] : 0.f;
     for (int p = 1; p < splits; ++p) s += part[p * count + i];
     dw[i] = s;
 }

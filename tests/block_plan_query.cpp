@@ -28,7 +28,7 @@ extern "C" int kept_grad_plan(int N, int I, int O, int dtype, long long *out)
     KeptGradPlan p;
     const int rc = plan_kept_grad(p, N, I, O, dtype);
     if (rc != kStatusOk) return rc;
-    const long long v[] = {p.slices, p.tile, p.step, p.a.itiles, p.a.otiles, p.a.splits, p.a.rows_per_split, p.blocks,
+    const long long v[] = {p.slices, p.tile, p.step, p.outputs, p.a.itiles, p.a.otiles, p.a.splits, p.a.rows_per_split, p.blocks,
                            (long long)p.part_bytes};
     std::copy(v, v + sizeof(v) / sizeof(v[0]), out);
     return kStatusOk;

@@ -47,3 +47,21 @@ def test_layer_norm_plans_cover_the_tensors(block_plans):
             if op == BWD and not p["wide"]:
                 # a thread's columns are summed over at most 256 rows in fp32
                 assert p["columns"] or p["apart"] or -(-N // (p["row_blocks"] * p["groups"])) <= 256
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("N,I,O", [(1, 1, (1 << 31) - 1), (1, 1, (1 << 31) - 127), (1, 1, (1 << 31) - 128), (1, (1 << 31) - 128, 1),
+                                   (1, (1 << 31) - 255, 1), (0, (1 << 31) - 1, 1), (0, 1, (1 << 31) - 1), (0, 46340, 46340),
+                                   (1, 3, (1 << 30) // 3 * 2), (2, 1, (1 << 30) - 1), (128, 1, (1 << 24) - 1), (129, 7, (1 << 24) - 200000)])
+def test_filter_gradients_of_the_longest_tensors(block_plans, N, I, O, dtype):
+    """Fewer than 2^31 elements each, as the header has it: positive counts, that a launch can hold, and nothing past the ends."""
+    p = block_plans.kept_grad(N, I, O, dtype)
+    assert min(p.values()) >= 0 and p["blocks"] * 256 < 1 << 32
+    if N == 0:
+        assert p["blocks"] == 0
+    elif N <= 128:
+        assert p["otiles"] * p["itiles"] == p["blocks"] and p["otiles"] * 128 >= p["outputs"]
+        assert p["outputs"] == O or p["outputs"] % 128 == 0
+        assert p["itiles"] * p["rows_per_split"] * 64 >= I
+    else:
+        assert p["otiles"] * p["tile"] >= O == p["outputs"] and p["itiles"] * p["tile"] >= I

@@ -224,6 +224,24 @@ def test_filters_and_samples_past_32_bits_of_bytes():
     assert dw.shape == (N, O) and (dw[-1] == 3).all() and (dw[0] == 3).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N,I,O", [(1, 1, (1 << 31) - 1), (1, (1 << 31) - 128, 1), (0, (1 << 31) - 1, 1), (0, 1, (1 << 31) - 1)])
+def test_filter_gradient_of_the_longest_tensors(N, I, O, dtype):
+    """Just below 2^31 elements: products of single values, exact."""
+    q = hp.Blocks.empty(N, I, "e4m3")
+    q.codes.fill_(0x38)                                              # 1, times powers of two in turn
+    q.scales.copy_(127 + torch.arange(q.scales.numel(), device="cuda", dtype=torch.int32).view(q.scales.shape) % 13)
+    dy = (torch.arange(O, device="cuda", dtype=torch.int32) % 251 - 125).to(dtype).view(1, O)[:N]
+    dw = torch.full((O, I), float("nan"), device="cuda")
+    hp.fc_bwd_filter_kept(q, dy, dw=dw)
+    if N == 0:
+        assert not dw.any()
+    elif I == 1:
+        assert torch.equal(dw.view(-1), dy.view(-1).float())
+    else:
+        assert torch.equal(dw.view(-1, 32), (q.scales.float() - 127).exp2().mul_(-125.0).view(-1, 1)[:I // 32].expand(-1, 32))
+
+
 def test_run_together():
     """A layer as it is trained and then served: normalised, kept, its gradients, its output in 4 bits; odd sizes, one stream."""
     N, I, O = 77, 1003, 515

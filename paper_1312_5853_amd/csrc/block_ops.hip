@@ -116,7 +116,7 @@ int run_layer_norm_bwd(LayerNormPlan &p, hipStream_t st)
         }
         if (a.part && p.apart) launch(layer_norm_columns<T, HELD>, (int64_t)a.part_rows * tiles, 1024, 0, st, a);
     }
-    if (sums && (a.N == 0 || !p.columns)) launch(layer_norm_join, 2 * tiles, 1024, 0, st, a);
+    if (sums && (a.N == 0 || !p.columns)) launch(layer_norm_join, p.join_blocks, 1024, 0, st, a);
     return check_launch();
 }
 

@@ -45,7 +45,7 @@ struct LayerNormPlan {
     bool wide;                    // rows longer than a work-group keeps
     bool columns, apart;          // backward: columns' sums by work-groups of their own, in the same launch or in one of their own
     int regs, threads;
-    int64_t blocks;
+    int64_t blocks, join_blocks;  // grids: of the kernel that takes rows, and of the one that joins the columns' sums
     size_t lds, part_bytes;
     LayerNormArgs a;
 };
@@ -105,6 +105,7 @@ inline int plan_layer_norm(LayerNormPlan &p, int op, int N, int C, int dtype)
         a.rows_per_part = std::max(1, parts_of(N, a.part_rows));
         a.part_rows = parts_of(N, a.rows_per_part);
     }
+    if (bwd) p.join_blocks = std::min(2 * ((C + 63) / 64), 1 << 21);         // (a launch has fewer than 2^32 threads)
     if (bwd) p.part_bytes = (size_t)round_up64((int64_t)a.part_rows * 2 * C * 4, 256);
     return kStatusOk;
 }

@@ -694,27 +694,30 @@ __global__ __launch_bounds__(1024) void layer_norm_join(const LayerNormArgs a)
 {
     __shared__ double lds[16][64];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-    const int which = blockIdx.x & 1, c = (blockIdx.x >> 1) * 64 + lane;
-    float *const out = which ? a.dbeta : a.dgamma;
-    if (!out) return;
-    double s = 0.0;
-    if (c < a.C) {
-        const float *p = a.part + (int64_t)which * a.C + c;
-        const int64_t pitch = 2 * (int64_t)a.C;
-        int i = wave;
-        for (; i + 48 < a.part_rows; i += 64) {
-            const float v[4] = {p[i * pitch], p[(i + 16) * pitch], p[(i + 32) * pitch], p[(i + 48) * pitch]};
+    for (int b = blockIdx.x; b < 2 * ((a.C + 63) / 64); b += gridDim.x) {
+        const int which = b & 1, c = (b >> 1) * 64 + lane;
+        float *const out = which ? a.dbeta : a.dgamma;
+        if (!out) continue;
+        double s = 0.0;
+        if (c < a.C) {
+            const float *p = a.part + (int64_t)which * a.C + c;
+            const int64_t pitch = 2 * (int64_t)a.C;
+            int i = wave;
+            for (; i + 48 < a.part_rows; i += 64) {
+                const float v[4] = {p[i * pitch], p[(i + 16) * pitch], p[(i + 32) * pitch], p[(i + 48) * pitch]};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) s += v[k];
+                for (int k = 0; k < 4; ++k) s += v[k];
+            }
+            for (; i < a.part_rows; i += 16) s += p[i * pitch];
         }
-        for (; i < a.part_rows; i += 16) s += p[i * pitch];
-    }
-    lds[wave][lane] = s;
-    __syncthreads();
-    if (wave == 0 && c < a.C) {
-        s = 0.0;
+        lds[wave][lane] = s;
+        __syncthreads();
+        if (wave == 0 && c < a.C) {
+            s = 0.0;
 #pragma unroll
-        for (int w = 0; w < 16; ++w) s += lds[w][lane];
-        out[c] = (float)s;
+            for (int w = 0; w < 16; ++w) s += lds[w][lane];
+            out[c] = (float)s;
+        }
+        __syncthreads();
     }
 }

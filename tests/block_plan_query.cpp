@@ -18,7 +18,7 @@ extern "C" int layer_norm_plan(int op, int N, int C, int dtype, long long *out)
     const int rc = plan_layer_norm(p, op, N, C, dtype);
     if (rc != kStatusOk) return rc;
     const long long v[] = {p.wide, p.columns, p.apart, p.regs, p.threads, p.blocks, (long long)p.lds, p.a.waves, p.a.groups,
-                           p.a.rows_per_part, p.a.part_rows, p.a.row_blocks, (long long)p.part_bytes};
+                           p.a.rows_per_part, p.a.part_rows, p.a.row_blocks, p.join_blocks, (long long)p.part_bytes};
     std::copy(v, v + sizeof(v) / sizeof(v[0]), out);
     return kStatusOk;
 }

@@ -81,7 +81,7 @@ def block_plans(tmp_path_factory):
 
     return types.SimpleNamespace(
         layer_norm=ask("layer_norm_plan", "wide columns apart regs threads blocks lds waves groups rows_per_part part_rows "
-                                          "row_blocks bytes".split()),
+                                          "row_blocks join_blocks bytes".split()),
         kept_grad=ask("kept_grad_plan", "slices tile step outputs itiles otiles splits rows_per_split blocks bytes".split()),
         q4=ask("q4_plan", "fused tile steps wide nrows orows bytes".split()))
 

@@ -44,9 +44,16 @@ def test_layer_norm_plans_cover_the_tensors(block_plans):
             if p["apart"]:
                 assert p["part_rows"] * p["rows_per_part"] >= N > (p["part_rows"] - 1) * p["rows_per_part"]
                 assert p["part_rows"] * -(-C // 64) * 1024 < 1 << 32
+            assert op == FWD or p["join_blocks"] * 1024 < 1 << 32
             if op == BWD and not p["wide"]:
                 # a thread's columns are summed over at most 256 rows in fp32
                 assert p["columns"] or p["apart"] or -(-N // (p["row_blocks"] * p["groups"])) <= 256
+
+
+def test_the_columns_of_the_longest_rows_are_joined_in_one_launch(block_plans):
+    for N in (0, 1, 700, 8191):
+        for C in (1 << 27, (1 << 27) - 63, (1 << 27) - 64):
+            assert block_plans.layer_norm(BWD, N, C, 0)["join_blocks"] * 1024 < 1 << 32
 
 
 @pytest.mark.parametrize("dtype", [0, 1])

@@ -210,6 +210,25 @@ def test_offsets_past_32_bits():
     assert torch.equal(dx[-3:], hp.layer_norm_bwd(x[-3:], x[-3:], few[1], few[2])[0])
 
 
+@pytest.mark.parametrize("C", [1 << 27, (1 << 27) - 5])
+def test_layer_norm_of_the_longest_rows(C):
+    """One row of ones and minus ones in turn (an odd number of values has one more of the ones), whose mean and squares are exact."""
+    x = torch.ones((1, C), device="cuda")
+    x[0, 1::2] = -1.0
+    dy = (torch.arange(C, device="cuda", dtype=torch.int32) % 7 - 3).float().view(1, C)
+    gamma = torch.full((C,), 2.0, device="cuda")
+    y, mean, rstd = hp.layer_norm_fwd(x, gamma, eps=1e-5)
+    m, r = float(mean), float(rstd)
+    assert abs(m - C % 2 / C) <= 64 * U * (1 + C % 2 / C) and abs(r - (1 + 1e-5 - (C % 2 / C) ** 2) ** -0.5) <= 64 * U
+    xh = (x.double() - m) * r
+    assert ((y.double() - 2 * xh).abs() <= 2 * 8 * U).all()
+    dx, dgamma, dbeta = hp.layer_norm_bwd(x, dy, mean, rstd, gamma)
+    assert torch.equal(dbeta, dy[0]) and ((dgamma.double() - (dy * xh)[0]).abs() <= 4 * 3 * U).all()
+    g = 2.0 * dy.double()
+    want = r * (g - g.mean() - xh * (g * xh).mean())
+    assert ((dx.double() - want).abs() <= (8 * 6 + 64 * 12) * U).all()
+
+
 def test_filters_and_samples_past_32_bits_of_bytes():
     """Outputs of 2^31 bytes and more."""
     N, I, O = 40000, 64, 16000                                       # y: 2.56e9 bytes

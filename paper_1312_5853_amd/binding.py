@@ -779,11 +779,18 @@ def group_norm_act_bwd(x, dy, mean, rstd, gamma=None, beta=None, act="relu", dx=
     return dx, dgamma, dbeta
 
 
+def _too_large(what):
+    """A size of 2^31 or more is refused here: ctypes would hand on its low 32 bits."""
+    raise ConvError(ERR_TOO_LARGE, what)
+
+
 def _rows_of(t, what):
     """(N, V, row stride) of a [N,V] tensor whose rows are dense."""
     shape, stride = t.shape, t.stride()
     if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1) or (shape[0] > 1 and stride[0] < shape[1]):
         raise ValueError("%s must be [N, V] with dense rows" % what)
+    if shape[0] >> 31 or shape[1] >> 31:
+        _too_large("a call on %s" % what)
     return shape[0], shape[1], (stride[0] if shape[0] > 1 else shape[1])
 
 
@@ -952,6 +959,8 @@ class Blocks:
             raise ValueError("codes and scales must be dense, with rows of %d values and their exponents" % (blocks * BLOCK_VALUES))
         if codes.get_device() != scales.get_device():
             raise ValueError("the tensors of a call must be on one GPU")
+        if shape[0] >> 31 or cols >> 31:
+            _too_large("Blocks")
         self.codes, self.scales, self.cols, self.format = codes, scales, cols, format
 
     @classmethod
@@ -1120,6 +1129,8 @@ def fc_bwd_filter_kept(q, dy, dw=None, ws=None, stream=None):
     if len(shape) != 2 or shape[0] != N or not dy.is_contiguous():
         raise ValueError("dy must be a dense tensor with the rows of q")
     O, dtype, d = shape[1], _glue_code(dy), dy.get_device()
+    if O >> 31:
+        _too_large("fc_bwd_filter_kept")
     if q.codes.get_device() != d:
         raise ValueError("the tensors of a call must be on one GPU")
     _on_gpu(d)
@@ -1152,6 +1163,8 @@ def fc_fwd_q4(x, w, bias=None, relu=False, y=None, ws=None, stream=None, out_bf1
     if len(shape) != 2 or shape[1] != I or not x.is_contiguous():
         raise ValueError("x must be a dense tensor with rows of %d values" % I)
     N, dtype, d = shape[0], _glue_code(x), x.get_device()
+    if N >> 31:
+        _too_large("fc_fwd_q4")
     if w.codes.get_device() != d:
         raise ValueError("the tensors of a call must be on one GPU")
     _on_gpu(d)

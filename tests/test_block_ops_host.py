@@ -233,3 +233,22 @@ def test_binding_refuses_what_the_library_cannot_see(lib):
                  lambda: b.fc_bwd_filter_kept(x, x), lambda: b.fc_fwd_q4(x, x), lambda: b.fc_fwd_q4(x.half(), q4)):
         with pytest.raises(TypeError):
             call()
+
+
+def test_binding_refuses_sizes_past_a_c_int(lib):
+    """A size of 2^32 + 1 must not reach the library as 1."""
+    from paper_1312_5853_amd import binding as b
+    far = (1 << 32) + 1
+    meta = lambda *s, dtype=torch.float32: torch.empty(s, dtype=dtype, device="meta")
+    byte = lambda *s: meta(*s, dtype=torch.uint8)
+    q8, q4 = b.Blocks(byte(1, 128), byte(1, 4), 1, "e4m3"), b.Blocks(byte(5, 64), byte(5, 4), 1, "e2m1")
+    for call in (lambda: b.quantize_blocks(meta(far, 1), "e4m3"), lambda: b.quantize_blocks(meta(1, far), "e4m3"),
+                 lambda: b.dequantize_blocks(q8, x=meta(far, 1)), lambda: b.layer_norm_fwd(meta(far, 1)),
+                 lambda: b.layer_norm_bwd(meta(far, 1), meta(far, 1), meta(far), meta(far)),
+                 lambda: b.layer_norm_bwd_kept(q8, meta(far, 1), meta(1), meta(1)),
+                 lambda: b.distill_loss_fwd(meta(far, 3), labels=meta(far, dtype=torch.int32)),
+                 lambda: b.fc_bwd_filter_kept(q8, meta(1, far)), lambda: b.fc_fwd_q4(meta(far, 1), q4),
+                 lambda: b.Blocks(byte(1, 128 * 2 ** 25), byte(1, 4 * 2 ** 25), far - 1, "e4m3"), lambda: b.Blocks.empty(far, 1, "e2m1", "meta")):
+        with pytest.raises(b.ConvError) as e:
+            call()
+        assert e.value.status == b.ERR_TOO_LARGE

@@ -210,6 +210,56 @@ def test_infinite_inputs_in_the_gradient(N, I, O, dtype):
     assert (np.abs(got[:, rest] - want) <= 2 * U * (N * (3 if dtype == "f32" else 1) + 64) * size + 1e-37).all()
 
 
+# whole numbers, which the sums keep exactly, in random places: a step's values in another's buffer would show
+FEW_STEPS = [(1, 9216, 4096), (9, 9217, 4001), (20, 9216, 4096), (50, 9216, 4096), (64, 9250, 4100), (100, 9230, 4096), (128, 9216, 4096),
+             (128, 50000, 130), (33, 100001, 70), (17, 100000, 20)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,I,O", FEW_STEPS)
+def test_filter_gradient_over_many_steps_of_inputs(N, I, O, dtype, block_plans):
+    """Few samples, and so many inputs that a work-group goes through three 64s of them at least, in its two buffers."""
+    p = block_plans.kept_grad(N, I, O, 0 if dtype == "f32" else 1)
+    assert p["slices"] and p["rows_per_split"] >= 3
+    _whole_gradient(N, I, O, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,I,O,tile", [(255, 300, 260, 128), (1000, 300, 260, 128), (900, 2100, 2100, 128), (2100, 4096, 3900, 256)])
+def test_filter_gradient_over_many_steps_of_rows(N, I, O, tile, dtype, block_plans):
+    """Tiles whose sums take four steps at least, most of them many more: all but the last two are of the loop that loads, converts
+    and multiplies at a time."""
+    p = block_plans.kept_grad(N, I, O, 0 if dtype == "f32" else 1)
+    assert not p["slices"] and p["tile"] == tile and p["rows_per_split"] >= 4 * p["step"]
+    _whole_gradient(N, I, O, dtype)
+
+
+def _whole_gradient(N, I, O, dtype):
+    g = torch.Generator(device="cuda").manual_seed(N + I)
+    x, dy = (torch.randint(-8, 9, (N, k), device="cuda", generator=g).float() for k in (I, O))
+    q = hp.quantize_blocks(x, "e4m3")
+    assert torch.equal(hp.dequantize_blocks(q), x)
+    dw = torch.full((O, I), float("nan"), device="cuda")
+    hp.fc_bwd_filter_kept(q, dy.to(DTYPES[dtype]), dw=dw)
+    assert torch.equal(dw, (dy.t().contiguous().double() @ x.double()).float())
+
+
+@pytest.mark.parametrize("N,I,O,tile,step", [(130, 200, 150, 128, 16), (256, 130, 260, 128, 16), (300, 200, 150, 128, 32),
+                                             (1100, 4000, 4000, 256, 32), (1100, 4003, 4001, 256, 32)])
+def test_filter_gradient_in_tiles_keeps_every_bit_of_fp32(N, I, O, tile, step, block_plans):
+    """One sample of ones among zeros: dw is its dy, all 24 bits of it, in whichever step and row of a step it lies."""
+    p = block_plans.kept_grad(N, I, O, 0)
+    assert not p["slices"] and (p["tile"], p["step"]) == (tile, step)
+    g = torch.Generator(device="cuda").manual_seed(N)
+    dy = torch.randn((N, O), device="cuda", generator=g)
+    assert (dy.view(torch.int32) & 255 != 0).float().mean() > 0.9    # (the third part is there)
+    for n in sorted({0, 1, 2, 3, 5, 15, step - 1, step, 2 * step + 7, N // 2, N - step, N - 3, N - 2, N - 1, (N - 1) // step * step}):
+        x = torch.zeros((N, I), device="cuda")
+        x[n] = 1.0
+        dw = hp.fc_bwd_filter_kept(hp.quantize_blocks(x, "e4m3"), dy)
+        assert torch.equal(dw, dy[n].view(O, 1).expand(O, I)), n
+
+
 def test_filter_gradient_of_no_samples():
     dw = torch.full((7, 40), 3.0, device="cuda")
     hp.fc_bwd_filter_kept(hp.Blocks.empty(0, 40, "e4m3"), torch.zeros((0, 7), device="cuda"), dw=dw)
@@ -264,6 +314,37 @@ def test_forward_of_whole_numbers_is_exact(N, I, O):
     want = x.astype(np.float64) @ w.T + bias
     assert np.array_equal(_host(hp.fc_fwd_q4(_dev(x), q, torch.from_numpy(bias).cuda())), want)
     assert np.array_equal(_host(hp.fc_fwd_q4(_dev(x), q, torch.from_numpy(bias).cuda(), relu=True)), np.maximum(want, 0))
+
+
+# as above: so many steps that every wavefront refills its ring of three buffers (x put into blocks in the call; by a launch of its own
+# in the three forms for few samples), and tiles that refill their four
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,I,O,kind", [(1, 9216, 70, "fused"), (3, 8320, 40, "fused"), (2, 16300, 33, "fused"), (12, 9216, 50, "rows"),
+                                        (16, 20000, 20, "rows"), (24, 9300, 100, "rows"), (32, 16384, 33, "rows"), (64, 8192, 300, "rows"),
+                                        (100, 9216, 70, "rows"), (128, 9216, 4096, "rows"), (1000, 4200, 1100, "tiles128"), (600, 1300, 2100, "tiles128"),
+                                        (1024, 4096, 4096, "tiles128"), (3600, 2200, 4000, "tiles256")])
+def test_forward_of_whole_numbers_over_many_steps(N, I, O, kind, dtype, block_plans):
+    p = block_plans.q4(N, I, O)
+    assert kind == ("fused" if p["fused"] else "tiles%d" % p["tile"] if p["tile"] else "rows")
+    if p["tile"]:
+        assert p["steps"] > 2 * 4
+    else:                                                            # pairs of steps to a wavefront
+        assert (p["steps"] + 1) // 2 // (4 if p["wide"] == 4 else 8) > 3
+    g = torch.Generator(device="cuda").manual_seed(N + I)
+    values = torch.tensor([0, 1, 2, 3, 4, 6, -1, -2, -3, -4, -6], device="cuda", dtype=torch.float32)
+    x, w = (values[torch.randint(0, 11, (k, I), device="cuda", generator=g)] for k in (N, O))
+    x[:, ::32] = 6.0
+    w[:, ::32] = -6.0
+    bias = torch.randint(-9, 10, (O,), device="cuda", generator=g).float()
+    q = hp.quantize_blocks(w, "e2m1")
+    assert torch.equal(hp.dequantize_blocks(q), w)
+    want = (x.double() @ w.double().t().contiguous() + bias.double()).float()
+    assert want.abs().max() < 2 ** 24
+    y = torch.full((N, O), float("nan"), device="cuda")
+    assert torch.equal(hp.fc_fwd_q4(x.to(DTYPES[dtype]), q, bias, y=y), want)
+    assert torch.equal(hp.fc_fwd_q4(x.to(DTYPES[dtype]), q, bias, relu=True), want.clamp_min(0.0))
+    if dtype == "bf16":
+        assert torch.equal(hp.fc_fwd_q4(x.bfloat16(), q, bias, out_bf16=True), want.bfloat16())
 
 
 @pytest.mark.parametrize("N", [1, 3, 40, 200])

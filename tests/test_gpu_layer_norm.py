@@ -228,3 +228,54 @@ def test_rows_whose_mean_times_rstd_is_past_fp32(N, C, dtype):
     assert (mean == 2.0 ** 110).all() and (np.abs(rstd - 1e6) <= 1).all()
     check_bwd(hp.layer_norm_bwd(xd, dyd, m, r, _vec(gamma)), x, dy, mean, rstd, gamma, dtype)
     check_bwd(hp.layer_norm_bwd_kept(hp.quantize_blocks(xd, "e4m3"), dyd, m, r, _vec(gamma)), x, dy, mean, rstd, gamma, dtype)
+
+
+# more rows than take their columns' sums in the same launch, of 8193 to 12288 values (16 to a thread with the sums) and of more (24, the
+# columns in a launch of their own)
+MANY = [(700, 9216), (1301, 8200), (650, 12288), (645, 12287), (700, 16001), (641, 18432)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,C", MANY)
+def test_many_long_rows(N, C, dtype, block_plans):
+    p, V = block_plans.layer_norm(hp.OP_BWD_DATA, N, C, 0 if dtype == "f32" else 1), 4 if dtype == "f32" else 8
+    assert not p["wide"] and not p["columns"] and p["apart"] == (C > 12288) and p["regs"] * V == (24 if C > 12288 else 16)
+    assert p["blocks"] < N                                           # some work-groups take several rows
+    run_case(N, C, dtype, seed=N + C)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,C", [(5, 300), (900, 70), (700, 5003), (700, 16001), (300, 20001)])
+def test_sums_and_statistics_that_nobody_wants(N, C, dtype):
+    """Through the C calls: NULL for dgamma, dbeta, or both, for mean and rstd of the forward pass, and no scratch where no sums are
+    made.  What is written is what a call for everything writes."""
+    g = np.random.Generator(np.random.Philox(N))
+    x, dy = _dev(_values((N, C), dtype, g), dtype), _dev(_values((N, C), dtype, g), dtype)
+    code, lib, stream = 0 if dtype == "f32" else 1, hp.lib(), torch.cuda.current_stream().cuda_stream
+    gamma, ptr = _vec(1.0 + 0.3 * g.standard_normal(C)), lambda t: 0 if t is None else t.data_ptr()
+    want = hp.layer_norm_fwd(x, gamma)
+    for keep in ((False, False), (True, False), (False, True)):
+        y = torch.full_like(x, float("nan"))
+        stats = [torch.full((N,), float("nan"), device="cuda") if k else None for k in keep]
+        assert lib.layer_norm_fwd(x.data_ptr(), C, gamma.data_ptr(), 0, y.data_ptr(), C, ptr(stats[0]), ptr(stats[1]), N, C, 1e-5, code,
+                                  stream) == hp.OK
+        assert torch.equal(y, want[0]) and all(s is None or torch.equal(s, w) for s, w in zip(stats, want[1:]))
+    mean, rstd = want[1:]
+    q = hp.quantize_blocks(x, "e4m3")
+    need = lib.layer_norm_workspace_bytes(hp.OP_BWD_DATA, N, C, code)
+    ws = torch.empty(need + 256, dtype=torch.uint8, device="cuda")
+    for name, source, whole in (("layer_norm_bwd", (x.data_ptr(), C), hp.layer_norm_bwd(x, dy, mean, rstd, gamma)),
+                                ("layer_norm_bwd_kept", (q.codes.data_ptr(), q.scales.data_ptr()),
+                                 hp.layer_norm_bwd_kept(q, dy, mean, rstd, gamma))):
+        for keep in ((False, False), (True, False), (False, True)):
+            dx = torch.full_like(x, float("nan"))
+            sums = [torch.full((C,), float("nan"), device="cuda") if k else None for k in keep]
+            scratch = (ws.data_ptr(), need) if any(keep) else (0, 0)
+            assert getattr(lib, name)(*source, dy.data_ptr(), C, gamma.data_ptr(), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), C,
+                                      ptr(sums[0]), ptr(sums[1]), N, C, code, *scratch, stream) == hp.OK
+            # (dx by another form of the kernel, whose sums the compiler may contract elsewhere)
+            assert all(s is None or torch.equal(s, w) for s, w in zip(sums, whole[1:]))
+            m, r = _host(mean), _host(rstd)
+            src = _host(x) if name == "layer_norm_bwd" else _host(hp.dequantize_blocks(q))
+            zero = [torch.from_numpy(v).float().cuda() for v in oracle.layer_norm_bwd(src, _host(dy), m, r, _host(gamma))[1:]]
+            check_bwd((dx, *zero), src, _host(dy), m, r, _host(gamma), dtype)

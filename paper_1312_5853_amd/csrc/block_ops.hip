@@ -90,11 +90,12 @@ void launch_layer_norm_bwd(const LayerNormPlan &p, int64_t blocks, hipStream_t s
 {
     constexpr int few = 8 * (int)sizeof(T) / 16;         // vectors of eight values
     if (few > 1 && p.regs == 1) return launch(layer_norm_bwd_rows<T, HELD, 1, SUMS, 1>, blocks, p.threads, p.lds, st, p.a);
-    // Two rows at a time in more than eight wavefronts of bfloat16 rows, whose loads cover more of the memory's latency: 6001 x 5003
-    // from 8 bits 48.8 us, and 52.5, over inputs that the last cache no longer holds (43 both where it does); with rows side by side
-    // it costs registers for nothing (8192 x 4096 39.0 us, and 37.4; 60000 x 300 31.7 and 28.5)
+    // Two rows at a time in more than eight wavefronts of bfloat16 rows (4097 to 8192 values), whose loads cover more of the memory's
+    // latency, where a work-group has sixteen rows or more.  us, two and one at a time: 6001 x 5003 53.2 and 53.9, from 8 bits 48.1 and
+    // 52.7; 4096 x 7001 46.7 and 50.9, 41.8 and 48.6; 12000 x 4100 81.9 and 86.2, 71.2 and 86.0; 12000 x 8192 120.6 and 116.0, 99.0 and
+    // 96.6; but 700 x 8192 17.7 and 16.4, 19.0 and 17.4; 2600 x 6144 27.6 and 25.4, 25.1 and 24.0
     if constexpr (SUMS && few == 1)
-        if (p.regs == few && p.a.waves > 8) return launch(layer_norm_bwd_rows<T, HELD, few, true, 2>, blocks, p.threads, p.lds, st, p.a);
+        if (p.regs == few && p.a.waves > 8 && p.a.N >= 4096) return launch(layer_norm_bwd_rows<T, HELD, few, true, 2>, blocks, p.threads, p.lds, st, p.a);
     if (p.regs == few) return launch(layer_norm_bwd_rows<T, HELD, few, SUMS, 1>, blocks, p.threads, p.lds, st, p.a);
     if (p.regs == 2 * few) return launch(layer_norm_bwd_rows<T, HELD, 2 * few, SUMS, 1>, blocks, p.threads, p.lds, st, p.a);
     if constexpr (!SUMS) launch(layer_norm_bwd_rows<T, HELD, 3 * few, SUMS, 1>, blocks, p.threads, p.lds, st, p.a);

@@ -215,7 +215,7 @@ def test_columns_of_rows_longer_than_a_work_group_keeps_over_many():
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("N,C", [(3, 1), (3, 5), (2, 9), (4, 300), (2, 4096), (2, 4100), (3, 5003), (2, 9217), (2, 16001), (2, 33000),
-                                 (3, 33003), (700, 301), (700, 4099), (700, 9217), (700, 16001)])
+                                 (3, 33003), (700, 301), (700, 4099), (4100, 4099), (700, 9217), (700, 16001)])
 def test_rows_whose_mean_times_rstd_is_past_fp32(N, C, dtype):
     """2^110 throughout, with the statistics of eps = 1e-12: every distance from the mean is zero and so is xh, whatever the threads
     without a value of the row make of the mean, -2^110 1e6 = -1.3e39."""
@@ -279,3 +279,9 @@ def test_sums_and_statistics_that_nobody_wants(N, C, dtype):
             src = _host(x) if name == "layer_norm_bwd" else _host(hp.dequantize_blocks(q))
             zero = [torch.from_numpy(v).float().cuda() for v in oracle.layer_norm_bwd(src, _host(dy), m, r, _host(gamma))[1:]]
             check_bwd((dx, *zero), src, _host(dy), m, r, _host(gamma), dtype)
+
+
+@pytest.mark.parametrize("N,C", [(4095, 4097), (4096, 4097), (4099, 5003), (4200, 8192)])
+def test_two_rows_at_a_time(N, C):
+    """bfloat16 rows of 4097 to 8192 values, from 4096 rows on two at a time."""
+    run_case(N, C, "bf16", seed=N)

@@ -2,7 +2,8 @@
 // no memory traffic at all, fp32 (v_mfma_f32_32x32x2_f32), bf16 and f16
 // (v_mfma_f32_32x32x16_bf16 / _f16; with operands that never change, and with
 // eight sets of pseudo-random operands cycled, which is what real data costs in
-// power and therefore in clock).  bench.py reports them as second denominators
+// power and therefore in clock), and 4 bits (v_mfma_scale_f32_32x32x64_f8f6f4 on
+// E2M1 codes, four sets).  bench.py reports them as second denominators
 // next to the published peaks.  It also measures what one CU moves per clock
 // through its LDS (ds_read_b128, ds_write_b128 from registers) and through the
 // vector memory path (16-byte loads of cache-resident data into registers, and
@@ -72,6 +73,34 @@ __global__ __launch_bounds__(256) void mfma_half_loop(float *out, int iters)
     float s = 0.f;
     for (int i = 0; i < 4; ++i)
         for (int v = 0; v < 16; ++v) s += acc[i][v];
+    out[blockIdx.x * 256 + threadIdx.x] = s;
+}
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// E2M1 codes under the exponent 2^-7, whose sums stay finite: 0.5 throughout, or every code at random
+template <bool RANDOM>
+__global__ __launch_bounds__(256) void mfma_fp4_loop(float *out, int iters)
+{
+    f32x16 acc[4][4];
+    for (int i = 0; i < 4; ++i)
+        for (int j = 0; j < 4; ++j)
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+    i32x8 a[4], b[4];
+    for (int s = 0; s < 4; ++s)
+        for (int k = 0; k < 8; ++k) {
+            a[s][k] = k < 4 ? (int)(RANDOM ? mix(threadIdx.x * 131 + s * 17 + k + 1) : 0x11111111u) : 0;
+            b[s][k] = k < 4 ? (int)(RANDOM ? mix(threadIdx.x * 257 + s * 29 + k + 99) : 0x11111111u) : 0;
+        }
+    for (int it = 0; it < iters; ++it)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a[i], b[j], acc[i][j], 4, 4, 0, 120, 0, 120);
+    float s = 0.f;
+    for (int i = 0; i < 4; ++i)
+        for (int j = 0; j < 4; ++j)
+            for (int v = 0; v < 16; ++v) s += acc[i][j][v];
     out[blockIdx.x * 256 + threadIdx.x] = s;
 }
 
@@ -174,6 +203,20 @@ int main()
         CHECK(hipEventSynchronize(e1));
         CHECK(hipEventElapsedTime(&ms, e0, e1));
         printf("%s wgs=%d ms=%.3f TFLOP/s=%.1f\n", half_names[rnd], bwgs, ms, bflops / ms / 1e9);
+    }
+    // 4 bits: 256 work-groups (their sums fill the registers: one wave per SIMD), 0.05 s each
+    void (*const fours[])(float *, int) = {mfma_fp4_loop<false>, mfma_fp4_loop<true>};
+    const char *const four_names[] = {"fp4_sustained_constant_operands ", "fp4_sustained_random_operands   "};
+    for (int rnd = 0; rnd < 2; ++rnd) {
+        const int fwgs = 256, fiters = 100000;
+        hipLaunchKernelGGL(fours[rnd], dim3(fwgs), dim3(256), 0, 0, d, 100);
+        CHECK(hipDeviceSynchronize());
+        CHECK(hipEventRecord(e0));
+        hipLaunchKernelGGL(fours[rnd], dim3(fwgs), dim3(256), 0, 0, d, fiters);
+        CHECK(hipEventRecord(e1));
+        CHECK(hipEventSynchronize(e1));
+        CHECK(hipEventElapsedTime(&ms, e0, e1));
+        printf("%s wgs=%d ms=%.3f TFLOP/s=%.1f\n", four_names[rnd], fwgs, ms, (double)fwgs * 4 * fiters * 16 * 131072.0 / ms / 1e9);
     }
     // bytes per clock and CU (at the 2.4 GHz peak clock) of LDS reads, LDS writes from registers, cache-resident
     // 16-byte loads into registers, and the same loads straight into LDS

@@ -30,6 +30,7 @@ class CompactNetwork(distill.DistilledNetwork):
         self.ln_dbeta = {k: torch.empty(i, **f) for k, i in sizes.items()}
         self.ln_mean = {k: torch.empty(N, **f) for k in sizes}
         self.ln_rstd = {k: torch.empty(N, **f) for k in sizes}
+        self.q4_stats = torch.empty(N, **f), torch.empty(N, **f)       # an evaluation's own: a backward pass may still need the others
         self.kept_a = {k: hp.Blocks.empty(N, i, "e4m3", device) for k, i in sizes.items()}
         self.kept_h = {k: hp.Blocks.empty(N, i, "e4m3", device) for k, i in sizes.items()}
         self.h = torch.empty(N * max(sizes.values()), **f)              # h, and what is read back, of one layer at a time
@@ -46,14 +47,13 @@ class CompactNetwork(distill.DistilledNetwork):
     def _output(self, name):
         return self.fc_y["fc8"] if name == "fc8" else self.out
 
-    def _norm_rows(self, name, a):
-        return hp.layer_norm_fwd(a, self.ln_gamma[name], self.ln_beta[name], y=self._rows(name), mean=self.ln_mean[name],
-                                 rstd=self.ln_rstd[name])[0]
+    def _norm_rows(self, name, a, mean, rstd):
+        return hp.layer_norm_fwd(a, self.ln_gamma[name], self.ln_beta[name], y=self._rows(name), mean=mean, rstd=rstd)[0]
 
     def forward(self):
         a = self.conv_forward().view(self.N, -1)
         for name in FC_NAMES:
-            h = self._norm_rows(name, a)
+            h = self._norm_rows(name, a, self.ln_mean[name], self.ln_rstd[name])
             hp.quantize_blocks(a, "e4m3", out=self.kept_a[name])
             hp.quantize_blocks(h, "e4m3", out=self.kept_h[name])
             a = hp.fc_fwd(h, self.fc_w[name], self.fc_b[name], relu=name != "fc8", y=self._output(name), ws=self.ws)
@@ -87,8 +87,8 @@ class CompactNetwork(distill.DistilledNetwork):
         """The logits of the present inputs with weights, and the layers' inputs, in 4 bits."""
         a = self.conv_forward().view(self.N, -1)
         for name in FC_NAMES:
-            a = hp.fc_fwd_q4(self._norm_rows(name, a), self.w4[name], self.fc_b[name], relu=name != "fc8", y=self._output(name),
-                             ws=self.ws)
+            a = hp.fc_fwd_q4(self._norm_rows(name, a, *self.q4_stats), self.w4[name], self.fc_b[name], relu=name != "fc8",
+                             y=self._output(name), ws=self.ws)
         return a
 
     def evaluate_q4(self):

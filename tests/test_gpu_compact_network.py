@@ -131,6 +131,18 @@ def test_evaluation_in_four_bits(net):
     assert abs(float(loss.mean()) - float(net.evaluate().mean())) < 0.5 * float(net.evaluate().mean())
 
 
+def test_an_evaluation_between_a_forward_and_a_backward_pass(net):
+    """What the backward pass needs of the forward pass stays."""
+    net.quantize()
+    grads = []
+    for between in (lambda: None, net.evaluate_q4):
+        hp.distill_loss_fwd_bwd(net.forward(), **net._terms(), dz=net.g8)
+        between()
+        net.backward()
+        grads.append([g.clone() for _, g in net.params])
+    assert all(torch.equal(a, b) for a, b in zip(*grads))
+
+
 def test_bytes_kept(net):
     held, full = net.kept_bytes()
     assert full == 2 * 4 * N * (9216 + 4096 + 4096) and held * 32 == full // 4 * 33

@@ -5,8 +5,9 @@ A layer takes h = layer_norm(a), a the activation below it.  Of a and h the step
 in place of 8): a for the norm's backward pass and for the ReLU below, h for the filter gradient; one buffer in fp32 serves all
 layers in turn, and one the outputs of the first two.  In all that is less of a saving than the blocks' own: a sample takes 35.9 KB
 of blocks and 53.2 KB of these two buffers, in fp32 h and the outputs would take 102.4; and fc6's input, the last pooling's
-output, stays in fp32 besides its blocks (36.9 KB either way).  An activation below 2^-10 times its block's power of two is kept as zero, and the ReLU then passes no gradient
-to it.  As in `stack`, this module owns buffers and the order of calls; all arithmetic happens in the library.
+output, stays in fp32 besides its blocks (36.9 KB either way).  An activation below 2^-10 times its block's power of two is kept
+as zero, and the ReLU then passes no gradient to it.  As in `stack`, this module owns buffers and the order of calls; all
+arithmetic happens in the library.
 """
 import torch
 

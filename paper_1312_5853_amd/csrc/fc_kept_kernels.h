@@ -13,7 +13,9 @@
 // Tiles of 64 TM outputs x 64 TN inputs, a quarter to each of four wavefronts, KS rows of n to a step.  Two buffers: while a step is
 // multiplied, the next one's values, which have come into registers meanwhile, are converted and stored piece by piece, and each
 // piece of the step after it is sent for as its registers become free.
-// Bound by the matrix units: 8192 rows 4096 -> 4096 bfloat16 220 us, 1250 TFLOP/s (a library product of bfloat16 tensors 1176).
+// Bound by the matrix units and the clock that their power leaves them: 8192 rows 4096 -> 4096 bfloat16 229 us from idle, up to 313
+// between 2 and 8 ms of such calls, 217 to 231 from 15 ms on, 1190 to 1270 TFLOP/s (a library product of bfloat16 tensors 8192^3
+// 1176 to 1200 in the same state).
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));

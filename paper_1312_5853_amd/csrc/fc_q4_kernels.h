@@ -74,8 +74,8 @@ __device__ __forceinline__ void store_block_q4(const Args &a, const float *bias,
 // 64 bytes apart, and the 16 lanes of a phase of ds_read_b128 then cover all banks.  The exponents of a step lie together (see
 // q4_prepare), four bytes to a row; a lane shifts its block's to the low byte.
 //
-// Bound by the matrix units at the clock that their power leaves: 8192 x 8192 -> 8192 259 to 285 us, 3.9 to 4.2 PFLOP/s (the
-// instruction alone 5.1 to 5.8 on such operands); the main loop is at 92 % of that, the rest its start and its stores.
+// Bound by the matrix units at the clock that their power leaves: 8192 x 8192 -> 8192 261 us from idle, up to 334 between 2 and 6 ms
+// of such calls, 250 to 260 in the long run: 3.3 to 4.4 PFLOP/s (the instruction alone, on random codes, 6.6).
 //
 // LDS: kQ4Stages buffers; step s is multiplied while those of s + 1 .. s + kQ4Stages - 1 are on their way.
 struct Q4TileArgs {
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(256) void q4_prepare(const Q4PrepArgs p)
 }
 
 // ---------------------------------------------------------------------------
-// Few samples: AO 16 outputs x J 16 samples to a work-group, whose eight wavefronts share the sum
+// Few samples: AO 16 outputs x J 16 samples to a work-group, whose wavefronts (eight; four for more than 32 samples) share the sum
 // ---------------------------------------------------------------------------
 // Bound by reading w once.  v_mfma_scale_f32_16x16x128_f8f6f4: lane l has row l % 16 and the 32 values of block l / 16.  The
 // wavefronts of a work-group take parts of the sum, each with a ring of STAGES buffers of its own in LDS, so that none waits for

@@ -210,7 +210,9 @@ __device__ __forceinline__ void load_affine(const float *p, int at, int left, fl
 }
 
 // Up to 16 values to a thread gamma and beta stay in registers; with 32 they are read again for every row, from the cache.  Bound by
-// memory: 16384 x 4096 bfloat16 51 us, 5.2 TB/s, as a copy; one row 4 us, most of it the launch.
+// memory: 16384 x 4096 bfloat16 51 us, 5.2 TB/s, as a copy; one row 4 us, most of it the launch.  With 32 values fp32 spills 40 registers
+// (bfloat16 2), and the rows take 1.6 to 2 times a copy of their bytes: 2000 x 16384 fp32 62 us, 4.2 TB/s, 2000 x 20000 120, 2.7,
+// 2000 x 32768 157, 3.3; bfloat16 33, 59 and 78.
 template <typename T, int R>
 __global__ __launch_bounds__(1024) void layer_norm_fwd_rows(const LayerNormArgs a)
 {
@@ -410,7 +412,8 @@ __device__ __forceinline__ void column_sums(const LayerNormArgs &a, int tile, in
 
 // dx, and every work-group's sums of the columns over its rows (SUMS); or, over few rows, dgamma and dbeta by work-groups of their
 // own, which read the rows once more, from the cache, and save the launch that joins.  gamma lies in LDS.  With 8 values to a
-// thread the next row's are on their way (8192 x 4096 bfloat16 43 us, 56 with 16 values, which leave room for half the wavefronts).
+// thread the next row's are on their way (a call of 8192 x 4096 bfloat16, its columns joined, 44 to 46 us; when it was chosen 43, and
+// 56 with 16 values, which leave room for half the wavefronts).
 // U rows at a time, with one barrier to all, where a work-group has no more rows side by side.
 // Bound by memory between a start and an end of 10 us together, and for few rows by those: 6001 x 5003 bfloat16 from 8 bits 45 us,
 // 3.4 TB/s, from 3000 rows on another thousand takes what a copy of its bytes does; 128 x 9216 fp32 8.7 us.

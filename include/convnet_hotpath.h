@@ -470,7 +470,8 @@ int dequantize_blocks(const void *codes, const void *scales, void *x, int64_t x_
  * those of the forward pass.
  * `dtype` names the element type of x, y, dy and dx as for the glue layers; arithmetic is fp32 (a row's sums over more than 32
  * values to a thread in 64 bits, a column's over at most 256 rows to a thread in fp32, the parts' in 64 bits), a bfloat16 result is
- * rounded once.  Rows lie x_stride, y_stride, ... elements apart (>= C) and may start anywhere.  eps > 0.  C <= 2^27,
+ * rounded once.  A row whose sum, or sum of squares of distances from its mean, is past fp32 has no statistics (mean infinite, or rstd 0).
+ * Rows lie x_stride, y_stride, ... elements apart (>= C) and may start anywhere.  eps > 0.  C <= 2^27,
  * N * C < 2^40.  N = 0 is allowed (tensors over it may be NULL; dgamma and dbeta become 0).  Outputs must not overlap inputs.
  * Scratch of the backward calls: layer_norm_workspace_bytes(CONV_OP_BWD_DATA, ...) bytes, 256-byte aligned (0 for invalid
  * arguments; none is needed without dgamma and dbeta).
